@@ -267,6 +267,134 @@ size_t gc_noalloc_scratch_bytes(void);
  * (a 4-byte device word the caller has zeroed).  Asynchronous on cuda_stream. */
 gc_status_t gc_selftest_bounded_wait(void* cuda_stream, void* status_dev, uint32_t limit_us);
 
+/* ------------------------------------------------------------------------------------------------
+ * Operators of a served attention block.  No counterpart in the paper, whose attention subgraph has one
+ * dense, static shape; these calls take the shapes a running server has: tokens of many sequences packed
+ * one behind the other, query heads that share key/value heads, a cache that grows.
+ *
+ *   gc_qk_norm_rope        RMS norm of every query and key head and the rotation by position, one pass
+ *   gc_kv4_append / _read  keys and values into a paged 4-bit cache, and back as the values it holds
+ *   gc_attention_kv4       a few new queries per sequence against that cache
+ *   gc_attention_prompt    whole prompts: packed sequences, causal or not, grouped heads
+ *
+ * Conventions beyond those above: each call enqueues its kernels on cuda_stream, on the device named in its
+ * descriptor (the calling thread's current device is restored), allocates nothing, keeps nothing between
+ * calls and may be captured.  What the host can see is refused before anything is launched.  What only the
+ * device sees (a slot, a page number, a length, a sequence offset outside its bounds) is checked there: the
+ * access is left out or clamped, the outputs of that call are undefined, and the first such finding is written
+ * to the status word the caller passed (device u32, zeroed by the caller; may be NULL), see gc_serving_status.
+ * Outputs must not overlap inputs, except that gc_qk_norm_rope may work in place (q_out = q, k_out = k with the
+ * same strides). */
+
+/* Rows of heads: element (token t, head h, i) at data + t * token_stride + h * head_stride + i, strides in elements. */
+typedef struct {
+  void* data;
+  int64_t token_stride;
+  int64_t head_stride;
+} gc_heads_t;
+
+/* y = x * rsqrt(mean(x^2) + eps) * weight over the head dimension (norm = 1; a NULL weight is all ones), or y = x
+ * (norm = 0); then, for i < rot_dim / 2, with phi = position * inv_freq[i], c = factor cos(phi), s = factor sin(phi):
+ *   (a, b) -> (a c - b s, b c + a s),  a = y[i], b = y[i + rot_dim / 2]     interleaved = 0
+ *                                      a = y[2 i], b = y[2 i + 1]           interleaved = 1
+ * Elements from rot_dim on are not rotated.  Computed in fp32 from exactly promoted inputs, phi in fp64, one rounding
+ * at the end.  dtype GC_F32 or GC_BF16 (also of the weights); head_dim even, 2 .. 256; rot_dim even, 0 .. head_dim. */
+typedef struct {
+  int32_t cuda_device;
+  int32_t dtype;
+  int64_t tokens;
+  int32_t q_heads, k_heads;      /* either may be 0 */
+  int32_t head_dim, rot_dim;
+  int32_t interleaved, norm;
+  float eps, attention_factor;
+  gc_heads_t q, k, q_out, k_out;
+  const void* q_weight;          /* [head_dim] or NULL */
+  const void* k_weight;
+  const int64_t* positions;      /* [tokens] */
+  const float* inv_freq;         /* [rot_dim / 2] */
+} gc_qk_norm_rope_t;
+gc_status_t gc_qk_norm_rope(void* cuda_stream, const gc_qk_norm_rope_t* d);
+
+/* A paged cache of keys and values in 4 bits.  All four arrays are dense:
+ *   codes   u8   [num_pages, kv_heads, page_size, head_dim / 2]          element 2 j of a row in the low half of byte j
+ *   params  bf16 [num_pages, kv_heads, page_size, head_dim / group, 2]   (lo, scale) of each group of a row
+ * Value held = lo + code * scale.  On writing: lo = the largest bf16 <= min of the group, scale = the smallest bf16 >=
+ * (max - lo) / 15, code = the integer nearest to (x - lo) / scale, ties to even (0 where scale is 0) - decided on the
+ * exact quotients, so results are reproducible bit for bit.  (Quantize elsewhere in this library multiplies by a
+ * rounded reciprocal; here that would move exact quotients off the borders between codes.)  A group with a non-finite
+ * element, or whose max - lo leaves fp32, is held as NaN.
+ * A token lives at slot = page * page_size + offset.  page_size a power of two, 16 .. 256; head_dim 64, 96 or 128;
+ * group 32, 64 or 128, a divisor of head_dim.  Pointers 16-byte aligned. */
+typedef struct {
+  int32_t cuda_device;
+  int32_t page_size;
+  int64_t num_pages;
+  int32_t kv_heads, head_dim, group, reserved_;
+  void* k_codes;
+  void* k_params;
+  void* v_codes;
+  void* v_params;
+  uint32_t* status;              /* device status word or NULL */
+} gc_kv4_cache_t;
+
+/* Write k / v rows [tokens, kv_heads, head_dim] (GC_F32 or GC_BF16) into the cache at slots[t]; a negative slot is
+ * skipped.  A slot named twice in one call holds a mixture of its rows. */
+gc_status_t gc_kv4_append(void* cuda_stream, const gc_kv4_cache_t* cache, int32_t dtype, int64_t tokens,
+                          const gc_heads_t* k, const gc_heads_t* v, const int64_t* slots);
+/* Read the values held at slots[t] into k / v rows; rows of negative slots are left as they were. */
+gc_status_t gc_kv4_read(void* cuda_stream, const gc_kv4_cache_t* cache, int32_t dtype, int64_t tokens,
+                        const gc_heads_t* k, const gc_heads_t* v, const int64_t* slots);
+
+/* out[b, j, h] = softmax_t(scale * q[b, j, h] . K[t]) V over the cached tokens t < lengths[b] - (queries - 1) + j of
+ * sequence b (the new tokens' rows have been appended; length counts them); zero where there is none.  K / V are the
+ * values held of head h / (q_heads / kv_heads).  q, out bf16: element (b, j, h, i) at b * batch_stride + j *
+ * query_stride + h * head_stride + i, 16-byte aligned rows.  block_table: page of tokens [p * page_size, ...) of
+ * sequence b at [b * table_stride + p], p < table_width; entries beyond a sequence's length are not looked at.
+ * max_length: an upper bound of lengths the caller knows (a longer sequence is an error found on the device); the
+ * split of the work over the GPU goes by it.  Scores and sums in fp32, probabilities times scale rounded to bf16 (half a
+ * bf16 step each, the only rounding before the output's).  queries 1 .. 16, scale finite and > 0. */
+typedef struct {
+  int32_t batch, queries, q_heads;
+  int32_t table_width;
+  int64_t table_stride;
+  int32_t max_length;
+  float scale;
+  const void* q;
+  int64_t q_batch_stride, q_query_stride, q_head_stride;
+  void* out;
+  int64_t o_batch_stride, o_query_stride, o_head_stride;
+  const int32_t* block_table;
+  const int32_t* lengths;        /* [batch] */
+} gc_attention_kv4_t;
+/* Bytes of 16-byte aligned device scratch the call needs (0: none; contents need no initialisation; it must not be shared
+ * by calls that can overlap). */
+gc_status_t gc_attention_kv4_workspace_bytes(const gc_kv4_cache_t* cache, const gc_attention_kv4_t* d, size_t* bytes);
+gc_status_t gc_attention_kv4(void* cuda_stream, const gc_kv4_cache_t* cache, const gc_attention_kv4_t* d,
+                             void* workspace_dev, size_t workspace_bytes);
+
+/* out = softmax(scale * Q K^T) V for `batch` sequences packed one behind the other: sequence b owns query rows
+ * [cu_q[b], cu_q[b + 1]) and key rows [cu_k[b], cu_k[b + 1]).  causal = 1: query row i of nq sees keys j <= i + nk - nq
+ * (aligned to the end, so a prompt may continue earlier keys).  A row that sees nothing is zero; rows of out that no
+ * sequence owns are left as they were.  bf16, head_dim 64, 96 or 128, fp32 statistics and sums, probabilities rounded to
+ * bf16 for the second product.  Rows 16-byte aligned (pointers, and strides multiples of 8 elements). */
+typedef struct {
+  int32_t cuda_device;
+  int32_t batch;
+  int64_t q_tokens, k_tokens;    /* rows of q / out and of k / v in all */
+  int32_t q_heads, kv_heads, head_dim, causal;
+  float scale;
+  int32_t reserved_;
+  gc_heads_t q, k, v, out;
+  const int32_t* cu_q;           /* [batch + 1], non-decreasing, within 0 .. q_tokens */
+  const int32_t* cu_k;
+  uint32_t* status;
+} gc_attention_prompt_t;
+gc_status_t gc_attention_prompt(void* cuda_stream, const gc_attention_prompt_t* d);
+
+/* Synchronise the stream, read a status word and clear it: GC_OK, GC_ERR_TIMEOUT (a bounded device-side wait expired),
+ * GC_ERR_INVALID_ARG (a slot, page, length or offset was out of bounds) or GC_ERR_CUDA. */
+gc_status_t gc_serving_status(void* cuda_stream, uint32_t* status_dev);
+
 const char* gc_last_error(void);
 const char* gc_version(void);
 

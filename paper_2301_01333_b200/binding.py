@@ -35,6 +35,8 @@ EXPORTS = [
     "gc_execute_host_async", "gc_host_wait",
     "gc_query_status", "gc_launches_per_execute", "gc_plan_description", "gc_last_error", "gc_version",
     "gc_matmul_s32_noalloc", "gc_noalloc_scratch_bytes", "gc_selftest_bounded_wait", "gc_invalidate_constants",
+    "gc_qk_norm_rope", "gc_kv4_append", "gc_kv4_read", "gc_attention_kv4_workspace_bytes", "gc_attention_kv4",
+    "gc_attention_prompt", "gc_serving_status",
 ]
 
 
@@ -52,6 +54,39 @@ class gc_op_t(C.Structure):
 class gc_compile_options_t(C.Structure):
     _fields_ = [("force_generic", C.c_int32), ("no_chain_fusion", C.c_int32), ("streaming_attention", C.c_int32),
                 ("exact_max_softmax", C.c_int32), ("grid_wide_chain", C.c_int32), ("reserved", C.c_int32 * 3)]
+
+
+class gc_heads_t(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class gc_qk_norm_rope_t(C.Structure):
+    _fields_ = [("cuda_device", C.c_int32), ("dtype", C.c_int32), ("tokens", C.c_int64), ("q_heads", C.c_int32),
+                ("k_heads", C.c_int32), ("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32),
+                ("norm", C.c_int32), ("eps", C.c_float), ("attention_factor", C.c_float), ("q", gc_heads_t), ("k", gc_heads_t),
+                ("q_out", gc_heads_t), ("k_out", gc_heads_t), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p),
+                ("positions", C.c_void_p), ("inv_freq", C.c_void_p)]
+
+
+class gc_kv4_cache_t(C.Structure):
+    _fields_ = [("cuda_device", C.c_int32), ("page_size", C.c_int32), ("num_pages", C.c_int64), ("kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("group", C.c_int32), ("reserved_", C.c_int32), ("k_codes", C.c_void_p),
+                ("k_params", C.c_void_p), ("v_codes", C.c_void_p), ("v_params", C.c_void_p), ("status", C.c_void_p)]
+
+
+class gc_attention_kv4_t(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("queries", C.c_int32), ("q_heads", C.c_int32), ("table_width", C.c_int32),
+                ("table_stride", C.c_int64), ("max_length", C.c_int32), ("scale", C.c_float), ("q", C.c_void_p),
+                ("q_batch_stride", C.c_int64), ("q_query_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("out", C.c_void_p), ("o_batch_stride", C.c_int64), ("o_query_stride", C.c_int64),
+                ("o_head_stride", C.c_int64), ("block_table", C.c_void_p), ("lengths", C.c_void_p)]
+
+
+class gc_attention_prompt_t(C.Structure):
+    _fields_ = [("cuda_device", C.c_int32), ("batch", C.c_int32), ("q_tokens", C.c_int64), ("k_tokens", C.c_int64),
+                ("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("causal", C.c_int32),
+                ("scale", C.c_float), ("reserved_", C.c_int32), ("q", gc_heads_t), ("k", gc_heads_t), ("v", gc_heads_t),
+                ("out", gc_heads_t), ("cu_q", C.c_void_p), ("cu_k", C.c_void_p), ("status", C.c_void_p)]
 
 
 class GcError(RuntimeError):
@@ -101,6 +136,17 @@ def load_library() -> C.CDLL:
     lib.gc_invalidate_constants.restype = i32
     lib.gc_selftest_bounded_wait.argtypes = [vp, vp, C.c_uint32]
     lib.gc_selftest_bounded_wait.restype = i32
+    heads = C.POINTER(gc_heads_t)
+    lib.gc_qk_norm_rope.argtypes = [vp, C.POINTER(gc_qk_norm_rope_t)]
+    lib.gc_kv4_append.argtypes = [vp, C.POINTER(gc_kv4_cache_t), i32, C.c_int64, heads, heads, vp]
+    lib.gc_kv4_read.argtypes = [vp, C.POINTER(gc_kv4_cache_t), i32, C.c_int64, heads, heads, vp]
+    lib.gc_attention_kv4_workspace_bytes.argtypes = [C.POINTER(gc_kv4_cache_t), C.POINTER(gc_attention_kv4_t), C.POINTER(sz)]
+    lib.gc_attention_kv4.argtypes = [vp, C.POINTER(gc_kv4_cache_t), C.POINTER(gc_attention_kv4_t), vp, sz]
+    lib.gc_attention_prompt.argtypes = [vp, C.POINTER(gc_attention_prompt_t)]
+    lib.gc_serving_status.argtypes = [vp, vp]
+    for name in ("gc_qk_norm_rope", "gc_kv4_append", "gc_kv4_read", "gc_attention_kv4_workspace_bytes", "gc_attention_kv4",
+                 "gc_attention_prompt", "gc_serving_status"):
+        getattr(lib, name).restype = i32
     for name in ("gc_partition_create", "gc_compile", "gc_workspace_bytes", "gc_set_workspace", "gc_execute",
                  "gc_host_staging_bytes", "gc_set_host_staging", "gc_execute_host", "gc_execute_host_async",
                  "gc_host_wait", "gc_query_status", "gc_launches_per_execute"):
@@ -264,6 +310,47 @@ def gc_matmul_s32_noalloc(stream: int, a_ptr: int, w_ptr: int, out_ptr: int, m: 
 def gc_selftest_bounded_wait(stream: int, status_ptr: int, limit_us: int) -> None:
     """Launch the kernel whose wait cannot be satisfied; after limit_us it writes a timeout code to *status_ptr."""
     _check(load_library().gc_selftest_bounded_wait(C.c_void_p(stream), C.c_void_p(status_ptr), limit_us))
+
+
+def gc_qk_norm_rope(stream: int, desc: gc_qk_norm_rope_t) -> None:
+    st = load_library().gc_qk_norm_rope(stream, desc)
+    if st:
+        raise GcError(st, gc_last_error())
+
+
+def gc_kv4_append(stream: int, cache: gc_kv4_cache_t, dtype: int, tokens: int, k: gc_heads_t, v: gc_heads_t, slots: int) -> None:
+    st = load_library().gc_kv4_append(stream, cache, dtype, tokens, k, v, slots)
+    if st:
+        raise GcError(st, gc_last_error())
+
+
+def gc_kv4_read(stream: int, cache: gc_kv4_cache_t, dtype: int, tokens: int, k: gc_heads_t, v: gc_heads_t, slots: int) -> None:
+    st = load_library().gc_kv4_read(stream, cache, dtype, tokens, k, v, slots)
+    if st:
+        raise GcError(st, gc_last_error())
+
+
+def gc_attention_kv4_workspace_bytes(cache: gc_kv4_cache_t, desc: gc_attention_kv4_t) -> int:
+    n = C.c_size_t()
+    _check(load_library().gc_attention_kv4_workspace_bytes(cache, desc, n))
+    return n.value
+
+
+def gc_attention_kv4(stream: int, cache: gc_kv4_cache_t, desc: gc_attention_kv4_t, workspace_ptr: int, workspace_bytes: int) -> None:
+    st = load_library().gc_attention_kv4(stream, cache, desc, workspace_ptr, workspace_bytes)
+    if st:
+        raise GcError(st, gc_last_error())
+
+
+def gc_attention_prompt(stream: int, desc: gc_attention_prompt_t) -> None:
+    st = load_library().gc_attention_prompt(stream, desc)
+    if st:
+        raise GcError(st, gc_last_error())
+
+
+def gc_serving_status(stream: int, status_ptr: int) -> None:
+    """Synchronise the stream, read and clear the status word; raises GcError for what the device found."""
+    _check(load_library().gc_serving_status(stream, status_ptr))
 
 
 class CompiledPartition:

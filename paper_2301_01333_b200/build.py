@@ -14,8 +14,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgc_b200.so")
 SOURCES = ["gc_api.cu", "gc_noalloc.cu", "kernels_generic.cu", "kernels_gemm_tc.cu", "kernels_gemm_tc2.cu", "kernels_chain.cu", "kernels_chain_cluster.cu",
-           "kernels_sdpa_tc.cu", "kernels_sdpa_wide.cu", "kernels_sdpa_long.cu", "kernels_sdpa_small.cu"]
-HEADERS = ["gc_internal.h", "ptx.cuh", "epilogue.cuh", "gemm_epilogue.cuh", os.path.join("..", "..", "include", "gc.h")]
+           "kernels_sdpa_tc.cu", "kernels_sdpa_wide.cu", "kernels_sdpa_long.cu", "kernels_sdpa_small.cu",
+           "gc_serving.cu", "kernels_qk_norm_rope.cu", "kernels_kv4.cu", "kernels_attn_kv4.cu", "kernels_attn_prompt.cu"]
+HEADERS = ["gc_internal.h", "ptx.cuh", "epilogue.cuh", "gemm_epilogue.cuh", "serving.cuh", os.path.join("..", "..", "include", "gc.h")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",

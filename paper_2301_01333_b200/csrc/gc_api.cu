@@ -349,6 +349,23 @@ static gc_status_t make_tmap3(CUtensorMap* m, const void* ptr, int dtype, uint64
   return GC_OK;
 }
 
+// 3-D view (head dimension, heads, tokens) of bf16 rows with any strides, for gc_serving.cu: a box is `box_tokens` rows of
+// one head, `box_inner` elements wide, under the 128-byte swizzle.  Rows and columns past the end read as zeros.
+gc_status_t gc_make_tmap_heads(CUtensorMap* m, const void* ptr, uint64_t inner, uint64_t heads, uint64_t tokens,
+                               uint64_t head_stride_bytes, uint64_t token_stride_bytes, uint32_t box_inner, uint32_t box_tokens) {
+  EncodeTiledFn enc = get_encode();
+  if (!enc) return fail(GC_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+  cuuint64_t gdim[3] = {inner, heads, tokens};
+  cuuint64_t gstr[2] = {head_stride_bytes, token_stride_bytes};
+  cuuint32_t box[3] = {box_inner, 1, box_tokens};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), gdim, gstr, box, estr,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(GC_ERR_CUDA, "cuTensorMapEncodeTiled (heads) failed with code %d", (int)r);
+  return GC_OK;
+}
+
 // ------------------------------------------------------------------------------------------------
 // pattern formation
 // ------------------------------------------------------------------------------------------------

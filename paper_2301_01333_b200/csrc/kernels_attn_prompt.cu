@@ -1,0 +1,544 @@
+// Attention of whole prompts: sequences of any length packed one behind the other, causal or not, query heads in groups
+// that share a key/value head, head width 64, 96 or 128, bf16.
+//
+//   O = softmax(scale Q K^T) V, blockwise over 128 keys: with m a running reference, p = 2^(c s - c m), c = scale log2(e),
+//   l = sum p and O = sum p V carried along; when m is raised both are multiplied by 2^(c (m_old - m_new)).
+//
+// Bound by the tensor cores and, as closely, by the exponentials: per 128 x 128 tile of scores with D = 128 two products of
+// 512 clocks each against 16384 exponentials, 16 a clock: 1024 clocks.  The two have to run side by side, so a CTA owns two
+// tiles of 128 query rows (256 neighbouring rows of one head) and alternates: while the softmax warps of one tile turn its
+// scores into probabilities, the tensor core works for the other.
+//   warps 0-3, 4-7   softmax of tile 0 / 1, one query row per thread: 128 scores from tensor memory into registers at once,
+//                    maximum, exponentials, row sum; the bf16 probabilities go back over the scores they came from, as the
+//                    A operand of the second product in tensor memory; at the end of a tile they scale and store its O
+//   warp 8           TMA producer: Q tiles, and K and V blocks through one ring
+//   warp 9           MMA issuer: S = Q K^T (both operands in shared memory), O += P V (P in tensor memory, V as stored,
+//                    keys along the rows).  The tensor core works off one thread's products in order, which is what lets S of
+//                    the next block overwrite P of this one, and makes "S complete" imply "O complete".
+// Tensor memory: two score tiles of 128 columns and two outputs of D <= 128: all 512 columns.
+//   * The reference m is raised only when a score exceeds it by 2^8 (as in the cache attention): after the first block the
+//     output is almost never touched, and raising it is the softmax warps' own business - no extra role, no extra hand-over.
+//   * Persistent CTAs; the work list (256 query rows of a sequence, times heads) is made by each CTA from the sequence offsets
+//     and sorted by its number of key blocks, longest first, dealt out back and forth.  The first scores of the next item are
+//     issued before the last output of the current one has been stored.
+//   * Rows of another sequence may follow a sequence's own in a tile.  Foreign keys are masked by selection; foreign value
+//     rows are overwritten with zeros in shared memory (0 times a stored infinity would be NaN); foreign query rows are not
+//     stored.
+#include "ptx.cuh"
+#include "serving.cuh"
+
+namespace gc {
+
+namespace {
+constexpr int AP_THREADS = 384;               // three warpgroups; the last two warps only hand their registers over
+constexpr int AP_MAX_LIST = 1024;                // work list entries kept (and sorted) in shared memory
+constexpr float AP_RAISE = 8.0f;
+
+template <int D>
+struct PromptLayout {
+  static constexpr int NSUB = (D + 63) / 64;     // 64-element sub-tiles of 128-byte rows
+  static constexpr int SUB = 128 * 128;
+  static constexpr int TILE = NSUB * SUB;        // 128 rows of Q, K or V
+  static constexpr int STAGES = D == 64 ? 8 : 4;
+  static constexpr int BARS = 2 * STAGES + 10;
+  static constexpr int LIST = AP_MAX_LIST * 8;
+  static constexpr size_t SMEM = 1024 + static_cast<size_t>(2 + STAGES) * TILE + LIST + BARS * 8 + 64;
+};
+
+__device__ __forceinline__ float ap_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t ap_pack(float lo, float hi) {
+  const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&b);
+}
+// D[tmem] (+)= A[tmem] * B[smem]: A holds 16-bit elements, two per column
+__device__ __forceinline__ void umma_ts_bf16(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred P;\n\tsetp.ne.b32 P, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, P;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// All 128 score columns of a warp's 32 rows, loads and their wait in one statement: the registers are written
+// asynchronously, and nothing may move or spill them in between.
+__device__ __forceinline__ void tmem_ld128(uint32_t taddr, uint32_t (&r)[128]) {
+  asm volatile(
+      "{\n\t.reg .b32 t;\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, "
+      "%40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, "
+      "%63}, [%128];\n\t"
+      "add.u32 t, %128, 64;\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%64, %65, %66, %67, %68, %69, %70, %71, %72, %73, %74, %75, %76, %77, %78, "
+      "%79, %80, %81, %82, %83, %84, %85, %86, %87, %88, %89, %90, %91, %92, %93, %94, %95, %96, %97, %98, %99, %100, "
+      "%101, %102, %103, %104, %105, %106, %107, %108, %109, %110, %111, %112, %113, %114, %115, %116, %117, %118, %119, "
+      "%120, %121, %122, %123, %124, %125, %126, %127}, [t];\n\t"
+      "tcgen05.wait::ld.sync.aligned;\n\t}"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+        "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]),
+        "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]),
+        "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]),
+        "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]),
+        "=r"(r[63]), "=r"(r[64]), "=r"(r[65]), "=r"(r[66]), "=r"(r[67]), "=r"(r[68]), "=r"(r[69]), "=r"(r[70]), "=r"(r[71]),
+        "=r"(r[72]), "=r"(r[73]), "=r"(r[74]), "=r"(r[75]), "=r"(r[76]), "=r"(r[77]), "=r"(r[78]), "=r"(r[79]), "=r"(r[80]),
+        "=r"(r[81]), "=r"(r[82]), "=r"(r[83]), "=r"(r[84]), "=r"(r[85]), "=r"(r[86]), "=r"(r[87]), "=r"(r[88]), "=r"(r[89]),
+        "=r"(r[90]), "=r"(r[91]), "=r"(r[92]), "=r"(r[93]), "=r"(r[94]), "=r"(r[95]), "=r"(r[96]), "=r"(r[97]), "=r"(r[98]),
+        "=r"(r[99]), "=r"(r[100]), "=r"(r[101]), "=r"(r[102]), "=r"(r[103]), "=r"(r[104]), "=r"(r[105]), "=r"(r[106]),
+        "=r"(r[107]), "=r"(r[108]), "=r"(r[109]), "=r"(r[110]), "=r"(r[111]), "=r"(r[112]), "=r"(r[113]), "=r"(r[114]),
+        "=r"(r[115]), "=r"(r[116]), "=r"(r[117]), "=r"(r[118]), "=r"(r[119]), "=r"(r[120]), "=r"(r[121]), "=r"(r[122]),
+        "=r"(r[123]), "=r"(r[124]), "=r"(r[125]), "=r"(r[126]), "=r"(r[127])
+      : "r"(taddr)
+      : "memory");
+}
+
+// One sequence's rows, from its offsets; offsets that decrease or leave the tensors are cut to size.
+struct Seq {
+  int q0, nq, k0, nk;
+};
+__device__ __forceinline__ Seq seq_of(const PromptParams& p, int b) {
+  Seq s;
+  const int tq = static_cast<int>(p.q_tokens), tk = static_cast<int>(p.k_tokens);
+  s.q0 = min(max(p.cu_q[b], 0), tq);
+  s.nq = max(min(p.cu_q[b + 1], tq) - s.q0, 0);
+  s.k0 = min(max(p.cu_k[b], 0), tk);
+  s.nk = max(min(p.cu_k[b + 1], tk) - s.k0, 0);
+  return s;
+}
+// Keys row i of a sequence sees.
+__device__ __forceinline__ int row_limit(const PromptParams& p, const Seq& s, int i) {
+  return i >= s.nq ? 0 : p.causal ? max(i + 1 + s.nk - s.nq, 0) : s.nk;
+}
+// 128-key blocks the tile of rows [r0, r0 + 128) needs.
+__device__ __forceinline__ int tile_blocks(const PromptParams& p, const Seq& s, int r0) {
+  return r0 >= s.nq ? 0 : (row_limit(p, s, min(r0 + 127, s.nq - 1)) + 127) >> 7;
+}
+
+struct Item {
+  Seq s;
+  int row0, head;                // first of the 256 query rows, within the sequence
+  int n[2];                      // key blocks of the two tiles
+  bool valid;
+};
+}  // namespace
+
+template <int D>
+__global__ void __launch_bounds__(AP_THREADS, 1)
+attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                   const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PromptParams p, const int listed, const int most) {
+  using L = PromptLayout<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* sQ = smem;                                           // [2] tiles
+  uint8_t* sKV = sQ + 2 * L::TILE;                              // [STAGES] tiles
+  int* s_item = reinterpret_cast<int*>(sKV + L::STAGES * L::TILE);      // sequence of each entry, then its block
+  int* s_tmp = s_item + AP_MAX_LIST;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(s_tmp + AP_MAX_LIST);
+  const uint32_t b0 = smem_u32(bars);
+  const uint32_t bar_q_full = b0, bar_q_empty = b0 + 16, bar_s_full = b0 + 32, bar_p_full = b0 + 48, bar_o_full = b0 + 64;   // [2] each
+  const uint32_t bar_kv_full = b0 + 80, bar_kv_empty = bar_kv_full + 8 * L::STAGES;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + L::BARS);
+  int* s_total = reinterpret_cast<int*>(tmem_slot + 1);
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar_q_full + 8 * i, 1);
+      mbar_init(bar_q_empty + 8 * i, 1);
+      mbar_init(bar_s_full + 8 * i, 1);
+      mbar_init(bar_p_full + 8 * i, 4);
+      mbar_init(bar_o_full + 8 * i, 1);
+    }
+    for (int i = 0; i < L::STAGES; ++i) {
+      mbar_init(bar_kv_full + 8 * i, 1);
+      mbar_init(bar_kv_empty + 8 * i, 1);
+    }
+    fence_mbar_init();
+    tma_prefetch_desc(&tmQ);
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
+  }
+  if (warp == 9) {
+    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_relinquish();
+  }
+  // ---- the work list
+  if (warp == 0) {
+    int total = 0;
+    for (int s0 = 0; s0 < p.B; s0 += 32) {
+      const int b = s0 + lane;
+      int nb = 0;
+      if (b < p.B) {
+        const Seq s = seq_of(p, b);
+        nb = (s.nq + 255) >> 8;
+        if (blockIdx.x == 0 && (p.cu_q[b] != s.q0 || p.cu_q[b + 1] != s.q0 + s.nq || p.cu_k[b] != s.k0 || p.cu_k[b + 1] != s.k0 + s.nk))
+          report(p.status, DEV_BAD_OFFSETS);
+      }
+      int incl = nb;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
+      }
+      if (listed) {
+        // (overlapping sequences, an error reported above, could have more blocks than the list holds: cut off)
+        for (int i = 0; i < nb && total + incl - nb + i < AP_MAX_LIST; ++i) s_tmp[total + incl - nb + i] = b << 12 | i;
+      }
+      total = min(total + __shfl_sync(0xffffffffu, incl, 31), most);
+    }
+    if (lane == 0) *s_total = total;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const int entries = *s_total;
+  if (listed) {
+    auto cost = [&](int e) {
+      const Seq s = seq_of(p, e >> 12);
+      const int r0 = (e & 4095) * 256;
+      return tile_blocks(p, s, r0) + tile_blocks(p, s, r0 + 128);
+    };
+    // costs first (packed above the entry's number so that equal ones keep their order), then each entry's rank
+    int mine[(AP_MAX_LIST + AP_THREADS - 1) / AP_THREADS], key[(AP_MAX_LIST + AP_THREADS - 1) / AP_THREADS];
+#pragma unroll
+    for (int k = 0; k < (AP_MAX_LIST + AP_THREADS - 1) / AP_THREADS; ++k) {
+      const int e = tid + k * AP_THREADS;
+      mine[k] = key[k] = 0;
+      if (e < entries) {
+        mine[k] = s_tmp[e];
+        key[k] = cost(mine[k]);
+        s_item[e] = key[k];
+      }
+    }
+    __syncthreads();
+    int rank[(AP_MAX_LIST + AP_THREADS - 1) / AP_THREADS];
+#pragma unroll
+    for (int k = 0; k < (AP_MAX_LIST + AP_THREADS - 1) / AP_THREADS; ++k) {
+      const int e = tid + k * AP_THREADS;
+      rank[k] = 0;
+      if (e < entries)
+        for (int f = 0; f < entries; ++f) rank[k] += s_item[f] > key[k] || (s_item[f] == key[k] && f < e);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < (AP_MAX_LIST + AP_THREADS - 1) / AP_THREADS; ++k)
+      if (tid + k * AP_THREADS < entries) s_item[rank[k]] = mine[k];
+    __syncthreads();
+  }
+  // Item number r of this CTA; called by whole warps.
+  const int64_t items = static_cast<int64_t>(entries) * p.Hq;
+  auto item_of = [&](int r) {
+    Item it;
+    const int64_t g = static_cast<int64_t>(r) * gridDim.x + ((r & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+    it.valid = g < items;
+    it.n[0] = it.n[1] = 0;
+    it.row0 = it.head = 0;
+    it.s = Seq{0, 0, 0, 0};
+    if (!it.valid) return it;
+    const int e = static_cast<int>(g / p.Hq);
+    it.head = static_cast<int>(g - static_cast<int64_t>(e) * p.Hq);
+    int b = 0, blk = 0;
+    if (listed) {
+      b = s_item[e] >> 12;
+      blk = s_item[e] & 4095;
+    } else {
+      int before = 0;
+      for (int s0 = 0; s0 < p.B; s0 += 32) {
+        const int nb = s0 + lane < p.B ? (seq_of(p, s0 + lane).nq + 255) >> 8 : 0;
+        int incl = nb;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int o = __shfl_up_sync(0xffffffffu, incl, d);
+          if (lane >= d) incl += o;
+        }
+        const uint32_t hit = __ballot_sync(0xffffffffu, before + incl > e);
+        if (hit) {
+          const int w = __ffs(hit) - 1;
+          b = s0 + w;
+          const int first = before + __shfl_sync(0xffffffffu, incl - nb, w), count = __shfl_sync(0xffffffffu, nb, w);
+          blk = count - 1 - (e - first);                        // the longest rows of a sequence first
+          break;
+        }
+        before += __shfl_sync(0xffffffffu, incl, 31);
+      }
+    }
+    it.s = seq_of(p, b);
+    it.row0 = blk * 256;
+    it.n[0] = tile_blocks(p, it.s, it.row0);
+    it.n[1] = tile_blocks(p, it.s, it.row0 + 128);
+    return it;
+  };
+
+  // Registers: 168 a thread at launch, 504 in each lane's three warps of a scheduler; 2 x 208 + 80 = 496.
+  bool failed = false;
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    // ------------------------------------------------------------------ softmax and output
+    const int t = warp >> 2, row = tid & 127;
+    const uint32_t t_lane = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    const uint32_t s_addr = t_lane + t * 128, o_addr = t_lane + 256 + t * 128;
+    uint32_t ring = 0, sn = 0, on = 0;
+    const float c = p.c;
+    for (int r = 0; !failed; ++r) {
+      const Item it = item_of(r);
+      if (!it.valid) break;
+      const int my_row = it.row0 + t * 128 + row;
+      const int lim = row_limit(p, it.s, my_row), n = it.n[t];
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < n; ++j) {
+        if (!__all_sync(0xffffffffu, mbar_wait(bar_s_full + 8 * t, sn & 1))) { failed = true; break; }
+        ++sn;
+        tc_fence_after();
+        uint32_t v[128];
+        tmem_ld128(s_addr, v);
+        const int left = lim - j * 128;
+        if (__any_sync(0xffffffffu, left < 128)) {
+#pragma unroll
+          for (int i = 0; i < 128; ++i)
+            if (i >= left) v[i] = 0xff800000u;                   // minus infinity, whatever the score was
+        }
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int i = 0; i < 128; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(v[i]));
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        if (__any_sync(0xffffffffu, (top - m) * c > AP_RAISE)) {
+          const float mn = fmaxf(m, top);
+          const float f = mn == m ? 1.f : ap_ex2((m - mn) * c);  // 0 from the initial minus infinity
+          m = mn;
+          l *= f;
+          if (j > 0) {
+            // S of this block is complete, hence so is the product of the block before: O is at rest
+#pragma unroll 1
+            for (int k = 0; k < D / 32; ++k) {
+              uint32_t w[32];
+              tmem_ld32(o_addr + k * 32, w);
+              tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) * f);
+              tmem_st32(o_addr + k * 32, w);
+            }
+          }
+        }
+        const float off = m == -INFINITY ? 0.f : -m * c;
+        float ls[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t w[32];
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const float e0 = ap_ex2(fmaf(__uint_as_float(v[h * 64 + 2 * i]), c, off));
+            const float e1 = ap_ex2(fmaf(__uint_as_float(v[h * 64 + 2 * i + 1]), c, off));
+            ls[(2 * i) & 3] += e0;
+            ls[(2 * i + 1) & 3] += e1;
+            w[i] = ap_pack(e0, e1);
+          }
+          tmem_st32(s_addr + h * 32, w);
+        }
+        l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+        if (j * 128 + 128 > it.s.nk) {
+          // the sequence ends inside this block: whatever follows it in V becomes zero
+          const uint32_t pos = ring + 2 * j + 1, st = pos % L::STAGES;
+          if (!__all_sync(0xffffffffu, mbar_wait(bar_kv_full + 8 * st, (pos / L::STAGES) & 1))) { failed = true; break; }
+          if (j * 128 + row >= it.s.nk) {
+#pragma unroll
+            for (int k = 0; k < L::NSUB; ++k) {
+              uint4* z = reinterpret_cast<uint4*>(sKV + st * L::TILE + k * L::SUB + row * 128);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) z[i] = make_uint4(0, 0, 0, 0);
+            }
+          }
+          fence_proxy_async_smem();
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_p_full + 8 * t);
+      }
+      if (failed) break;
+      ring += 2 * max(it.n[0], it.n[1]);
+      const bool store = my_row < it.s.nq;
+      __nv_bfloat16* dst = p.o + static_cast<int64_t>(it.s.q0 + my_row) * p.o_tok + static_cast<int64_t>(it.head) * p.o_head;
+      if (n == 0) {
+        if (store) {
+#pragma unroll
+          for (int i = 0; i < D / 8; ++i) reinterpret_cast<uint4*>(dst)[i] = make_uint4(0, 0, 0, 0);
+        }
+        continue;
+      }
+      if (!__all_sync(0xffffffffu, mbar_wait(bar_o_full + 8 * t, on & 1))) { failed = true; break; }
+      ++on;
+      tc_fence_after();
+      const float rl = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll 1
+      for (int k = 0; k < D / 32; ++k) {
+        uint32_t w[32];
+        tmem_ld32(o_addr + k * 32, w);
+        tmem_wait_ld();
+        if (store) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = ap_pack(__uint_as_float(w[8 * i + 2 * e]) * rl, __uint_as_float(w[8 * i + 2 * e + 1]) * rl);
+            reinterpret_cast<uint4*>(dst)[k * 4 + i] = make_uint4(x[0], x[1], x[2], x[3]);
+          }
+        }
+      }
+      tc_fence_before();
+    }
+    if (failed && lane == 0) report(p.status, DEV_TIMEOUT_EPILOGUE);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (warp == 8) {
+      // ------------------------------------------------------------------ TMA producer
+      uint32_t ring = 0, qn[2] = {0, 0};
+      const int g = p.Hq / p.Hk;
+      for (int r = 0;; ++r) {
+        const Item it = item_of(r);
+        if (!it.valid) break;
+        if (lane == 0) {
+          const int kvh = it.head / g;
+          auto load_q = [&](int t) -> bool {
+            if (it.n[t] == 0) return true;
+            if (!mbar_wait(bar_q_empty + 8 * t, (qn[t] & 1) ^ 1)) return false;
+            ++qn[t];
+            mbar_arrive_expect_tx(bar_q_full + 8 * t, static_cast<uint32_t>(L::TILE));
+            for (int j = 0; j < L::NSUB; ++j)
+              tma_load_3d(smem_u32(sQ) + t * L::TILE + j * L::SUB, &tmQ, j * 64, it.head, it.s.q0 + it.row0 + t * 128, bar_q_full + 8 * t);
+            return true;
+          };
+          auto load_kv = [&](const CUtensorMap* tm, int blk) -> bool {
+            const uint32_t st = ring % L::STAGES, use = ring / L::STAGES;
+            ++ring;
+            if (!mbar_wait(bar_kv_empty + 8 * st, (use & 1) ^ 1)) return false;
+            mbar_arrive_expect_tx(bar_kv_full + 8 * st, static_cast<uint32_t>(L::TILE));
+            for (int j = 0; j < L::NSUB; ++j)
+              tma_load_3d(smem_u32(sKV) + st * L::TILE + j * L::SUB, tm, j * 64, kvh, it.s.k0 + blk * 128, bar_kv_full + 8 * st);
+            return true;
+          };
+          const int n = max(it.n[0], it.n[1]);
+          failed = !load_q(0);
+          for (int j = 0; j < n && !failed; ++j) {
+            failed = !load_kv(&tmK, j);
+            if (j == 0 && !failed) failed = !load_q(1);
+            if (!failed) failed = !load_kv(&tmV, j);
+          }
+          if (failed) report(p.status, DEV_TIMEOUT_PRODUCER);
+        }
+        if (__any_sync(0xffffffffu, failed)) break;
+      }
+    } else if (warp == 9) {
+      // ------------------------------------------------------------------ MMA issuer
+      const uint32_t idesc_s = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, 128, 128);
+      const uint32_t idesc_o = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, 128, D, 0, 1);
+      uint32_t ring = 0, qn[2] = {0, 0}, pn[2] = {0, 0};
+      // S of tile t = Q_t K^T with the K block of ring position `pos`
+      auto scores = [&](int t, uint32_t pos) {
+        const uint32_t kb = smem_u32(sKV) + (pos % L::STAGES) * L::TILE, qb = smem_u32(sQ) + t * L::TILE;
+  #pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t off = (k >> 2) * L::SUB + (k & 3) * 32;
+          umma_ss<KIND_BF16>(tmem_base + t * 128, make_smem_desc(qb + off, 16, 1024, SWZ_128B), make_smem_desc(kb + off, 16, 1024, SWZ_128B),
+                             idesc_s, k != 0);
+        }
+        umma_commit(bar_s_full + 8 * t);
+      };
+      auto kv_ready = [&](uint32_t pos) { return mbar_wait(bar_kv_full + 8 * (pos % L::STAGES), (pos / L::STAGES) & 1); };
+      // the first scores of an item's tile t
+      auto first_scores = [&](const Item& it, int t) -> bool {
+        if (it.n[t] == 0) return true;
+        if (!mbar_wait(bar_q_full + 8 * t, qn[t] & 1) || !kv_ready(ring)) return false;
+        ++qn[t];
+        tc_fence_after();
+        scores(t, ring);
+        if (it.n[t] == 1) umma_commit(bar_q_empty + 8 * t);
+        return true;
+      };
+      Item it = item_of(0);
+      if (it.valid && lane == 0) {
+        failed = !first_scores(it, 0) || !first_scores(it, 1);
+        if (!failed && max(it.n[0], it.n[1])) umma_commit(bar_kv_empty + 8 * (ring % L::STAGES));
+      }
+      for (int r = 0; it.valid; ++r) {
+        if (__any_sync(0xffffffffu, failed)) break;
+        const Item next = item_of(r + 1);
+        const int n = max(it.n[0], it.n[1]);
+        if (lane == 0) {
+          // ring position of K_j: ring + 2 j, of V_j: ring + 2 j + 1
+          for (int j = 0; j < n && !failed; ++j) {
+            const uint32_t kpos = ring + 2 * j + 2, vpos = ring + 2 * j + 1;
+            const bool last = j + 1 == n;
+            if (last) ring += 2 * n;                               // the next item's first K block is kpos as well
+  #pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              if (failed) break;
+              if (j < it.n[t]) {
+                if (!mbar_wait(bar_p_full + 8 * t, pn[t] & 1) || !kv_ready(vpos)) { failed = true; break; }
+                ++pn[t];
+                tc_fence_after();
+                const uint32_t vb = smem_u32(sKV) + (vpos % L::STAGES) * L::TILE;
+  #pragma unroll
+                for (int k = 0; k < 8; ++k)                        // 16 keys per MMA
+                  umma_ts_bf16(tmem_base + 256 + t * 128, tmem_base + t * 128 + k * 8,
+                               make_smem_desc(vb + k * 16 * 128, L::SUB, 1024, SWZ_128B), idesc_o, !(j == 0 && k == 0));
+                if (j + 1 == it.n[t]) umma_commit(bar_o_full + 8 * t);
+              }
+              if (j + 1 < it.n[t]) {
+                if (!kv_ready(kpos)) { failed = true; break; }
+                tc_fence_after();
+                scores(t, kpos);
+                if (j + 2 == it.n[t]) umma_commit(bar_q_empty + 8 * t);
+              }
+              if (last && next.valid && !first_scores(next, t)) { failed = true; break; }
+            }
+            if (failed) break;
+            umma_commit(bar_kv_empty + 8 * (vpos % L::STAGES));
+            if (!last || (next.valid && max(next.n[0], next.n[1]))) umma_commit(bar_kv_empty + 8 * (kpos % L::STAGES));
+          }
+          if (n == 0 && next.valid && !failed) {
+            failed = !first_scores(next, 0) || !first_scores(next, 1);
+            if (!failed && max(next.n[0], next.n[1])) umma_commit(bar_kv_empty + 8 * (ring % L::STAGES));
+          }
+          if (failed) report(p.status, DEV_TIMEOUT_MMA);
+        }
+        it = next;
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, 512);
+  }
+}
+
+template <int D>
+static cudaError_t prompt_run(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const PromptParams& p, int num_sms,
+                              cudaStream_t s) {
+  auto kern = attn_prompt_kernel<D>;
+  cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), PromptLayout<D>::SMEM);
+  if (e != cudaSuccess) return e;
+  // what the offsets can come to at most: every sequence may end inside a block
+  const int64_t entries = p.q_tokens / 256 + p.B;
+  const int64_t items = entries * p.Hq;
+  const int grid = static_cast<int>(items < num_sms ? items : num_sms);
+  // the list packs a block number into 12 bits
+  const int listed = entries <= AP_MAX_LIST && p.q_tokens <= 256 * 4096LL;
+  kern<<<grid, AP_THREADS, PromptLayout<D>::SMEM, s>>>(tmQ, tmK, tmV, p, listed, static_cast<int>(entries));
+  return cudaGetLastError();
+}
+
+cudaError_t launch_attn_prompt(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const PromptParams& p, int num_sms,
+                               cudaStream_t s) {
+  if (p.D == 64) return prompt_run<64>(tmQ, tmK, tmV, p, num_sms, s);
+  if (p.D == 96) return prompt_run<96>(tmQ, tmK, tmV, p, num_sms, s);
+  return prompt_run<128>(tmQ, tmK, tmV, p, num_sms, s);
+}
+
+}  // namespace gc

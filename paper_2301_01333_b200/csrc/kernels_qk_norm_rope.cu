@@ -1,0 +1,284 @@
+// RMS norm of every query and key head and the rotation of its elements by position, one pass over the data.
+//
+//   y = x * rsqrt(mean(x^2) + eps) * w ;   (a, b) -> (a cos phi - b sin phi, b cos phi + a sin phi),  phi = pos * inv_freq[i]
+//
+// Bound by memory: every element is read once and written once, about 12 operations each.  The angles of a token are the
+// same for all of its heads, so a CTA takes whole tokens, evaluates cos / sin once per (token, pair) into shared memory
+// (the product pos * inv_freq and its reduction by multiples of 2 pi in fp64, since a far position times a frequency
+// leaves fp32 no fraction), and walks the heads: L lanes per row hold W = 16 bytes of elements each, reduce the square
+// sum with shuffles, and hand the normalised row over in shared memory, where the other half of a pair is picked up.
+// Rows that are not 16-byte aligned (or a head dimension that is no multiple of 8 / 4) take the same code with W = 1.
+#include "serving.cuh"
+
+namespace gc {
+
+namespace {
+constexpr int QN_THREADS = 256;
+
+struct QkParams {
+  gc_heads_t q, k, q_out, k_out;
+  const void* q_weight;
+  const void* k_weight;
+  const int64_t* positions;
+  const float* inv_freq;
+  int64_t tokens;
+  int q_heads, rows;           // rows of a token: q_heads + k_heads
+  int D, half, interleaved, norm;
+  float eps, factor;
+  int tb;                      // tokens per CTA
+  int rows_per_cta;            // rows of each token one CTA takes (grid.y parts of them)
+  int log_l;                   // log2 of the lanes per row
+};
+
+template <typename T>
+__device__ __forceinline__ float to_f(T x);
+template <>
+__device__ __forceinline__ float to_f<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T>
+__device__ __forceinline__ T from_f(float x);
+template <>
+__device__ __forceinline__ float from_f<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// cos and sin of pos * f, both times `factor`.  2 pi = TWO_PI_HI + TWO_PI_LO to about 106 bits.
+__device__ __forceinline__ void turn_of(int64_t pos, float f, float factor, float* c, float* s) {
+  constexpr double TWO_PI_HI = 6.283185307179586232, TWO_PI_LO = 2.4492935982947064e-16;
+  const double phi = static_cast<double>(pos) * static_cast<double>(f);
+  const double n = rint(phi * (1.0 / TWO_PI_HI));
+  const float r = static_cast<float>(fma(-n, TWO_PI_LO, fma(-n, TWO_PI_HI, phi)));
+  float sn, cs;
+  sincosf(r, &sn, &cs);
+  *c = cs * factor;
+  *s = sn * factor;
+}
+}  // namespace
+
+// T: element type, W: consecutive elements per lane (16 bytes, or 1), CH: chunks of L * W elements per row
+template <typename T, int W, int CH>
+__global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const __grid_constant__ QkParams p) {
+  extern __shared__ float4 smem4[];
+  const int L = 1 << p.log_l, slots = QN_THREADS >> p.log_l;
+  float* s_row = reinterpret_cast<float*>(smem4);                        // [slots][D rounded up to 4]
+  const int pitch = (p.D + 3) & ~3, tpitch = (p.half + 3) & ~3;
+  float* s_cos = s_row + slots * pitch;                                  // [tb][half]
+  float* s_sin = s_cos + p.tb * tpitch;
+  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * p.tb;
+  const int nt = static_cast<int>(p.tokens - t0 < p.tb ? p.tokens - t0 : p.tb);
+  const int r0 = blockIdx.y * p.rows_per_cta;
+  const int nr = p.rows - r0 < p.rows_per_cta ? p.rows - r0 : p.rows_per_cta;
+
+  for (int i = threadIdx.x; i < nt * p.half; i += QN_THREADS) {
+    const int t = i / p.half, j = i - t * p.half;
+    turn_of(p.positions[t0 + t], p.inv_freq[j], p.factor, s_cos + t * tpitch + j, s_sin + t * tpitch + j);
+  }
+  __syncthreads();
+
+  const int lane = threadIdx.x & (L - 1), slot = threadIdx.x >> p.log_l;
+  float* row = s_row + slot * pitch;
+  const int total = nt * nr, rot = 2 * p.half;
+  const bool vec_pairs = W > 1 && p.half % W == 0;
+  for (int base = 0; base < total; base += slots) {
+    const int u = base + slot;
+    const bool live = u < total;
+    const int t = live ? u / nr : 0, h = live ? r0 + u - t * nr : 0;
+    const bool is_q = h < p.q_heads;
+    const gc_heads_t& src = is_q ? p.q : p.k;
+    const gc_heads_t& dst = is_q ? p.q_out : p.k_out;
+    const int hh = is_q ? h : h - p.q_heads;
+    const T* x = static_cast<const T*>(src.data) + (t0 + t) * src.token_stride + hh * src.head_stride;
+    T* o = static_cast<T*>(dst.data) + (t0 + t) * dst.token_stride + hh * dst.head_stride;
+    const T* w = static_cast<const T*>(is_q ? p.q_weight : p.k_weight);
+    float y[CH][W];
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int e = (c * L + lane) * W;
+      if (live && e < p.D) {
+        if constexpr (W > 1) {
+          const uint4 v = *reinterpret_cast<const uint4*>(x + e);
+          const T* ve = reinterpret_cast<const T*>(&v);
+#pragma unroll
+          for (int i = 0; i < W; ++i) y[c][i] = to_f<T>(ve[i]);
+        } else {
+          y[c][0] = to_f<T>(x[e]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i) y[c][i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < W; ++i) sum = fmaf(y[c][i], y[c][i], sum);
+    }
+    if (p.norm) {
+      for (int d = L >> 1; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      const float inv = 1.0f / sqrtf(sum / static_cast<float>(p.D) + p.eps);
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const int e = (c * L + lane) * W;
+        if (live && e < p.D) {
+          if (w) {
+            if constexpr (W > 1) {
+              const uint4 v = *reinterpret_cast<const uint4*>(w + e);
+              const T* ve = reinterpret_cast<const T*>(&v);
+#pragma unroll
+              for (int i = 0; i < W; ++i) y[c][i] = y[c][i] * inv * to_f<T>(ve[i]);
+            } else {
+              y[c][0] = y[c][0] * inv * to_f<T>(w[e]);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < W; ++i) y[c][i] *= inv;
+          }
+        }
+      }
+    }
+    const float* ct = s_cos + t * tpitch;
+    const float* st = s_sin + t * tpitch;
+    if (W > 1 && p.interleaved) {
+      // both elements of a pair lie in the lane's own chunk
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const int e = (c * L + lane) * W;
+#pragma unroll
+        for (int i = 0; i + 1 < W; i += 2) {
+          if (e + i < rot) {
+            const int j = (e + i) >> 1;
+            const float a = y[c][i], b = y[c][i + 1], cs = ct[j], sn = st[j];
+            y[c][i] = a * cs - b * sn;
+            y[c][i + 1] = b * cs + a * sn;
+          }
+        }
+      }
+    } else if (rot) {
+      __syncwarp();                                                      // the previous row has been read
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const int e = (c * L + lane) * W;
+        if (e < p.D) {
+          if constexpr (W == 8) {
+            *reinterpret_cast<float4*>(row + e) = make_float4(y[c][0], y[c][1], y[c][2], y[c][3]);
+            *reinterpret_cast<float4*>(row + e + 4) = make_float4(y[c][4], y[c][5], y[c][6], y[c][7]);
+          } else if constexpr (W == 4) {
+            *reinterpret_cast<float4*>(row + e) = make_float4(y[c][0], y[c][1], y[c][2], y[c][3]);
+          } else {
+            row[e] = y[c][0];
+          }
+        }
+      }
+      __syncwarp();
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const int e = (c * L + lane) * W;
+        if (e < rot) {
+          if (vec_pairs) {
+            // half layout, the chunk on one side of the middle: partners and angles are vectors
+            const bool low = e < p.half;
+            const int j = low ? e : e - p.half, pe = low ? e + p.half : j;
+#pragma unroll
+            for (int i = 0; i < W; i += (W >= 4 ? 4 : 1)) {
+              if constexpr (W >= 4) {
+                const float4 b = *reinterpret_cast<const float4*>(row + pe + i);
+                const float4 cs = *reinterpret_cast<const float4*>(ct + j + i);
+                const float4 sn = *reinterpret_cast<const float4*>(st + j + i);
+                const float g = low ? -1.f : 1.f;
+                y[c][i] = fmaf(y[c][i], cs.x, g * b.x * sn.x);
+                y[c][i + 1] = fmaf(y[c][i + 1], cs.y, g * b.y * sn.y);
+                y[c][i + 2] = fmaf(y[c][i + 2], cs.z, g * b.z * sn.z);
+                y[c][i + 3] = fmaf(y[c][i + 3], cs.w, g * b.w * sn.w);
+              }
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+              const int ee = e + i;
+              if (ee < rot) {
+                const bool low = p.interleaved ? !(ee & 1) : ee < p.half;
+                const int j = p.interleaved ? ee >> 1 : (low ? ee : ee - p.half);
+                const int pe = p.interleaved ? ee ^ 1 : (low ? ee + p.half : j);
+                const float b = row[pe];
+                y[c][i] = y[c][i] * ct[j] + (low ? -b : b) * st[j];
+              }
+            }
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int e = (c * L + lane) * W;
+      if (live && e < p.D) {
+        if constexpr (W > 1) {
+          uint4 v;
+          T* ve = reinterpret_cast<T*>(&v);
+#pragma unroll
+          for (int i = 0; i < W; ++i) ve[i] = from_f<T>(y[c][i]);
+          *reinterpret_cast<uint4*>(o + e) = v;
+        } else {
+          o[e] = from_f<T>(y[c][0]);
+        }
+      }
+    }
+  }
+}
+
+static bool aligned_heads(const gc_heads_t& h, int heads, int w, int esz) {
+  return heads == 0 || (reinterpret_cast<uintptr_t>(h.data) % 16 == 0 && h.token_stride % w == 0 && h.head_stride % w == 0 && w * esz == 16);
+}
+
+template <typename T, int W, int CH>
+static cudaError_t launch_t(const QkParams& p, dim3 grid, size_t smem, cudaStream_t s) {
+  auto kern = qk_norm_rope_kernel<T, W, CH>;
+  if (smem > 48 * 1024) {
+    cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
+    if (e != cudaSuccess) return e;
+  }
+  kern<<<grid, QN_THREADS, smem, s>>>(p);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_qk_norm_rope(const gc_qk_norm_rope_t& d, int num_sms, cudaStream_t s) {
+  const bool f32 = d.dtype == GC_F32;
+  const int esz = f32 ? 4 : 2;
+  const int wv = 16 / esz;
+  const bool vec = d.head_dim % wv == 0 && aligned_heads(d.q, d.q_heads, wv, esz) && aligned_heads(d.k, d.k_heads, wv, esz) &&
+                   aligned_heads(d.q_out, d.q_heads, wv, esz) && aligned_heads(d.k_out, d.k_heads, wv, esz) &&
+                   reinterpret_cast<uintptr_t>(d.q_weight) % 16 == 0 && reinterpret_cast<uintptr_t>(d.k_weight) % 16 == 0;
+  const int w = vec ? wv : 1;
+  const int lanes = (d.head_dim + w - 1) / w;
+  int log_l = 0;
+  while (log_l < 5 && (1 << log_l) < lanes) ++log_l;
+  const int slots = QN_THREADS >> log_l;
+  QkParams p = {};
+  p.q = d.q; p.k = d.k; p.q_out = d.q_out; p.k_out = d.k_out;
+  p.q_weight = d.q_weight; p.k_weight = d.k_weight;
+  p.positions = d.positions; p.inv_freq = d.inv_freq;
+  p.tokens = d.tokens;
+  p.q_heads = d.q_heads; p.rows = d.q_heads + d.k_heads;
+  p.D = d.head_dim; p.half = d.rot_dim / 2; p.interleaved = d.interleaved; p.norm = d.norm;
+  p.eps = d.eps; p.factor = d.attention_factor;
+  p.log_l = log_l;
+  // Four tokens per CTA keep its 256 threads busy while the angles are evaluated; with few tokens one per CTA, its heads
+  // spread over as many CTAs as there are SMs (each evaluates the angles again: a few hundred clocks, all at once).
+  p.tb = d.tokens >= 8LL * num_sms ? 4 : 1;
+  int64_t parts = 1;
+  if (d.tokens < num_sms) {
+    parts = num_sms / d.tokens;
+    const int most = (p.rows + slots - 1) / slots;
+    if (parts > most) parts = most;
+  }
+  p.rows_per_cta = static_cast<int>((p.rows + parts - 1) / parts);
+  const int64_t gx = (d.tokens + p.tb - 1) / p.tb;
+  if (gx > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
+  const dim3 grid(static_cast<unsigned>(gx), static_cast<unsigned>((p.rows + p.rows_per_cta - 1) / p.rows_per_cta));
+  const size_t smem = (static_cast<size_t>(slots) * ((d.head_dim + 3) & ~3) + 2 * static_cast<size_t>(p.tb) * ((p.half + 3) & ~3)) * 4;
+  if (f32) {
+    if (!vec) return launch_t<float, 1, 8>(p, grid, smem, s);
+    return lanes > 32 ? launch_t<float, 4, 2>(p, grid, smem, s) : launch_t<float, 4, 1>(p, grid, smem, s);
+  }
+  return vec ? launch_t<__nv_bfloat16, 8, 1>(p, grid, smem, s) : launch_t<__nv_bfloat16, 1, 8>(p, grid, smem, s);
+}
+
+}  // namespace gc

@@ -1,0 +1,63 @@
+// Declarations shared by the host side (gc_serving.cu) and the kernels of the served attention block.
+#pragma once
+#include <cuda_bf16.h>
+
+#include "gc_internal.h"
+
+namespace gc {
+
+// Status word values of the checks the device makes (the bounded waits use those of ptx.cuh).
+enum : uint32_t {
+  DEV_BAD_SLOT = 0x201,
+  DEV_BAD_PAGE = 0x202,
+  DEV_BAD_LENGTH = 0x203,
+  DEV_BAD_OFFSETS = 0x204,
+};
+
+struct Kv4AttnParams {
+  int B, n, Hq, Hk, g;              // g: query heads per key/value head; columns of a unit = n * g
+  int page_shift, width, max_len;
+  int64_t num_pages, table_stride;
+  float c;                          // scale * log2(e)
+  int split_len, n_split;           // tokens per CTA (a multiple of 32) and CTAs per unit
+  int col_chunks;                   // CTAs that share the columns of a unit
+  const __nv_bfloat16* q;
+  int64_t qb, qn, qh;
+  __nv_bfloat16* o;
+  int64_t ob, on, oh;
+  const int* table;
+  const int* lengths;
+  const uint8_t* k_codes;
+  const uint32_t* k_params;         // one (lo, scale) pair per word
+  const uint8_t* v_codes;
+  const uint32_t* v_params;
+  float* ws;
+  uint32_t* status;
+};
+// Columns (query, head) one CTA of the kernel for this many columns covers.
+int attn_kv4_cols(int columns);
+// Resident CTAs per SM the split of the work is planned for.
+int attn_kv4_resident(int head_dim, int group, int cols);
+cudaError_t launch_attn_kv4(const Kv4AttnParams& p, int head_dim, int group, int num_sms, cudaStream_t s);
+
+struct PromptParams {
+  int B, Hq, Hk, D, causal;
+  int64_t q_tokens, k_tokens;
+  float c;                          // scale * log2(e)
+  __nv_bfloat16* o;
+  int64_t o_tok, o_head;
+  const int* cu_q;
+  const int* cu_k;
+  uint32_t* status;
+};
+// tmQ / tmK / tmV: 3-D maps (head dimension, heads, tokens), boxes of 64 x 1 x 128, 128-byte swizzle
+cudaError_t launch_attn_prompt(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const PromptParams& p,
+                               int num_sms, cudaStream_t s);
+
+cudaError_t launch_qk_norm_rope(const gc_qk_norm_rope_t& d, int num_sms, cudaStream_t s);
+cudaError_t launch_kv4_append(const gc_kv4_cache_t& c, int dtype, int64_t tokens, const gc_heads_t& k, const gc_heads_t& v,
+                              const int64_t* slots, cudaStream_t s);
+cudaError_t launch_kv4_read(const gc_kv4_cache_t& c, int dtype, int64_t tokens, const gc_heads_t& k, const gc_heads_t& v,
+                            const int64_t* slots, cudaStream_t s);
+
+}  // namespace gc

@@ -1,0 +1,422 @@
+"""The operators of the served attention block on a B200 against plain 64-bit forms.
+
+Tolerances count roundings: half a step of a type relative to the value is U[type] = finfo.eps / 2; sums of n terms in fp32
+are off by at most n U[f32] times the sum of the terms' sizes; ex2.approx and the reciprocal by 2 U[f32]."""
+import math
+
+import pytest
+import torch
+
+import serving_reference as R
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = {t: torch.finfo(t).eps / 2 for t in (torch.bfloat16, torch.float32)}
+U32 = U[torch.float32]
+
+
+@pytest.fixture(scope="module")
+def S():
+    from paper_2301_01333_b200 import build as gc_build
+    gc_build.build()
+    from paper_2301_01333_b200 import serving
+    return serving
+
+
+def gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def randn(*shape, g, dtype=torch.float32, scale=1.0):
+    return (scale * torch.randn(*shape, generator=g, device=DEV)).to(dtype)
+
+
+def within(got, ref, tol):
+    if got.numel() == 0:
+        return
+    assert torch.isfinite(got).all()
+    off = (got.double() - ref).abs() - tol
+    assert off.max().item() <= 0, f"off by {off.max().item()} more than allowed"
+
+
+# ------------------------------------------------------------------------------------------------ norm and rotation
+def rope_case(S, t, hq, hk, d, rot, dtype, interleaved, norm=True, weights=True, factor=1.0, far=4096, strided=True, seed=0, pad=0):
+    g = gen(seed)
+    if strided:
+        x = randn(t, hq + 2 * hk + 1, d + pad, g=g, dtype=dtype, scale=2.0)[..., :d]
+        q, k = x[:, :hq], x[:, hq + 1:hq + 1 + hk]
+    else:
+        q, k = randn(t, hq, d, g=g, dtype=dtype), randn(t, hk, d, g=g, dtype=dtype)
+    pos = torch.randint(-3, far, (t,), generator=g, device=DEV)
+    inv = S.rotary_inv_freq(rot, device=DEV)
+    qw, kw = (randn(d, g=g, dtype=dtype), randn(d, g=g, dtype=dtype)) if weights else (None, None)
+    qo, ko = S.qk_norm_rope(q, k, pos, inv, qw, kw, norm=norm, eps=1e-5, interleaved=interleaved, attention_factor=factor)
+    for x, w, got in ((q, qw, qo), (k, kw, ko)):
+        ref, size = R.rope(x, w, pos, inv, norm, 1e-5, interleaved, factor)
+        # the norm: a sum of d squares under a root (d / 2), root, quotient, two products; the rotation: angle rounded to fp32
+        # below pi (4 U), sincosf (4 U), factor, two products, a sum
+        tol = (d / 2 + 4 + 12) * U32 * size * abs(factor) + (U[dtype] * ref.abs() if dtype != torch.float32 else 0)
+        within(got, ref, tol + 1e-30)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,rot", [(128, 128), (128, 64), (64, 64), (96, 48), (80, 80), (256, 256), (192, 50), (32, 2), (18, 10), (2, 2), (128, 0)])
+def test_rope_layouts(S, dtype, interleaved, d, rot):
+    rope_case(S, 5, 6, 2, d, rot, dtype, interleaved)
+
+
+@pytest.mark.parametrize("t,hq,hk", [(1, 1, 1), (1, 32, 8), (3, 0, 2), (7, 5, 0), (1300, 3, 1), (1501, 8, 2)])
+def test_rope_sizes(S, t, hq, hk):
+    rope_case(S, t, hq, hk, 128, 128, torch.bfloat16, False, seed=t)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rope_far_positions_factor_and_options(S, dtype):
+    rope_case(S, 9, 4, 4, 128, 128, dtype, False, factor=1.3, far=1 << 30)
+    rope_case(S, 9, 4, 4, 64, 32, dtype, True, norm=False, factor=-0.5)
+    rope_case(S, 9, 4, 4, 64, 64, dtype, False, weights=False, strided=False)
+    rope_case(S, 9, 4, 4, 64, 64, dtype, False, pad=1)          # rows that are not 16-byte aligned
+
+
+def test_rope_in_place_and_no_tokens(S):
+    g = gen(1)
+    qkv = randn(33, 10, 64, g=g, dtype=torch.bfloat16)
+    q, k, rest = qkv[:, :6], qkv[:, 6:8], qkv[:, 8:].clone()
+    pos, inv = torch.arange(33, device=DEV), S.rotary_inv_freq(64, device=DEV)
+    qo, ko = S.qk_norm_rope(q, k, pos, inv)
+    S.qk_norm_rope(q, k, pos, inv, q_out=q, k_out=k)
+    assert torch.equal(q, qo) and torch.equal(k, ko) and torch.equal(qkv[:, 8:], rest)
+    a, b = S.qk_norm_rope(q[:0], k[:0], pos[:0], inv)
+    assert a.shape == (0, 6, 64) and b.shape == (0, 2, 64)
+
+
+def test_rope_zero_rows_and_non_finite_rows_stay_apart(S):
+    g = gen(2)
+    x = randn(4, 3, 128, g=g, dtype=torch.float32)
+    x[1] = 0
+    x[2, 1, 7] = math.inf
+    pos, inv = torch.arange(4, device=DEV), S.rotary_inv_freq(128, device=DEV)
+    q, _ = S.qk_norm_rope(x, x[:, :1], pos, inv)
+    assert (q[1] == 0).all() and torch.isnan(q[2, 1]).any()
+    assert torch.isfinite(q[0]).all() and torch.isfinite(q[3]).all() and torch.isfinite(q[2, 0]).all()
+
+
+# ------------------------------------------------------------------------------------------------ the cache
+def spread(t, page, pages, g):
+    order = torch.randperm(pages, generator=g, device=DEV)
+    at = torch.arange(t, device=DEV)
+    return order[at // page] * page + at % page
+
+
+SHAPES = [(64, 32), (64, 64), (96, 32), (128, 32), (128, 64), (128, 128)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d,group", SHAPES)
+@pytest.mark.parametrize("t,h,page", [(1, 1, 16), (37, 3, 32), (130, 2, 256)])
+def test_cache_write_and_read_are_exact(S, dtype, d, group, t, h, page):
+    g = gen(t + d)
+    pages = -(-t // page) + 2
+    cache = S.KV4Cache.allocate(pages, page, h, d, group)
+    slots = spread(t, page, pages, g)
+    if t > 5:
+        slots[4] = -1
+    kv = randn(t, 2 * h + 1, d, g=g) * torch.exp2(3 * randn(d, g=g))
+    kv[0, 0] = 1.5                                               # one value throughout: scale 0
+    if t > 20:
+        kv[7] = (torch.arange(d, device=DEV) % 16) * 0.5 + 0.25 * (torch.arange(d, device=DEV) % 2)    # ties between codes
+        kv[8] = 0
+        kv[9] = 1e-39                                            # subnormal
+        kv[10] = torch.where(torch.arange(d, device=DEV) % 2 == 0, 1e-42, 3e-41)
+    kv = kv.to(dtype)
+    k, v = kv[:, :h], kv[:, h:2 * h]
+    before = [x.clone() for x in (cache.k_codes, cache.k_params, cache.v_codes, cache.v_params)]
+    cache.append(k, v, slots)
+    cache.query_status()
+    ok = slots >= 0
+    p, o = slots[ok] // page, slots[ok] % page
+    for x, codes, params, c0, p0 in ((k, cache.k_codes, cache.k_params, before[0], before[1]),
+                                     (v, cache.v_codes, cache.v_params, before[2], before[3])):
+        code, lo, scale = R.quantise(x[ok], group)
+        got = codes[p, :, o]
+        assert torch.equal(torch.stack([got & 15, got >> 4], -1).flatten(-2).double(), code)
+        assert torch.equal(params[p, :, o].double(), torch.stack([lo, scale], -1))
+        c0[p, :, o], p0[p, :, o] = got, params[p, :, o]          # and nothing else was written
+        assert torch.equal(codes, c0) and torch.equal(params, p0)
+    for out in (torch.float32, torch.bfloat16):
+        ko, vo = torch.full((t, h, d), 7.0, dtype=out, device=DEV), torch.full((t, h + 1, d), 7.0, dtype=out, device=DEV)[:, :h]
+        cache.read(slots, k_out=ko, v_out=vo)
+        for got, codes, params in ((ko, cache.k_codes, cache.k_params), (vo, cache.v_codes, cache.v_params)):
+            want = R.values(codes[p, :, o], params[p, :, o])[0].float().to(out)      # the product is exact, the sum rounded once
+            assert torch.equal(got[ok], want) and (got[~ok] == 7.0).all()
+
+
+def test_cache_rows_that_are_not_aligned(S):
+    g = gen(5)
+    cache = S.KV4Cache.allocate(3, 16, 2, 64, 32)
+    x = randn(20, 4, 65, g=g, dtype=torch.bfloat16)[..., 1:]
+    slots = spread(20, 16, 3, g)
+    cache.append(x[:, :2], x[:, 2:], slots)
+    a = cache.read(slots, torch.float32)
+    y = torch.empty(20, 4, 67, device=DEV)[..., 3:]
+    cache.read(slots, k_out=y[:, :2], v_out=y[:, 2:])
+    assert torch.equal(a[0], y[:, :2]) and torch.equal(a[1], y[:, 2:])
+    code, lo, scale = R.quantise(x[:, :2], 32)
+    held = (lo[..., None] + code.unflatten(-1, (2, 32)) * scale[..., None]).flatten(-2)
+    assert torch.equal(a[0].double(), held.float().double())
+
+
+def test_cache_non_finite_groups_are_held_as_nan(S):
+    cache = S.KV4Cache.allocate(1, 16, 1, 128, 32)
+    x = torch.ones(4, 1, 128, device=DEV)
+    x[0, 0, 3], x[1, 0, 40], x[2, 0, 70], x[2, 0, 71] = math.nan, -math.inf, 3e38, -3e38
+    x[3, 0, 96:] = torch.arange(32, device=DEV)
+    slots = torch.arange(4, device=DEV)
+    cache.append(x, torch.zeros_like(x), slots)
+    k, v = cache.read(slots, torch.float32)
+    bad = torch.zeros(4, 4, dtype=torch.bool, device=DEV)
+    bad[0, 0] = bad[1, 1] = bad[2, 2] = True
+    nan = torch.isnan(k[:, 0]).unflatten(-1, (4, 32))
+    assert torch.equal(nan.all(-1), bad) and torch.equal(nan.any(-1), bad) and (v == 0).all()
+
+
+def test_cache_slots_out_of_bounds_are_reported(S):
+    cache = S.KV4Cache.allocate(2, 16, 1, 64, 64)
+    x = torch.ones(3, 1, 64, device=DEV)
+    for call in (lambda s: cache.append(x, x, s), lambda s: cache.read(s)):
+        call(torch.tensor([0, 32, 1], device=DEV))
+        with pytest.raises(S.GcError, match="slot"):
+            cache.query_status()
+        cache.query_status()                                     # cleared
+    assert (cache.read(torch.tensor([0, 1], device=DEV), torch.float32)[0] == 1).all()
+
+
+# ------------------------------------------------------------------------------------------------ attention over the cache
+def filled_cache(S, pages, page, h, d, group, g):
+    cache = S.KV4Cache.allocate(pages, page, h, d, group)
+    for codes, params in ((cache.k_codes, cache.k_params), (cache.v_codes, cache.v_params)):
+        codes.copy_(torch.randint(0, 256, codes.shape, generator=g, device=DEV, dtype=torch.uint8))
+        params[..., 0] = -2.2 - 0.4 * randn(*params.shape[:-1], g=g)
+        params[..., 1] = 0.2 + 0.2 * torch.rand(params.shape[:-1], generator=g, device=DEV)
+    return cache
+
+
+def table_of(lens, page, pages, g, width=None):
+    need = [-(-n // page) for n in lens]
+    width = width or max(need + [1])
+    table = torch.full((len(lens), width), -7, dtype=torch.int32, device=DEV)
+    order, at = torch.randperm(pages, generator=g, device=DEV).to(torch.int32), 0
+    for b, n in enumerate(need):
+        table[b, :n] = order[at:at + n]
+        at += n
+    return table
+
+
+def attend_reference(cache, q, table, lens, scale, group, edge=False):
+    b, n, hq, d = q.shape
+    g = hq // cache.kv_heads
+    o = torch.zeros(q.shape, dtype=torch.float64, device=DEV)
+    tol = torch.zeros_like(o)
+    for i, m in enumerate(lens):
+        if m == 0:
+            continue
+        pages = table[i, :-(-m // cache.page_size)].long()
+        k, _ = R.values(cache.k_codes[pages].transpose(1, 2).flatten(0, 1)[:m], cache.k_params[pages].transpose(1, 2).flatten(0, 1)[:m])
+        v, lo = R.values(cache.v_codes[pages].transpose(1, 2).flatten(0, 1)[:m], cache.v_params[pages].transpose(1, 2).flatten(0, 1)[:m])
+        ks = cache.k_params[pages].double().abs().nan_to_num(0.).amax()
+        lim = torch.arange(n, device=DEV) + (m - n + 1)
+        for h in range(hq):
+            qq = q[i, :, h].double()
+            f = R.head if edge else R.head_all
+            o[i, :, h], size = f(qq, k[:, h // g], v[:, h // g], lim, scale)
+            _, coded = f(qq, k[:, h // g], (v - lo)[:, h // g], lim, scale)
+            # p' = bf16(p scale): half a step of every code's part.  An exponent is a sum of d products of q and 16 + code,
+            # minus 16 sum q (sizes up to 47 scale sum |q| in all, d + 4 fp32 steps): p is off by that relative to itself, and
+            # so is the sum of p; then the offsets' sum and the sum over keys, in fp32 (16 / 15 and n terms, |v| + 32 scale each)
+            expo = scale * ks * 47 * qq.abs().sum(-1, keepdim=True) * (d + 4) * U32 + 4 * U32
+            tol[i, :, h] = U[torch.bfloat16] * coded + (2 * expo + (m / 64 + 64) * 40 * U32) * (size + 1) + U[torch.bfloat16] * o[i, :, h].abs()
+    return o, tol
+
+
+def attend_case(S, lens, n, hq, hk, d, group, page, seed=0, max_length=None, scale=None, qscale=1.0):
+    g = gen(seed)
+    pages = sum(-(-x // page) for x in lens) + 2
+    cache = filled_cache(S, pages, page, hk, d, group, g)
+    table = table_of(lens, page, pages, g)
+    q = randn(len(lens), n, hq + 1, d, g=g, dtype=torch.bfloat16, scale=qscale)[:, :, :hq]
+    out = cache.attend(q, table, torch.tensor(lens, dtype=torch.int32, device=DEV), max_length=max_length, scale=scale)
+    cache.query_status()
+    ref, tol = attend_reference(cache, q, table, lens, d ** -0.5 if scale is None else scale, group)
+    within(out, ref, tol)
+    return cache, q, table, out
+
+
+@pytest.mark.parametrize("d,group", SHAPES)
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("hq,hk", [(4, 4), (8, 2), (14, 2), (16, 1)])
+def test_attend_shapes(S, d, group, page, hq, hk):
+    attend_case(S, [1, 77, 0, 300, 16, 31, 33], 1, hq, hk, d, group, page, seed=d + group)
+
+
+@pytest.mark.parametrize("n", [1, 2, 5, 16])
+@pytest.mark.parametrize("hq,hk", [(2, 2), (12, 2), (48, 2)])
+def test_attend_several_queries(S, n, hq, hk):
+    attend_case(S, [n, n - 1, 1, 200, 513], n, hq, hk, 128, 64, 32, seed=n)
+
+
+@pytest.mark.parametrize("lens", [[1], [256], [257], [4000], [5001, 3, 2600]])
+@pytest.mark.parametrize("max_length", [None, 8192])
+def test_attend_split_lengths(S, lens, max_length):
+    g = gen(9)
+    page = 64
+    pages = sum(-(-x // page) for x in lens) + 2
+    cache = filled_cache(S, pages, page, 2, 128, 64, g)
+    table = table_of(lens, page, pages, g, width=128)
+    q = randn(len(lens), 1, 8, 128, g=g, dtype=torch.bfloat16)
+    out = cache.attend(q, table, torch.tensor(lens, dtype=torch.int32, device=DEV), max_length=max_length)
+    ref, tol = attend_reference(cache, q, table, lens, 128 ** -0.5, 64)
+    within(out, ref, tol)
+    again = cache.attend(q, table, torch.tensor(lens, dtype=torch.int32, device=DEV), max_length=max_length)
+    assert torch.equal(out, again)                               # joined in a fixed order
+    cache.query_status()
+
+
+def test_attend_scores_that_rise_and_fall(S):
+    # scores of hundreds of binades in both directions: the reference has to be raised many times, and old parts vanish
+    attend_case(S, [700, 129], 1, 8, 2, 128, 32, 16, seed=3, qscale=40.0)
+    attend_case(S, [700, 129], 2, 8, 2, 64, 64, 16, seed=4, scale=3.0)
+
+
+@pytest.mark.parametrize("d,group", SHAPES)
+def test_attend_ignores_what_lies_behind_a_sequence(S, d, group):
+    g = gen(11)
+    lens, page, n = [37, 5, 18], 32, 3
+    cache = filled_cache(S, 5, page, 2, d, group, g)
+    table = table_of(lens, page, 5, g)
+    for b, m in enumerate(lens):                                 # infinities and NaN in every slot behind the last token
+        last = table[b, (m - 1) // page]
+        for params in (cache.k_params, cache.v_params):
+            params[last, :, m % page or page:] = torch.tensor([math.nan, math.inf], device=DEV, dtype=torch.bfloat16)
+    for params in (cache.k_params, cache.v_params):              # and in the newest token of one sequence: its last query's business
+        params[table[0, 36 // page], :, 36 % page] = math.nan
+    q = randn(3, n, 4, d, g=g, dtype=torch.bfloat16)
+    out = cache.attend(q, table, torch.tensor(lens, dtype=torch.int32, device=DEV))
+    ref, tol = attend_reference(cache, q, table, lens, d ** -0.5, group, edge=True)
+    assert torch.isnan(out[0, 2]).all()
+    out[0, 2], ref[0, 2], tol[0, 2] = 0, 0, 0
+    within(out, ref, tol)
+
+
+def test_attend_reports_bad_pages_and_lengths(S):
+    g = gen(12)
+    cache = filled_cache(S, 4, 16, 1, 64, 64, g)
+    q = randn(2, 1, 2, 64, g=g, dtype=torch.bfloat16)
+    table = torch.tensor([[0, 4], [1, 2]], dtype=torch.int32, device=DEV)
+    lens = torch.tensor([20, 20], dtype=torch.int32, device=DEV)
+    out = cache.attend(q, table, lens)
+    with pytest.raises(S.GcError, match="page"):
+        cache.query_status()
+    ref, tol = attend_reference(cache, q[1:], table[1:], [20], 0.125, 64)
+    within(out[1:], ref, tol)                                    # the other sequence is untouched by it
+    for bad in ([33, 1], [-1, 1]):
+        cache.attend(q, torch.zeros_like(table), torch.tensor(bad, dtype=torch.int32, device=DEV))
+        with pytest.raises(S.GcError, match="length"):
+            cache.query_status()
+    cache.attend(q, torch.zeros_like(table), torch.tensor([32, 0], dtype=torch.int32, device=DEV), max_length=32)
+    cache.query_status()
+
+
+# ------------------------------------------------------------------------------------------------ prompts
+def prompt_case(S, nq, nk, hq, hk, d, causal, seed=0, tail=0, scale=None, qscale=1.0, poison=False):
+    g = gen(seed)
+    cu_q = torch.tensor([0] + nq, device=DEV).cumsum(0).to(torch.int32)
+    cu_k = torch.tensor([0] + nk, device=DEV).cumsum(0).to(torch.int32)
+    tq, tk = sum(nq) + tail, sum(nk) + tail
+    q = randn(tq, hq + 1, d, g=g, dtype=torch.bfloat16, scale=qscale)[:, :hq]
+    kv = randn(tk, 2 * hk, d, g=g, dtype=torch.bfloat16)
+    k, v = kv[:, :hk], kv[:, hk:]
+    if poison:                                                   # rows no sequence owns hold anything
+        k[sum(nk):], v[sum(nk):], q[sum(nq):] = math.nan, math.inf, math.nan
+    out = torch.full((tq, hq, d), 0.25, dtype=torch.bfloat16, device=DEV)
+    status = S.new_status(DEV)
+    S.attention_prompt(q, k, v, cu_q, cu_k, causal=causal, out=out, scale=scale, status=status)
+    S.query_status(status)
+    c = d ** -0.5 if scale is None else scale
+    for b in range(len(nq)):
+        a0, a1, c0, c1 = int(cu_q[b]), int(cu_q[b + 1]), int(cu_k[b]), int(cu_k[b + 1])
+        lim = torch.arange(a1 - a0, device=DEV) + (nk[b] - nq[b] + 1) if causal else torch.full((a1 - a0,), nk[b], device=DEV)
+        for h in range(hq):
+            if a1 == a0:
+                continue
+            qq = q[a0:a1, h].double()
+            kk, vv = k[c0:c1, h // (hq // hk)].double(), v[c0:c1, h // (hq // hk)].double()
+            ref, size = R.head_all(qq, kk, vv, lim, c)
+            big = (qq.abs() @ kk.abs().T).amax(-1, keepdim=True) if c1 > c0 else torch.zeros(a1 - a0, 1, device=DEV)
+            # p rounded to bf16 (half a step of every term); exponents: d fp32 steps of their size, and the reference; sums over
+            # nk keys in fp32; the output's rounding
+            tol = U[torch.bfloat16] * size + 2 * (c * big * (d + 4) * U32 + 4 * U32) * size + (nk[b] / 16 + 16) * U32 * size + U[torch.bfloat16] * ref.abs()
+            within(out[a0:a1, h], ref, tol)
+    assert (out[sum(nq):] == 0.25).all()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("n", [1, 2, 127, 128, 129, 255, 256, 257, 400])
+def test_prompt_lengths(S, causal, d, n):
+    prompt_case(S, [n], [n], 2, 1, d, causal, seed=n)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d", [64, 96, 128])
+def test_prompt_packed(S, causal, d):
+    n = [3, 0, 200, 1, 513, 64, 0, 130]
+    prompt_case(S, n, n, 6, 2, d, causal, seed=d, tail=70, poison=True)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_prompt_continued_and_rows_that_see_nothing(S, causal):
+    prompt_case(S, [5, 300, 1, 7, 260, 40], [700, 301, 129, 0, 3, 40], 4, 4, 128, causal, seed=1)
+    prompt_case(S, [5, 300, 1, 7, 260, 40], [128, 301, 256, 0, 140, 39], 3, 1, 64, causal, seed=2)
+
+
+def test_prompt_more_work_than_ctas(S):
+    prompt_case(S, [900, 17, 1500, 333], [900, 17, 1500, 333], 16, 4, 128, True, seed=3)
+    prompt_case(S, [900, 17, 1500, 333], [1000, 900, 1600, 333], 32, 32, 64, True, seed=4)
+
+
+def test_prompt_many_sequences(S):
+    # more pieces than the sorted work list holds
+    g = torch.Generator().manual_seed(0)
+    n = torch.randint(0, 5, (1400,), generator=g).tolist()
+    n[700] = 300
+    prompt_case(S, n, n, 1, 1, 64, True, seed=5)
+
+
+def test_prompt_scores_that_rise(S):
+    prompt_case(S, [700], [700], 2, 2, 128, True, seed=6, qscale=30.0)
+    prompt_case(S, [700], [700], 2, 2, 64, False, seed=7, scale=4.0)
+
+
+def test_prompt_neighbours_that_are_not_finite(S):
+    # keys, values and queries of one sequence hold NaN and infinities: its neighbours, whose tiles reach into it, stay clean;
+    # so do the rows before a NaN key of their own sequence
+    g = gen(8)
+    cu = torch.tensor([0, 130, 258, 328], dtype=torch.int32, device=DEV)
+    q, k, v = (randn(328, 2, 64, g=g, dtype=torch.bfloat16) for _ in range(3))
+    clean = S.attention_prompt(q, k, v, cu)
+    q[130:258], k[130:200], v[130:258] = math.nan, math.inf, math.inf
+    k[129], k[327] = math.nan, math.nan
+    got = S.attention_prompt(q, k, v, cu)
+    keep = torch.ones(328, dtype=torch.bool, device=DEV)
+    keep[129:258], keep[327] = False, False
+    assert torch.equal(got[keep], clean[keep]) and torch.isnan(got[[129, 327]]).all()
+
+
+def test_prompt_offsets_out_of_bounds_are_reported(S):
+    q = torch.zeros(300, 2, 64, dtype=torch.bfloat16, device=DEV)
+    for cu in ([0, 200, 100, 300], [0, 301, 301, 301], [-1, 10, 20, 300]):
+        status = S.new_status(DEV)
+        S.attention_prompt(q, q, q, torch.tensor(cu, dtype=torch.int32, device=DEV), status=status)
+        with pytest.raises(S.GcError, match="offsets"):
+            S.query_status(status)
