@@ -1,7 +1,7 @@
 """In-tree build of the CUDA library (sm_100a only) with nvcc.
 
 ``python -m paper_2301_01333_b200.build`` compiles ``csrc/*.cu`` into ``libgc_b200.so`` next to this
-file.  nvcc cross-compiles without a GPU, so this also runs on a CPU-only box.
+file, and ``csrc/serving_torch.cpp``, the torch side of ``serving.py``, into ``_serving.so``.  nvcc cross-compiles without a GPU, so this also runs on a CPU-only box.
 """
 from __future__ import annotations
 
@@ -13,6 +13,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgc_b200.so")
+TORCH_LIB = os.path.join(HERE, "_serving.so")
+TORCH_SOURCE = os.path.join(CSRC, "serving_torch.cpp")
 SOURCES = ["gc_api.cu", "gc_noalloc.cu", "kernels_generic.cu", "kernels_gemm_tc.cu", "kernels_gemm_tc2.cu", "kernels_chain.cu", "kernels_chain_cluster.cu",
            "kernels_sdpa_tc.cu", "kernels_sdpa_wide.cu", "kernels_sdpa_long.cu", "kernels_sdpa_small.cu",
            "gc_serving.cu", "kernels_qk_norm_rope.cu", "kernels_kv4.cu", "kernels_attn_kv4.cu", "kernels_attn_prompt.cu"]
@@ -38,10 +40,44 @@ def _stale() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _torch_stale() -> bool:
+    deps = [TORCH_SOURCE, os.path.join(HERE, "..", "include", "gc.h")]
+    return not os.path.exists(TORCH_LIB) or any(os.path.getmtime(d) > os.path.getmtime(TORCH_LIB) for d in deps)
+
+
+def _torch_command():
+    """The command that compiles ``_serving.so`` against the installed torch and the library next to it."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension as X
+    inc = X.include_paths() + [sysconfig.get_paths()["include"], "/usr/local/cuda/include"]
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    return (["g++", "-O2", "-std=c++20", "-fPIC", "-shared", "-fvisibility=hidden",
+             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+            + [a for d in inc for a in ("-isystem", d)] + [TORCH_SOURCE, "-o", TORCH_LIB + ".new", LIB, "-L" + libs]
+            + ["-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN"])
+
+
+def _build_torch(verbose: bool) -> None:
+    r = subprocess.run(_torch_command(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if verbose or r.returncode != 0:
+        sys.stderr.write(r.stdout)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed on serving_torch.cpp")
+    os.replace(TORCH_LIB + ".new", TORCH_LIB)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile the library if it is missing or older than its sources; return its path."""
-    if not force and not _stale():
-        return LIB
+    """Compile what is missing or older than its sources; return the path of the CUDA library."""
+    if force or _stale():
+        _build_cuda(verbose)
+    if force or _torch_stale():
+        _build_torch(verbose)
+    return LIB
+
+
+def _build_cuda(verbose: bool) -> None:
     nvcc = _nvcc()
     objs = []
     bdir = os.path.join(HERE, "build")
@@ -58,12 +94,11 @@ def build(force: bool = False, verbose: bool = False) -> str:
             sys.stderr.write(out)
         if p.returncode != 0:
             raise RuntimeError(f"nvcc failed on {s}")
-    cmd = [nvcc, "-shared", "-o", LIB] + objs + ["-gencode", "arch=compute_100a,code=sm_100a", "-cudart", "static"]
+    cmd = [nvcc, "-shared", "-o", LIB, "-Xlinker", "-soname=libgc_b200.so"] + objs + ["-gencode", "arch=compute_100a,code=sm_100a", "-cudart", "static"]
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if r.returncode != 0:
         sys.stderr.write(r.stdout)
         raise RuntimeError("link failed")
-    return LIB
 
 
 if __name__ == "__main__":

@@ -10,9 +10,10 @@
 //     the number 16 + code, exactly, and one shift and one logic instruction make two of them.  Scales and offsets are
 //     applied to sums, never to elements:
 //       q . K[t]            = scale_t * (sum_i q_i (16 + code_i) - 16 sum_i q_i) + lo_t * sum_i q_i       per group
-//       sum_t p_t V[t][d]   = sum_t p'_t (16 + code_td) + sum_t (p_t lo_t - 16 p'_t),   p'_t = bf16(p_t scale_t)
+//       sum_t p_t V[t][d]   = sum_t p'_t (16 + code_td) + sum_t (p_t (lo_t + 7.5 scale_t) - 23.5 p'_t),   p'_t = bf16(p_t scale_t)
 //     The first sum of each line is the MMA's (fp32 accumulators, -16 sum q as their initial value in the first); the
-//     others are a few fp32 operations per (token, column).  p' is the only rounding before the output's.
+//     others are a few fp32 operations per (token, column).  p' is the only rounding before the output's; what it rounds is the
+//     distance from the middle of the group's range (code - 7.5), half of what the distance from lo would lose.
 //   * m16n8k16 MMAs with the codes as the 16-row operand: tokens are the rows of the first product and the reduction of the
 //     second, so a lane's nibbles are always neighbours in memory (head-dimension neighbours; the order inside a reduction
 //     axis is free, Q and P are permuted to match), and 8 columns cost 8, not 16.
@@ -349,11 +350,12 @@ __global__ void __launch_bounds__(AK_THREADS) attn_kv4_kernel(const __grid_const
 #pragma unroll
       for (int j = 0; j < NG; ++j) {
         const uint32_t pa = lds32(vp + (ta * NG + j) * 4), pb = lds32(vp + ((ta + 8) * NG + j) * 4);
+        const float ma = fmaf(7.5f, bf_hi(pa), bf_lo(pa)), mb = fmaf(7.5f, bf_hi(pb), bf_lo(pb));     // the middle of a group's range
         uint32_t bf[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float x0 = pw[nt][0] * bf_hi(pa), x1 = pw[nt][1] * bf_hi(pa), x2 = pw[nt][2] * bf_hi(pb), x3 = pw[nt][3] * bf_hi(pb);
-          float y0 = pw[nt][0] * bf_lo(pa), y1 = pw[nt][1] * bf_lo(pa), y2 = pw[nt][2] * bf_lo(pb), y3 = pw[nt][3] * bf_lo(pb);
+          float y0 = pw[nt][0] * ma, y1 = pw[nt][1] * ma, y2 = pw[nt][2] * mb, y3 = pw[nt][3] * mb;
           if (edge) {                                            // a weight of zero hides whatever the cache holds there
             if (s[mt][nt][0] == -INFINITY) x0 = y0 = 0.f;
             if (s[mt][nt][1] == -INFINITY) x1 = y1 = 0.f;
@@ -361,8 +363,8 @@ __global__ void __launch_bounds__(AK_THREADS) attn_kv4_kernel(const __grid_const
             if (s[mt][nt][3] == -INFINITY) x3 = y3 = 0.f;
           }
           const uint32_t ua = pack_bf16(x0, x1), ub = pack_bf16(x2, x3);
-          z[nt][j][0] += fmaf(-16.f, bf_lo(ua) + bf_lo(ub), y0 + y2);
-          z[nt][j][1] += fmaf(-16.f, bf_hi(ua) + bf_hi(ub), y1 + y3);
+          z[nt][j][0] += fmaf(-23.5f, bf_lo(ua) + bf_lo(ub), y0 + y2);
+          z[nt][j][1] += fmaf(-23.5f, bf_hi(ua) + bf_hi(ub), y1 + y3);
           bf[nt][0] = transpose8x8(ua);
           bf[nt][1] = transpose8x8(ub);
         }
