@@ -4,16 +4,21 @@
 //
 // A column is one (query, query head) of those that share a key/value head.  The floor is the cache read once; a key
 // element is half a byte, so the work per byte is what has to be kept small: at the copy bandwidth of the whole GPU an SM
-// has 2.8 lane-instructions per element of K or V.
+// has 2.8 lane-instructions per element of K or V, 1.4 of them on the integer / logic pipe.
 //
-//   * The codes go into the matrix instruction as they are.  A nibble moved to bits 3..6 of a bf16 with exponent of 16 is
-//     the number 16 + code, exactly, and one shift and one logic instruction make two of them.  Scales and offsets are
-//     applied to sums, never to elements:
-//       q . K[t]            = scale_t * (sum_i q_i (16 + code_i) - 16 sum_i q_i) + lo_t * sum_i q_i       per group
-//       sum_t p_t V[t][d]   = sum_t p'_t (16 + code_td) + sum_t (p_t (lo_t + 7.5 scale_t) - 23.5 p'_t),   p'_t = bf16(p_t scale_t)
-//     The first sum of each line is the MMA's (fp32 accumulators, -16 sum q as their initial value in the first); the
-//     others are a few fp32 operations per (token, column).  p' is the only rounding before the output's; what it rounds is the
-//     distance from the middle of the group's range (code - 7.5), half of what the distance from lo would lose.
+//   * The codes go into the matrix instruction as they are.  A nibble in the low bits of the mantissa of a 16-bit float whose
+//     exponent makes that bit worth 1 is the number (a power of two) + code, exactly, and one logic instruction makes two
+//     of them.  Scales and offsets are applied to sums, never to elements:
+//       q . K[t]            = scale_t * (sum_i q_i (off_i + code_i) - sum_i off_i q_i) + lo_t * sum_i q_i          per group
+//       sum_t p_t V[t][d]   = sum_t p'_t (off_d + code_td) + sum_t p_t (lo_t + 7.5 scale_t) - (off_d + 7.5) sum_t p'_t
+//     with p'_t = bf16(p_t scale_t).  The first sum of each line is the MMA's (fp32 accumulators, - sum off q as their initial
+//     value in the first), and so is the last of the second (a product with ones); the others are a few fp32 operations per
+//     (token, column).  p' is the only rounding before the output's; what it rounds is the distance from the middle of the
+//     group's range (code - 7.5), half of what the distance from lo would lose.
+//   * Keys are fp16 operands: ten mantissa bits hold both nibbles of a byte where they lie (off 1024 and 64), 5 instructions
+//     for 8 elements.  q, bf16, becomes fp16 exactly after a division of its row by a power of two near its largest element
+//     (elements below 2^-14 of that keep an absolute 2^-25 of it).  Weights p' need bf16's range, so values are bf16
+//     operands: off 128 and, one shift later, 16; 8 instructions for 8 elements with the joining of token pairs.
 //   * m16n8k16 MMAs with the codes as the 16-row operand: tokens are the rows of the first product and the reduction of the
 //     second, so a lane's nibbles are always neighbours in memory (head-dimension neighbours; the order inside a reduction
 //     axis is free, Q and P are permuted to match), and 8 columns cost 8, not 16.
@@ -23,6 +28,10 @@
 //     (when a sequence is split) by a second small kernel in a fixed order.
 //   * The running maximum is a reference that is only raised when a score exceeds it by 2^8: one vote per tile instead
 //     of a reduction, and the sums stay far inside fp32.
+#include <cuda_fp16.h>
+
+#include <type_traits>
+
 #include "ptx.cuh"
 #include "serving.cuh"
 
@@ -32,7 +41,7 @@ namespace {
 constexpr int AK_WARPS = 4;
 constexpr int AK_THREADS = AK_WARPS * 32;
 constexpr int AK_TILE = 32;                  // tokens per tile of a warp
-constexpr int AK_STAGES = 4;
+constexpr int AK_STAGES = 3;
 constexpr float AK_RAISE = 8.0f;             // binades a score may exceed the reference by
 
 template <int D, int G>
@@ -50,32 +59,57 @@ __device__ __forceinline__ float ak_ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Addresses are a register plus a constant: an addition per access would go to the pipe that unpacks the codes.
+template <int DST, int SRC>
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  asm volatile("cp.async.cg.shared.global [%0 + %2], [%1 + %3], 16;" ::"r"(dst), "l"(src), "n"(DST), "n"(SRC) : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+template <int OFF>
 __device__ __forceinline__ uint32_t lds32(uint32_t a) {
   uint32_t v;
-  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
+  asm volatile("ld.shared.b32 %0, [%1 + %2];" : "=r"(v) : "r"(a), "n"(OFF));
   return v;
 }
+template <int OFF>
 __device__ __forceinline__ uint32_t lds16(uint32_t a) {
   uint16_t v;
-  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
+  asm volatile("ld.shared.u16 %0, [%1 + %2];" : "=h"(v) : "r"(a), "n"(OFF));
   return v;
 }
+template <int OFF>
 __device__ __forceinline__ uint2 lds64(uint32_t a) {
   uint2 v;
-  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2 + %3];" : "=r"(v.x), "=r"(v.y) : "r"(a), "n"(OFF));
   return v;
 }
-// nibble i of each 16-bit half as the bf16 number 16 + nibble
-template <int I>
-__device__ __forceinline__ uint32_t nib(uint32_t w) {
-  const uint32_t s = I == 0 ? w << 3 : w >> (I == 0 ? 0 : 4 * I - 3);
-  return (s & 0x00780078u) | 0x41804180u;
+// f(constant 0), f(constant 1), ... : loops whose index has to be one
+template <int N, typename F, int I = 0>
+__device__ __forceinline__ void each(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    each<N, F, I + 1>(static_cast<F&&>(f));
+  }
+}
+// (w & mask) | bits in one instruction (written out: left to itself the compiler made two of it)
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(w), "r"(mask), "r"(bits));
+  return r;
+}
+// two nibbles of 16-bit halves as floats: bits 0..3 of the halves as fp16 1024 + code, bits 4..7 as 64 + code
+__device__ __forceinline__ uint32_t nib_h0(uint32_t w) { return and_or(w, 0x000f000fu, 0x64006400u); }
+__device__ __forceinline__ uint32_t nib_h1(uint32_t w) { return and_or(w, 0x00f000f0u, 0x54005400u); }
+// the same as bf16: 128 + code, and (from bits 4..7) 16 + code
+__device__ __forceinline__ uint32_t nib_b0(uint32_t w) { return and_or(w, 0x000f000fu, 0x43004300u); }
+__device__ __forceinline__ uint32_t nib_b1(uint32_t w) { return and_or(w >> 1, 0x00780078u, 0x41804180u); }
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -96,22 +130,34 @@ __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w <<
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 // Byte offset of 16-byte chunk c of token row r in a codes tile.  The exclusive-or spreads the rows that one load
-// instruction touches over all banks: eight rows with the same chunk (keys), rows 0..3, 4..7, ... with two neighbouring
-// chunks (values).
+// instruction touches over all banks: eight rows with the same chunk (keys, 4 bytes a lane), rows 0, 4, 1, 5 and 2, 6, 3, 7 with
+// two neighbouring chunks (keys, 8 bytes a lane), rows 0..3, 4..7, ... with two neighbouring chunks (values).
+// CTAs per SM the registers are cut for: outputs take D / 8 registers per eight columns, and every group of the head
+// dimension ten more, which have to fit in 128 (four CTAs), 168 (three) or 255 (two).
+constexpr int ak_blocks(int D, int G, int NT) {
+  if (NT == 1) return D / G <= 2 ? 4 : 3;
+  return D == 64 || D == G ? 3 : 2;
+}
+// First of the eight elements of a row that word w of lane tg holds, KP words at a time per lane.
+template <int KP>
+__device__ __forceinline__ int key_elem(int w, int tg) {
+  return (w / KP) * (32 * KP) + tg * (8 * KP) + (w % KP) * 8;
+}
 template <int D>
 __device__ __forceinline__ uint32_t code_off(int r, int c) {
   if constexpr (D == 64) return r * 32 + ((c ^ ((r >> 2) & 1)) << 4);
   const int k = (r >> 1) & 3;
-  return r * 64 + ((c ^ ((k >> 1) | ((k & 1) << 1))) << 4);
+  return r * 64 + ((c ^ (((k & 1) << 1) ^ ((k >> 1) * 3))) << 4);
 }
 }  // namespace
 
 // NT: groups of eight columns per CTA
 template <int D, int G, int NT>
-__global__ void __launch_bounds__(AK_THREADS) attn_kv4_kernel(const __grid_constant__ Kv4AttnParams p) {
+__global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kernel(const __grid_constant__ Kv4AttnParams p) {
   using L = KvLayout<D, G>;
   constexpr int NG = L::NG, KW = D / 32, MT = D / 16, COLS = 8 * NT;
   constexpr int UG = G / 32;                                     // 16-bit units of V per lane, token and group
+  constexpr int KP = G >= 64 ? 2 : 1;                            // words of K a lane loads at a time
   extern __shared__ uint4 smem_u4[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(smem_u4);
 
@@ -130,53 +176,90 @@ __global__ void __launch_bounds__(AK_THREADS) attn_kv4_kernel(const __grid_const
   const int t_end = min(len, t_begin + p.split_len);
   if (split > 0 && t_begin >= len) return;                       // the joining kernel knows which splits exist
 
-  // Queries as the second operand of the first product: lane (gr, tg) holds of column gr the eight elements 8 tg .. 8 tg + 7
-  // of every 32, in pairs (0,4), (1,5), (2,6), (3,7), the order in which the nibbles of a word come apart.
+  // Queries as the second operand of the first product: lane (gr, tg) holds of column gr, of every KS elements, the
+  // eight (or sixteen, where a group spans 64) that its lane of the first operand holds: element 8 x + y of the lane's run
+  // in the order (0,4), (1,5), (2,6), (3,7) in which the nibbles of a word come apart.
   uint32_t qf[NT][KW][4];
   float sq[NT][NG][2];                                           // sum of q over a group, columns 2 tg and 2 tg + 1
+  float s0[NT][NG][2];                                           // - sum of off q
+  float ce[NT][2];                                               // c times the power of two q was divided by
   int lim[NT][2];                                                // tokens that column sees
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int col = col0 + nt * 8 + gr;
-    float s[NG];
-#pragma unroll
-    for (int j = 0; j < NG; ++j) s[j] = 0.f;
     const bool ok = col < columns;
     const int qi = ok ? col / p.g : 0, hh = ok ? col - qi * p.g : 0;
     const __nv_bfloat16* qrow = p.q + b * p.qb + qi * p.qn + static_cast<int64_t>(hk * p.g + hh) * p.qh;
+    uint4 v[KW];
+    float top = 0.f;
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (ok) v = *reinterpret_cast<const uint4*>(qrow + 32 * w + 8 * tg);
-      qf[nt][w][0] = __byte_perm(v.x, v.z, 0x5410);              // elements 0, 4
-      qf[nt][w][1] = __byte_perm(v.x, v.z, 0x7632);              // 1, 5
-      qf[nt][w][2] = __byte_perm(v.y, v.w, 0x5410);              // 2, 6
-      qf[nt][w][3] = __byte_perm(v.y, v.w, 0x7632);              // 3, 7
+      v[w] = make_uint4(0, 0, 0, 0);
+      if (ok) v[w] = *reinterpret_cast<const uint4*>(qrow + key_elem<KP>(w, tg));
+      const uint32_t x[4] = {v[w].x, v[w].y, v[w].z, v[w].w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[w * 32 / G] += bf_lo(qf[nt][w][i]) + bf_hi(qf[nt][w][i]);
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(bf_lo(x[i])), fabsf(bf_hi(x[i]))));
+    }
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    // 2^e >= top > 2^(e - 1): q / 2^e lies in [-1, 1].  (Rows of zeros and of infinities: e = 0; subnormal tops: the smallest e.)
+    const int ex = static_cast<int>(__float_as_uint(top) >> 23);
+    const int e = top == 0.f || ex == 255 ? 0 : max(ex, 1) - 126;
+    const float down = __uint_as_float(static_cast<uint32_t>(127 - e / 2) << 23), down2 = __uint_as_float(static_cast<uint32_t>(127 - (e - e / 2)) << 23);
+    float ss[NG], so[NG];
+#pragma unroll
+    for (int j = 0; j < NG; ++j) ss[j] = so[j] = 0.f;
+#pragma unroll
+    for (int w = 0; w < KW; ++w) {
+      const uint32_t x[4] = {v[w].x, v[w].y, v[w].z, v[w].w};
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        y[2 * i] = bf_lo(x[i]) * down * down2;
+        y[2 * i + 1] = bf_hi(x[i]) * down * down2;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const __half2 h = __floats2half2_rn(y[i], y[i + 4]);
+        qf[nt][w][i] = *reinterpret_cast<const uint32_t*>(&h);
+        const float two = __low2float(h) + __high2float(h);
+        ss[w * 32 / G] += two;
+        so[w * 32 / G] += two * (i & 1 ? -64.f : -1024.f);
+      }
     }
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
-      s[j] += __shfl_xor_sync(0xffffffffu, s[j], 1);
-      s[j] += __shfl_xor_sync(0xffffffffu, s[j], 2);
-      sq[nt][j][0] = __shfl_sync(0xffffffffu, s[j], 8 * tg);
-      sq[nt][j][1] = __shfl_sync(0xffffffffu, s[j], 8 * tg + 4);
+#pragma unroll
+      for (int d = 1; d < 4; d <<= 1) {
+        ss[j] += __shfl_xor_sync(0xffffffffu, ss[j], d);
+        so[j] += __shfl_xor_sync(0xffffffffu, so[j], d);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        sq[nt][j][i] = __shfl_sync(0xffffffffu, ss[j], 8 * tg + 4 * i);
+        s0[nt][j][i] = __shfl_sync(0xffffffffu, so[j], 8 * tg + 4 * i);
+      }
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int cc = col0 + nt * 8 + 2 * tg + i;
       lim[nt][i] = cc < columns ? len - (p.n - 1) + cc / p.g : 0;
+      const int ee = __shfl_sync(0xffffffffu, e, 8 * tg + 4 * i);
+      ce[nt][i] = p.c * __uint_as_float(static_cast<uint32_t>(127 + ee / 2) << 23) * __uint_as_float(static_cast<uint32_t>(127 + ee - ee / 2) << 23);
     }
   }
 
-  float o[NT][MT][4], m[NT][2], l[NT][2], z[NT][NG][2];
+  float o[NT][MT][4], mneg[NT][2], thr[NT][2], l[NT][2], z[NT][NG][2], ws[NT][NG][4];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
     for (int i = 0; i < MT; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
 #pragma unroll
+    for (int j = 0; j < NG; ++j) ws[nt][j][0] = ws[nt][j][1] = ws[nt][j][2] = ws[nt][j][3] = 0.f;
+#pragma unroll
     for (int i = 0; i < 2; ++i) {
-      m[nt][i] = -INFINITY;
+      mneg[nt][i] = INFINITY;                                    // minus the reference, in binades; none yet
+      thr[nt][i] = -INFINITY;                                    // the score (before ce) from which it has to be raised
       l[nt][i] = 0.f;
 #pragma unroll
       for (int j = 0; j < NG; ++j) z[nt][j][i] = 0.f;
@@ -185,12 +268,20 @@ __global__ void __launch_bounds__(AK_THREADS) attn_kv4_kernel(const __grid_const
 
   const int tiles = t_end > t_begin ? (t_end - t_begin + AK_TILE - 1) / AK_TILE : 0;
   const int mine = tiles > warp ? (tiles - warp + AK_WARPS - 1) / AK_WARPS : 0;      // tiles warp, warp + 4, ...
-  uint8_t* ring = smem + warp * L::RING;
-  const uint32_t ring_a = smem_u32(ring);
+  const uint32_t ring_a = smem_u32(smem + warp * L::RING);
   const int* trow = p.table + b * p.table_stride;
   const int page_mask = (1 << p.page_shift) - 1;
+  const bool one_page = p.page_shift >= 5;                       // a tile of 32 tokens lies in one page, else in two
 
-  // Page numbers of 16 tiles at a time, two per tile (a tile of 32 tokens is two pages of 16 at worst), one per lane.
+  // 16-byte chunks of codes a lane copies of each half tile, and where they go
+  constexpr int CH = L::ROW / 16, N = 16 * CH, IT = (N + 31) / 32, PN = NG * 4;
+  uint32_t soff[IT];
+#pragma unroll
+  for (int k = 0; k < IT; ++k) {
+    const int x = k * 32 + lane, r = x / CH;
+    soff[k] = code_off<D>(r, x - r * CH);
+  }
+  // Page numbers of 16 tiles at a time, two per tile, one per lane.
   int pages = 0;
   auto fetch_pages = [&](int i) {
     const int tok = t_begin + (warp + AK_WARPS * (i + (lane >> 1))) * AK_TILE + (lane & 1) * 16;
@@ -203,92 +294,112 @@ __global__ void __launch_bounds__(AK_THREADS) attn_kv4_kernel(const __grid_const
       }
     }
   };
+  const uint32_t poff = (lane & 15) * 16 + (lane < 16 ? 0 : L::PARAMS);
+  // half 0 or 1 of the tile at shared address st from row `row` of the cache
+  auto copy_half = [&](auto half_c, uint32_t st, int64_t row) {
+    constexpr int H = decltype(half_c)::value;
+    const uint8_t* ks = p.k_codes + row * L::ROW + lane * 16;
+    const uint8_t* vs = p.v_codes + row * L::ROW + lane * 16;
+    each<IT>([&](auto k) {
+      if (N % 32 == 0 || k * 32 + lane < N) {
+        cp_async16<H * 16 * L::PITCH, k * 512>(st + soff[k], ks);
+        cp_async16<H * 16 * L::PITCH + L::CODES, k * 512>(st + soff[k], vs);
+      }
+    });
+    if ((lane & 15) < PN) {
+      const uint8_t* src = reinterpret_cast<const uint8_t*>((lane < 16 ? p.k_params : p.v_params) + row * NG) + (lane & 15) * 16;
+      cp_async16<2 * L::CODES + H * (16 * NG * 4), 0>(st + poff, src);
+    }
+  };
+  uint32_t st_in = ring_a;                                       // the stage the next copy goes to
   auto issue = [&](int i) {
     if (i < mine) {
       if ((i & 15) == 0) fetch_pages(i);
       const int t0 = t_begin + (warp + AK_WARPS * i) * AK_TILE;
-      const uint32_t st = ring_a + (i % AK_STAGES) * L::STAGE;
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int page = __shfl_sync(0xffffffffu, pages, 2 * (i & 15) + half);
-        const int tok = t0 + half * 16;
-        if (tok < t_end) {
-          const int64_t row = ((static_cast<int64_t>(page) * p.Hk + hk) << p.page_shift) + (tok & page_mask);
-          constexpr int CH = L::ROW / 16, N = 16 * CH;           // 16-byte chunks per token, per half tile
-          const uint8_t* ks = p.k_codes + row * L::ROW;
-          const uint8_t* vs = p.v_codes + row * L::ROW;
-#pragma unroll
-          for (int x0 = 0; x0 < N; x0 += 32) {
-            const int x = x0 + lane;
-            if (N % 32 == 0 || x < N) {
-              const int r = x / CH, c = x - r * CH;
-              const uint32_t off = code_off<D>(half * 16 + r, c);
-              cp_async16(st + off, ks + x * 16);
-              cp_async16(st + L::CODES + off, vs + x * 16);
-            }
-          }
-          constexpr int PN = 16 * NG * 4 / 16;                   // chunks of parameters: 4 to 16
-          if (lane < PN) cp_async16(st + 2 * L::CODES + half * (16 * NG * 4) + lane * 16, reinterpret_cast<const uint8_t*>(p.k_params + row * NG) + lane * 16);
-          else if (lane >= 16 && lane - 16 < PN)
-            cp_async16(st + 2 * L::CODES + L::PARAMS + half * (16 * NG * 4) + (lane - 16) * 16, reinterpret_cast<const uint8_t*>(p.v_params + row * NG) + (lane - 16) * 16);
-        }
-      }
+      const int pa = __shfl_sync(0xffffffffu, pages, 2 * (i & 15)), pb = __shfl_sync(0xffffffffu, pages, 2 * (i & 15) + 1);
+      const int64_t row = ((static_cast<int64_t>(pa) * p.Hk + hk) << p.page_shift) + (t0 & page_mask);
+      copy_half(std::integral_constant<int, 0>{}, st_in, row);
+      if (t0 + 16 < t_end)
+        copy_half(std::integral_constant<int, 1>{}, st_in, one_page ? row + 16 : (static_cast<int64_t>(pb) * p.Hk + hk) << p.page_shift);
     }
     cp_commit();
+    st_in += L::STAGE;
+    if (st_in == ring_a + L::RING) st_in = ring_a;
   };
 
 #pragma unroll
   for (int i = 0; i < AK_STAGES - 1; ++i) issue(i);
 
-  for (int i = 0; i < mine; ++i) {
-    cp_wait<AK_STAGES - 2>();
-    __syncwarp();
+  // Row r of a 16-row operand is token perm(r) = r / 2 (r even), 4 + r / 2 (r odd), + 8 above
+  const int pr = (gr >> 1) + ((gr & 1) << 2);
+  uint32_t koff[KW / KP], voff[NG][2];                           // where a lane's codes lie in the first rows of a tile
+#pragma unroll
+  for (int w = 0; w < KW / KP; ++w) koff[w] = code_off<D>(pr, (w * KP * 16 + tg * KP * 4) >> 4) + ((w * KP * 16 + tg * KP * 4) & 15);
+#pragma unroll
+  for (int j = 0; j < NG; ++j) {
+    const int byte = j * (G / 2) + gr * (G / 16);
+    voff[j][0] = code_off<D>(tg, byte >> 4) + (byte & 15);
+    voff[j][1] = code_off<D>(tg + 4, byte >> 4) + (byte & 15);   // rows 4 and 12 apart have another key, rows 8 and 16 apart the same
+  }
+  // One tile: scores, reference, probabilities, second product.  EDGE: some column may not see all of it (the columns'
+  // limits lie within n of the sequence's end; padding columns see nothing and are left as they come: nobody reads them).
+  auto tile = [&](auto edge_c, int i, uint32_t kc) {
+    constexpr bool EDGE = decltype(edge_c)::value;
     const int t0 = t_begin + (warp + AK_WARPS * i) * AK_TILE;
-    const uint32_t kc = ring_a + (i % AK_STAGES) * L::STAGE, vc = kc + L::CODES, kp = vc + L::CODES, vp = kp + L::PARAMS;
-
-    // ---- scores of 32 tokens.  Row r of a 16-row operand is token perm(r) = r / 2 (r even), 4 + r / 2 (r odd), + 8 above
-    const int pr = (gr >> 1) + ((gr & 1) << 2);
+    const uint32_t kp = kc + pr * NG * 4;
     float s[2][NT][4];
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
-      const int ta = mt * 16 + pr;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) s[mt][nt][0] = s[mt][nt][1] = s[mt][nt][2] = s[mt][nt][3] = 0.f;
-#pragma unroll
-      for (int j = 0; j < NG; ++j) {
+    each<2>([&](auto mt_c) {
+      constexpr int mt = decltype(mt_c)::value;
+      each<NG>([&](auto j_c) {
+        constexpr int j = decltype(j_c)::value;
         float acc[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          acc[nt][0] = acc[nt][2] = -16.f * sq[nt][j][0];
-          acc[nt][1] = acc[nt][3] = -16.f * sq[nt][j][1];
+          acc[nt][0] = acc[nt][2] = s0[nt][j][0];
+          acc[nt][1] = acc[nt][3] = s0[nt][j][1];
         }
 #pragma unroll
-        for (int w = j * (G / 32); w < (j + 1) * (G / 32); ++w) {
-          const uint32_t ka = lds32(kc + code_off<D>(ta, w) + tg * 4), kb = lds32(kc + code_off<D>(ta + 8, w) + tg * 4);
-          const uint32_t a0 = nib<0>(ka), a1 = nib<0>(kb), a2 = nib<1>(ka), a3 = nib<1>(kb);
-          const uint32_t c0 = nib<2>(ka), c1 = nib<2>(kb), c2 = nib<3>(ka), c3 = nib<3>(kb);
+        for (int w0 = j * (G / 32); w0 < (j + 1) * (G / 32); w0 += KP) {
+          uint32_t ka[KP], kb[KP];
+          const uint32_t aa = kc + koff[w0 / KP];                // 8 rows further down: the same key
+          constexpr int ra = mt * 16 * L::PITCH, rb = ra + 8 * L::PITCH;
+          if constexpr (KP == 2) {
+            const uint2 x = lds64<ra>(aa), y = lds64<rb>(aa);
+            ka[0] = x.x; ka[1] = x.y; kb[0] = y.x; kb[1] = y.y;
+          } else {
+            ka[0] = lds32<ra>(aa);
+            kb[0] = lds32<rb>(aa);
+          }
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            mma_bf16(acc[nt], a0, a1, a2, a3, qf[nt][w][0], qf[nt][w][1]);
-            mma_bf16(acc[nt], c0, c1, c2, c3, qf[nt][w][2], qf[nt][w][3]);
+          for (int x = 0; x < KP; ++x) {
+            const uint32_t ah = ka[x] >> 8, bh8 = kb[x] >> 8;
+            const uint32_t a0 = nib_h0(ka[x]), a1 = nib_h0(kb[x]), a2 = nib_h1(ka[x]), a3 = nib_h1(kb[x]);
+            const uint32_t c0 = nib_h0(ah), c1 = nib_h0(bh8), c2 = nib_h1(ah), c3 = nib_h1(bh8);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              mma_f16(acc[nt], a0, a1, a2, a3, qf[nt][w0 + x][0], qf[nt][w0 + x][1]);
+              mma_f16(acc[nt], c0, c1, c2, c3, qf[nt][w0 + x][2], qf[nt][w0 + x][3]);
+            }
           }
         }
-        const uint32_t pa = lds32(kp + (ta * NG + j) * 4), pb = lds32(kp + ((ta + 8) * NG + j) * 4);
+        constexpr int po = 2 * L::CODES + (mt * 16 * NG + j) * 4;
+        const uint32_t pa = lds32<po>(kp), pb = lds32<po + 8 * NG * 4>(kp);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          s[mt][nt][0] = fmaf(bf_hi(pa), acc[nt][0], fmaf(bf_lo(pa), sq[nt][j][0], s[mt][nt][0]));
-          s[mt][nt][1] = fmaf(bf_hi(pa), acc[nt][1], fmaf(bf_lo(pa), sq[nt][j][1], s[mt][nt][1]));
-          s[mt][nt][2] = fmaf(bf_hi(pb), acc[nt][2], fmaf(bf_lo(pb), sq[nt][j][0], s[mt][nt][2]));
-          s[mt][nt][3] = fmaf(bf_hi(pb), acc[nt][3], fmaf(bf_lo(pb), sq[nt][j][1], s[mt][nt][3]));
+          if (j == 0) {
+            s[mt][nt][0] = fmaf(bf_hi(pa), acc[nt][0], bf_lo(pa) * sq[nt][j][0]);
+            s[mt][nt][1] = fmaf(bf_hi(pa), acc[nt][1], bf_lo(pa) * sq[nt][j][1]);
+            s[mt][nt][2] = fmaf(bf_hi(pb), acc[nt][2], bf_lo(pb) * sq[nt][j][0]);
+            s[mt][nt][3] = fmaf(bf_hi(pb), acc[nt][3], bf_lo(pb) * sq[nt][j][1]);
+          } else {
+            s[mt][nt][0] = fmaf(bf_hi(pa), acc[nt][0], fmaf(bf_lo(pa), sq[nt][j][0], s[mt][nt][0]));
+            s[mt][nt][1] = fmaf(bf_hi(pa), acc[nt][1], fmaf(bf_lo(pa), sq[nt][j][1], s[mt][nt][1]));
+            s[mt][nt][2] = fmaf(bf_hi(pb), acc[nt][2], fmaf(bf_lo(pb), sq[nt][j][0], s[mt][nt][2]));
+            s[mt][nt][3] = fmaf(bf_hi(pb), acc[nt][3], fmaf(bf_lo(pb), sq[nt][j][1], s[mt][nt][3]));
+          }
         }
-      }
-    }
-    // Some column may not see all of this tile: the columns' limits lie within n of the sequence's end, padding columns
-    // see nothing and are left as they come (nobody reads them).
-    const bool edge = t0 + AK_TILE > len - (p.n - 1) || t0 + AK_TILE > t_end;
-    if (edge) {
-#pragma unroll
-      for (int mt = 0; mt < 2; ++mt) {
+      });
+      if constexpr (EDGE) {
         const int ta = t0 + mt * 16 + pr;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -299,31 +410,36 @@ __global__ void __launch_bounds__(AK_THREADS) attn_kv4_kernel(const __grid_const
           }
         }
       }
-    }
+    });
     // ---- the reference of the exponentials
     bool over = false;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float mx = fmaxf(fmaxf(s[0][nt][e], s[0][nt][e + 2]), fmaxf(s[1][nt][e], s[1][nt][e + 2]));
-        over |= mx * p.c > m[nt][e] + AK_RAISE;
-      }
+      for (int e = 0; e < 2; ++e)
+        over |= fmaxf(fmaxf(s[0][nt][e], s[0][nt][e + 2]), fmaxf(s[1][nt][e], s[1][nt][e + 2])) > thr[nt][e];
     }
     if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float mx = fmaxf(fmaxf(s[0][nt][e], s[0][nt][e + 2]), fmaxf(s[1][nt][e], s[1][nt][e + 2])) * p.c;
+          float mx = fmaxf(fmaxf(s[0][nt][e], s[0][nt][e + 2]), fmaxf(s[1][nt][e], s[1][nt][e + 2]));
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-          const float mn = fmaxf(m[nt][e], mx);
-          const float f = m[nt][e] == mn ? 1.f : ak_ex2(m[nt][e] - mn);      // 0 from the initial minus infinity
-          m[nt][e] = mn;
+          const float mo = -mneg[nt][e], mn = fmaxf(mo, mx * ce[nt][e]);
+          const float f = mo == mn ? 1.f : ak_ex2(mo - mn);      // 0 from the initial minus infinity
+          if (mo != mn) {
+            mneg[nt][e] = -mn;
+            thr[nt][e] = mx + AK_RAISE / ce[nt][e];
+          }
           l[nt][e] *= f;
 #pragma unroll
-          for (int j = 0; j < NG; ++j) z[nt][j][e] *= f;
+          for (int j = 0; j < NG; ++j) {
+            z[nt][j][e] *= f;
+            ws[nt][j][e] *= f;
+            ws[nt][j][e + 2] *= f;
+          }
 #pragma unroll
           for (int k = 0; k < MT; ++k) {
             o[nt][k][e] *= f;
@@ -333,73 +449,86 @@ __global__ void __launch_bounds__(AK_THREADS) attn_kv4_kernel(const __grid_const
       }
     }
     // ---- probabilities and the second product, 16 tokens at a time
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
-      const int ta = mt * 16 + pr;
+    each<2>([&](auto mt_c) {
+      constexpr int mt = decltype(mt_c)::value;
       float pw[NT][4];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const float r0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], r1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
-        pw[nt][0] = ak_ex2(fmaf(s[mt][nt][0], p.c, -r0));
-        pw[nt][1] = ak_ex2(fmaf(s[mt][nt][1], p.c, -r1));
-        pw[nt][2] = ak_ex2(fmaf(s[mt][nt][2], p.c, -r0));
-        pw[nt][3] = ak_ex2(fmaf(s[mt][nt][3], p.c, -r1));
+        pw[nt][0] = ak_ex2(fmaf(s[mt][nt][0], ce[nt][0], mneg[nt][0]));
+        pw[nt][1] = ak_ex2(fmaf(s[mt][nt][1], ce[nt][1], mneg[nt][1]));
+        pw[nt][2] = ak_ex2(fmaf(s[mt][nt][2], ce[nt][0], mneg[nt][0]));
+        pw[nt][3] = ak_ex2(fmaf(s[mt][nt][3], ce[nt][1], mneg[nt][1]));
+        if constexpr (EDGE) {                                    // (a column that has seen nothing yet has no reference)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (s[mt][nt][e] == -INFINITY) pw[nt][e] = 0.f;
+        }
         l[nt][0] += pw[nt][0] + pw[nt][2];
         l[nt][1] += pw[nt][1] + pw[nt][3];
       }
-#pragma unroll
-      for (int j = 0; j < NG; ++j) {
-        const uint32_t pa = lds32(vp + (ta * NG + j) * 4), pb = lds32(vp + ((ta + 8) * NG + j) * 4);
-        const float ma = fmaf(7.5f, bf_hi(pa), bf_lo(pa)), mb = fmaf(7.5f, bf_hi(pb), bf_lo(pb));     // the middle of a group's range
+      each<NG>([&](auto j_c) {
+        constexpr int j = decltype(j_c)::value;
+        constexpr int po = 2 * L::CODES + L::PARAMS + (mt * 16 * NG + j) * 4;
+        const uint32_t pa = lds32<po>(kp), pb = lds32<po + 8 * NG * 4>(kp);
+        const float sa = bf_hi(pa), sb = bf_hi(pb);
+        const float ma = fmaf(7.5f, sa, bf_lo(pa)), mb = fmaf(7.5f, sb, bf_lo(pb));     // the middle of a group's range
         uint32_t bf[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          float x0 = pw[nt][0] * bf_hi(pa), x1 = pw[nt][1] * bf_hi(pa), x2 = pw[nt][2] * bf_hi(pb), x3 = pw[nt][3] * bf_hi(pb);
-          float y0 = pw[nt][0] * ma, y1 = pw[nt][1] * ma, y2 = pw[nt][2] * mb, y3 = pw[nt][3] * mb;
-          if (edge) {                                            // a weight of zero hides whatever the cache holds there
-            if (s[mt][nt][0] == -INFINITY) x0 = y0 = 0.f;
-            if (s[mt][nt][1] == -INFINITY) x1 = y1 = 0.f;
-            if (s[mt][nt][2] == -INFINITY) x2 = y2 = 0.f;
-            if (s[mt][nt][3] == -INFINITY) x3 = y3 = 0.f;
+          float x0 = pw[nt][0] * sa, x1 = pw[nt][1] * sa, x2 = pw[nt][2] * sb, x3 = pw[nt][3] * sb;
+          if constexpr (EDGE) {                                  // a weight of zero hides whatever the cache holds there
+            const bool h0 = s[mt][nt][0] == -INFINITY, h1 = s[mt][nt][1] == -INFINITY, h2 = s[mt][nt][2] == -INFINITY, h3 = s[mt][nt][3] == -INFINITY;
+            x0 = h0 ? 0.f : x0;
+            x1 = h1 ? 0.f : x1;
+            x2 = h2 ? 0.f : x2;
+            x3 = h3 ? 0.f : x3;
+            z[nt][j][0] += (h0 ? 0.f : pw[nt][0] * ma) + (h2 ? 0.f : pw[nt][2] * mb);
+            z[nt][j][1] += (h1 ? 0.f : pw[nt][1] * ma) + (h3 ? 0.f : pw[nt][3] * mb);
+          } else {
+            z[nt][j][0] = fmaf(pw[nt][0], ma, fmaf(pw[nt][2], mb, z[nt][j][0]));
+            z[nt][j][1] = fmaf(pw[nt][1], ma, fmaf(pw[nt][3], mb, z[nt][j][1]));
           }
-          const uint32_t ua = pack_bf16(x0, x1), ub = pack_bf16(x2, x3);
-          z[nt][j][0] += fmaf(-23.5f, bf_lo(ua) + bf_lo(ub), y0 + y2);
-          z[nt][j][1] += fmaf(-23.5f, bf_hi(ua) + bf_hi(ub), y1 + y3);
-          bf[nt][0] = transpose8x8(ua);
-          bf[nt][1] = transpose8x8(ub);
+          bf[nt][0] = transpose8x8(pack_bf16(x0, x1));
+          bf[nt][1] = transpose8x8(pack_bf16(x2, x3));
+          mma_bf16(ws[nt][j], 0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u, bf[nt][0], bf[nt][1]);
         }
-        // lane (gr, tg): tokens tg, tg + 4, tg + 8, tg + 12 of the 16; elements j G + gr G / 8 + 4 u + nibble
-        const int tv = mt * 16 + tg;
+        // lane (gr, tg): tokens tg, tg + 4, tg + 8, tg + 12 of the 16; elements j G + gr G / 8 + 2 byte + nibble
         uint32_t vw[4][(UG + 1) / 2];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int byte = j * (G / 2) + gr * (G / 16);
-          const uint32_t a = vc + code_off<D>(tv + 4 * k, byte >> 4) + (byte & 15);
-          if constexpr (UG == 1) vw[k][0] = lds16(a);
-          if constexpr (UG == 2) vw[k][0] = lds32(a);
+        each<4>([&](auto k) {
+          const uint32_t a = kc + voff[j][k & 1];
+          constexpr int ro = L::CODES + (mt * 16 + (k & 2) * 4) * L::PITCH;
+          if constexpr (UG == 1) vw[k][0] = lds16<ro>(a);
+          if constexpr (UG == 2) vw[k][0] = lds32<ro>(a);
           if constexpr (UG == 4) {
-            const uint2 t = lds64(a);
+            const uint2 t = lds64<ro>(a);
             vw[k][0] = t.x;
             vw[k][1] = t.y;
           }
-        }
+        });
 #pragma unroll
-        for (int u = 0; u < UG; ++u) {
-          const uint32_t sel = (u & 1) ? 0x7632u : 0x5410u;
-          const uint32_t x = __byte_perm(vw[0][u >> 1], vw[1][u >> 1], sel), y = __byte_perm(vw[2][u >> 1], vw[3][u >> 1], sel);
-          const uint32_t a0 = nib<0>(x), a1 = nib<1>(x), a2 = nib<0>(y), a3 = nib<1>(y);
-          const uint32_t c0 = nib<2>(x), c1 = nib<3>(x), c2 = nib<2>(y), c3 = nib<3>(y);
-          const int k = (j * UG + u) * 2;
+        for (int u = 0; u < 2 * UG; ++u) {
+          // byte u of the lane's run, of tokens (0, 1) and (2, 3) of its four
+          const uint32_t sel = 0x0400u | ((u & 3) * 0x1111u);
+          const uint32_t x = __byte_perm(vw[0][u >> 2], vw[1][u >> 2], sel), y = __byte_perm(vw[2][u >> 2], vw[3][u >> 2], sel);
+          const uint32_t a0 = nib_b0(x), a1 = nib_b1(x), a2 = nib_b0(y), a3 = nib_b1(y);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            mma_bf16(o[nt][k], a0, a1, a2, a3, bf[nt][0], bf[nt][1]);
-            mma_bf16(o[nt][k + 1], c0, c1, c2, c3, bf[nt][0], bf[nt][1]);
-          }
+          for (int nt = 0; nt < NT; ++nt) mma_bf16(o[nt][j * 2 * UG + u], a0, a1, a2, a3, bf[nt][0], bf[nt][1]);
         }
-      }
-    }
+      });
+    });
+  };
+
+  uint32_t st_out = ring_a;                                      // the stage the next tile is read from
+  for (int i = 0; i < mine; ++i) {
+    cp_wait<AK_STAGES - 2>();
+    __syncwarp();
+    const int t_next = t_begin + (warp + AK_WARPS * i) * AK_TILE + AK_TILE;
+    if (t_next > len - (p.n - 1) || t_next > t_end) tile(std::true_type{}, i, st_out);
+    else tile(std::false_type{}, i, st_out);
     __syncwarp();
     issue(i + AK_STAGES - 1);
+    st_out += L::STAGE;
+    if (st_out == ring_a + L::RING) st_out = ring_a;
   }
   cp_wait<0>();
 
@@ -432,12 +561,13 @@ __global__ void __launch_bounds__(AK_THREADS) attn_kv4_kernel(const __grid_const
 #pragma unroll
         for (int u = 0; u < UG; ++u) {
           const int k = (j * UG + u) * 2;
+          const float even = fmaf(-135.5f, ws[nt][j][e], z[nt][j][e]), odd = fmaf(-23.5f, ws[nt][j][e], z[nt][j][e]);
           *reinterpret_cast<float4*>(row + j * G + gr * (G / 8) + 4 * u) =
-              make_float4(o[nt][k][e] + z[nt][j][e], o[nt][k][e + 2] + z[nt][j][e], o[nt][k + 1][e] + z[nt][j][e], o[nt][k + 1][e + 2] + z[nt][j][e]);
+              make_float4(o[nt][k][e] + even, o[nt][k][e + 2] + odd, o[nt][k + 1][e] + even, o[nt][k + 1][e + 2] + odd);
         }
       }
       if (gr == 0) {
-        s_m[warp * COLS + col] = m[nt][e];
+        s_m[warp * COLS + col] = -mneg[nt][e];
         s_l[warp * COLS + col] = l[nt][e];
       }
     }
@@ -551,7 +681,7 @@ cudaError_t ak_cols(const Kv4AttnParams& p, cudaStream_t s) {
 }
 }  // namespace
 
-int attn_kv4_resident(int head_dim, int group, int cols) { return cols == 8 ? 4 : 3; }
+int attn_kv4_resident(int head_dim, int group, int cols) { return ak_blocks(head_dim, group, cols / 8); }
 
 cudaError_t launch_attn_kv4(const Kv4AttnParams& p, int D, int G, int num_sms, cudaStream_t s) {
   if (D == 64) return G == 32 ? ak_cols<64, 32>(p, s) : ak_cols<64, 64>(p, s);
