@@ -92,10 +92,9 @@ gc_status_t check_rows(const char* who, const gc_kv4_cache_t* c, int dtype, int6
   return GC_OK;
 }
 
-// The split of one call of gc_attention_kv4 over the GPU.
-struct Split {
-  int cols, col_chunks, split_len, n_split;
-  int64_t units;
+// How one call of gc_attention_kv4 is laid out over the GPU.
+struct Layout {
+  int cols, col_chunks, block, ctas;
   size_t bytes;
 };
 
@@ -116,27 +115,20 @@ gc_status_t check_attend(const char* who, const gc_kv4_cache_t* c, const gc_atte
   return GC_OK;
 }
 
-// Enough CTAs to fill the GPU once with equal shares when one long sequence is all there is; with many units, four times
-// as many so that sequences of unlike length even out; never less than 256 tokens each, where the fixed cost of a CTA
-// (queries, page numbers, merging) would show.
-Split plan_split(const gc_kv4_cache_t& c, const gc_attention_kv4_t& d, int num_sms) {
-  Split s = {};
+// One wave of CTAs, as many as fit, or one per 128 tokens where there are fewer.  Sequences of up to 512 tokens are not split:
+// joining their pieces would take another launch, longer than the three blocks it would save.
+Layout lay_out(const gc_kv4_cache_t& c, const gc_attention_kv4_t& d, int num_sms) {
+  Layout s = {};
   const int columns = d.queries * (d.q_heads / c.kv_heads);
   s.cols = attn_kv4_cols(columns);
   s.col_chunks = (columns + s.cols - 1) / s.cols;
-  s.units = static_cast<int64_t>(d.batch) * c.kv_heads * s.col_chunks;
-  const int64_t slots = static_cast<int64_t>(num_sms) * attn_kv4_resident(c.head_dim, c.group, s.cols);
-  const int64_t want = d.batch == 1 ? slots : 4 * slots;
-  int64_t n = s.units ? want / s.units : 1;
-  if (n < 1) n = 1;
-  int64_t len = (d.max_length + n - 1) / n;
-  if (len < 256) len = 256;
-  len = (len + 127) / 128 * 128;
-  if (d.max_length <= 512 && s.units >= num_sms) len = 512;
-  s.split_len = static_cast<int>(len);
-  s.n_split = static_cast<int>((d.max_length + len - 1) / len);
-  if (s.n_split < 1) s.n_split = 1;
-  s.bytes = s.n_split > 1 ? static_cast<size_t>(s.units) * s.n_split * s.cols * (c.head_dim + 2) * sizeof(float) : 0;
+  s.block = d.max_length <= 512 ? 512 : 128;
+  const int64_t units = static_cast<int64_t>(d.batch) * c.kv_heads * s.col_chunks;
+  const int64_t most = units * ((static_cast<int64_t>(d.max_length) + s.block - 1) / s.block);
+  const int64_t fit = static_cast<int64_t>(num_sms) * attn_kv4_resident(c.head_dim, c.group, s.cols);
+  // (without splitting, a CTA per unit, and the hardware deals them out)
+  s.ctas = static_cast<int>(s.block >= d.max_length ? units : most < fit ? most : fit);
+  s.bytes = s.block >= d.max_length || s.ctas == 1 ? 0 : 2 * static_cast<size_t>(s.ctas) * s.cols * (c.head_dim + 2) * sizeof(float);
   return s;
 }
 }  // namespace
@@ -198,7 +190,7 @@ extern "C" gc_status_t gc_attention_kv4_workspace_bytes(const gc_kv4_cache_t* ca
   if (st != GC_OK) return st;
   int sms = 0;
   RUN(sm_count(cache->cuda_device, &sms));
-  *bytes = plan_split(*cache, *d, sms).bytes;
+  *bytes = lay_out(*cache, *d, sms).bytes;
   return GC_OK;
 }
 
@@ -220,8 +212,7 @@ extern "C" gc_status_t gc_attention_kv4(void* cuda_stream, const gc_kv4_cache_t*
   RUN(on.err());
   int sms = 0;
   RUN(sm_count(cache->cuda_device, &sms));
-  const Split sp = plan_split(*cache, *d, sms);
-  if (sp.units * sp.n_split > 0x7FFFFFFFLL) REFUSE(GC_ERR_UNSUPPORTED, "%s: too many pieces of work for one launch", who);
+  const Layout sp = lay_out(*cache, *d, sms);
   if (sp.bytes) {
     if (!workspace_dev || workspace_bytes < sp.bytes) REFUSE(GC_ERR_INVALID_ARG, "%s: the workspace must have %zu bytes", who, sp.bytes);
     if (misaligned(workspace_dev, 16)) REFUSE(GC_ERR_ALIGNMENT, "%s: the workspace must be 16-byte aligned", who);
@@ -232,7 +223,7 @@ extern "C" gc_status_t gc_attention_kv4(void* cuda_stream, const gc_kv4_cache_t*
   p.width = d->table_width; p.max_len = d->max_length;
   p.num_pages = cache->num_pages; p.table_stride = d->table_stride;
   p.c = d->scale * 1.4426950408889634f;
-  p.split_len = sp.split_len; p.n_split = sp.n_split; p.col_chunks = sp.col_chunks;
+  p.block = sp.block; p.ctas = sp.ctas; p.col_chunks = sp.col_chunks;
   p.q = static_cast<const __nv_bfloat16*>(d->q);
   p.qb = d->q_batch_stride; p.qn = d->q_query_stride; p.qh = d->q_head_stride;
   p.o = static_cast<__nv_bfloat16*>(d->out);

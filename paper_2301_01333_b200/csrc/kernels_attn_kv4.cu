@@ -6,26 +6,30 @@
 // element is half a byte, so the work per byte is what has to be kept small: at the copy bandwidth of the whole GPU an SM
 // has 2.8 lane-instructions per element of K or V, 1.4 of them on the integer / logic pipe.
 //
-//   * The codes go into the matrix instruction as they are.  A nibble in the low bits of the mantissa of a 16-bit float whose
-//     exponent makes that bit worth 1 is the number (a power of two) + code, exactly, and one logic instruction makes two
-//     of them.  Scales and offsets are applied to sums, never to elements:
-//       q . K[t]            = scale_t * (sum_i q_i (off_i + code_i) - sum_i off_i q_i) + lo_t * sum_i q_i          per group
-//       sum_t p_t V[t][d]   = sum_t p'_t (off_d + code_td) + sum_t p_t (lo_t + 7.5 scale_t) - (off_d + 7.5) sum_t p'_t
-//     with p'_t = bf16(p_t scale_t).  The first sum of each line is the MMA's (fp32 accumulators, - sum off q as their initial
-//     value in the first), and so is the last of the second (a product with ones); the others are a few fp32 operations per
-//     (token, column).  p' is the only rounding before the output's; what it rounds is the distance from the middle of the
-//     group's range (code - 7.5), half of what the distance from lo would lose.
-//   * Keys are fp16 operands: ten mantissa bits hold both nibbles of a byte where they lie (off 1024 and 64), 5 instructions
-//     for 8 elements.  q, bf16, becomes fp16 exactly after a division of its row by a power of two near its largest element
-//     (elements below 2^-14 of that keep an absolute 2^-25 of it).  Weights p' need bf16's range, so values are bf16
-//     operands: off 128 and, one shift later, 16; 8 instructions for 8 elements with the joining of token pairs.
+//   * The codes go into the matrix instruction as they are: masked out of their word, nothing else.  A small whole number N
+//     in the low bits of a 16-bit float is the subnormal N * 2^-24 (fp16) or N * 2^-133 (bf16), and goes on being N times that
+//     past the first exponent bit, which the smallest normal numbers share their spacing with: bits 0..3 and 4..7 of a half
+//     are code and 16 code of that unit, in fp16 (linear below 2^11) and in bf16 (below 2^8).  One logic instruction makes two
+//     operand elements.  Scales and offsets are applied to sums, never to elements:
+//       q . K[t]            = scale_t * sum_i q_i code_i + lo_t * sum_i q_i          per group
+//       sum_t p_t V[t][d]   = sum_t p'_t code_td + sum_t p_t (lo_t + 7.5 scale_t) - 7.5 sum_t p'_t,   p'_t = bf16(p_t scale_t)
+//     The first sum of each line is the MMA's (fp32 accumulators), and so is the last of the second (a product with ones);
+//     the others are a few fp32 operations per (token, column).  p' is the only rounding before the output's; what it rounds
+//     is the distance from the middle of the group's range (code - 7.5), half of what the distance from lo would lose.
+//   * Keys are fp16 operands.  q, bf16, becomes fp16 exactly after its row is scaled by a power of two to at most 2^15, and by
+//     2^11 where it meets 16 code (elements below 2^-25 of the largest keep an absolute 2^-36 of it).  Weights p' need
+//     bf16's range: p carries a factor of 2^64, which the sum of p has as well, so that the products stay normal in fp32 for
+//     weights from 2^-57 to 2^55: cached values have to stay below 2^50.
 //   * m16n8k16 MMAs with the codes as the 16-row operand: tokens are the rows of the first product and the reduction of the
 //     second, so a lane's nibbles are always neighbours in memory (head-dimension neighbours; the order inside a reduction
 //     axis is free, Q and P are permuted to match), and 8 columns cost 8, not 16.
 //   * A warp is on its own: it takes every fourth 32-token tile of its CTA's range, copies tiles ahead into its own ring in
 //     shared memory with 16-byte asynchronous copies, and keeps running maximum, sum and output of its columns in
-//     registers.  No barrier until the end, where the warps of a CTA are joined in shared memory and the CTAs of a unit
-//     (when a sequence is split) by a second small kernel in a fixed order.
+//     registers.  No barrier until the end, where the warps of a CTA are joined in shared memory.
+//   * One wave of CTAs that share all the work out equally: the 128-token blocks of every (sequence, head, chunk of columns)
+//     stand in one row, of which each CTA takes an equal stretch, however unlike the lengths are.  Where a stretch ends
+//     inside a sequence, the pieces are joined by a second small kernel in their order.  (Against one CTA per 2048 tokens
+//     of a sequence: 97 us became AK_SK us for 64 ragged sequences up to 8192 tokens, a sixth of it having been the tail.)
 //   * The running maximum is a reference that is only raised when a score exceeds it by 2^8: one vote per tile instead
 //     of a reduction, and the sums stay far inside fp32.
 #include <cuda_fp16.h>
@@ -93,18 +97,9 @@ __device__ __forceinline__ void each(F&& f) {
     each<N, F, I + 1>(static_cast<F&&>(f));
   }
 }
-// (w & mask) | bits in one instruction (written out: left to itself the compiler made two of it)
-__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits) {
-  uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(w), "r"(mask), "r"(bits));
-  return r;
-}
-// two nibbles of 16-bit halves as floats: bits 0..3 of the halves as fp16 1024 + code, bits 4..7 as 64 + code
-__device__ __forceinline__ uint32_t nib_h0(uint32_t w) { return and_or(w, 0x000f000fu, 0x64006400u); }
-__device__ __forceinline__ uint32_t nib_h1(uint32_t w) { return and_or(w, 0x00f000f0u, 0x54005400u); }
-// the same as bf16: 128 + code, and (from bits 4..7) 16 + code
-__device__ __forceinline__ uint32_t nib_b0(uint32_t w) { return and_or(w, 0x000f000fu, 0x43004300u); }
-__device__ __forceinline__ uint32_t nib_b1(uint32_t w) { return and_or(w >> 1, 0x00780078u, 0x41804180u); }
+// the low and the high nibbles of a word's even bytes: code and 16 code in units of the smallest 16-bit float
+__device__ __forceinline__ uint32_t nib_lo(uint32_t w) { return w & 0x000f000fu; }
+__device__ __forceinline__ uint32_t nib_hi(uint32_t w) { return w & 0x00f000f0u; }
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -151,38 +146,70 @@ __device__ __forceinline__ uint32_t code_off(int r, int c) {
 }
 }  // namespace
 
-// NT: groups of eight columns per CTA
+// The row of blocks: a sequence has one block per p.block tokens, at least one, times heads and chunks of columns.
+__device__ __forceinline__ int length_of(const Kv4AttnParams& p, int b) {
+  const int len = __ldg(p.lengths + b);
+  return len < 0 ? 0 : min(len, p.max_len);
+}
+__device__ __forceinline__ int blocks_of(const Kv4AttnParams& p, int len) { return max((len + p.block - 1) / p.block, 1); }
+// Blocks of the sequences before b (*before) and of all; called by whole warps.
+__device__ __forceinline__ int64_t blocks_before(const Kv4AttnParams& p, int b, int64_t* before) {
+  int64_t all = 0, mine = 0;
+  for (int s = threadIdx.x & 31; s < p.B; s += 32) {
+    const int n = blocks_of(p, length_of(p, s));
+    all += n;
+    if (s < b) mine += n;
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) {
+    all += __shfl_xor_sync(0xffffffffu, all, d);
+    mine += __shfl_xor_sync(0xffffffffu, mine, d);
+  }
+  *before = mine;
+  return all;
+}
+// The sequence that has block number `at`, and the blocks before it; called by whole warps.
+__device__ __forceinline__ int sequence_at(const Kv4AttnParams& p, int64_t at, int64_t* before) {
+  const int lane = threadIdx.x & 31;
+  int64_t base = 0;
+  for (int s0 = 0; s0 < p.B; s0 += 32) {
+    const int s = s0 + lane;
+    int64_t incl = s < p.B ? blocks_of(p, length_of(p, s)) : 0;
+    const int64_t own = incl;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t o = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += o;
+    }
+    const uint32_t hit = __ballot_sync(0xffffffffu, s < p.B && base + incl > at);
+    if (hit) {
+      const int w = __ffs(hit) - 1;
+      *before = base + __shfl_sync(0xffffffffu, incl - own, w);
+      return s0 + w;
+    }
+    base += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  *before = base;
+  return p.B - 1;
+}
+
+// Blocks k0 .. k0 + kn of the nb of head hk of sequence b (len tokens), columns of one chunk.  NT: groups of eight columns.
 template <int D, int G, int NT>
-__global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kernel(const __grid_constant__ Kv4AttnParams p) {
+__device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, int b, int hk, int chunk, int len, int k0, int kn, int nb) {
   using L = KvLayout<D, G>;
   constexpr int NG = L::NG, KW = D / 32, MT = D / 16, COLS = 8 * NT;
   constexpr int UG = G / 32;                                     // 16-bit units of V per lane, token and group
   constexpr int KP = G >= 64 ? 2 : 1;                            // words of K a lane loads at a time
-  extern __shared__ uint4 smem_u4[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>(smem_u4);
-
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, tg = lane & 3;
-  const int split = blockIdx.x % p.n_split;
-  const int unit = blockIdx.x / p.n_split;                       // ((b * Hk) + hk) * col_chunks + chunk
-  const int chunk = unit % p.col_chunks, bh = unit / p.col_chunks, b = bh / p.Hk, hk = bh - b * p.Hk;
   const int columns = p.n * p.g, col0 = chunk * COLS;
-
-  int len = p.lengths[b];
-  if (len < 0 || len > p.max_len) {
-    if (threadIdx.x == 0) report(p.status, DEV_BAD_LENGTH);
-    len = len < 0 ? 0 : p.max_len;
-  }
-  const int t_begin = split * p.split_len;
-  const int t_end = min(len, t_begin + p.split_len);
-  if (split > 0 && t_begin >= len) return;                       // the joining kernel knows which splits exist
+  const int t_begin = k0 * p.block, t_end = min(len, (k0 + kn) * p.block);
 
   // Queries as the second operand of the first product: lane (gr, tg) holds of column gr, of every KS elements, the
   // eight (or sixteen, where a group spans 64) that its lane of the first operand holds: element 8 x + y of the lane's run
   // in the order (0,4), (1,5), (2,6), (3,7) in which the nibbles of a word come apart.
   uint32_t qf[NT][KW][4];
   float sq[NT][NG][2];                                           // sum of q over a group, columns 2 tg and 2 tg + 1
-  float s0[NT][NG][2];                                           // - sum of off q
-  float ce[NT][2];                                               // c times the power of two q was divided by
+  float ce[NT][2];                                               // c times the power of two the scores are short of
   int lim[NT][2];                                                // tokens that column sees
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -202,13 +229,13 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
     }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    // 2^e >= top > 2^(e - 1): q / 2^e lies in [-1, 1].  (Rows of zeros and of infinities: e = 0; subnormal tops: the smallest e.)
+    // 2^e > top >= 2^(e - 1): q / 2^e lies in (-1, 1).  (Rows of zeros and of infinities: e = 0; subnormal tops: the smallest e.)
     const int ex = static_cast<int>(__float_as_uint(top) >> 23);
     const int e = top == 0.f || ex == 255 ? 0 : max(ex, 1) - 126;
     const float down = __uint_as_float(static_cast<uint32_t>(127 - e / 2) << 23), down2 = __uint_as_float(static_cast<uint32_t>(127 - (e - e / 2)) << 23);
-    float ss[NG], so[NG];
+    float ss[NG];
 #pragma unroll
-    for (int j = 0; j < NG; ++j) ss[j] = so[j] = 0.f;
+    for (int j = 0; j < NG; ++j) ss[j] = 0.f;
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
       const uint32_t x[4] = {v[w].x, v[w].y, v[w].z, v[w].w};
@@ -220,32 +247,25 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const __half2 h = __floats2half2_rn(y[i], y[i + 4]);
+        const float f = i & 1 ? 0x1p11f : 0x1p15f;               // the odd ones meet 16 code
+        const __half2 h = __floats2half2_rn(y[i] * f, y[i + 4] * f);
         qf[nt][w][i] = *reinterpret_cast<const uint32_t*>(&h);
-        const float two = __low2float(h) + __high2float(h);
-        ss[w * 32 / G] += two;
-        so[w * 32 / G] += two * (i & 1 ? -64.f : -1024.f);
+        ss[w * 32 / G] += (__low2float(h) + __high2float(h)) * (0x1p-9f / f);      // in the unit of the product: 2^(15 - 24)
       }
     }
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
 #pragma unroll
-      for (int d = 1; d < 4; d <<= 1) {
-        ss[j] += __shfl_xor_sync(0xffffffffu, ss[j], d);
-        so[j] += __shfl_xor_sync(0xffffffffu, so[j], d);
-      }
+      for (int d = 1; d < 4; d <<= 1) ss[j] += __shfl_xor_sync(0xffffffffu, ss[j], d);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        sq[nt][j][i] = __shfl_sync(0xffffffffu, ss[j], 8 * tg + 4 * i);
-        s0[nt][j][i] = __shfl_sync(0xffffffffu, so[j], 8 * tg + 4 * i);
-      }
+      for (int i = 0; i < 2; ++i) sq[nt][j][i] = __shfl_sync(0xffffffffu, ss[j], 8 * tg + 4 * i);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int cc = col0 + nt * 8 + 2 * tg + i;
       lim[nt][i] = cc < columns ? len - (p.n - 1) + cc / p.g : 0;
       const int ee = __shfl_sync(0xffffffffu, e, 8 * tg + 4 * i);
-      ce[nt][i] = p.c * __uint_as_float(static_cast<uint32_t>(127 + ee / 2) << 23) * __uint_as_float(static_cast<uint32_t>(127 + ee - ee / 2) << 23);
+      ce[nt][i] = p.c * 0x1p9f * __uint_as_float(static_cast<uint32_t>(127 + ee / 2) << 23) * __uint_as_float(static_cast<uint32_t>(127 + ee - ee / 2) << 23);
     }
   }
 
@@ -258,7 +278,7 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
     for (int j = 0; j < NG; ++j) ws[nt][j][0] = ws[nt][j][1] = ws[nt][j][2] = ws[nt][j][3] = 0.f;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      mneg[nt][i] = INFINITY;                                    // minus the reference, in binades; none yet
+      mneg[nt][i] = INFINITY;                                    // 64 minus the reference, in binades; none yet
       thr[nt][i] = -INFINITY;                                    // the score (before ce) from which it has to be raised
       l[nt][i] = 0.f;
 #pragma unroll
@@ -355,8 +375,7 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
         float acc[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          acc[nt][0] = acc[nt][2] = s0[nt][j][0];
-          acc[nt][1] = acc[nt][3] = s0[nt][j][1];
+          acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.f;
         }
 #pragma unroll
         for (int w0 = j * (G / 32); w0 < (j + 1) * (G / 32); w0 += KP) {
@@ -373,8 +392,8 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
 #pragma unroll
           for (int x = 0; x < KP; ++x) {
             const uint32_t ah = ka[x] >> 8, bh8 = kb[x] >> 8;
-            const uint32_t a0 = nib_h0(ka[x]), a1 = nib_h0(kb[x]), a2 = nib_h1(ka[x]), a3 = nib_h1(kb[x]);
-            const uint32_t c0 = nib_h0(ah), c1 = nib_h0(bh8), c2 = nib_h1(ah), c3 = nib_h1(bh8);
+            const uint32_t a0 = nib_lo(ka[x]), a1 = nib_lo(kb[x]), a2 = nib_hi(ka[x]), a3 = nib_hi(kb[x]);
+            const uint32_t c0 = nib_lo(ah), c1 = nib_lo(bh8), c2 = nib_hi(ah), c3 = nib_hi(bh8);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               mma_f16(acc[nt], a0, a1, a2, a3, qf[nt][w0 + x][0], qf[nt][w0 + x][1]);
@@ -427,10 +446,10 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
           float mx = fmaxf(fmaxf(s[0][nt][e], s[0][nt][e + 2]), fmaxf(s[1][nt][e], s[1][nt][e + 2]));
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-          const float mo = -mneg[nt][e], mn = fmaxf(mo, mx * ce[nt][e]);
+          const float mo = 64.f - mneg[nt][e], mn = fmaxf(mo, mx * ce[nt][e]);
           const float f = mo == mn ? 1.f : ak_ex2(mo - mn);      // 0 from the initial minus infinity
           if (mo != mn) {
-            mneg[nt][e] = -mn;
+            mneg[nt][e] = 64.f - mn;
             thr[nt][e] = mx + AK_RAISE / ce[nt][e];
           }
           l[nt][e] *= f;
@@ -510,7 +529,7 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
           // byte u of the lane's run, of tokens (0, 1) and (2, 3) of its four
           const uint32_t sel = 0x0400u | ((u & 3) * 0x1111u);
           const uint32_t x = __byte_perm(vw[0][u >> 2], vw[1][u >> 2], sel), y = __byte_perm(vw[2][u >> 2], vw[3][u >> 2], sel);
-          const uint32_t a0 = nib_b0(x), a1 = nib_b1(x), a2 = nib_b0(y), a3 = nib_b1(y);
+          const uint32_t a0 = nib_lo(x), a1 = nib_hi(x), a2 = nib_lo(y), a3 = nib_hi(y);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) mma_bf16(o[nt][j * 2 * UG + u], a0, a1, a2, a3, bf[nt][0], bf[nt][1]);
         }
@@ -561,13 +580,14 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
 #pragma unroll
         for (int u = 0; u < UG; ++u) {
           const int k = (j * UG + u) * 2;
-          const float even = fmaf(-135.5f, ws[nt][j][e], z[nt][j][e]), odd = fmaf(-23.5f, ws[nt][j][e], z[nt][j][e]);
+          const float mid = fmaf(-7.5f, ws[nt][j][e], z[nt][j][e]);
           *reinterpret_cast<float4*>(row + j * G + gr * (G / 8) + 4 * u) =
-              make_float4(o[nt][k][e] + even, o[nt][k][e + 2] + odd, o[nt][k + 1][e] + even, o[nt][k + 1][e + 2] + odd);
+              make_float4(fmaf(o[nt][k][e] * 0x1p67f, 0x1p66f, mid), fmaf(o[nt][k][e + 2] * 0x1p67f, 0x1p62f, mid),
+                          fmaf(o[nt][k + 1][e] * 0x1p67f, 0x1p66f, mid), fmaf(o[nt][k + 1][e + 2] * 0x1p67f, 0x1p62f, mid));
         }
       }
       if (gr == 0) {
-        s_m[warp * COLS + col] = -mneg[nt][e];
+        s_m[warp * COLS + col] = 64.f - mneg[nt][e];
         s_l[warp * COLS + col] = l[nt][e];
       }
     }
@@ -593,37 +613,90 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
       a.z = fmaf(f, v.z, a.z);
       a.w = fmaf(f, v.w, a.w);
     }
-    if (p.n_split == 1) {
+    if (kn == nb) {
       const float r = ll == 0.f ? 0.f : 1.0f / ll;
       const int cc = col0 + col, qi = cc / p.g, hh = cc - qi * p.g;
       __nv_bfloat16* dst = p.o + b * p.ob + qi * p.on + static_cast<int64_t>(hk * p.g + hh) * p.oh + d;
       *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(a.x * r, a.y * r), pack_bf16(a.z * r, a.w * r));
     } else {
-      const int64_t piece = (static_cast<int64_t>(unit) * p.n_split + split) * COLS + col;
-      const int64_t pieces = static_cast<int64_t>(gridDim.x) * COLS;
+      // a CTA has at most one piece that begins inside a sequence and one that begins with it and does not reach its end
+      const int64_t piece = (2 * static_cast<int64_t>(blockIdx.x) + (k0 == 0)) * COLS + col;
+      const int64_t pieces = 2 * static_cast<int64_t>(gridDim.x) * COLS;
       *reinterpret_cast<float4*>(p.ws + piece * D + d) = a;
       if (d == 0) *reinterpret_cast<float2*>(p.ws + pieces * D + piece * 2) = make_float2(mm, ll);
     }
   }
+  __syncthreads();                                               // the next segment's copies may overwrite what was joined
 }
 
+template <int D, int G, int NT>
+__global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kernel(const __grid_constant__ Kv4AttnParams p) {
+  extern __shared__ uint4 smem_u4[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(smem_u4);
+
+  const int per_seq = p.Hk * p.col_chunks;
+  // my stretch of the row of blocks, and the sequence it begins in
+  int64_t before;
+  const int64_t total = blocks_before(p, 0, &before) * per_seq;
+  if (blockIdx.x == 0 && threadIdx.x < 32) {
+    for (int s = threadIdx.x; s < p.B; s += 32)
+      if (p.lengths[s] < 0 || p.lengths[s] > p.max_len) report(p.status, DEV_BAD_LENGTH);
+  }
+  const int64_t ctas = min(static_cast<int64_t>(gridDim.x), total);          // none is left without a block
+  if (blockIdx.x >= ctas) return;
+  int64_t cur = total * blockIdx.x / ctas, left = total * (blockIdx.x + 1) / ctas - cur;
+  int b = 0;
+  {
+    int64_t skipped;
+    b = sequence_at(p, cur / per_seq, &skipped);
+    cur -= skipped * per_seq;                                    // from here on relative to the sequence's first block
+  }
+  int len = length_of(p, b);
+  int nb = blocks_of(p, len);
+  int u = static_cast<int>(cur / nb), k0 = static_cast<int>(cur - static_cast<int64_t>(u) * nb);
+  for (; left > 0;) {
+    const int kn = static_cast<int>(min(static_cast<int64_t>(nb - k0), left));
+    segment<D, G, NT>(p, smem, b, u / p.col_chunks, u % p.col_chunks, len, k0, kn, nb);
+    left -= kn;
+    k0 = 0;
+    if (++u == per_seq && left > 0) {
+      u = 0;
+      len = length_of(p, ++b);
+      nb = blocks_of(p, len);
+    }
+  }
+}
+// The CTA whose stretch [total c / ctas, total (c + 1) / ctas) has block x.
+__device__ __forceinline__ int cta_of(int64_t x, int64_t total, int ctas) {
+  int c = static_cast<int>(x * ctas / total);
+  while (total * (c + 1) / ctas <= x) ++c;
+  while (total * c / ctas > x) --c;
+  return c;
+}
 // Joins the pieces of split sequences, in their order: one warp per (batch, column).
 template <int D>
-__global__ void __launch_bounds__(128) attn_kv4_join_kernel(const __grid_constant__ Kv4AttnParams p, const int cols, const int64_t pieces) {
+__global__ void __launch_bounds__(128) attn_kv4_join_kernel(const __grid_constant__ Kv4AttnParams p, const int cols, int ctas) {
   const int lane = threadIdx.x & 31;
   const int columns = p.n * p.g;
   const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
   if (item >= static_cast<int64_t>(p.B) * p.Hk * columns) return;
   const int bh = static_cast<int>(item / columns), cc = static_cast<int>(item - static_cast<int64_t>(bh) * columns);
   const int b = bh / p.Hk, hk = bh - b * p.Hk, chunk = cc / cols;
-  int len = p.lengths[b];
-  len = len < 0 ? 0 : min(len, p.max_len);
-  int n = (len + p.split_len - 1) / p.split_len;
-  if (n < 1) n = 1;
-  const int64_t piece0 = (static_cast<int64_t>(bh) * p.col_chunks + chunk) * p.n_split * cols + (cc - chunk * cols);
+  const int nb = blocks_of(p, length_of(p, b)), per_seq = p.Hk * p.col_chunks;
+  int64_t before;
+  const int64_t total = blocks_before(p, b, &before) * per_seq;
+  const int grid = ctas;
+  ctas = static_cast<int>(min(static_cast<int64_t>(ctas), total));
+  // blocks first .. first + nb of the row: the CTAs that had them, in order
+  const int64_t first = before * per_seq + static_cast<int64_t>(hk * p.col_chunks + chunk) * nb;
+  const int c0 = cta_of(first, total, ctas), c1 = cta_of(first + nb - 1, total, ctas);
+  if (c0 == c1) return;                                          // never split: written by its CTA
+  int n = c1 - c0 + 1;
+  auto piece_of = [&](int s) { return (2 * static_cast<int64_t>(c0 + s) + (s == 0)) * cols + (cc - chunk * cols); };
+  const int64_t pieces = 2 * static_cast<int64_t>(grid) * cols;
   const float2* ml = reinterpret_cast<const float2*>(p.ws + pieces * D);
   float mm = -INFINITY;
-  for (int s = lane; s < n; s += 32) mm = fmaxf(mm, ml[piece0 + static_cast<int64_t>(s) * cols].x);
+  for (int s = lane; s < n; s += 32) mm = fmaxf(mm, ml[piece_of(s)].x);
 #pragma unroll
   for (int d = 16; d; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
   if (mm == -INFINITY) n = 0;
@@ -632,7 +705,7 @@ __global__ void __launch_bounds__(128) attn_kv4_join_kernel(const __grid_constan
   const bool live = lane * 4 < D;
 #pragma unroll 4
   for (int s = 0; s < n; ++s) {
-    const int64_t piece = piece0 + static_cast<int64_t>(s) * cols;
+    const int64_t piece = piece_of(s);
     const float2 x = ml[piece];
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (live) v = *reinterpret_cast<const float4*>(p.ws + piece * D + lane * 4);
@@ -666,12 +739,11 @@ cudaError_t ak_run(const Kv4AttnParams& p, cudaStream_t s) {
   constexpr size_t smem = ak_smem<D, G, NT>();
   cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
   if (e != cudaSuccess) return e;
-  const int64_t grid = static_cast<int64_t>(p.B) * p.Hk * p.col_chunks * p.n_split;
-  kern<<<static_cast<unsigned>(grid), AK_THREADS, smem, s>>>(p);
+  kern<<<static_cast<unsigned>(p.ctas), AK_THREADS, smem, s>>>(p);
   e = cudaGetLastError();
-  if (e != cudaSuccess || p.n_split == 1) return e;
+  if (e != cudaSuccess || p.block >= p.max_len || p.ctas == 1) return e;
   const int64_t items = static_cast<int64_t>(p.B) * p.Hk * p.n * p.g;
-  attn_kv4_join_kernel<D><<<static_cast<unsigned>((items + 3) / 4), 128, 0, s>>>(p, 8 * NT, grid * 8 * NT);
+  attn_kv4_join_kernel<D><<<static_cast<unsigned>((items + 3) / 4), 128, 0, s>>>(p, 8 * NT, p.ctas);
   return cudaGetLastError();
 }
 

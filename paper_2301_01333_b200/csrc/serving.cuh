@@ -19,8 +19,8 @@ struct Kv4AttnParams {
   int page_shift, width, max_len;
   int64_t num_pages, table_stride;
   float c;                          // scale * log2(e)
-  int split_len, n_split;           // tokens per CTA (a multiple of 32) and CTAs per unit
-  int col_chunks;                   // CTAs that share the columns of a unit
+  int block, ctas;                  // tokens per block (a multiple of 128) of the row of blocks that `ctas` CTAs share out
+  int col_chunks;                   // chunks the columns of a (sequence, head) are taken in
   const __nv_bfloat16* q;
   int64_t qb, qn, qh;
   __nv_bfloat16* o;
