@@ -46,6 +46,7 @@ constexpr int AK_WARPS = 4;
 constexpr int AK_THREADS = AK_WARPS * 32;
 constexpr int AK_TILE = 32;                  // tokens per tile of a warp
 constexpr int AK_STAGES = 3;
+constexpr int AK_START = 2;
 constexpr float AK_RAISE = 8.0f;             // binades a score may exceed the reference by
 
 template <int D, int G>
@@ -146,12 +147,14 @@ __device__ __forceinline__ uint32_t code_off(int r, int c) {
 }
 }  // namespace
 
-// The row of blocks: a sequence has one block per p.block tokens, at least one, times heads and chunks of columns.
+// The row of blocks: a sequence has one block per p.block tokens, at least one, times heads and chunks of columns.  A piece of
+// work costs its blocks and a start (positions, page numbers, queries, joining the warps) worth about AK_START blocks: the row
+// has that many empty ones ahead of every sequence's own, so that stretches of many short sequences are no longer than others.
 __device__ __forceinline__ int length_of(const Kv4AttnParams& p, int b) {
   const int len = __ldg(p.lengths + b);
   return len < 0 ? 0 : min(len, p.max_len);
 }
-__device__ __forceinline__ int blocks_of(const Kv4AttnParams& p, int len) { return max((len + p.block - 1) / p.block, 1); }
+__device__ __forceinline__ int blocks_of(const Kv4AttnParams& p, int len) { return max((len + p.block - 1) / p.block, 1) + AK_START; }
 // Blocks of the sequences before b (*before) and of all; called by whole warps.
 __device__ __forceinline__ int64_t blocks_before(const Kv4AttnParams& p, int b, int64_t* before) {
   int64_t all = 0, mine = 0;
@@ -203,6 +206,75 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, tg = lane & 3;
   const int columns = p.n * p.g, col0 = chunk * COLS;
   const int t_begin = k0 * p.block, t_end = min(len, (k0 + kn) * p.block);
+
+  const int tiles = t_end > t_begin ? (t_end - t_begin + AK_TILE - 1) / AK_TILE : 0;
+  const int mine = tiles > warp ? (tiles - warp + AK_WARPS - 1) / AK_WARPS : 0;      // tiles warp, warp + 4, ...
+  const uint32_t ring_a = smem_u32(smem + warp * L::RING);
+  const int* trow = p.table + b * p.table_stride;
+  const int page_mask = (1 << p.page_shift) - 1;
+  const bool one_page = p.page_shift >= 5;                       // a tile of 32 tokens lies in one page, else in two
+
+  // 16-byte chunks of codes a lane copies of each half tile, and where they go
+  constexpr int CH = L::ROW / 16, N = 16 * CH, IT = (N + 31) / 32, PN = NG * 4;
+  uint32_t soff[IT];
+#pragma unroll
+  for (int k = 0; k < IT; ++k) {
+    const int x = k * 32 + lane, r = x / CH;
+    soff[k] = code_off<D>(r, x - r * CH);
+  }
+  // Page numbers of 16 tiles at a time, two per tile, one per lane.
+  int pages = 0;
+  auto fetch_pages = [&](int i) {
+    const int tok = t_begin + (warp + AK_WARPS * (i + (lane >> 1))) * AK_TILE + (lane & 1) * 16;
+    pages = 0;
+    if (tok < t_end) {
+      pages = __ldg(trow + (tok >> p.page_shift));
+      if (pages < 0 || pages >= p.num_pages) {
+        report(p.status, DEV_BAD_PAGE);
+        pages = 0;
+      }
+    }
+  };
+  const uint32_t poff = (lane & 15) * 16 + (lane < 16 ? 0 : L::PARAMS);
+  const uint8_t* kbase = p.k_codes + lane * 16;
+  const int64_t to_v = p.v_codes - p.k_codes;
+  const uint8_t* pbase = reinterpret_cast<const uint8_t*>(lane < 16 ? p.k_params : p.v_params) + (lane & 15) * 16;
+  // half H of the tile at shared address st, of which the first half would be row `row` of the cache
+  auto copy_half = [&](auto half_c, uint32_t st, const uint8_t* ks, const uint8_t* vs, const uint8_t* ps) {
+    constexpr int H = decltype(half_c)::value, TO = H * 16 * L::PITCH, FROM = H * 16 * L::ROW, PB = H * 16 * NG * 4;
+    each<IT>([&](auto k) {
+      if (N % 32 == 0 || k * 32 + lane < N) {
+        cp_async16<TO, FROM + k * 512>(st + soff[k], ks);
+        cp_async16<TO + L::CODES, FROM + k * 512>(st + soff[k], vs);
+      }
+    });
+    if ((lane & 15) < PN) cp_async16<2 * L::CODES + PB, PB>(st + poff, ps);
+  };
+  uint32_t st_in = ring_a;                                       // the stage the next copy goes to
+  auto issue = [&](int i) {
+    if (i < mine) {
+      if ((i & 15) == 0) fetch_pages(i);
+      const int t0 = t_begin + (warp + AK_WARPS * i) * AK_TILE;
+      const int64_t row = ((static_cast<int64_t>(__shfl_sync(0xffffffffu, pages, 2 * (i & 15))) * p.Hk + hk) << p.page_shift) + (t0 & page_mask);
+      const uint8_t* ks = kbase + row * L::ROW;
+      const uint8_t* ps = pbase + row * (NG * 4);
+      copy_half(std::integral_constant<int, 0>{}, st_in, ks, ks + to_v, ps);
+      if (t0 + 16 < t_end) {
+        if (!one_page) {                                         // the second half's rows, 16 of them back
+          const int64_t row1 = ((static_cast<int64_t>(__shfl_sync(0xffffffffu, pages, 2 * (i & 15) + 1)) * p.Hk + hk) << p.page_shift) - 16;
+          ks = kbase + row1 * L::ROW;
+          ps = pbase + row1 * (NG * 4);
+        }
+        copy_half(std::integral_constant<int, 1>{}, st_in, ks, ks + to_v, ps);
+      }
+    }
+    cp_commit();
+    st_in += L::STAGE;
+    if (st_in == ring_a + L::RING) st_in = ring_a;
+  };
+
+#pragma unroll
+  for (int i = 0; i < AK_STAGES - 1; ++i) issue(i);              // under way while the queries are prepared
 
   // Queries as the second operand of the first product: lane (gr, tg) holds of column gr, of every KS elements, the
   // eight (or sixteen, where a group spans 64) that its lane of the first operand holds: element 8 x + y of the lane's run
@@ -286,70 +358,6 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
     }
   }
 
-  const int tiles = t_end > t_begin ? (t_end - t_begin + AK_TILE - 1) / AK_TILE : 0;
-  const int mine = tiles > warp ? (tiles - warp + AK_WARPS - 1) / AK_WARPS : 0;      // tiles warp, warp + 4, ...
-  const uint32_t ring_a = smem_u32(smem + warp * L::RING);
-  const int* trow = p.table + b * p.table_stride;
-  const int page_mask = (1 << p.page_shift) - 1;
-  const bool one_page = p.page_shift >= 5;                       // a tile of 32 tokens lies in one page, else in two
-
-  // 16-byte chunks of codes a lane copies of each half tile, and where they go
-  constexpr int CH = L::ROW / 16, N = 16 * CH, IT = (N + 31) / 32, PN = NG * 4;
-  uint32_t soff[IT];
-#pragma unroll
-  for (int k = 0; k < IT; ++k) {
-    const int x = k * 32 + lane, r = x / CH;
-    soff[k] = code_off<D>(r, x - r * CH);
-  }
-  // Page numbers of 16 tiles at a time, two per tile, one per lane.
-  int pages = 0;
-  auto fetch_pages = [&](int i) {
-    const int tok = t_begin + (warp + AK_WARPS * (i + (lane >> 1))) * AK_TILE + (lane & 1) * 16;
-    pages = 0;
-    if (tok < t_end) {
-      pages = __ldg(trow + (tok >> p.page_shift));
-      if (pages < 0 || pages >= p.num_pages) {
-        report(p.status, DEV_BAD_PAGE);
-        pages = 0;
-      }
-    }
-  };
-  const uint32_t poff = (lane & 15) * 16 + (lane < 16 ? 0 : L::PARAMS);
-  // half 0 or 1 of the tile at shared address st from row `row` of the cache
-  auto copy_half = [&](auto half_c, uint32_t st, int64_t row) {
-    constexpr int H = decltype(half_c)::value;
-    const uint8_t* ks = p.k_codes + row * L::ROW + lane * 16;
-    const uint8_t* vs = p.v_codes + row * L::ROW + lane * 16;
-    each<IT>([&](auto k) {
-      if (N % 32 == 0 || k * 32 + lane < N) {
-        cp_async16<H * 16 * L::PITCH, k * 512>(st + soff[k], ks);
-        cp_async16<H * 16 * L::PITCH + L::CODES, k * 512>(st + soff[k], vs);
-      }
-    });
-    if ((lane & 15) < PN) {
-      const uint8_t* src = reinterpret_cast<const uint8_t*>((lane < 16 ? p.k_params : p.v_params) + row * NG) + (lane & 15) * 16;
-      cp_async16<2 * L::CODES + H * (16 * NG * 4), 0>(st + poff, src);
-    }
-  };
-  uint32_t st_in = ring_a;                                       // the stage the next copy goes to
-  auto issue = [&](int i) {
-    if (i < mine) {
-      if ((i & 15) == 0) fetch_pages(i);
-      const int t0 = t_begin + (warp + AK_WARPS * i) * AK_TILE;
-      const int pa = __shfl_sync(0xffffffffu, pages, 2 * (i & 15)), pb = __shfl_sync(0xffffffffu, pages, 2 * (i & 15) + 1);
-      const int64_t row = ((static_cast<int64_t>(pa) * p.Hk + hk) << p.page_shift) + (t0 & page_mask);
-      copy_half(std::integral_constant<int, 0>{}, st_in, row);
-      if (t0 + 16 < t_end)
-        copy_half(std::integral_constant<int, 1>{}, st_in, one_page ? row + 16 : (static_cast<int64_t>(pb) * p.Hk + hk) << p.page_shift);
-    }
-    cp_commit();
-    st_in += L::STAGE;
-    if (st_in == ring_a + L::RING) st_in = ring_a;
-  };
-
-#pragma unroll
-  for (int i = 0; i < AK_STAGES - 1; ++i) issue(i);
-
   // Row r of a 16-row operand is token perm(r) = r / 2 (r even), 4 + r / 2 (r odd), + 8 above
   const int pr = (gr >> 1) + ((gr & 1) << 2);
   uint32_t koff[KW / KP], voff[NG][2];                           // where a lane's codes lie in the first rows of a tile
@@ -368,57 +376,73 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
     const int t0 = t_begin + (warp + AK_WARPS * i) * AK_TILE;
     const uint32_t kp = kc + pr * NG * 4;
     float s[2][NT][4];
-    each<2>([&](auto mt_c) {
-      constexpr int mt = decltype(mt_c)::value;
-      each<NG>([&](auto j_c) {
-        constexpr int j = decltype(j_c)::value;
-        float acc[NT][4];
+    // Sums of one (16 rows, group) depend on one another: where registers allow, those of all groups take turns, else those
+    // of the two row blocks.
+    constexpr int JI = NG * NT <= 2 ? NG : 1;                    // groups in turn
+    each<NG / JI>([&](auto jo_c) {
+      float acc[JI][2][NT][4];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.f;
-        }
+      for (int j = 0; j < JI; ++j)
 #pragma unroll
-        for (int w0 = j * (G / 32); w0 < (j + 1) * (G / 32); w0 += KP) {
-          uint32_t ka[KP], kb[KP];
-          const uint32_t aa = kc + koff[w0 / KP];                // 8 rows further down: the same key
-          constexpr int ra = mt * 16 * L::PITCH, rb = ra + 8 * L::PITCH;
-          if constexpr (KP == 2) {
-            const uint2 x = lds64<ra>(aa), y = lds64<rb>(aa);
-            ka[0] = x.x; ka[1] = x.y; kb[0] = y.x; kb[1] = y.y;
-          } else {
-            ka[0] = lds32<ra>(aa);
-            kb[0] = lds32<rb>(aa);
-          }
+        for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-          for (int x = 0; x < KP; ++x) {
-            const uint32_t ah = ka[x] >> 8, bh8 = kb[x] >> 8;
-            const uint32_t a0 = nib_lo(ka[x]), a1 = nib_lo(kb[x]), a2 = nib_hi(ka[x]), a3 = nib_hi(kb[x]);
-            const uint32_t c0 = nib_lo(ah), c1 = nib_lo(bh8), c2 = nib_hi(ah), c3 = nib_hi(bh8);
+          for (int nt = 0; nt < NT; ++nt) acc[j][mt][nt][0] = acc[j][mt][nt][1] = acc[j][mt][nt][2] = acc[j][mt][nt][3] = 0.f;
+      each<G / 32 / KP>([&](auto w_c) {
+        each<JI>([&](auto ji_c) {
+          each<2>([&](auto mt_c) {
+            constexpr int ji = decltype(ji_c)::value, mt = decltype(mt_c)::value;
+            constexpr int w0 = (decltype(jo_c)::value * JI + ji) * (G / 32) + decltype(w_c)::value * KP;
+            uint32_t ka[KP], kb[KP];
+            const uint32_t aa = kc + koff[w0 / KP];              // 8 rows further down: the same key
+            constexpr int ra = mt * 16 * L::PITCH, rb = ra + 8 * L::PITCH;
+            if constexpr (KP == 2) {
+              const uint2 x = lds64<ra>(aa), y = lds64<rb>(aa);
+              ka[0] = x.x; ka[1] = x.y; kb[0] = y.x; kb[1] = y.y;
+            } else {
+              ka[0] = lds32<ra>(aa);
+              kb[0] = lds32<rb>(aa);
+            }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              mma_f16(acc[nt], a0, a1, a2, a3, qf[nt][w0 + x][0], qf[nt][w0 + x][1]);
-              mma_f16(acc[nt], c0, c1, c2, c3, qf[nt][w0 + x][2], qf[nt][w0 + x][3]);
+            for (int x = 0; x < KP; ++x) {
+              const uint32_t ah = ka[x] >> 8, bh8 = kb[x] >> 8;
+              const uint32_t a0 = nib_lo(ka[x]), a1 = nib_lo(kb[x]), a2 = nib_hi(ka[x]), a3 = nib_hi(kb[x]);
+              const uint32_t c0 = nib_lo(ah), c1 = nib_lo(bh8), c2 = nib_hi(ah), c3 = nib_hi(bh8);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                mma_f16(acc[ji][mt][nt], a0, a1, a2, a3, qf[nt][w0 + x][0], qf[nt][w0 + x][1]);
+                mma_f16(acc[ji][mt][nt], c0, c1, c2, c3, qf[nt][w0 + x][2], qf[nt][w0 + x][3]);
+              }
+            }
+          });
+        });
+      });
+      each<JI>([&](auto ji_c) {
+        each<2>([&](auto mt_c) {
+          constexpr int ji = decltype(ji_c)::value, mt = decltype(mt_c)::value, j = decltype(jo_c)::value * JI + ji;
+          constexpr int po = 2 * L::CODES + (mt * 16 * NG + j) * 4;
+          const uint32_t pa = lds32<po>(kp), pb = lds32<po + 8 * NG * 4>(kp);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            const float* ac = acc[ji][mt][nt];
+            float* sc = s[mt][nt];
+            if (j == 0) {
+              sc[0] = fmaf(bf_hi(pa), ac[0], bf_lo(pa) * sq[nt][j][0]);
+              sc[1] = fmaf(bf_hi(pa), ac[1], bf_lo(pa) * sq[nt][j][1]);
+              sc[2] = fmaf(bf_hi(pb), ac[2], bf_lo(pb) * sq[nt][j][0]);
+              sc[3] = fmaf(bf_hi(pb), ac[3], bf_lo(pb) * sq[nt][j][1]);
+            } else {
+              sc[0] = fmaf(bf_hi(pa), ac[0], fmaf(bf_lo(pa), sq[nt][j][0], sc[0]));
+              sc[1] = fmaf(bf_hi(pa), ac[1], fmaf(bf_lo(pa), sq[nt][j][1], sc[1]));
+              sc[2] = fmaf(bf_hi(pb), ac[2], fmaf(bf_lo(pb), sq[nt][j][0], sc[2]));
+              sc[3] = fmaf(bf_hi(pb), ac[3], fmaf(bf_lo(pb), sq[nt][j][1], sc[3]));
             }
           }
-        }
-        constexpr int po = 2 * L::CODES + (mt * 16 * NG + j) * 4;
-        const uint32_t pa = lds32<po>(kp), pb = lds32<po + 8 * NG * 4>(kp);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          if (j == 0) {
-            s[mt][nt][0] = fmaf(bf_hi(pa), acc[nt][0], bf_lo(pa) * sq[nt][j][0]);
-            s[mt][nt][1] = fmaf(bf_hi(pa), acc[nt][1], bf_lo(pa) * sq[nt][j][1]);
-            s[mt][nt][2] = fmaf(bf_hi(pb), acc[nt][2], bf_lo(pb) * sq[nt][j][0]);
-            s[mt][nt][3] = fmaf(bf_hi(pb), acc[nt][3], bf_lo(pb) * sq[nt][j][1]);
-          } else {
-            s[mt][nt][0] = fmaf(bf_hi(pa), acc[nt][0], fmaf(bf_lo(pa), sq[nt][j][0], s[mt][nt][0]));
-            s[mt][nt][1] = fmaf(bf_hi(pa), acc[nt][1], fmaf(bf_lo(pa), sq[nt][j][1], s[mt][nt][1]));
-            s[mt][nt][2] = fmaf(bf_hi(pb), acc[nt][2], fmaf(bf_lo(pb), sq[nt][j][0], s[mt][nt][2]));
-            s[mt][nt][3] = fmaf(bf_hi(pb), acc[nt][3], fmaf(bf_lo(pb), sq[nt][j][1], s[mt][nt][3]));
-          }
-        }
+        });
       });
-      if constexpr (EDGE) {
+    });
+    if constexpr (EDGE) {
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt) {
         const int ta = t0 + mt * 16 + pr;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -429,7 +453,7 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
           }
         }
       }
-    });
+    }
     // ---- the reference of the exponentials
     bool over = false;
 #pragma unroll
@@ -656,7 +680,8 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
   int u = static_cast<int>(cur / nb), k0 = static_cast<int>(cur - static_cast<int64_t>(u) * nb);
   for (; left > 0;) {
     const int kn = static_cast<int>(min(static_cast<int64_t>(nb - k0), left));
-    segment<D, G, NT>(p, smem, b, u / p.col_chunks, u % p.col_chunks, len, k0, kn, nb);
+    const int first = max(k0 - AK_START, 0), behind = k0 + kn - AK_START;
+    if (behind > first) segment<D, G, NT>(p, smem, b, u / p.col_chunks, u % p.col_chunks, len, first, behind - first, nb - AK_START);
     left -= kn;
     k0 = 0;
     if (++u == per_seq && left > 0) {
@@ -689,7 +714,7 @@ __global__ void __launch_bounds__(128) attn_kv4_join_kernel(const __grid_constan
   ctas = static_cast<int>(min(static_cast<int64_t>(ctas), total));
   // blocks first .. first + nb of the row: the CTAs that had them, in order
   const int64_t first = before * per_seq + static_cast<int64_t>(hk * p.col_chunks + chunk) * nb;
-  const int c0 = cta_of(first, total, ctas), c1 = cta_of(first + nb - 1, total, ctas);
+  const int c0 = cta_of(first + AK_START, total, ctas), c1 = cta_of(first + nb - 1, total, ctas);
   if (c0 == c1) return;                                          // never split: written by its CTA
   int n = c1 - c0 + 1;
   auto piece_of = [&](int s) { return (2 * static_cast<int64_t>(c0 + s) + (s == 0)) * cols + (cc - chunk * cols); };
