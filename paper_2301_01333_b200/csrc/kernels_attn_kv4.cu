@@ -128,12 +128,9 @@ __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 
 // Byte offset of 16-byte chunk c of token row r in a codes tile.  The exclusive-or spreads the rows that one load
 // instruction touches over all banks: eight rows with the same chunk (keys, 4 bytes a lane), rows 0, 4, 1, 5 and 2, 6, 3, 7 with
 // two neighbouring chunks (keys, 8 bytes a lane), rows 0..3, 4..7, ... with two neighbouring chunks (values).
-// CTAs per SM the registers are cut for: outputs take D / 8 registers per eight columns, and every group of the head
-// dimension ten more, which have to fit in 128 (four CTAs), 168 (three) or 255 (two).
-constexpr int ak_blocks(int D, int G, int NT) {
-  if (NT == 1) return D / G <= 2 ? 4 : 3;
-  return D == 64 || D == G ? 3 : 2;
-}
+// CTAs per SM the registers are cut for: 168 for one group of columns, 255 for two.  (More CTAs with fewer registers were slower:
+// at 128 the products of a tile can no longer be kept apart, 87 against 78 us for 64 ragged sequences.)
+constexpr int ak_blocks(int D, int G, int NT) { return NT == 1 ? 3 : D == 64 ? 3 : 2; }
 // First of the eight elements of a row that word w of lane tg holds, KP words at a time per lane.
 template <int KP>
 __device__ __forceinline__ int key_elem(int w, int tg) {
@@ -378,7 +375,7 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
     float s[2][NT][4];
     // Sums of one (16 rows, group) depend on one another: where registers allow, those of all groups take turns, else those
     // of the two row blocks.
-    constexpr int JI = NG * NT <= 2 ? NG : 1;                    // groups in turn
+    constexpr int JI = NG <= 2 ? NG : NT > 1 ? 1 : NG == 3 ? 3 : 2;            // groups in turn
     each<NG / JI>([&](auto jo_c) {
       float acc[JI][2][NT][4];
 #pragma unroll
@@ -388,33 +385,40 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) acc[j][mt][nt][0] = acc[j][mt][nt][1] = acc[j][mt][nt][2] = acc[j][mt][nt][3] = 0.f;
       each<G / 32 / KP>([&](auto w_c) {
+        uint32_t raw[JI][2][2][KP];                              // words of rows gr and gr + 8
         each<JI>([&](auto ji_c) {
           each<2>([&](auto mt_c) {
             constexpr int ji = decltype(ji_c)::value, mt = decltype(mt_c)::value;
             constexpr int w0 = (decltype(jo_c)::value * JI + ji) * (G / 32) + decltype(w_c)::value * KP;
-            uint32_t ka[KP], kb[KP];
             const uint32_t aa = kc + koff[w0 / KP];              // 8 rows further down: the same key
             constexpr int ra = mt * 16 * L::PITCH, rb = ra + 8 * L::PITCH;
             if constexpr (KP == 2) {
               const uint2 x = lds64<ra>(aa), y = lds64<rb>(aa);
-              ka[0] = x.x; ka[1] = x.y; kb[0] = y.x; kb[1] = y.y;
+              raw[ji][mt][0][0] = x.x; raw[ji][mt][0][1] = x.y;
+              raw[ji][mt][1][0] = y.x; raw[ji][mt][1][1] = y.y;
             } else {
-              ka[0] = lds32<ra>(aa);
-              kb[0] = lds32<rb>(aa);
-            }
-#pragma unroll
-            for (int x = 0; x < KP; ++x) {
-              const uint32_t ah = ka[x] >> 8, bh8 = kb[x] >> 8;
-              const uint32_t a0 = nib_lo(ka[x]), a1 = nib_lo(kb[x]), a2 = nib_hi(ka[x]), a3 = nib_hi(kb[x]);
-              const uint32_t c0 = nib_lo(ah), c1 = nib_lo(bh8), c2 = nib_hi(ah), c3 = nib_hi(bh8);
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                mma_f16(acc[ji][mt][nt], a0, a1, a2, a3, qf[nt][w0 + x][0], qf[nt][w0 + x][1]);
-                mma_f16(acc[ji][mt][nt], c0, c1, c2, c3, qf[nt][w0 + x][2], qf[nt][w0 + x][3]);
-              }
+              raw[ji][mt][0][0] = lds32<ra>(aa);
+              raw[ji][mt][1][0] = lds32<rb>(aa);
             }
           });
         });
+#pragma unroll
+        for (int x = 0; x < KP; ++x) {
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {                 // neighbouring products belong to different sums
+#pragma unroll
+            for (int ji = 0; ji < JI; ++ji) {
+#pragma unroll
+              for (int mt = 0; mt < 2; ++mt) {
+                const int w = (decltype(jo_c)::value * JI + ji) * (G / 32) + decltype(w_c)::value * KP + x;
+                const uint32_t ka = half ? raw[ji][mt][0][x] >> 8 : raw[ji][mt][0][x], kb = half ? raw[ji][mt][1][x] >> 8 : raw[ji][mt][1][x];
+                const uint32_t a0 = nib_lo(ka), a1 = nib_lo(kb), a2 = nib_hi(ka), a3 = nib_hi(kb);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma_f16(acc[ji][mt][nt], a0, a1, a2, a3, qf[nt][w][2 * half], qf[nt][w][2 * half + 1]);
+              }
+            }
+          }
+        }
       });
       each<JI>([&](auto ji_c) {
         each<2>([&](auto mt_c) {
