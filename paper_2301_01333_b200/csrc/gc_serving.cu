@@ -88,7 +88,7 @@ gc_status_t check_rows(const char* who, const gc_kv4_cache_t* c, int dtype, int6
   const int esz = dtype == GC_F32 ? 4 : 2;
   if ((st = check_heads(who, "k", *k, esz, false)) != GC_OK) return st;
   if ((st = check_heads(who, "v", *v, esz, false)) != GC_OK) return st;
-  if (tokens > (1LL << 40) / c->kv_heads) REFUSE(GC_ERR_UNSUPPORTED, "%s: too many rows for one launch", who);
+  if (tokens > 0x7FFFFFFFLL / c->kv_heads) REFUSE(GC_ERR_UNSUPPORTED, "%s: too many rows for one launch", who);
   return GC_OK;
 }
 
