@@ -2,12 +2,14 @@
 //
 //   y = x * rsqrt(mean(x^2) + eps) * w ;   (a, b) -> (a cos phi - b sin phi, b cos phi + a sin phi),  phi = pos * inv_freq[i]
 //
-// Bound by memory: every element is read once and written once, about 12 operations each.  The angles of a token are the
-// same for all of its heads, so a CTA takes whole tokens, evaluates cos / sin once per (token, pair) into shared memory
+// Bound by memory: every element is read once and written once, about 7 operations each.  The angles of a token are the
+// same for all of its heads, so a CTA takes whole tokens and evaluates cos / sin once per (token, pair) into shared memory
 // (the product pos * inv_freq and its reduction by multiples of 2 pi in fp64, since a far position times a frequency
-// leaves fp32 no fraction), and walks the heads: L lanes per row hold W = 16 bytes of elements each, reduce the square
-// sum with shuffles, and hand the normalised row over in shared memory, where the other half of a pair is picked up.
-// Rows that are not 16-byte aligned (or a head dimension that is no multiple of 8 / 4) take the same code with W = 1.
+// leaves fp32 no fraction).  Then a few lanes share a row, two 16-byte vectors each, chosen so that both halves of every
+// pair are in one lane: vectors j and j + rot / 2, or two neighbours where pairs are interleaved.  A lane keeps its angles
+// and weights in registers and walks the heads of its token, the next row's loads under way while it works on one.
+// Rows that are not 16-byte aligned, or whose sizes do not come out in such vectors, take a second kernel, which hands the
+// normalised row over in shared memory, where the other half of a pair is picked up.
 #include "serving.cuh"
 
 namespace gc {
@@ -114,7 +116,7 @@ __global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const __grid_c
     }
     if (p.norm) {
       for (int d = L >> 1; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-      const float inv = 1.0f / sqrtf(sum / static_cast<float>(p.D) + p.eps);
+      const float inv = rsqrtf(sum / static_cast<float>(p.D) + p.eps);
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
         const int e = (c * L + lane) * W;
@@ -224,13 +226,139 @@ __global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const __grid_c
   }
 }
 
+// W: elements in 16 bytes.  L = 1 << log_l lanes per row, two vectors of W elements each (D / (2 W) lanes of them busy).
+template <typename T, int W, bool INTERLEAVED>
+__global__ void __launch_bounds__(QN_THREADS, 3) qk_norm_rope_pairs_kernel(const __grid_constant__ QkParams p) {
+  extern __shared__ float4 smem4[];
+  const int tpitch = (p.half + W - 1) / W * W;                   // angles of a token, padded to whole vectors
+  float* s_cos = reinterpret_cast<float*>(smem4);
+  float* s_sin = s_cos + p.tb * tpitch;
+  const int L = 1 << p.log_l, item = threadIdx.x & (L - 1);
+  const int slot = threadIdx.x >> p.log_l, per_token = (QN_THREADS >> p.log_l) / p.tb;         // rows a token's slots take at a time
+  const int t = slot / per_token, s0 = slot - t * per_token;
+  const bool mine = 2 * W * item < p.D;                          // else a lane without elements, there for the shuffles
+  // the two vectors, and the first angle
+  const int low = p.half / W;                                    // vectors below the middle (not interleaved)
+  const bool turns = INTERLEAVED || item < low;
+  const int e0 = INTERLEAVED ? 2 * W * item : turns ? W * item : 2 * p.half + 2 * W * (item - low);
+  const int e1 = !INTERLEAVED && turns ? p.half + W * item : e0 + W;
+  const int angles = max(min(p.half - W * item, W), 0);          // pairs of this lane that turn (interleaved; else all or none)
+  const int r0 = blockIdx.y * p.rows_per_cta, r1 = min(r0 + p.rows_per_cta, p.rows);
+  // groups of tb tokens, a grid's width apart
+  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * p.tb; t0 < p.tokens; t0 += static_cast<int64_t>(gridDim.x) * p.tb) {
+    const int nt = static_cast<int>(p.tokens - t0 < p.tb ? p.tokens - t0 : p.tb);
+    const bool live_token = t < nt;
+    if (mine && live_token) {                                      // the first rows on their way while the angles are evaluated
+      const bool is_q = r0 + s0 < p.q_heads;
+      const gc_heads_t& src = is_q ? p.q : p.k;
+      const T* x = static_cast<const T*>(src.data) + (t0 + t) * src.token_stride + (is_q ? r0 + s0 : r0 + s0 - p.q_heads) * src.head_stride;
+      if (r0 + s0 < r1) asm volatile("prefetch.global.L2 [%0];" ::"l"(x + e0));
+    }
+    __syncthreads();                                               // the last group's angles have been read
+    for (int i = threadIdx.x; i < nt * p.half; i += QN_THREADS) {
+      const int tt = i / p.half, j = i - tt * p.half;
+      turn_of(p.positions[t0 + tt], p.inv_freq[j], p.factor, s_cos + tt * tpitch + j, s_sin + tt * tpitch + j);
+    }
+    __syncthreads();
+    float cs[W], sn[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const bool ok = mine && turns && live_token && i < angles;
+      cs[i] = ok ? s_cos[t * tpitch + W * item + i] : 1.f;
+      sn[i] = ok ? s_sin[t * tpitch + W * item + i] : 0.f;
+    }
+
+    // heads [h, end) of q or k, this slot's every per_token-th; whole warps go through together
+    auto walk = [&](const gc_heads_t& src, const gc_heads_t& dst, const void* weight, int h, int end) {
+      if (h >= end) return;
+      const T* x = static_cast<const T*>(src.data) + (t0 + t) * src.token_stride + (h + s0) * src.head_stride;
+      T* o = static_cast<T*>(dst.data) + (t0 + t) * dst.token_stride + (h + s0) * dst.head_stride;
+      const int64_t xs = per_token * src.head_stride, os = per_token * dst.head_stride;
+      auto load = [&](bool ok, uint4* a, uint4* b) {
+        *a = *b = make_uint4(0, 0, 0, 0);
+        if (ok) {
+          *a = *reinterpret_cast<const uint4*>(x + e0);
+          *b = *reinterpret_cast<const uint4*>(x + e1);
+        }
+      };
+      bool ok = mine && live_token && h + s0 < end;
+      uint4 a, b;
+      load(ok, &a, &b);
+      float w0[W], w1[W];
+#pragma unroll
+      for (int i = 0; i < W; ++i) w0[i] = w1[i] = 1.f;
+      if (p.norm && weight && mine) {
+        const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const T*>(weight) + e0), b = *reinterpret_cast<const uint4*>(static_cast<const T*>(weight) + e1);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          w0[i] = to_f<T>(reinterpret_cast<const T*>(&a)[i]);
+          w1[i] = to_f<T>(reinterpret_cast<const T*>(&b)[i]);
+        }
+      }
+      for (; h < end; h += per_token) {
+        float y0[W], y1[W];
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          y0[i] = to_f<T>(reinterpret_cast<const T*>(&a)[i]);
+          y1[i] = to_f<T>(reinterpret_cast<const T*>(&b)[i]);
+          sum = fmaf(y0[i], y0[i], fmaf(y1[i], y1[i], sum));
+        }
+        const bool next = mine && live_token && h + per_token + s0 < end;
+        x += xs;
+        load(next, &a, &b);
+        if (p.norm) {
+          for (int d = L >> 1; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+          const float inv = rsqrtf(sum / static_cast<float>(p.D) + p.eps);
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            y0[i] *= inv * w0[i];
+            y1[i] *= inv * w1[i];
+          }
+        }
+        if constexpr (INTERLEAVED) {
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            float* y = i < W / 2 ? y0 + 2 * i : y1 + 2 * (i - W / 2);
+            const float u = y[0], v = y[1];
+            if (i < angles) {
+              y[0] = fmaf(u, cs[i], -(v * sn[i]));
+              y[1] = fmaf(v, cs[i], u * sn[i]);
+            }
+          }
+        } else if (turns) {
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            const float u = y0[i], v = y1[i];
+            y0[i] = fmaf(u, cs[i], -(v * sn[i]));
+            y1[i] = fmaf(v, cs[i], u * sn[i]);
+          }
+        }
+        if (ok) {
+          uint4 c, d;
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            reinterpret_cast<T*>(&c)[i] = from_f<T>(y0[i]);
+            reinterpret_cast<T*>(&d)[i] = from_f<T>(y1[i]);
+          }
+          *reinterpret_cast<uint4*>(o + e0) = c;
+          *reinterpret_cast<uint4*>(o + e1) = d;
+        }
+        o += os;
+        ok = next;
+      }
+    };
+    walk(p.q, p.q_out, p.q_weight, r0, min(r1, p.q_heads));
+    walk(p.k, p.k_out, p.k_weight, max(r0 - p.q_heads, 0), r1 - p.q_heads);
+  }
+}
+
 static bool aligned_heads(const gc_heads_t& h, int heads, int w, int esz) {
   return heads == 0 || (reinterpret_cast<uintptr_t>(h.data) % 16 == 0 && h.token_stride % w == 0 && h.head_stride % w == 0 && w * esz == 16);
 }
 
-template <typename T, int W, int CH>
-static cudaError_t launch_t(const QkParams& p, dim3 grid, size_t smem, cudaStream_t s) {
-  auto kern = qk_norm_rope_kernel<T, W, CH>;
+template <typename K>
+static cudaError_t launch_t(K kern, const QkParams& p, dim3 grid, size_t smem, cudaStream_t s) {
   if (smem > 48 * 1024) {
     cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
     if (e != cudaSuccess) return e;
@@ -246,8 +374,10 @@ cudaError_t launch_qk_norm_rope(const gc_qk_norm_rope_t& d, int num_sms, cudaStr
   const bool vec = d.head_dim % wv == 0 && aligned_heads(d.q, d.q_heads, wv, esz) && aligned_heads(d.k, d.k_heads, wv, esz) &&
                    aligned_heads(d.q_out, d.q_heads, wv, esz) && aligned_heads(d.k_out, d.k_heads, wv, esz) &&
                    reinterpret_cast<uintptr_t>(d.q_weight) % 16 == 0 && reinterpret_cast<uintptr_t>(d.k_weight) % 16 == 0;
+  // both halves of every pair in one lane's two vectors
+  const bool pairs = vec && d.head_dim % (2 * wv) == 0 && (d.interleaved || ((d.rot_dim / 2) % wv == 0 && (d.head_dim - d.rot_dim) % (2 * wv) == 0));
   const int w = vec ? wv : 1;
-  const int lanes = (d.head_dim + w - 1) / w;
+  const int lanes = pairs ? d.head_dim / (2 * wv) : (d.head_dim + w - 1) / w;
   int log_l = 0;
   while (log_l < 5 && (1 << log_l) < lanes) ++log_l;
   const int slots = QN_THREADS >> log_l;
@@ -273,12 +403,27 @@ cudaError_t launch_qk_norm_rope(const gc_qk_norm_rope_t& d, int num_sms, cudaStr
   const int64_t gx = (d.tokens + p.tb - 1) / p.tb;
   if (gx > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
   const dim3 grid(static_cast<unsigned>(gx), static_cast<unsigned>((p.rows + p.rows_per_cta - 1) / p.rows_per_cta));
+  using bf16 = __nv_bfloat16;
+  if (pairs) {
+    // With many tokens eight to a CTA, so that a thread's angles and weights serve several rows, and as many CTAs as fit at
+    // once (three per SM), which walk over the groups; fewer to a CTA while that leaves SMs without work.
+    dim3 pg = grid;
+    if (d.tokens >= 4LL * num_sms) {
+      p.tb = d.tokens >= 48LL * num_sms ? 8 : d.tokens >= 8LL * num_sms ? 4 : 2;
+      if (p.tb > slots) p.tb = slots;
+      const int64_t groups = (d.tokens + p.tb - 1) / p.tb;
+      pg.x = static_cast<unsigned>(groups < 3LL * num_sms ? groups : 3LL * num_sms);
+    }
+    const size_t smem = 2 * static_cast<size_t>(p.tb) * ((p.half + wv - 1) / wv * wv) * 4;
+    if (f32) return d.interleaved ? launch_t(qk_norm_rope_pairs_kernel<float, 4, true>, p, pg, smem, s) : launch_t(qk_norm_rope_pairs_kernel<float, 4, false>, p, pg, smem, s);
+    return d.interleaved ? launch_t(qk_norm_rope_pairs_kernel<bf16, 8, true>, p, pg, smem, s) : launch_t(qk_norm_rope_pairs_kernel<bf16, 8, false>, p, pg, smem, s);
+  }
   const size_t smem = (static_cast<size_t>(slots) * ((d.head_dim + 3) & ~3) + 2 * static_cast<size_t>(p.tb) * ((p.half + 3) & ~3)) * 4;
   if (f32) {
-    if (!vec) return launch_t<float, 1, 8>(p, grid, smem, s);
-    return lanes > 32 ? launch_t<float, 4, 2>(p, grid, smem, s) : launch_t<float, 4, 1>(p, grid, smem, s);
+    if (!vec) return launch_t(qk_norm_rope_kernel<float, 1, 8>, p, grid, smem, s);
+    return lanes > 32 ? launch_t(qk_norm_rope_kernel<float, 4, 2>, p, grid, smem, s) : launch_t(qk_norm_rope_kernel<float, 4, 1>, p, grid, smem, s);
   }
-  return vec ? launch_t<__nv_bfloat16, 8, 1>(p, grid, smem, s) : launch_t<__nv_bfloat16, 1, 8>(p, grid, smem, s);
+  return vec ? launch_t(qk_norm_rope_kernel<bf16, 8, 1>, p, grid, smem, s) : launch_t(qk_norm_rope_kernel<bf16, 1, 8>, p, grid, smem, s);
 }
 
 }  // namespace gc
