@@ -8,16 +8,19 @@
 // 512 clocks each against 16384 exponentials, 16 a clock: 1024 clocks.  The two have to run side by side, so a CTA owns two
 // tiles of 128 query rows (256 neighbouring rows of one head) and alternates: while the softmax warps of one tile turn its
 // scores into probabilities, the tensor core works for the other.
-//   warps 0-3, 4-7   softmax of tile 0 / 1, one query row per thread: 128 scores from tensor memory into registers at once,
-//                    maximum, exponentials, row sum; the bf16 probabilities go back over the scores they came from, as the
-//                    A operand of the second product in tensor memory; at the end of a tile they scale and store its O
-//   warp 8           TMA producer: Q tiles, and K and V blocks through one ring
-//   warp 9           MMA issuer: S = Q K^T (both operands in shared memory), O += P V (P in tensor memory, V as stored,
+//   warps 0-7, 8-15  softmax of tile 0 / 1, two threads per query row: 64 scores each from tensor memory into registers at
+//                    once, maximum, exponentials, row sum; the bf16 probabilities go back over the scores they came from, as
+//                    the A operand of the second product in tensor memory; at the end of a tile they scale and store its O.
+//                    (With one thread per row, two warps per scheduler left its latencies bare: 1148 us for one prompt of
+//                    16384 tokens, 16 heads of 128, against AP_2T us.)
+//   warp 16          TMA producer: Q tiles, and K and V blocks through one ring
+//   warp 17          MMA issuer: S = Q K^T (both operands in shared memory), O += P V (P in tensor memory, V as stored,
 //                    keys along the rows).  The tensor core works off one thread's products in order, which is what lets S of
 //                    the next block overwrite P of this one, and makes "S complete" imply "O complete".
 // Tensor memory: two score tiles of 128 columns and two outputs of D <= 128: all 512 columns.
 //   * The reference m is raised only when a score exceeds it by 2^8 (as in the cache attention): after the first block the
 //     output is almost never touched, and raising it is the softmax warps' own business - no extra role, no extra hand-over.
+//     The two threads of a row need not compare their maxima for it: one barrier with a vote says whether any row has to.
 //   * Persistent CTAs; the work list (256 query rows of a sequence, times heads) is made by each CTA from the sequence offsets
 //     and sorted by its number of key blocks, longest first, dealt out back and forth.  The first scores of the next item are
 //     issued before the last output of the current one has been stored.
@@ -30,7 +33,7 @@
 namespace gc {
 
 namespace {
-constexpr int AP_THREADS = 384;               // three warpgroups; the last two warps only hand their registers over
+constexpr int AP_THREADS = 640;               // five warpgroups; the last two warps only hand their registers over
 constexpr int AP_MAX_LIST = 1024;                // work list entries kept (and sorted) in shared memory
 constexpr float AP_RAISE = 8.0f;
 
@@ -42,7 +45,8 @@ struct PromptLayout {
   static constexpr int STAGES = D == 64 ? 8 : 4;
   static constexpr int BARS = 2 * STAGES + 10;
   static constexpr int LIST = AP_MAX_LIST * 8;
-  static constexpr size_t SMEM = 1024 + static_cast<size_t>(2 + STAGES) * TILE + LIST + BARS * 8 + 64;
+  static constexpr int STAT = 2 * 2 * 128 * 4;   // one float per thread of the softmax warps
+  static constexpr size_t SMEM = 1024 + static_cast<size_t>(2 + STAGES) * TILE + LIST + STAT + BARS * 8 + 128;
 };
 
 __device__ __forceinline__ float ap_ex2(float x) {
@@ -62,38 +66,69 @@ __device__ __forceinline__ void umma_ts_bf16(uint32_t d_tmem, uint32_t a_tmem, u
       ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// All 128 score columns of a warp's 32 rows, loads and their wait in one statement: the registers are written
-// asynchronously, and nothing may move or spill them in between.
-__device__ __forceinline__ void tmem_ld128(uint32_t taddr, uint32_t (&r)[128]) {
+// 64 columns of a warp's 32 rows, the load and its wait in one statement: the registers are written asynchronously, and
+// nothing may move or spill them in between.
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t (&r)[64]) {
   asm volatile(
-      "{\n\t.reg .b32 t;\n\t"
-      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, "
-      "%40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, "
-      "%63}, [%128];\n\t"
-      "add.u32 t, %128, 64;\n\t"
-      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%64, %65, %66, %67, %68, %69, %70, %71, %72, %73, %74, %75, %76, %77, %78, "
-      "%79, %80, %81, %82, %83, %84, %85, %86, %87, %88, %89, %90, %91, %92, %93, %94, %95, %96, %97, %98, %99, %100, "
-      "%101, %102, %103, %104, %105, %106, %107, %108, %109, %110, %111, %112, %113, %114, %115, %116, %117, %118, %119, "
-      "%120, %121, %122, %123, %124, %125, %126, %127}, [t];\n\t"
-      "tcgen05.wait::ld.sync.aligned;\n\t}"
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, "
+      "%22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, %40, %41, "
+      "%42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, "
+      "%62, %63}, [%64];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
-        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
-        "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]),
-        "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]),
-        "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]),
-        "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]),
-        "=r"(r[63]), "=r"(r[64]), "=r"(r[65]), "=r"(r[66]), "=r"(r[67]), "=r"(r[68]), "=r"(r[69]), "=r"(r[70]), "=r"(r[71]),
-        "=r"(r[72]), "=r"(r[73]), "=r"(r[74]), "=r"(r[75]), "=r"(r[76]), "=r"(r[77]), "=r"(r[78]), "=r"(r[79]), "=r"(r[80]),
-        "=r"(r[81]), "=r"(r[82]), "=r"(r[83]), "=r"(r[84]), "=r"(r[85]), "=r"(r[86]), "=r"(r[87]), "=r"(r[88]), "=r"(r[89]),
-        "=r"(r[90]), "=r"(r[91]), "=r"(r[92]), "=r"(r[93]), "=r"(r[94]), "=r"(r[95]), "=r"(r[96]), "=r"(r[97]), "=r"(r[98]),
-        "=r"(r[99]), "=r"(r[100]), "=r"(r[101]), "=r"(r[102]), "=r"(r[103]), "=r"(r[104]), "=r"(r[105]), "=r"(r[106]),
-        "=r"(r[107]), "=r"(r[108]), "=r"(r[109]), "=r"(r[110]), "=r"(r[111]), "=r"(r[112]), "=r"(r[113]), "=r"(r[114]),
-        "=r"(r[115]), "=r"(r[116]), "=r"(r[117]), "=r"(r[118]), "=r"(r[119]), "=r"(r[120]), "=r"(r[121]), "=r"(r[122]),
-        "=r"(r[123]), "=r"(r[124]), "=r"(r[125]), "=r"(r[126]), "=r"(r[127])
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]),
+        "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]),
+        "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]),
+        "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]),
+        "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
       : "r"(taddr)
       : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+// Two fp32 operations in one instruction, each rounded on its own.
+__device__ __forceinline__ uint64_t pair2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpair2(uint64_t v, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(v)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// Barrier of the 256 softmax threads of a tile; the second form also tells whether any of them had `v`.
+__device__ __forceinline__ void tile_sync(int t) { asm volatile("bar.sync %0, 256;" ::"r"(t + 1) : "memory"); }
+__device__ __forceinline__ bool tile_any(int t, bool v) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %2, 0;\n\t"
+      "bar.red.or.pred q, %1, 256, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"(t + 1), "r"(static_cast<uint32_t>(v))
+      : "memory");
+  return r != 0;
 }
 
 // One sequence's rows, from its offsets; offsets that decrease or leave the tensors are cut to size.
@@ -137,12 +172,14 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   uint8_t* sKV = sQ + 2 * L::TILE;                              // [STAGES] tiles
   int* s_item = reinterpret_cast<int*>(sKV + L::STAGES * L::TILE);      // sequence of each entry, then its block
   int* s_tmp = s_item + AP_MAX_LIST;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(s_tmp + AP_MAX_LIST);
+  float* s_stat = reinterpret_cast<float*>(s_tmp + AP_MAX_LIST);        // [tile][half of the columns][row]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(s_stat + L::STAT / 4);
   const uint32_t b0 = smem_u32(bars);
   const uint32_t bar_q_full = b0, bar_q_empty = b0 + 16, bar_s_full = b0 + 32, bar_p_full = b0 + 48, bar_o_full = b0 + 64;   // [2] each
   const uint32_t bar_kv_full = b0 + 80, bar_kv_empty = bar_kv_full + 8 * L::STAGES;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + L::BARS);
   int* s_total = reinterpret_cast<int*>(tmem_slot + 1);
+  volatile int* s_dead = s_total + 1;                           // [2]: a softmax warp of the tile has given up waiting
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
@@ -150,19 +187,20 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       mbar_init(bar_q_full + 8 * i, 1);
       mbar_init(bar_q_empty + 8 * i, 1);
       mbar_init(bar_s_full + 8 * i, 1);
-      mbar_init(bar_p_full + 8 * i, 4);
+      mbar_init(bar_p_full + 8 * i, 8);
       mbar_init(bar_o_full + 8 * i, 1);
     }
     for (int i = 0; i < L::STAGES; ++i) {
       mbar_init(bar_kv_full + 8 * i, 1);
       mbar_init(bar_kv_empty + 8 * i, 1);
     }
+    s_dead[0] = s_dead[1] = 0;
     fence_mbar_init();
     tma_prefetch_desc(&tmQ);
     tma_prefetch_desc(&tmK);
     tma_prefetch_desc(&tmV);
   }
-  if (warp == 9) {
+  if (warp == 17) {
     tmem_alloc(smem_u32(tmem_slot), 512);
     tmem_relinquish();
   }
@@ -274,127 +312,143 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     return it;
   };
 
-  // Registers: 168 a thread at launch, 504 in each lane's three warps of a scheduler; 2 x 208 + 80 = 496.
+  // Registers: 96 a thread at launch, 480 in each lane's five warps of a scheduler; 4 x 104 + 64 = 480.
   bool failed = false;
-  if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+  if (warp < 16) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
     // ------------------------------------------------------------------ softmax and output
-    const int t = warp >> 2, row = tid & 127;
+    // A wait that gives up must not leave the other warps of the tile in a barrier: the warp goes on taking part, and all
+    // of them leave together after the vote that follows.
+    const int t = warp >> 3, half = (warp >> 2) & 1, row = (warp & 3) * 32 + lane;
     const uint32_t t_lane = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-    const uint32_t s_addr = t_lane + t * 128, o_addr = t_lane + 256 + t * 128;
+    const uint32_t s_addr = t_lane + t * 128 + half * 64, o_addr = t_lane + 256 + t * 128 + half * (D / 2);
+    float* my_stat = s_stat + (t * 2 + half) * 128 + row;
+    const float* other_stat = s_stat + (t * 2 + (half ^ 1)) * 128 + row;
     uint32_t ring = 0, sn = 0, on = 0;
     const float c = p.c;
-    for (int r = 0; !failed; ++r) {
+    bool leave = false;
+    for (int r = 0; !leave; ++r) {
       const Item it = item_of(r);
       if (!it.valid) break;
       const int my_row = it.row0 + t * 128 + row;
       const int lim = row_limit(p, it.s, my_row), n = it.n[t];
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < n; ++j) {
-        if (!__all_sync(0xffffffffu, mbar_wait(bar_s_full + 8 * t, sn & 1))) { failed = true; break; }
+        if (!__all_sync(0xffffffffu, mbar_wait(bar_s_full + 8 * t, sn & 1))) failed = true;
         ++sn;
         tc_fence_after();
-        uint32_t v[128];
-        tmem_ld128(s_addr, v);
-        const int left = lim - j * 128;
-        if (__any_sync(0xffffffffu, left < 128)) {
+        uint32_t v[64];
+        tmem_ld64(s_addr, v);
+        const int left = lim - j * 128 - half * 64;
+        if (__any_sync(0xffffffffu, left < 64)) {
 #pragma unroll
-          for (int i = 0; i < 128; ++i)
+          for (int i = 0; i < 64; ++i)
             if (i >= left) v[i] = 0xff800000u;                   // minus infinity, whatever the score was
         }
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        float top = __uint_as_float(v[0]), top1 = __uint_as_float(v[1]);
 #pragma unroll
-        for (int i = 0; i < 128; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(v[i]));
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-        if (__any_sync(0xffffffffu, (top - m) * c > AP_RAISE)) {
-          const float mn = fmaxf(m, top);
+        for (int i = 2; i < 62; i += 4) {
+          top = max3(top, __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
+          top1 = max3(top1, __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
+        }
+        top = fmaxf(max3(top, __uint_as_float(v[62]), __uint_as_float(v[63])), top1);
+        if (tile_any(t, (top - m) * c > AP_RAISE || failed)) {
+          *my_stat = top;
+          if (failed) s_dead[t] = 1;
+          tile_sync(t);
+          const float mn = fmaxf(m, fmaxf(top, *other_stat));
+          if (s_dead[t]) leave = true;
+          tile_sync(t);                                          // read before the next one is written
+          if (leave) break;
           const float f = mn == m ? 1.f : ap_ex2((m - mn) * c);  // 0 from the initial minus infinity
           m = mn;
           l *= f;
           if (j > 0) {
-            // S of this block is complete, hence so is the product of the block before: O is at rest
+            // S of this block is complete, hence so is the product of the block before: O is at rest; half its columns each
 #pragma unroll 1
             for (int k = 0; k < D / 32; ++k) {
-              uint32_t w[32];
-              tmem_ld32(o_addr + k * 32, w);
+              uint32_t w[16];
+              tmem_ld16(o_addr + k * 16, w);
               tmem_wait_ld();
 #pragma unroll
-              for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) * f);
-              tmem_st32(o_addr + k * 32, w);
+              for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) * f);
+              tmem_st16(o_addr + k * 16, w);
             }
           }
         }
         const float off = m == -INFINITY ? 0.f : -m * c;
-        float ls[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint64_t c2 = pair2(c, c), off2 = pair2(off, off);
+        uint64_t ls[2] = {0, 0};
+        uint32_t w[32];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t w[32];
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const float e0 = ap_ex2(fmaf(__uint_as_float(v[h * 64 + 2 * i]), c, off));
-            const float e1 = ap_ex2(fmaf(__uint_as_float(v[h * 64 + 2 * i + 1]), c, off));
-            ls[(2 * i) & 3] += e0;
-            ls[(2 * i + 1) & 3] += e1;
-            w[i] = ap_pack(e0, e1);
-          }
-          tmem_st32(s_addr + h * 32, w);
+        for (int i = 0; i < 32; ++i) {
+          float e0, e1;
+          unpair2(fma2(pair2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), c2, off2), &e0, &e1);
+          e0 = ap_ex2(e0);
+          e1 = ap_ex2(e1);
+          ls[i & 1] = add2(ls[i & 1], pair2(e0, e1));
+          w[i] = ap_pack(e0, e1);
         }
-        l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+        tmem_st32(s_addr, w);
+        float l0, l1;
+        unpair2(add2(ls[0], ls[1]), &l0, &l1);
+        l += l0 + l1;
         if (j * 128 + 128 > it.s.nk) {
-          // the sequence ends inside this block: whatever follows it in V becomes zero
+          // the sequence ends inside this block: whatever follows it in V becomes zero (each thread of a row its 64 elements)
           const uint32_t pos = ring + 2 * j + 1, st = pos % L::STAGES;
-          if (!__all_sync(0xffffffffu, mbar_wait(bar_kv_full + 8 * st, (pos / L::STAGES) & 1))) { failed = true; break; }
-          if (j * 128 + row >= it.s.nk) {
+          if (!__all_sync(0xffffffffu, mbar_wait(bar_kv_full + 8 * st, (pos / L::STAGES) & 1))) failed = true;
+          if (!failed && j * 128 + row >= it.s.nk && half < L::NSUB) {
+            uint4* z = reinterpret_cast<uint4*>(sKV + st * L::TILE + half * L::SUB + row * 128);
 #pragma unroll
-            for (int k = 0; k < L::NSUB; ++k) {
-              uint4* z = reinterpret_cast<uint4*>(sKV + st * L::TILE + k * L::SUB + row * 128);
-#pragma unroll
-              for (int i = 0; i < 8; ++i) z[i] = make_uint4(0, 0, 0, 0);
-            }
+            for (int i = 0; i < 8; ++i) z[i] = make_uint4(0, 0, 0, 0);
           }
           fence_proxy_async_smem();
         }
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar_p_full + 8 * t);
+        if (lane == 0 && !failed) mbar_arrive(bar_p_full + 8 * t);
       }
-      if (failed) break;
+      if (leave) break;
       ring += 2 * max(it.n[0], it.n[1]);
       const bool store = my_row < it.s.nq;
-      __nv_bfloat16* dst = p.o + static_cast<int64_t>(it.s.q0 + my_row) * p.o_tok + static_cast<int64_t>(it.head) * p.o_head;
+      __nv_bfloat16* dst = p.o + static_cast<int64_t>(it.s.q0 + my_row) * p.o_tok + static_cast<int64_t>(it.head) * p.o_head + half * (D / 2);
       if (n == 0) {
         if (store) {
 #pragma unroll
-          for (int i = 0; i < D / 8; ++i) reinterpret_cast<uint4*>(dst)[i] = make_uint4(0, 0, 0, 0);
+          for (int i = 0; i < D / 16; ++i) reinterpret_cast<uint4*>(dst)[i] = make_uint4(0, 0, 0, 0);
         }
         continue;
       }
-      if (!__all_sync(0xffffffffu, mbar_wait(bar_o_full + 8 * t, on & 1))) { failed = true; break; }
+      *my_stat = l;
+      if (!__all_sync(0xffffffffu, mbar_wait(bar_o_full + 8 * t, on & 1))) failed = true;
       ++on;
       tc_fence_after();
+      if (tile_any(t, failed)) break;
+      l += *other_stat;
       const float rl = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll 1
       for (int k = 0; k < D / 32; ++k) {
-        uint32_t w[32];
-        tmem_ld32(o_addr + k * 32, w);
+        uint32_t w[16];
+        tmem_ld16(o_addr + k * 16, w);
         tmem_wait_ld();
         if (store) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < 2; ++i) {
             uint32_t x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = ap_pack(__uint_as_float(w[8 * i + 2 * e]) * rl, __uint_as_float(w[8 * i + 2 * e + 1]) * rl);
-            reinterpret_cast<uint4*>(dst)[k * 4 + i] = make_uint4(x[0], x[1], x[2], x[3]);
+            reinterpret_cast<uint4*>(dst)[k * 2 + i] = make_uint4(x[0], x[1], x[2], x[3]);
           }
         }
       }
       tc_fence_before();
+      tile_sync(t);                                              // the sums have been read
     }
     if (failed && lane == 0) report(p.status, DEV_TIMEOUT_EPILOGUE);
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    if (warp == 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp == 16) {
       // ------------------------------------------------------------------ TMA producer
       uint32_t ring = 0, qn[2] = {0, 0};
       const int g = p.Hq / p.Hk;
@@ -432,7 +486,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         }
         if (__any_sync(0xffffffffu, failed)) break;
       }
-    } else if (warp == 9) {
+    } else if (warp == 17) {
       // ------------------------------------------------------------------ MMA issuer
       const uint32_t idesc_s = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, 128, 128);
       const uint32_t idesc_o = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, 128, D, 0, 1);
@@ -484,7 +538,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                 const uint32_t vb = smem_u32(sKV) + (vpos % L::STAGES) * L::TILE;
   #pragma unroll
                 for (int k = 0; k < 8; ++k)                        // 16 keys per MMA
-                  umma_ts_bf16(tmem_base + 256 + t * 128, tmem_base + t * 128 + k * 8,
+                  umma_ts_bf16(tmem_base + 256 + t * 128, tmem_base + t * 128 + (k >> 2) * 64 + (k & 3) * 8,
                                make_smem_desc(vb + k * 16 * 128, L::SUB, 1024, SWZ_128B), idesc_o, !(j == 0 && k == 0));
                 if (j + 1 == it.n[t]) umma_commit(bar_o_full + 8 * t);
               }
@@ -512,7 +566,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == 17) {
     tc_fence_after();
     tmem_dealloc(tmem_base, 512);
   }
