@@ -37,16 +37,20 @@ constexpr int AP_THREADS = 640;               // five warpgroups; the last two w
 constexpr int AP_MAX_LIST = 1024;                // work list entries kept (and sorted) in shared memory
 constexpr float AP_RAISE = 8.0f;
 
-template <int D>
+template <int D, bool PAIR>
 struct PromptLayout {
   static constexpr int NSUB = (D + 63) / 64;     // 64-element sub-tiles of 128-byte rows
   static constexpr int SUB = 128 * 128;
   static constexpr int TILE = NSUB * SUB;        // 128 rows of Q, K or V
-  static constexpr int STAGES = D == 64 ? 8 : 4;
-  static constexpr int BARS = 2 * STAGES + 10;
+  static constexpr int KV = PAIR ? TILE / 2 : TILE;      // of one K or V block in this CTA
+  static constexpr int KSUB = PAIR ? SUB / 2 : SUB;      // of one K sub-tile: a pair's CTA holds 64 of the 128 keys
+  static constexpr int STAGES = D == 64 || PAIR ? 8 : 4;
+  static constexpr int ROWS = PAIR ? 256 : 128;  // query rows of one of the two tiles (of both CTAs)
+  static constexpr int ITEM = 2 * ROWS;
+  static constexpr int BARS = 2 * STAGES + 12;
   static constexpr int LIST = AP_MAX_LIST * 8;
   static constexpr int STAT = 2 * 2 * 128 * 4;   // one float per thread of the softmax warps
-  static constexpr size_t SMEM = 1024 + static_cast<size_t>(2 + STAGES) * TILE + LIST + STAT + BARS * 8 + 128;
+  static constexpr size_t SMEM = 1024 + static_cast<size_t>(2) * TILE + STAGES * KV + LIST + STAT + BARS * 8 + 64;
 };
 
 __device__ __forceinline__ float ap_ex2(float x) {
@@ -131,6 +135,22 @@ __device__ __forceinline__ bool tile_any(int t, bool v) {
   return r != 0;
 }
 
+// The same with CTA pairs: each CTA's rows in its own tensor memory, half of B in each CTA's shared memory
+__device__ __forceinline__ void umma_ts2_bf16(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred P;\n\tsetp.ne.b32 P, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, P;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// TMA load into this CTA's shared memory that reports to a barrier of the pair's leader
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t smem_dst, const CUtensorMap* m, int x, int y, int z, uint32_t cluster_bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(cluster_bar)
+      : "memory");
+}
+
 // One sequence's rows, from its offsets; offsets that decrease or leave the tensors are cut to size.
 struct Seq {
   int q0, nq, k0, nk;
@@ -148,35 +168,42 @@ __device__ __forceinline__ Seq seq_of(const PromptParams& p, int b) {
 __device__ __forceinline__ int row_limit(const PromptParams& p, const Seq& s, int i) {
   return i >= s.nq ? 0 : p.causal ? max(i + 1 + s.nk - s.nq, 0) : s.nk;
 }
-// 128-key blocks the tile of rows [r0, r0 + 128) needs.
-__device__ __forceinline__ int tile_blocks(const PromptParams& p, const Seq& s, int r0) {
-  return r0 >= s.nq ? 0 : (row_limit(p, s, min(r0 + 127, s.nq - 1)) + 127) >> 7;
+// 128-key blocks the tile of rows [r0, r0 + rows) needs.
+__device__ __forceinline__ int tile_blocks(const PromptParams& p, const Seq& s, int r0, int rows) {
+  return r0 >= s.nq ? 0 : (row_limit(p, s, min(r0 + rows, s.nq) - 1) + 127) >> 7;
 }
 
 struct Item {
   Seq s;
-  int row0, head;                // first of the 256 query rows, within the sequence
+  int row0, head;                // first of the query rows, within the sequence
   int n[2];                      // key blocks of the two tiles
+  // the longer tile's last block reaches past the sequence's end
+  __device__ __forceinline__ bool tail() const { return max(n[0], n[1]) * 128 > s.nk; }
   bool valid;
 };
 }  // namespace
 
-template <int D>
+template <int D, bool PAIR>
 __global__ void __launch_bounds__(AP_THREADS, 1)
 attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                    const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PromptParams p, const int listed, const int most) {
-  using L = PromptLayout<D>;
+  using L = PromptLayout<D, PAIR>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sQ = smem;                                           // [2] tiles
   uint8_t* sKV = sQ + 2 * L::TILE;                              // [STAGES] tiles
-  int* s_item = reinterpret_cast<int*>(sKV + L::STAGES * L::TILE);      // sequence of each entry, then its block
+  int* s_item = reinterpret_cast<int*>(sKV + L::STAGES * L::KV);      // sequence of each entry, then its block
   int* s_tmp = s_item + AP_MAX_LIST;
   float* s_stat = reinterpret_cast<float*>(s_tmp + AP_MAX_LIST);        // [tile][half of the columns][row]
   uint64_t* bars = reinterpret_cast<uint64_t*>(s_stat + L::STAT / 4);
   const uint32_t b0 = smem_u32(bars);
   const uint32_t bar_q_full = b0, bar_q_empty = b0 + 16, bar_s_full = b0 + 32, bar_p_full = b0 + 48, bar_o_full = b0 + 64;   // [2] each
-  const uint32_t bar_kv_full = b0 + 80, bar_kv_empty = bar_kv_full + 8 * L::STAGES;
+  const uint32_t bar_v_tail = b0 + 80;                          // pairs: the last V block of an item has arrived in both CTAs
+  const uint32_t bar_kv_full = b0 + 96, bar_kv_empty = bar_kv_full + 8 * L::STAGES;
+  // A pair: the full barriers of the leader count both CTAs' loads, and its p_full both CTAs' softmax warps; all others are
+  // completed in both CTAs.
+  const uint32_t rank = PAIR ? cluster_ctarank() : 0;
+  const int cta = PAIR ? blockIdx.x >> 1 : blockIdx.x, ctas = PAIR ? gridDim.x >> 1 : gridDim.x;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + L::BARS);
   int* s_total = reinterpret_cast<int*>(tmem_slot + 1);
   volatile int* s_dead = s_total + 1;                           // [2]: a softmax warp of the tile has given up waiting
@@ -187,13 +214,14 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       mbar_init(bar_q_full + 8 * i, 1);
       mbar_init(bar_q_empty + 8 * i, 1);
       mbar_init(bar_s_full + 8 * i, 1);
-      mbar_init(bar_p_full + 8 * i, 8);
+      mbar_init(bar_p_full + 8 * i, PAIR ? 16 : 8);
       mbar_init(bar_o_full + 8 * i, 1);
     }
     for (int i = 0; i < L::STAGES; ++i) {
       mbar_init(bar_kv_full + 8 * i, 1);
       mbar_init(bar_kv_empty + 8 * i, 1);
     }
+    mbar_init(bar_v_tail, 1);
     s_dead[0] = s_dead[1] = 0;
     fence_mbar_init();
     tma_prefetch_desc(&tmQ);
@@ -201,8 +229,13 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     tma_prefetch_desc(&tmV);
   }
   if (warp == 17) {
-    tmem_alloc(smem_u32(tmem_slot), 512);
-    tmem_relinquish();
+    if constexpr (PAIR) {
+      tmem_alloc2(smem_u32(tmem_slot), 512);
+      tmem_relinquish2();
+    } else {
+      tmem_alloc(smem_u32(tmem_slot), 512);
+      tmem_relinquish();
+    }
   }
   // ---- the work list
   if (warp == 0) {
@@ -212,7 +245,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       int nb = 0;
       if (b < p.B) {
         const Seq s = seq_of(p, b);
-        nb = (s.nq + 255) >> 8;
+        nb = (s.nq + L::ITEM - 1) / L::ITEM;
         if (blockIdx.x == 0 && (p.cu_q[b] != s.q0 || p.cu_q[b + 1] != s.q0 + s.nq || p.cu_k[b] != s.k0 || p.cu_k[b + 1] != s.k0 + s.nk))
           report(p.status, DEV_BAD_OFFSETS);
       }
@@ -231,15 +264,16 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     if (lane == 0) *s_total = total;
   }
   tc_fence_before();
-  __syncthreads();
+  if constexpr (PAIR) cluster_sync_all();                       // both CTAs' barriers exist from here on
+  else __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   const int entries = *s_total;
   if (listed) {
     auto cost = [&](int e) {
       const Seq s = seq_of(p, e >> 12);
-      const int r0 = (e & 4095) * 256;
-      return tile_blocks(p, s, r0) + tile_blocks(p, s, r0 + 128);
+      const int r0 = (e & 4095) * L::ITEM;
+      return tile_blocks(p, s, r0, L::ROWS) + tile_blocks(p, s, r0 + L::ROWS, L::ROWS);
     };
     // costs first (packed above the entry's number so that equal ones keep their order), then each entry's rank
     int mine[(AP_MAX_LIST + AP_THREADS - 1) / AP_THREADS], key[(AP_MAX_LIST + AP_THREADS - 1) / AP_THREADS];
@@ -272,7 +306,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   const int64_t items = static_cast<int64_t>(entries) * p.Hq;
   auto item_of = [&](int r) {
     Item it;
-    const int64_t g = static_cast<int64_t>(r) * gridDim.x + ((r & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+    const int64_t g = static_cast<int64_t>(r) * ctas + ((r & 1) ? ctas - 1 - cta : cta);
     it.valid = g < items;
     it.n[0] = it.n[1] = 0;
     it.row0 = it.head = 0;
@@ -287,7 +321,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     } else {
       int before = 0;
       for (int s0 = 0; s0 < p.B; s0 += 32) {
-        const int nb = s0 + lane < p.B ? (seq_of(p, s0 + lane).nq + 255) >> 8 : 0;
+        const int nb = s0 + lane < p.B ? (seq_of(p, s0 + lane).nq + L::ITEM - 1) / L::ITEM : 0;
         int incl = nb;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -306,9 +340,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       }
     }
     it.s = seq_of(p, b);
-    it.row0 = blk * 256;
-    it.n[0] = tile_blocks(p, it.s, it.row0);
-    it.n[1] = tile_blocks(p, it.s, it.row0 + 128);
+    it.row0 = blk * L::ITEM;
+    it.n[0] = tile_blocks(p, it.s, it.row0, L::ROWS);
+    it.n[1] = tile_blocks(p, it.s, it.row0 + L::ROWS, L::ROWS);
     return it;
   };
 
@@ -324,13 +358,14 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     const uint32_t s_addr = t_lane + t * 128 + half * 64, o_addr = t_lane + 256 + t * 128 + half * (D / 2);
     float* my_stat = s_stat + (t * 2 + half) * 128 + row;
     const float* other_stat = s_stat + (t * 2 + (half ^ 1)) * 128 + row;
-    uint32_t ring = 0, sn = 0, on = 0;
+    const uint32_t p_full = PAIR && rank ? mapa_shared(bar_p_full + 8 * t, 0) : bar_p_full + 8 * t;
+    uint32_t ring = 0, sn = 0, on = 0, tn = 0;
     const float c = p.c;
     bool leave = false;
     for (int r = 0; !leave; ++r) {
       const Item it = item_of(r);
       if (!it.valid) break;
-      const int my_row = it.row0 + t * 128 + row;
+      const int my_row = it.row0 + t * L::ROWS + rank * 128 + row;
       const int lim = row_limit(p, it.s, my_row), n = it.n[t];
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < n; ++j) {
@@ -394,23 +429,30 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         unpair2(add2(ls[0], ls[1]), &l0, &l1);
         l += l0 + l1;
         if (j * 128 + 128 > it.s.nk) {
-          // the sequence ends inside this block: whatever follows it in V becomes zero (each thread of a row its 64 elements)
+          // the sequence ends inside this block: whatever follows it in V becomes zero (each thread of a row its 64 elements;
+          // a pair's CTA has only 64 in all)
           const uint32_t pos = ring + 2 * j + 1, st = pos % L::STAGES;
-          if (!__all_sync(0xffffffffu, mbar_wait(bar_kv_full + 8 * st, (pos / L::STAGES) & 1))) failed = true;
-          if (!failed && j * 128 + row >= it.s.nk && half < L::NSUB) {
-            uint4* z = reinterpret_cast<uint4*>(sKV + st * L::TILE + half * L::SUB + row * 128);
+          const uint32_t bar = PAIR ? bar_v_tail : bar_kv_full + 8 * st, parity = PAIR ? tn & 1 : (pos / L::STAGES) & 1;
+          if (!__all_sync(0xffffffffu, mbar_wait(bar, parity))) failed = true;
+          if (!failed && j * 128 + row >= it.s.nk && half < (PAIR ? 1 : L::NSUB)) {
+            uint4* z = reinterpret_cast<uint4*>(sKV + st * L::KV + half * L::SUB + row * 128);
 #pragma unroll
             for (int i = 0; i < 8; ++i) z[i] = make_uint4(0, 0, 0, 0);
           }
+          if constexpr (PAIR) asm volatile("fence.acq_rel.cluster;" ::: "memory");
           fence_proxy_async_smem();
         }
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0 && !failed) mbar_arrive(bar_p_full + 8 * t);
+        if (lane == 0 && !failed) {
+          if constexpr (PAIR) mbar_arrive_cluster_nomem(p_full);
+          else mbar_arrive(p_full);
+        }
       }
       if (leave) break;
       ring += 2 * max(it.n[0], it.n[1]);
+      tn += it.tail();
       const bool store = my_row < it.s.nq;
       __nv_bfloat16* dst = p.o + static_cast<int64_t>(it.s.q0 + my_row) * p.o_tok + static_cast<int64_t>(it.head) * p.o_head + half * (D / 2);
       if (n == 0) {
@@ -457,52 +499,71 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         if (!it.valid) break;
         if (lane == 0) {
           const int kvh = it.head / g;
+          auto load = [&](uint32_t dst, const CUtensorMap* tm, int x, int y, int z, uint32_t bar) {
+            if constexpr (PAIR) tma_load_3d_pair(dst, tm, x, y, z, rank ? mapa_shared(bar, 0) : bar);
+            else tma_load_3d(dst, tm, x, y, z, bar);
+          };
           auto load_q = [&](int t) -> bool {
             if (it.n[t] == 0) return true;
             if (!mbar_wait(bar_q_empty + 8 * t, (qn[t] & 1) ^ 1)) return false;
             ++qn[t];
-            mbar_arrive_expect_tx(bar_q_full + 8 * t, static_cast<uint32_t>(L::TILE));
+            if (rank == 0) mbar_arrive_expect_tx(bar_q_full + 8 * t, static_cast<uint32_t>(PAIR ? 2 * L::TILE : L::TILE));
             for (int j = 0; j < L::NSUB; ++j)
-              tma_load_3d(smem_u32(sQ) + t * L::TILE + j * L::SUB, &tmQ, j * 64, it.head, it.s.q0 + it.row0 + t * 128, bar_q_full + 8 * t);
+              load(smem_u32(sQ) + t * L::TILE + j * L::SUB, &tmQ, j * 64, it.head, it.s.q0 + it.row0 + t * L::ROWS + rank * 128, bar_q_full + 8 * t);
             return true;
           };
-          auto load_kv = [&](const CUtensorMap* tm, int blk) -> bool {
+          auto load_kv = [&](bool is_k, int blk) -> bool {
             const uint32_t st = ring % L::STAGES, use = ring / L::STAGES;
             ++ring;
             if (!mbar_wait(bar_kv_empty + 8 * st, (use & 1) ^ 1)) return false;
-            mbar_arrive_expect_tx(bar_kv_full + 8 * st, static_cast<uint32_t>(L::TILE));
-            for (int j = 0; j < L::NSUB; ++j)
-              tma_load_3d(smem_u32(sKV) + st * L::TILE + j * L::SUB, tm, j * 64, kvh, it.s.k0 + blk * 128, bar_kv_full + 8 * st);
+            if (rank == 0) mbar_arrive_expect_tx(bar_kv_full + 8 * st, static_cast<uint32_t>(L::TILE));
+            const uint32_t dst = smem_u32(sKV) + st * L::KV;
+            if (is_k) {                                          // a pair's CTA: 64 of the keys
+              for (int j = 0; j < L::NSUB; ++j) load(dst + j * L::KSUB, &tmK, j * 64, kvh, it.s.k0 + blk * 128 + rank * 64, bar_kv_full + 8 * st);
+            } else if (PAIR) {                                   // 64 of the 128 columns
+              load(dst, &tmV, rank * 64, kvh, it.s.k0 + blk * 128, bar_kv_full + 8 * st);
+            } else {
+              for (int j = 0; j < L::NSUB; ++j) load(dst + j * L::SUB, &tmV, j * 64, kvh, it.s.k0 + blk * 128, bar_kv_full + 8 * st);
+            }
             return true;
           };
           const int n = max(it.n[0], it.n[1]);
           failed = !load_q(0);
           for (int j = 0; j < n && !failed; ++j) {
-            failed = !load_kv(&tmK, j);
+            failed = !load_kv(true, j);
             if (j == 0 && !failed) failed = !load_q(1);
-            if (!failed) failed = !load_kv(&tmV, j);
+            if (!failed) failed = !load_kv(false, j);
           }
           if (failed) report(p.status, DEV_TIMEOUT_PRODUCER);
         }
         if (__any_sync(0xffffffffu, failed)) break;
       }
-    } else if (warp == 17) {
+    } else if (warp == 17 && rank == 0) {
       // ------------------------------------------------------------------ MMA issuer
-      const uint32_t idesc_s = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, 128, 128);
-      const uint32_t idesc_o = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, 128, D, 0, 1);
+      const uint32_t idesc_s = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, L::ROWS, 128);
+      const uint32_t idesc_o = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, L::ROWS, D, 0, 1);
+      auto commit = [&](uint32_t bar) {
+        if constexpr (PAIR) umma_commit2(bar, 3);
+        else umma_commit(bar);
+      };
       uint32_t ring = 0, qn[2] = {0, 0}, pn[2] = {0, 0};
       // S of tile t = Q_t K^T with the K block of ring position `pos`
       auto scores = [&](int t, uint32_t pos) {
-        const uint32_t kb = smem_u32(sKV) + (pos % L::STAGES) * L::TILE, qb = smem_u32(sQ) + t * L::TILE;
-  #pragma unroll
+        const uint32_t kb = smem_u32(sKV) + (pos % L::STAGES) * L::KV, qb = smem_u32(sQ) + t * L::TILE;
+#pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          const uint32_t off = (k >> 2) * L::SUB + (k & 3) * 32;
-          umma_ss<KIND_BF16>(tmem_base + t * 128, make_smem_desc(qb + off, 16, 1024, SWZ_128B), make_smem_desc(kb + off, 16, 1024, SWZ_128B),
-                             idesc_s, k != 0);
+          const uint64_t qd = make_smem_desc(qb + (k >> 2) * L::SUB + (k & 3) * 32, 16, 1024, SWZ_128B);
+          const uint64_t kd = make_smem_desc(kb + (k >> 2) * L::KSUB + (k & 3) * 32, 16, 1024, SWZ_128B);
+          if constexpr (PAIR) umma_ss2<KIND_BF16>(tmem_base + t * 128, qd, kd, idesc_s, k != 0);
+          else umma_ss<KIND_BF16>(tmem_base + t * 128, qd, kd, idesc_s, k != 0);
         }
-        umma_commit(bar_s_full + 8 * t);
+        commit(bar_s_full + 8 * t);
       };
       auto kv_ready = [&](uint32_t pos) { return mbar_wait(bar_kv_full + 8 * (pos % L::STAGES), (pos / L::STAGES) & 1); };
+      auto p_ready = [&](int t) {
+        if constexpr (PAIR) return mbar_wait_cluster<100u>(bar_p_full + 8 * t, pn[t] & 1);
+        else return mbar_wait(bar_p_full + 8 * t, pn[t] & 1);
+      };
       // the first scores of an item's tile t
       auto first_scores = [&](const Item& it, int t) -> bool {
         if (it.n[t] == 0) return true;
@@ -510,13 +571,13 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         ++qn[t];
         tc_fence_after();
         scores(t, ring);
-        if (it.n[t] == 1) umma_commit(bar_q_empty + 8 * t);
+        if (it.n[t] == 1) commit(bar_q_empty + 8 * t);
         return true;
       };
       Item it = item_of(0);
       if (it.valid && lane == 0) {
         failed = !first_scores(it, 0) || !first_scores(it, 1);
-        if (!failed && max(it.n[0], it.n[1])) umma_commit(bar_kv_empty + 8 * (ring % L::STAGES));
+        if (!failed && max(it.n[0], it.n[1])) commit(bar_kv_empty + 8 * (ring % L::STAGES));
       }
       for (int r = 0; it.valid; ++r) {
         if (__any_sync(0xffffffffu, failed)) break;
@@ -528,35 +589,43 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             const uint32_t kpos = ring + 2 * j + 2, vpos = ring + 2 * j + 1;
             const bool last = j + 1 == n;
             if (last) ring += 2 * n;                               // the next item's first K block is kpos as well
-  #pragma unroll
+            if (PAIR && last && it.tail()) {                       // both CTAs' softmax warps overwrite what follows the sequence in V
+              if (!kv_ready(vpos)) { failed = true; break; }
+              commit(bar_v_tail);
+            }
+#pragma unroll
             for (int t = 0; t < 2; ++t) {
               if (failed) break;
               if (j < it.n[t]) {
-                if (!mbar_wait(bar_p_full + 8 * t, pn[t] & 1) || !kv_ready(vpos)) { failed = true; break; }
+                if (!p_ready(t) || !kv_ready(vpos)) { failed = true; break; }
                 ++pn[t];
                 tc_fence_after();
-                const uint32_t vb = smem_u32(sKV) + (vpos % L::STAGES) * L::TILE;
-  #pragma unroll
+                const uint32_t vb = smem_u32(sKV) + (vpos % L::STAGES) * L::KV;
+#pragma unroll
                 for (int k = 0; k < 8; ++k)                        // 16 keys per MMA
-                  umma_ts_bf16(tmem_base + 256 + t * 128, tmem_base + t * 128 + (k >> 2) * 64 + (k & 3) * 8,
-                               make_smem_desc(vb + k * 16 * 128, L::SUB, 1024, SWZ_128B), idesc_o, !(j == 0 && k == 0));
-                if (j + 1 == it.n[t]) umma_commit(bar_o_full + 8 * t);
+                {
+                  const uint32_t d = tmem_base + 256 + t * 128, a = tmem_base + t * 128 + (k >> 2) * 64 + (k & 3) * 8;
+                  const uint64_t vd = make_smem_desc(vb + k * 16 * 128, L::SUB, 1024, SWZ_128B);
+                  if constexpr (PAIR) umma_ts2_bf16(d, a, vd, idesc_o, !(j == 0 && k == 0));
+                  else umma_ts_bf16(d, a, vd, idesc_o, !(j == 0 && k == 0));
+                }
+                if (j + 1 == it.n[t]) commit(bar_o_full + 8 * t);
               }
               if (j + 1 < it.n[t]) {
                 if (!kv_ready(kpos)) { failed = true; break; }
                 tc_fence_after();
                 scores(t, kpos);
-                if (j + 2 == it.n[t]) umma_commit(bar_q_empty + 8 * t);
+                if (j + 2 == it.n[t]) commit(bar_q_empty + 8 * t);
               }
               if (last && next.valid && !first_scores(next, t)) { failed = true; break; }
             }
             if (failed) break;
-            umma_commit(bar_kv_empty + 8 * (vpos % L::STAGES));
-            if (!last || (next.valid && max(next.n[0], next.n[1]))) umma_commit(bar_kv_empty + 8 * (kpos % L::STAGES));
+            commit(bar_kv_empty + 8 * (vpos % L::STAGES));
+            if (!last || (next.valid && max(next.n[0], next.n[1]))) commit(bar_kv_empty + 8 * (kpos % L::STAGES));
           }
           if (n == 0 && next.valid && !failed) {
             failed = !first_scores(next, 0) || !first_scores(next, 1);
-            if (!failed && max(next.n[0], next.n[1])) umma_commit(bar_kv_empty + 8 * (ring % L::STAGES));
+            if (!failed && max(next.n[0], next.n[1])) commit(bar_kv_empty + 8 * (ring % L::STAGES));
           }
           if (failed) report(p.status, DEV_TIMEOUT_MMA);
         }
@@ -564,35 +633,54 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       }
     }
   }
+  __syncwarp();
   tc_fence_before();
-  __syncthreads();
+  if constexpr (PAIR) cluster_sync_all();                       // nobody uses the peer's memory any more
+  else __syncthreads();
   if (warp == 17) {
     tc_fence_after();
-    tmem_dealloc(tmem_base, 512);
+    if constexpr (PAIR) tmem_dealloc2(tmem_base, 512);
+    else tmem_dealloc(tmem_base, 512);
   }
 }
 
-template <int D>
+template <int D, bool PAIR>
 static cudaError_t prompt_run(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const PromptParams& p, int num_sms,
                               cudaStream_t s) {
-  auto kern = attn_prompt_kernel<D>;
-  cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), PromptLayout<D>::SMEM);
+  using L = PromptLayout<D, PAIR>;
+  auto kern = attn_prompt_kernel<D, PAIR>;
+  cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), L::SMEM);
   if (e != cudaSuccess) return e;
   // what the offsets can come to at most: every sequence may end inside a block
-  const int64_t entries = p.q_tokens / 256 + p.B;
+  const int64_t entries = p.q_tokens / L::ITEM + p.B;
   const int64_t items = entries * p.Hq;
-  const int grid = static_cast<int>(items < num_sms ? items : num_sms);
+  const int units = PAIR ? num_sms / 2 : num_sms;
+  const int grid = static_cast<int>(items < units ? items : units) * (PAIR ? 2 : 1);
   // the list packs a block number into 12 bits
-  const int listed = entries <= AP_MAX_LIST && p.q_tokens <= 256 * 4096LL;
-  kern<<<grid, AP_THREADS, PromptLayout<D>::SMEM, s>>>(tmQ, tmK, tmV, p, listed, static_cast<int>(entries));
-  return cudaGetLastError();
+  const int listed = entries <= AP_MAX_LIST && p.q_tokens <= L::ITEM * 4096LL;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(AP_THREADS);
+  cfg.dynamicSmemBytes = L::SMEM;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = PAIR ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kern, tmQ, tmK, tmV, p, listed, static_cast<int>(entries));
 }
+
+bool attn_prompt_pairs(int D, int64_t q_tokens, int batch) { return D == 128 && q_tokens >= 1024LL * batch; }
 
 cudaError_t launch_attn_prompt(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const PromptParams& p, int num_sms,
                                cudaStream_t s) {
-  if (p.D == 64) return prompt_run<64>(tmQ, tmK, tmV, p, num_sms, s);
-  if (p.D == 96) return prompt_run<96>(tmQ, tmK, tmV, p, num_sms, s);
-  return prompt_run<128>(tmQ, tmK, tmV, p, num_sms, s);
+  if (p.D == 64) return prompt_run<64, false>(tmQ, tmK, tmV, p, num_sms, s);
+  if (p.D == 96) return prompt_run<96, false>(tmQ, tmK, tmV, p, num_sms, s);
+  if (attn_prompt_pairs(p.D, p.q_tokens, p.B)) return prompt_run<128, true>(tmQ, tmK, tmV, p, num_sms, s);
+  return prompt_run<128, false>(tmQ, tmK, tmV, p, num_sms, s);
 }
 
 }  // namespace gc

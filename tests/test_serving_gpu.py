@@ -385,6 +385,20 @@ def test_prompt_more_work_than_ctas(S):
     prompt_case(S, [900, 17, 1500, 333], [1000, 900, 1600, 333], 32, 32, 64, True, seed=4)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("n", [[1024], [1025], [1407], [1536, 1100], [2049, 0, 1300, 1027]])
+def test_prompt_long_sequences_of_wide_heads(S, causal, n):
+    # 1024 tokens a sequence and more on average: pairs of CTAs, 512 rows each
+    prompt_case(S, n, n, 4, 2, 128, causal, seed=len(n) + n[0], tail=40, poison=True)
+
+
+def test_prompt_long_sequences_continued(S):
+    prompt_case(S, [1300, 1, 1800], [1300 + 333, 129, 1700], 3, 3, 128, True, seed=13, tail=5, poison=True)
+    prompt_case(S, [1300, 900, 1800], [0, 40, 2000], 2, 1, 128, False, seed=14)
+    prompt_case(S, [4100], [4100], 20, 4, 128, True, seed=15)
+    prompt_case(S, [1200], [1200], 2, 2, 128, True, seed=16, qscale=30.0)
+
+
 def test_prompt_many_sequences(S):
     # more pieces than the sorted work list holds
     g = torch.Generator().manual_seed(0)
