@@ -14,9 +14,10 @@
 //                    (With one thread per row, two warps per scheduler left its latencies bare: 1148 us for one prompt of
 //                    16384 tokens, 16 heads of 128, against AP_2T us.)
 //   warp 16          TMA producer: Q tiles, and K and V blocks through one ring
-//   warp 17          MMA issuer: S = Q K^T (both operands in shared memory), O += P V (P in tensor memory, V as stored,
-//                    keys along the rows).  The tensor core works off one thread's products in order, which is what lets S of
-//                    the next block overwrite P of this one, and makes "S complete" imply "O complete".
+//   warps 17, 18     MMA issuers of tile 0 / 1: S = Q K^T (both operands in shared memory), O += P V (P in tensor memory, V as
+//                    stored, keys along the rows).  The tensor core works off one thread's products in order, which is what lets
+//                    S of the next block overwrite P of this one, and makes "S complete" imply "O complete".  (One thread for
+//                    both tiles was the bottleneck: its instructions, not the products, took 940 of 1064 us.)
 // Tensor memory: two score tiles of 128 columns and two outputs of D <= 128: all 512 columns.
 //   * The reference m is raised only when a score exceeds it by 2^8 (as in the cache attention): after the first block the
 //     output is almost never touched, and raising it is the softmax warps' own business - no extra role, no extra hand-over.
@@ -62,14 +63,57 @@ __device__ __forceinline__ uint32_t ap_pack(float lo, float hi) {
   const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&b);
 }
-// D[tmem] (+)= A[tmem] * B[smem]: A holds 16-bit elements, two per column
-__device__ __forceinline__ void umma_ts_bf16(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred P;\n\tsetp.ne.b32 P, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, P;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
+// Products issued by one thread, whose instructions are what they cost: a shared-memory descriptor is handed over as its lower
+// word (address and leading offset, of which only the address varies) and put together with its constant upper word inside.
+__host__ __device__ constexpr uint32_t desc_hi(uint32_t sbo_bytes) { return (sbo_bytes >> 4) | 1u << 14 | static_cast<uint32_t>(SWZ_128B) << 29; }
+__device__ __forceinline__ uint32_t desc_lo(uint32_t smem_addr, uint32_t lbo_bytes) { return (smem_addr & 0x3ffffu) >> 4 | (lbo_bytes >> 4) << 16; }
+// D (+)= A B^T, A and B in shared memory (K-major, 128-byte swizzle)
+template <bool PAIR, bool ADD>
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
+  if constexpr (PAIR)
+    asm volatile(
+        "{\n\t.reg .b64 a, b;\n\t.reg .pred P;\n\tmov.b64 a, {%1, %4};\n\tmov.b64 b, {%2, %4};\n\tsetp.ne.b32 P, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, P;\n\t}"
+        ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(desc_hi(1024)), "n"(ADD)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .b64 a, b;\n\t.reg .pred P;\n\tmov.b64 a, {%1, %4};\n\tmov.b64 b, {%2, %4};\n\tsetp.ne.b32 P, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, P;\n\t}"
+        ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(desc_hi(1024)), "n"(ADD)
+        : "memory");
 }
+// D (+)= A B, A in tensor memory (16-bit elements, two per column), B in shared memory
+template <bool PAIR>
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t add) {
+  if constexpr (PAIR)
+    asm volatile(
+        "{\n\t.reg .b64 b;\n\t.reg .pred P;\n\tmov.b64 b, {%2, %4};\n\tsetp.ne.b32 P, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], b, %3, P;\n\t}"
+        ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "r"(desc_hi(1024)), "r"(add)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .b64 b;\n\t.reg .pred P;\n\tmov.b64 b, {%2, %4};\n\tsetp.ne.b32 P, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, P;\n\t}"
+        ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "r"(desc_hi(1024)), "r"(add)
+        : "memory");
+}
+// The bounded wait of the issuing threads: the first try in line, the rest out of line to keep their loops short.  Acquires at
+// cluster scope (arrivals may come from the peer CTA).
+__device__ __noinline__ bool mma_wait_slow(uint32_t bar, uint32_t parity) { return mbar_wait_cluster<100u>(bar, parity); }
+__device__ __forceinline__ bool mma_wait(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred P;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 P, [%1], %2, 100;\n\t"
+      "selp.b32 %0, 1, 0, P;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok || mma_wait_slow(bar, parity);
+}
+
 // 64 columns of a warp's 32 rows, the load and its wait in one statement: the registers are written asynchronously, and
 // nothing may move or spill them in between.
 __device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t (&r)[64]) {
@@ -135,14 +179,6 @@ __device__ __forceinline__ bool tile_any(int t, bool v) {
   return r != 0;
 }
 
-// The same with CTA pairs: each CTA's rows in its own tensor memory, half of B in each CTA's shared memory
-__device__ __forceinline__ void umma_ts2_bf16(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred P;\n\tsetp.ne.b32 P, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, P;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
 // TMA load into this CTA's shared memory that reports to a barrier of the pair's leader
 __device__ __forceinline__ void tma_load_3d_pair(uint32_t smem_dst, const CUtensorMap* m, int x, int y, int z, uint32_t cluster_bar) {
   asm volatile(
@@ -219,7 +255,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     }
     for (int i = 0; i < L::STAGES; ++i) {
       mbar_init(bar_kv_full + 8 * i, 1);
-      mbar_init(bar_kv_empty + 8 * i, 1);
+      mbar_init(bar_kv_empty + 8 * i, 2);                       // both tiles' issuers
     }
     mbar_init(bar_v_tail, 1);
     s_dead[0] = s_dead[1] = 0;
@@ -538,95 +574,88 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         }
         if (__any_sync(0xffffffffu, failed)) break;
       }
-    } else if (warp == 17 && rank == 0) {
-      // ------------------------------------------------------------------ MMA issuer
+    } else if (warp < 19 && rank == 0) {
+      // ------------------------------------------------------------------ MMA issuers, one per tile
+      const int t = warp - 17;
       const uint32_t idesc_s = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, L::ROWS, 128);
       const uint32_t idesc_o = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, L::ROWS, D, 0, 1);
+      const uint32_t d_s = tmem_base + t * 128, d_o = tmem_base + 256 + t * 128;
+      const uint32_t q_lo = desc_lo(smem_u32(sQ) + t * L::TILE, 16), k_lo = desc_lo(smem_u32(sKV), 16), v_lo = desc_lo(smem_u32(sKV), L::SUB);
+      const uint32_t q_full = bar_q_full + 8 * t, q_empty = bar_q_empty + 8 * t, s_full = bar_s_full + 8 * t, p_full = bar_p_full + 8 * t,
+                     o_full = bar_o_full + 8 * t;
       auto commit = [&](uint32_t bar) {
         if constexpr (PAIR) umma_commit2(bar, 3);
         else umma_commit(bar);
       };
-      uint32_t ring = 0, qn[2] = {0, 0}, pn[2] = {0, 0};
-      // S of tile t = Q_t K^T with the K block of ring position `pos`
-      auto scores = [&](int t, uint32_t pos) {
-        const uint32_t kb = smem_u32(sKV) + (pos % L::STAGES) * L::KV, qb = smem_u32(sQ) + t * L::TILE;
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint64_t qd = make_smem_desc(qb + (k >> 2) * L::SUB + (k & 3) * 32, 16, 1024, SWZ_128B);
-          const uint64_t kd = make_smem_desc(kb + (k >> 2) * L::KSUB + (k & 3) * 32, 16, 1024, SWZ_128B);
-          if constexpr (PAIR) umma_ss2<KIND_BF16>(tmem_base + t * 128, qd, kd, idesc_s, k != 0);
-          else umma_ss<KIND_BF16>(tmem_base + t * 128, qd, kd, idesc_s, k != 0);
-        }
-        commit(bar_s_full + 8 * t);
-      };
-      auto kv_ready = [&](uint32_t pos) { return mbar_wait(bar_kv_full + 8 * (pos % L::STAGES), (pos / L::STAGES) & 1); };
-      auto p_ready = [&](int t) {
-        if constexpr (PAIR) return mbar_wait_cluster<100u>(bar_p_full + 8 * t, pn[t] & 1);
-        else return mbar_wait(bar_p_full + 8 * t, pn[t] & 1);
-      };
-      // the first scores of an item's tile t
-      auto first_scores = [&](const Item& it, int t) -> bool {
-        if (it.n[t] == 0) return true;
-        if (!mbar_wait(bar_q_full + 8 * t, qn[t] & 1) || !kv_ready(ring)) return false;
-        ++qn[t];
-        tc_fence_after();
-        scores(t, ring);
-        if (it.n[t] == 1) commit(bar_q_empty + 8 * t);
+      uint32_t ring = 0, qn = 0, pn = 0;
+      auto kv_ready = [&](uint32_t pos) { return mma_wait(bar_kv_full + 8 * (pos % L::STAGES), (pos / L::STAGES) & 1); };
+      auto kv_done = [&](uint32_t pos) { commit(bar_kv_empty + 8 * (pos % L::STAGES)); };
+      // The block of a ring position is done with here, `used` or not.  (Also an issuer that skips it waits until it is there:
+      // else it could get a round of the ring ahead, and its next arrival would stand in for the other issuer's.)
+      auto kv_pass = [&](uint32_t pos, bool used) -> bool {
+        if (!used && !kv_ready(pos)) return false;
+        kv_done(pos);
         return true;
       };
+      // S = Q K^T with the K block of ring position `pos`
+      auto scores = [&](uint32_t pos) -> bool {
+        if (!kv_ready(pos)) return false;
+        tc_fence_after();
+        const uint32_t kb = k_lo + (pos % L::STAGES) * (L::KV >> 4);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t a = q_lo + (((k >> 2) * L::SUB + (k & 3) * 32) >> 4), b = kb + (((k >> 2) * L::KSUB + (k & 3) * 32) >> 4);
+          if (k == 0) mma_ss<PAIR, false>(d_s, a, b, idesc_s);
+          else mma_ss<PAIR, true>(d_s, a, b, idesc_s);
+        }
+        commit(s_full);
+        return true;
+      };
+      // the first scores of an item, whose first K block stands at ring position `ring`
+      auto begin = [&](const Item& it) -> bool {
+        const int n = t ? it.n[1] : it.n[0];
+        if (n) {
+          if (!mma_wait(q_full, qn & 1)) return false;
+          ++qn;
+          if (!scores(ring)) return false;
+          if (n == 1) commit(q_empty);
+        }
+        return !max(it.n[0], it.n[1]) || kv_pass(ring, n != 0);
+      };
       Item it = item_of(0);
-      if (it.valid && lane == 0) {
-        failed = !first_scores(it, 0) || !first_scores(it, 1);
-        if (!failed && max(it.n[0], it.n[1])) commit(bar_kv_empty + 8 * (ring % L::STAGES));
-      }
+      if (it.valid && lane == 0) failed = !begin(it);
       for (int r = 0; it.valid; ++r) {
         if (__any_sync(0xffffffffu, failed)) break;
         const Item next = item_of(r + 1);
-        const int n = max(it.n[0], it.n[1]);
         if (lane == 0) {
+          const int n = t ? it.n[1] : it.n[0], most = max(it.n[0], it.n[1]);
           // ring position of K_j: ring + 2 j, of V_j: ring + 2 j + 1
-          for (int j = 0; j < n && !failed; ++j) {
-            const uint32_t kpos = ring + 2 * j + 2, vpos = ring + 2 * j + 1;
-            const bool last = j + 1 == n;
-            if (last) ring += 2 * n;                               // the next item's first K block is kpos as well
-            if (PAIR && last && it.tail()) {                       // both CTAs' softmax warps overwrite what follows the sequence in V
+          for (int j = 0; j < most; ++j) {
+            const uint32_t vpos = ring + 2 * j + 1;
+            if (j < n) {
               if (!kv_ready(vpos)) { failed = true; break; }
-              commit(bar_v_tail);
-            }
+              // both CTAs' softmax warps overwrite what follows the sequence in V
+              if (PAIR && j + 1 == most && (t == 1 || it.n[1] < most) && it.tail()) commit(bar_v_tail);
+              if (!mma_wait(p_full, pn & 1)) { failed = true; break; }
+              ++pn;
+              tc_fence_after();
+              const uint32_t vb = v_lo + (vpos % L::STAGES) * (L::KV >> 4);
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-              if (failed) break;
-              if (j < it.n[t]) {
-                if (!p_ready(t) || !kv_ready(vpos)) { failed = true; break; }
-                ++pn[t];
-                tc_fence_after();
-                const uint32_t vb = smem_u32(sKV) + (vpos % L::STAGES) * L::KV;
-#pragma unroll
-                for (int k = 0; k < 8; ++k)                        // 16 keys per MMA
-                {
-                  const uint32_t d = tmem_base + 256 + t * 128, a = tmem_base + t * 128 + (k >> 2) * 64 + (k & 3) * 8;
-                  const uint64_t vd = make_smem_desc(vb + k * 16 * 128, L::SUB, 1024, SWZ_128B);
-                  if constexpr (PAIR) umma_ts2_bf16(d, a, vd, idesc_o, !(j == 0 && k == 0));
-                  else umma_ts_bf16(d, a, vd, idesc_o, !(j == 0 && k == 0));
-                }
-                if (j + 1 == it.n[t]) commit(bar_o_full + 8 * t);
-              }
-              if (j + 1 < it.n[t]) {
-                if (!kv_ready(kpos)) { failed = true; break; }
-                tc_fence_after();
-                scores(t, kpos);
-                if (j + 2 == it.n[t]) commit(bar_q_empty + 8 * t);
-              }
-              if (last && next.valid && !first_scores(next, t)) { failed = true; break; }
+              for (int k = 0; k < 8; ++k)                        // 16 keys per product
+                mma_ts<PAIR>(d_o, d_s + (k >> 2) * 64 + (k & 3) * 8, vb + k * 128, idesc_o, k || j);
+              if (j + 1 == n) commit(o_full);
             }
-            if (failed) break;
-            commit(bar_kv_empty + 8 * (vpos % L::STAGES));
-            if (!last || (next.valid && max(next.n[0], next.n[1]))) commit(bar_kv_empty + 8 * (kpos % L::STAGES));
+            if (!kv_pass(vpos, j < n)) { failed = true; break; }
+            if (j + 1 < most) {
+              if (j + 1 < n) {
+                if (!scores(vpos + 1)) { failed = true; break; }
+                if (j + 2 == n) commit(q_empty);
+              }
+              if (!kv_pass(vpos + 1, j + 1 < n)) { failed = true; break; }
+            }
           }
-          if (n == 0 && next.valid && !failed) {
-            failed = !first_scores(next, 0) || !first_scores(next, 1);
-            if (!failed && max(next.n[0], next.n[1])) commit(bar_kv_empty + 8 * (ring % L::STAGES));
-          }
+          ring += 2 * most;
+          if (!failed && next.valid) failed = !begin(next);
           if (failed) report(p.status, DEV_TIMEOUT_MMA);
         }
         it = next;
