@@ -48,7 +48,7 @@ struct PromptLayout {
   static constexpr int STAGES = D == 64 || PAIR ? 8 : 4;
   static constexpr int ROWS = PAIR ? 256 : 128;  // query rows of one of the two tiles (of both CTAs)
   static constexpr int ITEM = 2 * ROWS;
-  static constexpr int BARS = 2 * STAGES + 12;
+  static constexpr int BARS = 2 * STAGES + 14;
   static constexpr int LIST = AP_MAX_LIST * 8;
   static constexpr int STAT = 2 * 2 * 128 * 4;   // one float per thread of the softmax warps
   static constexpr size_t SMEM = 1024 + static_cast<size_t>(2) * TILE + STAGES * KV + LIST + STAT + BARS * 8 + 64;
@@ -234,6 +234,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   uint64_t* bars = reinterpret_cast<uint64_t*>(s_stat + L::STAT / 4);
   const uint32_t b0 = smem_u32(bars);
   const uint32_t bar_q_full = b0, bar_q_empty = b0 + 16, bar_s_full = b0 + 32, bar_p_full = b0 + 48, bar_o_full = b0 + 64;   // [2] each
+  const uint32_t bar_turn = b0 + 16 * (5 + 1) + 16 * L::STAGES;   // [2]: the tile may issue its next batch of products
   const uint32_t bar_v_tail = b0 + 80;                          // pairs: the last V block of an item has arrived in both CTAs
   const uint32_t bar_kv_full = b0 + 96, bar_kv_empty = bar_kv_full + 8 * L::STAGES;
   // A pair: the full barriers of the leader count both CTAs' loads, and its p_full both CTAs' softmax warps; all others are
@@ -252,6 +253,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       mbar_init(bar_s_full + 8 * i, 1);
       mbar_init(bar_p_full + 8 * i, PAIR ? 16 : 8);
       mbar_init(bar_o_full + 8 * i, 1);
+      mbar_init(bar_turn + 8 * i, 1);
     }
     for (int i = 0; i < L::STAGES; ++i) {
       mbar_init(bar_kv_full + 8 * i, 1);
@@ -590,17 +592,13 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       uint32_t ring = 0, qn = 0, pn = 0;
       auto kv_ready = [&](uint32_t pos) { return mma_wait(bar_kv_full + 8 * (pos % L::STAGES), (pos / L::STAGES) & 1); };
       auto kv_done = [&](uint32_t pos) { commit(bar_kv_empty + 8 * (pos % L::STAGES)); };
-      // The block of a ring position is done with here, `used` or not.  (Also an issuer that skips it waits until it is there:
-      // else it could get a round of the ring ahead, and its next arrival would stand in for the other issuer's.)
-      auto kv_pass = [&](uint32_t pos, bool used) -> bool {
-        if (!used && !kv_ready(pos)) return false;
-        kv_done(pos);
-        return true;
-      };
+      // The tiles take turns, one batch of products (O += P V, next S) each: products of both at once would complete both
+      // tiles' scores together and leave the tensor core idle while both softmaxes run.
+      uint32_t turn = 0;
+      auto my_turn = [&]() { return mma_wait(bar_turn + 8 * t, (turn++ & 1) ^ (t == 0)); };
+      auto your_turn = [&]() { mbar_arrive(bar_turn + 8 * (t ^ 1)); };
       // S = Q K^T with the K block of ring position `pos`
-      auto scores = [&](uint32_t pos) -> bool {
-        if (!kv_ready(pos)) return false;
-        tc_fence_after();
+      auto scores = [&](uint32_t pos) {
         const uint32_t kb = k_lo + (pos % L::STAGES) * (L::KV >> 4);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
@@ -609,18 +607,20 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           else mma_ss<PAIR, true>(d_s, a, b, idesc_s);
         }
         commit(s_full);
-        return true;
       };
       // the first scores of an item, whose first K block stands at ring position `ring`
       auto begin = [&](const Item& it) -> bool {
         const int n = t ? it.n[1] : it.n[0];
-        if (n) {
-          if (!mma_wait(q_full, qn & 1)) return false;
-          ++qn;
-          if (!scores(ring)) return false;
+        if (n && !mma_wait(q_full, qn++ & 1)) return false;
+        if (max(it.n[0], it.n[1])) {
+          if (!kv_ready(ring) || !my_turn()) return false;
+          tc_fence_after();
+          if (n) scores(ring);
+          your_turn();
           if (n == 1) commit(q_empty);
+          kv_done(ring);
         }
-        return !max(it.n[0], it.n[1]) || kv_pass(ring, n != 0);
+        return true;
       };
       Item it = item_of(0);
       if (it.valid && lane == 0) failed = !begin(it);
@@ -632,27 +632,26 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           // ring position of K_j: ring + 2 j, of V_j: ring + 2 j + 1
           for (int j = 0; j < most; ++j) {
             const uint32_t vpos = ring + 2 * j + 1;
+            // (Also an issuer that skips a block waits until it is there: else it could get a round of the ring ahead, and its
+            // next arrival would stand in for the other issuer's.)
+            if (!kv_ready(vpos) || (j + 1 < most && !kv_ready(vpos + 1))) { failed = true; break; }
+            // both CTAs' softmax warps overwrite what follows the sequence in V
+            if (PAIR && j + 1 == most && j < n && (t == 1 || it.n[1] < most) && it.tail()) commit(bar_v_tail);
+            if (j < n && !mma_wait(p_full, pn++ & 1)) { failed = true; break; }
+            if (!my_turn()) { failed = true; break; }
+            tc_fence_after();
             if (j < n) {
-              if (!kv_ready(vpos)) { failed = true; break; }
-              // both CTAs' softmax warps overwrite what follows the sequence in V
-              if (PAIR && j + 1 == most && (t == 1 || it.n[1] < most) && it.tail()) commit(bar_v_tail);
-              if (!mma_wait(p_full, pn & 1)) { failed = true; break; }
-              ++pn;
-              tc_fence_after();
               const uint32_t vb = v_lo + (vpos % L::STAGES) * (L::KV >> 4);
 #pragma unroll
               for (int k = 0; k < 8; ++k)                        // 16 keys per product
                 mma_ts<PAIR>(d_o, d_s + (k >> 2) * 64 + (k & 3) * 8, vb + k * 128, idesc_o, k || j);
-              if (j + 1 == n) commit(o_full);
+              if (j + 1 < n) scores(vpos + 1);
+              else commit(o_full);
             }
-            if (!kv_pass(vpos, j < n)) { failed = true; break; }
-            if (j + 1 < most) {
-              if (j + 1 < n) {
-                if (!scores(vpos + 1)) { failed = true; break; }
-                if (j + 2 == n) commit(q_empty);
-              }
-              if (!kv_pass(vpos + 1, j + 1 < n)) { failed = true; break; }
-            }
+            your_turn();
+            kv_done(vpos);
+            if (j + 1 < most) kv_done(vpos + 1);
+            if (j + 2 == n) commit(q_empty);
           }
           ring += 2 * most;
           if (!failed && next.valid) failed = !begin(next);
