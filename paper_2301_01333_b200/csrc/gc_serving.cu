@@ -266,7 +266,7 @@ extern "C" gc_status_t gc_attention_prompt(void* cuda_stream, const gc_attention
     // the stride of an axis of one element is never used: any valid one
     const uint64_t hs = heads == 1 ? d->head_dim : src[i]->head_stride, ts = tokens == 1 ? heads * d->head_dim : src[i]->token_stride;
     if (hs == 0 || ts == 0) REFUSE(GC_ERR_UNSUPPORTED, "%s: q, k and v need strides other than 0", who);
-    st = gc_make_tmap_heads(&tm[i], src[i]->data, d->head_dim, heads, tokens, hs * 2, ts * 2, 64, i == 1 && attn_prompt_pairs(d->head_dim, d->q_tokens, d->batch) ? 64 : 128);
+    st = gc_make_tmap_heads(&tm[i], src[i]->data, d->head_dim, heads, tokens, hs * 2, ts * 2, 64, 128);
     if (st != GC_OK) return st;
   }
   PromptParams p = {};

@@ -4,21 +4,25 @@
 //   O = softmax(scale Q K^T) V, blockwise over 128 keys: with m a running reference, p = 2^(c s - c m), c = scale log2(e),
 //   l = sum p and O = sum p V carried along; when m is raised both are multiplied by 2^(c (m_old - m_new)).
 //
-// Bound by the tensor cores and, as closely, by the exponentials: per 128 x 128 tile of scores with D = 128 two products of
-// 512 clocks each against 16384 exponentials, 16 a clock: 1024 clocks.  The two have to run side by side, so a CTA owns two
-// tiles of 128 query rows (256 neighbouring rows of one head) and alternates: while the softmax warps of one tile turn its
-// scores into probabilities, the tensor core works for the other.
+// Bound by the tensor cores and, as closely, by the exponentials: per 128 x 128 scores with D = 128 two products of 512 clocks
+// each against 16384 exponentials, 16 a clock: 1024 clocks.  The two have to run side by side, so a CTA owns two tiles of 128
+// query rows (256 neighbouring rows of one head) and alternates: while the softmax warps of one tile turn its scores into
+// probabilities, the tensor core works for the other.
 //   warps 0-7, 8-15  softmax of tile 0 / 1, two threads per query row: 64 scores each from tensor memory into registers at
 //                    once, maximum, exponentials, row sum; the bf16 probabilities go back over the scores they came from, as
-//                    the A operand of the second product in tensor memory; at the end of a tile they scale and store its O.
-//                    (With one thread per row, two warps per scheduler left its latencies bare: 1148 us for one prompt of
-//                    16384 tokens, 16 heads of 128, against AP_2T us.)
+//                    the A operand of the second product in tensor memory, in two parts, so that the product with the first
+//                    runs while the second is made; at the end of a tile they scale and store its O
 //   warp 16          TMA producer: Q tiles, and K and V blocks through one ring
 //   warps 17, 18     MMA issuers of tile 0 / 1: S = Q K^T (both operands in shared memory), O += P V (P in tensor memory, V as
 //                    stored, keys along the rows).  The tensor core works off one thread's products in order, which is what lets
-//                    S of the next block overwrite P of this one, and makes "S complete" imply "O complete".  (One thread for
-//                    both tiles was the bottleneck: its instructions, not the products, took 940 of 1064 us.)
+//                    S of the next block overwrite P of this one, and makes "S complete" imply "O complete".  Their batches
+//                    take turns.
 // Tensor memory: two score tiles of 128 columns and two outputs of D <= 128: all 512 columns.
+// How it got there, for one prompt of 16384 tokens, 16 heads of 128 (1.1 TFLOP): one thread per row 1148 us; two threads per row
+// 1064; an issuing thread per tile (one thread's instructions for both were the bottleneck), taking turns (both tiles'
+// products at once complete both scores together, and the tensor core idles while both softmaxes run) 957; P in two parts
+// AP_NOW.  No gain: CTA pairs (M = 256, half of K and V in each CTA); part of the exponentials on the FMA pipe; two score
+// buffers of 64 keys per tile, which takes the hand-over out of the way but makes S slower (N = 64: 1001 us).
 //   * The reference m is raised only when a score exceeds it by 2^8 (as in the cache attention): after the first block the
 //     output is almost never touched, and raising it is the softmax warps' own business - no extra role, no extra hand-over.
 //     The two threads of a row need not compare their maxima for it: one barrier with a vote says whether any row has to.
@@ -38,20 +42,16 @@ constexpr int AP_THREADS = 640;               // five warpgroups; the last two w
 constexpr int AP_MAX_LIST = 1024;                // work list entries kept (and sorted) in shared memory
 constexpr float AP_RAISE = 8.0f;
 
-template <int D, bool PAIR>
+template <int D>
 struct PromptLayout {
   static constexpr int NSUB = (D + 63) / 64;     // 64-element sub-tiles of 128-byte rows
   static constexpr int SUB = 128 * 128;
   static constexpr int TILE = NSUB * SUB;        // 128 rows of Q, K or V
-  static constexpr int KV = PAIR ? TILE / 2 : TILE;      // of one K or V block in this CTA
-  static constexpr int KSUB = PAIR ? SUB / 2 : SUB;      // of one K sub-tile: a pair's CTA holds 64 of the 128 keys
-  static constexpr int STAGES = D == 64 || PAIR ? 8 : 4;
-  static constexpr int ROWS = PAIR ? 256 : 128;  // query rows of one of the two tiles (of both CTAs)
-  static constexpr int ITEM = 2 * ROWS;
+  static constexpr int STAGES = D == 64 ? 8 : 4;
   static constexpr int BARS = 2 * STAGES + 14;
   static constexpr int LIST = AP_MAX_LIST * 8;
   static constexpr int STAT = 2 * 2 * 128 * 4;   // one float per thread of the softmax warps
-  static constexpr size_t SMEM = 1024 + static_cast<size_t>(2) * TILE + STAGES * KV + LIST + STAT + BARS * 8 + 64;
+  static constexpr size_t SMEM = 1024 + static_cast<size_t>(2 + STAGES) * TILE + LIST + STAT + BARS * 8 + 64;
 };
 
 __device__ __forceinline__ float ap_ex2(float x) {
@@ -68,51 +68,25 @@ __device__ __forceinline__ uint32_t ap_pack(float lo, float hi) {
 __host__ __device__ constexpr uint32_t desc_hi(uint32_t sbo_bytes) { return (sbo_bytes >> 4) | 1u << 14 | static_cast<uint32_t>(SWZ_128B) << 29; }
 __device__ __forceinline__ uint32_t desc_lo(uint32_t smem_addr, uint32_t lbo_bytes) { return (smem_addr & 0x3ffffu) >> 4 | (lbo_bytes >> 4) << 16; }
 // D (+)= A B^T, A and B in shared memory (K-major, 128-byte swizzle)
-template <bool PAIR, bool ADD>
+template <bool ADD>
 __device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
-  if constexpr (PAIR)
-    asm volatile(
-        "{\n\t.reg .b64 a, b;\n\t.reg .pred P;\n\tmov.b64 a, {%1, %4};\n\tmov.b64 b, {%2, %4};\n\tsetp.ne.b32 P, %5, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, P;\n\t}"
-        ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(desc_hi(1024)), "n"(ADD)
-        : "memory");
-  else
-    asm volatile(
+  asm volatile(
         "{\n\t.reg .b64 a, b;\n\t.reg .pred P;\n\tmov.b64 a, {%1, %4};\n\tmov.b64 b, {%2, %4};\n\tsetp.ne.b32 P, %5, 0;\n\t"
         "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, P;\n\t}"
         ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(desc_hi(1024)), "n"(ADD)
         : "memory");
 }
 // D (+)= A B, A in tensor memory (16-bit elements, two per column), B in shared memory
-template <bool PAIR>
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t add) {
-  if constexpr (PAIR)
-    asm volatile(
-        "{\n\t.reg .b64 b;\n\t.reg .pred P;\n\tmov.b64 b, {%2, %4};\n\tsetp.ne.b32 P, %5, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], b, %3, P;\n\t}"
-        ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "r"(desc_hi(1024)), "r"(add)
-        : "memory");
-  else
-    asm volatile(
+  asm volatile(
         "{\n\t.reg .b64 b;\n\t.reg .pred P;\n\tmov.b64 b, {%2, %4};\n\tsetp.ne.b32 P, %5, 0;\n\t"
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, P;\n\t}"
         ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "r"(desc_hi(1024)), "r"(add)
         : "memory");
 }
-// The bounded wait of the issuing threads: the first try in line, the rest out of line to keep their loops short.  Acquires at
-// cluster scope (arrivals may come from the peer CTA).
-__device__ __noinline__ bool mma_wait_slow(uint32_t bar, uint32_t parity) { return mbar_wait_cluster<100u>(bar, parity); }
-__device__ __forceinline__ bool mma_wait(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred P;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 P, [%1], %2, 100;\n\t"
-      "selp.b32 %0, 1, 0, P;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok || mma_wait_slow(bar, parity);
-}
+// The bounded wait of the issuing threads: the first try in line, the rest out of line to keep their loops short.
+__device__ __noinline__ bool mma_wait_slow(uint32_t bar, uint32_t parity) { return mbar_wait_prompt(bar, parity); }
+__device__ __forceinline__ bool mma_wait(uint32_t bar, uint32_t parity) { return mbar_try_wait(bar, parity, 100u) || mma_wait_slow(bar, parity); }
 
 // 64 columns of a warp's 32 rows, the load and its wait in one statement: the registers are written asynchronously, and
 // nothing may move or spill them in between.
@@ -179,14 +153,6 @@ __device__ __forceinline__ bool tile_any(int t, bool v) {
   return r != 0;
 }
 
-// TMA load into this CTA's shared memory that reports to a barrier of the pair's leader
-__device__ __forceinline__ void tma_load_3d_pair(uint32_t smem_dst, const CUtensorMap* m, int x, int y, int z, uint32_t cluster_bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];"
-      ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(cluster_bar)
-      : "memory");
-}
-
 // One sequence's rows, from its offsets; offsets that decrease or leave the tensors are cut to size.
 struct Seq {
   int q0, nq, k0, nk;
@@ -204,43 +170,37 @@ __device__ __forceinline__ Seq seq_of(const PromptParams& p, int b) {
 __device__ __forceinline__ int row_limit(const PromptParams& p, const Seq& s, int i) {
   return i >= s.nq ? 0 : p.causal ? max(i + 1 + s.nk - s.nq, 0) : s.nk;
 }
-// 128-key blocks the tile of rows [r0, r0 + rows) needs.
-__device__ __forceinline__ int tile_blocks(const PromptParams& p, const Seq& s, int r0, int rows) {
-  return r0 >= s.nq ? 0 : (row_limit(p, s, min(r0 + rows, s.nq) - 1) + 127) >> 7;
+// 128-key blocks the tile of rows [r0, r0 + 128) needs.
+__device__ __forceinline__ int tile_blocks(const PromptParams& p, const Seq& s, int r0) {
+  return r0 >= s.nq ? 0 : (row_limit(p, s, min(r0 + 127, s.nq - 1)) + 127) >> 7;
 }
 
 struct Item {
   Seq s;
-  int row0, head;                // first of the query rows, within the sequence
+  int row0, head;                // first of the 256 query rows, within the sequence
   int n[2];                      // key blocks of the two tiles
-  // the longer tile's last block reaches past the sequence's end
-  __device__ __forceinline__ bool tail() const { return max(n[0], n[1]) * 128 > s.nk; }
   bool valid;
 };
 }  // namespace
 
-template <int D, bool PAIR>
+template <int D>
 __global__ void __launch_bounds__(AP_THREADS, 1)
 attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                    const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PromptParams p, const int listed, const int most) {
-  using L = PromptLayout<D, PAIR>;
+  using L = PromptLayout<D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sQ = smem;                                           // [2] tiles
   uint8_t* sKV = sQ + 2 * L::TILE;                              // [STAGES] tiles
-  int* s_item = reinterpret_cast<int*>(sKV + L::STAGES * L::KV);      // sequence of each entry, then its block
+  int* s_item = reinterpret_cast<int*>(sKV + L::STAGES * L::TILE);      // sequence of each entry, then its block
   int* s_tmp = s_item + AP_MAX_LIST;
   float* s_stat = reinterpret_cast<float*>(s_tmp + AP_MAX_LIST);        // [tile][half of the columns][row]
   uint64_t* bars = reinterpret_cast<uint64_t*>(s_stat + L::STAT / 4);
   const uint32_t b0 = smem_u32(bars);
-  const uint32_t bar_q_full = b0, bar_q_empty = b0 + 16, bar_s_full = b0 + 32, bar_p_full = b0 + 48, bar_o_full = b0 + 64;   // [2] each
-  const uint32_t bar_turn = b0 + 16 * (5 + 1) + 16 * L::STAGES;   // [2]: the tile may issue its next batch of products
-  const uint32_t bar_v_tail = b0 + 80;                          // pairs: the last V block of an item has arrived in both CTAs
-  const uint32_t bar_kv_full = b0 + 96, bar_kv_empty = bar_kv_full + 8 * L::STAGES;
-  // A pair: the full barriers of the leader count both CTAs' loads, and its p_full both CTAs' softmax warps; all others are
-  // completed in both CTAs.
-  const uint32_t rank = PAIR ? cluster_ctarank() : 0;
-  const int cta = PAIR ? blockIdx.x >> 1 : blockIdx.x, ctas = PAIR ? gridDim.x >> 1 : gridDim.x;
+  // [2] each: per tile; part h of the probabilities of tile t at 8 (2 t + h)
+  const uint32_t bar_q_full = b0, bar_q_empty = b0 + 16, bar_s_full = b0 + 32, bar_p_full = b0 + 48, bar_o_full = b0 + 80;
+  const uint32_t bar_turn = b0 + 96;                            // [2]: the tile may issue its next batch of products
+  const uint32_t bar_kv_full = b0 + 112, bar_kv_empty = bar_kv_full + 8 * L::STAGES;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + L::BARS);
   int* s_total = reinterpret_cast<int*>(tmem_slot + 1);
   volatile int* s_dead = s_total + 1;                           // [2]: a softmax warp of the tile has given up waiting
@@ -251,15 +211,14 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       mbar_init(bar_q_full + 8 * i, 1);
       mbar_init(bar_q_empty + 8 * i, 1);
       mbar_init(bar_s_full + 8 * i, 1);
-      mbar_init(bar_p_full + 8 * i, PAIR ? 16 : 8);
       mbar_init(bar_o_full + 8 * i, 1);
       mbar_init(bar_turn + 8 * i, 1);
     }
+    for (int i = 0; i < 4; ++i) mbar_init(bar_p_full + 8 * i, 8);
     for (int i = 0; i < L::STAGES; ++i) {
       mbar_init(bar_kv_full + 8 * i, 1);
       mbar_init(bar_kv_empty + 8 * i, 2);                       // both tiles' issuers
     }
-    mbar_init(bar_v_tail, 1);
     s_dead[0] = s_dead[1] = 0;
     fence_mbar_init();
     tma_prefetch_desc(&tmQ);
@@ -267,13 +226,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     tma_prefetch_desc(&tmV);
   }
   if (warp == 17) {
-    if constexpr (PAIR) {
-      tmem_alloc2(smem_u32(tmem_slot), 512);
-      tmem_relinquish2();
-    } else {
-      tmem_alloc(smem_u32(tmem_slot), 512);
-      tmem_relinquish();
-    }
+    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_relinquish();
   }
   // ---- the work list
   if (warp == 0) {
@@ -283,7 +237,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       int nb = 0;
       if (b < p.B) {
         const Seq s = seq_of(p, b);
-        nb = (s.nq + L::ITEM - 1) / L::ITEM;
+        nb = (s.nq + 255) / 256;
         if (blockIdx.x == 0 && (p.cu_q[b] != s.q0 || p.cu_q[b + 1] != s.q0 + s.nq || p.cu_k[b] != s.k0 || p.cu_k[b + 1] != s.k0 + s.nk))
           report(p.status, DEV_BAD_OFFSETS);
       }
@@ -302,16 +256,15 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     if (lane == 0) *s_total = total;
   }
   tc_fence_before();
-  if constexpr (PAIR) cluster_sync_all();                       // both CTAs' barriers exist from here on
-  else __syncthreads();
+  __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   const int entries = *s_total;
   if (listed) {
     auto cost = [&](int e) {
       const Seq s = seq_of(p, e >> 12);
-      const int r0 = (e & 4095) * L::ITEM;
-      return tile_blocks(p, s, r0, L::ROWS) + tile_blocks(p, s, r0 + L::ROWS, L::ROWS);
+      const int r0 = (e & 4095) * 256;
+      return tile_blocks(p, s, r0) + tile_blocks(p, s, r0 + 128);
     };
     // costs first (packed above the entry's number so that equal ones keep their order), then each entry's rank
     int mine[(AP_MAX_LIST + AP_THREADS - 1) / AP_THREADS], key[(AP_MAX_LIST + AP_THREADS - 1) / AP_THREADS];
@@ -344,7 +297,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   const int64_t items = static_cast<int64_t>(entries) * p.Hq;
   auto item_of = [&](int r) {
     Item it;
-    const int64_t g = static_cast<int64_t>(r) * ctas + ((r & 1) ? ctas - 1 - cta : cta);
+    const int64_t g = static_cast<int64_t>(r) * gridDim.x + ((r & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
     it.valid = g < items;
     it.n[0] = it.n[1] = 0;
     it.row0 = it.head = 0;
@@ -359,7 +312,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     } else {
       int before = 0;
       for (int s0 = 0; s0 < p.B; s0 += 32) {
-        const int nb = s0 + lane < p.B ? (seq_of(p, s0 + lane).nq + L::ITEM - 1) / L::ITEM : 0;
+        const int nb = s0 + lane < p.B ? (seq_of(p, s0 + lane).nq + 255) / 256 : 0;
         int incl = nb;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -378,9 +331,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       }
     }
     it.s = seq_of(p, b);
-    it.row0 = blk * L::ITEM;
-    it.n[0] = tile_blocks(p, it.s, it.row0, L::ROWS);
-    it.n[1] = tile_blocks(p, it.s, it.row0 + L::ROWS, L::ROWS);
+    it.row0 = blk * 256;
+    it.n[0] = tile_blocks(p, it.s, it.row0);
+    it.n[1] = tile_blocks(p, it.s, it.row0 + 128);
     return it;
   };
 
@@ -396,19 +349,18 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     const uint32_t s_addr = t_lane + t * 128 + half * 64, o_addr = t_lane + 256 + t * 128 + half * (D / 2);
     float* my_stat = s_stat + (t * 2 + half) * 128 + row;
     const float* other_stat = s_stat + (t * 2 + (half ^ 1)) * 128 + row;
-    const uint32_t p_full = PAIR && rank ? mapa_shared(bar_p_full + 8 * t, 0) : bar_p_full + 8 * t;
-    uint32_t ring = 0, sn = 0, on = 0, tn = 0;
+    uint32_t ring = 0, cnt = 0, on = 0;                          // ring positions, this tile's blocks and outputs so far
     const float c = p.c;
     bool leave = false;
     for (int r = 0; !leave; ++r) {
       const Item it = item_of(r);
       if (!it.valid) break;
-      const int my_row = it.row0 + t * L::ROWS + rank * 128 + row;
+      const int my_row = it.row0 + t * 128 + row;
       const int lim = row_limit(p, it.s, my_row), n = it.n[t];
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < n; ++j) {
-        if (!__all_sync(0xffffffffu, mbar_wait(bar_s_full + 8 * t, sn & 1))) failed = true;
-        ++sn;
+        if (!__all_sync(0xffffffffu, mbar_wait(bar_s_full + 8 * t, cnt & 1))) failed = true;
+        ++cnt;
         tc_fence_after();
         uint32_t v[64];
         tmem_ld64(s_addr, v);
@@ -451,46 +403,42 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         }
         const float off = m == -INFINITY ? 0.f : -m * c;
         const uint64_t c2 = pair2(c, c), off2 = pair2(off, off);
-        uint64_t ls[2] = {0, 0};
-        uint32_t w[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          float e0, e1;
-          unpair2(fma2(pair2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), c2, off2), &e0, &e1);
-          e0 = ap_ex2(e0);
-          e1 = ap_ex2(e1);
-          ls[i & 1] = add2(ls[i & 1], pair2(e0, e1));
-          w[i] = ap_pack(e0, e1);
-        }
-        tmem_st32(s_addr, w);
-        float l0, l1;
-        unpair2(add2(ls[0], ls[1]), &l0, &l1);
-        l += l0 + l1;
         if (j * 128 + 128 > it.s.nk) {
-          // the sequence ends inside this block: whatever follows it in V becomes zero (each thread of a row its 64 elements;
-          // a pair's CTA has only 64 in all)
+          // the sequence ends inside this block: whatever follows it in V becomes zero (each thread of a row its 64 elements)
           const uint32_t pos = ring + 2 * j + 1, st = pos % L::STAGES;
-          const uint32_t bar = PAIR ? bar_v_tail : bar_kv_full + 8 * st, parity = PAIR ? tn & 1 : (pos / L::STAGES) & 1;
-          if (!__all_sync(0xffffffffu, mbar_wait(bar, parity))) failed = true;
-          if (!failed && j * 128 + row >= it.s.nk && half < (PAIR ? 1 : L::NSUB)) {
-            uint4* z = reinterpret_cast<uint4*>(sKV + st * L::KV + half * L::SUB + row * 128);
+          if (!__all_sync(0xffffffffu, mbar_wait(bar_kv_full + 8 * st, (pos / L::STAGES) & 1))) failed = true;
+          if (!failed && j * 128 + row >= it.s.nk && half < L::NSUB) {
+            uint4* z = reinterpret_cast<uint4*>(sKV + st * L::TILE + half * L::SUB + row * 128);
 #pragma unroll
             for (int i = 0; i < 8; ++i) z[i] = make_uint4(0, 0, 0, 0);
           }
-          if constexpr (PAIR) asm volatile("fence.acq_rel.cluster;" ::: "memory");
           fence_proxy_async_smem();
         }
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0 && !failed) {
-          if constexpr (PAIR) mbar_arrive_cluster_nomem(p_full);
-          else mbar_arrive(p_full);
+        uint64_t ls[2] = {0, 0};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t w[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float e0, e1;
+            unpair2(fma2(pair2(__uint_as_float(v[h * 32 + 2 * i]), __uint_as_float(v[h * 32 + 2 * i + 1])), c2, off2), &e0, &e1);
+            e0 = ap_ex2(e0);
+            e1 = ap_ex2(e1);
+            ls[i & 1] = add2(ls[i & 1], pair2(e0, e1));
+            w[i] = ap_pack(e0, e1);
+          }
+          tmem_st16(s_addr + h * 16, w);
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0 && !failed) mbar_arrive(bar_p_full + 8 * (2 * t + h));
         }
+        float l0, l1;
+        unpair2(add2(ls[0], ls[1]), &l0, &l1);
+        l += l0 + l1;
       }
       if (leave) break;
       ring += 2 * max(it.n[0], it.n[1]);
-      tn += it.tail();
       const bool store = my_row < it.s.nq;
       __nv_bfloat16* dst = p.o + static_cast<int64_t>(it.s.q0 + my_row) * p.o_tok + static_cast<int64_t>(it.head) * p.o_head + half * (D / 2);
       if (n == 0) {
@@ -537,76 +485,61 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         if (!it.valid) break;
         if (lane == 0) {
           const int kvh = it.head / g;
-          auto load = [&](uint32_t dst, const CUtensorMap* tm, int x, int y, int z, uint32_t bar) {
-            if constexpr (PAIR) tma_load_3d_pair(dst, tm, x, y, z, rank ? mapa_shared(bar, 0) : bar);
-            else tma_load_3d(dst, tm, x, y, z, bar);
-          };
           auto load_q = [&](int t) -> bool {
             if (it.n[t] == 0) return true;
             if (!mbar_wait(bar_q_empty + 8 * t, (qn[t] & 1) ^ 1)) return false;
             ++qn[t];
-            if (rank == 0) mbar_arrive_expect_tx(bar_q_full + 8 * t, static_cast<uint32_t>(PAIR ? 2 * L::TILE : L::TILE));
+            mbar_arrive_expect_tx(bar_q_full + 8 * t, static_cast<uint32_t>(L::TILE));
             for (int j = 0; j < L::NSUB; ++j)
-              load(smem_u32(sQ) + t * L::TILE + j * L::SUB, &tmQ, j * 64, it.head, it.s.q0 + it.row0 + t * L::ROWS + rank * 128, bar_q_full + 8 * t);
+              tma_load_3d(smem_u32(sQ) + t * L::TILE + j * L::SUB, &tmQ, j * 64, it.head, it.s.q0 + it.row0 + t * 128, bar_q_full + 8 * t);
             return true;
           };
-          auto load_kv = [&](bool is_k, int blk) -> bool {
+          auto load_kv = [&](const CUtensorMap* tm, int tile) -> bool {
             const uint32_t st = ring % L::STAGES, use = ring / L::STAGES;
             ++ring;
             if (!mbar_wait(bar_kv_empty + 8 * st, (use & 1) ^ 1)) return false;
-            if (rank == 0) mbar_arrive_expect_tx(bar_kv_full + 8 * st, static_cast<uint32_t>(L::TILE));
-            const uint32_t dst = smem_u32(sKV) + st * L::KV;
-            if (is_k) {                                          // a pair's CTA: 64 of the keys
-              for (int j = 0; j < L::NSUB; ++j) load(dst + j * L::KSUB, &tmK, j * 64, kvh, it.s.k0 + blk * 128 + rank * 64, bar_kv_full + 8 * st);
-            } else if (PAIR) {                                   // 64 of the 128 columns
-              load(dst, &tmV, rank * 64, kvh, it.s.k0 + blk * 128, bar_kv_full + 8 * st);
-            } else {
-              for (int j = 0; j < L::NSUB; ++j) load(dst + j * L::SUB, &tmV, j * 64, kvh, it.s.k0 + blk * 128, bar_kv_full + 8 * st);
-            }
+            mbar_arrive_expect_tx(bar_kv_full + 8 * st, static_cast<uint32_t>(L::TILE));
+            for (int j = 0; j < L::NSUB; ++j)
+              tma_load_3d(smem_u32(sKV) + st * L::TILE + j * L::SUB, tm, j * 64, kvh, it.s.k0 + tile * 128, bar_kv_full + 8 * st);
             return true;
           };
           const int n = max(it.n[0], it.n[1]);
           failed = !load_q(0);
           for (int j = 0; j < n && !failed; ++j) {
-            failed = !load_kv(true, j);
+            failed = !load_kv(&tmK, j);
             if (j == 0 && !failed) failed = !load_q(1);
-            if (!failed) failed = !load_kv(false, j);
+            if (!failed) failed = !load_kv(&tmV, j);
           }
           if (failed) report(p.status, DEV_TIMEOUT_PRODUCER);
         }
         if (__any_sync(0xffffffffu, failed)) break;
       }
-    } else if (warp < 19 && rank == 0) {
+    } else if (warp < 19) {
       // ------------------------------------------------------------------ MMA issuers, one per tile
       const int t = warp - 17;
-      const uint32_t idesc_s = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, L::ROWS, 128);
-      const uint32_t idesc_o = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, L::ROWS, D, 0, 1);
+      const uint32_t idesc_s = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, 128, 128);
+      const uint32_t idesc_o = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, 128, D, 0, 1);
       const uint32_t d_s = tmem_base + t * 128, d_o = tmem_base + 256 + t * 128;
       const uint32_t q_lo = desc_lo(smem_u32(sQ) + t * L::TILE, 16), k_lo = desc_lo(smem_u32(sKV), 16), v_lo = desc_lo(smem_u32(sKV), L::SUB);
-      const uint32_t q_full = bar_q_full + 8 * t, q_empty = bar_q_empty + 8 * t, s_full = bar_s_full + 8 * t, p_full = bar_p_full + 8 * t,
+      const uint32_t q_full = bar_q_full + 8 * t, q_empty = bar_q_empty + 8 * t, s_full = bar_s_full + 8 * t, p_full = bar_p_full + 16 * t,
                      o_full = bar_o_full + 8 * t;
-      auto commit = [&](uint32_t bar) {
-        if constexpr (PAIR) umma_commit2(bar, 3);
-        else umma_commit(bar);
-      };
       uint32_t ring = 0, qn = 0, pn = 0;
       auto kv_ready = [&](uint32_t pos) { return mma_wait(bar_kv_full + 8 * (pos % L::STAGES), (pos / L::STAGES) & 1); };
-      auto kv_done = [&](uint32_t pos) { commit(bar_kv_empty + 8 * (pos % L::STAGES)); };
-      // The tiles take turns, one batch of products (O += P V, next S) each: products of both at once would complete both
-      // tiles' scores together and leave the tensor core idle while both softmaxes run.
+      auto kv_done = [&](uint32_t pos) { umma_commit(bar_kv_empty + 8 * (pos % L::STAGES)); };
+      // The tiles take turns, one batch of products (O += P V, next S) each.
       uint32_t turn = 0;
       auto my_turn = [&]() { return mma_wait(bar_turn + 8 * t, (turn++ & 1) ^ (t == 0)); };
       auto your_turn = [&]() { mbar_arrive(bar_turn + 8 * (t ^ 1)); };
       // S = Q K^T with the K block of ring position `pos`
       auto scores = [&](uint32_t pos) {
-        const uint32_t kb = k_lo + (pos % L::STAGES) * (L::KV >> 4);
+        const uint32_t kb = k_lo + (pos % L::STAGES) * (L::TILE >> 4);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          const uint32_t a = q_lo + (((k >> 2) * L::SUB + (k & 3) * 32) >> 4), b = kb + (((k >> 2) * L::KSUB + (k & 3) * 32) >> 4);
-          if (k == 0) mma_ss<PAIR, false>(d_s, a, b, idesc_s);
-          else mma_ss<PAIR, true>(d_s, a, b, idesc_s);
+          const uint32_t off = ((k >> 2) * L::SUB + (k & 3) * 32) >> 4;
+          if (k == 0) mma_ss<false>(d_s, q_lo + off, kb + off, idesc_s);
+          else mma_ss<true>(d_s, q_lo + off, kb + off, idesc_s);
         }
-        commit(s_full);
+        umma_commit(s_full);
       };
       // the first scores of an item, whose first K block stands at ring position `ring`
       auto begin = [&](const Item& it) -> bool {
@@ -617,7 +550,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           tc_fence_after();
           if (n) scores(ring);
           your_turn();
-          if (n == 1) commit(q_empty);
+          if (n == 1) umma_commit(q_empty);
           kv_done(ring);
         }
         return true;
@@ -635,23 +568,25 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             // (Also an issuer that skips a block waits until it is there: else it could get a round of the ring ahead, and its
             // next arrival would stand in for the other issuer's.)
             if (!kv_ready(vpos) || (j + 1 < most && !kv_ready(vpos + 1))) { failed = true; break; }
-            // both CTAs' softmax warps overwrite what follows the sequence in V
-            if (PAIR && j + 1 == most && j < n && (t == 1 || it.n[1] < most) && it.tail()) commit(bar_v_tail);
-            if (j < n && !mma_wait(p_full, pn++ & 1)) { failed = true; break; }
+            if (j < n && !mma_wait(p_full, pn & 1)) { failed = true; break; }
             if (!my_turn()) { failed = true; break; }
             tc_fence_after();
             if (j < n) {
-              const uint32_t vb = v_lo + (vpos % L::STAGES) * (L::KV >> 4);
+              const uint32_t vb = v_lo + (vpos % L::STAGES) * (L::TILE >> 4);
+              // 16 keys per product; each thread of a row makes 64 keys' probabilities, 32 of them in the first part
 #pragma unroll
-              for (int k = 0; k < 8; ++k)                        // 16 keys per product
-                mma_ts<PAIR>(d_o, d_s + (k >> 2) * 64 + (k & 3) * 8, vb + k * 128, idesc_o, k || j);
+              for (int k = 0; k < 8; k += (k & 1) ? 3 : 1) mma_ts(d_o, d_s + (k >> 2) * 64 + (k & 1) * 8, vb + k * 128, idesc_o, k || j);
+              if (!mma_wait(p_full + 8, pn++ & 1)) { failed = true; break; }
+              tc_fence_after();
+#pragma unroll
+              for (int k = 2; k < 8; k += (k & 1) ? 3 : 1) mma_ts(d_o, d_s + (k >> 2) * 64 + 16 + (k & 1) * 8, vb + k * 128, idesc_o, 1);
               if (j + 1 < n) scores(vpos + 1);
-              else commit(o_full);
+              else umma_commit(o_full);
             }
             your_turn();
             kv_done(vpos);
             if (j + 1 < most) kv_done(vpos + 1);
-            if (j + 2 == n) commit(q_empty);
+            if (j + 2 == n) umma_commit(q_empty);
           }
           ring += 2 * most;
           if (!failed && next.valid) failed = !begin(next);
@@ -663,52 +598,34 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   }
   __syncwarp();
   tc_fence_before();
-  if constexpr (PAIR) cluster_sync_all();                       // nobody uses the peer's memory any more
-  else __syncthreads();
+  __syncthreads();
   if (warp == 17) {
     tc_fence_after();
-    if constexpr (PAIR) tmem_dealloc2(tmem_base, 512);
-    else tmem_dealloc(tmem_base, 512);
+    tmem_dealloc(tmem_base, 512);
   }
 }
 
-template <int D, bool PAIR>
+template <int D>
 static cudaError_t prompt_run(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const PromptParams& p, int num_sms,
                               cudaStream_t s) {
-  using L = PromptLayout<D, PAIR>;
-  auto kern = attn_prompt_kernel<D, PAIR>;
-  cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), L::SMEM);
+  auto kern = attn_prompt_kernel<D>;
+  cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), PromptLayout<D>::SMEM);
   if (e != cudaSuccess) return e;
   // what the offsets can come to at most: every sequence may end inside a block
-  const int64_t entries = p.q_tokens / L::ITEM + p.B;
+  const int64_t entries = p.q_tokens / 256 + p.B;
   const int64_t items = entries * p.Hq;
-  const int units = PAIR ? num_sms / 2 : num_sms;
-  const int grid = static_cast<int>(items < units ? items : units) * (PAIR ? 2 : 1);
+  const int grid = static_cast<int>(items < num_sms ? items : num_sms);
   // the list packs a block number into 12 bits
-  const int listed = entries <= AP_MAX_LIST && p.q_tokens <= L::ITEM * 4096LL;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(grid));
-  cfg.blockDim = dim3(AP_THREADS);
-  cfg.dynamicSmemBytes = L::SMEM;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = PAIR ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kern, tmQ, tmK, tmV, p, listed, static_cast<int>(entries));
+  const int listed = entries <= AP_MAX_LIST && p.q_tokens <= 256 * 4096LL;
+  kern<<<grid, AP_THREADS, PromptLayout<D>::SMEM, s>>>(tmQ, tmK, tmV, p, listed, static_cast<int>(entries));
+  return cudaGetLastError();
 }
-
-bool attn_prompt_pairs(int D, int64_t q_tokens, int batch) { return D == 128 && q_tokens >= 1024LL * batch; }
 
 cudaError_t launch_attn_prompt(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const PromptParams& p, int num_sms,
                                cudaStream_t s) {
-  if (p.D == 64) return prompt_run<64, false>(tmQ, tmK, tmV, p, num_sms, s);
-  if (p.D == 96) return prompt_run<96, false>(tmQ, tmK, tmV, p, num_sms, s);
-  if (attn_prompt_pairs(p.D, p.q_tokens, p.B)) return prompt_run<128, true>(tmQ, tmK, tmV, p, num_sms, s);
-  return prompt_run<128, false>(tmQ, tmK, tmV, p, num_sms, s);
+  if (p.D == 64) return prompt_run<64>(tmQ, tmK, tmV, p, num_sms, s);
+  if (p.D == 96) return prompt_run<96>(tmQ, tmK, tmV, p, num_sms, s);
+  return prompt_run<128>(tmQ, tmK, tmV, p, num_sms, s);
 }
 
 }  // namespace gc

@@ -50,9 +50,7 @@ struct PromptParams {
   const int* cu_k;
   uint32_t* status;
 };
-// Whether pairs of CTAs take these prompts.
-bool attn_prompt_pairs(int D, int64_t q_tokens, int batch);
-// tmQ / tmK / tmV: 3-D maps (head dimension, heads, tokens), boxes of 64 x 1 x 128 (K for pairs: 64 x 1 x 64), 128-byte swizzle
+// tmQ / tmK / tmV: 3-D maps (head dimension, heads, tokens), boxes of 64 x 1 x 128, 128-byte swizzle
 cudaError_t launch_attn_prompt(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const PromptParams& p,
                                int num_sms, cudaStream_t s);
 
