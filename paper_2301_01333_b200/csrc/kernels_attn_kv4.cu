@@ -29,7 +29,7 @@
 //   * One wave of CTAs that share all the work out equally: the 128-token blocks of every (sequence, head, chunk of columns)
 //     stand in one row, of which each CTA takes an equal stretch, however unlike the lengths are.  Where a stretch ends
 //     inside a sequence, the pieces are joined by a second small kernel in their order.  (Against one CTA per 2048 tokens
-//     of a sequence: 97 us became AK_SK us for 64 ragged sequences up to 8192 tokens, a sixth of it having been the tail.)
+//     of a sequence: with equal costs for unlike pieces 97 us, so 88 for 64 ragged sequences up to 8192 tokens.)
 //   * The running maximum is a reference that is only raised when a score exceeds it by 2^8: one vote per tile instead
 //     of a reduction, and the sums stay far inside fp32.
 #include <cuda_fp16.h>
@@ -663,25 +663,33 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
   uint8_t* smem = reinterpret_cast<uint8_t*>(smem_u4);
 
   const int per_seq = p.Hk * p.col_chunks;
-  // my stretch of the row of blocks, and the sequence it begins in
-  int64_t before;
-  const int64_t total = blocks_before(p, 0, &before) * per_seq;
-  if (blockIdx.x == 0 && threadIdx.x < 32) {
-    for (int s = threadIdx.x; s < p.B; s += 32)
-      if (p.lengths[s] < 0 || p.lengths[s] > p.max_len) report(p.status, DEV_BAD_LENGTH);
-  }
-  const int64_t ctas = min(static_cast<int64_t>(gridDim.x), total);          // none is left without a block
-  if (blockIdx.x >= ctas) return;
-  int64_t cur = total * blockIdx.x / ctas, left = total * (blockIdx.x + 1) / ctas - cur;
-  int b = 0;
-  {
-    int64_t skipped;
+  int b, u, len, nb, k0 = 0;                                     // sequence, (head, chunk), its length, blocks, first block of mine
+  int64_t left;                                                  // blocks to do
+  if (p.block >= p.max_len) {                                    // nothing is split: a CTA per (sequence, head, chunk)
+    b = blockIdx.x / per_seq;
+    u = blockIdx.x - b * per_seq;
+    if (u == 0 && threadIdx.x == 0 && (p.lengths[b] < 0 || p.lengths[b] > p.max_len)) report(p.status, DEV_BAD_LENGTH);
+    len = length_of(p, b);
+    left = nb = blocks_of(p, len);
+  } else {
+    // my stretch of the row of blocks, and the sequence it begins in
+    int64_t before;
+    const int64_t total = blocks_before(p, 0, &before) * per_seq;
+    if (blockIdx.x == 0 && threadIdx.x < 32) {
+      for (int s = threadIdx.x; s < p.B; s += 32)
+        if (p.lengths[s] < 0 || p.lengths[s] > p.max_len) report(p.status, DEV_BAD_LENGTH);
+    }
+    const int64_t ctas = min(static_cast<int64_t>(gridDim.x), total);        // none is left without a block
+    if (blockIdx.x >= ctas) return;
+    int64_t cur = total * blockIdx.x / ctas, skipped;
+    left = total * (blockIdx.x + 1) / ctas - cur;
     b = sequence_at(p, cur / per_seq, &skipped);
     cur -= skipped * per_seq;                                    // from here on relative to the sequence's first block
+    len = length_of(p, b);
+    nb = blocks_of(p, len);
+    u = static_cast<int>(cur / nb);
+    k0 = static_cast<int>(cur - static_cast<int64_t>(u) * nb);
   }
-  int len = length_of(p, b);
-  int nb = blocks_of(p, len);
-  int u = static_cast<int>(cur / nb), k0 = static_cast<int>(cur - static_cast<int64_t>(u) * nb);
   for (; left > 0;) {
     const int kn = static_cast<int>(min(static_cast<int64_t>(nb - k0), left));
     const int first = max(k0 - AK_START, 0), behind = k0 + kn - AK_START;

@@ -21,7 +21,7 @@
 // How it got there, for one prompt of 16384 tokens, 16 heads of 128 (1.1 TFLOP): one thread per row 1148 us; two threads per row
 // 1064; an issuing thread per tile (one thread's instructions for both were the bottleneck), taking turns (both tiles'
 // products at once complete both scores together, and the tensor core idles while both softmaxes run) 957; P in two parts
-// AP_NOW.  No gain: CTA pairs (M = 256, half of K and V in each CTA); part of the exponentials on the FMA pipe; two score
+// 917 (1200 TFLOP/s).  No gain: CTA pairs (M = 256, half of K and V in each CTA); part of the exponentials on the FMA pipe; two score
 // buffers of 64 keys per tile, which takes the hand-over out of the way but makes S slower (N = 64: 1001 us).
 //   * The reference m is raised only when a score exceeds it by 2^8 (as in the cache attention): after the first block the
 //     output is almost never touched, and raising it is the softmax warps' own business - no extra role, no extra hand-over.
@@ -260,7 +260,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   const int entries = *s_total;
-  if (listed) {
+  const int64_t items = static_cast<int64_t>(entries) * p.Hq;
+  const bool sorted = listed && items > gridDim.x;              // (with one item per CTA at most there is no order to keep)
+  const int* list = sorted ? s_item : s_tmp;
+  if (sorted) {
     auto cost = [&](int e) {
       const Seq s = seq_of(p, e >> 12);
       const int r0 = (e & 4095) * 256;
@@ -294,7 +297,6 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     __syncthreads();
   }
   // Item number r of this CTA; called by whole warps.
-  const int64_t items = static_cast<int64_t>(entries) * p.Hq;
   auto item_of = [&](int r) {
     Item it;
     const int64_t g = static_cast<int64_t>(r) * gridDim.x + ((r & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
@@ -307,8 +309,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     it.head = static_cast<int>(g - static_cast<int64_t>(e) * p.Hq);
     int b = 0, blk = 0;
     if (listed) {
-      b = s_item[e] >> 12;
-      blk = s_item[e] & 4095;
+      b = list[e] >> 12;
+      blk = list[e] & 4095;
     } else {
       int before = 0;
       for (int s0 = 0; s0 < p.B; s0 += 32) {
