@@ -434,3 +434,205 @@ def test_prompt_offsets_out_of_bounds_are_reported(S):
         S.attention_prompt(q, q, q, torch.tensor(cu, dtype=torch.int32, device=DEV), status=status)
         with pytest.raises(S.GcError, match="offsets"):
             S.query_status(status)
+
+
+# ------------------------------------------------------------------------------------------------ together, streams, graphs
+class Block:
+    """An attention block as a server would run it: projections are given; norm and rotation, cache, attention."""
+
+    def __init__(self, S, hq, hk, d, page, pages, group, seed):
+        g = gen(seed)
+        self.S, self.hq, self.hk, self.d, self.page = S, hq, hk, d, page
+        self.cache = S.KV4Cache.allocate(pages, page, hk, d, group)
+        self.inv = S.rotary_inv_freq(d, scaling="bands", factor=4.0, original_length=256, device=DEV)
+        self.qw, self.kw = 1 + 0.1 * randn(d, g=g, dtype=torch.bfloat16), 1 + 0.1 * randn(d, g=g, dtype=torch.bfloat16)
+
+    def turn(self, qkv, pos):
+        q, k = self.S.qk_norm_rope(qkv[:, :self.hq], qkv[:, self.hq:self.hq + self.hk], pos, self.inv, self.qw, self.kw)
+        return q, k, qkv[:, self.hq + self.hk:]
+
+
+@pytest.mark.parametrize("d,group,hq,hk", [(128, 32, 8, 2), (64, 64, 12, 12), (96, 32, 6, 1)])
+def test_block_prompt_then_steps(S, d, group, hq, hk):
+    """Two prompts, then three steps of one token and one of two: each query's output against 64-bit attention over what
+    the cache holds (the prompt's own attention over the values read back from it), from the same rotated queries."""
+    g = gen(40 + d)
+    page, lens = 16, [70, 33]
+    blk = Block(S, hq, hk, d, page, 16, group, 41)
+    table = torch.tensor([[3, 1, 4, 15, 9, 2], [6, 5, 8, 7, 0, 10]], dtype=torch.int32, device=DEV)
+
+    def slots(b, first, n):
+        t = torch.arange(first, first + n, device=DEV)
+        return table[b, t // page].long() * page + t % page
+    # prompts
+    qkv = randn(sum(lens), hq + 2 * hk, d, g=g, dtype=torch.bfloat16)
+    pos = torch.cat([torch.arange(n, device=DEV) for n in lens])
+    where = torch.cat([slots(b, 0, n) for b, n in enumerate(lens)])
+    q, k, v = blk.turn(qkv, pos)
+    blk.cache.append(k, v, where)
+    k_held, v_held = blk.cache.read(where)
+    cu = torch.tensor([0, lens[0], sum(lens)], dtype=torch.int32, device=DEV)
+    status = S.new_status(DEV)
+    out = S.attention_prompt(q, k_held, v_held, cu, status=status)
+    S.query_status(status)
+    start = 0
+    for b, n in enumerate(lens):
+        for h in range(hq):
+            kk, vv = k_held[start:start + n, h // (hq // hk)].double(), v_held[start:start + n, h // (hq // hk)].double()
+            ref, size = R.head_all(q[start:start + n, h].double(), kk, vv, torch.arange(1, n + 1, device=DEV), d ** -0.5)
+            expo = d ** -0.5 * (q[start:start + n, h].double().abs() @ kk.abs().T).amax(-1, keepdim=True) * (d + 4) * U32 + 4 * U32
+            within(out[start:start + n, h], ref, (2 * U[torch.bfloat16] + 2 * expo + 100 * U32) * size)
+        start += n
+    # steps
+    for n in (1, 1, 1, 2):
+        qkv = randn(2 * n, hq + 2 * hk, d, g=g, dtype=torch.bfloat16)
+        pos = torch.cat([torch.arange(m, m + n, device=DEV) for m in lens])
+        q, k, v = blk.turn(qkv, pos)
+        blk.cache.append(k, v, torch.cat([slots(b, m, n) for b, m in enumerate(lens)]))
+        lens = [m + n for m in lens]
+        q = q.unflatten(0, (2, n))
+        out = blk.cache.attend(q, table, torch.tensor(lens, dtype=torch.int32, device=DEV))
+        ref, tol = attend_reference(blk.cache, q, table, lens, d ** -0.5, group)
+        within(out, ref, tol)
+    blk.cache.query_status()
+
+
+def _step_inputs(S, seed, t=64, hq=8, hk=2, d=128, page=32):
+    g = gen(seed)
+    blk = Block(S, hq, hk, d, page, 400, 64, seed)
+    lens = torch.randint(2000, 2600, (3,), generator=g, device=DEV).to(torch.int32)
+    table = torch.randperm(400, generator=g, device=DEV).to(torch.int32)[:300].reshape(3, 100)
+    qkv = randn(3, hq + 2 * hk, d, g=g, dtype=torch.bfloat16)
+    for codes, params in ((blk.cache.k_codes, blk.cache.k_params), (blk.cache.v_codes, blk.cache.v_params)):
+        codes.copy_(torch.randint(0, 256, codes.shape, generator=g, device=DEV, dtype=torch.uint8))
+        params[..., 0] = -1 + 0.1 * randn(*params.shape[:-1], g=g)
+        params[..., 1] = 0.1
+    prompt = randn(700, hq + 2 * hk, d, g=g, dtype=torch.bfloat16)
+    cu = torch.tensor([0, 300, 301, 700], dtype=torch.int32, device=DEV)
+
+    def step():
+        q, k, v = blk.turn(qkv, (lens - 1).long())
+        last = (lens - 1).long()
+        blk.cache.append(k, v, table.gather(1, (last // page)[:, None])[:, 0].long() * page + last % page)
+        kr, vr = blk.cache.read(last)
+        o = blk.cache.attend(q[:, None], table, lens, max_length=3200)
+        p = S.attention_prompt(prompt[:, :hq], prompt[:, hq:hq + hk], prompt[:, hq + hk:], cu)
+        return [q, k, kr, vr, o, p]
+    return step, qkv, blk
+
+
+def test_two_captured_graphs_share_nothing(S):
+    steps = [_step_inputs(S, s) for s in (51, 52)]
+    want = [[x.clone() for x in step()] for step, _, _ in steps]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for step, _, _ in steps:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(step())
+        graphs.append(g)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for rep in range(3):
+        for o in outs:
+            for x in o:
+                x.fill_(math.nan)
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):                        # both at once, on streams of their own
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for o, w in zip(outs, want):
+            assert all(torch.equal(x, y) for x, y in zip(o, w))
+    for (_, qkv, blk), o, g, w in zip(steps, outs, graphs, want):   # a replay sees new inputs
+        qkv.copy_(-qkv)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o[0], -w[0]) and not torch.equal(o[4], w[4])
+        blk.cache.query_status()
+
+
+def test_calls_on_a_stream_of_their_own(S):
+    step, qkv, _ = _step_inputs(S, 61)
+    want = [x.clone() for x in step()]
+    real = qkv.clone()
+    qkv.zero_()
+    step()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+        qkv.copy_(real)                                          # a launch on another stream would overtake this, and see zeros
+        got = step()
+    s.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+def test_results_do_not_depend_on_the_run(S):
+    step, _, _ = _step_inputs(S, 71)
+    first = [x.clone() for x in step()]
+    for _ in range(5):
+        assert all(torch.equal(x, y) for x, y in zip(step(), first))
+
+
+def test_cache_of_more_than_two_to_the_32_bytes(S):
+    # codes beyond 4 GB: the last pages of a cache of 270000 pages of 256 tokens, one head of 128
+    free, _ = torch.cuda.mem_get_info()
+    if free < 24 << 30:
+        pytest.skip("not enough memory")
+    pages, page = 270000, 256
+    assert pages * page * 64 > 1 << 32
+    cache = S.KV4Cache.allocate(pages, page, 1, 128, 128)
+    g = gen(81)
+    n = 300
+    k, v = randn(n, 1, 128, g=g, dtype=torch.bfloat16), randn(n, 1, 128, g=g, dtype=torch.bfloat16)
+    table = torch.tensor([[pages - 1, pages - 3]], dtype=torch.int32, device=DEV)
+    t = torch.arange(n, device=DEV)
+    slots = table[0, t // page].long() * page + t % page
+    cache.append(k, v, slots)
+    code, lo, scale = R.quantise(k, 128)
+    kr, _ = cache.read(slots, torch.float32)
+    assert torch.equal(kr.double(), (lo + code * scale).float().double())
+    q = randn(1, 1, 4, 128, g=g, dtype=torch.bfloat16)
+    out = cache.attend(q, table, torch.tensor([n], dtype=torch.int32, device=DEV))
+    ref, tol = attend_reference(cache, q, table, [n], 128 ** -0.5, 128)
+    within(out, ref, tol)
+    cache.query_status()
+
+
+def test_refusals_leave_everything_as_it_was(S):
+    cache = S.KV4Cache.allocate(4, 16, 2, 64, 32)
+    x = torch.ones(3, 2, 64, device=DEV, dtype=torch.bfloat16)
+    slots = torch.arange(3, device=DEV)
+    q = torch.ones(1, 1, 4, 64, device=DEV, dtype=torch.bfloat16)
+    table, lens = torch.zeros(1, 4, dtype=torch.int32, device=DEV), torch.ones(1, dtype=torch.int32, device=DEV)
+    cu = torch.tensor([0, 3], dtype=torch.int32, device=DEV)
+    out = torch.full((3, 2, 64), 5.0, device=DEV, dtype=torch.bfloat16)
+    inv = S.rotary_inv_freq(64, device=DEV)
+    V, T, G = ValueError, TypeError, S.GcError
+    cases = [
+        (V, lambda: cache.append(x[:2], x, slots)), (V, lambda: cache.append(x, x.float(), slots)), (T, lambda: cache.append(x.half(), x.half(), slots)),
+        (V, lambda: cache.append(x, x, slots.int())), (V, lambda: cache.append(x.cpu(), x, slots)), (V, lambda: cache.append(x, x, slots[None])),
+        (V, lambda: cache.append(x.transpose(1, 2).contiguous().transpose(1, 2), x, slots)),
+        (V, lambda: cache.read(slots, k_out=out[:1].expand(3, 2, 64), v_out=out)), (T, lambda: cache.read(slots, torch.float16)),
+        (V, lambda: cache.attend(q.float(), table, lens)), (V, lambda: cache.attend(q[..., :32], table, lens)), (V, lambda: cache.attend(q, table.long(), lens)),
+        (V, lambda: cache.attend(q, table, lens.long())), (V, lambda: cache.attend(q, table.expand(2, 4), lens)), (G, lambda: cache.attend(q, table, lens, max_length=65)),
+        (G, lambda: cache.attend(q, table, lens, max_length=-1)), (G, lambda: cache.attend(q, table, lens, scale=0.0)), (G, lambda: cache.attend(q, table, lens, scale=math.nan)),
+        (G, lambda: cache.attend(q[:, :, :3], table, lens)), (G, lambda: cache.attend(q.expand(1, 17, 4, 64), table, lens)),
+        (V, lambda: cache.attend(q, table, lens, out=q[:, :, :1].expand(1, 1, 4, 64))),
+        (G, lambda: cache.attend(torch.ones(1, 1, 4, 65, device=DEV, dtype=torch.bfloat16)[..., 1:], table, lens)),
+        (V, lambda: S.attention_prompt(x.float(), x, x, cu)), (V, lambda: S.attention_prompt(x, x[:, :, :32], x, cu)), (G, lambda: S.attention_prompt(x, x, x, cu, scale=-1.0)),
+        (V, lambda: S.attention_prompt(x, x, x, cu.long())), (V, lambda: S.attention_prompt(x, x, x, cu, cu[:1])), (V, lambda: S.attention_prompt(x, x, x, cu, out=out[:1])),
+        (V, lambda: S.attention_prompt(x, x, x, cu, out=out[:1].expand(3, 2, 64))), (G, lambda: S.attention_prompt(x[..., :32], x[..., :32], x[..., :32], cu)),
+        (G, lambda: S.attention_prompt(x, torch.ones(3, 3, 64, device=DEV, dtype=torch.bfloat16), torch.ones(3, 3, 64, device=DEV, dtype=torch.bfloat16), cu)),
+        (G, lambda: S.attention_prompt(x, x[:, :1].expand(3, 2, 64), x, cu)),
+        (V, lambda: S.qk_norm_rope(x, x, slots.int(), inv)), (V, lambda: S.qk_norm_rope(x, x.float(), slots, inv)), (T, lambda: S.qk_norm_rope(x.half(), x.half(), slots, inv)),
+        (G, lambda: S.qk_norm_rope(x, x, slots, torch.ones(33, device=DEV))), (G, lambda: S.qk_norm_rope(x, x, slots, inv, eps=-1.0)),
+        (V, lambda: S.qk_norm_rope(x, x, slots, inv, x[0, 0].float())), (V, lambda: S.qk_norm_rope(x, x, slots, inv, q_out=out[:1].expand(3, 2, 64))),
+        (G, lambda: S.qk_norm_rope(x[..., :63], x[..., :63], slots, inv[:8])), (T, lambda: S.qk_norm_rope(x, None, slots, inv)),
+    ]
+    for i, (kind, call) in enumerate(cases):
+        with pytest.raises(kind):
+            call()
+            print("case", i, "was not refused")
+    assert (cache.k_codes == 0).all() and (cache.v_params == 0).all() and (out == 5.0).all()
+    cache.query_status()
