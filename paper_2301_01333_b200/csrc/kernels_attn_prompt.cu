@@ -38,7 +38,7 @@
 namespace gc {
 
 namespace {
-constexpr int AP_THREADS = 640;               // five warpgroups; the last two warps only hand their registers over
+constexpr int AP_THREADS = 384;               // three warpgroups; the last warp only hands its registers over
 constexpr int AP_MAX_LIST = 1024;                // work list entries kept (and sorted) in shared memory
 constexpr float AP_RAISE = 8.0f;
 
@@ -50,8 +50,7 @@ struct PromptLayout {
   static constexpr int STAGES = D == 64 ? 8 : 4;
   static constexpr int BARS = 2 * STAGES + 14;
   static constexpr int LIST = AP_MAX_LIST * 8;
-  static constexpr int STAT = 2 * 2 * 128 * 4;   // one float per thread of the softmax warps
-  static constexpr size_t SMEM = 1024 + static_cast<size_t>(2 + STAGES) * TILE + LIST + STAT + BARS * 8 + 64;
+  static constexpr size_t SMEM = 1024 + static_cast<size_t>(2 + STAGES) * TILE + LIST + BARS * 8 + 64;
 };
 
 __device__ __forceinline__ float ap_ex2(float x) {
@@ -138,21 +137,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// Barrier of the 256 softmax threads of a tile; the second form also tells whether any of them had `v`.
-__device__ __forceinline__ void tile_sync(int t) { asm volatile("bar.sync %0, 256;" ::"r"(t + 1) : "memory"); }
-__device__ __forceinline__ bool tile_any(int t, bool v) {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.u32 p, %2, 0;\n\t"
-      "bar.red.or.pred q, %1, 256, p;\n\t"
-      "selp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(r)
-      : "r"(t + 1), "r"(static_cast<uint32_t>(v))
-      : "memory");
-  return r != 0;
-}
-
 // One sequence's rows, from its offsets; offsets that decrease or leave the tensors are cut to size.
 struct Seq {
   int q0, nq, k0, nk;
@@ -194,8 +178,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   uint8_t* sKV = sQ + 2 * L::TILE;                              // [STAGES] tiles
   int* s_item = reinterpret_cast<int*>(sKV + L::STAGES * L::TILE);      // sequence of each entry, then its block
   int* s_tmp = s_item + AP_MAX_LIST;
-  float* s_stat = reinterpret_cast<float*>(s_tmp + AP_MAX_LIST);        // [tile][half of the columns][row]
-  uint64_t* bars = reinterpret_cast<uint64_t*>(s_stat + L::STAT / 4);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(s_tmp + AP_MAX_LIST);
   const uint32_t b0 = smem_u32(bars);
   // [2] each: per tile; part h of the probabilities of tile t at 8 (2 t + h)
   const uint32_t bar_q_full = b0, bar_q_empty = b0 + 16, bar_s_full = b0 + 32, bar_p_full = b0 + 48, bar_o_full = b0 + 80;
@@ -203,7 +186,6 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   const uint32_t bar_kv_full = b0 + 112, bar_kv_empty = bar_kv_full + 8 * L::STAGES;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + L::BARS);
   int* s_total = reinterpret_cast<int*>(tmem_slot + 1);
-  volatile int* s_dead = s_total + 1;                           // [2]: a softmax warp of the tile has given up waiting
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
@@ -214,18 +196,17 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       mbar_init(bar_o_full + 8 * i, 1);
       mbar_init(bar_turn + 8 * i, 1);
     }
-    for (int i = 0; i < 4; ++i) mbar_init(bar_p_full + 8 * i, 8);
+    for (int i = 0; i < 4; ++i) mbar_init(bar_p_full + 8 * i, 4);
     for (int i = 0; i < L::STAGES; ++i) {
       mbar_init(bar_kv_full + 8 * i, 1);
       mbar_init(bar_kv_empty + 8 * i, 2);                       // both tiles' issuers
     }
-    s_dead[0] = s_dead[1] = 0;
     fence_mbar_init();
     tma_prefetch_desc(&tmQ);
     tma_prefetch_desc(&tmK);
     tma_prefetch_desc(&tmV);
   }
-  if (warp == 17) {
+  if (warp == 9) {
     tmem_alloc(smem_u32(tmem_slot), 512);
     tmem_relinquish();
   }
@@ -339,61 +320,53 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     return it;
   };
 
-  // Registers: 96 a thread at launch, 480 in each lane's five warps of a scheduler; 4 x 104 + 64 = 480.
+  // Registers: 168 a thread at launch, 504 in each lane's three warps of a scheduler; 2 x 208 + 88 = 504.
   bool failed = false;
-  if (warp < 16) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ------------------------------------------------------------------ softmax and output
-    // A wait that gives up must not leave the other warps of the tile in a barrier: the warp goes on taking part, and all
-    // of them leave together after the vote that follows.
-    const int t = warp >> 3, half = (warp >> 2) & 1, row = (warp & 3) * 32 + lane;
+    const int t = warp >> 2, row = tid & 127;
     const uint32_t t_lane = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-    const uint32_t s_addr = t_lane + t * 128 + half * 64, o_addr = t_lane + 256 + t * 128 + half * (D / 2);
-    float* my_stat = s_stat + (t * 2 + half) * 128 + row;
-    const float* other_stat = s_stat + (t * 2 + (half ^ 1)) * 128 + row;
-    uint32_t ring = 0, cnt = 0, on = 0;                          // ring positions, this tile's blocks and outputs so far
+    const uint32_t s_addr = t_lane + t * 128, o_addr = t_lane + 256 + t * 128;
+    uint32_t ring = 0, sn = 0, on = 0;
     const float c = p.c;
-    bool leave = false;
-    for (int r = 0; !leave; ++r) {
+    for (int r = 0; !failed; ++r) {
       const Item it = item_of(r);
       if (!it.valid) break;
       const int my_row = it.row0 + t * 128 + row;
       const int lim = row_limit(p, it.s, my_row), n = it.n[t];
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < n; ++j) {
-        if (!__all_sync(0xffffffffu, mbar_wait(bar_s_full + 8 * t, cnt & 1))) failed = true;
-        ++cnt;
+        if (!__all_sync(0xffffffffu, mbar_wait(bar_s_full + 8 * t, sn & 1))) { failed = true; break; }
+        ++sn;
         tc_fence_after();
-        uint32_t v[64];
-        tmem_ld64(s_addr, v);
-        const int left = lim - j * 128 - half * 64;
-        if (__any_sync(0xffffffffu, left < 64)) {
+        uint32_t v[2][64];
+        tmem_ld64(s_addr, v[0]);
+        tmem_ld64(s_addr + 64, v[1]);
+        const int left = lim - j * 128;
+        if (__any_sync(0xffffffffu, left < 128)) {
 #pragma unroll
-          for (int i = 0; i < 64; ++i)
-            if (i >= left) v[i] = 0xff800000u;                   // minus infinity, whatever the score was
+          for (int i = 0; i < 128; ++i)
+            if (i >= left) v[i >> 6][i & 63] = 0xff800000u;      // minus infinity, whatever the score was
         }
-        float top = __uint_as_float(v[0]), top1 = __uint_as_float(v[1]);
+        float top[4];
 #pragma unroll
-        for (int i = 2; i < 62; i += 4) {
-          top = max3(top, __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
-          top1 = max3(top1, __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
+        for (int i = 0; i < 4; ++i) top[i] = max3(__uint_as_float(v[i >> 1][(i & 1) * 32]), __uint_as_float(v[i >> 1][(i & 1) * 32 + 1]), -INFINITY);
+#pragma unroll
+        for (int i = 2; i < 32; i += 2) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) top[k] = max3(top[k], __uint_as_float(v[k >> 1][(k & 1) * 32 + i]), __uint_as_float(v[k >> 1][(k & 1) * 32 + i + 1]));
         }
-        top = fmaxf(max3(top, __uint_as_float(v[62]), __uint_as_float(v[63])), top1);
-        if (tile_any(t, (top - m) * c > AP_RAISE || failed)) {
-          *my_stat = top;
-          if (failed) s_dead[t] = 1;
-          tile_sync(t);
-          const float mn = fmaxf(m, fmaxf(top, *other_stat));
-          if (s_dead[t]) leave = true;
-          tile_sync(t);                                          // read before the next one is written
-          if (leave) break;
+        const float mx = max3(max3(top[0], top[1], top[2]), top[3], top[3]);
+        if (__any_sync(0xffffffffu, (mx - m) * c > AP_RAISE)) {
+          const float mn = fmaxf(m, mx);
           const float f = mn == m ? 1.f : ap_ex2((m - mn) * c);  // 0 from the initial minus infinity
           m = mn;
           l *= f;
           if (j > 0) {
-            // S of this block is complete, hence so is the product of the block before: O is at rest; half its columns each
+            // S of this block is complete, hence so is the product of the block before: O is at rest
 #pragma unroll 1
-            for (int k = 0; k < D / 32; ++k) {
+            for (int k = 0; k < D / 16; ++k) {
               uint32_t w[16];
               tmem_ld16(o_addr + k * 16, w);
               tmem_wait_ld();
@@ -406,79 +379,78 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         const float off = m == -INFINITY ? 0.f : -m * c;
         const uint64_t c2 = pair2(c, c), off2 = pair2(off, off);
         if (j * 128 + 128 > it.s.nk) {
-          // the sequence ends inside this block: whatever follows it in V becomes zero (each thread of a row its 64 elements)
+          // the sequence ends inside this block: whatever follows it in V becomes zero
           const uint32_t pos = ring + 2 * j + 1, st = pos % L::STAGES;
-          if (!__all_sync(0xffffffffu, mbar_wait(bar_kv_full + 8 * st, (pos / L::STAGES) & 1))) failed = true;
-          if (!failed && j * 128 + row >= it.s.nk && half < L::NSUB) {
-            uint4* z = reinterpret_cast<uint4*>(sKV + st * L::TILE + half * L::SUB + row * 128);
+          if (!__all_sync(0xffffffffu, mbar_wait(bar_kv_full + 8 * st, (pos / L::STAGES) & 1))) { failed = true; break; }
+          if (j * 128 + row >= it.s.nk) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = make_uint4(0, 0, 0, 0);
+            for (int k = 0; k < L::NSUB; ++k) {
+              uint4* z = reinterpret_cast<uint4*>(sKV + st * L::TILE + k * L::SUB + row * 128);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) z[i] = make_uint4(0, 0, 0, 0);
+            }
           }
           fence_proxy_async_smem();
         }
         uint64_t ls[2] = {0, 0};
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          uint32_t w[16];
+          uint32_t w[32];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
+          for (int i = 0; i < 32; ++i) {
             float e0, e1;
-            unpair2(fma2(pair2(__uint_as_float(v[h * 32 + 2 * i]), __uint_as_float(v[h * 32 + 2 * i + 1])), c2, off2), &e0, &e1);
+            unpair2(fma2(pair2(__uint_as_float(v[h][2 * i]), __uint_as_float(v[h][2 * i + 1])), c2, off2), &e0, &e1);
             e0 = ap_ex2(e0);
             e1 = ap_ex2(e1);
             ls[i & 1] = add2(ls[i & 1], pair2(e0, e1));
             w[i] = ap_pack(e0, e1);
           }
-          tmem_st16(s_addr + h * 16, w);
+          tmem_st32(s_addr + h * 32, w);
           tmem_wait_st();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0 && !failed) mbar_arrive(bar_p_full + 8 * (2 * t + h));
+          if (lane == 0) mbar_arrive(bar_p_full + 8 * (2 * t + h));
         }
         float l0, l1;
         unpair2(add2(ls[0], ls[1]), &l0, &l1);
         l += l0 + l1;
       }
-      if (leave) break;
+      if (failed) break;
       ring += 2 * max(it.n[0], it.n[1]);
       const bool store = my_row < it.s.nq;
-      __nv_bfloat16* dst = p.o + static_cast<int64_t>(it.s.q0 + my_row) * p.o_tok + static_cast<int64_t>(it.head) * p.o_head + half * (D / 2);
+      __nv_bfloat16* dst = p.o + static_cast<int64_t>(it.s.q0 + my_row) * p.o_tok + static_cast<int64_t>(it.head) * p.o_head;
       if (n == 0) {
         if (store) {
 #pragma unroll
-          for (int i = 0; i < D / 16; ++i) reinterpret_cast<uint4*>(dst)[i] = make_uint4(0, 0, 0, 0);
+          for (int i = 0; i < D / 8; ++i) reinterpret_cast<uint4*>(dst)[i] = make_uint4(0, 0, 0, 0);
         }
         continue;
       }
-      *my_stat = l;
-      if (!__all_sync(0xffffffffu, mbar_wait(bar_o_full + 8 * t, on & 1))) failed = true;
+      if (!__all_sync(0xffffffffu, mbar_wait(bar_o_full + 8 * t, on & 1))) { failed = true; break; }
       ++on;
       tc_fence_after();
-      if (tile_any(t, failed)) break;
-      l += *other_stat;
       const float rl = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll 1
       for (int k = 0; k < D / 32; ++k) {
-        uint32_t w[16];
-        tmem_ld16(o_addr + k * 16, w);
+        uint32_t w[32];
+        tmem_ld32(o_addr + k * 32, w);
         tmem_wait_ld();
         if (store) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
+          for (int i = 0; i < 4; ++i) {
             uint32_t x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = ap_pack(__uint_as_float(w[8 * i + 2 * e]) * rl, __uint_as_float(w[8 * i + 2 * e + 1]) * rl);
-            reinterpret_cast<uint4*>(dst)[k * 2 + i] = make_uint4(x[0], x[1], x[2], x[3]);
+            reinterpret_cast<uint4*>(dst)[k * 4 + i] = make_uint4(x[0], x[1], x[2], x[3]);
           }
         }
       }
       tc_fence_before();
-      tile_sync(t);                                              // the sums have been read
     }
     if (failed && lane == 0) report(p.status, DEV_TIMEOUT_EPILOGUE);
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    if (warp == 16) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == 8) {
       // ------------------------------------------------------------------ TMA producer
       uint32_t ring = 0, qn[2] = {0, 0};
       const int g = p.Hq / p.Hk;
@@ -516,9 +488,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         }
         if (__any_sync(0xffffffffu, failed)) break;
       }
-    } else if (warp < 19) {
+    } else if (warp < 11) {
       // ------------------------------------------------------------------ MMA issuers, one per tile
-      const int t = warp - 17;
+      const int t = warp - 9;
       const uint32_t idesc_s = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, 128, 128);
       const uint32_t idesc_o = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, 128, D, 0, 1);
       const uint32_t d_s = tmem_base + t * 128, d_o = tmem_base + 256 + t * 128;
@@ -575,13 +547,13 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             tc_fence_after();
             if (j < n) {
               const uint32_t vb = v_lo + (vpos % L::STAGES) * (L::TILE >> 4);
-              // 16 keys per product; each thread of a row makes 64 keys' probabilities, 32 of them in the first part
+              // 16 keys per product, half of them with each part of P
 #pragma unroll
-              for (int k = 0; k < 8; k += (k & 1) ? 3 : 1) mma_ts(d_o, d_s + (k >> 2) * 64 + (k & 1) * 8, vb + k * 128, idesc_o, k || j);
+              for (int k = 0; k < 4; ++k) mma_ts(d_o, d_s + k * 8, vb + k * 128, idesc_o, k || j);
               if (!mma_wait(p_full + 8, pn++ & 1)) { failed = true; break; }
               tc_fence_after();
 #pragma unroll
-              for (int k = 2; k < 8; k += (k & 1) ? 3 : 1) mma_ts(d_o, d_s + (k >> 2) * 64 + 16 + (k & 1) * 8, vb + k * 128, idesc_o, 1);
+              for (int k = 4; k < 8; ++k) mma_ts(d_o, d_s + k * 8, vb + k * 128, idesc_o, 1);
               if (j + 1 < n) scores(vpos + 1);
               else umma_commit(o_full);
             }
@@ -601,7 +573,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (warp == 17) {
+  if (warp == 9) {
     tc_fence_after();
     tmem_dealloc(tmem_base, 512);
   }
