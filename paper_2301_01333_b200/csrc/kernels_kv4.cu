@@ -244,9 +244,18 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_append_kernel(const __grid_con
         while (border) {                                         // (ties are not rare in bf16: one element in 200)
           const int e = __ffs(border) - 1, sh = 4 * (e & 7);
           border &= border - 1;
-          const uint32_t c = code_of(pick(raw[i], e), lo, scale, inv) << sh, keep = ~(15u << sh);
-          if (e < 8) word[0] = (word[0] & keep) | c;
-          else word[1] = (word[1] & keep) | c;
+          const float x = pick(raw[i], e), d = x - lo;
+          const uint32_t was = (e < 8 ? word[0] : word[1]) >> sh & 15u;
+          const float r = fmaf(8388608.0f - __uint_as_float(was | 0x4b000000u), scale, d);       // d - code scale, exact here
+          uint32_t is = was;
+          if (fabsf(r) == 0.5f * scale && d + lo == x && x - d == lo) {
+            if (was & 1u) is = r > 0.0f ? was + 1 : was - 1;     // a tie of exact numbers: the even one
+          } else {
+            is = code_of(x, lo, scale, inv);
+          }
+          const uint32_t flip = (was ^ is) << sh;
+          word[0] ^= e < 8 ? flip : 0u;
+          word[1] ^= e < 8 ? 0u : flip;
         }
       }
     }
