@@ -352,7 +352,8 @@ gc_status_t gc_kv4_read(void* cuda_stream, const gc_kv4_cache_t* cache, int32_t 
  * sequence b at [b * table_stride + p], p < table_width; entries beyond a sequence's length are not looked at.
  * max_length: an upper bound of lengths the caller knows (a longer sequence is an error found on the device); the
  * split of the work over the GPU goes by it.  Scores and sums in fp32, probabilities times scale rounded to bf16 (half a
- * bf16 step each, the only rounding before the output's).  queries 1 .. 16, scale finite and > 0. */
+ * bf16 step each, the only rounding before the output's).  queries 1 .. 16, scale finite and > 0.  Values held
+ * should lie between 2^-40 and 2^32 in size (the sums carry a factor of 2^64 and bf16's smallest unit).  What a query does not see has no influence on it, whatever is held there. */
 typedef struct {
   int32_t batch, queries, q_heads;
   int32_t table_width;
@@ -376,7 +377,9 @@ gc_status_t gc_attention_kv4(void* cuda_stream, const gc_kv4_cache_t* cache, con
  * [cu_q[b], cu_q[b + 1]) and key rows [cu_k[b], cu_k[b + 1]).  causal = 1: query row i of nq sees keys j <= i + nk - nq
  * (aligned to the end, so a prompt may continue earlier keys).  A row that sees nothing is zero; rows of out that no
  * sequence owns are left as they were.  bf16, head_dim 64, 96 or 128, fp32 statistics and sums, probabilities rounded to
- * bf16 for the second product.  Rows 16-byte aligned (pointers, and strides multiples of 8 elements). */
+ * bf16 for the second product.  Rows 16-byte aligned (pointers, and strides multiples of 8 elements).  Sequences do not touch
+ * one another, and a key that a row does not see has no influence on it; a non-finite value (V) may also reach rows of its
+ * own sequence that do not see it (a weight of zero times infinity). */
 typedef struct {
   int32_t cuda_device;
   int32_t batch;

@@ -8,24 +8,26 @@
 // each against 16384 exponentials, 16 a clock: 1024 clocks.  The two have to run side by side, so a CTA owns two tiles of 128
 // query rows (256 neighbouring rows of one head) and alternates: while the softmax warps of one tile turn its scores into
 // probabilities, the tensor core works for the other.
-//   warps 0-7, 8-15  softmax of tile 0 / 1, two threads per query row: 64 scores each from tensor memory into registers at
-//                    once, maximum, exponentials, row sum; the bf16 probabilities go back over the scores they came from, as
-//                    the A operand of the second product in tensor memory, in two parts, so that the product with the first
-//                    runs while the second is made; at the end of a tile they scale and store its O
-//   warp 16          TMA producer: Q tiles, and K and V blocks through one ring
-//   warps 17, 18     MMA issuers of tile 0 / 1: S = Q K^T (both operands in shared memory), O += P V (P in tensor memory, V as
+//   warps 0-3, 4-7   softmax of tile 0 / 1, one query row per thread: 128 scores from tensor memory into registers at once,
+//                    maximum (three-input), exponentials, row sum (two sums an instruction); the bf16 probabilities go back over
+//                    the scores they came from, as the A operand of the second product in tensor memory, in two parts, so that
+//                    the product with the first runs while the second is made; at the end of a tile they scale and store its O
+//   warp 8           TMA producer: Q tiles, and K and V blocks through one ring
+//   warps 9, 10      MMA issuers of tile 0 / 1: S = Q K^T (both operands in shared memory), O += P V (P in tensor memory, V as
 //                    stored, keys along the rows).  The tensor core works off one thread's products in order, which is what lets
 //                    S of the next block overwrite P of this one, and makes "S complete" imply "O complete".  Their batches
 //                    take turns.
 // Tensor memory: two score tiles of 128 columns and two outputs of D <= 128: all 512 columns.
-// How it got there, for one prompt of 16384 tokens, 16 heads of 128 (1.1 TFLOP): one thread per row 1148 us; two threads per row
-// 1064; an issuing thread per tile (one thread's instructions for both were the bottleneck), taking turns (both tiles'
-// products at once complete both scores together, and the tensor core idles while both softmaxes run) 957; P in two parts
-// 917 (1200 TFLOP/s).  No gain: CTA pairs (M = 256, half of K and V in each CTA); part of the exponentials on the FMA pipe; two score
-// buffers of 64 keys per tile, which takes the hand-over out of the way but makes S slower (N = 64: 1001 us).
+// How it got there, for one prompt of 16384 tokens, 16 heads of 128 (1.1 TFLOP): one issuing thread for both tiles 1148 us, with
+// two threads per row 1064 (its instructions were the bottleneck: products alone took 940); an issuing thread per tile with lean
+// descriptors, taking turns (both tiles' products at once complete both scores together, and the tensor core idles while
+// both softmaxes run: 1242) 957; probabilities in two parts 917; one thread per row, without the votes and sums two threads
+// share, 865 = 1270 TFLOP/s, the tensor pipe busy 71 % of the time (products alone: 714).  What is left is the way round: scores
+// complete, softmax, probabilities handed over, with only two tiles to alternate between.  No gain: CTA pairs (M = 256, half
+// of K and V in each CTA); part of the exponentials on the FMA pipe (865 without any exponentials as well); probabilities in four
+// parts (945); two score buffers of 64 keys per tile, which takes the hand-over out of the way but makes S slower (N = 64: 1001).
 //   * The reference m is raised only when a score exceeds it by 2^8 (as in the cache attention): after the first block the
 //     output is almost never touched, and raising it is the softmax warps' own business - no extra role, no extra hand-over.
-//     The two threads of a row need not compare their maxima for it: one barrier with a vote says whether any row has to.
 //   * Persistent CTAs; the work list (256 query rows of a sequence, times heads) is made by each CTA from the sequence offsets
 //     and sorted by its number of key blocks, longest first, dealt out back and forth.  The first scores of the next item are
 //     issued before the last output of the current one has been stored.

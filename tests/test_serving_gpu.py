@@ -308,6 +308,16 @@ def test_attend_ignores_what_lies_behind_a_sequence(S, d, group):
     within(out, ref, tol)
 
 
+@pytest.mark.parametrize("power", [30, -36])
+def test_attend_values_of_unlike_size(S, power):
+    # values times a power of two: every step scales with it exactly, and nothing overflows or vanishes
+    cache, q, table, out = attend_case(S, [900, 33, 257], 2, 8, 2, 128, 32, 16, seed=5)
+    cache.v_params.mul_(2.0 ** power)
+    cache.k_params.mul_(2.0 ** power)
+    big = cache.attend((q.float() * 2.0 ** -power).bfloat16(), table, torch.tensor([900, 33, 257], dtype=torch.int32, device=DEV))
+    assert torch.equal(big, out * 2.0 ** power)
+
+
 def test_attend_reports_bad_pages_and_lengths(S):
     g = gen(12)
     cache = filled_cache(S, 4, 16, 1, 64, 64, g)
