@@ -279,7 +279,7 @@ gc_status_t gc_selftest_bounded_wait(void* cuda_stream, void* status_dev, uint32
  *
  * Conventions beyond those above: each call enqueues its kernels on cuda_stream, on the device named in its
  * descriptor (the calling thread's current device is restored), allocates nothing, keeps nothing between
- * calls and may be captured.  What the host can see is refused before anything is launched.  What only the
+ * calls and may be captured (after a first call outside a capture, which loads its kernels).  What the host can see is refused before anything is launched.  What only the
  * device sees (a slot, a page number, a length, a sequence offset outside its bounds) is checked there: the
  * access is left out or clamped, the outputs of that call are undefined, and the first such finding is written
  * to the status word the caller passed (device u32, zeroed by the caller; may be NULL), see gc_serving_status.

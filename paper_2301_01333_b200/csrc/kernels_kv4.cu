@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_read_kernel(const __grid_const
   for (int i = 0; i < ITEMS; ++i) {
     if (slot[i] < 0) continue;
     T* dst = static_cast<T*>(x.data) + t[i] * x.token_stride + h[i] * x.head_stride + j * 8;
-    if constexpr (VEC && sizeof(T) == 2) {
+    if constexpr (sizeof(T) == 2) {
       // pairs (0,4), (1,5), (2,6), (3,7): 128 + code, minus 128, times scale plus lo in one rounding
       const uint32_t lo2 = __byte_perm(pw[i], 0, 0x1010), sc2 = __byte_perm(pw[i], 0, 0x3232);
       const uint32_t m128 = 0xc300c300u;
@@ -311,8 +311,13 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_read_kernel(const __grid_const
         const __nv_bfloat162 f = __hfma2(c, *reinterpret_cast<const __nv_bfloat162*>(&sc2), *reinterpret_cast<const __nv_bfloat162*>(&lo2));
         v[e] = *reinterpret_cast<const uint32_t*>(&f);
       }
-      *reinterpret_cast<uint4*>(dst) = make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410),
-                                                  __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632));
+      const uint32_t w[4] = {__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632)};
+      if constexpr (VEC) {
+        *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) reinterpret_cast<uint16_t*>(dst)[e] = static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)));
+      }
     } else {
       const float lo = __uint_as_float(pw[i] << 16), scale = __uint_as_float(pw[i] & 0xffff0000u);
       float v[8];

@@ -390,6 +390,15 @@ def test_prompt_continued_and_rows_that_see_nothing(S, causal):
     prompt_case(S, [5, 300, 1, 7, 260, 40], [128, 301, 256, 0, 140, 39], 3, 1, 64, causal, seed=2)
 
 
+def test_prompt_without_any_key_and_without_any_row(S):
+    prompt_case(S, [3, 300], [0, 0], 2, 1, 64, True, seed=1)
+    x = torch.zeros(0, 2, 64, dtype=torch.bfloat16, device=DEV)
+    cu = torch.zeros(3, dtype=torch.int32, device=DEV)
+    assert S.attention_prompt(x, x, x, cu).shape == (0, 2, 64)
+    y = torch.full((4, 2, 64), 3.0, dtype=torch.bfloat16, device=DEV)
+    assert (S.attention_prompt(y, y, y, cu[:1], out=y.clone()) == 3.0).all()          # no sequence: nothing is written
+
+
 def test_prompt_more_work_than_ctas(S):
     prompt_case(S, [900, 17, 1500, 333], [900, 17, 1500, 333], 16, 4, 128, True, seed=3)
     prompt_case(S, [900, 17, 1500, 333], [1000, 900, 1600, 333], 32, 32, 64, True, seed=4)
