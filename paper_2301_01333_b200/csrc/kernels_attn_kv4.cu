@@ -666,6 +666,7 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
   extern __shared__ uint4 smem_u4[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(smem_u4);
 
+  wait_for_predecessor();
   const int per_seq = p.Hk * p.col_chunks;
   int b, u, len, nb, k0 = 0;                                     // sequence, (head, chunk), its length, blocks, first block of mine
   int64_t left;                                                  // blocks to do
@@ -717,6 +718,7 @@ __device__ __forceinline__ int cta_of(int64_t x, int64_t total, int ctas) {
 // Joins the pieces of split sequences, in their order: one warp per (batch, column).
 template <int D>
 __global__ void __launch_bounds__(128) attn_kv4_join_kernel(const __grid_constant__ Kv4AttnParams p, const int cols, int ctas) {
+  wait_for_predecessor();
   const int lane = threadIdx.x & 31;
   const int columns = p.n * p.g;
   const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
@@ -780,12 +782,10 @@ cudaError_t ak_run(const Kv4AttnParams& p, cudaStream_t s) {
   constexpr size_t smem = ak_smem<D, G, NT>();
   cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
   if (e != cudaSuccess) return e;
-  kern<<<static_cast<unsigned>(p.ctas), AK_THREADS, smem, s>>>(p);
-  e = cudaGetLastError();
+  e = launch_following(kern, dim3(static_cast<unsigned>(p.ctas)), AK_THREADS, smem, s, p);
   if (e != cudaSuccess || p.block >= p.max_len || p.ctas == 1) return e;
   const int64_t items = static_cast<int64_t>(p.B) * p.Hk * p.n * p.g;
-  attn_kv4_join_kernel<D><<<static_cast<unsigned>((items + 3) / 4), 128, 0, s>>>(p, 8 * NT, p.ctas);
-  return cudaGetLastError();
+  return launch_following(attn_kv4_join_kernel<D>, dim3(static_cast<unsigned>((items + 3) / 4)), 128, 0, s, p, 8 * NT, p.ctas);
 }
 
 template <int D, int G>

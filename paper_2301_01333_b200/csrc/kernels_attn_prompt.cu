@@ -212,6 +212,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     tmem_alloc(smem_u32(tmem_slot), 512);
     tmem_relinquish();
   }
+  wait_for_predecessor();
   // ---- the work list
   if (warp == 0) {
     int total = 0;
@@ -593,8 +594,7 @@ static cudaError_t prompt_run(const CUtensorMap& tmQ, const CUtensorMap& tmK, co
   const int grid = static_cast<int>(items < num_sms ? items : num_sms);
   // the list packs a block number into 12 bits
   const int listed = entries <= AP_MAX_LIST && p.q_tokens <= 256 * 4096LL;
-  kern<<<grid, AP_THREADS, PromptLayout<D>::SMEM, s>>>(tmQ, tmK, tmV, p, listed, static_cast<int>(entries));
-  return cudaGetLastError();
+  return launch_following(kern, dim3(static_cast<unsigned>(grid)), AP_THREADS, PromptLayout<D>::SMEM, s, tmQ, tmK, tmV, p, listed, static_cast<int>(entries));
 }
 
 cudaError_t launch_attn_prompt(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const PromptParams& p, int num_sms,

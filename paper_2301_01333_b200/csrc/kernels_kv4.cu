@@ -174,6 +174,7 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
 template <typename T, int D, int G, bool VEC>
 __global__ void __launch_bounds__(KV_THREADS) kv4_append_kernel(const __grid_constant__ Kv4Params p) {
   constexpr int LANES = D / 16, GL = G / 16, NG = D / G, ITEMS = 2, ROWS = KV_THREADS / LANES;
+  wait_for_predecessor();
   const int which = blockIdx.y, j = threadIdx.x % LANES;
   const uint32_t row0 = blockIdx.x * (ROWS * ITEMS) + threadIdx.x / LANES;
   const gc_heads_t& x = p.x[which];
@@ -271,6 +272,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_append_kernel(const __grid_con
 template <typename T, int D, int G, bool VEC>
 __global__ void __launch_bounds__(KV_THREADS) kv4_read_kernel(const __grid_constant__ Kv4Params p) {
   constexpr int LANES = D / 8, GL = G / 8, NG = D / G, ITEMS = 4, ROWS = KV_THREADS / LANES;
+  wait_for_predecessor();
   const int which = blockIdx.y, j = threadIdx.x % LANES;
   const uint32_t row0 = blockIdx.x * (ROWS * ITEMS) + threadIdx.x / LANES;
   const gc_heads_t& x = p.x[which];
@@ -345,14 +347,8 @@ cudaError_t run(const Kv4Params& p, bool vec, cudaStream_t s) {
   const uint32_t per = READ ? KV_THREADS / (D / 8) * 4 : KV_THREADS / (D / 16) * 2;
   const uint32_t gx = (p.rows + per - 1) / per;
   const dim3 grid(gx, 2);
-  if constexpr (READ) {
-    if (vec) kv4_read_kernel<T, D, G, true><<<grid, KV_THREADS, 0, s>>>(p);
-    else kv4_read_kernel<T, D, G, false><<<grid, KV_THREADS, 0, s>>>(p);
-  } else {
-    if (vec) kv4_append_kernel<T, D, G, true><<<grid, KV_THREADS, 0, s>>>(p);
-    else kv4_append_kernel<T, D, G, false><<<grid, KV_THREADS, 0, s>>>(p);
-  }
-  return cudaGetLastError();
+  if constexpr (READ) return launch_following(vec ? kv4_read_kernel<T, D, G, true> : kv4_read_kernel<T, D, G, false>, grid, KV_THREADS, 0, s, p);
+  else return launch_following(vec ? kv4_append_kernel<T, D, G, true> : kv4_append_kernel<T, D, G, false>, grid, KV_THREADS, 0, s, p);
 }
 
 template <bool READ, typename T>

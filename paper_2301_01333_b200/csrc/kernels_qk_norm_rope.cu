@@ -64,6 +64,7 @@ __device__ __forceinline__ void turn_of(int64_t pos, float f, float factor, floa
 template <typename T, int W, int CH>
 __global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const __grid_constant__ QkParams p) {
   extern __shared__ float4 smem4[];
+  wait_for_predecessor();
   const int L = 1 << p.log_l, slots = QN_THREADS >> p.log_l;
   float* s_row = reinterpret_cast<float*>(smem4);                        // [slots][D rounded up to 4]
   const int pitch = (p.D + 3) & ~3, tpitch = (p.half + 3) & ~3;
@@ -232,6 +233,7 @@ __global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const __grid_c
 template <typename T, int W, bool INTERLEAVED>
 __global__ void __launch_bounds__(QN_THREADS, 3) qk_norm_rope_pairs_kernel(const __grid_constant__ QkParams p) {
   extern __shared__ float4 smem4[];
+  wait_for_predecessor();
   const int tpitch = (p.half + W - 1) / W * W;                   // angles of a token, padded to whole vectors
   float* s_cos = reinterpret_cast<float*>(smem4);
   float* s_sin = s_cos + p.tb * tpitch;
@@ -365,8 +367,7 @@ static cudaError_t launch_t(K kern, const QkParams& p, dim3 grid, size_t smem, c
     cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
     if (e != cudaSuccess) return e;
   }
-  kern<<<grid, QN_THREADS, smem, s>>>(p);
-  return cudaGetLastError();
+  return launch_following(kern, grid, QN_THREADS, smem, s, p);
 }
 
 cudaError_t launch_qk_norm_rope(const gc_qk_norm_rope_t& d, int num_sms, cudaStream_t s) {

@@ -14,6 +14,28 @@ enum : uint32_t {
   DEV_BAD_OFFSETS = 0x204,
 };
 
+// Launches of this block follow one another closely: each may be set up while the kernel before it on the stream still runs
+// (programmatic dependent launch), and every thread of every kernel passes wait_for_predecessor() before it touches global memory
+// or returns - also where it has nothing to do: a kernel that ended without waiting would let the one behind it overtake the
+// one before it.
+__device__ __forceinline__ void wait_for_predecessor() {
+  asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
+}
+template <typename... P, typename... A>
+cudaError_t launch_following(void (*kern)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
+}
+
 struct Kv4AttnParams {
   int B, n, Hq, Hk, g;              // g: query heads per key/value head; columns of a unit = n * g
   int page_shift, width, max_len;
