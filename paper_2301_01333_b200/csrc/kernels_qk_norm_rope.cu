@@ -47,6 +47,22 @@ __device__ __forceinline__ float from_f<float>(float x) { return x; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
+// 16 bytes of rounded elements
+template <typename T>
+__device__ __forceinline__ uint4 pack16(const float* y) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&b);
+    } else {
+      w[i] = __float_as_uint(y[i]);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // cos and sin of pos * f, both times `factor`.  2 pi = TWO_PI_HI + TWO_PI_LO to about 106 bits.
 __device__ __forceinline__ void turn_of(int64_t pos, float f, float factor, float* c, float* s) {
   constexpr double TWO_PI_HI = 6.283185307179586232, TWO_PI_LO = 2.4492935982947064e-16;
@@ -237,6 +253,15 @@ __global__ void __launch_bounds__(QN_THREADS, 3) qk_norm_rope_pairs_kernel(const
   const int tpitch = (p.half + W - 1) / W * W;                   // angles of a token, padded to whole vectors
   float* s_cos = reinterpret_cast<float*>(smem4);
   float* s_sin = s_cos + p.tb * tpitch;
+  // pair i of a lane: elements i of its two vectors, or neighbours in one of them
+  auto turn = [](float (&y0)[W], float (&y1)[W], int i, float c, float s) {
+    float& a = INTERLEAVED ? (i < W / 2 ? y0[(2 * i) % W] : y1[(2 * i) % W]) : y0[i];
+    float& b = INTERLEAVED ? (i < W / 2 ? y0[(2 * i + 1) % W] : y1[(2 * i + 1) % W]) : y1[i];
+    const float u = a, v = b;
+    a = fmaf(u, c, -(v * s));
+    b = fmaf(v, c, u * s);
+  };
+  const float inv_d = 1.0f / static_cast<float>(p.D);
   const int L = 1 << p.log_l, item = threadIdx.x & (L - 1);
   const int slot = threadIdx.x >> p.log_l, per_token = (QN_THREADS >> p.log_l) / p.tb;         // rows a token's slots take at a time
   const int t = slot / per_token, s0 = slot - t * per_token;
@@ -311,42 +336,30 @@ __global__ void __launch_bounds__(QN_THREADS, 3) qk_norm_rope_pairs_kernel(const
         const bool next = mine && live_token && h + per_token + s0 < end;
         x += xs;
         load(next, &a, &b);
+        if (mine && live_token && h + 2 * per_token + s0 < end) {       // and the one after it on its way to the L2
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(x + xs + e0));
+          if (!INTERLEAVED) asm volatile("prefetch.global.L2 [%0];" ::"l"(x + xs + e1));
+        }
         if (p.norm) {
           for (int d = L >> 1; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-          const float inv = rsqrtf(sum / static_cast<float>(p.D) + p.eps);
+          const float inv = rsqrtf(fmaf(sum, inv_d, p.eps));
 #pragma unroll
           for (int i = 0; i < W; ++i) {
             y0[i] *= inv * w0[i];
             y1[i] *= inv * w1[i];
           }
         }
-        if constexpr (INTERLEAVED) {
+        if (turns && angles >= W) {                              // all pairs of the lane
 #pragma unroll
-          for (int i = 0; i < W; ++i) {
-            float* y = i < W / 2 ? y0 + 2 * i : y1 + 2 * (i - W / 2);
-            const float u = y[0], v = y[1];
-            if (i < angles) {
-              y[0] = fmaf(u, cs[i], -(v * sn[i]));
-              y[1] = fmaf(v, cs[i], u * sn[i]);
-            }
-          }
-        } else if (turns) {
+          for (int i = 0; i < W; ++i) turn(y0, y1, i, cs[i], sn[i]);
+        } else if (INTERLEAVED && angles > 0) {                  // the first few
 #pragma unroll
-          for (int i = 0; i < W; ++i) {
-            const float u = y0[i], v = y1[i];
-            y0[i] = fmaf(u, cs[i], -(v * sn[i]));
-            y1[i] = fmaf(v, cs[i], u * sn[i]);
-          }
+          for (int i = 0; i < W; ++i)
+            if (i < angles) turn(y0, y1, i, cs[i], sn[i]);
         }
         if (ok) {
-          uint4 c, d;
-#pragma unroll
-          for (int i = 0; i < W; ++i) {
-            reinterpret_cast<T*>(&c)[i] = from_f<T>(y0[i]);
-            reinterpret_cast<T*>(&d)[i] = from_f<T>(y1[i]);
-          }
-          *reinterpret_cast<uint4*>(o + e0) = c;
-          *reinterpret_cast<uint4*>(o + e1) = d;
+          *reinterpret_cast<uint4*>(o + e0) = pack16<T>(y0);
+          *reinterpret_cast<uint4*>(o + e1) = pack16<T>(y1);
         }
         o += os;
         ok = next;
@@ -408,11 +421,11 @@ cudaError_t launch_qk_norm_rope(const gc_qk_norm_rope_t& d, int num_sms, cudaStr
   const dim3 grid(static_cast<unsigned>(gx), static_cast<unsigned>((p.rows + p.rows_per_cta - 1) / p.rows_per_cta));
   using bf16 = __nv_bfloat16;
   if (pairs) {
-    // With many tokens eight to a CTA, so that a thread's angles and weights serve several rows, and as many CTAs as fit at
-    // once (three per SM), which walk over the groups; fewer to a CTA while that leaves SMs without work.
+    // With many tokens four to a CTA, so that a thread's angles and weights serve several rows, and as many CTAs as fit at
+    // once (three per SM), which walk over the groups; two to a CTA where four would leave SMs without work.
     dim3 pg = grid;
     if (d.tokens >= 4LL * num_sms) {
-      p.tb = d.tokens >= 48LL * num_sms ? 8 : d.tokens >= 8LL * num_sms ? 4 : 2;
+      p.tb = d.tokens >= 8LL * num_sms ? 4 : 2;
       if (p.tb > slots) p.tb = slots;
       const int64_t groups = (d.tokens + p.tb - 1) / p.tb;
       pg.x = static_cast<unsigned>(groups < 3LL * num_sms ? groups : 3LL * num_sms);
