@@ -35,7 +35,7 @@
 // Measured: 64 ragged sequences up to 8192 tokens, 8 heads of 128, groups of 64 (323 MB): 78 us = 4.1 TB/s; without any arithmetic
 // the same copies take 62, so the rest is instructions that the copies of 12 warps do not cover (about 610 a tile and eight columns,
 // half of them on the integer / logic pipe).  One sequence of 131071 tokens, 32 columns (142 MB, read twice, the second time from
-// the L2): 93 us, bound by instructions; its products alone, 8 clocks each on a scheduler, are 33.
+// the L2): 90 us, bound by instructions; its products alone, 8 clocks each on a scheduler, are 33.
 #include <cuda_fp16.h>
 
 #include <type_traits>
@@ -715,13 +715,18 @@ __device__ __forceinline__ int cta_of(int64_t x, int64_t total, int ctas) {
   while (total * c / ctas > x) --c;
   return c;
 }
-// Joins the pieces of split sequences, in their order: one warp per (batch, column).
-template <int D>
-__global__ void __launch_bounds__(128) attn_kv4_join_kernel(const __grid_constant__ Kv4AttnParams p, const int cols, int ctas) {
+// Joins the pieces of a split sequence for one column, in a fixed order.  JW = 1: a warp per column, four to a CTA.  JW = 8:
+// a CTA per column, each warp every eighth piece, then the warps; for sequences in many pieces, which one warp would read one
+// memory latency after the other (one sequence of 8000 tokens in 55: 27 us against 17; but 64 of them in two or three: 125
+// against 136, for so many CTAs have to be started).
+template <int D, int JW>
+__global__ void __launch_bounds__(JW == 1 ? 128 : JW * 32) attn_kv4_join_kernel(const __grid_constant__ Kv4AttnParams p, const int cols, int ctas) {
   wait_for_predecessor();
-  const int lane = threadIdx.x & 31;
+  __shared__ float4 s_o[JW][32];
+  __shared__ float s_l[JW];
+  const int lane = threadIdx.x & 31, warp = JW == 1 ? 0 : threadIdx.x >> 5;
   const int columns = p.n * p.g;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
+  const int64_t item = JW == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5) : blockIdx.x;
   if (item >= static_cast<int64_t>(p.B) * p.Hk * columns) return;
   const int bh = static_cast<int>(item / columns), cc = static_cast<int>(item - static_cast<int64_t>(bh) * columns);
   const int b = bh / p.Hk, hk = bh - b * p.Hk, chunk = cc / cols;
@@ -734,36 +739,51 @@ __global__ void __launch_bounds__(128) attn_kv4_join_kernel(const __grid_constan
   const int64_t first = before * per_seq + static_cast<int64_t>(hk * p.col_chunks + chunk) * nb;
   const int c0 = cta_of(first + AK_START, total, ctas), c1 = cta_of(first + nb - 1, total, ctas);
   if (c0 == c1) return;                                          // never split: written by its CTA
-  int n = c1 - c0 + 1;
+  const int n = c1 - c0 + 1;
   auto piece_of = [&](int s) { return (2 * static_cast<int64_t>(c0 + s) + (s == 0)) * cols + (cc - chunk * cols); };
-  const int64_t pieces = 2 * static_cast<int64_t>(grid) * cols;
-  const float2* ml = reinterpret_cast<const float2*>(p.ws + pieces * D);
+  const float2* ml = reinterpret_cast<const float2*>(p.ws + 2 * static_cast<int64_t>(grid) * cols * D);
   float mm = -INFINITY;
   for (int s = lane; s < n; s += 32) mm = fmaxf(mm, ml[piece_of(s)].x);
 #pragma unroll
   for (int d = 16; d; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
-  if (mm == -INFINITY) n = 0;
   float ll = 0.f;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
   const bool live = lane * 4 < D;
+  if (mm != -INFINITY) {
 #pragma unroll 4
-  for (int s = 0; s < n; ++s) {
-    const int64_t piece = piece_of(s);
-    const float2 x = ml[piece];
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (live) v = *reinterpret_cast<const float4*>(p.ws + piece * D + lane * 4);
-    const float f = ak_ex2(x.x - mm);                            // 0 for a piece in which this column sees nothing
-    ll = fmaf(f, x.y, ll);
-    a.x = fmaf(f, v.x, a.x);
-    a.y = fmaf(f, v.y, a.y);
-    a.z = fmaf(f, v.z, a.z);
-    a.w = fmaf(f, v.w, a.w);
+    for (int s = warp; s < n; s += JW) {
+      const int64_t piece = piece_of(s);
+      const float2 x = ml[piece];
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (live) v = *reinterpret_cast<const float4*>(p.ws + piece * D + lane * 4);
+      const float f = ak_ex2(x.x - mm);                          // 0 for a piece in which this column sees nothing
+      ll = fmaf(f, x.y, ll);
+      a.x = fmaf(f, v.x, a.x);
+      a.y = fmaf(f, v.y, a.y);
+      a.z = fmaf(f, v.z, a.z);
+      a.w = fmaf(f, v.w, a.w);
+    }
   }
+  if constexpr (JW > 1) {
+    s_o[warp][lane] = a;
+    if (lane == 0) s_l[warp] = ll;
+    __syncthreads();
+    if (warp != 0) return;
+#pragma unroll
+    for (int w = 1; w < JW; ++w) {
+      const float4 v = s_o[w][lane];
+      a.x += v.x;
+      a.y += v.y;
+      a.z += v.z;
+      a.w += v.w;
+      ll += s_l[w];
+    }
+  }
+  if (!live) return;
   const float r = ll == 0.f ? 0.f : 1.0f / ll;
   const int qi = cc / p.g, hh = cc - qi * p.g;
-  if (live)
-    *reinterpret_cast<uint2*>(p.o + b * p.ob + qi * p.on + static_cast<int64_t>(hk * p.g + hh) * p.oh + lane * 4) =
-        make_uint2(pack_bf16(a.x * r, a.y * r), pack_bf16(a.z * r, a.w * r));
+  *reinterpret_cast<uint2*>(p.o + b * p.ob + qi * p.on + static_cast<int64_t>(hk * p.g + hh) * p.oh + lane * 4) =
+      make_uint2(pack_bf16(a.x * r, a.y * r), pack_bf16(a.z * r, a.w * r));
 }
 
 int attn_kv4_cols(int columns) { return columns <= 8 ? 8 : 16; }
@@ -785,7 +805,11 @@ cudaError_t ak_run(const Kv4AttnParams& p, cudaStream_t s) {
   e = launch_following(kern, dim3(static_cast<unsigned>(p.ctas)), AK_THREADS, smem, s, p);
   if (e != cudaSuccess || p.block >= p.max_len || p.ctas == 1) return e;
   const int64_t items = static_cast<int64_t>(p.B) * p.Hk * p.n * p.g;
-  return launch_following(attn_kv4_join_kernel<D>, dim3(static_cast<unsigned>((items + 3) / 4)), 128, 0, s, p, 8 * NT, p.ctas);
+  if (items > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
+  // pieces of a sequence and head, about: CTAs per (sequence, head, chunk)
+  if (p.ctas >= 4LL * p.B * p.Hk * p.col_chunks)
+    return launch_following(attn_kv4_join_kernel<D, 8>, dim3(static_cast<unsigned>(items)), 256, 0, s, p, 8 * NT, p.ctas);
+  return launch_following(attn_kv4_join_kernel<D, 1>, dim3(static_cast<unsigned>((items + 3) / 4)), 128, 0, s, p, 8 * NT, p.ctas);
 }
 
 template <int D, int G>
