@@ -152,7 +152,7 @@ __device__ __forceinline__ uint32_t code_off(int r, int c) {
 // work costs its blocks and a start (positions, page numbers, queries, joining the warps) worth about AK_START blocks: the row
 // has that many empty ones ahead of every sequence's own, so that stretches of many short sequences are no longer than others.
 __device__ __forceinline__ int length_of(const Kv4AttnParams& p, int b) {
-  const int len = __ldg(p.lengths + b);
+  const int len = p.lengths[b];
   return len < 0 ? 0 : min(len, p.max_len);
 }
 __device__ __forceinline__ int blocks_of(const Kv4AttnParams& p, int len) { return max((len + p.block - 1) / p.block, 1) + AK_START; }
@@ -229,7 +229,7 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
     const int tok = t_begin + (warp + AK_WARPS * (i + (lane >> 1))) * AK_TILE + (lane & 1) * 16;
     pages = 0;
     if (tok < t_end) {
-      pages = __ldg(trow + (tok >> p.page_shift));
+      pages = trow[tok >> p.page_shift];
       if (pages < 0 || pages >= p.num_pages) {
         report(p.status, DEV_BAD_PAGE);
         pages = 0;

@@ -91,7 +91,7 @@ __device__ __forceinline__ Raw<T> load16(const T* x) {
   if constexpr (VEC) {
 #pragma unroll
     for (int i = 0; i < static_cast<int>(sizeof(T)); ++i) {
-      const uint4 u = __ldg(reinterpret_cast<const uint4*>(x) + i);
+      const uint4 u = reinterpret_cast<const uint4*>(x)[i];
       r.w[4 * i] = u.x; r.w[4 * i + 1] = u.y; r.w[4 * i + 2] = u.z; r.w[4 * i + 3] = u.w;
     }
   } else if constexpr (sizeof(T) == 2) {
@@ -187,7 +187,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_append_kernel(const __grid_con
     uint32_t t;
     split_row(p, row, &t, &head[i]);
     raw[i] = load16<T, VEC>(static_cast<const T*>(x.data) + t * x.token_stride + head[i] * x.head_stride + j * 16);
-    slot[i] = __ldg(p.slots + t);
+    slot[i] = p.slots[t];
   }
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_read_kernel(const __grid_const
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
     split_row(p, min(row0 + i * ROWS, p.rows - 1), &t[i], &h[i]);
-    slot[i] = row0 + i * ROWS < p.rows ? __ldg(p.slots + t[i]) : -1;
+    slot[i] = row0 + i * ROWS < p.rows ? p.slots[t[i]] : -1;
   }
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
@@ -294,8 +294,8 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_read_kernel(const __grid_const
     if (slot[i] < 0) continue;
     const int64_t page = slot[i] >> p.page_shift;
     const int64_t r = ((page * p.heads + h[i]) << p.page_shift) + (slot[i] & ((1 << p.page_shift) - 1));
-    word[i] = __ldg(reinterpret_cast<const uint32_t*>(p.codes[which] + r * (D / 2) + j * 4));
-    pw[i] = __ldg(p.params[which] + r * NG + j / GL);
+    word[i] = *reinterpret_cast<const uint32_t*>(p.codes[which] + r * (D / 2) + j * 4);
+    pw[i] = p.params[which][r * NG + j / GL];
   }
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
