@@ -112,6 +112,8 @@ gc_status_t check_attend(const char* who, const gc_kv4_cache_t* c, const gc_atte
     REFUSE(GC_ERR_SHAPE, "%s: max_length %d exceeds table_width %d pages of %d", who, d->max_length, d->table_width, c->page_size);
   if (d->max_length > 0x7FFFFFFF - 65536) REFUSE(GC_ERR_UNSUPPORTED, "%s: max_length too large", who);
   if (static_cast<int64_t>(d->batch) * c->kv_heads > (1 << 22)) REFUSE(GC_ERR_UNSUPPORTED, "%s: batch times heads too large", who);
+  if (static_cast<int64_t>(d->batch) * d->queries * d->q_heads > 0x7FFFFFFF)
+    REFUSE(GC_ERR_UNSUPPORTED, "%s: batch times queries times heads too large", who);
   return GC_OK;
 }
 

@@ -805,7 +805,6 @@ cudaError_t ak_run(const Kv4AttnParams& p, cudaStream_t s) {
   e = launch_following(kern, dim3(static_cast<unsigned>(p.ctas)), AK_THREADS, smem, s, p);
   if (e != cudaSuccess || p.block >= p.max_len || p.ctas == 1) return e;
   const int64_t items = static_cast<int64_t>(p.B) * p.Hk * p.n * p.g;
-  if (items > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
   // pieces of a sequence and head, about: CTAs per (sequence, head, chunk)
   if (p.ctas >= 4LL * p.B * p.Hk * p.col_chunks)
     return launch_following(attn_kv4_join_kernel<D, 8>, dim3(static_cast<unsigned>(items)), 256, 0, s, p, 8 * NT, p.ctas);

@@ -101,6 +101,11 @@ def test_attention_kv4_refusals(S):
     B.gc_attention_kv4(0, cache(), attend(batch=0), None, 0)
 
 
+def test_attention_kv4_refuses_more_rows_than_a_launch_takes(S):
+    many = dict(batch=1 << 20, queries=16, q_heads=512)          # 2^20 x 16 x 512 = 2^33 rows of the output
+    refused(UNSUPPORTED, lambda: B.gc_attention_kv4(0, cache(), attend(**many), None, 0))
+
+
 def test_attention_prompt_refusals(S):
     for status, kw in [(UNSUPPORTED, dict(head_dim=80)), (SHAPE, dict(batch=-1)), (SHAPE, dict(q_heads=3)), (SHAPE, dict(kv_heads=0)),
                        (ARG, dict(scale=math.nan)), (ARG, dict(scale=-1.0)), (UNSUPPORTED, dict(q_tokens=1 << 29)), (ARG, dict(q=heads(0))),
