@@ -282,6 +282,13 @@ def test_attend_split_lengths(S, lens, max_length):
     cache.query_status()
 
 
+@pytest.mark.parametrize("d,group", SHAPES)
+@pytest.mark.parametrize("n", [1, 3])
+@pytest.mark.parametrize("lens,hq,hk", [([6000], 6, 2), ([9000, 40], 4, 2), ([700 + 97 * i for i in range(15)], 8, 8)])
+def test_attend_in_many_and_in_few_pieces(S, d, group, n, lens, hq, hk):
+    attend_case(S, lens, n, hq, hk, d, group, 64, seed=n + d)
+
+
 def test_attend_scores_that_rise_and_fall(S):
     # scores of hundreds of binades in both directions: the reference has to be raised many times, and old parts vanish
     attend_case(S, [700, 129], 1, 8, 2, 128, 32, 16, seed=3, qscale=40.0)
@@ -584,6 +591,57 @@ def test_calls_on_a_stream_of_their_own(S):
         got = step()
     s.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+def test_calls_that_follow_one_another_closely(S):
+    # each call reads what the one before it wrote (or overwrites what it read), with nothing of another kind in between; rows
+    # begin in the middle of a memory sector.  Against the same calls with the device at rest between them.
+    g = gen(81)
+    b, hq, hk, d, page, rounds = 300, 8, 2, 64, 16, 24
+    room = randn(b * (hq + 2 * hk) * d + 8, g=g, dtype=torch.bfloat16)
+    begin = room.clone()
+    rows = room[8:].view(b, hq + 2 * hk, d)
+    q, k, v = rows[:, :hq], rows[:, hq:hq + hk], rows[:, hq + hk:]
+    pages = -(-rounds // page)
+    table = torch.randperm(b * pages, generator=g, device=DEV).to(torch.int32).reshape(b, pages)
+    inv = S.rotary_inv_freq(d, device=DEV)
+    pos = [torch.randint(0, 5000, (b,), generator=g, device=DEV) for _ in range(rounds)]
+    slots = [table[:, i // page].long() * page + i % page for i in range(rounds)]
+    lens = [torch.full((b,), i + 1, dtype=torch.int32, device=DEV) for i in range(rounds)]
+    cu = torch.arange(b + 1, dtype=torch.int32, device=DEV)
+    cache = S.KV4Cache.allocate(b * pages, page, hk, d, 32)
+    mid = torch.empty(b, 1, hq, d, dtype=torch.bfloat16, device=DEV)
+
+    def run(between):
+        room.copy_(begin)
+        for x in (cache.k_codes, cache.k_params, cache.v_codes, cache.v_params):
+            x.zero_()
+        kept = []
+        for i in range(rounds):
+            S.qk_norm_rope(q, k, pos[i], inv, q_out=q, k_out=k)
+            between()
+            cache.append(k, v, slots[i])
+            between()
+            cache.attend(q[:, None], table, lens[i], out=mid)
+            between()
+            S.attention_prompt(mid[:, 0], k, v, cu, out=q)
+            between()
+            cache.read(slots[i], k_out=k, v_out=v)
+            between()
+            if i % 6 == 5:
+                kept.append((room.clone(), mid.clone()))
+        return kept + [(cache.k_codes.clone(), cache.v_params.clone())]
+    want = run(torch.cuda.synchronize)
+    run(lambda: None)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run(lambda: None)
+    for _ in range(5):
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(got, want):
+            assert torch.equal(x[0], y[0]) and torch.equal(x[1], y[1])
+    cache.query_status()
 
 
 def test_results_do_not_depend_on_the_run(S):
