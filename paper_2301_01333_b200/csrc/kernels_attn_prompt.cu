@@ -573,6 +573,11 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       }
     }
   }
+  if (failed) {                                                  // copies and products in flight come to rest before the block exits
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000ull) {
+    }
+  }
   __syncwarp();
   tc_fence_before();
   __syncthreads();
