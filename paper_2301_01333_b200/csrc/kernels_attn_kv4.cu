@@ -35,7 +35,7 @@
 // Measured: 64 ragged sequences up to 8192 tokens, 8 heads of 128, groups of 64 (323 MB): 78 us = 4.1 TB/s; without any arithmetic
 // the same copies take 62, so the rest is instructions that the copies of 12 warps do not cover (about 610 a tile and eight columns,
 // half of them on the integer / logic pipe).  One sequence of 131071 tokens, 32 columns (142 MB, read twice, the second time from
-// the L2): 90 us, bound by instructions; its products alone, 8 clocks each on a scheduler, are 33.
+// the L2): 87 us, bound by instructions; its products alone, 8 clocks each on a scheduler, are 33.
 #include <cuda_fp16.h>
 
 #include <type_traits>
@@ -666,7 +666,8 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
   extern __shared__ uint4 smem_u4[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(smem_u4);
 
-  wait_for_predecessor();
+  // (in this order: the joining kernel reads the lengths before it waits, so it must not start before they are there)
+  asm volatile("griddepcontrol.wait;\n\tgriddepcontrol.launch_dependents;" ::: "memory");
   const int per_seq = p.Hk * p.col_chunks;
   int b, u, len, nb, k0 = 0;                                     // sequence, (head, chunk), its length, blocks, first block of mine
   int64_t left;                                                  // blocks to do
@@ -718,16 +719,17 @@ __device__ __forceinline__ int cta_of(int64_t x, int64_t total, int ctas) {
 // Joins the pieces of a split sequence for one column, in a fixed order.  JW = 1: a warp per column, four to a CTA.  JW = 8:
 // a CTA per column, each warp every eighth piece, then the warps; for sequences in many pieces, which one warp would read one
 // memory latency after the other (one sequence of 8000 tokens in 55: 27 us against 17; but 64 of them in two or three: 125
-// against 136, for so many CTAs have to be started).
+// against 136, for so many CTAs have to be started).  Where the pieces are is found out while the last CTAs of the kernel before
+// are still at work: one sequence of 8000 tokens 17.6, so 14.4 us; 64 of 1000 35.8, so 32.5.
 template <int D, int JW>
 __global__ void __launch_bounds__(JW == 1 ? 128 : JW * 32) attn_kv4_join_kernel(const __grid_constant__ Kv4AttnParams p, const int cols, int ctas) {
-  wait_for_predecessor();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   __shared__ float4 s_o[JW][32];
   __shared__ float s_l[JW];
   const int lane = threadIdx.x & 31, warp = JW == 1 ? 0 : threadIdx.x >> 5;
   const int columns = p.n * p.g;
-  const int64_t item = JW == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5) : blockIdx.x;
-  if (item >= static_cast<int64_t>(p.B) * p.Hk * columns) return;
+  const int64_t items = static_cast<int64_t>(p.B) * p.Hk * columns;
+  const int64_t item = min(JW == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5) : blockIdx.x, items - 1);   // (a surplus warp repeats the last)
   const int bh = static_cast<int>(item / columns), cc = static_cast<int>(item - static_cast<int64_t>(bh) * columns);
   const int b = bh / p.Hk, hk = bh - b * p.Hk, chunk = cc / cols;
   const int nb = blocks_of(p, length_of(p, b)), per_seq = p.Hk * p.col_chunks;
@@ -738,6 +740,7 @@ __global__ void __launch_bounds__(JW == 1 ? 128 : JW * 32) attn_kv4_join_kernel(
   // blocks first .. first + nb of the row: the CTAs that had them, in order
   const int64_t first = before * per_seq + static_cast<int64_t>(hk * p.col_chunks + chunk) * nb;
   const int c0 = cta_of(first + AK_START, total, ctas), c1 = cta_of(first + nb - 1, total, ctas);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   if (c0 == c1) return;                                          // never split: written by its CTA
   const int n = c1 - c0 + 1;
   auto piece_of = [&](int s) { return (2 * static_cast<int64_t>(c0 + s) + (s == 0)) * cols + (cc - chunk * cols); };
