@@ -94,7 +94,7 @@ gc_status_t check_rows(const char* who, const gc_kv4_cache_t* c, int dtype, int6
 
 // How one call of gc_attention_kv4 is laid out over the GPU.
 struct Layout {
-  int cols, col_chunks, block, ctas;
+  int cols, col_chunks, block, ctas, solo;
   size_t bytes;
 };
 
@@ -118,18 +118,25 @@ gc_status_t check_attend(const char* who, const gc_kv4_cache_t* c, const gc_atte
 }
 
 // One wave of CTAs, as many as fit, or one per 128 tokens where there are fewer.  Sequences of up to 512 tokens are not split:
-// joining their pieces would take another launch, longer than the three blocks it would save.
+// joining their pieces would take another launch, longer than the three blocks it would save.  Where there are more units of
+// work (sequence, head, chunk of columns) than CTAs fit, or a unit is a single tile, a warp takes a unit alone: what such a unit
+// costs is its chain of latencies, of which four times as many then overlap, and no warps have to be joined.  64 tokens, 120
+// sequences of 8 heads: 7.6 us against 14.0; 225 tokens, 8 queries of 64 heads on 4, 120 sequences: 65 against 135; 512
+// tokens, 200 sequences: 28 against 37; but 40 sequences of 512, fewer than fit: 16 against 11.  Up to 1024 tokens from three
+// times that many on (1000 tokens, 200 sequences: 50 against 61; 120 of them: 44 against 40): a long sequence among many
+// short ones is one warp's work.
 Layout lay_out(const gc_kv4_cache_t& c, const gc_attention_kv4_t& d, int num_sms) {
   Layout s = {};
   const int columns = d.queries * (d.q_heads / c.kv_heads);
   s.cols = attn_kv4_cols(columns);
   s.col_chunks = (columns + s.cols - 1) / s.cols;
-  s.block = d.max_length <= 512 ? 512 : 128;
   const int64_t units = static_cast<int64_t>(d.batch) * c.kv_heads * s.col_chunks;
-  const int64_t most = units * ((static_cast<int64_t>(d.max_length) + s.block - 1) / s.block);
   const int64_t fit = static_cast<int64_t>(num_sms) * attn_kv4_resident(c.head_dim, c.group, s.cols);
+  s.solo = d.max_length <= 32 || units > (d.max_length <= 512 ? fit : d.max_length <= 1024 ? 3 * fit : INT64_MAX);
+  s.block = s.solo || d.max_length <= 512 ? 1024 : 128;
+  const int64_t most = units * ((static_cast<int64_t>(d.max_length) + s.block - 1) / s.block);
   // (without splitting, a CTA per unit, and the hardware deals them out)
-  s.ctas = static_cast<int>(s.block >= d.max_length ? units : most < fit ? most : fit);
+  s.ctas = static_cast<int>(s.solo ? (units + 3) / 4 : s.block >= d.max_length ? units : most < fit ? most : fit);
   s.bytes = s.block >= d.max_length || s.ctas == 1 ? 0 : 2 * static_cast<size_t>(s.ctas) * s.cols * (c.head_dim + 2) * sizeof(float);
   return s;
 }
@@ -225,7 +232,7 @@ extern "C" gc_status_t gc_attention_kv4(void* cuda_stream, const gc_kv4_cache_t*
   p.width = d->table_width; p.max_len = d->max_length;
   p.num_pages = cache->num_pages; p.table_stride = d->table_stride;
   p.c = d->scale * 1.4426950408889634f;
-  p.block = sp.block; p.ctas = sp.ctas; p.col_chunks = sp.col_chunks;
+  p.block = sp.block; p.ctas = sp.ctas; p.col_chunks = sp.col_chunks; p.solo = sp.solo;
   p.q = static_cast<const __nv_bfloat16*>(d->q);
   p.qb = d->q_batch_stride; p.qn = d->q_query_stride; p.qh = d->q_head_stride;
   p.o = static_cast<__nv_bfloat16*>(d->out);

@@ -30,6 +30,7 @@
 //     stand in one row, of which each CTA takes an equal stretch, however unlike the lengths are.  Where a stretch ends
 //     inside a sequence, the pieces are joined by a second small kernel in their order.  (Against one CTA per 2048 tokens
 //     of a sequence: with equal costs for unlike pieces 97 us, so 88 for 64 ragged sequences up to 8192 tokens.)
+//   * Many short sequences: a warp per (sequence, head, chunk of columns), which writes its rows itself (gc_serving.cu says when).
 //   * The running maximum is a reference that is only raised when a score exceeds it by 2^8: one vote per tile instead
 //     of a reduction, and the sums stay far inside fp32.
 // Measured: 64 ragged sequences up to 8192 tokens, 8 heads of 128, groups of 64 (323 MB): 78 us = 4.1 TB/s; without any arithmetic
@@ -198,7 +199,8 @@ __device__ __forceinline__ int sequence_at(const Kv4AttnParams& p, int64_t at, i
 }
 
 // Blocks k0 .. k0 + kn of the nb of head hk of sequence b (len tokens), columns of one chunk.  NT: groups of eight columns.
-template <int D, int G, int NT>
+// SOLO: this warp alone does all of it.
+template <int D, int G, int NT, bool SOLO>
 __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, int b, int hk, int chunk, int len, int k0, int kn, int nb) {
   using L = KvLayout<D, G>;
   constexpr int NG = L::NG, KW = D / 32, MT = D / 16, COLS = 8 * NT;
@@ -209,7 +211,8 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
   const int t_begin = k0 * p.block, t_end = min(len, (k0 + kn) * p.block);
 
   const int tiles = t_end > t_begin ? (t_end - t_begin + AK_TILE - 1) / AK_TILE : 0;
-  const int mine = tiles > warp ? (tiles - warp + AK_WARPS - 1) / AK_WARPS : 0;      // tiles warp, warp + 4, ...
+  const int mine = SOLO ? tiles : tiles > warp ? (tiles - warp + AK_WARPS - 1) / AK_WARPS : 0;      // tiles warp, warp + 4, ...
+  auto token_of = [&](int i) { return t_begin + (SOLO ? i : warp + AK_WARPS * i) * AK_TILE; };
   const uint32_t ring_a = smem_u32(smem + warp * L::RING);
   const int* trow = p.table + b * p.table_stride;
   const int page_mask = (1 << p.page_shift) - 1;
@@ -226,7 +229,7 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
   // Page numbers of 16 tiles at a time, two per tile, one per lane.
   int pages = 0;
   auto fetch_pages = [&](int i) {
-    const int tok = t_begin + (warp + AK_WARPS * (i + (lane >> 1))) * AK_TILE + (lane & 1) * 16;
+    const int tok = token_of(i + (lane >> 1)) + (lane & 1) * 16;
     pages = 0;
     if (tok < t_end) {
       pages = trow[tok >> p.page_shift];
@@ -255,7 +258,7 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
   auto issue = [&](int i) {
     if (i < mine) {
       if ((i & 15) == 0) fetch_pages(i);
-      const int t0 = t_begin + (warp + AK_WARPS * i) * AK_TILE;
+      const int t0 = token_of(i);
       const int64_t row = ((static_cast<int64_t>(__shfl_sync(0xffffffffu, pages, 2 * (i & 15))) * p.Hk + hk) << p.page_shift) + (t0 & page_mask);
       const uint8_t* ks = kbase + row * L::ROW;
       const uint8_t* ps = pbase + row * (NG * 4);
@@ -374,7 +377,7 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
   // limits lie within n of the sequence's end; padding columns see nothing and are left as they come: nobody reads them).
   auto tile = [&](auto edge_c, int i, uint32_t kc) {
     constexpr bool EDGE = decltype(edge_c)::value;
-    const int t0 = t_begin + (warp + AK_WARPS * i) * AK_TILE;
+    const int t0 = token_of(i);
     const uint32_t kp = kc + pr * NG * 4;
     float s[2][NT][4];
     // Sums of one (16 rows, group) depend on one another: where registers allow, those of all groups take turns, else those
@@ -573,7 +576,7 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
   for (int i = 0; i < mine; ++i) {
     cp_wait<AK_STAGES - 2>();
     __syncwarp();
-    const int t_next = t_begin + (warp + AK_WARPS * i) * AK_TILE + AK_TILE;
+    const int t_next = token_of(i) + AK_TILE;
     if (t_next > len - (p.n - 1) || t_next > t_end) tile(std::true_type{}, i, st_out);
     else tile(std::false_type{}, i, st_out);
     __syncwarp();
@@ -595,6 +598,31 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
         for (int j = 0; j < NG; ++j) z[nt][j][e] += __shfl_xor_sync(0xffffffffu, z[nt][j][e], d);
       }
     }
+  }
+  if constexpr (SOLO) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int cc = col0 + nt * 8 + 2 * tg + e;
+        if (cc >= columns) continue;
+        const float r = l[nt][e] == 0.f ? 0.f : 1.0f / l[nt][e];
+        const int qi = cc / p.g, hh = cc - qi * p.g;
+        __nv_bfloat16* dst = p.o + b * p.ob + qi * p.on + static_cast<int64_t>(hk * p.g + hh) * p.oh + gr * (G / 8);
+#pragma unroll
+        for (int j = 0; j < NG; ++j) {
+          const float mid = fmaf(-7.5f, ws[nt][j][e], z[nt][j][e]);
+#pragma unroll
+          for (int u = 0; u < UG; ++u) {
+            const int k = (j * UG + u) * 2;
+            *reinterpret_cast<uint2*>(dst + j * G + 4 * u) =
+                make_uint2(pack_bf16(fmaf(o[nt][k][e] * 0x1p67f, 0x1p66f, mid) * r, fmaf(o[nt][k][e + 2] * 0x1p67f, 0x1p62f, mid) * r),
+                           pack_bf16(fmaf(o[nt][k + 1][e] * 0x1p67f, 0x1p66f, mid) * r, fmaf(o[nt][k + 1][e + 2] * 0x1p67f, 0x1p62f, mid) * r));
+          }
+        }
+      }
+    }
+    return;
   }
   __syncthreads();                                               // the rings are free
   constexpr int OP = D + 4;                                      // row pitch: neighbouring columns on other banks
@@ -661,7 +689,7 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
   __syncthreads();                                               // the next segment's copies may overwrite what was joined
 }
 
-template <int D, int G, int NT>
+template <int D, int G, int NT, bool SOLO>
 __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kernel(const __grid_constant__ Kv4AttnParams p) {
   extern __shared__ uint4 smem_u4[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(smem_u4);
@@ -671,6 +699,15 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
   const int per_seq = p.Hk * p.col_chunks;
   int b, u, len, nb, k0 = 0;                                     // sequence, (head, chunk), its length, blocks, first block of mine
   int64_t left;                                                  // blocks to do
+  if constexpr (SOLO) {                                          // a warp per (sequence, head, chunk)
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * AK_WARPS + (threadIdx.x >> 5);
+    if (unit >= static_cast<int64_t>(p.B) * per_seq) return;
+    b = static_cast<int>(unit / per_seq);
+    u = static_cast<int>(unit - static_cast<int64_t>(b) * per_seq);
+    if (u == 0 && (threadIdx.x & 31) == 0 && (p.lengths[b] < 0 || p.lengths[b] > p.max_len)) report(p.status, DEV_BAD_LENGTH);
+    segment<D, G, NT, true>(p, smem, b, u / p.col_chunks, u % p.col_chunks, length_of(p, b), 0, 1, 1);
+    return;
+  }
   if (p.block >= p.max_len) {                                    // nothing is split: a CTA per (sequence, head, chunk)
     b = blockIdx.x / per_seq;
     u = blockIdx.x - b * per_seq;
@@ -699,7 +736,7 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
   for (; left > 0;) {
     const int kn = static_cast<int>(min(static_cast<int64_t>(nb - k0), left));
     const int first = max(k0 - AK_START, 0), behind = k0 + kn - AK_START;
-    if (behind > first) segment<D, G, NT>(p, smem, b, u / p.col_chunks, u % p.col_chunks, len, first, behind - first, nb - AK_START);
+    if (behind > first) segment<D, G, NT, false>(p, smem, b, u / p.col_chunks, u % p.col_chunks, len, first, behind - first, nb - AK_START);
     left -= kn;
     k0 = 0;
     if (++u == per_seq && left > 0) {
@@ -801,7 +838,7 @@ constexpr size_t ak_smem() {
 
 template <int D, int G, int NT>
 cudaError_t ak_run(const Kv4AttnParams& p, cudaStream_t s) {
-  auto kern = attn_kv4_kernel<D, G, NT>;
+  auto kern = p.solo ? attn_kv4_kernel<D, G, NT, true> : attn_kv4_kernel<D, G, NT, false>;
   constexpr size_t smem = ak_smem<D, G, NT>();
   cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
   if (e != cudaSuccess) return e;

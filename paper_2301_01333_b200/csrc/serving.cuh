@@ -44,6 +44,7 @@ struct Kv4AttnParams {
   float c;                          // scale * log2(e)
   int block, ctas;                  // tokens per block (a multiple of 128) of the row of blocks that `ctas` CTAs share out
   int col_chunks;                   // chunks the columns of a (sequence, head) are taken in
+  int solo;                         // 1: a warp per (sequence, head, chunk), nothing split
   const __nv_bfloat16* q;
   int64_t qb, qn, qh;
   __nv_bfloat16* o;

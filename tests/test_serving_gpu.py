@@ -289,6 +289,44 @@ def test_attend_in_many_and_in_few_pieces(S, d, group, n, lens, hq, hk):
     attend_case(S, lens, n, hq, hk, d, group, 64, seed=n + d)
 
 
+@pytest.mark.parametrize("d,group", SHAPES)
+@pytest.mark.parametrize("n,hq,hk", [(1, 16, 16), (3, 32, 16), (5, 32, 8)])
+def test_attend_many_short_sequences(S, d, group, n, hq, hk):
+    lens = [7 * i * i % 131 for i in range(30)]
+    attend_case(S, lens, n, hq, hk, d, group, 16, seed=n + d)
+    attend_case(S, [x % 33 for x in lens[:7]], n, hq, hk, d, group, 32, seed=n + d + 1, max_length=32)
+
+
+def test_attend_many_longer_sequences(S):
+    attend_case(S, [13 * i * i % 701 + 1 for i in range(89)] + [1000], 1, 32, 16, 128, 64, 64, seed=5)
+
+
+@pytest.mark.parametrize("n", [1, 3])
+def test_attend_many_short_sequences_ignore_what_lies_behind(S, n):
+    g = gen(19)
+    b, page, h, d, group = 70, 32, 8, 128, 64
+    lens = [1 + 11 * i % 95 for i in range(b)]
+    cache = filled_cache(S, 3 * b, page, h, d, group, g)
+    table = torch.randperm(3 * b, generator=g, device=DEV).to(torch.int32).reshape(b, 3)
+    q = randn(b, n, 2 * h, d, g=g, dtype=torch.bfloat16)
+    ln = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    want = cache.attend(q, table, ln)
+    ref, tol = attend_reference(cache, q, table, lens, d ** -0.5, group)
+    within(want, ref, tol)
+    for i, m in enumerate(lens):
+        for t in range(m, 3 * page):
+            for params in (cache.k_params, cache.v_params):
+                params[table[i, t // page], :, t % page] = torch.tensor([math.nan, math.inf], device=DEV, dtype=torch.bfloat16)
+    for i, m in enumerate(lens):                                 # pages behind the last are not looked at either
+        table[i, -(-m // page):] = 1 << 30
+    assert torch.equal(cache.attend(q, table, ln), want)
+    cache.query_status()
+    ln[5], ln[6] = 97, -1
+    cache.attend(q, table, ln)
+    with pytest.raises(S.GcError):
+        cache.query_status()
+
+
 def test_attend_scores_that_rise_and_fall(S):
     # scores of hundreds of binades in both directions: the reference has to be raised many times, and old parts vanish
     attend_case(S, [700, 129], 1, 8, 2, 128, 32, 16, seed=3, qscale=40.0)
