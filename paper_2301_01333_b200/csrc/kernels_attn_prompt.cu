@@ -28,7 +28,7 @@
 // parts (945); two score buffers of 64 keys per tile, which takes the hand-over out of the way but makes S slower (N = 64: 1001).
 //   * The reference m is raised only when a score exceeds it by 2^8 (as in the cache attention): after the first block the
 //     output is almost never touched, and raising it is the softmax warps' own business - no extra role, no extra hand-over.
-//   * Persistent CTAs; the work list (256 query rows of a sequence, times heads) is made by each CTA from the sequence offsets
+//   * Persistent CTAs; the work list (256 query rows of a sequence, or 128 where there is little work, times heads) is made by each CTA from the sequence offsets
 //     and sorted by its number of key blocks, longest first, dealt out back and forth.  The first scores of the next item are
 //     issued before the last output of the current one has been stored.
 //   * Rows of another sequence may follow a sequence's own in a tile.  Foreign keys are masked by selection; foreign value
@@ -172,7 +172,7 @@ struct Item {
 template <int D>
 __global__ void __launch_bounds__(AP_THREADS, 1)
 attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                   const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PromptParams p, const int listed, const int most) {
+                   const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PromptParams p, const int listed, const int most, const int log_rows) {
   using L = PromptLayout<D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -221,7 +221,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       int nb = 0;
       if (b < p.B) {
         const Seq s = seq_of(p, b);
-        nb = (s.nq + 255) / 256;
+        nb = (s.nq + (1 << log_rows) - 1) >> log_rows;
         if (blockIdx.x == 0 && (p.cu_q[b] != s.q0 || p.cu_q[b + 1] != s.q0 + s.nq || p.cu_k[b] != s.k0 || p.cu_k[b + 1] != s.k0 + s.nk))
           report(p.status, DEV_BAD_OFFSETS);
       }
@@ -250,8 +250,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   if (sorted) {
     auto cost = [&](int e) {
       const Seq s = seq_of(p, e >> 12);
-      const int r0 = (e & 4095) * 256;
-      return tile_blocks(p, s, r0) + tile_blocks(p, s, r0 + 128);
+      const int r0 = (e & 4095) << log_rows;
+      return tile_blocks(p, s, r0) + (log_rows == 8 ? tile_blocks(p, s, r0 + 128) : 0);
     };
     // costs first (packed above the entry's number so that equal ones keep their order), then each entry's rank
     int mine[(AP_MAX_LIST + AP_THREADS - 1) / AP_THREADS], key[(AP_MAX_LIST + AP_THREADS - 1) / AP_THREADS];
@@ -298,7 +298,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     } else {
       int before = 0;
       for (int s0 = 0; s0 < p.B; s0 += 32) {
-        const int nb = s0 + lane < p.B ? (seq_of(p, s0 + lane).nq + 255) / 256 : 0;
+        const int nb = s0 + lane < p.B ? (seq_of(p, s0 + lane).nq + (1 << log_rows) - 1) >> log_rows : 0;
         int incl = nb;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -317,9 +317,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       }
     }
     it.s = seq_of(p, b);
-    it.row0 = blk * 256;
+    it.row0 = blk << log_rows;
     it.n[0] = tile_blocks(p, it.s, it.row0);
-    it.n[1] = tile_blocks(p, it.s, it.row0 + 128);
+    it.n[1] = log_rows == 8 ? tile_blocks(p, it.s, it.row0 + 128) : 0;
     return it;
   };
 
@@ -420,7 +420,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       }
       if (failed) break;
       ring += 2 * max(it.n[0], it.n[1]);
-      const bool store = my_row < it.s.nq;
+      const bool store = my_row < it.s.nq && t * 128 < 1 << log_rows;
       __nv_bfloat16* dst = p.o + static_cast<int64_t>(it.s.q0 + my_row) * p.o_tok + static_cast<int64_t>(it.head) * p.o_head;
       if (n == 0) {
         if (store) {
@@ -593,13 +593,16 @@ static cudaError_t prompt_run(const CUtensorMap& tmQ, const CUtensorMap& tmK, co
   auto kern = attn_prompt_kernel<D>;
   cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), PromptLayout<D>::SMEM);
   if (e != cudaSuccess) return e;
-  // what the offsets can come to at most: every sequence may end inside a block
-  const int64_t entries = p.q_tokens / 256 + p.B;
+  // 256 rows to an item, or 128 where even those leave SMs without work: the one tile then has the tensor core to itself (one
+  // prompt of 1693 tokens, 2 heads of 128: 36.7, so 32.8 us; 2048, 8 heads: 36.2, so 32.9; 512, 16 heads: 15.4, so 13.4)
+  // (entries: what the offsets can come to at most, for every sequence may end inside a block)
+  const int log_rows = (p.q_tokens / 128 + p.B) * p.Hq <= num_sms ? 7 : 8;
+  const int64_t entries = (p.q_tokens >> log_rows) + p.B;
   const int64_t items = entries * p.Hq;
   const int grid = static_cast<int>(items < num_sms ? items : num_sms);
   // the list packs a block number into 12 bits
   const int listed = entries <= AP_MAX_LIST && p.q_tokens <= 256 * 4096LL;
-  return launch_following(kern, dim3(static_cast<unsigned>(grid)), AP_THREADS, PromptLayout<D>::SMEM, s, tmQ, tmK, tmV, p, listed, static_cast<int>(entries));
+  return launch_following(kern, dim3(static_cast<unsigned>(grid)), AP_THREADS, PromptLayout<D>::SMEM, s, tmQ, tmK, tmV, p, listed, static_cast<int>(entries), log_rows);
 }
 
 cudaError_t launch_attn_prompt(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const PromptParams& p, int num_sms,
