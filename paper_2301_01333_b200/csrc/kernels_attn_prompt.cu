@@ -28,9 +28,9 @@
 // parts (945); two score buffers of 64 keys per tile, which takes the hand-over out of the way but makes S slower (N = 64: 1001).
 //   * The reference m is raised only when a score exceeds it by 2^8 (as in the cache attention): after the first block the
 //     output is almost never touched, and raising it is the softmax warps' own business - no extra role, no extra hand-over.
-//   * Persistent CTAs; the work list (256 query rows of a sequence, or 128 where there is little work, times heads) is made by each CTA from the sequence offsets
-//     and sorted by its number of key blocks, longest first, dealt out back and forth.  The first scores of the next item are
-//     issued before the last output of the current one has been stored.
+//   * Persistent CTAs; the work list (256 query rows of a sequence, or 128 where there is little work, times heads) is made by
+//     each CTA from the sequence offsets and sorted by its number of key blocks, longest first, dealt out back and forth.  The
+//     first scores of the next item are issued before the last output of the current one has been stored.
 //   * Rows of another sequence may follow a sequence's own in a tile.  Foreign keys are masked by selection; foreign value
 //     rows are overwritten with zeros in shared memory (0 times a stored infinity would be NaN); foreign query rows are not
 //     stored.

@@ -430,6 +430,13 @@ def test_prompt_packed(S, causal, d):
 
 
 @pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("n", [1, 127, 128, 129, 255, 256, 257, 400])
+def test_prompt_lengths_of_many_heads(S, causal, d, n):
+    prompt_case(S, [n, 130, 0, n + 3], [n + 1, 130, 5, n], 40, 8, d, causal, seed=n, tail=3, poison=True)
+
+
+@pytest.mark.parametrize("causal", [True, False])
 def test_prompt_continued_and_rows_that_see_nothing(S, causal):
     prompt_case(S, [5, 300, 1, 7, 260, 40], [700, 301, 129, 0, 3, 40], 4, 4, 128, causal, seed=1)
     prompt_case(S, [5, 300, 1, 7, 260, 40], [128, 301, 256, 0, 140, 39], 3, 1, 64, causal, seed=2)
