@@ -1,0 +1,69 @@
+"""The operators of the served attention block on a B200, at the edges of what their documentation allows: numbers that are not
+finite, batches that are laid out in unusual ways, calls right behind what wrote their inputs."""
+import math
+
+import pytest
+import torch
+
+import serving_reference as R
+from test_serving_gpu import DEV, S, attend_reference, filled_cache, gen, randn, table_of, within  # noqa: F401 (S: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------ numbers that are not finite
+@pytest.mark.parametrize("d,group", [(64, 64), (96, 32), (128, 32), (128, 128)])
+@pytest.mark.parametrize("n", [1, 3])
+@pytest.mark.parametrize("lens,bound", [([33, 5, 18], 96), ([20, 31, 32], 32), ([2000, 150, 6000], 6016)])
+def test_attend_of_queries_that_are_not_finite(S, d, group, n, lens, bound):
+    # a query that holds a NaN has no finite score: its output is NaN, in one piece or many, and no other query's is touched
+    g = gen(d + n)
+    page, hk, hq = 32, 2, 6
+    pages = sum(-(-x // page) for x in lens) + 2
+    cache = filled_cache(S, pages, page, hk, d, group, g)
+    table = table_of(lens, page, pages, g, width=bound // page)
+    ln = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    q = randn(len(lens), n, hq, d, g=g, dtype=torch.bfloat16)
+    want = cache.attend(q, table, ln, max_length=bound)
+    q[0, n - 1, 1, 5] = math.nan
+    q[2, 0, 4] = math.nan
+    got = cache.attend(q, table, ln, max_length=bound)
+    bad = torch.zeros(got.shape[:3], dtype=torch.bool, device=DEV)
+    bad[0, n - 1, 1] = bad[2, 0, 4] = True
+    assert torch.isnan(got[bad]).all() and torch.equal(got[~bad], want[~bad])
+    cache.query_status()
+
+
+@pytest.mark.parametrize("d,group", [(64, 64), (96, 32), (128, 64)])
+@pytest.mark.parametrize("lens,bound", [([40, 33], 96), ([32, 9], 32), ([3000, 600], 3008)])
+def test_attend_over_keys_that_are_all_held_as_nan(S, d, group, lens, bound):
+    # every key of one head is held as NaN, so no score is a number: the queries of that head are NaN, those of the other are not
+    g = gen(d)
+    page, hk, hq = 32, 2, 4
+    pages = sum(-(-x // page) for x in lens) + 2
+    cache = filled_cache(S, pages, page, hk, d, group, g)
+    table = table_of(lens, page, pages, g, width=bound // page)
+    ln = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    q = randn(len(lens), 1, hq, d, g=g, dtype=torch.bfloat16)
+    want = cache.attend(q, table, ln, max_length=bound)
+    cache.k_params[:, 0] = math.nan
+    got = cache.attend(q, table, ln, max_length=bound)
+    assert torch.isnan(got[:, :, :2]).all() and torch.equal(got[:, :, 2:], want[:, :, 2:])
+    cache.query_status()
+
+
+def test_attend_over_a_stretch_of_keys_held_as_nan(S):
+    # one stretch of 700 tokens, more than any warp's tiles in a row: whoever sees it is NaN
+    g = gen(3)
+    page, m = 64, 5000
+    cache = filled_cache(S, 80, page, 1, 128, 128, g)
+    table = table_of([m, m], page, 160, g)[:1].clamp(max=79)
+    table[0] = torch.randperm(80, generator=g, device=DEV)[:table.shape[1]].to(torch.int32)
+    ln = torch.tensor([m], dtype=torch.int32, device=DEV)
+    q = randn(1, 1, 4, 128, g=g, dtype=torch.bfloat16)
+    for t in range(1200, 1900):
+        cache.k_params[table[0, t // page], :, t % page] = math.nan
+    assert torch.isnan(cache.attend(q, table, ln)).all()
+    ln[0] = 1200
+    ref, tol = attend_reference(cache, q, table, [1200], 128 ** -0.5, 128)
+    within(cache.attend(q, table, ln), ref, tol)
