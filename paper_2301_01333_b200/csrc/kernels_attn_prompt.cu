@@ -212,7 +212,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     tmem_alloc(smem_u32(tmem_slot), 512);
     tmem_relinquish();
   }
-  wait_for_predecessor();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   // ---- the work list
   if (warp == 0) {
     int total = 0;
@@ -242,6 +242,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  // Not before this block has its tensor memory: a block of the next kernel that took the columns first would wait for this
+  // kernel's end, and this one for the columns.
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t tmem_base = *tmem_slot;
   const int entries = *s_total;
   const int64_t items = static_cast<int64_t>(entries) * p.Hq;

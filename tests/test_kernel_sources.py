@@ -1,0 +1,32 @@
+"""Rules that every kernel has to keep for the ones around it, read off the sources: a mistake here would hang the GPU, so it is not
+left to a run to find."""
+import os
+import re
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2301_01333_b200", "csrc")
+SOURCES = sorted(f for f in os.listdir(CSRC) if f.endswith(".cu"))
+
+
+def code_of(name):
+    with open(os.path.join(CSRC, name)) as f:
+        return re.sub(r"//[^\n]*", "", f.read())
+
+
+@pytest.mark.parametrize("name", SOURCES)
+def test_tensor_memory_is_taken_before_the_next_kernel_may_start(name):
+    """From the moment a kernel lets its successor start, the successor's blocks can take tensor memory and then wait for this
+    kernel's end; one warp of a block takes the columns, so a barrier of the block has to lie in between."""
+    code = code_of(name)
+    for take in re.finditer(r"\btmem_alloc2?\(smem", code):
+        rest = code[take.end():]
+        go = re.search(r"griddepcontrol\.launch_dependents|wait_for_predecessor\(\)", rest)
+        if go:
+            assert re.search(r"__syncthreads\(\)|cluster_sync_all\(\)", rest[:go.start()]), f"{name}: the next kernel may start too early"
+
+
+def test_the_rule_is_looked_for_where_it_matters():
+    taking = [n for n in SOURCES if re.search(r"\btmem_alloc2?\(smem", code_of(n))]
+    letting = [n for n in taking if "launch_dependents" in code_of(n) or "wait_for_predecessor" in code_of(n)]
+    assert "kernels_attn_prompt.cu" in letting and "kernels_gemm_tc.cu" in letting and len(letting) >= 8

@@ -67,3 +67,50 @@ def test_attend_over_a_stretch_of_keys_held_as_nan(S):
     ln[0] = 1200
     ref, tol = attend_reference(cache, q, table, [1200], 128 ** -0.5, 128)
     within(cache.attend(q, table, ln), ref, tol)
+
+
+# ------------------------------------------------------------------------------------------------ next to the framework's other kernels
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompts_between_attention_subgraphs(S, d):
+    # both kinds hold tensor memory, and blocks of both fit on an SM side by side: calls right behind one another, in a captured
+    # graph too, give what they give alone
+    from paper_2301_01333_b200 import binding as B
+    from paper_2301_01333_b200 import workloads as W
+    w = W.mha_bf16(batch=16, heads=12, seq=128, head_dim=64)
+    part = B.CompiledPartition(w.graph, 0)
+    ins, outs = B.device_inputs(w), B.device_outputs(w.graph)
+    g = gen(d)
+    n = [100, 30, 700, 1, 260]
+    cu = torch.tensor([0] + n, device=DEV).cumsum(0).to(torch.int32)
+    x = randn(sum(n), 12, d, g=g, dtype=torch.bfloat16)
+    o = torch.zeros(sum(n), 8, d, dtype=torch.bfloat16, device=DEV)
+    status = S.new_status(DEV)
+
+    def prompt():
+        S.attention_prompt(x[:, :8], x[:, 8:10], x[:, 10:], cu, out=o, status=status)
+    part.execute(ins, outs)
+    prompt()
+    torch.cuda.synchronize()
+    want = o.clone(), outs[0].clone()
+
+    def run():
+        for _ in range(20):
+            part.execute(ins, outs)
+            prompt()
+            prompt()
+            part.execute(ins, outs)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for _ in range(3):
+        o.fill_(math.nan)
+        outs[0].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, want[0]) and torch.equal(outs[0], want[1])
+    S.query_status(status)
+    part.query_status()
+    del graph
+    part.close()
