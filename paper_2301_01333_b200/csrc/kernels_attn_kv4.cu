@@ -659,15 +659,16 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
     float mm = -INFINITY;
 #pragma unroll
     for (int w = 0; w < AK_WARPS; ++w) mm = fmaxf(mm, s_m[w * COLS + col]);
+    // A warp in which the column saw nothing has minus infinity, and sums of zero; one whose scores are all NaN has minus infinity
+    // too, but sums that are NaN, which a factor of zero lets through.
+    const float ref = mm == -INFINITY ? 0.f : mm;
     float ll = 0.f;
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < AK_WARPS; ++w) {
-      const float lw = s_l[w * COLS + col];
-      if (lw == 0.f) continue;                                   // it saw nothing.  (Scores that are all NaN have no maximum, but their sum is NaN)
-      const float f = ak_ex2(s_m[w * COLS + col] - mm);
+      const float f = ak_ex2(s_m[w * COLS + col] - ref);
       const float4 v = *reinterpret_cast<const float4*>(s_o + (w * COLS + col) * OP + d);
-      ll = fmaf(f, lw, ll);
+      ll = fmaf(f, s_l[w * COLS + col], ll);
       a.x = fmaf(f, v.x, a.x);
       a.y = fmaf(f, v.y, a.y);
       a.z = fmaf(f, v.z, a.z);
@@ -789,14 +790,14 @@ __global__ void __launch_bounds__(JW == 1 ? 128 : JW * 32) attn_kv4_join_kernel(
   float ll = 0.f;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
   const bool live = lane * 4 < D;
+  const float ref = mm == -INFINITY ? 0.f : mm;                  // (as where the warps are joined: NaN sums pass)
 #pragma unroll 4
   for (int s = warp; s < n; s += JW) {
     const int64_t piece = piece_of(s);
     const float2 x = ml[piece];
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (live) v = *reinterpret_cast<const float4*>(p.ws + piece * D + lane * 4);
-    // a piece in which this column sees nothing has a sum of zero (one whose scores are all NaN has no maximum either, but a NaN sum)
-    const float f = x.y == 0.f ? 0.f : ak_ex2(x.x - mm);
+    const float f = ak_ex2(x.x - ref);                           // 0 for a piece in which this column sees nothing
     ll = fmaf(f, x.y, ll);
     a.x = fmaf(f, v.x, a.x);
     a.y = fmaf(f, v.y, a.y);
