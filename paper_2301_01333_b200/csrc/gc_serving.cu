@@ -137,7 +137,8 @@ Layout lay_out(const gc_kv4_cache_t& c, const gc_attention_kv4_t& d, int num_sms
   const int64_t most = units * ((static_cast<int64_t>(d.max_length) + s.block - 1) / s.block);
   // (without splitting, a CTA per unit, and the hardware deals them out)
   s.ctas = static_cast<int>(s.solo ? (units + 3) / 4 : s.block >= d.max_length ? units : most < fit ? most : fit);
-  s.bytes = s.block >= d.max_length || s.ctas == 1 ? 0 : 2 * static_cast<size_t>(s.ctas) * s.cols * (c.head_dim + 2) * sizeof(float);
+  // two pieces a CTA (outputs, maximum and sum of every column), and which they are
+  s.bytes = s.block >= d.max_length || s.ctas == 1 ? 0 : s.ctas * (2 * static_cast<size_t>(s.cols) * (c.head_dim + 2) * sizeof(float) + 8);
   return s;
 }
 }  // namespace

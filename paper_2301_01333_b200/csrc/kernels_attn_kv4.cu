@@ -157,20 +157,12 @@ __device__ __forceinline__ int length_of(const Kv4AttnParams& p, int b) {
   return len < 0 ? 0 : min(len, p.max_len);
 }
 __device__ __forceinline__ int blocks_of(const Kv4AttnParams& p, int len) { return max((len + p.block - 1) / p.block, 1) + AK_START; }
-// Blocks of the sequences before b (*before) and of all; called by whole warps.
-__device__ __forceinline__ int64_t blocks_before(const Kv4AttnParams& p, int b, int64_t* before) {
-  int64_t all = 0, mine = 0;
-  for (int s = threadIdx.x & 31; s < p.B; s += 32) {
-    const int n = blocks_of(p, length_of(p, s));
-    all += n;
-    if (s < b) mine += n;
-  }
+// Blocks of all sequences; called by whole warps.
+__device__ __forceinline__ int64_t all_blocks(const Kv4AttnParams& p) {
+  int64_t all = 0;
+  for (int s = threadIdx.x & 31; s < p.B; s += 32) all += blocks_of(p, length_of(p, s));
 #pragma unroll
-  for (int d = 16; d; d >>= 1) {
-    all += __shfl_xor_sync(0xffffffffu, all, d);
-    mine += __shfl_xor_sync(0xffffffffu, mine, d);
-  }
-  *before = mine;
+  for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
   return all;
 }
 // The sequence that has block number `at`, and the blocks before it; called by whole warps.
@@ -690,13 +682,22 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
   __syncthreads();                                               // the next segment's copies may overwrite what was joined
 }
 
+// Which (sequence, head, chunk) a CTA left a piece of: one that begins with it and does not reach its end, and one that begins
+// inside it; -1: none.  Behind the pieces in the workspace, one per CTA.
+struct PiecesOf {
+  int start, inside;
+};
+template <int D>
+__device__ __forceinline__ PiecesOf* pieces_of(const Kv4AttnParams& p, int cols, int ctas) {
+  return reinterpret_cast<PiecesOf*>(p.ws + 2 * static_cast<int64_t>(ctas) * cols * (D + 2));
+}
+
 template <int D, int G, int NT, bool SOLO>
 __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kernel(const __grid_constant__ Kv4AttnParams p) {
   extern __shared__ uint4 smem_u4[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(smem_u4);
 
-  // (in this order: the joining kernel reads the lengths before it waits, so it must not start before they are there)
-  asm volatile("griddepcontrol.wait;\n\tgriddepcontrol.launch_dependents;" ::: "memory");
+  wait_for_predecessor();
   const int per_seq = p.Hk * p.col_chunks;
   int b, u, len, nb, k0 = 0;                                     // sequence, (head, chunk), its length, blocks, first block of mine
   int64_t left;                                                  // blocks to do
@@ -717,8 +718,8 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
     left = nb = blocks_of(p, len);
   } else {
     // my stretch of the row of blocks, and the sequence it begins in
-    int64_t before;
-    const int64_t total = blocks_before(p, 0, &before) * per_seq;
+    const int64_t total = all_blocks(p) * per_seq;
+    if (gridDim.x > 1 && threadIdx.x == 0) *(pieces_of<D>(p, 8 * NT, gridDim.x) + blockIdx.x) = {-1, -1};
     if (blockIdx.x == 0 && threadIdx.x < 32) {
       for (int s = threadIdx.x; s < p.B; s += 32)
         if (p.lengths[s] < 0 || p.lengths[s] > p.max_len) report(p.status, DEV_BAD_LENGTH);
@@ -737,7 +738,13 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
   for (; left > 0;) {
     const int kn = static_cast<int>(min(static_cast<int64_t>(nb - k0), left));
     const int first = max(k0 - AK_START, 0), behind = k0 + kn - AK_START;
-    if (behind > first) segment<D, G, NT, false>(p, smem, b, u / p.col_chunks, u % p.col_chunks, len, first, behind - first, nb - AK_START);
+    if (behind > first) {
+      if (behind - first < nb - AK_START && threadIdx.x == 0) {
+        PiecesOf* mine = pieces_of<D>(p, 8 * NT, gridDim.x) + blockIdx.x;
+        (first == 0 ? mine->start : mine->inside) = b * per_seq + u;
+      }
+      segment<D, G, NT, false>(p, smem, b, u / p.col_chunks, u % p.col_chunks, len, first, behind - first, nb - AK_START);
+    }
     left -= kn;
     k0 = 0;
     if (++u == per_seq && left > 0) {
@@ -747,20 +754,13 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
     }
   }
 }
-// The CTA whose stretch [total c / ctas, total (c + 1) / ctas) has block x.
-__device__ __forceinline__ int cta_of(int64_t x, int64_t total, int ctas) {
-  int c = static_cast<int>(x * ctas / total);
-  while (total * (c + 1) / ctas <= x) ++c;
-  while (total * c / ctas > x) --c;
-  return c;
-}
 // Joins the pieces of a split sequence for one column, in a fixed order.  JW = 1: a warp per column, four to a CTA.  JW = 8:
 // a CTA per column, each warp every eighth piece, then the warps; for sequences in many pieces, which one warp would read one
 // memory latency after the other (one sequence of 8000 tokens in 55: 27 us against 17; but 64 of them in two or three: 125
-// against 136, for so many CTAs have to be started).  Where the pieces are is found out while the last CTAs of the kernel before
-// are still at work: one sequence of 8000 tokens 17.6, so 14.4 us; 64 of 1000 35.8, so 32.5.
+// against 136, for so many CTAs have to be started).  Which CTAs left the pieces is looked up in what they noted, so that nothing is read
+// before the wait.
 template <int D, int JW>
-__global__ void __launch_bounds__(JW == 1 ? 128 : JW * 32) attn_kv4_join_kernel(const __grid_constant__ Kv4AttnParams p, const int cols, int ctas) {
+__global__ void __launch_bounds__(JW == 1 ? 128 : JW * 32) attn_kv4_join_kernel(const __grid_constant__ Kv4AttnParams p, const int cols, const int ctas) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   __shared__ float4 s_o[JW][32];
   __shared__ float s_l[JW];
@@ -770,19 +770,29 @@ __global__ void __launch_bounds__(JW == 1 ? 128 : JW * 32) attn_kv4_join_kernel(
   const int64_t item = min(JW == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5) : blockIdx.x, items - 1);   // (a surplus warp repeats the last)
   const int bh = static_cast<int>(item / columns), cc = static_cast<int>(item - static_cast<int64_t>(bh) * columns);
   const int b = bh / p.Hk, hk = bh - b * p.Hk, chunk = cc / cols;
-  const int nb = blocks_of(p, length_of(p, b)), per_seq = p.Hk * p.col_chunks;
-  int64_t before;
-  const int64_t total = blocks_before(p, b, &before) * per_seq;
-  const int grid = ctas;
-  ctas = static_cast<int>(min(static_cast<int64_t>(ctas), total));
-  // blocks first .. first + nb of the row: the CTAs that had them, in order
-  const int64_t first = before * per_seq + static_cast<int64_t>(hk * p.col_chunks + chunk) * nb;
-  const int c0 = cta_of(first + AK_START, total, ctas), c1 = cta_of(first + nb - 1, total, ctas);
+  const int unit = bh * p.col_chunks + chunk;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (c0 == c1) return;                                          // never split: written by its CTA
-  const int n = c1 - c0 + 1;
+  // the CTA it begins in, and how many more have a piece of it: those that follow
+  const PiecesOf* noted = pieces_of<D>(p, cols, ctas);
+  int c0 = -1, n = 0;
+  for (int s0 = lane; s0 < ctas; s0 += 512) {                    // (three CTAs an SM: one round of loads, all under way at once)
+    int2 x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      x[i] = make_int2(-1, -1);
+      if (s0 + 32 * i < ctas) x[i] = *reinterpret_cast<const int2*>(noted + s0 + 32 * i);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (x[i].x == unit) c0 = s0 + 32 * i;
+      n += x[i].y == unit;
+    }
+  }
+  c0 = __reduce_max_sync(0xffffffffu, c0);
+  if (c0 < 0) return;                                            // never split: written by its CTA
+  n = __reduce_add_sync(0xffffffffu, n) + 1;
   auto piece_of = [&](int s) { return (2 * static_cast<int64_t>(c0 + s) + (s == 0)) * cols + (cc - chunk * cols); };
-  const float2* ml = reinterpret_cast<const float2*>(p.ws + 2 * static_cast<int64_t>(grid) * cols * D);
+  const float2* ml = reinterpret_cast<const float2*>(p.ws + 2 * static_cast<int64_t>(ctas) * cols * D);
   float mm = -INFINITY;
   for (int s = lane; s < n; s += 32) mm = fmaxf(mm, ml[piece_of(s)].x);
 #pragma unroll

@@ -17,8 +17,8 @@ enum : uint32_t {
 // Launches of this block follow one another closely: each may be set up while the kernel before it on the stream still runs
 // (programmatic dependent launch), and every thread of every kernel passes wait_for_predecessor() before it touches global memory
 // or returns - also where it has nothing to do: a kernel that ended without waiting would let the one behind it overtake the
-// one before it.  (One exception: the kernel that joins the pieces of a cache attention reads the sequences' lengths first.  The
-// kernel before it lets it start only once it has waited itself.)
+// one before it.  A kernel that takes tensor memory lets the next one start only once every one of its blocks has it, with a
+// barrier in between: a block of the next kernel could take the columns first, and the two would wait for each other.
 __device__ __forceinline__ void wait_for_predecessor() {
   asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
 }

@@ -30,3 +30,18 @@ def test_the_rule_is_looked_for_where_it_matters():
     taking = [n for n in SOURCES if re.search(r"\btmem_alloc2?\(smem", code_of(n))]
     letting = [n for n in taking if "launch_dependents" in code_of(n) or "wait_for_predecessor" in code_of(n)]
     assert "kernels_attn_prompt.cu" in letting and "kernels_gemm_tc.cu" in letting and len(letting) >= 8
+
+
+@pytest.mark.parametrize("name", [n for n in SOURCES if "launch_following(" in code_of(n)])
+def test_nothing_is_read_before_the_kernel_has_waited(name):
+    """Kernels that are started while the one before them still runs read its results, and those of the ones before it, only behind
+    griddepcontrol.wait; nothing else promises that they are there."""
+    code = code_of(name)
+    kernels = re.split(r"__global__ void", code)[1:]
+    assert kernels
+    for k in kernels:
+        wait = re.search(r"griddepcontrol\.wait|wait_for_predecessor\(\)", k)
+        assert wait, "a kernel that does not wait"
+        ahead = k[k.index("{"):wait.start()]
+        found = re.search(r"length_of|blocks_of|all_blocks|sequence_at|seq_of|\bp\.(\w+)\[|p\.ws|->|ld\.global|cp\.async", ahead)
+        assert not found, f"{name}: '{found.group(0)}' ahead of the wait"

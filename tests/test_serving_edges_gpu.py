@@ -114,3 +114,46 @@ def test_prompts_between_attention_subgraphs(S, d):
     part.query_status()
     del graph
     part.close()
+
+
+# ------------------------------------------------------------------------------------------------ right behind what wrote the inputs
+@pytest.mark.parametrize("lens,hq,hk,n", [([2046], 8, 2, 1), ([1278, 3070, 126, 5], 8, 8, 2), ([1023 + 128 * i for i in range(20)], 4, 1, 1)])
+def test_attend_right_behind_the_kernel_that_moves_the_lengths(S, lens, hq, hk, n):
+    # a captured step that adds one to the lengths in place, directly before attention in pieces, over the border of a block of 128
+    g = gen(len(lens))
+    page, bound = 64, 4096
+    pages = sum(-(-(x + 8) // page) for x in lens)
+    cache = filled_cache(S, pages, page, hk, 128, 64, g)
+    table = table_of([x + 8 for x in lens], page, pages, g, width=bound // page)
+    q = randn(len(lens), n, hq, 128, g=g, dtype=torch.bfloat16)
+    ln = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    start = ln.clone()
+    want = []
+    for i in range(6):
+        fresh = start + (i + 1)
+        torch.cuda.synchronize()
+        want.append(cache.attend(q, table, fresh, max_length=bound))
+    ref, tol = attend_reference(cache, q, table, [x + 6 for x in lens], 128 ** -0.5, 64)
+    within(want[-1], ref, tol)
+    out = torch.empty_like(q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ln.add_(1)
+        cache.attend(q, table, ln, max_length=bound, out=out)
+    for rep in range(4):
+        ln.copy_(start)
+        for w in want:                                           # one replay behind the other, nothing in between but the copy
+            graph.replay()
+            assert torch.equal(out.clone(), w)
+    one = torch.cuda.CUDAGraph()
+    outs = [torch.empty_like(q) for _ in want]
+    with torch.cuda.graph(one):                                  # and all steps in one graph
+        for o in outs:
+            ln.add_(1)
+            cache.attend(q, table, ln, max_length=bound, out=o)
+    for rep in range(4):
+        ln.copy_(start)
+        one.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want))
+    cache.query_status()
