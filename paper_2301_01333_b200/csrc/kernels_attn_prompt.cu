@@ -283,7 +283,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       if (tid + k * AP_THREADS < entries) s_item[rank[k]] = mine[k];
     __syncthreads();
   }
-  // Item number r of this CTA; called by whole warps.
+  // Item number r of this CTA; called by whole warps, with r rising: beyond what the list holds, the search for an entry's sequence
+  // goes on where the last one of this warp ended (from the first sequence on each time, 4000 prompts of 64 tokens, 16
+  // heads, took 31 ms).
+  int group = 0, before = 0;                                     // sequences from `group` on, entries ahead of them
   auto item_of = [&](int r) {
     Item it;
     const int64_t g = static_cast<int64_t>(r) * gridDim.x + ((r & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
@@ -299,9 +302,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       b = list[e] >> 12;
       blk = list[e] & 4095;
     } else {
-      int before = 0;
-      for (int s0 = 0; s0 < p.B; s0 += 32) {
-        const int nb = s0 + lane < p.B ? (seq_of(p, s0 + lane).nq + (1 << log_rows) - 1) >> log_rows : 0;
+      for (; group < p.B; group += 32) {
+        const int nb = group + lane < p.B ? (seq_of(p, group + lane).nq + (1 << log_rows) - 1) >> log_rows : 0;
         int incl = nb;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -311,7 +313,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         const uint32_t hit = __ballot_sync(0xffffffffu, before + incl > e);
         if (hit) {
           const int w = __ffs(hit) - 1;
-          b = s0 + w;
+          b = group + w;
           const int first = before + __shfl_sync(0xffffffffu, incl - nb, w), count = __shfl_sync(0xffffffffu, nb, w);
           blk = count - 1 - (e - first);                        // the longest rows of a sequence first
           break;

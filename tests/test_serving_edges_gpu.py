@@ -157,3 +157,56 @@ def test_attend_right_behind_the_kernel_that_moves_the_lengths(S, lens, hq, hk, 
         torch.cuda.synchronize()
         assert all(torch.equal(o, w) for o, w in zip(outs, want))
     cache.query_status()
+
+
+# ------------------------------------------------------------------------------------------------ prompts in unusual batches
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d,hq,hk", [(64, 6, 2), (128, 16, 4), (96, 5, 5)])
+def test_prompt_batches_beyond_the_work_list(S, causal, d, hq, hk):
+    # more pieces than the sorted list holds, several heads, sequences of several pieces among empty ones: bit for bit what the same
+    # sequences give a hundred at a time, and a few of them against 64 bits
+    r = torch.Generator().manual_seed(d)
+    n = torch.randint(0, 40, (2500,), generator=r)
+    n[torch.randint(0, 2500, (300,), generator=r)] = 0
+    n[[3, 900, 901, 2499]] = torch.tensor([700, 257, 513, 1100])
+    lens = n.tolist()
+    cu = torch.tensor([0] + lens).cumsum(0).to(torch.int32)
+    g = gen(d)
+    x = randn(int(cu[-1]) + 9, hq + 2 * hk, d, g=g, dtype=torch.bfloat16)
+    q, k, v = x[:, :hq], x[:, hq:hq + hk], x[:, hq + hk:]
+    status = S.new_status(DEV)
+    out = torch.full((x.shape[0], hq, d), 0.25, dtype=torch.bfloat16, device=DEV)
+    S.attention_prompt(q, k, v, cu.to(DEV), causal=causal, out=out, status=status)
+    S.query_status(status)
+    assert (out[int(cu[-1]):] == 0.25).all()
+    for b0 in range(0, 2500, 100):
+        t0, t1 = int(cu[b0]), int(cu[b0 + 100])
+        part = S.attention_prompt(q[t0:t1], k[t0:t1], v[t0:t1], (cu[b0:b0 + 101] - t0).to(DEV), causal=causal)
+        assert torch.equal(out[t0:t1], part)
+    U = torch.finfo(torch.bfloat16).eps / 2
+    for b in (0, 3, 900, 1501, 2499):
+        t0, m = int(cu[b]), lens[b]
+        if m == 0:
+            continue
+        lim = torch.arange(1, m + 1, device=DEV) if causal else torch.full((m,), m, device=DEV)
+        for h in range(hq):
+            ref, size = R.head_all(q[t0:t0 + m, h].double(), k[t0:t0 + m, h // (hq // hk)].double(), v[t0:t0 + m, h // (hq // hk)].double(), lim, d ** -0.5)
+            # probabilities rounded to bf16 and the output's own rounding; what fp32 adds is below a hundredth of that
+            within(out[t0:t0 + m, h], ref, 1.01 * U * size + U * ref.abs() + 1e-6)
+
+
+def test_prompt_work_grows_with_the_batch_and_not_with_its_square(S):
+    def took(batch):
+        x = torch.zeros(batch, 1, 64, dtype=torch.bfloat16, device=DEV)
+        cu, out = torch.arange(batch + 1, dtype=torch.int32, device=DEV), torch.empty_like(x)
+        best = math.inf
+        for _ in range(5):
+            begin, end = torch.cuda.Event(True), torch.cuda.Event(True)
+            torch.cuda.synchronize()
+            begin.record()
+            S.attention_prompt(x, x, x, cu, out=out)
+            end.record()
+            end.synchronize()
+            best = min(best, begin.elapsed_time(end))
+        return best
+    assert took(16000) < 60 * took(1000)                         # sixteen times the work; searched from the start each time, it is hundreds
