@@ -1,7 +1,9 @@
 """In-tree build of the CUDA library (sm_100a only) with nvcc.
 
 ``python -m paper_2301_01333_b200.build`` compiles ``csrc/*.cu`` into ``libgc_b200.so`` next to this
-file, and ``csrc/serving_torch.cpp``, the torch side of ``serving.py``, into ``_serving.so``.  nvcc cross-compiles without a GPU, so this also runs on a CPU-only box.
+file, and ``csrc/serving_torch.cpp``, the torch side of ``serving.py``, into ``_serving.so``.  nvcc cross-compiles without a GPU,
+so this also runs on a CPU-only box.  The C interface needs nothing but nvcc: where torch, its headers, Python's or a C++20 g++
+are missing, the torch side is left out, with a line that says so, and only ``serving.py`` cannot be imported.
 """
 from __future__ import annotations
 
@@ -45,6 +47,23 @@ def _torch_stale() -> bool:
     return not os.path.exists(TORCH_LIB) or any(os.path.getmtime(d) > os.path.getmtime(TORCH_LIB) for d in deps)
 
 
+def _torch_side_lacks() -> str:
+    """What the torch side cannot be compiled without and is not there, or an empty string."""
+    import sysconfig
+    try:
+        import torch
+        from torch.utils import cpp_extension as X
+    except ImportError as e:
+        return f"torch ({e})"
+    if not any(os.path.exists(os.path.join(d, "ATen", "core", "Tensor.h")) for d in X.include_paths()):
+        return f"the headers of torch {torch.__version__}"
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        return "Python.h"
+    if not shutil.which("g++") or subprocess.run(["g++", "-std=c++20", "-fsyntax-only", "-x", "c++", os.devnull], capture_output=True).returncode:
+        return "a g++ that knows C++20"
+    return ""
+
+
 def _torch_command():
     """The command that compiles ``_serving.so`` against the installed torch and the library next to it."""
     import sysconfig
@@ -73,7 +92,11 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if force or _stale():
         _build_cuda(verbose)
     if force or _torch_stale():
-        _build_torch(verbose)
+        lacks = _torch_side_lacks()
+        if lacks:
+            sys.stderr.write(f"serving.py's torch side is left out: {lacks} is missing\n")
+        else:
+            _build_torch(verbose)
     return LIB
 
 
