@@ -42,9 +42,23 @@ def _stale() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _torch_abi() -> str:
+    """The torch and the Python that the torch side is compiled for; stands in ``_serving.so`` as a text."""
+    import importlib.metadata
+    import sysconfig
+    try:
+        version = importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:
+        version = "none"
+    return f"built for torch {version}, {sysconfig.get_config_var('SOABI')}"
+
+
 def _torch_stale() -> bool:
     deps = [TORCH_SOURCE, os.path.join(HERE, "..", "include", "gc.h")]
-    return not os.path.exists(TORCH_LIB) or any(os.path.getmtime(d) > os.path.getmtime(TORCH_LIB) for d in deps)
+    if not os.path.exists(TORCH_LIB) or any(os.path.getmtime(d) > os.path.getmtime(TORCH_LIB) for d in deps):
+        return True
+    with open(TORCH_LIB, "rb") as f:
+        return _torch_abi().encode() + b"\0" not in f.read()
 
 
 def _torch_side_lacks() -> str:
@@ -73,7 +87,7 @@ def _torch_command():
     inc = X.include_paths() + [sysconfig.get_paths()["include"], "/usr/local/cuda/include"]
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     return (["g++", "-O2", "-std=c++20", "-fPIC", "-shared", "-fvisibility=hidden",
-             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DSERVING_ABI="{_torch_abi()}"']
             + [a for d in inc for a in ("-isystem", d)] + [TORCH_SOURCE, "-o", TORCH_LIB + ".new", LIB, "-L" + libs]
             + ["-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN"])
 

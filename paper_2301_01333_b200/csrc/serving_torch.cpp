@@ -291,4 +291,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_serving", nullptr, -1, methods, n
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__serving(void) { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__serving(void) {
+  PyObject* m = PyModule_Create(&module);
+  // which torch and Python this was compiled for: the build looks for the text and compiles again under others
+  if (m && PyModule_AddStringConstant(m, "abi", SERVING_ABI)) Py_CLEAR(m);
+  return m;
+}

@@ -45,3 +45,19 @@ def test_a_mistake_in_the_torch_side_still_fails_the_build(elsewhere, monkeypatc
     monkeypatch.setattr(B, "TORCH_SOURCE", str(bad))
     with pytest.raises(RuntimeError):
         B.build()
+
+
+def test_the_torch_side_is_compiled_again_for_another_torch(monkeypatch):
+    import importlib.metadata
+    B.build()
+    assert not B._torch_stale()
+    real = importlib.metadata.version
+    monkeypatch.setattr(importlib.metadata, "version", lambda name: "9.9.9" if name == "torch" else real(name))
+    assert B._torch_stale()
+
+
+def test_the_torch_side_says_what_it_was_compiled_for():
+    import importlib.metadata
+    B.build()
+    from paper_2301_01333_b200 import _serving
+    assert importlib.metadata.version("torch") in _serving.abi
