@@ -4,6 +4,7 @@
 // against 6 us a call).  serving.py is the public face; nothing here computes.
 #include <ATen/cuda/EmptyTensor.h>
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
@@ -43,7 +44,10 @@ std::string shape_of(const at::Tensor& t) {
 
 const at::Tensor& tensor(PyObject* o, const char* name) {
   if (!THPVariable_Check(o)) throw TypeFault(std::string(name) + " must be a torch.Tensor");
-  return THPVariable_Unpack(o);
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (t.requires_grad() && at::GradMode::is_enabled())
+    refuse("%s requires a gradient, which this call does not give: detach it, or call under torch.no_grad()", name);
+  return t;
 }
 bool given(PyObject* o) { return o != Py_None; }
 

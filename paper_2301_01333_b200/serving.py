@@ -1,9 +1,10 @@
 """The operators of a served attention block on torch tensors: argument checks and marshalling for the ``gc_qk_norm_rope``,
 ``gc_kv4_*`` and ``gc_attention_*`` entry points of ``include/gc.h``, which state what each computes.
 
-They serve: no gradient is recorded.  All of them are asynchronous on the current stream of their tensors' device, take strided tensors (the last dimension
-contiguous), can be captured into a CUDA graph (after a first call outside the capture, which loads their kernels), and raise ``GcError`` (or ``TypeError`` / ``ValueError`` for tensors of the
-wrong type, shape or device) before anything is launched.  What only the device can see - a slot, page, length or offset out
+They serve: no gradient is recorded, and a tensor that requires one is refused unless gradients are off (``torch.no_grad()``).
+All of them are asynchronous on the current stream of their tensors' device, take strided tensors (the last dimension
+contiguous), can be captured into a CUDA graph (after a first call outside the capture, which loads their kernels), and raise
+``GcError`` (or ``TypeError`` / ``ValueError`` for tensors of the wrong type, shape or device) before anything is launched.  What only the device can see - a slot, page, length or offset out
 of bounds - leaves the outputs of that call undefined and is recorded in a status word: ``KV4Cache.query_status()``, or
 ``query_status(word)`` for the word given to ``attention_prompt``.
 """

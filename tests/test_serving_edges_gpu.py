@@ -210,3 +210,31 @@ def test_prompt_work_grows_with_the_batch_and_not_with_its_square(S):
             best = min(best, begin.elapsed_time(end))
         return best
     assert took(16000) < 60 * took(1000)                         # sixteen times the work; searched from the start each time, it is hundreds
+
+
+# ------------------------------------------------------------------------------------------------ gradients
+def test_tensors_that_require_a_gradient_are_refused(S):
+    x = torch.ones(3, 2, 64, device=DEV, dtype=torch.bfloat16)
+    g = x.clone().requires_grad_()
+    w = torch.nn.Parameter(x[0, 0].clone())
+    pos, inv = torch.arange(3, device=DEV), S.rotary_inv_freq(64, device=DEV)
+    cu = torch.tensor([0, 3], dtype=torch.int32, device=DEV)
+    cache = S.KV4Cache.allocate(2, 16, 2, 64, 32)
+    table, lens = torch.zeros(1, 1, dtype=torch.int32, device=DEV), torch.ones(1, dtype=torch.int32, device=DEV)
+    cache.append(x, x, pos)
+    calls = [lambda: S.qk_norm_rope(g, x, pos, inv), lambda: S.qk_norm_rope(x, g, pos, inv), lambda: S.qk_norm_rope(x, x, pos, inv, w),
+             lambda: S.qk_norm_rope(x, x, pos, inv, None, w), lambda: S.qk_norm_rope(x, x, pos, inv, q_out=g.clone()),
+             lambda: S.qk_norm_rope(x, x, pos, inv, k_out=g.clone()), lambda: cache.append(g, x, pos), lambda: cache.append(x, g, pos),
+             lambda: cache.read(pos, k_out=g.clone()), lambda: cache.read(pos, v_out=g.clone()), lambda: cache.attend(g[None, :1], table, lens),
+             lambda: cache.attend(x[None, :1], table, lens, out=g[None, :1].clone()), lambda: S.attention_prompt(g, x, x, cu),
+             lambda: S.attention_prompt(x, g, x, cu), lambda: S.attention_prompt(x, x, g, cu), lambda: S.attention_prompt(x, x, x, cu, out=g.clone())]
+    for i, call in enumerate(calls):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+            print("call", i, "was not refused")
+    with torch.no_grad():
+        for call in calls:
+            call()
+    with torch.inference_mode():
+        S.qk_norm_rope(x, x, pos, inv, w)
+    cache.query_status()
