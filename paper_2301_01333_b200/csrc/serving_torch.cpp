@@ -87,6 +87,14 @@ at::Tensor empty(at::IntArrayRef sizes, at::ScalarType type, const at::Device& d
 
 void* stream_of(int device) { return c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(device)).stream(); }
 
+// Tells autograd that a tensor the caller handed over has been written to (one it keeps for a backward pass is then missed there).
+void written(const at::Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+void written(PyObject* tensors) {
+  for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(tensors); ++i) written(THPVariable_Unpack(PyTuple_GET_ITEM(tensors, i)));
+}
+
 void check(gc_status_t st) {
   if (st != GC_OK) throw GcFault{st};
 }
@@ -169,14 +177,16 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     d.q_out = heads(qo, "q_out", d.tokens, d.q_heads, d.head_dim, type, device, true);
     d.k_out = heads(ko, "k_out", d.tokens, d.k_heads, d.head_dim, type, device, true);
     check(gc_qk_norm_rope(stream_of(d.cuda_device), &d));
+    if (given(a[10])) written(qo);
+    if (given(a[11])) written(ko);
     THPObjectPtr x(THPVariable_Wrap(qo)), y(THPVariable_Wrap(ko));
     return x && y ? PyTuple_Pack(2, x.get(), y.get()) : nullptr;
   });
 }
 
-// (cache, k, v, slots)
+// (cache, k, v, slots, the cache's four tensors)
 PyObject* kv4_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 4, [&]() -> PyObject* {
+  return guarded(n, 5, [&]() -> PyObject* {
     const gc_kv4_cache_t* c = cache_at(a[0]);
     const at::Tensor &k = tensor(a[1], "k"), &v = tensor(a[2], "v"), &slots = tensor(a[3], "slots");
     const at::Device device = device_of(c);
@@ -186,6 +196,7 @@ PyObject* kv4_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const gc_heads_t kh = heads(k, "k", tokens, c->kv_heads, c->head_dim, k.scalar_type(), device, false);
     const gc_heads_t vh = heads(v, "v", tokens, c->kv_heads, c->head_dim, k.scalar_type(), device, false);
     check(gc_kv4_append(stream_of(c->cuda_device), c, type, tokens, &kh, &vh, s));
+    written(a[4]);
     Py_RETURN_NONE;
   });
 }
@@ -202,6 +213,8 @@ PyObject* kv4_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const gc_heads_t kh = heads(k, "k_out", tokens, c->kv_heads, c->head_dim, k.scalar_type(), device, true);
     const gc_heads_t vh = heads(v, "v_out", tokens, c->kv_heads, c->head_dim, k.scalar_type(), device, true);
     check(gc_kv4_read(stream_of(c->cuda_device), c, type, tokens, &kh, &vh, s));
+    written(k);
+    written(v);
     Py_RETURN_NONE;
   });
 }
@@ -248,6 +261,7 @@ PyObject* kv4_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
     at::Tensor ws;
     if (need) ws = empty({static_cast<int64_t>(need)}, at::kByte, device);
     check(gc_attention_kv4(stream_of(c->cuda_device), c, &d, need ? ws.data_ptr() : nullptr, need));
+    if (given(a[6])) written(out);
     return THPVariable_Wrap(out);
   });
 }
@@ -279,6 +293,7 @@ PyObject* attention_prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
     d.out = heads(out, "out", d.q_tokens, d.q_heads, d.head_dim, at::kBFloat16, device, true);
     if (given(a[8])) d.status = const_cast<uint32_t*>(static_cast<const uint32_t*>(vec(tensor(a[8], "status"), "status", 1, at::kInt, device)));
     check(gc_attention_prompt(stream_of(d.cuda_device), &d));
+    written(out);
     return Py_NewRef(a[7]);
   });
 }

@@ -103,7 +103,7 @@ class KV4Cache:
         if self.device.type != "cuda":
             raise ValueError(f"a cache lives on a CUDA device, not {self.device}")
         self.pages, self.kv_heads, self.page_size, self.head_dim, self.group = pages, heads, page, 2 * half, 2 * half // groups
-        self.k_codes, self.k_params, self.v_codes, self.v_params = k_codes, k_params, v_codes, v_params
+        self.k_codes, self.k_params, self.v_codes, self.v_params = self._tensors = k_codes, k_params, v_codes, v_params
         self.status = new_status(self.device)
         self._desc = B.gc_kv4_cache_t(self.device.index, page, pages, heads, 2 * half, self.group, 0, k_codes.data_ptr(), k_params.data_ptr(),
                                       v_codes.data_ptr(), v_params.data_ptr(), self.status.data_ptr())
@@ -126,7 +126,7 @@ class KV4Cache:
     def append(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
         """Write rows k, v [tokens, kv_heads, head_dim] (fp32 or bf16) at slots (int64 [tokens], page * page_size + offset;
         negative: the row is skipped).  No slot may be named twice in a call."""
-        _serving.kv4_append(self._at, k, v, slots)
+        _serving.kv4_append(self._at, k, v, slots, self._tensors)
 
     def read(self, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16, k_out: Optional[torch.Tensor] = None,
              v_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:

@@ -238,3 +238,31 @@ def test_tensors_that_require_a_gradient_are_refused(S):
     with torch.inference_mode():
         S.qk_norm_rope(x, x, pos, inv, w)
     cache.query_status()
+
+
+def test_outputs_that_were_given_count_as_written(S):
+    # what autograd keeps for a backward pass and a call then overwrites is missed there, as after any write in place
+    x = torch.ones(3, 2, 64, device=DEV, dtype=torch.bfloat16)
+    pos, inv = torch.arange(3, device=DEV), S.rotary_inv_freq(64, device=DEV)
+    cu = torch.tensor([0, 3], dtype=torch.int32, device=DEV)
+    cache = S.KV4Cache.allocate(2, 16, 2, 64, 32)
+    table, lens = torch.zeros(1, 1, dtype=torch.int32, device=DEV), torch.ones(1, dtype=torch.int32, device=DEV)
+    a, b = torch.empty_like(x), torch.empty_like(x)
+    one = torch.empty(1, 1, 2, 64, device=DEV, dtype=torch.bfloat16)
+    for call, outs in ((lambda: S.qk_norm_rope(x, x, pos, inv, q_out=a, k_out=b), (a, b)),
+                       (lambda: cache.append(x, x, pos), (cache.k_codes, cache.k_params, cache.v_codes, cache.v_params)),
+                       (lambda: cache.read(pos, k_out=a, v_out=b), (a, b)), (lambda: cache.attend(x[None, :1], table, lens, out=one), (one,)),
+                       (lambda: S.attention_prompt(x, x, x, cu, out=a), (a,))):
+        before = [t._version for t in outs]
+        inputs = x._version
+        call()
+        assert [t._version for t in outs] == [v + 1 for v in before] and x._version == inputs
+    w = torch.ones_like(a).requires_grad_()
+    y = (w * a).sum()
+    S.attention_prompt(x, x, x, cu, out=a)
+    with pytest.raises(RuntimeError, match="inplace"):
+        y.backward()
+    with torch.inference_mode():                                 # tensors without a count
+        c = torch.empty_like(x)
+        S.attention_prompt(x, x, x, cu, out=c)
+    cache.query_status()
