@@ -118,7 +118,15 @@ int32_t small(int64_t v, const char* name) {
   if (v < INT32_MIN || v > INT32_MAX) refuse("%s is out of range", name);
   return static_cast<int32_t>(v);
 }
-const gc_kv4_cache_t* cache_at(PyObject* o) { return static_cast<const gc_kv4_cache_t*>(PyLong_AsVoidPtr(o)); }
+// The descriptor of a cache, whose pointers must still be those of its tensors (set_, resize_ or an assigned .data move them).
+const gc_kv4_cache_t* cache_at(PyObject* at, PyObject* tensors) {
+  const gc_kv4_cache_t* c = static_cast<const gc_kv4_cache_t*>(PyLong_AsVoidPtr(at));
+  const void* held[4] = {c->k_codes, c->k_params, c->v_codes, c->v_params};
+  for (int i = 0; i < 4; ++i)
+    if (THPVariable_Unpack(PyTuple_GET_ITEM(tensors, i)).data_ptr() != held[i])
+      refuse("a tensor of the cache has moved since the KV4Cache was made: make another one over the tensors as they are now");
+  return c;
+}
 at::Device device_of(const gc_kv4_cache_t* c) { return at::Device(at::kCUDA, static_cast<c10::DeviceIndex>(c->cuda_device)); }
 
 // Runs `f`, turning what it throws into Python exceptions.
@@ -187,7 +195,7 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // (cache, k, v, slots, the cache's four tensors)
 PyObject* kv4_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 5, [&]() -> PyObject* {
-    const gc_kv4_cache_t* c = cache_at(a[0]);
+    const gc_kv4_cache_t* c = cache_at(a[0], a[4]);
     const at::Tensor &k = tensor(a[1], "k"), &v = tensor(a[2], "v"), &slots = tensor(a[3], "slots");
     const at::Device device = device_of(c);
     const int32_t type = row_type(k, "k");
@@ -201,10 +209,10 @@ PyObject* kv4_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (cache, slots, k_out, v_out)
+// (cache, slots, k_out, v_out, the cache's four tensors)
 PyObject* kv4_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 4, [&]() -> PyObject* {
-    const gc_kv4_cache_t* c = cache_at(a[0]);
+  return guarded(n, 5, [&]() -> PyObject* {
+    const gc_kv4_cache_t* c = cache_at(a[0], a[4]);
     const at::Tensor &slots = tensor(a[1], "slots"), &k = tensor(a[2], "k_out"), &v = tensor(a[3], "v_out");
     const at::Device device = device_of(c);
     const int32_t type = row_type(k, "k_out");
@@ -219,10 +227,10 @@ PyObject* kv4_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (cache, q, block_table, lengths, scale, max_length, out)
+// (cache, q, block_table, lengths, scale, max_length, out, the cache's four tensors)
 PyObject* kv4_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 7, [&]() -> PyObject* {
-    const gc_kv4_cache_t* c = cache_at(a[0]);
+  return guarded(n, 8, [&]() -> PyObject* {
+    const gc_kv4_cache_t* c = cache_at(a[0], a[7]);
     const at::Tensor &q = tensor(a[1], "q"), &table = tensor(a[2], "block_table"), &lengths = tensor(a[3], "lengths");
     const at::Device device = device_of(c);
     if (q.dim() != 4 || q.scalar_type() != at::kBFloat16 || q.device() != device || q.size(3) != c->head_dim || q.stride(3) != 1)

@@ -85,7 +85,8 @@ class KV4Cache:
       params  bfloat16 [pages, kv_heads, page_size, head_dim / group, 2]
 
     page_size a power of two from 16 to 256, head_dim 64, 96 or 128, group 32, 64 or 128.  The object keeps the tensors alive
-    and a status word, nothing else: it may be used on any stream, as far as the caller orders the accesses."""
+    and a status word, nothing else: it may be used on any stream, as far as the caller orders the accesses.  It is made for these
+    tensors: they cannot be replaced by others, and a call is refused once the memory of one has been."""
 
     def __init__(self, k_codes: torch.Tensor, k_params: torch.Tensor, v_codes: torch.Tensor, v_params: torch.Tensor):
         if k_codes.dim() != 4 or k_params.dim() != 5:
@@ -108,6 +109,11 @@ class KV4Cache:
         self._desc = B.gc_kv4_cache_t(self.device.index, page, pages, heads, 2 * half, self.group, 0, k_codes.data_ptr(), k_params.data_ptr(),
                                       v_codes.data_ptr(), v_params.data_ptr(), self.status.data_ptr())
         self._at = ctypes.addressof(self._desc)
+
+    def __setattr__(self, name, value):
+        if "_at" in self.__dict__ and name in self.__dict__:
+            raise AttributeError(f"{name} of a KV4Cache is fixed: make another one over other tensors")
+        super().__setattr__(name, value)
 
     @classmethod
     def allocate(cls, pages: int, page_size: int, kv_heads: int, head_dim: int, group: int = 64, device="cuda") -> "KV4Cache":
@@ -137,7 +143,7 @@ class KV4Cache:
             shape = (slots.shape[0], self.kv_heads, self.head_dim)
             made = torch.zeros(shape, dtype=dtype if like is None else like.dtype, device=self.device)
             k_out, v_out = (made, torch.zeros_like(made)) if like is None else (made if k_out is None else k_out, made if v_out is None else v_out)
-        _serving.kv4_read(self._at, slots, k_out, v_out)
+        _serving.kv4_read(self._at, slots, k_out, v_out, self._tensors)
         return k_out, v_out
 
     def attend(self, q: torch.Tensor, block_table: torch.Tensor, lengths: torch.Tensor, *, scale: Optional[float] = None,
@@ -146,7 +152,7 @@ class KV4Cache:
         order) names, lengths (int32 [batch]) counting the tokens appended so far, the queries' own among them: query j sees
         the first lengths - (queries - 1) + j of them.  scale: head_dim ** -0.5 if not given; max_length: a bound of lengths the
         caller knows (the work is laid out for it; a longer sequence is an error), width * page_size if not given."""
-        return _serving.kv4_attend(self._at, q, block_table, lengths, scale, max_length, out)
+        return _serving.kv4_attend(self._at, q, block_table, lengths, scale, max_length, out, self._tensors)
 
     def query_status(self) -> None:
         """Synchronise the current stream; raise GcError if a call found a slot, page or length out of bounds since the last one."""

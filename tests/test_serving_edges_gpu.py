@@ -266,3 +266,24 @@ def test_outputs_that_were_given_count_as_written(S):
         c = torch.empty_like(x)
         S.attention_prompt(x, x, x, cu, out=c)
     cache.query_status()
+
+
+# ------------------------------------------------------------------------------------------------ the cache's memory
+def test_a_cache_is_made_for_its_tensors(S):
+    # the kernels get pointers that were taken once: other tensors, or other memory under the same ones, must not go unnoticed
+    cache = S.KV4Cache.allocate(2, 16, 2, 64, 32)
+    x, slots = torch.ones(3, 2, 64, device=DEV), torch.arange(3, device=DEV)
+    cache.append(x, x, slots)
+    for name in ("k_codes", "k_params", "v_codes", "v_params", "status", "page_size"):
+        with pytest.raises(AttributeError, match="fixed"):
+            setattr(cache, name, getattr(cache, name))
+    cache.note = "other names are free"
+    table, lens = torch.zeros(1, 1, dtype=torch.int32, device=DEV), torch.ones(1, dtype=torch.int32, device=DEV)
+    kept = cache.v_params.data
+    cache.v_params.data = kept.clone()
+    for call in (lambda: cache.append(x, x, slots), lambda: cache.read(slots), lambda: cache.attend(torch.ones(1, 1, 4, 64, device=DEV).bfloat16(), table, lens)):
+        with pytest.raises(ValueError, match="moved"):
+            call()
+    cache.v_params.data = kept
+    assert (cache.read(slots, torch.float32)[1] == 1).all()
+    cache.query_status()
