@@ -5,14 +5,14 @@ They serve: no gradient is recorded, and a tensor that requires one is refused u
 All of them are asynchronous on the current stream of their tensors' device, take strided tensors (the last dimension
 contiguous), can be captured into a CUDA graph (after a first call outside the capture, which loads their kernels), and raise
 ``GcError`` (or ``TypeError`` / ``ValueError`` for tensors of the wrong type, shape or device) before anything is launched.  What only the device can see - a slot, page, length or offset out
-of bounds - leaves the outputs of that call undefined and is recorded in a status word: ``KV4Cache.query_status()``, or
-``query_status(word)`` for the word given to ``attention_prompt``.
+of bounds - leaves the outputs of that call undefined and is recorded in a status word: ``KV4Cache.query_status()`` for a cache's
+calls, ``query_status()`` for those of ``attention_prompt``, or ``query_status(word)`` where it was given a word of its own.
 """
 from __future__ import annotations
 
 import ctypes
 import math
-from typing import Optional, Tuple
+from typing import Dict, Optional, Tuple
 
 import torch
 
@@ -72,8 +72,26 @@ def new_status(device="cuda") -> torch.Tensor:
     return torch.zeros(1, dtype=torch.int32, device=device)
 
 
-def query_status(word: torch.Tensor) -> None:
-    """Synchronise the current stream; raise GcError for what the device recorded in `word`, and clear it."""
+_words: Dict[int, torch.Tensor] = {}            # by device: the word of attention_prompt calls that are given none
+
+
+def _word_of(device: torch.device) -> torch.Tensor:
+    word = _words.get(device.index)
+    if word is None:
+        with torch.cuda.device(device):
+            if torch.cuda.is_current_stream_capturing():
+                raise ValueError("a device's first attention_prompt is made outside of a capture, or is given a status word")
+            word = new_status(device)
+            torch.cuda.current_stream().synchronize()            # the word is zero before a call on any stream
+        word = _words.setdefault(device.index, word)
+    return word
+
+
+def query_status(word: Optional[torch.Tensor] = None) -> None:
+    """Synchronise the current stream; raise GcError for what the device recorded in `word`, and clear it.  Without a word: what
+    ``attention_prompt`` calls on the current device recorded that were given none."""
+    if word is None:
+        word = _word_of(torch.device("cuda", torch.cuda.current_device()))
     with torch.cuda.device(word.device):
         B.gc_serving_status(torch.cuda.current_stream(word.device).cuda_stream, word.data_ptr())
 
@@ -165,7 +183,10 @@ def attention_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: to
     """Attention of packed sequences, bf16: q [q_tokens, q_heads, head_dim], k and v [k_tokens, kv_heads, head_dim]; sequence b owns
     query rows cu_q[b] .. cu_q[b + 1] and key rows cu_k[b] .. cu_k[b + 1] (int32 [batch + 1]; cu_k = cu_q if not given).  causal:
     query row i of nq sees the first i + 1 + nk - nq keys.  A row that sees none is zero; rows no sequence owns are left as they
-    were in a given `out`, and are zero in one made here."""
+    were in a given `out`, and are zero in one made here.  status: a word (``new_status``) for what only the device can see; the
+    device's own, which ``query_status()`` reads, if not given."""
     if out is None:
         out = torch.zeros(q.shape, dtype=torch.bfloat16, device=q.device)
+    if status is None and q.is_cuda:
+        status = _word_of(q.device)
     return _serving.attention_prompt(q, k, v, cu_q, cu_k, causal, scale, out, status)

@@ -287,3 +287,45 @@ def test_a_cache_is_made_for_its_tensors(S):
     cache.v_params.data = kept
     assert (cache.read(slots, torch.float32)[1] == 1).all()
     cache.query_status()
+
+
+# ------------------------------------------------------------------------------------------------ status words
+def test_prompt_without_a_status_word_of_its_own_is_heard_of(S, monkeypatch):
+    q = torch.zeros(300, 2, 64, dtype=torch.bfloat16, device=DEV)
+    bad = torch.tensor([0, 200, 100, 300], dtype=torch.int32, device=DEV)
+    good = torch.tensor([0, 100, 200, 300], dtype=torch.int32, device=DEV)
+    S.query_status()                                             # nothing has gone wrong yet
+    S.attention_prompt(q, q, q, bad)
+    with pytest.raises(S.GcError, match="offsets"):
+        S.query_status()
+    S.query_status()                                             # cleared
+    own = S.new_status(DEV)
+    S.attention_prompt(q, q, q, bad, status=own)
+    S.attention_prompt(q, q, q, good)
+    S.query_status()
+    with pytest.raises(S.GcError, match="offsets"):
+        S.query_status(own)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        S.attention_prompt(q, q, q, bad)
+        with pytest.raises(S.GcError, match="offsets"):
+            S.query_status()
+    offsets, out = good.clone(), torch.empty_like(q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        S.attention_prompt(q, q, q, offsets, out=out)
+    graph.replay()
+    S.query_status()
+    offsets.copy_(bad)
+    graph.replay()
+    with pytest.raises(S.GcError, match="offsets"):
+        S.query_status()
+    monkeypatch.setattr(S, "_words", {})                         # as if no call had been made yet
+    other = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(other):
+        with pytest.raises(ValueError, match="capture"):
+            S.attention_prompt(q, q, q, good, out=out)
+        S.attention_prompt(q, q, q, good, out=out, status=own)
+    other.replay()
+    S.query_status(own)
