@@ -352,8 +352,10 @@ gc_status_t gc_kv4_read(void* cuda_stream, const gc_kv4_cache_t* cache, int32_t 
  * sequence b at [b * table_stride + p], p < table_width; entries beyond a sequence's length are not looked at.
  * max_length: an upper bound of lengths the caller knows (a longer sequence is an error found on the device); the
  * split of the work over the GPU goes by it.  Scores and sums in fp32, probabilities times scale rounded to bf16 (half a
- * bf16 step each, the only rounding before the output's).  queries 1 .. 16, scale finite and > 0.  Values held
- * should lie between 2^-40 and 2^32 in size (the sums carry a factor of 2^64 and bf16's smallest unit).  What a query does not see has no influence on it, whatever is held there. */
+ * bf16 step each, the only rounding before the output's).  queries 1 .. 16, scale finite and > 0.  A group of values whose
+ * middle or scale exceeds 2^32 in size is more than the sums can hold: that is recorded in the status word (keys may have any
+ * size).  A token whose weight times its value's scale lies below 2^-57 may be missing from the sums, so that values below about
+ * 2^-40 in size lose relative accuracy.  What a query does not see has no influence on it, whatever is held there. */
 typedef struct {
   int32_t batch, queries, q_heads;
   int32_t table_width;

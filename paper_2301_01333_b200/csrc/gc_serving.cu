@@ -305,6 +305,7 @@ extern "C" gc_status_t gc_serving_status(void* cuda_stream, uint32_t* status_dev
     case DEV_BAD_PAGE: return gc_set_error(GC_ERR_INVALID_ARG, "a page number in the block table lies outside the cache");
     case DEV_BAD_LENGTH: return gc_set_error(GC_ERR_INVALID_ARG, "a sequence is longer than max_length, or its length is negative");
     case DEV_BAD_OFFSETS: return gc_set_error(GC_ERR_INVALID_ARG, "sequence offsets decrease or leave the packed tokens");
+    case DEV_LARGE_VALUE: return gc_set_error(GC_ERR_INVALID_ARG, "a value in the cache exceeds 2^32 in size, more than attention over it can sum");
     default: break;
   }
   REFUSE(GC_ERR_TIMEOUT, "a device-side wait expired (code 0x%x)", word);

@@ -53,6 +53,7 @@ constexpr int AK_TILE = 32;                  // tokens per tile of a warp
 constexpr int AK_STAGES = 3;
 constexpr int AK_START = 2;
 constexpr float AK_RAISE = 8.0f;             // binades a score may exceed the reference by
+constexpr float AK_LARGEST = 0x1p32f;        // middle or scale of a group of values, above which sums could leave fp32
 
 template <int D, int G>
 struct KvLayout {
@@ -117,6 +118,11 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float ak_max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t r;
@@ -338,6 +344,7 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
   }
 
   float o[NT][MT][4], mneg[NT][2], thr[NT][2], l[NT][2], z[NT][NG][2], ws[NT][NG][4];
+  float largest = 0.f;                                           // middle or scale of the values seen (NaN apart)
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -518,6 +525,14 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
         const uint32_t pa = lds32<po>(kp), pb = lds32<po + 8 * NG * 4>(kp);
         const float sa = bf_hi(pa), sb = bf_hi(pb);
         const float ma = fmaf(7.5f, sa, bf_lo(pa)), mb = fmaf(7.5f, sb, bf_lo(pb));     // the middle of a group's range
+        if constexpr (EDGE) {
+          const int ta = t0 + mt * 16 + pr;
+          if (ta < t_end) largest = ak_max3(largest, sa, fabsf(ma));
+          if (ta + 8 < t_end) largest = ak_max3(largest, sb, fabsf(mb));
+        } else {
+          largest = ak_max3(largest, sa, sb);
+          largest = ak_max3(largest, fabsf(ma), fabsf(mb));
+        }
         uint32_t bf[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -577,6 +592,7 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
     if (st_out == ring_a + L::RING) st_out = ring_a;
   }
   cp_wait<0>();
+  if (largest > AK_LARGEST) report(p.status, DEV_LARGE_VALUE);
 
   // ---- join the warps: (m, l) and the outputs of every column through shared memory
 #pragma unroll

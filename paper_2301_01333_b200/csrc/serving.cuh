@@ -12,6 +12,7 @@ enum : uint32_t {
   DEV_BAD_PAGE = 0x202,
   DEV_BAD_LENGTH = 0x203,
   DEV_BAD_OFFSETS = 0x204,
+  DEV_LARGE_VALUE = 0x205,
 };
 
 // Launches of this block follow one another closely: each may be set up while the kernel before it on the stream still runs

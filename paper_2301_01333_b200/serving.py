@@ -169,7 +169,8 @@ class KV4Cache:
         """Attention of q bf16 [batch, queries, q_heads, head_dim] over the sequences block_table (int32 [batch, width], pages in
         order) names, lengths (int32 [batch]) counting the tokens appended so far, the queries' own among them: query j sees
         the first lengths - (queries - 1) + j of them.  scale: head_dim ** -0.5 if not given; max_length: a bound of lengths the
-        caller knows (the work is laid out for it; a longer sequence is an error), width * page_size if not given."""
+        caller knows (the work is laid out for it; a longer sequence is an error), width * page_size if not given.  A value above 2^32
+        in size, which the sums could not hold, is reported by ``query_status()``; below 2^-40 they lose accuracy."""
         return _serving.kv4_attend(self._at, q, block_table, lengths, scale, max_length, out, self._tensors)
 
     def query_status(self) -> None:

@@ -329,3 +329,53 @@ def test_prompt_without_a_status_word_of_its_own_is_heard_of(S, monkeypatch):
         S.attention_prompt(q, q, q, good, out=out, status=own)
     other.replay()
     S.query_status(own)
+
+
+# ------------------------------------------------------------------------------------------------ sizes of values
+def sized_cache(S, m, n, size_k=1.0, size_v=1.0, seed=0):
+    g = gen(seed)
+    cache = filled_cache(S, 2 + m // 64, 64, 2, 128, 32, g)
+    cache.k_params.mul_(size_k)
+    cache.v_params.mul_(size_v)
+    table = table_of([m], 64, 2 + m // 64, g)
+    q = randn(1, n, 4, 128, g=g, dtype=torch.bfloat16, scale=1.0 / size_k)
+    return cache, table, q, torch.tensor([m], dtype=torch.int32, device=DEV)
+
+
+@pytest.mark.parametrize("m", [20, 400, 3000])
+@pytest.mark.parametrize("n", [1, 5])
+def test_attend_reports_values_it_cannot_sum(S, m, n):
+    cache, table, q, ln = sized_cache(S, m, n)
+    want = cache.attend(q, table, ln)
+    cache.query_status()
+    held = cache.v_params.clone()
+    at = m // 2
+    for big in ((2.0 ** 34, 0.5), (-(2.0 ** 34), 0.5), (-1.0, 2.0 ** 33), (3e38, 0.0)):
+        cache.v_params[table[0, at // 64], 1, at % 64, 2] = torch.tensor(big, device=DEV).bfloat16()
+        cache.attend(q, table, ln)
+        with pytest.raises(S.GcError, match="exceeds"):
+            cache.query_status()
+        cache.v_params.copy_(held)
+    for t in range(m, table.shape[1] * 64):                      # behind the sequence, and in keys, any size is fine
+        cache.v_params[table[0, t // 64], :, t % 64] = 2.0 ** 60
+    cache.k_params[table[0, at // 64], 0, at % 64] = 2.0 ** -60
+    cache.attend(q, table, ln)
+    cache.query_status()
+    cache.v_params[table[0, at // 64], 1, at % 64, 2] = math.nan  # a group that could not be held is no matter of size
+    out = cache.attend(q, table, ln)
+    cache.query_status()
+    assert torch.isnan(out[0, -1, 2:, 64:96]).all() and torch.isfinite(out[:, :, 2:, :64]).all() and want.shape == out.shape
+
+
+@pytest.mark.parametrize("power_k,power_v", [(0, 29), (60, 0), (-60, 0), (0, -39)])
+def test_attend_sizes_of_keys_and_values(S, power_k, power_v):
+    m = 700
+    cache, table, q, ln = sized_cache(S, m, 3, 2.0 ** power_k, 2.0 ** power_v)
+    out = cache.attend(q, table, ln)
+    cache.query_status()
+    cache.v_params.mul_(2.0 ** -power_v)                         # exactly the values of ordinary size
+    cache.k_params.mul_(2.0 ** -power_k)
+    q = (q.double() * 2.0 ** power_k).bfloat16()
+    ref, tol = attend_reference(cache, q, table, [m], 128 ** -0.5, 32)
+    # a weight times a scale below 2^-57 may be missing: at most 15 of them for each token
+    within(out.double() * 2.0 ** -power_v, ref, tol + 15 * m * 2.0 ** (-57 - power_v))
