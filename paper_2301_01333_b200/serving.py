@@ -92,6 +92,10 @@ def query_status(word: Optional[torch.Tensor] = None) -> None:
     ``attention_prompt`` calls on the current device recorded that were given none."""
     if word is None:
         word = _word_of(torch.device("cuda", torch.cuda.current_device()))
+    if not isinstance(word, torch.Tensor):
+        raise TypeError("a status word is a torch.Tensor, as new_status makes it")
+    if word.dtype != torch.int32 or word.numel() != 1 or not word.is_cuda:
+        raise ValueError(f"a status word is one int32 on a CUDA device, as new_status makes it, not {word.dtype} {tuple(word.shape)} on {word.device}")
     with torch.cuda.device(word.device):
         B.gc_serving_status(torch.cuda.current_stream(word.device).cuda_stream, word.data_ptr())
 
@@ -107,6 +111,9 @@ class KV4Cache:
     tensors: they cannot be replaced by others, and a call is refused once the memory of one has been."""
 
     def __init__(self, k_codes: torch.Tensor, k_params: torch.Tensor, v_codes: torch.Tensor, v_params: torch.Tensor):
+        for name, t in (("k_codes", k_codes), ("k_params", k_params), ("v_codes", v_codes), ("v_params", v_params)):
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{name} must be a torch.Tensor")
         if k_codes.dim() != 4 or k_params.dim() != 5:
             raise ValueError("codes must be [pages, heads, page_size, head_dim / 2], params [pages, heads, page_size, groups, 2]")
         pages, heads, page, half = k_codes.shape
@@ -156,6 +163,10 @@ class KV4Cache:
              v_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """The values held at slots, [tokens, kv_heads, head_dim], of type dtype or that of the outputs given; rows of negative
         slots are left as they were (zeros in outputs made here)."""
+        if not isinstance(slots, torch.Tensor):
+            raise TypeError("slots must be a torch.Tensor")
+        if slots.dim() != 1:
+            raise ValueError(f"slots must be a vector, not {tuple(slots.shape)}")
         if k_out is None or v_out is None:
             like = k_out if k_out is not None else v_out
             shape = (slots.shape[0], self.kv_heads, self.head_dim)
@@ -186,6 +197,8 @@ def attention_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: to
     query row i of nq sees the first i + 1 + nk - nq keys.  A row that sees none is zero; rows no sequence owns are left as they
     were in a given `out`, and are zero in one made here.  status: a word (``new_status``) for what only the device can see; the
     device's own, which ``query_status()`` reads, if not given."""
+    if not isinstance(q, torch.Tensor):
+        raise TypeError("q must be a torch.Tensor")
     if out is None:
         out = torch.zeros(q.shape, dtype=torch.bfloat16, device=q.device)
     if status is None and q.is_cuda:

@@ -379,3 +379,12 @@ def test_attend_sizes_of_keys_and_values(S, power_k, power_v):
     ref, tol = attend_reference(cache, q, table, [m], 128 ** -0.5, 32)
     # a weight times a scale below 2^-57 may be missing: at most 15 of them for each token
     within(out.double() * 2.0 ** -power_v, ref, tol + 15 * m * 2.0 ** (-57 - power_v))
+
+
+def test_slots_that_are_no_vector_are_refused(S):
+    cache = S.KV4Cache.allocate(2, 16, 2, 64, 32)
+    for bad, kind in ((None, TypeError), ([0, 1], TypeError), (torch.zeros((), dtype=torch.int64, device=DEV), ValueError),
+                      (torch.zeros(2, 2, dtype=torch.int64, device=DEV), ValueError), (torch.zeros(2, dtype=torch.int32, device=DEV), ValueError)):
+        with pytest.raises(kind, match="slots"):
+            cache.read(bad)
+    cache.query_status()

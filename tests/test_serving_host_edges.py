@@ -16,3 +16,15 @@ def test_tensors_that_require_a_gradient_are_refused(S):
             call()
         with torch.no_grad(), pytest.raises(ValueError, match="CUDA"):      # and not where gradients are off
             call()
+
+
+def test_arguments_that_are_no_tensors_are_refused_as_such(S):
+    p, cu = torch.zeros(2, 2, 64).bfloat16(), torch.tensor([0, 2], dtype=torch.int32)
+    codes, params = torch.zeros(2, 1, 16, 32, dtype=torch.uint8), torch.zeros(2, 1, 16, 2, 2, dtype=torch.bfloat16)
+    for call in (lambda: S.attention_prompt(None, p, p, cu), lambda: S.attention_prompt(p, 3, p, cu), lambda: S.attention_prompt(p, p, p, [0, 2]),
+                 lambda: S.KV4Cache(None, params, codes, params), lambda: S.KV4Cache(codes, params, codes, 1), lambda: S.query_status(0)):
+        with pytest.raises(TypeError, match="torch.Tensor"):
+            call()
+    for word in (torch.zeros(1, dtype=torch.int32), torch.zeros(1), torch.zeros(2, dtype=torch.int32)):
+        with pytest.raises(ValueError, match="status word"):
+            S.query_status(word)
