@@ -34,6 +34,8 @@
 //   * Rows of another sequence may follow a sequence's own in a tile.  Foreign keys are masked by selection; foreign value
 //     rows are overwritten with zeros in shared memory (0 times a stored infinity would be NaN); foreign query rows are not
 //     stored.
+#include <atomic>
+
 #include "ptx.cuh"
 #include "serving.cuh"
 
@@ -43,6 +45,10 @@ namespace {
 constexpr int AP_THREADS = 384;               // three warpgroups; the last warp only hands its registers over
 constexpr int AP_MAX_LIST = 1024;                // work list entries kept (and sorted) in shared memory
 constexpr float AP_RAISE = 8.0f;
+// Registers a thread: what the kernel has to be compiled to, and what the softmax warpgroups take and the other one gives.  Taking
+// more than the block was launched with would wait for good, so a kernel compiled to fewer is not launched.
+constexpr int AP_REGS = 168, AP_REGS_SOFTMAX = 208, AP_REGS_OTHER = 88;
+static_assert(2 * AP_REGS_SOFTMAX + AP_REGS_OTHER <= 3 * AP_REGS, "the warpgroups' shares exceed the launch's registers");
 
 template <int D>
 struct PromptLayout {
@@ -328,10 +334,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     return it;
   };
 
-  // Registers: 168 a thread at launch, 504 in each lane's three warps of a scheduler; 2 x 208 + 88 = 504.
   bool failed = false;
   if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(AP_REGS_SOFTMAX));
     // ------------------------------------------------------------------ softmax and output
     const int t = warp >> 2, row = tid & 127;
     const uint32_t t_lane = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
@@ -457,7 +462,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     }
     if (failed && lane == 0) report(p.status, DEV_TIMEOUT_EPILOGUE);
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(AP_REGS_OTHER));
     if (warp == 8) {
       // ------------------------------------------------------------------ TMA producer
       uint32_t ring = 0, qn[2] = {0, 0};
@@ -596,6 +601,14 @@ template <int D>
 static cudaError_t prompt_run(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const PromptParams& p, int num_sms,
                               cudaStream_t s) {
   auto kern = attn_prompt_kernel<D>;
+  static std::atomic<int> regs{0};
+  if (regs.load(std::memory_order_relaxed) == 0) {
+    cudaFuncAttributes a;
+    const cudaError_t e = cudaFuncGetAttributes(&a, kern);
+    if (e != cudaSuccess) return e;
+    regs.store(a.numRegs, std::memory_order_relaxed);
+  }
+  if (regs.load(std::memory_order_relaxed) < AP_REGS) return cudaErrorLaunchOutOfResources;
   cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), PromptLayout<D>::SMEM);
   if (e != cudaSuccess) return e;
   // 256 rows to an item, or 128 where even those leave SMs without work: the one tile then has the tensor core to itself (one

@@ -45,3 +45,11 @@ def test_nothing_is_read_before_the_kernel_has_waited(name):
         ahead = k[k.index("{"):wait.start()]
         found = re.search(r"length_of|blocks_of|all_blocks|sequence_at|seq_of|\bp\.(\w+)\[|p\.ws|->|ld\.global|cp\.async", ahead)
         assert not found, f"{name}: '{found.group(0)}' ahead of the wait"
+
+
+@pytest.mark.parametrize("name", [n for n in SOURCES if "setmaxnreg.inc" in code_of(n)])
+def test_registers_are_only_taken_where_the_launch_has_them(name):
+    """setmaxnreg.inc beyond the registers a block was launched with waits for good, and how many those are is the compiler's
+    decision: the host has to ask before it launches, and the shares have to add up."""
+    code = code_of(name)
+    assert re.search(r"numRegs", code) and re.search(r"static_assert\([^;]*REGS", code), f"{name} trusts the compiler's register count"
