@@ -6,7 +6,8 @@ import pytest
 import torch
 
 import serving_reference as R
-from test_serving_gpu import DEV, S, attend_reference, filled_cache, gen, randn, table_of, within  # noqa: F401 (S: the fixture)
+from test_serving_gpu import (DEV, S, attend_reference, filled_cache, gen, prompt_case, randn, rope_case, table_of,  # noqa: F401 (S: the fixture)
+                              within)
 
 pytestmark = pytest.mark.gpu
 
@@ -388,3 +389,21 @@ def test_slots_that_are_no_vector_are_refused(S):
         with pytest.raises(kind, match="slots"):
             cache.read(bad)
     cache.query_status()
+
+
+# ------------------------------------------------------------------------------------------------ launch shapes
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("t", [593, 700, 1183, 1187])
+@pytest.mark.parametrize("d,rot,pad", [(128, 128, 0), (128, 64, 0), (96, 96, 0), (80, 48, 0), (64, 64, 1), (50, 22, 0)])
+def test_rope_several_tokens_to_a_block(S, dtype, interleaved, t, d, rot, pad):
+    # two and four tokens to a block, the last block not full: lanes without elements, partly rotated heads, rows that are not aligned
+    rope_case(S, t, 3, 2, d, rot, dtype, interleaved, seed=t + d, pad=pad)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads", [16, 17])
+@pytest.mark.parametrize("n", [[1024], [1025], [130, 1, 700, 60]])
+def test_prompt_items_of_128_and_of_256_rows(S, causal, heads, n):
+    # (tokens / 128 + sequences) x heads is 144 and 153 for 1024 tokens, either side of 148 SMs, where items become twice as long
+    prompt_case(S, n, n, heads, 1 if heads == 16 else 17, 64, causal, seed=heads + len(n), tail=3, poison=True)
