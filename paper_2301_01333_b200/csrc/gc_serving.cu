@@ -230,7 +230,7 @@ extern "C" gc_status_t gc_attention_kv4(void* cuda_stream, const gc_kv4_cache_t*
   Kv4AttnParams p = {};
   p.B = d->batch; p.n = d->queries; p.Hq = d->q_heads; p.Hk = cache->kv_heads; p.g = d->q_heads / cache->kv_heads;
   while ((1 << p.page_shift) < cache->page_size) ++p.page_shift;
-  p.width = d->table_width; p.max_len = d->max_length;
+  p.max_len = d->max_length;
   p.num_pages = cache->num_pages; p.table_stride = d->table_stride;
   p.c = d->scale * 1.4426950408889634f;
   p.block = sp.block; p.ctas = sp.ctas; p.col_chunks = sp.col_chunks; p.solo = sp.solo;
@@ -243,7 +243,7 @@ extern "C" gc_status_t gc_attention_kv4(void* cuda_stream, const gc_kv4_cache_t*
   p.v_codes = static_cast<const uint8_t*>(cache->v_codes); p.v_params = static_cast<const uint32_t*>(cache->v_params);
   p.ws = static_cast<float*>(workspace_dev);
   p.status = cache->status;
-  RUN(launch_attn_kv4(p, cache->head_dim, cache->group, sms, static_cast<cudaStream_t>(cuda_stream)));
+  RUN(launch_attn_kv4(p, cache->head_dim, cache->group, static_cast<cudaStream_t>(cuda_stream)));
   return GC_OK;
 }
 

@@ -33,10 +33,12 @@
 //   * Many short sequences: a warp per (sequence, head, chunk of columns), which writes its rows itself (gc_serving.cu says when).
 //   * The running maximum is a reference that is only raised when a score exceeds it by 2^8: one vote per tile instead
 //     of a reduction, and the sums stay far inside fp32.
-// Measured: 64 ragged sequences up to 8192 tokens, 8 heads of 128, groups of 64 (323 MB): 77 us = 4.2 TB/s; without any arithmetic
-// the same copies take 62, so the rest is instructions that the copies of 12 warps do not cover (about 610 a tile and eight columns,
+//   * The size of the values is watched on the way (one running maximum): sums of values above 2^32 could leave fp32, which is
+//     recorded in the status word.  It costs 1 us of 77 on the ragged batch below.
+// Measured: 64 ragged sequences up to 8192 tokens, 8 heads of 128, groups of 64 (323 MB): 77.5 us = 4.2 TB/s; without any arithmetic
+// the same copies take 62, so the rest is instructions that the copies of 12 warps do not cover (about 620 a tile and eight columns,
 // half of them on the integer / logic pipe).  One sequence of 131071 tokens, 32 columns (142 MB, read twice, the second time from
-// the L2): 87 us, bound by instructions; its products alone, 8 clocks each on a scheduler, are 33.
+// the L2): 85 us, bound by instructions; its products alone, 8 clocks each on a scheduler, are 33.
 #include <cuda_fp16.h>
 
 #include <type_traits>
@@ -136,17 +138,18 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// Byte offset of 16-byte chunk c of token row r in a codes tile.  The exclusive-or spreads the rows that one load
-// instruction touches over all banks: eight rows with the same chunk (keys, 4 bytes a lane), rows 0, 4, 1, 5 and 2, 6, 3, 7 with
-// two neighbouring chunks (keys, 8 bytes a lane), rows 0..3, 4..7, ... with two neighbouring chunks (values).
-// CTAs per SM the registers are cut for: 168 for one group of columns, 255 for two.  (More CTAs with fewer registers were slower:
-// at 128 the products of a tile can no longer be kept apart, 87 against 78 us for 64 ragged sequences.)
+// CTAs per SM the registers are cut for: 168 for one group of columns, 255 for two (168 at width 64).  Not everything fits: two
+// groups with scales for every 32 elements spill up to 144 bytes a thread.  (More CTAs with fewer
+// registers were slower: at 128 the products of a tile can no longer be kept apart, 87 against 78 us for 64 ragged sequences.)
 constexpr int ak_blocks(int D, int G, int NT) { return NT == 1 ? 3 : D == 64 ? 3 : 2; }
 // First of the eight elements of a row that word w of lane tg holds, KP words at a time per lane.
 template <int KP>
 __device__ __forceinline__ int key_elem(int w, int tg) {
   return (w / KP) * (32 * KP) + tg * (8 * KP) + (w % KP) * 8;
 }
+// Byte offset of 16-byte chunk c of token row r in a codes tile.  The exclusive-or spreads the rows that one load
+// instruction touches over all banks: eight rows with the same chunk (keys, 4 bytes a lane), rows 0, 4, 1, 5 and 2, 6, 3, 7 with
+// two neighbouring chunks (keys, 8 bytes a lane), rows 0..3, 4..7, ... with two neighbouring chunks (values).
 template <int D>
 __device__ __forceinline__ uint32_t code_off(int r, int c) {
   if constexpr (D == 64) return r * 32 + ((c ^ ((r >> 2) & 1)) << 4);
@@ -278,7 +281,7 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
 #pragma unroll
   for (int i = 0; i < AK_STAGES - 1; ++i) issue(i);              // under way while the queries are prepared
 
-  // Queries as the second operand of the first product: lane (gr, tg) holds of column gr, of every KS elements, the
+  // Queries as the second operand of the first product: lane (gr, tg) holds of column gr, of every 32 KP elements, the
   // eight (or sixteen, where a group spans 64) that its lane of the first operand holds: element 8 x + y of the lane's run
   // in the order (0,4), (1,5), (2,6), (3,7) in which the nibbles of a word come apart.
   uint32_t qf[NT][KW][4];
@@ -773,8 +776,9 @@ __global__ void __launch_bounds__(AK_THREADS, ak_blocks(D, G, NT)) attn_kv4_kern
 // Joins the pieces of a split sequence for one column, in a fixed order.  JW = 1: a warp per column, four to a CTA.  JW = 8:
 // a CTA per column, each warp every eighth piece, then the warps; for sequences in many pieces, which one warp would read one
 // memory latency after the other (one sequence of 8000 tokens in 55: 27 us against 17; but 64 of them in two or three: 125
-// against 136, for so many CTAs have to be started).  Which CTAs left the pieces is looked up in what they noted, so that nothing is read
-// before the wait.
+// against 136, for so many CTAs have to be started).  The choice goes by the average: one long sequence among many short ones is
+// joined by one warp a column.  Which CTAs left the pieces is looked up in what they noted, so that nothing is read before the wait
+// (one sequence of 8000 tokens 14.2 us; with the lengths read ahead of the wait, which nothing allows, 13.5).
 template <int D, int JW>
 __global__ void __launch_bounds__(JW == 1 ? 128 : JW * 32) attn_kv4_join_kernel(const __grid_constant__ Kv4AttnParams p, const int cols, const int ctas) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -885,7 +889,7 @@ cudaError_t ak_cols(const Kv4AttnParams& p, cudaStream_t s) {
 
 int attn_kv4_resident(int head_dim, int group, int cols) { return ak_blocks(head_dim, group, cols / 8); }
 
-cudaError_t launch_attn_kv4(const Kv4AttnParams& p, int D, int G, int num_sms, cudaStream_t s) {
+cudaError_t launch_attn_kv4(const Kv4AttnParams& p, int D, int G, cudaStream_t s) {
   if (D == 64) return G == 32 ? ak_cols<64, 32>(p, s) : ak_cols<64, 64>(p, s);
   if (D == 96) return ak_cols<96, 32>(p, s);
   return G == 32 ? ak_cols<128, 32>(p, s) : G == 64 ? ak_cols<128, 64>(p, s) : ak_cols<128, 128>(p, s);

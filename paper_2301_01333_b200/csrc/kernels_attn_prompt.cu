@@ -22,7 +22,8 @@
 // two threads per row 1064 (its instructions were the bottleneck: products alone took 940); an issuing thread per tile with lean
 // descriptors, taking turns (both tiles' products at once complete both scores together, and the tensor core idles while
 // both softmaxes run: 1242) 957; probabilities in two parts 917; one thread per row, without the votes and sums two threads
-// share, 865 = 1270 TFLOP/s, the tensor pipe busy 71 % of the time (products alone: 714).  What is left is the way round: scores
+// share, 865 = 1270 TFLOP/s, the tensor pipe busy 71 % of the time (products alone: 714).  All these are replays with pauses in between;
+// back to back, under the power cap, it is 1000 us = 1100 TFLOP/s.  What is left is the way round: scores
 // complete, softmax, probabilities handed over, with only two tiles to alternate between.  No gain: CTA pairs (M = 256, half
 // of K and V in each CTA); part of the exponentials on the FMA pipe (865 without any exponentials as well); probabilities in four
 // parts (945); two score buffers of 64 keys per tile, which takes the hand-over out of the way but makes S slower (N = 64: 1001).
@@ -30,7 +31,12 @@
 //     output is almost never touched, and raising it is the softmax warps' own business - no extra role, no extra hand-over.
 //   * Persistent CTAs; the work list (256 query rows of a sequence, or 128 where there is little work, times heads) is made by
 //     each CTA from the sequence offsets and sorted by its number of key blocks, longest first, dealt out back and forth.  The
-//     first scores of the next item are issued before the last output of the current one has been stored.
+//     first scores of the next item are issued before the last output of the current one has been stored.  Beyond 1024 entries there is
+//     no list: items go by the sequences' order, and each warp finds its next one from where the last was (64 tokens, 16 / 4
+//     heads of 64: 500 prompts 206 us with the list, 1000 without it 560, 4000 2000).  The sorting compares all pairs: 11 us of a
+//     call with 500 entries, 45 with 1000 (prompts of one token, 38 and 82 us in all; 148 of them, which need no order, 10).
+//   * Sequences of up to 128 rows leave the second tile of their items empty, so that softmax and products take turns with
+//     nothing beside them: 300 prompts of 100 tokens, 32 / 8 heads of 128, 317 us where the memory alone would be 95.
 //   * Rows of another sequence may follow a sequence's own in a tile.  Foreign keys are masked by selection; foreign value
 //     rows are overwritten with zeros in shared memory (0 times a stored infinity would be NaN); foreign query rows are not
 //     stored.
@@ -46,7 +52,8 @@ constexpr int AP_THREADS = 384;               // three warpgroups; the last warp
 constexpr int AP_MAX_LIST = 1024;                // work list entries kept (and sorted) in shared memory
 constexpr float AP_RAISE = 8.0f;
 // Registers a thread: what the kernel has to be compiled to, and what the softmax warpgroups take and the other one gives.  Taking
-// more than the block was launched with would wait for good, so a kernel compiled to fewer is not launched.
+// more than the block was launched with would wait for good, so a kernel compiled to fewer is not launched.  (30 bytes a thread are
+// spilled all the same.)
 constexpr int AP_REGS = 168, AP_REGS_SOFTMAX = 208, AP_REGS_OTHER = 88;
 static_assert(2 * AP_REGS_SOFTMAX + AP_REGS_OTHER <= 3 * AP_REGS, "the warpgroups' shares exceed the launch's registers");
 

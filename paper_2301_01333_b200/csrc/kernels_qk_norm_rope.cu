@@ -422,11 +422,11 @@ cudaError_t launch_qk_norm_rope(const gc_qk_norm_rope_t& d, int num_sms, cudaStr
   using bf16 = __nv_bfloat16;
   if (pairs) {
     // With many tokens four to a CTA, so that a thread's angles and weights serve several rows, and as many CTAs as fit at
-    // once (three per SM), which walk over the groups; two to a CTA where four would leave SMs without work.
+    // once (three per SM), which walk over the groups; two to a CTA where four would leave SMs without work.  (A CTA has at least
+    // eight rows at a time, so a token at least two.)
     dim3 pg = grid;
     if (d.tokens >= 4LL * num_sms) {
       p.tb = d.tokens >= 8LL * num_sms ? 4 : 2;
-      if (p.tb > slots) p.tb = slots;
       const int64_t groups = (d.tokens + p.tb - 1) / p.tb;
       pg.x = static_cast<unsigned>(groups < 3LL * num_sms ? groups : 3LL * num_sms);
     }

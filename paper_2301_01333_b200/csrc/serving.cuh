@@ -40,7 +40,7 @@ cudaError_t launch_following(void (*kern)(P...), dim3 grid, int threads, size_t 
 
 struct Kv4AttnParams {
   int B, n, Hq, Hk, g;              // g: query heads per key/value head; columns of a unit = n * g
-  int page_shift, width, max_len;
+  int page_shift, max_len;
   int64_t num_pages, table_stride;
   float c;                          // scale * log2(e)
   int block, ctas;                  // tokens per block (a multiple of 128) of the row of blocks that `ctas` CTAs share out
@@ -63,7 +63,7 @@ struct Kv4AttnParams {
 int attn_kv4_cols(int columns);
 // Resident CTAs per SM the split of the work is planned for.
 int attn_kv4_resident(int head_dim, int group, int cols);
-cudaError_t launch_attn_kv4(const Kv4AttnParams& p, int head_dim, int group, int num_sms, cudaStream_t s);
+cudaError_t launch_attn_kv4(const Kv4AttnParams& p, int head_dim, int group, cudaStream_t s);
 
 struct PromptParams {
   int B, Hq, Hk, D, causal;
