@@ -354,7 +354,7 @@ gc_status_t gc_kv4_read(void* cuda_stream, const gc_kv4_cache_t* cache, int32_t 
  * split of the work over the GPU goes by it.  Scores and sums in fp32, probabilities times scale rounded to bf16 (half a
  * bf16 step each, the only rounding before the output's).  queries 1 .. 16, scale finite and > 0.  A group of values whose
  * middle or scale exceeds 2^32 in size is more than the sums can hold: that is recorded in the status word (keys may have any
- * size).  A token whose weight times its value's scale lies below 2^-57 may be missing from the sums, so that values below about
+ * size), and so is a finite score (scale times the product) that exceeds 2^26.  A token whose weight times its value's scale lies below 2^-57 may be missing from the sums, so that values below about
  * 2^-40 in size lose relative accuracy.  What a query does not see has no influence on it, whatever is held there. */
 typedef struct {
   int32_t batch, queries, q_heads;
@@ -379,7 +379,7 @@ gc_status_t gc_attention_kv4(void* cuda_stream, const gc_kv4_cache_t* cache, con
  * [cu_q[b], cu_q[b + 1]) and key rows [cu_k[b], cu_k[b + 1]).  causal = 1: query row i of nq sees keys j <= i + nk - nq
  * (aligned to the end, so a prompt may continue earlier keys).  A row that sees nothing is zero; rows of out that no
  * sequence owns are left as they were.  bf16, head_dim 64, 96 or 128, fp32 statistics and sums, probabilities rounded to
- * bf16 for the second product.  Rows 16-byte aligned (pointers, and strides multiples of 8 elements).  Sequences do not touch
+ * bf16 for the second product.  A finite score that exceeds 2^26 in size is recorded in the status word.  Rows 16-byte aligned (pointers, and strides multiples of 8 elements).  Sequences do not touch
  * one another, and a key that a row does not see has no influence on it; a non-finite value (V) may also reach rows of its
  * own sequence that do not see it (a weight of zero times infinity). */
 typedef struct {

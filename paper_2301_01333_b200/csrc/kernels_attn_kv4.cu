@@ -33,12 +33,12 @@
 //   * Many short sequences: a warp per (sequence, head, chunk of columns), which writes its rows itself (gc_serving.cu says when).
 //   * The running maximum is a reference that is only raised when a score exceeds it by 2^8: one vote per tile instead
 //     of a reduction, and the sums stay far inside fp32.
-//   * The size of the values is watched on the way (one running maximum): sums of values above 2^32 could leave fp32, which is
-//     recorded in the status word.  It costs 1 us of 77 on the ragged batch below.
-// Measured: 64 ragged sequences up to 8192 tokens, 8 heads of 128, groups of 64 (323 MB): 77.5 us = 4.2 TB/s; without any arithmetic
+//   * The sizes of the values (one running maximum) and of the reference, when it is raised, are watched: sums of values above 2^32
+//     and weights of scores above 2^26 could leave fp32, which is recorded in the status word.  1.5 us of 76 on the batch below.
+// Measured: 64 ragged sequences up to 8192 tokens, 8 heads of 128, groups of 64 (323 MB): 78 us = 4.1 TB/s; without any arithmetic
 // the same copies take 62, so the rest is instructions that the copies of 12 warps do not cover (about 620 a tile and eight columns,
 // half of them on the integer / logic pipe).  One sequence of 131071 tokens, 32 columns (142 MB, read twice, the second time from
-// the L2): 85 us, bound by instructions; its products alone, 8 clocks each on a scheduler, are 33.
+// the L2): 86 us, bound by instructions; its products alone, 8 clocks each on a scheduler, are 33.
 #include <cuda_fp16.h>
 
 #include <type_traits>
@@ -476,6 +476,7 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
         over |= fmaxf(fmaxf(s[0][nt][e], s[0][nt][e + 2]), fmaxf(s[1][nt][e], s[1][nt][e + 2])) > thr[nt][e];
     }
     if (__any_sync(0xffffffffu, over)) {
+      bool too_large = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -486,6 +487,7 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
           const float mo = 64.f - mneg[nt][e], mn = fmaxf(mo, mx * ce[nt][e]);
           const float f = mo == mn ? 1.f : ak_ex2(mo - mn);      // 0 from the initial minus infinity
           if (mo != mn) {
+            too_large |= score_too_large(mn);
             mneg[nt][e] = 64.f - mn;
             thr[nt][e] = mx + AK_RAISE / ce[nt][e];
           }
@@ -503,6 +505,7 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
           }
         }
       }
+      if (too_large) report(p.status, DEV_LARGE_SCORE);
     }
     // ---- probabilities and the second product, 16 tokens at a time
     each<2>([&](auto mt_c) {

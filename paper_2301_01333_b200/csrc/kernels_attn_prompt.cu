@@ -33,7 +33,7 @@
 //     each CTA from the sequence offsets and sorted by its number of key blocks, longest first, dealt out back and forth.  The
 //     first scores of the next item are issued before the last output of the current one has been stored.  Beyond 1024 entries there is
 //     no list: items go by the sequences' order, and each warp finds its next one from where the last was (64 tokens, 16 / 4
-//     heads of 64: 500 prompts 206 us with the list, 1000 without it 560, 4000 2000).  The sorting compares all pairs: 11 us of a
+//     heads of 64: 500 prompts 209 us with the list, 1000 without it 560, 4000 2000).  The sorting compares all pairs: 11 us of a
 //     call with 500 entries, 45 with 1000 (prompts of one token, 38 and 82 us in all; 148 of them, which need no order, 10).
 //   * Sequences of up to 128 rows leave the second tile of their items empty, so that softmax and products take turns with
 //     nothing beside them: 300 prompts of 100 tokens, 32 / 8 heads of 128, 317 us where the memory alone would be 95.
@@ -380,6 +380,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         const float mx = max3(max3(top[0], top[1], top[2]), top[3], top[3]);
         if (__any_sync(0xffffffffu, (mx - m) * c > AP_RAISE)) {
           const float mn = fmaxf(m, mx);
+          if (score_too_large(mn * c)) report(p.status, DEV_LARGE_SCORE);
           const float f = mn == m ? 1.f : ap_ex2((m - mn) * c);  // 0 from the initial minus infinity
           m = mn;
           l *= f;

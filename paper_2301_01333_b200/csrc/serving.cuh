@@ -1,6 +1,7 @@
 // Declarations shared by the host side (gc_serving.cu) and the kernels of the served attention block.
 #pragma once
 #include <cuda_bf16.h>
+#include <math.h>
 
 #include "gc_internal.h"
 
@@ -13,7 +14,14 @@ enum : uint32_t {
   DEV_BAD_LENGTH = 0x203,
   DEV_BAD_OFFSETS = 0x204,
   DEV_LARGE_VALUE = 0x205,
+  DEV_LARGE_SCORE = 0x206,
 };
+
+// Scores times log2(e) above which weights could leave fp32: 2^26 log2(e).  (Exponents are taken relative to a reference rounded to 2^-24
+// of itself.  What that is off by, up to 3 binades here and 60 at 2^30, all weights of a row carry as a common factor.)
+// Infinite scores are another matter: their rows are NaN.
+constexpr float LARGEST_SCORE = 0x1p26f * 1.4426950408889634f;
+__device__ __forceinline__ bool score_too_large(float s) { return fabsf(s) > LARGEST_SCORE && fabsf(s) < INFINITY; }
 
 // Launches of this block follow one another closely: each may be set up while the kernel before it on the stream still runs
 // (programmatic dependent launch), and every thread of every kernel passes wait_for_predecessor() before it touches global memory

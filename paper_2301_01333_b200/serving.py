@@ -181,7 +181,8 @@ class KV4Cache:
         order) names, lengths (int32 [batch]) counting the tokens appended so far, the queries' own among them: query j sees
         the first lengths - (queries - 1) + j of them.  scale: head_dim ** -0.5 if not given; max_length: a bound of lengths the
         caller knows (the work is laid out for it; a longer sequence is an error), width * page_size if not given.  A value above 2^32
-        in size, which the sums could not hold, is reported by ``query_status()``; below 2^-40 they lose accuracy."""
+        or a score above 2^26 in size, more than the sums and weights can hold, is reported by ``query_status()``; values below
+        2^-40 lose accuracy."""
         return _serving.kv4_attend(self._at, q, block_table, lengths, scale, max_length, out, self._tensors)
 
     def query_status(self) -> None:
@@ -196,7 +197,7 @@ def attention_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: to
     query rows cu_q[b] .. cu_q[b + 1] and key rows cu_k[b] .. cu_k[b + 1] (int32 [batch + 1]; cu_k = cu_q if not given).  causal:
     query row i of nq sees the first i + 1 + nk - nq keys.  A row that sees none is zero; rows no sequence owns are left as they
     were in a given `out`, and are zero in one made here.  status: a word (``new_status``) for what only the device can see; the
-    device's own, which ``query_status()`` reads, if not given."""
+    device's own, which ``query_status()`` reads, if not given.  A finite score above 2^26 in size is reported there as well."""
     if not isinstance(q, torch.Tensor):
         raise TypeError("q must be a torch.Tensor")
     if out is None:

@@ -407,3 +407,34 @@ def test_rope_several_tokens_to_a_block(S, dtype, interleaved, t, d, rot, pad):
 def test_prompt_items_of_128_and_of_256_rows(S, causal, heads, n):
     # (tokens / 128 + sequences) x heads is 144 and 153 for 1024 tokens, either side of 148 SMs, where items become twice as long
     prompt_case(S, n, n, heads, 1 if heads == 16 else 17, 64, causal, seed=heads + len(n), tail=3, poison=True)
+
+
+# ------------------------------------------------------------------------------------------------ sizes of scores
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_too_large_for_their_weights_are_reported(S, sign):
+    # every key is the same, so every output is 1, or, with scores (2^17 sqrt(128) sizes) above 2^26, the call says that it cannot tell
+    d, m = 128, 300
+    k, v = torch.full((m, 1, d), 2.0 ** 17, device=DEV).bfloat16(), torch.ones(m, 1, d, device=DEV).bfloat16()
+    cu = torch.tensor([0, m], dtype=torch.int32, device=DEV)
+    cache = S.KV4Cache.allocate(20, 16, 1, d, 128)
+    cache.append(k, v, torch.arange(m, device=DEV))
+    table, ln = torch.arange(20, dtype=torch.int32, device=DEV)[None], torch.tensor([m], dtype=torch.int32, device=DEV)
+    status = S.new_status(DEV)
+    for size, bad in ((1.0, False), (1.37, False), (1.37 * 2.0 ** 4, False), (1.37 * 2.0 ** 14, True), (1.71 * 2.0 ** 20, True)):
+        q = torch.full((m, 2, d), sign * size, device=DEV).bfloat16()
+        for call, query in ((lambda: S.attention_prompt(q, k, v, cu, status=status), lambda: S.query_status(status)),
+                            (lambda: cache.attend(q[None, :1], table, ln), cache.query_status),
+                            (lambda: cache.attend(q[None, :5], table.expand(1, 20), ln, max_length=m), cache.query_status)):
+            out = call()
+            if bad:
+                with pytest.raises(S.GcError, match="score"):
+                    query()
+            else:
+                query()
+                # the weights are rounded to bf16, and so is the output: half a step each
+                within(out, torch.ones_like(out, dtype=torch.float64), torch.full_like(out, 1 / 128, dtype=torch.float64))
+    q = torch.full((m, 2, d), sign * math.inf, device=DEV).bfloat16()      # infinite scores: NaN, and nothing to report
+    S.attention_prompt(q, k, v, cu, status=status)
+    S.query_status(status)
+    cache.attend(q[None, :1], table, ln)
+    cache.query_status()
