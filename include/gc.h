@@ -275,6 +275,8 @@ gc_status_t gc_selftest_bounded_wait(void* cuda_stream, void* status_dev, uint32
  *   gc_qk_norm_rope        RMS norm of every query and key head and the rotation by position, one pass
  *   gc_kv4_append / _read  keys and values into a paged 4-bit cache, and back as the values it holds
  *   gc_attention_kv4       a few new queries per sequence against that cache
+ *   gc_attention_kv4_chunk any number of new tokens per sequence against it
+ *   gc_kv4_weigh / _evict  the attention weight its tokens receive, and those with the most kept
  *   gc_attention_prompt    whole prompts: packed sequences, causal or not, grouped heads
  *
  * Conventions beyond those above: each call enqueues its kernels on cuda_stream, on the device named in its
@@ -374,6 +376,84 @@ typedef struct {
 gc_status_t gc_attention_kv4_workspace_bytes(const gc_kv4_cache_t* cache, const gc_attention_kv4_t* d, size_t* bytes);
 gc_status_t gc_attention_kv4(void* cuda_stream, const gc_kv4_cache_t* cache, const gc_attention_kv4_t* d,
                              void* workspace_dev, size_t workspace_bytes);
+/* The same, and lse[b, j, h] (fp32, dense [batch, queries, q_heads]) = log sum_t exp(scale * q[b, j, h] . K[t]) over the tokens the
+ * query sees: what gc_kv4_weigh needs; minus infinity where it sees none. */
+gc_status_t gc_attention_kv4_lse(void* cuda_stream, const gc_kv4_cache_t* cache, const gc_attention_kv4_t* d, float* lse_dev,
+                                 void* workspace_dev, size_t workspace_bytes);
+
+/* Chunks of new tokens against the cache: sequence b owns query rows [cu_q[b], cu_q[b + 1]), nq of them, none among them and
+ * any number; its new tokens' keys and values have been appended and lengths[b] counts them:
+ *   out[i, h] = softmax_t(scale * q[i, h] . K[t]) V over the cached tokens t < lengths[b] - nq + 1 + (i - cu_q[b])
+ * A row that sees nothing (more new tokens than length) is zero; rows no sequence owns are left as they were.  q, out bf16, rows 16-byte
+ * aligned.  K and V are the values held rounded to bf16, as gc_kv4_read gives them (half a bf16 step each; gc_attention_kv4 does
+ * without); scores, statistics and sums fp32, probabilities rounded to bf16.  block_table, max_length: as for gc_attention_kv4, and
+ * so is what the status word reports (values above 2^32, scores above 2^26 in size, pages and lengths out of bounds), offsets that
+ * decrease or leave the packed tokens besides.  What a row does not see has no influence on it, whatever is held there; a
+ * group of values that is not finite counts as NaN.  Sequences may share pages. */
+typedef struct {
+  int32_t batch, q_heads;
+  int64_t q_tokens;              /* rows of q / out in all */
+  int32_t table_width, max_length;
+  int64_t table_stride;
+  float scale;
+  int32_t reserved_;
+  gc_heads_t q, out;
+  const int32_t* cu_q;           /* [batch + 1], non-decreasing, within 0 .. q_tokens */
+  const int32_t* block_table;
+  const int32_t* lengths;        /* [batch] */
+} gc_attention_kv4_chunk_t;
+/* Bytes of 16-byte aligned device scratch (no initialisation; not shared by calls that can overlap). */
+gc_status_t gc_attention_kv4_chunk_workspace_bytes(const gc_kv4_cache_t* cache, const gc_attention_kv4_chunk_t* d, size_t* bytes);
+gc_status_t gc_attention_kv4_chunk(void* cuda_stream, const gc_kv4_cache_t* cache, const gc_attention_kv4_chunk_t* d, void* workspace_dev,
+                                   size_t workspace_bytes);
+
+/* The attention weight every cached token receives, fp32 [num_pages, kv_heads, page_size], paged like the cache: for the tokens
+ * t < lengths[b] of every sequence
+ *   out[t, hk] = decay * weights[t, hk] + sum over queries j that see t and query heads h that share hk of exp(scale * q[b, j, h] . K[t] - lse[b, j, h])
+ * with q, lengths, block_table, max_length and scale as in the attention call, and the lse it gave.  A query whose lse is minus infinity
+ * adds nothing; with a decay of 0 what `weights` holds is not looked at.  out may be weights; other places of it are left as they
+ * were.  All in fp32 from the exact values held.  A page may be named by one sequence of a call only. */
+typedef struct {
+  int32_t batch, queries, q_heads, table_width;
+  int64_t table_stride;
+  int32_t max_length;
+  float scale;
+  const void* q;
+  int64_t q_batch_stride, q_query_stride, q_head_stride;
+  const float* lse;              /* [batch, queries, q_heads] */
+  const int32_t* block_table;
+  const int32_t* lengths;        /* [batch] */
+  const float* weights;
+  float* out;
+  float decay;
+  int32_t reserved_;
+} gc_kv4_weigh_t;
+gc_status_t gc_kv4_weigh(void* cuda_stream, const gc_kv4_cache_t* cache, const gc_kv4_weigh_t* d);
+
+/* Eviction: of every sequence with n = lengths[b] > keep tokens, each key/value head keeps its own `keep`: the newest `recent` ones, and of
+ * the others the keep - recent with the largest scores (equal ones: the older; NaN counts as largest).  scores: fp32, paged like the
+ * cache.  The kept tokens take positions 0 .. keep - 1: those from there stay where they are, and the holes
+ * between them are filled, in order, with the kept ones from behind, in order.  (Attention does not mind the order of the tokens a query sees.)
+ * Shorter sequences keep all.  With m = min(n, keep):
+ *   out_lengths[b] = m;   kept[b, hk, i] = the position, before, of the token at i, or -1 for i >= m   (int32 [batch, kv_heads, keep])
+ * out_table null: in place; pages behind m are free then, and the scores of positions m .. n - 1 zero.  Else the kept tokens
+ * and their scores are copied to the pages out_table names, which must not be among those of block_table, and the scores of the
+ * rest of their last page are zero; block_table's pages are left as they were.  A page may be named by one sequence of a call only,
+ * except that block_table's may be shared where out_table is given. */
+typedef struct {
+  int32_t batch, keep, recent, max_length;
+  int32_t table_width, out_table_width;
+  int64_t table_stride, out_table_stride;
+  const int32_t* block_table;
+  const int32_t* out_table;
+  const int32_t* lengths;        /* [batch] */
+  int32_t* out_lengths;          /* [batch] */
+  int32_t* kept;
+  float* scores;
+} gc_kv4_evict_t;
+/* Bytes of 16-byte aligned device scratch (0: none). */
+gc_status_t gc_kv4_evict_workspace_bytes(const gc_kv4_cache_t* cache, const gc_kv4_evict_t* d, size_t* bytes);
+gc_status_t gc_kv4_evict(void* cuda_stream, const gc_kv4_cache_t* cache, const gc_kv4_evict_t* d, void* workspace_dev, size_t workspace_bytes);
 
 /* out = softmax(scale * Q K^T) V for `batch` sequences packed one behind the other: sequence b owns query rows
  * [cu_q[b], cu_q[b + 1]) and key rows [cu_k[b], cu_k[b + 1]).  causal = 1: query row i of nq sees keys j <= i + nk - nq

@@ -36,7 +36,8 @@ EXPORTS = [
     "gc_query_status", "gc_launches_per_execute", "gc_plan_description", "gc_last_error", "gc_version",
     "gc_matmul_s32_noalloc", "gc_noalloc_scratch_bytes", "gc_selftest_bounded_wait", "gc_invalidate_constants",
     "gc_qk_norm_rope", "gc_kv4_append", "gc_kv4_read", "gc_attention_kv4_workspace_bytes", "gc_attention_kv4",
-    "gc_attention_prompt", "gc_serving_status",
+    "gc_attention_prompt", "gc_serving_status", "gc_attention_kv4_lse", "gc_attention_kv4_chunk_workspace_bytes",
+    "gc_attention_kv4_chunk", "gc_kv4_weigh", "gc_kv4_evict_workspace_bytes", "gc_kv4_evict",
 ]
 
 
@@ -80,6 +81,27 @@ class gc_attention_kv4_t(C.Structure):
                 ("q_batch_stride", C.c_int64), ("q_query_stride", C.c_int64), ("q_head_stride", C.c_int64),
                 ("out", C.c_void_p), ("o_batch_stride", C.c_int64), ("o_query_stride", C.c_int64),
                 ("o_head_stride", C.c_int64), ("block_table", C.c_void_p), ("lengths", C.c_void_p)]
+
+
+class gc_attention_kv4_chunk_t(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("q_heads", C.c_int32), ("q_tokens", C.c_int64), ("table_width", C.c_int32),
+                ("max_length", C.c_int32), ("table_stride", C.c_int64), ("scale", C.c_float), ("reserved_", C.c_int32),
+                ("q", gc_heads_t), ("out", gc_heads_t), ("cu_q", C.c_void_p), ("block_table", C.c_void_p), ("lengths", C.c_void_p)]
+
+
+class gc_kv4_weigh_t(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("queries", C.c_int32), ("q_heads", C.c_int32), ("table_width", C.c_int32),
+                ("table_stride", C.c_int64), ("max_length", C.c_int32), ("scale", C.c_float), ("q", C.c_void_p),
+                ("q_batch_stride", C.c_int64), ("q_query_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("lse", C.c_void_p), ("block_table", C.c_void_p), ("lengths", C.c_void_p), ("weights", C.c_void_p),
+                ("out", C.c_void_p), ("decay", C.c_float), ("reserved_", C.c_int32)]
+
+
+class gc_kv4_evict_t(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("keep", C.c_int32), ("recent", C.c_int32), ("max_length", C.c_int32),
+                ("table_width", C.c_int32), ("out_table_width", C.c_int32), ("table_stride", C.c_int64),
+                ("out_table_stride", C.c_int64), ("block_table", C.c_void_p), ("out_table", C.c_void_p),
+                ("lengths", C.c_void_p), ("out_lengths", C.c_void_p), ("kept", C.c_void_p), ("scores", C.c_void_p)]
 
 
 class gc_attention_prompt_t(C.Structure):
@@ -144,8 +166,16 @@ def load_library() -> C.CDLL:
     lib.gc_attention_kv4.argtypes = [vp, C.POINTER(gc_kv4_cache_t), C.POINTER(gc_attention_kv4_t), vp, sz]
     lib.gc_attention_prompt.argtypes = [vp, C.POINTER(gc_attention_prompt_t)]
     lib.gc_serving_status.argtypes = [vp, vp]
+    cache = C.POINTER(gc_kv4_cache_t)
+    lib.gc_attention_kv4_lse.argtypes = [vp, cache, C.POINTER(gc_attention_kv4_t), vp, vp, sz]
+    lib.gc_attention_kv4_chunk_workspace_bytes.argtypes = [cache, C.POINTER(gc_attention_kv4_chunk_t), C.POINTER(sz)]
+    lib.gc_attention_kv4_chunk.argtypes = [vp, cache, C.POINTER(gc_attention_kv4_chunk_t), vp, sz]
+    lib.gc_kv4_weigh.argtypes = [vp, cache, C.POINTER(gc_kv4_weigh_t)]
+    lib.gc_kv4_evict_workspace_bytes.argtypes = [cache, C.POINTER(gc_kv4_evict_t), C.POINTER(sz)]
+    lib.gc_kv4_evict.argtypes = [vp, cache, C.POINTER(gc_kv4_evict_t), vp, sz]
     for name in ("gc_qk_norm_rope", "gc_kv4_append", "gc_kv4_read", "gc_attention_kv4_workspace_bytes", "gc_attention_kv4",
-                 "gc_attention_prompt", "gc_serving_status"):
+                 "gc_attention_prompt", "gc_serving_status", "gc_attention_kv4_lse", "gc_attention_kv4_chunk_workspace_bytes",
+                 "gc_attention_kv4_chunk", "gc_kv4_weigh", "gc_kv4_evict_workspace_bytes", "gc_kv4_evict"):
         getattr(lib, name).restype = i32
     for name in ("gc_partition_create", "gc_compile", "gc_workspace_bytes", "gc_set_workspace", "gc_execute",
                  "gc_host_staging_bytes", "gc_set_host_staging", "gc_execute_host", "gc_execute_host_async",
@@ -338,6 +368,42 @@ def gc_attention_kv4_workspace_bytes(cache: gc_kv4_cache_t, desc: gc_attention_k
 
 def gc_attention_kv4(stream: int, cache: gc_kv4_cache_t, desc: gc_attention_kv4_t, workspace_ptr: int, workspace_bytes: int) -> None:
     st = load_library().gc_attention_kv4(stream, cache, desc, workspace_ptr, workspace_bytes)
+    if st:
+        raise GcError(st, gc_last_error())
+
+
+def gc_attention_kv4_lse(stream: int, cache: gc_kv4_cache_t, desc: gc_attention_kv4_t, lse_ptr: int, workspace_ptr: int, workspace_bytes: int) -> None:
+    st = load_library().gc_attention_kv4_lse(stream, cache, desc, lse_ptr, workspace_ptr, workspace_bytes)
+    if st:
+        raise GcError(st, gc_last_error())
+
+
+def gc_attention_kv4_chunk_workspace_bytes(cache: gc_kv4_cache_t, desc: gc_attention_kv4_chunk_t) -> int:
+    n = C.c_size_t()
+    _check(load_library().gc_attention_kv4_chunk_workspace_bytes(cache, desc, n))
+    return n.value
+
+
+def gc_attention_kv4_chunk(stream: int, cache: gc_kv4_cache_t, desc: gc_attention_kv4_chunk_t, workspace_ptr: int, workspace_bytes: int) -> None:
+    st = load_library().gc_attention_kv4_chunk(stream, cache, desc, workspace_ptr, workspace_bytes)
+    if st:
+        raise GcError(st, gc_last_error())
+
+
+def gc_kv4_weigh(stream: int, cache: gc_kv4_cache_t, desc: gc_kv4_weigh_t) -> None:
+    st = load_library().gc_kv4_weigh(stream, cache, desc)
+    if st:
+        raise GcError(st, gc_last_error())
+
+
+def gc_kv4_evict_workspace_bytes(cache: gc_kv4_cache_t, desc: gc_kv4_evict_t) -> int:
+    n = C.c_size_t()
+    _check(load_library().gc_kv4_evict_workspace_bytes(cache, desc, n))
+    return n.value
+
+
+def gc_kv4_evict(stream: int, cache: gc_kv4_cache_t, desc: gc_kv4_evict_t, workspace_ptr: int, workspace_bytes: int) -> None:
+    st = load_library().gc_kv4_evict(stream, cache, desc, workspace_ptr, workspace_bytes)
     if st:
         raise GcError(st, gc_last_error())
 

@@ -204,9 +204,9 @@ extern "C" gc_status_t gc_attention_kv4_workspace_bytes(const gc_kv4_cache_t* ca
   return GC_OK;
 }
 
-extern "C" gc_status_t gc_attention_kv4(void* cuda_stream, const gc_kv4_cache_t* cache, const gc_attention_kv4_t* d, void* workspace_dev,
-                                        size_t workspace_bytes) {
-  const char* who = "gc_attention_kv4";
+namespace {
+gc_status_t attend(const char* who, void* cuda_stream, const gc_kv4_cache_t* cache, const gc_attention_kv4_t* d, float* lse, void* workspace_dev,
+                   size_t workspace_bytes) {
   gc_status_t st = check_attend(who, cache, d);
   if (st != GC_OK) return st;
   if (d->batch == 0) return GC_OK;
@@ -242,8 +242,225 @@ extern "C" gc_status_t gc_attention_kv4(void* cuda_stream, const gc_kv4_cache_t*
   p.k_codes = static_cast<const uint8_t*>(cache->k_codes); p.k_params = static_cast<const uint32_t*>(cache->k_params);
   p.v_codes = static_cast<const uint8_t*>(cache->v_codes); p.v_params = static_cast<const uint32_t*>(cache->v_params);
   p.ws = static_cast<float*>(workspace_dev);
+  p.lse = lse;
   p.status = cache->status;
   RUN(launch_attn_kv4(p, cache->head_dim, cache->group, static_cast<cudaStream_t>(cuda_stream)));
+  return GC_OK;
+}
+
+// Pages of a table whose row is `width` long, for up to `positions` tokens of a sequence.
+gc_status_t check_table(const char* who, const char* name, const gc_kv4_cache_t& c, const void* table, int width, int64_t stride, int64_t positions) {
+  if (width < 0 || stride < 0) REFUSE(GC_ERR_SHAPE, "%s: negative size of %s", who, name);
+  if (positions > static_cast<int64_t>(width) * c.page_size)
+    REFUSE(GC_ERR_SHAPE, "%s: %lld tokens exceed the %d pages of %d of %s", who, (long long)positions, width, c.page_size, name);
+  if (positions && !table) REFUSE(GC_ERR_INVALID_ARG, "%s: %s is null", who, name);
+  if (misaligned(table, 4)) REFUSE(GC_ERR_ALIGNMENT, "%s: %s must be 4-byte aligned", who, name);
+  return GC_OK;
+}
+int page_shift_of(const gc_kv4_cache_t& c) {
+  int s = 0;
+  while ((1 << s) < c.page_size) ++s;
+  return s;
+}
+
+// A CTA of the chunk kernel takes at least two blocks of keys: below that its beginning and the joining cost more than they spare.
+constexpr int CHUNK_LEAST = 2;
+
+gc_status_t check_chunk(const char* who, const gc_kv4_cache_t* c, const gc_attention_kv4_chunk_t* d) {
+  gc_status_t st = check_cache(who, c);
+  if (st != GC_OK) return st;
+  if (!d) REFUSE(GC_ERR_INVALID_ARG, "%s: null argument", who);
+  if (d->batch < 0 || d->q_tokens < 0) REFUSE(GC_ERR_SHAPE, "%s: negative size", who);
+  if (d->q_heads < 1 || d->q_heads % c->kv_heads) REFUSE(GC_ERR_SHAPE, "%s: %d query heads over %d key/value heads", who, d->q_heads, c->kv_heads);
+  if (d->q_heads / c->kv_heads > 256) REFUSE(GC_ERR_UNSUPPORTED, "%s: more than 256 query heads share a key/value head", who);
+  if (!(d->scale > 0.f) || !std::isfinite(d->scale)) REFUSE(GC_ERR_INVALID_ARG, "%s: scale must be finite and positive", who);
+  if (d->max_length < 0) REFUSE(GC_ERR_SHAPE, "%s: negative length", who);
+  if (d->max_length > 0x7FFFFFFF - 65536) REFUSE(GC_ERR_UNSUPPORTED, "%s: max_length too large", who);
+  const int64_t g = d->q_heads / c->kv_heads;
+  if (d->q_tokens * g > (1LL << 30) || d->q_tokens > (1LL << 30) || d->batch > (1 << 20)) REFUSE(GC_ERR_UNSUPPORTED, "%s: too many tokens or sequences", who);
+  if (attn_chunk_items(d->q_tokens, d->batch, static_cast<int>(g)) * (d->max_length / 128 + 2LL) > 0x7FFFFFFF)
+    REFUSE(GC_ERR_UNSUPPORTED, "%s: too many tokens for sequences of up to %d", who, d->max_length);
+  return GC_OK;
+}
+struct ChunkLaunch {
+  int64_t items;
+  int ctas;
+  size_t bytes;
+};
+ChunkLaunch lay_out_chunk(const gc_kv4_cache_t& c, const gc_attention_kv4_chunk_t& d, int sms) {
+  ChunkLaunch s;
+  s.items = attn_chunk_items(d.q_tokens, d.batch, d.q_heads / c.kv_heads);
+  s.ctas = attn_chunk_ctas(s.items, c.kv_heads, d.max_length, CHUNK_LEAST, sms);
+  s.bytes = attn_chunk_bytes(c.head_dim, s.ctas, s.items);
+  return s;
+}
+
+gc_status_t check_evict(const char* who, const gc_kv4_cache_t* c, const gc_kv4_evict_t* d) {
+  gc_status_t st = check_cache(who, c);
+  if (st != GC_OK) return st;
+  if (!d) REFUSE(GC_ERR_INVALID_ARG, "%s: null argument", who);
+  if (d->batch < 0 || d->max_length < 0) REFUSE(GC_ERR_SHAPE, "%s: negative size", who);
+  if (d->keep < 0 || d->recent < 0 || d->recent > d->keep) REFUSE(GC_ERR_INVALID_ARG, "%s: keep %d, of them recent %d", who, d->keep, d->recent);
+  if (d->max_length > 0x7FFFFFFF - 65536) REFUSE(GC_ERR_UNSUPPORTED, "%s: max_length too large", who);
+  const int64_t units = static_cast<int64_t>(d->batch) * c->kv_heads;
+  if (units > (1 << 24) || units * d->keep > 0x7FFFFFFF || (units << 8) > 0x7FFFFFFF)
+    REFUSE(GC_ERR_UNSUPPORTED, "%s: batch times heads times tokens to keep too large", who);
+  return GC_OK;
+}
+// Holes that can be filled: positions that stay in use, and tokens that leave.
+int64_t evict_list(const gc_kv4_evict_t& d) {
+  const int64_t leave = static_cast<int64_t>(d.max_length) - d.keep;
+  return leave <= 0 ? 0 : leave < d.keep ? leave : d.keep;
+}
+}  // namespace
+
+extern "C" gc_status_t gc_attention_kv4(void* cuda_stream, const gc_kv4_cache_t* cache, const gc_attention_kv4_t* d, void* workspace_dev,
+                                        size_t workspace_bytes) {
+  return attend("gc_attention_kv4", cuda_stream, cache, d, nullptr, workspace_dev, workspace_bytes);
+}
+
+extern "C" gc_status_t gc_attention_kv4_lse(void* cuda_stream, const gc_kv4_cache_t* cache, const gc_attention_kv4_t* d, float* lse_dev, void* workspace_dev,
+                                            size_t workspace_bytes) {
+  const char* who = "gc_attention_kv4_lse";
+  if (!lse_dev && d && d->batch > 0) REFUSE(GC_ERR_INVALID_ARG, "%s: null argument", who);
+  if (misaligned(lse_dev, 4)) REFUSE(GC_ERR_ALIGNMENT, "%s: lse must be 4-byte aligned", who);
+  return attend(who, cuda_stream, cache, d, lse_dev, workspace_dev, workspace_bytes);
+}
+
+extern "C" gc_status_t gc_attention_kv4_chunk_workspace_bytes(const gc_kv4_cache_t* cache, const gc_attention_kv4_chunk_t* d, size_t* bytes) {
+  const char* who = "gc_attention_kv4_chunk_workspace_bytes";
+  if (!bytes) REFUSE(GC_ERR_INVALID_ARG, "%s: null argument", who);
+  gc_status_t st = check_chunk(who, cache, d);
+  if (st != GC_OK) return st;
+  *bytes = 0;
+  if (d->batch == 0 || d->q_tokens == 0) return GC_OK;
+  int sms = 0;
+  RUN(sm_count(cache->cuda_device, &sms));
+  *bytes = lay_out_chunk(*cache, *d, sms).bytes;
+  return GC_OK;
+}
+
+extern "C" gc_status_t gc_attention_kv4_chunk(void* cuda_stream, const gc_kv4_cache_t* cache, const gc_attention_kv4_chunk_t* d, void* workspace_dev,
+                                              size_t workspace_bytes) {
+  const char* who = "gc_attention_kv4_chunk";
+  gc_status_t st = check_chunk(who, cache, d);
+  if (st != GC_OK) return st;
+  if (d->batch == 0 || d->q_tokens == 0) return GC_OK;
+  if (!d->cu_q || !d->lengths) REFUSE(GC_ERR_INVALID_ARG, "%s: null argument", who);
+  if (misaligned(d->cu_q, 4) || misaligned(d->lengths, 4)) REFUSE(GC_ERR_ALIGNMENT, "%s: cu_q and lengths must be 4-byte aligned", who);
+  if ((st = check_table(who, "block_table", *cache, d->block_table, d->table_width, d->table_stride, d->max_length)) != GC_OK) return st;
+  if ((st = check_heads(who, "q", d->q, 2, true)) != GC_OK || (st = check_heads(who, "out", d->out, 2, true)) != GC_OK) return st;
+  OnDevice on(cache->cuda_device);
+  RUN(on.err());
+  int sms = 0;
+  RUN(sm_count(cache->cuda_device, &sms));
+  const ChunkLaunch l = lay_out_chunk(*cache, *d, sms);
+  if (!workspace_dev || workspace_bytes < l.bytes) REFUSE(GC_ERR_INVALID_ARG, "%s: the workspace must have %zu bytes", who, l.bytes);
+  if (misaligned(workspace_dev, 16)) REFUSE(GC_ERR_ALIGNMENT, "%s: the workspace must be 16-byte aligned", who);
+  ChunkParams p = {};
+  p.B = d->batch; p.Hq = d->q_heads; p.Hk = cache->kv_heads; p.g = d->q_heads / cache->kv_heads;
+  p.page_shift = page_shift_of(*cache); p.max_len = d->max_length;
+  p.least = CHUNK_LEAST; p.most_items = static_cast<int>(l.items);
+  p.q_tokens = d->q_tokens; p.num_pages = cache->num_pages; p.table_stride = d->table_stride;
+  p.c = d->scale * 1.4426950408889634f;
+  p.q = static_cast<const __nv_bfloat16*>(d->q.data);
+  p.q_tok = d->q.token_stride; p.q_head = d->q.head_stride;
+  p.o = static_cast<__nv_bfloat16*>(d->out.data);
+  p.o_tok = d->out.token_stride; p.o_head = d->out.head_stride;
+  p.cu_q = d->cu_q; p.table = d->block_table; p.lengths = d->lengths;
+  p.k_codes = static_cast<const uint8_t*>(cache->k_codes); p.k_params = static_cast<const uint32_t*>(cache->k_params);
+  p.v_codes = static_cast<const uint8_t*>(cache->v_codes); p.v_params = static_cast<const uint32_t*>(cache->v_params);
+  p.ws = workspace_dev;
+  p.status = cache->status;
+  RUN(launch_attn_chunk(p, cache->head_dim, cache->group, l.ctas, static_cast<cudaStream_t>(cuda_stream)));
+  return GC_OK;
+}
+
+extern "C" gc_status_t gc_kv4_weigh(void* cuda_stream, const gc_kv4_cache_t* cache, const gc_kv4_weigh_t* d) {
+  const char* who = "gc_kv4_weigh";
+  gc_status_t st = check_cache(who, cache);
+  if (st != GC_OK) return st;
+  if (!d) REFUSE(GC_ERR_INVALID_ARG, "%s: null argument", who);
+  if (d->batch < 0 || d->q_heads < 1 || d->q_heads % cache->kv_heads)
+    REFUSE(GC_ERR_SHAPE, "%s: %d query heads over %d key/value heads", who, d->q_heads, cache->kv_heads);
+  if (d->queries < 1 || d->queries > 16) REFUSE(GC_ERR_UNSUPPORTED, "%s: %d queries per sequence (1 to 16)", who, d->queries);
+  if (d->q_heads / cache->kv_heads > 256) REFUSE(GC_ERR_UNSUPPORTED, "%s: more than 256 query heads share a key/value head", who);
+  if (!(d->scale > 0.f) || !std::isfinite(d->scale)) REFUSE(GC_ERR_INVALID_ARG, "%s: scale must be finite and positive", who);
+  if (!(d->decay >= 0.f) || !std::isfinite(d->decay)) REFUSE(GC_ERR_INVALID_ARG, "%s: decay must be finite and not negative", who);
+  if (d->max_length < 0) REFUSE(GC_ERR_SHAPE, "%s: negative length", who);
+  if (d->max_length > 0x7FFFFFFF - 65536) REFUSE(GC_ERR_UNSUPPORTED, "%s: max_length too large", who);
+  if (static_cast<int64_t>(d->batch) * cache->kv_heads > (1 << 22)) REFUSE(GC_ERR_UNSUPPORTED, "%s: batch times heads too large", who);
+  if (d->batch == 0 || d->max_length == 0) return GC_OK;
+  if (!d->q || !d->lse || !d->lengths || !d->weights || !d->out) REFUSE(GC_ERR_INVALID_ARG, "%s: null argument", who);
+  if ((st = check_table(who, "block_table", *cache, d->block_table, d->table_width, d->table_stride, d->max_length)) != GC_OK) return st;
+  const int64_t strides[3] = {d->q_batch_stride, d->q_query_stride, d->q_head_stride};
+  for (int64_t s : strides) {
+    if (s < 0) REFUSE(GC_ERR_SHAPE, "%s: negative stride", who);
+    if (s % 8) REFUSE(GC_ERR_ALIGNMENT, "%s: q needs 16-byte aligned rows", who);
+  }
+  if (misaligned(d->q, 16)) REFUSE(GC_ERR_ALIGNMENT, "%s: q needs 16-byte aligned rows", who);
+  if (misaligned(d->lse, 4) || misaligned(d->lengths, 4) || misaligned(d->weights, 4) || misaligned(d->out, 4))
+    REFUSE(GC_ERR_ALIGNMENT, "%s: an array is not aligned to its element size", who);
+  OnDevice on(cache->cuda_device);
+  RUN(on.err());
+  int sms = 0;
+  RUN(sm_count(cache->cuda_device, &sms));
+  WeighParams p = {};
+  p.B = d->batch; p.n = d->queries; p.Hq = d->q_heads; p.Hk = cache->kv_heads; p.g = d->q_heads / cache->kv_heads;
+  p.page_shift = page_shift_of(*cache); p.max_len = d->max_length;
+  p.num_pages = cache->num_pages; p.table_stride = d->table_stride;
+  p.c = d->scale * 1.4426950408889634f; p.decay = d->decay;
+  p.q = static_cast<const __nv_bfloat16*>(d->q);
+  p.qb = d->q_batch_stride; p.qn = d->q_query_stride; p.qh = d->q_head_stride;
+  p.lse = d->lse; p.table = d->block_table; p.lengths = d->lengths;
+  p.k_codes = static_cast<const uint8_t*>(cache->k_codes); p.k_params = static_cast<const uint32_t*>(cache->k_params);
+  p.weights = d->weights; p.out = d->out;
+  p.status = cache->status;
+  RUN(launch_kv4_weigh(p, cache->head_dim, cache->group, sms, static_cast<cudaStream_t>(cuda_stream)));
+  return GC_OK;
+}
+
+extern "C" gc_status_t gc_kv4_evict_workspace_bytes(const gc_kv4_cache_t* cache, const gc_kv4_evict_t* d, size_t* bytes) {
+  const char* who = "gc_kv4_evict_workspace_bytes";
+  if (!bytes) REFUSE(GC_ERR_INVALID_ARG, "%s: null argument", who);
+  gc_status_t st = check_evict(who, cache, d);
+  if (st != GC_OK) return st;
+  *bytes = static_cast<size_t>(d->batch) * cache->kv_heads * 2 * evict_list(*d) * sizeof(int32_t);
+  return GC_OK;
+}
+
+extern "C" gc_status_t gc_kv4_evict(void* cuda_stream, const gc_kv4_cache_t* cache, const gc_kv4_evict_t* d, void* workspace_dev, size_t workspace_bytes) {
+  const char* who = "gc_kv4_evict";
+  gc_status_t st = check_evict(who, cache, d);
+  if (st != GC_OK) return st;
+  if (d->batch == 0) return GC_OK;
+  if (!d->scores || !d->lengths || !d->out_lengths || (d->keep && !d->kept)) REFUSE(GC_ERR_INVALID_ARG, "%s: null argument", who);
+  if (misaligned(d->scores, 4) || misaligned(d->lengths, 4) || misaligned(d->out_lengths, 4) || misaligned(d->kept, 4))
+    REFUSE(GC_ERR_ALIGNMENT, "%s: an array is not aligned to its element size", who);
+  if ((st = check_table(who, "block_table", *cache, d->block_table, d->table_width, d->table_stride, d->max_length)) != GC_OK) return st;
+  if (d->out_table && (st = check_table(who, "out_table", *cache, d->out_table, d->out_table_width, d->out_table_stride,
+                                        d->keep < d->max_length ? d->keep : d->max_length)) != GC_OK)
+    return st;
+  const size_t need = static_cast<size_t>(d->batch) * cache->kv_heads * 2 * evict_list(*d) * sizeof(int32_t);
+  if (need && (!workspace_dev || workspace_bytes < need)) REFUSE(GC_ERR_INVALID_ARG, "%s: the workspace must have %zu bytes", who, need);
+  if (misaligned(workspace_dev, 4)) REFUSE(GC_ERR_ALIGNMENT, "%s: the workspace must be 4-byte aligned", who);
+  OnDevice on(cache->cuda_device);
+  RUN(on.err());
+  int sms = 0;
+  RUN(sm_count(cache->cuda_device, &sms));
+  EvictParams p = {};
+  p.B = d->batch; p.Hk = cache->kv_heads; p.keep = d->keep; p.recent = d->recent;
+  p.page_shift = page_shift_of(*cache); p.max_len = d->max_length;
+  p.in_place = d->out_table == nullptr; p.list_len = static_cast<int>(evict_list(*d));
+  p.num_pages = cache->num_pages;
+  p.table = d->block_table; p.table_stride = d->table_stride;
+  p.out_table = d->out_table ? d->out_table : d->block_table; p.out_stride = d->out_table ? d->out_table_stride : d->table_stride;
+  p.lengths = d->lengths; p.out_lengths = d->out_lengths; p.kept = d->kept; p.scores = d->scores;
+  p.k_codes = static_cast<uint8_t*>(cache->k_codes); p.k_params = static_cast<uint32_t*>(cache->k_params);
+  p.v_codes = static_cast<uint8_t*>(cache->v_codes); p.v_params = static_cast<uint32_t*>(cache->v_params);
+  p.ws = static_cast<int*>(workspace_dev);
+  p.status = cache->status;
+  RUN(launch_kv4_evict(p, cache->head_dim, cache->group, sms, static_cast<cudaStream_t>(cuda_stream)));
   return GC_OK;
 }
 

@@ -199,6 +199,13 @@ __device__ __forceinline__ int sequence_at(const Kv4AttnParams& p, int64_t at, i
   return p.B - 1;
 }
 
+// The logarithm of the sum of a column's exponentials, from its reference (in binades) and the sum relative to it, which carries
+// a factor of 2^64; minus infinity where the column saw nothing.
+__device__ __forceinline__ float log_of_sum(float m, float l) { return l == 0.f ? -INFINITY : (m + (log2f(l) - 64.f)) * 0.693147180559945309f; }
+__device__ __forceinline__ float* lse_of(const Kv4AttnParams& p, int b, int query, int head) {
+  return p.lse + (static_cast<int64_t>(b) * p.n + query) * p.Hq + head;
+}
+
 // Blocks k0 .. k0 + kn of the nb of head hk of sequence b (len tokens), columns of one chunk.  NT: groups of eight columns.
 // SOLO: this warp alone does all of it.
 template <int D, int G, int NT, bool SOLO>
@@ -622,6 +629,7 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
         if (cc >= columns) continue;
         const float r = l[nt][e] == 0.f ? 0.f : 1.0f / l[nt][e];
         const int qi = cc / p.g, hh = cc - qi * p.g;
+        if (p.lse && gr == 0) *lse_of(p, b, qi, hk * p.g + hh) = log_of_sum(64.f - mneg[nt][e], l[nt][e]);
         __nv_bfloat16* dst = p.o + b * p.ob + qi * p.on + static_cast<int64_t>(hk * p.g + hh) * p.oh + gr * (G / 8);
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
@@ -691,6 +699,7 @@ __device__ __forceinline__ void segment(const Kv4AttnParams& p, uint8_t* smem, i
     if (kn == nb) {
       const float r = ll == 0.f ? 0.f : 1.0f / ll;
       const int cc = col0 + col, qi = cc / p.g, hh = cc - qi * p.g;
+      if (p.lse && d == 0) *lse_of(p, b, qi, hk * p.g + hh) = log_of_sum(mm, ll);
       __nv_bfloat16* dst = p.o + b * p.ob + qi * p.on + static_cast<int64_t>(hk * p.g + hh) * p.oh + d;
       *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(a.x * r, a.y * r), pack_bf16(a.z * r, a.w * r));
     } else {
@@ -855,6 +864,7 @@ __global__ void __launch_bounds__(JW == 1 ? 128 : JW * 32) attn_kv4_join_kernel(
   if (!live) return;
   const float r = ll == 0.f ? 0.f : 1.0f / ll;
   const int qi = cc / p.g, hh = cc - qi * p.g;
+  if (p.lse && lane == 0) *lse_of(p, b, qi, hk * p.g + hh) = log_of_sum(mm, ll);
   *reinterpret_cast<uint2*>(p.o + b * p.ob + qi * p.on + static_cast<int64_t>(hk * p.g + hh) * p.oh + lane * 4) =
       make_uint2(pack_bf16(a.x * r, a.y * r), pack_bf16(a.z * r, a.w * r));
 }

@@ -65,6 +65,7 @@ struct Kv4AttnParams {
   const uint8_t* v_codes;
   const uint32_t* v_params;
   float* ws;
+  float* lse;                       // [B, n, Hq], or null
   uint32_t* status;
 };
 // Columns (query, head) one CTA of the kernel for this many columns covers.
@@ -72,6 +73,71 @@ int attn_kv4_cols(int columns);
 // Resident CTAs per SM the split of the work is planned for.
 int attn_kv4_resident(int head_dim, int group, int cols);
 cudaError_t launch_attn_kv4(const Kv4AttnParams& p, int head_dim, int group, cudaStream_t s);
+
+// Chunks of new tokens over the cache.
+struct ChunkParams {
+  int B, Hq, Hk, g;
+  int page_shift, max_len;
+  int least, most_items;            // units a CTA takes at least; items per head there can be
+  int64_t q_tokens, num_pages, table_stride;
+  float c;                          // scale * log2(e)
+  const __nv_bfloat16* q;
+  int64_t q_tok, q_head;
+  __nv_bfloat16* o;
+  int64_t o_tok, o_head;
+  const int* cu_q;
+  const int* table;
+  const int* lengths;
+  const uint8_t* k_codes;
+  const uint32_t* k_params;         // one (lo, scale) pair per word
+  const uint8_t* v_codes;
+  const uint32_t* v_params;
+  void* ws;
+  uint32_t* status;
+};
+int64_t attn_chunk_items(int64_t q_tokens, int B, int g);
+int attn_chunk_ctas(int64_t items, int Hk, int max_len, int least, int num_sms);
+size_t attn_chunk_bytes(int D, int ctas, int64_t most_items);
+cudaError_t launch_attn_chunk(const ChunkParams& p, int head_dim, int group, int ctas, cudaStream_t s);
+
+// The attention weight that cached tokens receive.
+struct WeighParams {
+  int B, n, Hq, Hk, g;
+  int page_shift, max_len;
+  int64_t num_pages, table_stride;
+  float c, decay;                   // scale * log2(e)
+  const __nv_bfloat16* q;
+  int64_t qb, qn, qh;
+  const float* lse;                 // [B, n, Hq]
+  const int* table;
+  const int* lengths;
+  const uint8_t* k_codes;
+  const uint32_t* k_params;
+  const float* weights;             // [pages, Hk, page]
+  float* out;
+  uint32_t* status;
+};
+cudaError_t launch_kv4_weigh(const WeighParams& p, int head_dim, int group, int num_sms, cudaStream_t s);
+
+struct EvictParams {
+  int B, Hk, keep, recent;
+  int page_shift, max_len;
+  int in_place, list_len, held_keys;
+  int64_t num_pages, table_stride, out_stride;
+  const int* table;
+  const int* out_table;
+  const int* lengths;
+  int* out_lengths;
+  int* kept;                        // [B, Hk, keep]
+  float* scores;                    // [pages, Hk, page]
+  uint8_t* k_codes;
+  uint32_t* k_params;
+  uint8_t* v_codes;
+  uint32_t* v_params;
+  int* ws;                          // [B, Hk, 2, list_len]
+  uint32_t* status;
+};
+cudaError_t launch_kv4_evict(EvictParams p, int head_dim, int group, int num_sms, cudaStream_t s);
 
 struct PromptParams {
   int B, Hq, Hk, D, causal;

@@ -227,19 +227,49 @@ PyObject* kv4_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (cache, q, block_table, lengths, scale, max_length, out, the cache's four tensors)
+int64_t stride(const at::Tensor& t, int i) { return t.size(i) > 1 ? t.stride(i) : 0; }
+
+// int32 [batch, width] of pages, a row contiguous
+void check_table(const at::Tensor& t, const char* name, int64_t batch, const at::Device& device) {
+  if (t.dim() != 2 || t.scalar_type() != at::kInt || t.size(0) != batch || t.device() != device || (t.size(1) > 1 && t.stride(1) != 1))
+    refuse("%s must be int32 [%lld, width] on %s, its rows contiguous, not %s", name, (long long)batch, device.str().c_str(),
+           shape_of(t).c_str());
+}
+// queries [batch, queries, q_heads, head_dim], the last dimension contiguous
+void check_queries(const at::Tensor& q, const gc_kv4_cache_t* c, const at::Device& device) {
+  if (q.dim() != 4 || q.scalar_type() != at::kBFloat16 || q.device() != device || q.size(3) != c->head_dim || q.stride(3) != 1)
+    refuse("q must be bfloat16 [batch, queries, q_heads, %d] on %s, its last dimension contiguous, not %s", c->head_dim,
+           device.str().c_str(), shape_of(q).c_str());
+}
+// a dense fp32 tensor of the given shape
+float* dense(const at::Tensor& t, const char* name, at::IntArrayRef sizes, const at::Device& device) {
+  if (t.scalar_type() != at::kFloat || t.sizes() != sizes || t.device() != device || !t.is_contiguous()) {
+    std::string want;
+    for (int64_t n : sizes) want += (want.empty() ? "" : ", ") + std::to_string(n);
+    refuse("%s must be a contiguous float32 tensor [%s] on %s, not %s", name, want.c_str(), device.str().c_str(), shape_of(t).c_str());
+  }
+  return static_cast<float*>(t.data_ptr());
+}
+// fp32 [pages, kv_heads, page_size], paged like the cache
+float* paged(const at::Tensor& t, const char* name, const gc_kv4_cache_t* c, const at::Device& device) {
+  return dense(t, name, {c->num_pages, c->kv_heads, c->page_size}, device);
+}
+// the bound of lengths: as given, or what the table has room for
+int32_t longest(PyObject* o, const at::Tensor& table, const gc_kv4_cache_t* c) {
+  return small(given(o) ? whole(o) : table.size(1) * c->page_size, "max_length");
+}
+float scale_of(PyObject* o, const gc_kv4_cache_t* c) {
+  return given(o) ? static_cast<float>(number(o)) : 1.0f / std::sqrt(static_cast<float>(c->head_dim));
+}
+
+// (cache, q, block_table, lengths, scale, max_length, out, lse, the cache's four tensors)
 PyObject* kv4_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 8, [&]() -> PyObject* {
-    const gc_kv4_cache_t* c = cache_at(a[0], a[7]);
+  return guarded(n, 9, [&]() -> PyObject* {
+    const gc_kv4_cache_t* c = cache_at(a[0], a[8]);
     const at::Tensor &q = tensor(a[1], "q"), &table = tensor(a[2], "block_table"), &lengths = tensor(a[3], "lengths");
     const at::Device device = device_of(c);
-    if (q.dim() != 4 || q.scalar_type() != at::kBFloat16 || q.device() != device || q.size(3) != c->head_dim || q.stride(3) != 1)
-      refuse("q must be bfloat16 [batch, queries, q_heads, %d] on %s, its last dimension contiguous, not %s", c->head_dim,
-             device.str().c_str(), shape_of(q).c_str());
-    if (table.dim() != 2 || table.scalar_type() != at::kInt || table.size(0) != q.size(0) || table.device() != device ||
-        (table.size(1) > 1 && table.stride(1) != 1))
-      refuse("block_table must be int32 [%lld, width] on %s, its rows contiguous, not %s", (long long)q.size(0), device.str().c_str(),
-             shape_of(table).c_str());
+    check_queries(q, c, device);
+    check_table(table, "block_table", q.size(0), device);
     const at::Tensor out = given(a[6]) ? tensor(a[6], "out") : empty(q.sizes(), at::kBFloat16, device);
     if (given(a[6])) {
       if (out.sizes() != q.sizes() || out.scalar_type() != at::kBFloat16 || out.device() != device || out.stride(3) != 1)
@@ -247,16 +277,14 @@ PyObject* kv4_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
       for (int i = 0; i < 3; ++i)
         if (out.size(i) > 1 && out.stride(i) == 0) refuse("out: an output cannot be an expanded tensor");
     }
-    auto stride = [](const at::Tensor& t, int i) { return t.size(i) > 1 ? t.stride(i) : 0; };
     gc_attention_kv4_t d = {};
     d.batch = small(q.size(0), "batch");
     d.queries = small(q.size(1), "queries");
     d.q_heads = small(q.size(2), "q_heads");
     d.table_width = small(table.size(1), "block_table");
     d.table_stride = stride(table, 0);
-    const int64_t bound = static_cast<int64_t>(d.table_width) * c->page_size;
-    d.max_length = small(given(a[5]) ? whole(a[5]) : bound, "max_length");
-    d.scale = given(a[4]) ? static_cast<float>(number(a[4])) : 1.0f / std::sqrt(static_cast<float>(c->head_dim));
+    d.max_length = longest(a[5], table, c);
+    d.scale = scale_of(a[4], c);
     d.q = q.data_ptr();
     d.q_batch_stride = stride(q, 0), d.q_query_stride = stride(q, 1), d.q_head_stride = stride(q, 2);
     d.out = out.data_ptr();
@@ -268,9 +296,122 @@ PyObject* kv4_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
     // from torch's allocator, so that calls on several streams or in several captured graphs never share it
     at::Tensor ws;
     if (need) ws = empty({static_cast<int64_t>(need)}, at::kByte, device);
-    check(gc_attention_kv4(stream_of(c->cuda_device), c, &d, need ? ws.data_ptr() : nullptr, need));
+    if (given(a[7])) {
+      const at::Tensor& lse = tensor(a[7], "lse");
+      float* at = dense(lse, "lse", {d.batch, d.queries, d.q_heads}, device);
+      check(gc_attention_kv4_lse(stream_of(c->cuda_device), c, &d, at, need ? ws.data_ptr() : nullptr, need));
+      written(lse);
+    } else {
+      check(gc_attention_kv4(stream_of(c->cuda_device), c, &d, need ? ws.data_ptr() : nullptr, need));
+    }
     if (given(a[6])) written(out);
     return THPVariable_Wrap(out);
+  });
+}
+
+// (cache, q, cu_q, block_table, lengths, scale, max_length, out, the cache's four tensors)
+PyObject* kv4_attend_chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject* {
+    const gc_kv4_cache_t* c = cache_at(a[0], a[8]);
+    const at::Tensor &q = tensor(a[1], "q"), &cu_q = tensor(a[2], "cu_q"), &table = tensor(a[3], "block_table"), &lengths = tensor(a[4], "lengths");
+    const at::Device device = device_of(c);
+    if (q.dim() != 3) refuse("q must be [tokens, q_heads, head_dim]");
+    if (cu_q.dim() != 1 || cu_q.size(0) < 1) refuse("cu_q must be a vector of batch + 1 offsets");
+    gc_attention_kv4_chunk_t d = {};
+    d.batch = small(cu_q.size(0) - 1, "cu_q");
+    d.q_heads = small(q.size(1), "q");
+    d.q_tokens = q.size(0);
+    check_table(table, "block_table", d.batch, device);
+    d.table_width = small(table.size(1), "block_table");
+    d.table_stride = stride(table, 0);
+    d.scale = scale_of(a[5], c);
+    d.max_length = longest(a[6], table, c);
+    d.q = heads(q, "q", d.q_tokens, d.q_heads, c->head_dim, at::kBFloat16, device, false);
+    const at::Tensor& out = tensor(a[7], "out");
+    d.out = heads(out, "out", d.q_tokens, d.q_heads, c->head_dim, at::kBFloat16, device, true);
+    d.cu_q = static_cast<const int32_t*>(vec(cu_q, "cu_q", d.batch + 1LL, at::kInt, device));
+    d.block_table = static_cast<const int32_t*>(table.data_ptr());
+    d.lengths = static_cast<const int32_t*>(vec(lengths, "lengths", d.batch, at::kInt, device));
+    size_t need = 0;
+    check(gc_attention_kv4_chunk_workspace_bytes(c, &d, &need));
+    at::Tensor ws;
+    if (need) ws = empty({static_cast<int64_t>(need)}, at::kByte, device);
+    check(gc_attention_kv4_chunk(stream_of(c->cuda_device), c, &d, need ? ws.data_ptr() : nullptr, need));
+    written(out);
+    return Py_NewRef(a[7]);
+  });
+}
+
+// (cache, weights, q, lse, block_table, lengths, scale, max_length, decay, out, the cache's four tensors)
+PyObject* kv4_weigh(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 11, [&]() -> PyObject* {
+    const gc_kv4_cache_t* c = cache_at(a[0], a[10]);
+    const at::Tensor &weights = tensor(a[1], "weights"), &q = tensor(a[2], "q"), &lse = tensor(a[3], "lse"), &table = tensor(a[4], "block_table"),
+                     &lengths = tensor(a[5], "lengths");
+    const at::Tensor& out = given(a[9]) ? tensor(a[9], "out") : weights;
+    const at::Device device = device_of(c);
+    check_queries(q, c, device);
+    check_table(table, "block_table", q.size(0), device);
+    gc_kv4_weigh_t d = {};
+    d.batch = small(q.size(0), "batch");
+    d.queries = small(q.size(1), "queries");
+    d.q_heads = small(q.size(2), "q_heads");
+    d.table_width = small(table.size(1), "block_table");
+    d.table_stride = stride(table, 0);
+    d.scale = scale_of(a[6], c);
+    d.max_length = longest(a[7], table, c);
+    d.decay = static_cast<float>(number(a[8]));
+    d.q = q.data_ptr();
+    d.q_batch_stride = stride(q, 0), d.q_query_stride = stride(q, 1), d.q_head_stride = stride(q, 2);
+    d.lse = dense(lse, "lse", {d.batch, d.queries, d.q_heads}, device);
+    d.block_table = static_cast<const int32_t*>(table.data_ptr());
+    d.lengths = static_cast<const int32_t*>(vec(lengths, "lengths", d.batch, at::kInt, device));
+    d.weights = paged(weights, "weights", c, device);
+    d.out = paged(out, "out", c, device);
+    check(gc_kv4_weigh(stream_of(c->cuda_device), c, &d));
+    written(out);
+    return Py_NewRef(given(a[9]) ? a[9] : a[1]);
+  });
+}
+
+// (cache, scores, block_table, lengths, keep, recent, max_length, out_table, the cache's four tensors)
+PyObject* kv4_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject* {
+    const gc_kv4_cache_t* c = cache_at(a[0], a[8]);
+    const at::Tensor &scores = tensor(a[1], "scores"), &table = tensor(a[2], "block_table"), &lengths = tensor(a[3], "lengths");
+    const at::Device device = device_of(c);
+    if (lengths.dim() != 1) refuse("lengths must be a vector");
+    gc_kv4_evict_t d = {};
+    d.batch = small(lengths.size(0), "lengths");
+    check_table(table, "block_table", d.batch, device);
+    d.table_width = small(table.size(1), "block_table");
+    d.table_stride = stride(table, 0);
+    d.keep = small(whole(a[4]), "keep");
+    d.recent = small(whole(a[5]), "recent");
+    d.max_length = longest(a[6], table, c);
+    d.block_table = static_cast<const int32_t*>(table.data_ptr());
+    d.lengths = static_cast<const int32_t*>(vec(lengths, "lengths", d.batch, at::kInt, device));
+    d.scores = paged(scores, "scores", c, device);
+    if (given(a[7])) {
+      const at::Tensor& to = tensor(a[7], "out_table");
+      check_table(to, "out_table", d.batch, device);
+      d.out_table_width = small(to.size(1), "out_table");
+      d.out_table_stride = stride(to, 0);
+      d.out_table = static_cast<const int32_t*>(to.data_ptr());
+      if (!d.out_table && d.batch) refuse("out_table has no pages");
+    }
+    size_t need = 0;
+    check(gc_kv4_evict_workspace_bytes(c, &d, &need));
+    const at::Tensor out = empty({d.batch}, at::kInt, device), kept = empty({d.batch, c->kv_heads, d.keep}, at::kInt, device);
+    d.out_lengths = static_cast<int32_t*>(out.data_ptr());
+    d.kept = static_cast<int32_t*>(kept.data_ptr());
+    at::Tensor ws;
+    if (need) ws = empty({static_cast<int64_t>(need)}, at::kByte, device);
+    check(gc_kv4_evict(stream_of(c->cuda_device), c, &d, need ? ws.data_ptr() : nullptr, need));
+    written(scores);
+    written(a[8]);
+    THPObjectPtr x(THPVariable_Wrap(out)), y(THPVariable_Wrap(kept));
+    return x && y ? PyTuple_Pack(2, x.get(), y.get()) : nullptr;
   });
 }
 
@@ -313,6 +454,7 @@ PyObject* set_error_class(PyObject*, PyObject* cls) {
 
 #define FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(qk_norm_rope), FAST(kv4_append), FAST(kv4_read), FAST(kv4_attend), FAST(attention_prompt),
+                         FAST(kv4_attend_chunk), FAST(kv4_weigh), FAST(kv4_evict),
                          {"set_error_class", set_error_class, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_serving", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

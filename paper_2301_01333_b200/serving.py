@@ -176,14 +176,53 @@ class KV4Cache:
         return k_out, v_out
 
     def attend(self, q: torch.Tensor, block_table: torch.Tensor, lengths: torch.Tensor, *, scale: Optional[float] = None,
-               max_length: Optional[int] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+               max_length: Optional[int] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of q bf16 [batch, queries, q_heads, head_dim] over the sequences block_table (int32 [batch, width], pages in
         order) names, lengths (int32 [batch]) counting the tokens appended so far, the queries' own among them: query j sees
         the first lengths - (queries - 1) + j of them.  scale: head_dim ** -0.5 if not given; max_length: a bound of lengths the
         caller knows (the work is laid out for it; a longer sequence is an error), width * page_size if not given.  A value above 2^32
         or a score above 2^26 in size, more than the sums and weights can hold, is reported by ``query_status()``; values below
-        2^-40 lose accuracy."""
-        return _serving.kv4_attend(self._at, q, block_table, lengths, scale, max_length, out, self._tensors)
+        2^-40 lose accuracy.  lse: fp32 [batch, queries, q_heads], dense, receives the logarithm of every row's sum of exponentials
+        (minus infinity where a row sees nothing), for ``weigh``."""
+        return _serving.kv4_attend(self._at, q, block_table, lengths, scale, max_length, out, lse, self._tensors)
+
+    def attend_chunk(self, q: torch.Tensor, cu_q: torch.Tensor, block_table: torch.Tensor, lengths: torch.Tensor, *,
+                     scale: Optional[float] = None, max_length: Optional[int] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of any number of new tokens per sequence, packed: q bf16 [q_tokens, q_heads, head_dim], of which sequence b owns rows
+        cu_q[b] .. cu_q[b + 1] (int32 [batch + 1]; none, one or thousands).  Their keys and values have been appended, and
+        lengths[b] counts them: row i of nq sees the first lengths[b] - nq + 1 + i tokens.  block_table, lengths, scale and max_length as
+        for ``attend``.  Keys and values are what ``read`` gives in bf16.  A row that sees nothing is zero; rows no sequence owns
+        are left as they were in a given `out`, and are zero in one made here."""
+        if not isinstance(q, torch.Tensor):
+            raise TypeError("q must be a torch.Tensor")
+        if out is None:
+            out = torch.zeros(q.shape, dtype=torch.bfloat16, device=self.device)
+        return _serving.kv4_attend_chunk(self._at, q, cu_q, block_table, lengths, scale, max_length, out, self._tensors)
+
+    def new_weights(self) -> torch.Tensor:
+        """Zeros, fp32 [pages, kv_heads, page_size], paged like the cache: what ``weigh`` adds to and ``evict`` goes by."""
+        return torch.zeros((self.pages, self.kv_heads, self.page_size), dtype=torch.float32, device=self.device)
+
+    def weigh(self, weights: torch.Tensor, q: torch.Tensor, lse: torch.Tensor, block_table: torch.Tensor, lengths: torch.Tensor, *,
+              scale: Optional[float] = None, max_length: Optional[int] = None, decay: float = 1.0,
+              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Adds to `weights` (``new_weights``) the attention weight every cached token receives from q, summed over the queries that see
+        it and the query heads that share its key/value head: decay * weights + sum of exp(scale * q . k - lse), at the tokens of
+        the sequences; written to `out` where that is given, which may be left as it is elsewhere.  q, block_table, lengths, scale and
+        max_length are those of the ``attend`` call that gave lse.  decay 0: what `weights` holds is not looked at.  A
+        page may be named by one sequence of a call only.  Returns the tensor written."""
+        return _serving.kv4_weigh(self._at, weights, q, lse, block_table, lengths, scale, max_length, decay, out, self._tensors)
+
+    def evict(self, scores: torch.Tensor, block_table: torch.Tensor, lengths: torch.Tensor, keep: int, recent: int = 0, *,
+              max_length: Optional[int] = None, out_table: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Keeps `keep` tokens of every longer sequence, for each key/value head its own: the newest `recent`, and of the others those
+        with the largest scores (fp32, like ``new_weights``; equal ones: the older; NaN counts as largest).  Kept tokens at positions below `keep` stay
+        where they are, the holes between them are filled in order with the kept ones from behind.  In place (pages behind the new
+        lengths are free then), or, with out_table (int32 [batch, width], pages not in block_table), as copies in other pages, with block_table's
+        left as they were.  Scores move along; those of positions given up in place, and of the rest of a copy's last page, are zero.  Returns the
+        new lengths (int32 [batch]) and kept, int32 [batch, kv_heads, keep]: where the token at each position was before, -1 behind a
+        sequence.  A page may be named by one sequence of a call only, except that block_table's may be shared where out_table is given."""
+        return _serving.kv4_evict(self._at, scores, block_table, lengths, keep, recent, max_length, out_table, self._tensors)
 
     def query_status(self) -> None:
         """Synchronise the current stream; raise GcError if a call found a slot, page or length out of bounds since the last one."""
