@@ -385,11 +385,12 @@ gc_status_t gc_attention_kv4_lse(void* cuda_stream, const gc_kv4_cache_t* cache,
  * any number; its new tokens' keys and values have been appended and lengths[b] counts them:
  *   out[i, h] = softmax_t(scale * q[i, h] . K[t]) V over the cached tokens t < lengths[b] - nq + 1 + (i - cu_q[b])
  * A row that sees nothing (more new tokens than length) is zero; rows no sequence owns are left as they were.  q, out bf16, rows 16-byte
- * aligned.  K and V are the values held rounded to bf16, as gc_kv4_read gives them (half a bf16 step each; gc_attention_kv4 does
- * without); scores, statistics and sums fp32, probabilities rounded to bf16.  block_table, max_length: as for gc_attention_kv4, and
- * so is what the status word reports (values above 2^32, scores above 2^26 in size, pages and lengths out of bounds), offsets that
+ * aligned.  Products of fp16 operands summed in fp32: K and V are the values held rounded to fp16, which may not exceed 65504 in size (that is
+ * recorded in the status word; below 2^-14 they lose relative accuracy), elements of q keep an absolute 2^-40 of their row's largest, and
+ * probabilities are rounded to fp16.  block_table, max_length: as for gc_attention_kv4, and so is what else the status
+ * word reports (scores above 2^26 in size, pages and lengths out of bounds), offsets that
  * decrease or leave the packed tokens besides.  What a row does not see has no influence on it, whatever is held there; a
- * group of values that is not finite counts as NaN.  Sequences may share pages. */
+ * group that is not finite counts as NaN.  Sequences may share pages. */
 typedef struct {
   int32_t batch, q_heads;
   int64_t q_tokens;              /* rows of q / out in all */

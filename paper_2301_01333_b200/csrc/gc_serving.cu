@@ -524,6 +524,7 @@ extern "C" gc_status_t gc_serving_status(void* cuda_stream, uint32_t* status_dev
     case DEV_BAD_OFFSETS: return gc_set_error(GC_ERR_INVALID_ARG, "sequence offsets decrease or leave the packed tokens");
     case DEV_LARGE_VALUE: return gc_set_error(GC_ERR_INVALID_ARG, "a value in the cache exceeds 2^32 in size, more than attention over it can sum");
     case DEV_LARGE_SCORE: return gc_set_error(GC_ERR_INVALID_ARG, "an attention score exceeds 2^26 in size, more than its weights can be taken from");
+    case DEV_LARGE_HALF: return gc_set_error(GC_ERR_INVALID_ARG, "a key or value in the cache exceeds 65504 in size, more than attention of chunks takes");
     default: break;
   }
   REFUSE(GC_ERR_TIMEOUT, "a device-side wait expired (code 0x%x)", word);

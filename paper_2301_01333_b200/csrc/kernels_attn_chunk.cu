@@ -1,14 +1,17 @@
 // Attention of chunks of new tokens over the paged 4-bit cache: any number of query rows per sequence, packed one behind the other.
 //
-//   O = softmax(scale Q K^T) V, blockwise over 128 keys with a running reference, as in the prompt attention; K, V = lo + code * scale,
-//   rounded to bf16 once (what reading the cache in bf16 gives) for tcgen05 products with fp32 accumulators.
+//   O = softmax(scale Q K^T) V, blockwise over 128 keys with a running reference, as in the prompt attention, K, V = lo + code * scale
+//
+// The products are tcgen05's with fp32 accumulators and fp16 operands: K, V and the probabilities are rounded once, to eleven bits.  (In bf16 the
+// rounding of K alone puts the output off by 3-5e-3 of its norm, which is mostly cancellation, where the output's own rounding is 1.7e-3.)  Q, bf16,
+// becomes fp16 exactly after its row is scaled by a power of two; probabilities, at most 2^4 relative to the reference, are lifted by 2^11.
 //
 // A row is a (token, query head) of those that share a key/value head, token by token, so that a block of keys, once widened, serves
 // all of them.  A CTA holds 256 rows in two tiles of 128, and per block of 128 keys at width 128 there are
 // two products of 512 clocks for each tile (2048 in all), as many clocks of exponentials (16 a clock), and 32768 elements to be
-// widened: 4.2 instructions for two of them, 540 of the 2048 issue slots of a scheduler.
+// widened: 3.4 instructions for two of them, 440 of the 2048 issue slots of a scheduler.
 //   warps 0-3, 4-7   softmax of tile 0 / 1, one row per thread (as in the prompt attention)
-//   warps 8-11       widen: a thread per key row; codes come from global memory into registers a block ahead, and go as bf16 into
+//   warps 8-11       widen: a thread per key row; codes come from global memory into registers a block ahead, and go as fp16 into
 //                    128-byte-swizzled tiles of a ring, where a thread's row makes the store free of bank conflicts.  The eight elements of a word come
 //                    apart as (0,4), (1,5), (2,6), (3,7) and stay in that order: Q's elements are put in the same one, and
 //                    the columns of O are put back in registers at the end.
@@ -20,6 +23,8 @@
 // takes an equal stretch; the pieces of an item that stretches cut are joined in their order by a second kernel.
 //   * A value that is not finite must not reach rows that do not see it (0 times NaN): such groups are widened as zeros and
 //     noted in a bit mask per block; a row that does see one gets NaN in that group's columns.
+#include <cuda_fp16.h>
+
 #include <atomic>
 
 #include "attn_tc.cuh"
@@ -32,8 +37,9 @@ namespace {
 constexpr int CK_THREADS = 512, CK_ROWS = 256;
 constexpr int CK_MAX_LIST = 1024;            // items per head that are listed in shared memory
 constexpr int CK_FLAGS = 8;                  // blocks whose notes of values that are not finite are kept
-constexpr float CK_RAISE = 8.0f;
-constexpr float CK_LARGEST = 0x1p32f;        // middle or scale of a group of values, above which sums could leave fp32
+constexpr float CK_RAISE = 4.0f;             // binades a score may exceed the reference by
+constexpr float CK_LIFT = 11.0f;             // binades the probabilities are lifted by: at most 2^15, and whole down to 2^-25 of the reference
+constexpr float CK_LARGEST = 65504.0f;       // the largest fp16
 // Registers a thread: what the kernel has to be compiled to, and the warpgroups' shares of them (kernels_attn_prompt.cu has the reason).
 constexpr int CK_REGS = 128, CK_REGS_SOFTMAX = 192, CK_REGS_WIDEN = 72, CK_REGS_MMA = 56;
 static_assert(2 * CK_REGS_SOFTMAX + CK_REGS_WIDEN + CK_REGS_MMA <= 4 * CK_REGS, "the warpgroups' shares exceed the launch's registers");
@@ -45,10 +51,33 @@ struct ChunkLayout {
   static constexpr int TILE = NSUB * SUB;        // 128 rows of Q, K or V
   static constexpr int STAGES = D == 64 ? 8 : 4;
   static constexpr int BARS = 2 * STAGES + 14;
-  // Q, ring, list, notes [CK_FLAGS][4 groups][4 words], one word a block that sums them up, sums of the second tile [3][128]
-  static constexpr int LIST = CK_MAX_LIST * 8, NOTES = CK_FLAGS * 16 * 4, ANY = CK_FLAGS * 4, SUMS = 3 * 128 * 4;
-  static constexpr size_t SMEM = 1024 + static_cast<size_t>(2 + STAGES) * TILE + LIST + NOTES + ANY + SUMS + BARS * 8 + 64 * 4;
+  // Q, ring, list, notes [CK_FLAGS][4 groups][4 words], one word a block that sums them up, sums of the second tile [3][128], factors
+  // of the rows [2][256]
+  static constexpr int LIST = CK_MAX_LIST * 8, NOTES = CK_FLAGS * 16 * 4, ANY = CK_FLAGS * 4, SUMS = 3 * 128 * 4, FACTORS = 2 * CK_ROWS * 4;
+  static constexpr size_t SMEM = 1024 + static_cast<size_t>(2 + STAGES) * TILE + LIST + NOTES + ANY + SUMS + FACTORS + BARS * 8 + 64 * 4;
 };
+
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ __half2 half2_of(uint32_t w) { return *reinterpret_cast<const __half2*>(&w); }
+// The parameters (lo, scale) of a group in fp16, lo and scale twice each; false where a value of the group is not finite in fp16
+// (a straight line in the code: its ends are what to look at).
+struct Params16 {
+  uint32_t lo2, scale2;
+};
+__device__ __forceinline__ bool fits_half(uint32_t par, uint32_t* status) {
+  const float lo = __uint_as_float(par << 16), scale = __uint_as_float(par & 0xffff0000u);
+  if (fmaxf(fabsf(lo), fabsf(fmaf(15.f, scale, lo))) <= CK_LARGEST && fabsf(scale) <= CK_LARGEST) return true;      // (the first holds for a NaN too)
+  if (fabsf(lo) < INFINITY && fabsf(scale) < INFINITY) report(status, DEV_LARGE_HALF);
+  return false;
+}
+__device__ __forceinline__ Params16 params16(uint32_t par) {
+  const uint32_t lo = pack_half(__uint_as_float(par << 16), __uint_as_float(par << 16));
+  const uint32_t scale = pack_half(__uint_as_float(par & 0xffff0000u), __uint_as_float(par & 0xffff0000u));
+  return Params16{lo, scale};
+}
 
 // One sequence: its query rows, and the tokens it has cached.
 struct ChunkSeq {
@@ -257,7 +286,8 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
   uint32_t* s_notes = reinterpret_cast<uint32_t*>(s_list + CK_MAX_LIST);        // [CK_FLAGS][4][4]
   uint32_t* s_any = s_notes + CK_FLAGS * 16;                    // [CK_FLAGS], a byte per widening warp
   float* s_second = reinterpret_cast<float*>(s_any + CK_FLAGS); // reference, sum and groups that are not finite of tile 1
-  uint64_t* bars = reinterpret_cast<uint64_t*>(s_second + 3 * 128);
+  float* s_factor = s_second + 3 * 128;                         // [2 segments][256]: c times the power of two a row's scores are short of
+  uint64_t* bars = reinterpret_cast<uint64_t*>(s_factor + 2 * CK_ROWS);
   const uint32_t b0 = smem_u32(bars);
   const uint32_t bar_q_full = b0, bar_q_empty = b0 + 8, bar_s_full = b0 + 16, bar_p_full = b0 + 32, bar_o_full = b0 + 64;
   const uint32_t bar_turn = b0 + 80, bar_second = b0 + 96, bar_joined = b0 + 104, bar_kv_full = b0 + 112, bar_kv_empty = bar_kv_full + 8 * L::STAGES;
@@ -319,16 +349,15 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
     const uint32_t t_lane = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t s_addr = t_lane + t * 128, o_addr = t_lane + 256 + t * 128;
     uint32_t sn = 0, on = 0, jn = 0, block = 0;                 // block: number of the segment's first among all of this CTA's
-    const float c = p.c;
     Seg s;
-    while (!failed && walk.next(s)) {
+    for (uint32_t seg = 0; !failed && walk.next(s); ++seg) {
       const bool twin = s.twin();
       const int my_row = s.row0 + (twin ? row : t * 128 + row);
       const bool mine = my_row < s.row0 + s.rows;
       const int token = mine ? my_row / p.g : 0;
       const int lim = mine ? max(min(s.ahead + token + 1, s.len), 0) : 0;
       const int j_first = twin ? s.j0 + t : s.j0, j_step = twin ? 2 : 1;
-      float m = -INFINITY, l = 0.f;
+      float m = -INFINITY, l = 0.f, c = 0.f;
       uint32_t poison = 0;                                      // groups of columns in which this row saw a value that is not finite
       int seen_blocks = 0;
       for (int j = j_first; j < s.j1; j += j_step) {
@@ -336,6 +365,7 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
         ++sn;
         tc_fence_after();
         uint32_t v[2][64];
+        if (j == j_first) c = s_factor[(seg & 1) * CK_ROWS + (twin ? row : t * 128 + row)];
         tmem_ld64(s_addr, v[0]);
         tmem_ld64(s_addr + 64, v[1]);
         const int left = lim - j * 128;
@@ -388,7 +418,7 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
           }
         }
         ++seen_blocks;
-        const float off = m == -INFINITY ? 0.f : -m * c;
+        const float off = m == -INFINITY ? 0.f : fmaf(-m, c, CK_LIFT);
         const uint64_t c2 = pair2(c, c), off2 = pair2(off, off);
         uint64_t ls[2] = {0, 0};
 #pragma unroll
@@ -401,7 +431,7 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
             e0 = ap_ex2(e0);
             e1 = ap_ex2(e1);
             ls[i & 1] = add2(ls[i & 1], pair2(e0, e1));
-            w[i] = ap_pack(e0, e1);
+            w[i] = pack_half(e0, e1);
           }
           tmem_st32(s_addr + h * 32, w);
           tmem_wait_st();
@@ -510,17 +540,22 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
       *reinterpret_cast<uint4*>(base + (c >> 3) * L::SUB + ((static_cast<uint32_t>(c & 7) << 4) ^ x7)) = make_uint4(w[0], w[1], w[2], w[3]);
     };
     auto widen = [&](uint8_t* base, const uint32_t (&code)[W], const uint32_t (&par)[NG]) {
+      Params16 x[NG];
+#pragma unroll
+      for (int g = 0; g < NG; ++g) x[g] = params16(par[g]);
 #pragma unroll
       for (int i = 0; i < W; ++i) {
-        const uint32_t lo2 = __byte_perm(par[i * 8 / G], 0, 0x1010), sc2 = __byte_perm(par[i * 8 / G], 0, 0x3232);
-        const uint32_t m128 = 0xc300c300u;
+        // a nibble in the low bits of a number from 1024 on, or four bits up in one from 64 on: that plus the code; then the code
+        // times scale plus lo in one rounding
+        const __half2 m1024 = half2_of(0xe400e400u), m64 = half2_of(0xd400d400u), lo2 = half2_of(x[i * 8 / G].lo2), sc2 = half2_of(x[i * 8 / G].scale2);
         uint32_t w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {                            // 128 + code, minus 128, times scale plus lo in one rounding
-          const uint32_t n = ((code[i] >> (4 * e)) & 0x000f000fu) | 0x43004300u;
-          const __nv_bfloat162 d = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&n), *reinterpret_cast<const __nv_bfloat162*>(&m128));
-          const __nv_bfloat162 f = __hfma2(d, *reinterpret_cast<const __nv_bfloat162*>(&sc2), *reinterpret_cast<const __nv_bfloat162*>(&lo2));
-          w[e] = *reinterpret_cast<const uint32_t*>(&f);
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t n = e ? code[i] >> 8 : code[i];
+          const __half2 a = __hfma2(__hadd2(half2_of((n & 0x000f000fu) | 0x64006400u), m1024), sc2, lo2);
+          const __half2 b = __hfma2(__hadd2(half2_of((n & 0x00f000f0u) | 0x54005400u), m64), sc2, lo2);
+          w[2 * e] = *reinterpret_cast<const uint32_t*>(&a);
+          w[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&b);
         }
         put(base, i, w);
       }
@@ -531,7 +566,7 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
       if (lane == 0) mbar_arrive(bar);
     };
     Seg s;
-    while (!failed && walk.next(s)) {
+    for (uint32_t seg = 0; !failed && walk.next(s); ++seg) {
       const int* table = p.table + s.b * p.table_stride;
       // the row of the cache that has token t, or -1
       auto row_of = [&](int t) -> int64_t {
@@ -568,12 +603,33 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
       for (int t = 0; t < (s.twin() ? 1 : 2); ++t) {
         const int my = t * 128 + r, token = (s.row0 + my) / p.g;
         const __nv_bfloat16* src = p.q + static_cast<int64_t>(s.q0 + token) * p.q_tok + static_cast<int64_t>(s.h * p.g + s.row0 + my - token * p.g) * p.q_head;
+        // fp16 after scaling by a power of two: the largest of a row lies in [2^14, 2^15)
+        float top = 0.f;
 #pragma unroll
         for (int i = 0; i < W; ++i) {
           uint4 x = make_uint4(0, 0, 0, 0);
           if (my < s.rows) x = reinterpret_cast<const uint4*>(src)[i];
-          const uint32_t w[4] = {__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632)};
-          put(q_row + t * L::TILE, i, w);
+          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = max3(top, fabsf(__uint_as_float(w[e] << 16)), fabsf(__uint_as_float(w[e] & 0xffff0000u)));
+        }
+        // (rows of zeros and of infinities: e = 0; the factor is applied in two halves, each of which is a normal number)
+        const int ex = static_cast<int>(__float_as_uint(top) >> 23), e = top == 0.f || ex == 255 ? 0 : max(ex, 1) - 141;
+        const float down = __uint_as_float(static_cast<uint32_t>(127 - e / 2) << 23), down2 = __uint_as_float(static_cast<uint32_t>(127 - (e - e / 2)) << 23);
+        s_factor[(seg & 1) * CK_ROWS + my] = p.c * __uint_as_float(static_cast<uint32_t>(127 + e / 2) << 23) * __uint_as_float(static_cast<uint32_t>(127 + e - e / 2) << 23);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          uint4 x = make_uint4(0, 0, 0, 0);
+          if (my < s.rows) x = reinterpret_cast<const uint4*>(src)[i];
+          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+          uint32_t y[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {                          // elements k and k + 4
+            const uint32_t a = w[k >> 1], b = w[2 + (k >> 1)];
+            const float fa = __uint_as_float(k & 1 ? a & 0xffff0000u : a << 16), fb = __uint_as_float(k & 1 ? b & 0xffff0000u : b << 16);
+            y[k] = pack_half(fa * down * down2, fb * down * down2);
+          }
+          put(q_row + t * L::TILE, i, y);
         }
       }
       handed(bar_q_full);
@@ -584,16 +640,16 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
         uint32_t any = 0;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          const float lo = __uint_as_float(vp[g] << 16), scale = __uint_as_float(vp[g] & 0xffff0000u);
-          const float mid = fmaf(7.5f, scale, lo);
-          const bool bad = !(fabsf(lo) < INFINITY && fabsf(scale) < INFINITY);
-          if (!bad && (fabsf(mid) > CK_LARGEST || fabsf(scale) > CK_LARGEST)) report(p.status, DEV_LARGE_VALUE);
+          const bool bad = !fits_half(vp[g], p.status);
           if (bad) vp[g] = 0;
           const uint32_t mask = __ballot_sync(0xffffffffu, bad);
           if (lane == 0) s_notes[slot * 16 + g * 4 + (warp & 3)] = mask;
           any |= mask;
         }
         if (lane == 0) reinterpret_cast<uint8_t*>(s_any + slot)[warp & 3] = any != 0;
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+          if (!fits_half(kp[g], p.status)) kp[g] = 0x7fc07fc0u;  // NaN: so are the scores of who sees it
         {
           const uint32_t st = ring % L::STAGES, use = ring / L::STAGES;
           ++ring;
@@ -615,7 +671,6 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
           ++ring;
           if (!mbar_wait(bar_kv_empty + 8 * st, (use & 1) ^ 1)) failed = true;
           if (__any_sync(0xffffffffu, failed)) { failed = true; break; }
-          // scale 0 and lo 0 where a group is not finite: its codes become zeros
           widen(kv_row + st * L::TILE, vw, vp);
           handed(bar_kv_full + 8 * st);
         }
@@ -631,8 +686,8 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
     if (warp < 14) {
       // ------------------------------------------------------------------ MMA issuers, one per tile
       const int t = warp - 12;
-      const uint32_t idesc_s = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, 128, 128);
-      const uint32_t idesc_o = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, 128, D, 0, 1);
+      const uint32_t idesc_s = make_idesc(ACC_F32, FMT_F16, FMT_F16, 128, 128);
+      const uint32_t idesc_o = make_idesc(ACC_F32, FMT_F16, FMT_F16, 128, D, 0, 1);
       const uint32_t d_s = tmem_base + t * 128, d_o = tmem_base + 256 + t * 128;
       const uint32_t q0_lo = desc_lo(smem_u32(sQ), 16), k_lo = desc_lo(smem_u32(sKV), 16), v_lo = desc_lo(smem_u32(sKV), L::SUB);
       const uint32_t s_full = bar_s_full + 8 * t, p_full = bar_p_full + 16 * t, o_full = bar_o_full + 8 * t;

@@ -15,6 +15,7 @@ enum : uint32_t {
   DEV_BAD_OFFSETS = 0x204,
   DEV_LARGE_VALUE = 0x205,
   DEV_LARGE_SCORE = 0x206,
+  DEV_LARGE_HALF = 0x207,
 };
 
 // Scores times log2(e) above which weights could leave fp32: 2^26 log2(e).  (Exponents are taken relative to a reference rounded to 2^-24
