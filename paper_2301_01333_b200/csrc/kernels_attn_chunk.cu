@@ -11,12 +11,12 @@
 // two products of 512 clocks for each tile (2048 in all), as many clocks of exponentials (16 a clock), and 32768 elements to be
 // widened: 3.4 instructions for two of them, 440 of the 2048 issue slots of a scheduler.
 //   warps 0-3, 4-7   softmax of tile 0 / 1, one row per thread (as in the prompt attention)
-//   warps 8-11       widen: a thread per key row; codes come from global memory into registers a block ahead, and go as fp16 into
-//                    128-byte-swizzled tiles of a ring, where a thread's row makes the store free of bank conflicts.  The eight elements of a word come
-//                    apart as (0,4), (1,5), (2,6), (3,7) and stay in that order: Q's elements are put in the same one, and
+//   warps 8-11       widen: codes and parameters out of staging, as fp16 into 128-byte-swizzled tiles of a ring.  The eight elements of a word
+//                    come apart as (0,4), (1,5), (2,6), (3,7) and stay in that order: Q's elements are put in the same one, and
 //                    the columns of O are put back in registers at the end.
 //   warps 12, 13     MMA issuers of tile 0 / 1, taking turns
 //   warp 14          notes down which pieces of split items this CTA leaves
+//   warp 15          bulk copies of codes and parameters, as they lie in the pages, a block and a half ahead
 // Where an item has at most 128 rows the two tiles are the same rows: they take the even and the odd blocks of keys, and
 // are joined at the end, the one reading the other's O from tensor memory.
 // The work is a row of units (one block of keys of one item; an item is 256 rows of a sequence, times heads), of which every CTA
@@ -25,7 +25,7 @@
 //     noted in a bit mask per block; a row that does see one gets NaN in that group's columns.
 #include <cuda_fp16.h>
 
-#include <atomic>
+#include <type_traits>
 
 #include "attn_tc.cuh"
 #include "ptx.cuh"
@@ -35,26 +35,23 @@ namespace gc {
 
 namespace {
 constexpr int CK_THREADS = 512, CK_ROWS = 256;
-constexpr int CK_MAX_LIST = 1024;            // items per head that are listed in shared memory
+constexpr int CK_MAX_LIST = 192;             // items per head that are listed in shared memory
 constexpr int CK_FLAGS = 8;                  // blocks whose notes of values that are not finite are kept
 constexpr float CK_RAISE = 4.0f;             // binades a score may exceed the reference by
 constexpr float CK_LIFT = 11.0f;             // binades the probabilities are lifted by: at most 2^15, and whole down to 2^-25 of the reference
 constexpr float CK_LARGEST = 65504.0f;       // the largest fp16
-// Registers a thread: what the kernel has to be compiled to, and the warpgroups' shares of them (kernels_attn_prompt.cu has the reason).
-constexpr int CK_REGS = 128, CK_REGS_SOFTMAX = 192, CK_REGS_WIDEN = 72, CK_REGS_MMA = 56;
-static_assert(2 * CK_REGS_SOFTMAX + CK_REGS_WIDEN + CK_REGS_MMA <= 4 * CK_REGS, "the warpgroups' shares exceed the launch's registers");
-
-template <int D>
+template <int D, int G>
 struct ChunkLayout {
   static constexpr int NSUB = (D + 63) / 64;     // 64-element sub-tiles of 128-byte rows
   static constexpr int SUB = 128 * 128;
   static constexpr int TILE = NSUB * SUB;        // 128 rows of Q, K or V
   static constexpr int STAGES = D == 64 ? 8 : 4;
-  static constexpr int BARS = 2 * STAGES + 14;
-  // Q, ring, list, notes [CK_FLAGS][4 groups][4 words], one word a block that sums them up, sums of the second tile [3][128], factors
-  // of the rows [2][256]
-  static constexpr int LIST = CK_MAX_LIST * 8, NOTES = CK_FLAGS * 16 * 4, ANY = CK_FLAGS * 4, SUMS = 3 * 128 * 4, FACTORS = 2 * CK_ROWS * 4;
-  static constexpr size_t SMEM = 1024 + static_cast<size_t>(2 + STAGES) * TILE + LIST + NOTES + ANY + SUMS + FACTORS + BARS * 8 + 64 * 4;
+  // codes and parameters of 128 key rows, K's or V's, as they lie in memory, and how many of these there are
+  static constexpr int NG = D / G, PITCH = D / 2, CODES = 128 * PITCH, STAGED = CODES + 128 * NG * 4, AHEAD = D == 64 ? 8 : 3;
+  static constexpr int BARS = 2 * STAGES + 2 * AHEAD + 14;
+  // Q, ring, staged codes, list, notes [CK_FLAGS][4 groups][4 words], one word a block that sums them up, sums of the second tile [3][128]
+  static constexpr int LIST = CK_MAX_LIST * 8, NOTES = CK_FLAGS * 16 * 4, ANY = CK_FLAGS * 4, SUMS = 3 * 128 * 4;
+  static constexpr size_t SMEM = 1024 + static_cast<size_t>(2 + STAGES) * TILE + AHEAD * STAGED + LIST + NOTES + ANY + SUMS + BARS * 8 + 64 * 4;
 };
 
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
@@ -77,6 +74,24 @@ __device__ __forceinline__ Params16 params16(uint32_t par) {
   const uint32_t lo = pack_half(__uint_as_float(par << 16), __uint_as_float(par << 16));
   const uint32_t scale = pack_half(__uint_as_float(par & 0xffff0000u), __uint_as_float(par & 0xffff0000u));
   return Params16{lo, scale};
+}
+
+// Bulk copy global -> shared of a multiple of 16 bytes, completion counted in bytes on an mbarrier of this CTA.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
 }
 
 // One sequence: its query rows, and the tokens it has cached.
@@ -147,15 +162,18 @@ __device__ __forceinline__ int block_scan(int v, int* s_sums, int* all) {
   return before + incl - v;
 }
 // Makes the list (never more than `most` items: offsets that overlap, an error, could ask for more); returns items and units.
+// s_seq: scratch, one entry a thread.
 template <typename List>
-__device__ int2 make_list(const ChunkParams& p, const List& list, int most, int* s_sums, int* s_first) {
+__device__ int2 make_list(const ChunkParams& p, const List& list, int most, int* s_sums, int4* s_seq) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   int items = 0;
+#pragma unroll 1
   for (int s0 = 0; s0 < p.B; s0 += CK_THREADS) {
-    const int b = s0 + tid;
+    const int b = s0 + tid, here = min(p.B - s0, CK_THREADS);
     int count = 0;
-    if (b < p.B) {
-      const ChunkSeq s = seq_of(p, b);
+    ChunkSeq s = {};
+    if (tid < here) {
+      s = seq_of(p, b);
       count = items_of(p, s);
       if (blockIdx.x == 0) {
         if (p.cu_q[b] != s.q0 || p.cu_q[b + 1] != s.q0 + s.nq) report(p.status, DEV_BAD_OFFSETS);
@@ -164,17 +182,19 @@ __device__ int2 make_list(const ChunkParams& p, const List& list, int most, int*
     }
     int all;
     const int before = block_scan(count, s_sums, &all);
-    s_first[tid] = items + before;
+    s_seq[tid] = make_int4(items + before, s.nq, s.len, count);
     __syncthreads();
-    for (int w = warp; w < CK_THREADS && s0 + w < p.B; w += CK_THREADS / 32) {
-      const ChunkSeq s = seq_of(p, s0 + w);
-      const int n = items_of(p, s), first = s_first[w];
-      for (int i = lane; i < n && first + i < most; i += 32) list.put(first + i, blocks_of(p, s, i), s0 + w, i);
+#pragma unroll 1
+    for (int w = warp; w < here; w += CK_THREADS / 32) {
+      const int4 x = s_seq[w];
+#pragma unroll 1
+      for (int i = lane; i < x.w && x.x + i < most; i += 32) list.put(x.x + i, blocks_of(p, ChunkSeq{0, x.y, x.z}, i), s0 + w, i);
     }
     items = min(items + all, most);
     __syncthreads();
   }
   int units = 0;
+#pragma unroll 1
   for (int e0 = 0; e0 < items; e0 += CK_THREADS) {
     const int e = e0 + tid, cost = e < items ? list.cost(e) : 0;
     int all;
@@ -186,8 +206,17 @@ __device__ int2 make_list(const ChunkParams& p, const List& list, int most, int*
   return make_int2(items, units);
 }
 
+// (A division of 64-bit numbers costs hundreds of clocks, and most are small.)
+__device__ __forceinline__ int64_t quotient(int64_t a, int b) {
+  return (a >> 32) == 0 ? static_cast<int64_t>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
+}
 // Where CTA number c's stretch begins.
-__device__ __forceinline__ int64_t cut(int64_t total, int c, int ctas) { return total / ctas * c + min(static_cast<int64_t>(c), total % ctas); }
+struct Cuts {
+  int64_t each;
+  int rest;
+  __device__ __forceinline__ Cuts(int64_t total, int ctas) : each(quotient(total, ctas)), rest(static_cast<int>(total - each * ctas)) {}
+  __device__ __forceinline__ int64_t at(int c) const { return each * c + min(c, rest); }
+};
 
 // Part of an item: blocks [j0, j1) of its n; a CTA's stretch is a sequence of them.
 struct Seg {
@@ -206,13 +235,17 @@ struct Walk {
   __device__ __forceinline__ Walk(const ChunkParams& p_, const List& l, int items_, int units_, int64_t from, int64_t to)
       : p(p_), list(l), items(items_), units(units_), left(to - from) {
     if (left <= 0) return;
-    h = static_cast<int>(from / units);
-    const int at = static_cast<int>(from - static_cast<int64_t>(h) * units);
-    int lo = 0, hi = items - 1;                                  // the last item that does not begin behind `at`
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (list.get(mid).before <= at) lo = mid;
-      else hi = mid - 1;
+    h = static_cast<int>(quotient(from, units));
+    const int at = static_cast<int>(from - static_cast<int64_t>(h) * units), lane = threadIdx.x & 31;
+    // the last item that does not begin behind `at`, 32 places at a time (whole warps make a walk together)
+    int lo = 0, n = items;
+#pragma unroll 1
+    while (n > 1) {
+      const int step = (n + 31) >> 5, i = lane * step;
+      const uint32_t hit = __ballot_sync(0xffffffffu, i < n && list.get(lo + min(i, n - 1)).before <= at);
+      const int last = __popc(hit) - 1;
+      lo += last * step;
+      n = min(step, n - last * step);
     }
     e = lo;
     j = at - list.get(e).before;
@@ -267,36 +300,39 @@ struct ChunkSpace {
 
 template <int D>
 __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_list_kernel(const __grid_constant__ ChunkParams p, const int ctas) {
-  __shared__ int s_sums[CK_THREADS / 32], s_first[CK_THREADS];
+  __shared__ int s_sums[CK_THREADS / 32];
+  __shared__ int4 s_seq[CK_THREADS];
   wait_for_predecessor();
   int4* list = ChunkSpace<D>(p.ws, ctas).list;
-  const int2 got = make_list(p, ListGlobal{list + 1}, p.most_items, s_sums, s_first);
+  const int2 got = make_list(p, ListGlobal{list + 1}, p.most_items, s_sums, s_seq);
   if (threadIdx.x == 0) list[0] = make_int4(got.x, got.y, 0, 0);
 }
 
 template <int D, int G, typename List>
 __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_constant__ ChunkParams p) {
-  using L = ChunkLayout<D>;
+  using L = ChunkLayout<D, G>;
+  static_assert(L::SMEM <= 232448, "more than an SM's shared memory");
   constexpr int NG = D / G;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sQ = smem;                                           // [2] tiles
   uint8_t* sKV = sQ + 2 * L::TILE;                              // [STAGES] tiles
-  uint2* s_list = reinterpret_cast<uint2*>(sKV + L::STAGES * L::TILE);
+  uint8_t* s_staging = sKV + L::STAGES * L::TILE;
+  uint2* s_list = reinterpret_cast<uint2*>(s_staging + L::AHEAD * L::STAGED);
   uint32_t* s_notes = reinterpret_cast<uint32_t*>(s_list + CK_MAX_LIST);        // [CK_FLAGS][4][4]
   uint32_t* s_any = s_notes + CK_FLAGS * 16;                    // [CK_FLAGS], a byte per widening warp
   float* s_second = reinterpret_cast<float*>(s_any + CK_FLAGS); // reference, sum and groups that are not finite of tile 1
-  float* s_factor = s_second + 3 * 128;                         // [2 segments][256]: c times the power of two a row's scores are short of
-  uint64_t* bars = reinterpret_cast<uint64_t*>(s_factor + 2 * CK_ROWS);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(s_second + 3 * 128);
   const uint32_t b0 = smem_u32(bars);
   const uint32_t bar_q_full = b0, bar_q_empty = b0 + 8, bar_s_full = b0 + 16, bar_p_full = b0 + 32, bar_o_full = b0 + 64;
   const uint32_t bar_turn = b0 + 80, bar_second = b0 + 96, bar_joined = b0 + 104, bar_kv_full = b0 + 112, bar_kv_empty = bar_kv_full + 8 * L::STAGES;
+  const uint32_t bar_code_full = bar_kv_empty + 8 * L::STAGES, bar_code_empty = bar_code_full + 8 * L::AHEAD;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + L::BARS);
   int* s_sums = reinterpret_cast<int*>(tmem_slot + 4);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    mbar_init(bar_q_full, 4);
+    mbar_init(bar_q_full, 8);                                   // the softmax warps
     mbar_init(bar_q_empty, 2);                                  // both tiles' issuers
     mbar_init(bar_second, 4);
     mbar_init(bar_joined, 4);
@@ -309,6 +345,10 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
     for (int i = 0; i < L::STAGES; ++i) {
       mbar_init(bar_kv_full + 8 * i, 4);
       mbar_init(bar_kv_empty + 8 * i, 2);
+    }
+    for (int i = 0; i < L::AHEAD; ++i) {
+      mbar_init(bar_code_full + 8 * i, 1);
+      mbar_init(bar_code_empty + 8 * i, 4);
     }
     fence_mbar_init();
   }
@@ -323,7 +363,7 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
   int2 size;
   if constexpr (std::is_same<List, ListShared>::value) {
     list.at = s_list;
-    size = make_list(p, list, CK_MAX_LIST, s_sums, reinterpret_cast<int*>(sQ));
+    size = make_list(p, list, CK_MAX_LIST, s_sums, reinterpret_cast<int4*>(sQ));
   } else {
     list.at = space.list + 1;
     size = make_int2(space.list[0].x, space.list[0].y);
@@ -335,67 +375,114 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
   // kernel's end, and this one for the columns.
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t tmem_base = *tmem_slot;
-  // Stretches of at least p.least units: fewer CTAs work where there is little to do.
+  // Stretches of at least 2^least_log units: fewer CTAs work where there is little to do.
   const int64_t total = static_cast<int64_t>(size.y) * p.Hk;
-  const int working = static_cast<int>(min(static_cast<int64_t>(ctas), max((total + p.least - 1) / p.least, static_cast<int64_t>(1))));
-  const int me = static_cast<int>(blockIdx.x);
-  Walk<List> walk(p, list, size.x, size.y, me < working ? cut(total, me, working) : 0, me < working ? cut(total, me + 1, working) : 0);
+  const int64_t fill = (total + (1 << p.least_log) - 1) >> p.least_log;
+  const int working = fill < ctas ? max(static_cast<int>(fill), 1) : ctas, me = static_cast<int>(blockIdx.x);
+  const Cuts cuts(total, working);
+  Walk<List> walk(p, list, size.x, size.y, me < working ? cuts.at(me) : 0, me < working ? cuts.at(me + 1) : 0);
 
   bool failed = false;
   if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(CK_REGS_SOFTMAX));
     // ------------------------------------------------------------------ softmax and output
     const int t = warp >> 2, row = tid & 127;
     const uint32_t t_lane = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t s_addr = t_lane + t * 128, o_addr = t_lane + 256 + t * 128;
-    uint32_t sn = 0, on = 0, jn = 0, block = 0;                 // block: number of the segment's first among all of this CTA's
+    uint32_t sn = 0, on = 0, jn = 0, qn = 0, block = 0;                 // block: number of the segment's first among all of this CTA's
     Seg s;
-    for (uint32_t seg = 0; !failed && walk.next(s); ++seg) {
+    while (!failed && walk.next(s)) {
       const bool twin = s.twin();
       const int my_row = s.row0 + (twin ? row : t * 128 + row);
       const bool mine = my_row < s.row0 + s.rows;
       const int token = mine ? my_row / p.g : 0;
       const int lim = mine ? max(min(s.ahead + token + 1, s.len), 0) : 0;
       const int j_first = twin ? s.j0 + t : s.j0, j_step = twin ? 2 : 1;
-      float m = -INFINITY, l = 0.f, c = 0.f;
+      float m = -INFINITY, l = 0.f, factor = 0.f;
       uint32_t poison = 0;                                      // groups of columns in which this row saw a value that is not finite
       int seen_blocks = 0;
-      for (int j = j_first; j < s.j1; j += j_step) {
-        if (!__all_sync(0xffffffffu, mbar_wait(bar_s_full + 8 * t, sn & 1))) { failed = true; break; }
-        ++sn;
-        tc_fence_after();
-        uint32_t v[2][64];
-        if (j == j_first) c = s_factor[(seg & 1) * CK_ROWS + (twin ? row : t * 128 + row)];
-        tmem_ld64(s_addr, v[0]);
-        tmem_ld64(s_addr + 64, v[1]);
-        const int left = lim - j * 128;
-        {
-          // (written before this block's keys were handed over, and not again before all rows have handed over their probabilities)
-          const uint32_t slot = (block + j - s.j0) % CK_FLAGS;
-          if (s_any[slot]) {
+      // ---- Q: fp16 after scaling by a power of two, so that the largest of a row lies in [2^14, 2^15).  A row is read by 16 (at width
+      // 64: 8) neighbouring lanes, the next rows while these are scaled.
+      constexpr int LPR = D == 64 ? 8 : 16, RPI = 32 / LPR, N = 32 / RPI;        // lanes to a row, rows to a load, loads
+      const int lc = lane % LPR, lr = lane / LPR;
+      const int64_t row_at = mine ? static_cast<int64_t>(s.h * p.g + my_row - token * p.g) : -1;      // head of this row
+      if (!__all_sync(0xffffffffu, mma_wait(bar_q_empty, (qn & 1) ^ 1))) { failed = true; break; }
+      ++qn;
+      {
+        const int64_t my_offset = mine ? static_cast<int64_t>(s.q0 + token) * p.q_tok + row_at * p.q_head : -1;
+        uint8_t* tile = sQ + t * L::TILE + (warp & 3) * 32 * 128 + (lc >> 3) * L::SUB;
+        auto read = [&](int i) {
+          const int64_t at = __shfl_sync(0xffffffffu, my_offset, i * RPI + lr);
+          return at >= 0 && lc < D / 8 ? reinterpret_cast<const uint4*>(p.q + at)[lc] : make_uint4(0, 0, 0, 0);
+        };
+        uint4 x = read(0), x1 = read(1);
+#pragma unroll 1
+        for (int i = 0; i < N; ++i) {
+          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+          x = x1;
+          if (i + 2 < N) x1 = read(i + 2);
+          float v[8], top = 0.f;
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
+          for (int e = 0; e < 4; ++e) {
+            v[2 * e] = __uint_as_float(w[e] << 16);
+            v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+            top = max3(top, fabsf(v[2 * e]), fabsf(v[2 * e + 1]));
+          }
 #pragma unroll
-              for (int w = 0; w < 4; ++w) {
-                const int k = left - 32 * w;
-                const uint32_t sees = k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u;
-                if (s_notes[slot * 16 + g * 4 + w] & sees) poison |= 1u << g;
-              }
+          for (int d = LPR / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+          // (rows of zeros and of infinities: as they are; rows below 2^-86 need not keep their eight bits, for their scores are nothing)
+          const int ex = static_cast<int>(__float_as_uint(top) >> 23), e = top == 0.f || ex == 255 ? 0 : max(ex - 141, -100);
+          const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+          const float up = __shfl_sync(0xffffffffu, p.c * __uint_as_float(static_cast<uint32_t>(127 + e) << 23), (lane % RPI) * LPR);
+          if (lane / RPI == i) factor = up;
+          const int r = i * RPI + lr;
+          if (lc < D / 8 && !(twin && t))
+            *reinterpret_cast<uint4*>(tile + r * 128 + (((lc ^ r) & 7) << 4)) =
+                make_uint4(pack_half(v[0] * down, v[4] * down), pack_half(v[1] * down, v[5] * down), pack_half(v[2] * down, v[6] * down), pack_half(v[3] * down, v[7] * down));
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_q_full);
+      }
+      const float c = factor;                                   // c times the power of two this row's scores are short of
+      // What was noted of block j's values, once a product that waited for them is known to be issued; they are overwritten eight blocks
+      // on, when all rows have handed over probabilities made after this look.
+      auto look = [&](int j) {
+        const uint32_t slot = (block + j - s.j0) % CK_FLAGS;
+        if (s_any[slot]) {
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const int k = lim - j * 128 - 32 * w;
+              const uint32_t sees = k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u;
+              if (s_notes[slot * 16 + g * 4 + w] & sees) poison |= 1u << g;
             }
           }
         }
-        if (__any_sync(0xffffffffu, left < 128)) {
+      };
+#pragma unroll 1
+      for (int j = j_first; j < s.j1; j += j_step) {
+        if (!__all_sync(0xffffffffu, mma_wait(bar_s_full + 8 * t, sn & 1))) { failed = true; break; }
+        ++sn;
+        tc_fence_after();
+        const int left = lim - j * 128;
+        if (seen_blocks) look(j - j_step);
+        // Scores are read twice, 32 at a time, for the maximum and for the exponentials: registers for all 128 would be there, but not the
+        // instruction cache for the unrolled code.
+        const bool masked = __any_sync(0xffffffffu, left < 128);
+        uint32_t v[32];
+        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+        for (int k = 0; k < 4; ++k) {
+          tmem_ld32(s_addr + k * 32, v);
+          tmem_wait_ld();
+          if (masked) {
 #pragma unroll
-          for (int i = 0; i < 128; ++i)
-            if (i >= left) v[i >> 6][i & 63] = 0xff800000u;      // minus infinity, whatever the score was
-        }
-        float top[4];
+            for (int i = 0; i < 32; ++i)
+              if (i >= left - k * 32) v[i] = 0xff800000u;        // minus infinity, whatever the score was
+          }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top[i] = max3(__uint_as_float(v[i >> 1][(i & 1) * 32]), __uint_as_float(v[i >> 1][(i & 1) * 32 + 1]), -INFINITY);
-#pragma unroll
-        for (int i = 2; i < 32; i += 2) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) top[k] = max3(top[k], __uint_as_float(v[k >> 1][(k & 1) * 32 + i]), __uint_as_float(v[k >> 1][(k & 1) * 32 + i + 1]));
+          for (int i = 0; i < 32; i += 2) top[i / 2 % 4] = max3(top[i / 2 % 4], __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
         }
         const float mx = max3(max3(top[0], top[1], top[2]), top[3], top[3]);
         if (__any_sync(0xffffffffu, (mx - m) * c > CK_RAISE)) {
@@ -421,35 +508,45 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
         const float off = m == -INFINITY ? 0.f : fmaf(-m, c, CK_LIFT);
         const uint64_t c2 = pair2(c, c), off2 = pair2(off, off);
         uint64_t ls[2] = {0, 0};
+#pragma unroll 1
+        for (int k = 0; k < 4; ++k) {
+          tmem_ld32(s_addr + k * 32, v);
+          tmem_wait_ld();
+          if (masked) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t w[32];
+            for (int i = 0; i < 32; ++i)
+              if (i >= left - k * 32) v[i] = 0xff800000u;
+          }
+          uint32_t w[16];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
+          for (int i = 0; i < 16; ++i) {
             float e0, e1;
-            unpair2(fma2(pair2(__uint_as_float(v[h][2 * i]), __uint_as_float(v[h][2 * i + 1])), c2, off2), &e0, &e1);
+            unpair2(fma2(pair2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), c2, off2), &e0, &e1);
             e0 = ap_ex2(e0);
             e1 = ap_ex2(e1);
             ls[i & 1] = add2(ls[i & 1], pair2(e0, e1));
             w[i] = pack_half(e0, e1);
           }
-          tmem_st32(s_addr + h * 32, w);
-          tmem_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar_p_full + 8 * (2 * t + h));
+          tmem_st16(s_addr + k * 16, w);                         // over scores that have been read
+          if (k & 1) {
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_p_full + 8 * (2 * t + (k >> 1)));
+          }
         }
         float l0, l1;
         unpair2(add2(ls[0], ls[1]), &l0, &l1);
         l += l0 + l1;
       }
       if (failed) break;
-      block += s.j1 - s.j0;
       if (seen_blocks) {
-        if (!__all_sync(0xffffffffu, mbar_wait(bar_o_full + 8 * t, on & 1))) { failed = true; break; }
+        if (!__all_sync(0xffffffffu, mma_wait(bar_o_full + 8 * t, on & 1))) { failed = true; break; }
         ++on;
         tc_fence_after();
+        look(j_first + (seen_blocks - 1) * j_step);
       }
+      block += s.j1 - s.j0;
       float f0 = 1.f, f1 = 0.f;
       bool second = false;                                      // tile 1 has a part of these rows
       if (twin && t == 1) {
@@ -460,13 +557,13 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_second);
-        if (!__all_sync(0xffffffffu, mbar_wait(bar_joined, jn & 1))) { failed = true; break; }
+        if (!__all_sync(0xffffffffu, mma_wait(bar_joined, jn & 1))) { failed = true; break; }
         ++jn;
         tc_fence_after();
         continue;
       }
       if (twin) {
-        if (!__all_sync(0xffffffffu, mbar_wait(bar_second, jn & 1))) { failed = true; break; }
+        if (!__all_sync(0xffffffffu, mma_wait(bar_second, jn & 1))) { failed = true; break; }
         ++jn;
         tc_fence_after();
         second = s.j1 - s.j0 > 1;
@@ -484,7 +581,8 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
       const int64_t piece = 2 * static_cast<int64_t>(me) + (s.j0 == 0);
       const int my_slot = my_row - s.row0;
       float4* po = space.o + piece * (D / 4) * CK_ROWS + my_slot;
-      __nv_bfloat16* dst = p.o + static_cast<int64_t>(s.q0 + token) * p.o_tok + static_cast<int64_t>(s.h * p.g + my_row - token * p.g) * p.o_head;
+      // Rows go out through this warp's own rows of Q, which no product reads any more, in Q's layout.
+      uint8_t* out = sQ + t * L::TILE + (warp & 3) * 32 * 128;
       if (!whole && mine) space.ml[piece * CK_ROWS + my_slot] = make_float2(m == -INFINITY ? -INFINITY : m * c, l);
 #pragma unroll 1
       for (int k = 0; k < D / 32; ++k) {
@@ -504,20 +602,32 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
 #pragma unroll
           for (int i = 0; i < 32; ++i) w[i] = 0x7fffffffu;
         }
-        if (mine) {
+        {
           // back into order: columns 8 i + (0, 4, 1, 5, 2, 6, 3, 7)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float e[8] = {__uint_as_float(w[8 * i]), __uint_as_float(w[8 * i + 2]), __uint_as_float(w[8 * i + 4]), __uint_as_float(w[8 * i + 6]),
                                 __uint_as_float(w[8 * i + 1]), __uint_as_float(w[8 * i + 3]), __uint_as_float(w[8 * i + 5]), __uint_as_float(w[8 * i + 7])};
             if (whole) {
-              reinterpret_cast<uint4*>(dst)[k * 4 + i] = make_uint4(ap_pack(e[0], e[1]), ap_pack(e[2], e[3]), ap_pack(e[4], e[5]), ap_pack(e[6], e[7]));
-            } else {
+              *reinterpret_cast<uint4*>(out + (k >> 1) * L::SUB + lane * 128 + ((((k & 1) * 4 + i) ^ (lane & 7)) << 4)) = make_uint4(ap_pack(e[0], e[1]), ap_pack(e[2], e[3]), ap_pack(e[4], e[5]), ap_pack(e[6], e[7]));
+            } else if (mine) {
               po[(k * 8 + 2 * i) * CK_ROWS] = make_float4(e[0], e[1], e[2], e[3]);
               po[(k * 8 + 2 * i + 1) * CK_ROWS] = make_float4(e[4], e[5], e[6], e[7]);
             }
           }
         }
+      }
+      if (whole) {                                              // as Q was read
+        const int64_t my_offset = mine ? static_cast<int64_t>(s.q0 + token) * p.o_tok + row_at * p.o_head : -1;
+        __syncwarp();
+#pragma unroll 2
+        for (int i = 0; i < N; ++i) {
+          const int r = i * RPI + lr;
+          const int64_t at = __shfl_sync(0xffffffffu, my_offset, r);
+          if (at >= 0 && lc < D / 8)
+            reinterpret_cast<uint4*>(p.o + at)[lc] = *reinterpret_cast<const uint4*>(out + (lc >> 3) * L::SUB + r * 128 + (((lc ^ r) & 7) << 4));
+        }
+        __syncwarp();
       }
       tc_fence_before();
       if (twin) {
@@ -527,162 +637,92 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
     }
     if (failed && lane == 0) report(p.status, DEV_TIMEOUT_EPILOGUE);
   } else if (warp < 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CK_REGS_WIDEN));
     // ------------------------------------------------------------------ widening
-    const int r = tid & 127;                                    // key row of a block, and row of a tile of Q
-    constexpr int W = D / 8;                                    // words of codes in a row
-    const uint32_t x7 = static_cast<uint32_t>(r & 7) << 4;
-    uint8_t* q_row = sQ + r * 128;
-    uint8_t* kv_row = sKV + r * 128;
-    uint32_t ring = 0, qn = 0, block = 0;
-    // 16 bytes of a row, chunk c of it, in a tile
-    auto put = [&](uint8_t* base, int c, const uint32_t (&w)[4]) {
-      *reinterpret_cast<uint4*>(base + (c >> 3) * L::SUB + ((static_cast<uint32_t>(c & 7) << 4) ^ x7)) = make_uint4(w[0], w[1], w[2], w[3]);
-    };
-    auto widen = [&](uint8_t* base, const uint32_t (&code)[W], const uint32_t (&par)[NG]) {
-      Params16 x[NG];
+    // A lane takes 16 bytes of codes (32 elements) of a row at a time, CH times.  At width 128 and 64 eight lanes take two neighbouring chunks
+    // of four rows, so that the four stores of 16 bytes that become of each touch all banks; at 96 a lane takes a row, and the rows' pitch spreads
+    // them.  Round k: 16 rows on, or two chunks on.
+    // (The rounds are a loop: unrolled, this code and the softmax's drive each other out of the instruction cache.)
+    constexpr int CH = D / 32;                                  // 16-byte chunks of codes in a row
+    const int row0 = (warp & 3) * 32 + (D == 96 ? lane : ((lane >> 3) & 3) * 4 + ((lane >> 1) & 3)), chunk0 = D == 96 ? 0 : lane & 1;
+    auto row_of = [&](int k) { return row0 + (D == 96 ? 0 : (k & 1) * 16); };
+    auto chunk_of = [&](int k) { return chunk0 + (D == 96 ? k : (k >> 1) * 2); };
+    const uint32_t code0 = smem_u32(s_staging) + row0 * L::PITCH + chunk0 * 16, par0 = smem_u32(s_staging) + L::CODES + row0 * NG * 4;
+    uint32_t to[4];                                             // of the four stores of a chunk, in the first tile
 #pragma unroll
-      for (int g = 0; g < NG; ++g) x[g] = params16(par[g]);
-#pragma unroll
-      for (int i = 0; i < W; ++i) {
-        // a nibble in the low bits of a number from 1024 on, or four bits up in one from 64 on: that plus the code; then the code
-        // times scale plus lo in one rounding
-        const __half2 m1024 = half2_of(0xe400e400u), m64 = half2_of(0xd400d400u), lo2 = half2_of(x[i * 8 / G].lo2), sc2 = half2_of(x[i * 8 / G].scale2);
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t n = e ? code[i] >> 8 : code[i];
-          const __half2 a = __hfma2(__hadd2(half2_of((n & 0x000f000fu) | 0x64006400u), m1024), sc2, lo2);
-          const __half2 b = __hfma2(__hadd2(half2_of((n & 0x00f000f0u) | 0x54005400u), m64), sc2, lo2);
-          w[2 * e] = *reinterpret_cast<const uint32_t*>(&a);
-          w[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&b);
-        }
-        put(base, i, w);
-      }
-    };
-    auto handed = [&](uint32_t bar) {
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar);
-    };
+    for (int y = 0; y < 4; ++y) to[y] = smem_u32(sKV) + row0 * 128 + (((chunk0 * 4 + y) ^ (row0 & 7)) << 4);
+    uint32_t ring = 0, used = 0, block = 0;
     Seg s;
-    for (uint32_t seg = 0; !failed && walk.next(s); ++seg) {
-      const int* table = p.table + s.b * p.table_stride;
-      // the row of the cache that has token t, or -1
-      auto row_of = [&](int t) -> int64_t {
-        if (t >= s.len) return -1;
-        const int page = table[t >> p.page_shift];
-        if (page < 0 || page >= p.num_pages) {
-          report(p.status, DEV_BAD_PAGE);
-          return -1;
-        }
-        return ((static_cast<int64_t>(page) * p.Hk + s.h) << p.page_shift) + (t & ((1 << p.page_shift) - 1));
-      };
-      auto load = [&](int64_t at, const uint8_t* codes, uint32_t (&w)[W]) {
-#pragma unroll
-        for (int i = 0; i < W / 4; ++i) {
-          uint4 x = make_uint4(0, 0, 0, 0);
-          if (at >= 0) x = *reinterpret_cast<const uint4*>(codes + at * (D / 2) + i * 16);
-          w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
-        }
-      };
-      auto load_par = [&](int64_t at, const uint32_t* par, uint32_t (&w)[NG]) {
-#pragma unroll
-        for (int g = 0; g < NG; ++g) w[g] = at >= 0 ? par[at * NG + g] : 0u;
-      };
-      uint32_t kw[W], vw[W], kp[NG], vp[NG];
-      int64_t at = row_of(s.j0 * 128 + r);
-      load(at, p.k_codes, kw);
-      load_par(at, p.k_params, kp);
-      load_par(at, p.v_params, vp);
-      // ---- Q
-      if (!mbar_wait(bar_q_empty, (qn & 1) ^ 1)) failed = true;
-      if (__any_sync(0xffffffffu, failed)) { failed = true; break; }
-      ++qn;
+    while (!failed && walk.next(s)) {
+      const int halves = 2 * (s.j1 - s.j0);
 #pragma unroll 1
-      for (int t = 0; t < (s.twin() ? 1 : 2); ++t) {
-        const int my = t * 128 + r, token = (s.row0 + my) / p.g;
-        const __nv_bfloat16* src = p.q + static_cast<int64_t>(s.q0 + token) * p.q_tok + static_cast<int64_t>(s.h * p.g + s.row0 + my - token * p.g) * p.q_head;
-        // fp16 after scaling by a power of two: the largest of a row lies in [2^14, 2^15)
-        float top = 0.f;
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-          uint4 x = make_uint4(0, 0, 0, 0);
-          if (my < s.rows) x = reinterpret_cast<const uint4*>(src)[i];
-          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) top = max3(top, fabsf(__uint_as_float(w[e] << 16)), fabsf(__uint_as_float(w[e] & 0xffff0000u)));
-        }
-        // (rows of zeros and of infinities: e = 0; the factor is applied in two halves, each of which is a normal number)
-        const int ex = static_cast<int>(__float_as_uint(top) >> 23), e = top == 0.f || ex == 255 ? 0 : max(ex, 1) - 141;
-        const float down = __uint_as_float(static_cast<uint32_t>(127 - e / 2) << 23), down2 = __uint_as_float(static_cast<uint32_t>(127 - (e - e / 2)) << 23);
-        s_factor[(seg & 1) * CK_ROWS + my] = p.c * __uint_as_float(static_cast<uint32_t>(127 + e / 2) << 23) * __uint_as_float(static_cast<uint32_t>(127 + e - e / 2) << 23);
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-          uint4 x = make_uint4(0, 0, 0, 0);
-          if (my < s.rows) x = reinterpret_cast<const uint4*>(src)[i];
-          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-          uint32_t y[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {                          // elements k and k + 4
-            const uint32_t a = w[k >> 1], b = w[2 + (k >> 1)];
-            const float fa = __uint_as_float(k & 1 ? a & 0xffff0000u : a << 16), fb = __uint_as_float(k & 1 ? b & 0xffff0000u : b << 16);
-            y[k] = pack_half(fa * down * down2, fb * down * down2);
+      for (int i = 0; i < halves; ++i) {                        // K and V in turn
+        const uint32_t stage = used % L::AHEAD, st = ring % L::STAGES;
+        const bool there = mma_wait(bar_code_full + 8 * stage, (used / L::AHEAD) & 1) && mma_wait(bar_kv_empty + 8 * st, ((ring / L::STAGES) & 1) ^ 1);
+        ++used;
+        ++ring;
+        if (!__all_sync(0xffffffffu, there)) { failed = true; break; }
+        const int left = s.len - (s.j0 + (i >> 1)) * 128;        // rows of the sequence from this block on
+        const uint32_t slot = (block + (i >> 1)) % CK_FLAGS;
+        bool any = false;
+        uint4 code = lds128(code0 + stage * L::STAGED);
+        uint32_t par = lds32(par0 + stage * L::STAGED + chunk0 * 32 / G * 4);
+#pragma unroll 1
+        for (int k = 0; k < CH; ++k) {
+          const bool own = row_of(k) < left;                    // behind the sequence: zeros, whatever lies there
+          uint32_t word[4] = {own ? code.x : 0u, own ? code.y : 0u, own ? code.z : 0u, own ? code.w : 0u}, pp = own ? par : 0u;
+          if (k + 1 < CH) {
+            code = lds128(code0 + stage * L::STAGED + (row_of(k + 1) - row0) * L::PITCH + (chunk_of(k + 1) - chunk0) * 16);
+            par = lds32(par0 + stage * L::STAGED + ((row_of(k + 1) - row0) * NG + chunk_of(k + 1) * 32 / G) * 4);
           }
-          put(q_row + t * L::TILE, i, y);
-        }
-      }
-      handed(bar_q_full);
-      // ---- K and V, block by block
-      for (int j = s.j0; j < s.j1; ++j) {
-        const uint32_t slot = (block + j - s.j0) % CK_FLAGS;
-        load(at, p.v_codes, vw);
-        uint32_t any = 0;
+          // lo below 2^15 and scale below 2^11 in size: all values fit; else a closer look
+          const bool close = (pp << 17) >= 0x47000000u << 1 || (pp & 0x7fff0000u) >= 0x45000000u;
+          if (__any_sync(0xffffffffu, close)) {
+            const bool bad = close && !fits_half(pp, p.status);
+            if (__any_sync(0xffffffffu, bad)) {
+              uint32_t* notes = s_notes + slot * 16 + (warp & 3);
+              if ((i & 1) && !any) {
+                if (lane < 4) notes[lane * 4] = 0;
+                __syncwarp();
+              }
+              any = true;
+              if (bad && (i & 1)) atomicOr(notes + chunk_of(k) * 32 / G * 4, 1u << (row_of(k) & 31));
+              // a key becomes NaN, and so do the scores of who sees it; a value zero
+              if (bad) pp = i & 1 ? 0u : 0x7fc07fc0u;
+              __syncwarp();
+            }
+          }
+          const Params16 x = params16(pp);
+          // a nibble in the low bits of a number from 1024 on, or four bits up in one from 64 on: that plus the code; then the code
+          // times scale plus lo in one rounding
+          const __half2 m1024 = half2_of(0xe400e400u), m64 = half2_of(0xd400d400u), lo2 = half2_of(x.lo2), sc2 = half2_of(x.scale2);
+          // (16 rows down: the same place of the swizzle; at width 96 the second chunk of a pair is four 16-byte places away)
+          const uint32_t tile = st * L::TILE + (D == 96 ? 0 : (k & 1) * 16 * 128) + (k >> 1) * L::SUB, flip = D == 96 ? (k & 1) * 64 : 0;
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          const bool bad = !fits_half(vp[g], p.status);
-          if (bad) vp[g] = 0;
-          const uint32_t mask = __ballot_sync(0xffffffffu, bad);
-          if (lane == 0) s_notes[slot * 16 + g * 4 + (warp & 3)] = mask;
-          any |= mask;
-        }
-        if (lane == 0) reinterpret_cast<uint8_t*>(s_any + slot)[warp & 3] = any != 0;
+          for (int y = 0; y < 4; ++y) {
+            uint32_t w[4];
 #pragma unroll
-        for (int g = 0; g < NG; ++g)
-          if (!fits_half(kp[g], p.status)) kp[g] = 0x7fc07fc0u;  // NaN: so are the scores of who sees it
-        {
-          const uint32_t st = ring % L::STAGES, use = ring / L::STAGES;
-          ++ring;
-          if (!mbar_wait(bar_kv_empty + 8 * st, (use & 1) ^ 1)) failed = true;
-          if (__any_sync(0xffffffffu, failed)) { failed = true; break; }
-          widen(kv_row + st * L::TILE, kw, kp);
-          handed(bar_kv_full + 8 * st);
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t n = e ? word[y] >> 8 : word[y];
+              const __half2 a = __hfma2(__hadd2(half2_of((n & 0x000f000fu) | 0x64006400u), m1024), sc2, lo2);
+              const __half2 b = __hfma2(__hadd2(half2_of((n & 0x00f000f0u) | 0x54005400u), m64), sc2, lo2);
+              w[2 * e] = *reinterpret_cast<const uint32_t*>(&a);
+              w[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&b);
+            }
+            sts128((to[y] ^ flip) + tile, w[0], w[1], w[2], w[3]);
+          }
         }
-        int64_t next = -1;
-        uint32_t vp_next[NG];
-        if (j + 1 < s.j1) {
-          next = row_of((j + 1) * 128 + r);
-          load(next, p.k_codes, kw);
-          load_par(next, p.k_params, kp);
+        if ((i & 1) && lane == 0) reinterpret_cast<uint8_t*>(s_any + slot)[warp & 3] = any;
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(bar_code_empty + 8 * stage);
+          mbar_arrive(bar_kv_full + 8 * st);
         }
-        load_par(next, p.v_params, vp_next);
-        {
-          const uint32_t st = ring % L::STAGES, use = ring / L::STAGES;
-          ++ring;
-          if (!mbar_wait(bar_kv_empty + 8 * st, (use & 1) ^ 1)) failed = true;
-          if (__any_sync(0xffffffffu, failed)) { failed = true; break; }
-          widen(kv_row + st * L::TILE, vw, vp);
-          handed(bar_kv_full + 8 * st);
-        }
-        at = next;
-#pragma unroll
-        for (int g = 0; g < NG; ++g) vp[g] = vp_next[g];
       }
       block += s.j1 - s.j0;
     }
     if (failed && lane == 0) report(p.status, DEV_TIMEOUT_PRODUCER);
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CK_REGS_MMA));
     if (warp < 14) {
       // ------------------------------------------------------------------ MMA issuers, one per tile
       const int t = warp - 12;
@@ -697,7 +737,7 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
         if (lane == 0) {
           const bool twin = s.twin();
           const int blocks = s.j1 - s.j0, n = twin ? (blocks + 1 - t) >> 1 : blocks;        // mine
-          const int turns = twin ? (blocks + 1) >> 1 : blocks;   // of each tile, after the first
+          const int turns = twin ? (blocks + 1) >> 1 : blocks;   // batches of each tile, after the first
           const uint32_t step = twin ? 4 : 2, first = ring + (twin ? 2 * t : 0);            // K of my block i: first + step i
           const uint32_t q_lo = q0_lo + (twin ? 0u : t * (L::TILE >> 4));
           auto kv_ready = [&](uint32_t pos) { return mma_wait(bar_kv_full + 8 * (pos % L::STAGES), (pos / L::STAGES) & 1); };
@@ -721,35 +761,36 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
           };
           // Also a tile without blocks of its own waits for Q, so that no issuer gets more than a segment ahead.
           failed = !mma_wait(bar_q_full, qn++ & 1);
-          if (!failed && n) failed = !kv_ready(first);
-          if (!failed) failed = !my_turn();
-          if (!failed) {
-            tc_fence_after();
-            if (n) scores(first);
-            your_turn();
-            if (n == 1) umma_commit(bar_q_empty);
-            if (n == 0) mbar_arrive(bar_q_empty);
-            if (n) kv_done(first);
-          }
-          for (int i = 0; i < n && !failed; ++i) {
+          if (n == 0) mbar_arrive(bar_q_empty);
+          // Batch i: O += P V of my block i, then S of the next one; the first batch has only the scores.
+#pragma unroll 1
+          for (int i = -1; i < n && !failed; ++i) {
             const uint32_t vpos = first + step * i + 1, kpos = first + step * (i + 1);
-            if (!kv_ready(vpos) || (i + 1 < n && !kv_ready(kpos)) || !mma_wait(p_full, pn & 1) || !my_turn()) { failed = true; break; }
+            if (i >= 0 && !(kv_ready(vpos) && mma_wait(p_full, pn & 1))) { failed = true; break; }
+            if (!my_turn()) { failed = true; break; }
             tc_fence_after();
-            const uint32_t vb = v_lo + (vpos % L::STAGES) * (L::TILE >> 4);
-            // 16 keys per product, half of them with each part of P
+            if (i >= 0) {
+              const uint32_t vb = v_lo + (vpos % L::STAGES) * (L::TILE >> 4);
+              // 16 keys per product, half of them with each part of P
 #pragma unroll
-            for (int k = 0; k < 4; ++k) mma_ts(d_o, d_s + k * 8, vb + k * 128, idesc_o, k || i);
-            if (!mma_wait(p_full + 8, pn++ & 1)) { failed = true; break; }
-            tc_fence_after();
+              for (int k = 0; k < 4; ++k) mma_ts(d_o, d_s + k * 8, vb + k * 128, idesc_o, k || i);
+              if (!mma_wait(p_full + 8, pn++ & 1)) { failed = true; break; }
+              tc_fence_after();
 #pragma unroll
-            for (int k = 4; k < 8; ++k) mma_ts(d_o, d_s + k * 8, vb + k * 128, idesc_o, 1);
-            if (i + 1 < n) scores(kpos);
-            else umma_commit(o_full);
+              for (int k = 4; k < 8; ++k) mma_ts(d_o, d_s + k * 8, vb + k * 128, idesc_o, 1);
+              kv_done(vpos);                                     // (before the wait: with twins the next keys may need its place)
+              if (i + 1 == n) umma_commit(o_full);
+            }
+            if (i + 1 < n) {
+              if (!kv_ready(kpos)) { failed = true; break; }
+              tc_fence_after();
+              scores(kpos);
+              kv_done(kpos);
+              if (i + 2 == n) umma_commit(bar_q_empty);
+            }
             your_turn();
-            kv_done(vpos);
-            if (i + 1 < n) kv_done(kpos);
-            if (i + 2 == n) umma_commit(bar_q_empty);
           }
+#pragma unroll 1
           for (int i = n; i < turns && !failed; ++i) {
             failed = !my_turn();
             your_turn();
@@ -773,6 +814,47 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
         }
       }
       if (lane == 0) space.note[me] = note;
+    } else {
+      // ------------------------------------------------------------------ codes and parameters on their way
+      const int piece_shift = min(p.page_shift, 7), pieces = 128 >> piece_shift, piece = 1 << piece_shift;      // of a block's rows in one page
+      uint32_t filled = 0;
+      Seg s;
+      while (!failed && walk.next(s)) {
+        const int* table = p.table + s.b * p.table_stride;
+        // the page that has my piece of block j (the lanes of a block's pieces), and the next block's on its way
+        auto page_of = [&](int j) {
+          const int t = j * 128 + lane * piece;
+          return lane < pieces && j < s.j1 && t < s.len ? table[t >> p.page_shift] : 0;
+        };
+        int next = page_of(s.j0);
+#pragma unroll 1
+        for (int j = s.j0; j < s.j1 && !failed; ++j) {
+          int page = next;
+          next = page_of(j + 1);
+          if (page < 0 || page >= p.num_pages) {
+            report(p.status, DEV_BAD_PAGE);
+            page = 0;
+          }
+          const int t = j * 128 + lane * piece;
+          const bool copies = lane < pieces && t < s.len;
+          const int64_t at = ((static_cast<int64_t>(page) * p.Hk + s.h) << p.page_shift) + (t & ((1 << p.page_shift) - 1));
+          const uint32_t count = static_cast<uint32_t>(min(pieces, max(0, (s.len - j * 128 + piece - 1) >> piece_shift)));
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            const uint32_t stage = filled % L::AHEAD, bar = bar_code_full + 8 * stage, to = smem_u32(s_staging) + stage * L::STAGED;
+            if (!mma_wait(bar_code_empty + 8 * stage, ((filled / L::AHEAD) & 1) ^ 1)) failed = true;
+            if (__any_sync(0xffffffffu, failed)) { failed = true; break; }
+            ++filled;
+            if (lane == 0) mbar_arrive_expect_tx(bar, count * (piece * static_cast<uint32_t>(L::PITCH + NG * 4)));
+            __syncwarp();
+            if (copies) {
+              bulk_load(to + lane * piece * L::PITCH, (v ? p.v_codes : p.k_codes) + at * L::PITCH, piece * L::PITCH, bar);
+              bulk_load(to + L::CODES + lane * piece * (NG * 4), (v ? p.v_params : p.k_params) + at * NG, piece * (NG * 4), bar);
+            }
+          }
+        }
+      }
+      if (failed && lane == 0) report(p.status, DEV_TIMEOUT_PRODUCER);
     }
   }
   if (failed) {                                                  // products in flight come to rest before the block exits
@@ -789,26 +871,38 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
   }
 }
 
-// Joins the pieces of the item that begins in CTA blockIdx.x without ending there: the following CTAs' first pieces, in order.  A
-// thread per row and 16 columns.
+// Joins the pieces of the item that begins in CTA blockIdx.x without ending there with the following CTAs' first pieces.  A block
+// has 32 rows and 32 columns: two warps of 16 columns, for each of them four that take every fourth piece and are then joined
+// in shared memory, all in a fixed order.  (With one thread for all pieces of a row, an item in 74 pieces took 115 us.)
+constexpr int CJ_WAYS = 4;
 template <int D>
-__global__ void __launch_bounds__(CK_ROWS) attn_chunk_join_kernel(const __grid_constant__ ChunkParams p, const int ctas) {
+__global__ void __launch_bounds__(2 * CJ_WAYS * 32) attn_chunk_join_kernel(const __grid_constant__ ChunkParams p, const int ctas) {
+  __shared__ float4 s_o[CJ_WAYS][2][4][32];
+  __shared__ float2 s_ml[CJ_WAYS][2][32];
   wait_for_predecessor();
   const ChunkSpace<D> space(p.ws, ctas);
-  const int c0 = blockIdx.x, row = threadIdx.x, col = blockIdx.y * 16;
+  const int lane = threadIdx.x & 31, way = threadIdx.x >> 6, half = threadIdx.x >> 5 & 1;
+  const int c0 = blockIdx.x, row = blockIdx.y * 32 + lane, col = blockIdx.z * 32 + half * 16;
   const Note note = space.note[c0];
-  if (row >= note.rows) return;
+  if (static_cast<int>(blockIdx.y) * 32 >= note.rows) return;
+  int n = 1;                                                     // pieces: up to the first that reaches the item's end
+  for (int c = c0 + 1;; c += 32) {
+    const uint32_t end = __ballot_sync(0xffffffffu, c + lane >= ctas || space.note[c + lane].ends);
+    n += end ? __ffs(end) : 32;
+    if (end) break;
+  }
+  n = min(n, ctas - c0);
   float m = -INFINITY, l = 0.f;
   float4 a[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) a[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int c = c0; c < ctas; ++c) {
-    const int64_t piece = 2 * static_cast<int64_t>(c) + (c == c0);
+#pragma unroll 2
+  for (int i = way; i < n; i += CJ_WAYS) {
+    const int64_t piece = 2 * static_cast<int64_t>(c0 + i) + (i == 0);
     const float2 x = space.ml[piece * CK_ROWS + row];
     float4 v[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = space.o[(piece * (D / 4) + col / 4 + k) * CK_ROWS + row];
-    const int ends = c == c0 ? 0 : space.note[c].ends;
     const float mn = fmaxf(m, x.x), ref = mn == -INFINITY ? 0.f : mn;
     const float f = ap_ex2(m - ref), g = ap_ex2(x.x - ref);      // 0 for what saw nothing; NaN sums pass
     m = mn;
@@ -820,7 +914,27 @@ __global__ void __launch_bounds__(CK_ROWS) attn_chunk_join_kernel(const __grid_c
       a[k].z = fmaf(a[k].z, f, v[k].z * g);
       a[k].w = fmaf(a[k].w, f, v[k].w * g);
     }
-    if (ends) break;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) s_o[way][half][k][lane] = a[k];
+  s_ml[way][half][lane] = make_float2(m, l);
+  __syncthreads();
+  if (way != 0 || row >= note.rows) return;
+#pragma unroll
+  for (int w = 1; w < CJ_WAYS; ++w) {
+    const float2 x = s_ml[w][half][lane];
+    const float mn = fmaxf(m, x.x), ref = mn == -INFINITY ? 0.f : mn;
+    const float f = ap_ex2(m - ref), g = ap_ex2(x.x - ref);
+    m = mn;
+    l = fmaf(l, f, x.y * g);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float4 v = s_o[w][half][k][lane];
+      a[k].x = fmaf(a[k].x, f, v.x * g);
+      a[k].y = fmaf(a[k].y, f, v.y * g);
+      a[k].z = fmaf(a[k].z, f, v.z * g);
+      a[k].w = fmaf(a[k].w, f, v.w * g);
+    }
   }
   const float r = l == 0.f ? 0.f : 1.0f / l;
   const int my_row = note.row0 + row, token = my_row / p.g;
@@ -835,23 +949,15 @@ namespace {
 template <int D, int G, typename List>
 cudaError_t run(const ChunkParams& p, int ctas, cudaStream_t s) {
   auto kern = attn_chunk_kernel<D, G, List>;
-  static std::atomic<int> regs{0};
-  if (regs.load(std::memory_order_relaxed) == 0) {
-    cudaFuncAttributes a;
-    const cudaError_t e = cudaFuncGetAttributes(&a, kern);
-    if (e != cudaSuccess) return e;
-    regs.store(a.numRegs, std::memory_order_relaxed);
-  }
-  if (regs.load(std::memory_order_relaxed) < CK_REGS) return cudaErrorLaunchOutOfResources;
-  cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), ChunkLayout<D>::SMEM);
+  cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), (ChunkLayout<D, G>::SMEM));
   if (e != cudaSuccess) return e;
   if (!std::is_same<List, ListShared>::value) {
     e = launch_following(attn_chunk_list_kernel<D>, dim3(1), CK_THREADS, 0, s, p, ctas);
     if (e != cudaSuccess) return e;
   }
-  e = launch_following(kern, dim3(static_cast<unsigned>(ctas)), CK_THREADS, ChunkLayout<D>::SMEM, s, p);
+  e = launch_following(kern, dim3(static_cast<unsigned>(ctas)), CK_THREADS, (ChunkLayout<D, G>::SMEM), s, p);
   if (e != cudaSuccess || ctas == 1) return e;
-  return launch_following(attn_chunk_join_kernel<D>, dim3(static_cast<unsigned>(ctas), D / 16), CK_ROWS, 0, s, p, ctas);
+  return launch_following(attn_chunk_join_kernel<D>, dim3(static_cast<unsigned>(ctas), CK_ROWS / 32, D / 32), 2 * CJ_WAYS * 32, 0, s, p, ctas);
 }
 template <int D, int G>
 cudaError_t by_list(const ChunkParams& p, int ctas, cudaStream_t s) {
@@ -863,11 +969,11 @@ size_t space_bytes(int ctas, int64_t most_items) {
 }
 }  // namespace
 
-// Items per head there can be at most (a sequence's last one may be short), and CTAs for them: one an SM, or one for every p.least
-// blocks of keys where that is fewer.
+// Items per head there can be at most (a sequence's last one may be short), and CTAs for them: one an SM, or one for every
+// 2^least_log blocks of keys where that is fewer.
 int64_t attn_chunk_items(int64_t q_tokens, int B, int g) { return q_tokens * g / CK_ROWS + B; }
-int attn_chunk_ctas(int64_t items, int Hk, int max_len, int least, int num_sms) {
-  const int64_t units = items * Hk * ((max_len + 127) / 128 + 1), want = (units + least - 1) / least;
+int attn_chunk_ctas(int64_t items, int Hk, int max_len, int least_log, int num_sms) {
+  const int64_t units = items * Hk * ((max_len + 127) / 128 + 1), want = (units >> least_log) + 1;
   return static_cast<int>(want < num_sms ? want : num_sms);
 }
 size_t attn_chunk_bytes(int D, int ctas, int64_t most_items) {
