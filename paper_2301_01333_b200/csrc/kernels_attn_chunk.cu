@@ -35,7 +35,7 @@ namespace gc {
 
 namespace {
 constexpr int CK_THREADS = 512, CK_ROWS = 256;
-constexpr int CK_MAX_LIST = 192;             // items per head that are listed in shared memory
+constexpr int CK_MAX_LIST = 160;             // items per head that are listed in shared memory
 constexpr int CK_FLAGS = 8;                  // blocks whose notes of values that are not finite are kept
 constexpr float CK_RAISE = 4.0f;             // binades a score may exceed the reference by
 constexpr float CK_LIFT = 11.0f;             // binades the probabilities are lifted by: at most 2^15, and whole down to 2^-25 of the reference
@@ -48,7 +48,7 @@ struct ChunkLayout {
   static constexpr int STAGES = D == 64 ? 8 : 4;
   // codes and parameters of 128 key rows, K's or V's, as they lie in memory, and how many of these there are
   static constexpr int NG = D / G, PITCH = D / 2, CODES = 128 * PITCH, STAGED = CODES + 128 * NG * 4, AHEAD = D == 64 ? 8 : 3;
-  static constexpr int BARS = 2 * STAGES + 2 * AHEAD + 14;
+  static constexpr int BARS = 2 * STAGES + 2 * AHEAD + 16;
   // Q, ring, staged codes, list, notes [CK_FLAGS][4 groups][4 words], one word a block that sums them up, sums of the second tile [3][128]
   static constexpr int LIST = CK_MAX_LIST * 8, NOTES = CK_FLAGS * 16 * 4, ANY = CK_FLAGS * 4, SUMS = 3 * 128 * 4;
   static constexpr size_t SMEM = 1024 + static_cast<size_t>(2 + STAGES) * TILE + AHEAD * STAGED + LIST + NOTES + ANY + SUMS + BARS * 8 + 64 * 4;
@@ -324,8 +324,8 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
   float* s_second = reinterpret_cast<float*>(s_any + CK_FLAGS); // reference, sum and groups that are not finite of tile 1
   uint64_t* bars = reinterpret_cast<uint64_t*>(s_second + 3 * 128);
   const uint32_t b0 = smem_u32(bars);
-  const uint32_t bar_q_full = b0, bar_q_empty = b0 + 8, bar_s_full = b0 + 16, bar_p_full = b0 + 32, bar_o_full = b0 + 64;
-  const uint32_t bar_turn = b0 + 80, bar_second = b0 + 96, bar_joined = b0 + 104, bar_kv_full = b0 + 112, bar_kv_empty = bar_kv_full + 8 * L::STAGES;
+  const uint32_t bar_q_full = b0, bar_q_empty = b0 + 8, bar_s_full = b0 + 16, bar_p_full = b0 + 48, bar_o_full = b0 + 80;
+  const uint32_t bar_second = b0 + 112, bar_joined = b0 + 120, bar_kv_full = b0 + 128, bar_kv_empty = bar_kv_full + 8 * L::STAGES;
   const uint32_t bar_code_full = bar_kv_empty + 8 * L::STAGES, bar_code_empty = bar_code_full + 8 * L::AHEAD;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + L::BARS);
   int* s_sums = reinterpret_cast<int*>(tmem_slot + 4);
@@ -336,12 +336,11 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
     mbar_init(bar_q_empty, 2);                                  // both tiles' issuers
     mbar_init(bar_second, 4);
     mbar_init(bar_joined, 4);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
       mbar_init(bar_s_full + 8 * i, 1);
       mbar_init(bar_o_full + 8 * i, 1);
-      mbar_init(bar_turn + 8 * i, 1);
+      mbar_init(bar_p_full + 8 * i, 4);
     }
-    for (int i = 0; i < 4; ++i) mbar_init(bar_p_full + 8 * i, 4);
     for (int i = 0; i < L::STAGES; ++i) {
       mbar_init(bar_kv_full + 8 * i, 4);
       mbar_init(bar_kv_empty + 8 * i, 2);
@@ -388,7 +387,7 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
     const int t = warp >> 2, row = tid & 127;
     const uint32_t t_lane = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t s_addr = t_lane + t * 128, o_addr = t_lane + 256 + t * 128;
-    uint32_t sn = 0, on = 0, jn = 0, qn = 0, block = 0;                 // block: number of the segment's first among all of this CTA's
+    uint32_t sn = 0, jn = 0, qn = 0, block = 0;                 // block: number of the segment's first among all of this CTA's
     Seg s;
     while (!failed && walk.next(s)) {
       const bool twin = s.twin();
@@ -410,34 +409,44 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
       {
         const int64_t my_offset = mine ? static_cast<int64_t>(s.q0 + token) * p.q_tok + row_at * p.q_head : -1;
         uint8_t* tile = sQ + t * L::TILE + (warp & 3) * 32 * 128 + (lc >> 3) * L::SUB;
+        constexpr int FLY = 4;
         auto read = [&](int i) {
           const int64_t at = __shfl_sync(0xffffffffu, my_offset, i * RPI + lr);
           return at >= 0 && lc < D / 8 ? reinterpret_cast<const uint4*>(p.q + at)[lc] : make_uint4(0, 0, 0, 0);
         };
-        uint4 x = read(0), x1 = read(1);
-#pragma unroll 1
-        for (int i = 0; i < N; ++i) {
-          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-          x = x1;
-          if (i + 2 < N) x1 = read(i + 2);
-          float v[8], top = 0.f;
+        uint4 x[FLY], next[FLY];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            v[2 * e] = __uint_as_float(w[e] << 16);
-            v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-            top = max3(top, fabsf(v[2 * e]), fabsf(v[2 * e + 1]));
+        for (int f = 0; f < FLY; ++f) next[f] = read(f);
+#pragma unroll 1
+        for (int i0 = 0; i0 < N; i0 += FLY) {
+#pragma unroll
+          for (int f = 0; f < FLY; ++f) x[f] = next[f];
+          if (i0 + FLY < N) {
+#pragma unroll
+            for (int f = 0; f < FLY; ++f) next[f] = read(i0 + FLY + f);
           }
 #pragma unroll
-          for (int d = LPR / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-          // (rows of zeros and of infinities: as they are; rows below 2^-86 need not keep their eight bits, for their scores are nothing)
-          const int ex = static_cast<int>(__float_as_uint(top) >> 23), e = top == 0.f || ex == 255 ? 0 : max(ex - 141, -100);
-          const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-          const float up = __shfl_sync(0xffffffffu, p.c * __uint_as_float(static_cast<uint32_t>(127 + e) << 23), (lane % RPI) * LPR);
-          if (lane / RPI == i) factor = up;
-          const int r = i * RPI + lr;
-          if (lc < D / 8 && !(twin && t))
-            *reinterpret_cast<uint4*>(tile + r * 128 + (((lc ^ r) & 7) << 4)) =
-                make_uint4(pack_half(v[0] * down, v[4] * down), pack_half(v[1] * down, v[5] * down), pack_half(v[2] * down, v[6] * down), pack_half(v[3] * down, v[7] * down));
+          for (int f = 0; f < FLY; ++f) {
+            const uint32_t w[4] = {x[f].x, x[f].y, x[f].z, x[f].w};
+            float v[8], top = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              v[2 * e] = __uint_as_float(w[e] << 16);
+              v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+              top = max3(top, fabsf(v[2 * e]), fabsf(v[2 * e + 1]));
+            }
+#pragma unroll
+            for (int d = LPR / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            // (rows of zeros and of infinities: as they are; rows below 2^-86 need not keep their eight bits, for their scores are nothing)
+            const int ex = static_cast<int>(__float_as_uint(top) >> 23), e = top == 0.f || ex == 255 ? 0 : max(ex - 141, -100);
+            const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+            const float up = __shfl_sync(0xffffffffu, p.c * __uint_as_float(static_cast<uint32_t>(127 + e) << 23), (lane % RPI) * LPR);
+            if (lane / RPI == i0 + f) factor = up;
+            const int r = (i0 + f) * RPI + lr;
+            if (lc < D / 8 && !(twin && t))
+              *reinterpret_cast<uint4*>(tile + r * 128 + (((lc ^ r) & 7) << 4)) =
+                  make_uint4(pack_half(v[0] * down, v[4] * down), pack_half(v[1] * down, v[5] * down), pack_half(v[2] * down, v[6] * down), pack_half(v[3] * down, v[7] * down));
+          }
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -461,28 +470,28 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
         }
       };
 #pragma unroll 1
-      for (int j = j_first; j < s.j1; j += j_step) {
-        if (!__all_sync(0xffffffffu, mma_wait(bar_s_full + 8 * t, sn & 1))) { failed = true; break; }
-        ++sn;
+      for (int x = 0; j_first + (x >> 1) * j_step < s.j1; ++x) {
+        const int j = j_first + (x >> 1) * j_step, h = x & 1;
+        if (!__all_sync(0xffffffffu, mma_wait(bar_s_full + 8 * (2 * t + h), sn & 1))) { failed = true; break; }
+        // the product before these scores: complete with them, but no phase of a barrier may be left out
+        if (x >= 2 && !__all_sync(0xffffffffu, mma_wait(bar_o_full + 8 * (2 * t + h), (sn - 1) & 1))) { failed = true; break; }
         tc_fence_after();
-        const int left = lim - j * 128;
-        if (seen_blocks) look(j - j_step);
-        // Scores are read twice, 32 at a time, for the maximum and for the exponentials: registers for all 128 would be there, but not the
-        // instruction cache for the unrolled code.
-        const bool masked = __any_sync(0xffffffffu, left < 128);
-        uint32_t v[32];
-        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
-        for (int k = 0; k < 4; ++k) {
-          tmem_ld32(s_addr + k * 32, v);
-          tmem_wait_ld();
-          if (masked) {
+        uint32_t v[64];
+        tmem_ld64(s_addr + h * 64, v);
+        if (h == 0 && seen_blocks) look(j - j_step);
+        const int left = lim - j * 128 - h * 64;
+        if (__any_sync(0xffffffffu, left < 64)) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (i >= left - k * 32) v[i] = 0xff800000u;        // minus infinity, whatever the score was
-          }
+          for (int i = 0; i < 64; ++i)
+            if (i >= left) v[i] = 0xff800000u;                   // minus infinity, whatever the score was
+        }
+        float top[4];
 #pragma unroll
-          for (int i = 0; i < 32; i += 2) top[i / 2 % 4] = max3(top[i / 2 % 4], __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
+        for (int i = 0; i < 4; ++i) top[i] = max3(__uint_as_float(v[16 * i]), __uint_as_float(v[16 * i + 1]), -INFINITY);
+#pragma unroll
+        for (int i = 2; i < 16; i += 2) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) top[k] = max3(top[k], __uint_as_float(v[16 * k + i]), __uint_as_float(v[16 * k + i + 1]));
         }
         const float mx = max3(max3(top[0], top[1], top[2]), top[3], top[3]);
         if (__any_sync(0xffffffffu, (mx - m) * c > CK_RAISE)) {
@@ -491,8 +500,10 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
           const float f = mn == m ? 1.f : ap_ex2((m - mn) * c);  // 0 from the initial minus infinity
           m = mn;
           l *= f;
-          if (seen_blocks > 0) {
-            // S of this block is complete, hence so is the product of the block before: O is at rest
+          if (x > 0) {
+            // the product of the half block before: O is at rest
+            if (!__all_sync(0xffffffffu, mma_wait(bar_o_full + 8 * (2 * t + (h ^ 1)), (sn - (h ^ 1)) & 1))) { failed = true; break; }
+            tc_fence_after();
 #pragma unroll 1
             for (int k = 0; k < D / 16; ++k) {
               uint32_t w[16];
@@ -504,45 +515,33 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
             }
           }
         }
-        ++seen_blocks;
         const float off = m == -INFINITY ? 0.f : fmaf(-m, c, CK_LIFT);
         const uint64_t c2 = pair2(c, c), off2 = pair2(off, off);
         uint64_t ls[2] = {0, 0};
-#pragma unroll 1
-        for (int k = 0; k < 4; ++k) {
-          tmem_ld32(s_addr + k * 32, v);
-          tmem_wait_ld();
-          if (masked) {
+        uint32_t w[32];
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (i >= left - k * 32) v[i] = 0xff800000u;
-          }
-          uint32_t w[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float e0, e1;
-            unpair2(fma2(pair2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), c2, off2), &e0, &e1);
-            e0 = ap_ex2(e0);
-            e1 = ap_ex2(e1);
-            ls[i & 1] = add2(ls[i & 1], pair2(e0, e1));
-            w[i] = pack_half(e0, e1);
-          }
-          tmem_st16(s_addr + k * 16, w);                         // over scores that have been read
-          if (k & 1) {
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar_p_full + 8 * (2 * t + (k >> 1)));
-          }
+        for (int i = 0; i < 32; ++i) {
+          float e0, e1;
+          unpair2(fma2(pair2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), c2, off2), &e0, &e1);
+          e0 = ap_ex2(e0);
+          e1 = ap_ex2(e1);
+          ls[i & 1] = add2(ls[i & 1], pair2(e0, e1));
+          w[i] = pack_half(e0, e1);
         }
+        tmem_st32(s_addr + h * 64, w);                           // over the scores
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_p_full + 8 * (2 * t + h));
         float l0, l1;
         unpair2(add2(ls[0], ls[1]), &l0, &l1);
         l += l0 + l1;
+        sn += h;
+        seen_blocks += h;
       }
       if (failed) break;
       if (seen_blocks) {
-        if (!__all_sync(0xffffffffu, mma_wait(bar_o_full + 8 * t, on & 1))) { failed = true; break; }
-        ++on;
+        if (!__all_sync(0xffffffffu, mma_wait(bar_o_full + 16 * t, (sn - 1) & 1) && mma_wait(bar_o_full + 16 * t + 8, (sn - 1) & 1))) { failed = true; break; }
         tc_fence_after();
         look(j_first + (seen_blocks - 1) * j_step);
       }
@@ -663,7 +662,14 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
         if (!__all_sync(0xffffffffu, there)) { failed = true; break; }
         const int left = s.len - (s.j0 + (i >> 1)) * 128;        // rows of the sequence from this block on
         const uint32_t slot = (block + (i >> 1)) % CK_FLAGS;
-        bool any = false;
+        bool any = false, close = false;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+          const uint32_t pp = lds32(par0 + stage * L::STAGED + ((row_of(k) - row0) * NG + chunk_of(k) * 32 / G) * 4);
+          // lo below 2^15 and scale below 2^11 in size: all values fit; else a closer look
+          close |= row_of(k) < left && ((pp << 17) >= 0x47000000u << 1 || (pp & 0x7fff0000u) >= 0x45000000u);
+        }
+        close = __any_sync(0xffffffffu, close);
         uint4 code = lds128(code0 + stage * L::STAGED);
         uint32_t par = lds32(par0 + stage * L::STAGED + chunk0 * 32 / G * 4);
 #pragma unroll 1
@@ -674,10 +680,8 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
             code = lds128(code0 + stage * L::STAGED + (row_of(k + 1) - row0) * L::PITCH + (chunk_of(k + 1) - chunk0) * 16);
             par = lds32(par0 + stage * L::STAGED + ((row_of(k + 1) - row0) * NG + chunk_of(k + 1) * 32 / G) * 4);
           }
-          // lo below 2^15 and scale below 2^11 in size: all values fit; else a closer look
-          const bool close = (pp << 17) >= 0x47000000u << 1 || (pp & 0x7fff0000u) >= 0x45000000u;
-          if (__any_sync(0xffffffffu, close)) {
-            const bool bad = close && !fits_half(pp, p.status);
+          if (close) {
+            const bool bad = !fits_half(pp, p.status);
             if (__any_sync(0xffffffffu, bad)) {
               uint32_t* notes = s_notes + slot * 16 + (warp & 3);
               if ((i & 1) && !any) {
@@ -726,18 +730,17 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
     if (warp < 14) {
       // ------------------------------------------------------------------ MMA issuers, one per tile
       const int t = warp - 12;
-      const uint32_t idesc_s = make_idesc(ACC_F32, FMT_F16, FMT_F16, 128, 128);
+      const uint32_t idesc_s = make_idesc(ACC_F32, FMT_F16, FMT_F16, 128, 64);
       const uint32_t idesc_o = make_idesc(ACC_F32, FMT_F16, FMT_F16, 128, D, 0, 1);
       const uint32_t d_s = tmem_base + t * 128, d_o = tmem_base + 256 + t * 128;
       const uint32_t q0_lo = desc_lo(smem_u32(sQ), 16), k_lo = desc_lo(smem_u32(sKV), 16), v_lo = desc_lo(smem_u32(sKV), L::SUB);
-      const uint32_t s_full = bar_s_full + 8 * t, p_full = bar_p_full + 16 * t, o_full = bar_o_full + 8 * t;
-      uint32_t ring = 0, qn = 0, pn = 0, turn = 0;
+      const uint32_t s_full = bar_s_full + 16 * t, p_full = bar_p_full + 16 * t, o_full = bar_o_full + 16 * t;
+      uint32_t ring = 0, qn = 0, pn = 0;
       Seg s;
       while (walk.next(s)) {
         if (lane == 0) {
           const bool twin = s.twin();
           const int blocks = s.j1 - s.j0, n = twin ? (blocks + 1 - t) >> 1 : blocks;        // mine
-          const int turns = twin ? (blocks + 1) >> 1 : blocks;   // batches of each tile, after the first
           const uint32_t step = twin ? 4 : 2, first = ring + (twin ? 2 * t : 0);            // K of my block i: first + step i
           const uint32_t q_lo = q0_lo + (twin ? 0u : t * (L::TILE >> 4));
           auto kv_ready = [&](uint32_t pos) { return mma_wait(bar_kv_full + 8 * (pos % L::STAGES), (pos / L::STAGES) & 1); };
@@ -747,53 +750,42 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
             if (twin) mbar_arrive(bar);
             umma_commit(bar);
           };
-          auto my_turn = [&]() { return mma_wait(bar_turn + 8 * t, (turn++ & 1) ^ (t == 0)); };
-          auto your_turn = [&]() { mbar_arrive(bar_turn + 8 * (t ^ 1)); };
-          auto scores = [&](uint32_t pos) {
-            const uint32_t kb = k_lo + (pos % L::STAGES) * (L::TILE >> 4);
+          // S of keys 64 h .. 64 h + 63 of the block at ring position `pos`
+          auto scores = [&](uint32_t pos, int h) {
+            const uint32_t kb = k_lo + (pos % L::STAGES) * (L::TILE >> 4) + h * (64 * 128 >> 4);
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
               const uint32_t off = ((k >> 2) * L::SUB + (k & 3) * 32) >> 4;
-              if (k == 0) mma_ss<false>(d_s, q_lo + off, kb + off, idesc_s);
-              else mma_ss<true>(d_s, q_lo + off, kb + off, idesc_s);
+              if (k == 0) mma_ss<false>(d_s + h * 64, q_lo + off, kb + off, idesc_s);
+              else mma_ss<true>(d_s + h * 64, q_lo + off, kb + off, idesc_s);
             }
-            umma_commit(s_full);
+            umma_commit(s_full + 8 * h);
           };
           // Also a tile without blocks of its own waits for Q, so that no issuer gets more than a segment ahead.
           failed = !mma_wait(bar_q_full, qn++ & 1);
           if (n == 0) mbar_arrive(bar_q_empty);
-          // Batch i: O += P V of my block i, then S of the next one; the first batch has only the scores.
+          // Batch x: O += P V of my half block x, then S of the second next one, which takes its place; the first two have only scores.
 #pragma unroll 1
-          for (int i = -1; i < n && !failed; ++i) {
+          for (int x = -2; x < 2 * n && !failed; ++x) {
+            const int h = x & 1, i = x >> 1;
             const uint32_t vpos = first + step * i + 1, kpos = first + step * (i + 1);
-            if (i >= 0 && !(kv_ready(vpos) && mma_wait(p_full, pn & 1))) { failed = true; break; }
-            if (!my_turn()) { failed = true; break; }
-            tc_fence_after();
-            if (i >= 0) {
-              const uint32_t vb = v_lo + (vpos % L::STAGES) * (L::TILE >> 4);
-              // 16 keys per product, half of them with each part of P
-#pragma unroll
-              for (int k = 0; k < 4; ++k) mma_ts(d_o, d_s + k * 8, vb + k * 128, idesc_o, k || i);
-              if (!mma_wait(p_full + 8, pn++ & 1)) { failed = true; break; }
+            if (x >= 0) {
+              if ((h == 0 && !kv_ready(vpos)) || !mma_wait(p_full + 8 * h, pn & 1)) { failed = true; break; }
               tc_fence_after();
+              const uint32_t vb = v_lo + (vpos % L::STAGES) * (L::TILE >> 4) + h * 512;
 #pragma unroll
-              for (int k = 4; k < 8; ++k) mma_ts(d_o, d_s + k * 8, vb + k * 128, idesc_o, 1);
-              kv_done(vpos);                                     // (before the wait: with twins the next keys may need its place)
-              if (i + 1 == n) umma_commit(o_full);
+              for (int k = 0; k < 4; ++k) mma_ts(d_o, d_s + h * 64 + k * 8, vb + k * 128, idesc_o, k || x);
+              umma_commit(o_full + 8 * h);
+              if (h) kv_done(vpos);
+              pn += h;
             }
-            if (i + 1 < n) {
-              if (!kv_ready(kpos)) { failed = true; break; }
+            if (x + 2 < 2 * n) {
+              if (h == 0 && !kv_ready(kpos)) { failed = true; break; }
               tc_fence_after();
-              scores(kpos);
-              kv_done(kpos);
-              if (i + 2 == n) umma_commit(bar_q_empty);
+              scores(kpos, h);
+              if (h) kv_done(kpos);
+              if (x + 3 == 2 * n) umma_commit(bar_q_empty);
             }
-            your_turn();
-          }
-#pragma unroll 1
-          for (int i = n; i < turns && !failed; ++i) {
-            failed = !my_turn();
-            your_turn();
           }
           ring += 2 * blocks;
           if (failed) report(p.status, DEV_TIMEOUT_MMA);
