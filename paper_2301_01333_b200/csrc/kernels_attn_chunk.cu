@@ -19,8 +19,8 @@
 //   warp 15          bulk copies of codes and parameters, as they lie in the pages, a block and a half ahead
 // Where an item has at most 128 rows the two tiles are the same rows: they take the even and the odd blocks of keys, and
 // are joined at the end, the one reading the other's O from tensor memory.
-// The work is a row of units (one block of keys of one item; an item is 256 rows of a sequence, times heads), of which every CTA
-// takes an equal stretch; the pieces of an item that stretches cut are joined in their order by a second kernel.
+// The work is a row of units (one block of keys of one item, and two for its beginning; an item is 256 rows of a sequence, times
+// heads), of which every CTA takes an equal stretch; the pieces of an item that stretches cut are joined in their order by a second kernel.
 //   * A value that is not finite must not reach rows that do not see it (0 times NaN): such groups are widened as zeros and
 //     noted in a bit mask per block; a row that does see one gets NaN in that group's columns.
 #include <cuda_fp16.h>
@@ -36,6 +36,7 @@ namespace gc {
 namespace {
 constexpr int CK_THREADS = 512, CK_ROWS = 256;
 constexpr int CK_MAX_LIST = 160;             // items per head that are listed in shared memory
+constexpr int CK_START = 2;                  // what beginning an item costs, in blocks of keys
 constexpr int CK_FLAGS = 8;                  // blocks whose notes of values that are not finite are kept
 constexpr float CK_RAISE = 4.0f;             // binades a score may exceed the reference by
 constexpr float CK_LIFT = 11.0f;             // binades the probabilities are lifted by: at most 2^15, and whole down to 2^-25 of the reference
@@ -188,7 +189,7 @@ __device__ int2 make_list(const ChunkParams& p, const List& list, int most, int*
     for (int w = warp; w < here; w += CK_THREADS / 32) {
       const int4 x = s_seq[w];
 #pragma unroll 1
-      for (int i = lane; i < x.w && x.x + i < most; i += 32) list.put(x.x + i, blocks_of(p, ChunkSeq{0, x.y, x.z}, i), s0 + w, i);
+      for (int i = lane; i < x.w && x.x + i < most; i += 32) list.put(x.x + i, blocks_of(p, ChunkSeq{0, x.y, x.z}, i) + CK_START, s0 + w, i);
     }
     items = min(items + all, most);
     __syncthreads();
@@ -251,26 +252,29 @@ struct Walk {
     j = at - list.get(e).before;
   }
   __device__ __forceinline__ bool next(Seg& s) {
-    if (left <= 0) return false;
-    const Entry x = list.get(e);
-    const ChunkSeq q = seq_of(p, x.b);
-    s.b = x.b;
-    s.h = h;
-    s.row0 = x.i * CK_ROWS;
-    s.rows = min(q.nq * p.g - s.row0, CK_ROWS);
-    s.q0 = q.q0;
-    s.len = q.len;
-    s.ahead = q.len - q.nq;
-    s.n = blocks_of(p, q, x.i);
-    s.j0 = j;
-    s.j1 = static_cast<int>(min(static_cast<int64_t>(s.n), j + left));
-    left -= s.j1 - s.j0;
-    j = 0;
-    if (++e == items) {
-      e = 0;
-      ++h;
+    while (left > 0) {
+      const Entry x = list.get(e);
+      const ChunkSeq q = seq_of(p, x.b);
+      s.h = h;
+      s.row0 = x.i * CK_ROWS;
+      s.rows = min(q.nq * p.g - s.row0, CK_ROWS);
+      s.q0 = q.q0;
+      s.len = q.len;
+      s.ahead = q.len - q.nq;
+      s.b = x.b;
+      s.n = blocks_of(p, q, x.i);
+      const int take = static_cast<int>(min(static_cast<int64_t>(s.n + CK_START - j), left));
+      s.j0 = max(j - CK_START, 0);
+      s.j1 = j + take - CK_START;
+      left -= take;
+      j = 0;
+      if (++e == items) {
+        e = 0;
+        ++h;
+      }
+      if (s.j1 > s.j0) return true;                              // (else the stretch ends before the item's first block)
     }
-    return true;
+    return false;
   }
 };
 
@@ -399,60 +403,56 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
       float m = -INFINITY, l = 0.f, factor = 0.f;
       uint32_t poison = 0;                                      // groups of columns in which this row saw a value that is not finite
       int seen_blocks = 0;
-      // ---- Q: fp16 after scaling by a power of two, so that the largest of a row lies in [2^14, 2^15).  A row is read by 16 (at width
-      // 64: 8) neighbouring lanes, the next rows while these are scaled.
+      // ---- Q: fp16 after scaling by a power of two, so that the largest element of this warp's 32 rows lies in [2^14, 2^15).  A row is read
+      // by 16 (at width 64: 8) neighbouring lanes, all rows at once.  (Scaled row by row: 5 us a segment where this takes 2.)
       constexpr int LPR = D == 64 ? 8 : 16, RPI = 32 / LPR, N = 32 / RPI;        // lanes to a row, rows to a load, loads
       const int lc = lane % LPR, lr = lane / LPR;
-      const int64_t row_at = mine ? static_cast<int64_t>(s.h * p.g + my_row - token * p.g) : -1;      // head of this row
-      if (!__all_sync(0xffffffffu, mma_wait(bar_q_empty, (qn & 1) ^ 1))) { failed = true; break; }
-      ++qn;
+      const int64_t my_head = mine ? static_cast<int64_t>(s.h * p.g + my_row - token * p.g) : -1;
       {
-        const int64_t my_offset = mine ? static_cast<int64_t>(s.q0 + token) * p.q_tok + row_at * p.q_head : -1;
-        uint8_t* tile = sQ + t * L::TILE + (warp & 3) * 32 * 128 + (lc >> 3) * L::SUB;
-        constexpr int FLY = 4;
-        auto read = [&](int i) {
+        const int64_t my_offset = mine ? static_cast<int64_t>(s.q0 + token) * p.q_tok + my_head * p.q_head : -1;
+        uint4 x[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
           const int64_t at = __shfl_sync(0xffffffffu, my_offset, i * RPI + lr);
-          return at >= 0 && lc < D / 8 ? reinterpret_cast<const uint4*>(p.q + at)[lc] : make_uint4(0, 0, 0, 0);
-        };
-        uint4 x[FLY], next[FLY];
+          x[i] = make_uint4(0, 0, 0, 0);
+          if (at >= 0 && lc < D / 8) x[i] = reinterpret_cast<const uint4*>(p.q + at)[lc];
+        }
+        float tops[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int f = 0; f < FLY; ++f) next[f] = read(f);
-#pragma unroll 1
-        for (int i0 = 0; i0 < N; i0 += FLY) {
+        for (int i = 0; i < N; ++i) {
+          const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
-          for (int f = 0; f < FLY; ++f) x[f] = next[f];
-          if (i0 + FLY < N) {
+          for (int e = 0; e < 4; ++e) tops[e] = max3(tops[e], fabsf(__uint_as_float(w[e] << 16)), fabsf(__uint_as_float(w[e] & 0xffff0000u)));
+        }
+        float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
 #pragma unroll
-            for (int f = 0; f < FLY; ++f) next[f] = read(i0 + FLY + f);
-          }
+        for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        // (zeros and infinities: as they are; rows below 2^-86 need not keep their eight bits, for their scores are nothing)
+        const int ex = static_cast<int>(__float_as_uint(top) >> 23), e = top == 0.f || ex == 255 ? 0 : max(ex - 141, -100);
+        const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+        factor = p.c * __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+        if (!__all_sync(0xffffffffu, mma_wait(bar_q_empty, (qn & 1) ^ 1))) { failed = true; break; }
+        ++qn;
+        if (!(twin && t) && lc < D / 8) {
+          uint8_t* tile = sQ + t * L::TILE + (warp & 3) * 32 * 128 + (lc >> 3) * L::SUB;
 #pragma unroll
-          for (int f = 0; f < FLY; ++f) {
-            const uint32_t w[4] = {x[f].x, x[f].y, x[f].z, x[f].w};
-            float v[8], top = 0.f;
+          for (int i = 0; i < N; ++i) {
+            const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+            float v[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              v[2 * e] = __uint_as_float(w[e] << 16);
-              v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-              top = max3(top, fabsf(v[2 * e]), fabsf(v[2 * e + 1]));
+            for (int k = 0; k < 4; ++k) {
+              v[2 * k] = __uint_as_float(w[k] << 16) * down;
+              v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u) * down;
             }
-#pragma unroll
-            for (int d = LPR / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            // (rows of zeros and of infinities: as they are; rows below 2^-86 need not keep their eight bits, for their scores are nothing)
-            const int ex = static_cast<int>(__float_as_uint(top) >> 23), e = top == 0.f || ex == 255 ? 0 : max(ex - 141, -100);
-            const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-            const float up = __shfl_sync(0xffffffffu, p.c * __uint_as_float(static_cast<uint32_t>(127 + e) << 23), (lane % RPI) * LPR);
-            if (lane / RPI == i0 + f) factor = up;
-            const int r = (i0 + f) * RPI + lr;
-            if (lc < D / 8 && !(twin && t))
-              *reinterpret_cast<uint4*>(tile + r * 128 + (((lc ^ r) & 7) << 4)) =
-                  make_uint4(pack_half(v[0] * down, v[4] * down), pack_half(v[1] * down, v[5] * down), pack_half(v[2] * down, v[6] * down), pack_half(v[3] * down, v[7] * down));
+            const int r = i * RPI + lr;
+            *reinterpret_cast<uint4*>(tile + r * 128 + (((lc ^ r) & 7) << 4)) = make_uint4(pack_half(v[0], v[4]), pack_half(v[1], v[5]), pack_half(v[2], v[6]), pack_half(v[3], v[7]));
           }
         }
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_q_full);
       }
-      const float c = factor;                                   // c times the power of two this row's scores are short of
+      const float c = factor;                                   // c times the power of two the scores are short of
       // What was noted of block j's values, once a product that waited for them is known to be issued; they are overwritten eight blocks
       // on, when all rows have handed over probabilities made after this look.
       auto look = [&](int j) {
@@ -617,7 +617,7 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
         }
       }
       if (whole) {                                              // as Q was read
-        const int64_t my_offset = mine ? static_cast<int64_t>(s.q0 + token) * p.o_tok + row_at * p.o_head : -1;
+        const int64_t my_offset = mine ? static_cast<int64_t>(s.q0 + token) * p.o_tok + my_head * p.o_head : -1;
         __syncwarp();
 #pragma unroll 2
         for (int i = 0; i < N; ++i) {
@@ -965,7 +965,7 @@ size_t space_bytes(int ctas, int64_t most_items) {
 // 2^least_log blocks of keys where that is fewer.
 int64_t attn_chunk_items(int64_t q_tokens, int B, int g) { return q_tokens * g / CK_ROWS + B; }
 int attn_chunk_ctas(int64_t items, int Hk, int max_len, int least_log, int num_sms) {
-  const int64_t units = items * Hk * ((max_len + 127) / 128 + 1), want = (units >> least_log) + 1;
+  const int64_t units = items * Hk * ((max_len + 127) / 128 + CK_START + 1), want = (units >> least_log) + 1;
   return static_cast<int>(want < num_sms ? want : num_sms);
 }
 size_t attn_chunk_bytes(int D, int ctas, int64_t most_items) {
