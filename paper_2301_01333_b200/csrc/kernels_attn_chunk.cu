@@ -37,6 +37,7 @@ namespace {
 constexpr int CK_THREADS = 512, CK_ROWS = 256;
 constexpr int CK_MAX_LIST = 160;             // items per head that are listed in shared memory
 constexpr int CK_START = 2;                  // what beginning an item costs, in blocks of keys
+constexpr int CK_FETCH = 6;                  // blocks of keys that are called into the L2 ahead of their copies
 constexpr int CK_FLAGS = 8;                  // blocks whose notes of values that are not finite are kept
 constexpr float CK_RAISE = 4.0f;             // binades a score may exceed the reference by
 constexpr float CK_LIFT = 11.0f;             // binades the probabilities are lifted by: at most 2^15, and whole down to 2^-25 of the reference
@@ -80,6 +81,9 @@ __device__ __forceinline__ Params16 params16(uint32_t par) {
 // Bulk copy global -> shared of a multiple of 16 bytes, completion counted in bytes on an mbarrier of this CTA.
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void bulk_prefetch(const void* src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
   uint4 v;
@@ -640,7 +644,6 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
     // A lane takes 16 bytes of codes (32 elements) of a row at a time, CH times.  At width 128 and 64 eight lanes take two neighbouring chunks
     // of four rows, so that the four stores of 16 bytes that become of each touch all banks; at 96 a lane takes a row, and the rows' pitch spreads
     // them.  Round k: 16 rows on, or two chunks on.
-    // (The rounds are a loop: unrolled, this code and the softmax's drive each other out of the instruction cache.)
     constexpr int CH = D / 32;                                  // 16-byte chunks of codes in a row
     const int row0 = (warp & 3) * 32 + (D == 96 ? lane : ((lane >> 3) & 3) * 4 + ((lane >> 1) & 3)), chunk0 = D == 96 ? 0 : lane & 1;
     auto row_of = [&](int k) { return row0 + (D == 96 ? 0 : (k & 1) * 16); };
@@ -656,46 +659,57 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
 #pragma unroll 1
       for (int i = 0; i < halves; ++i) {                        // K and V in turn
         const uint32_t stage = used % L::AHEAD, st = ring % L::STAGES;
-        const bool there = mma_wait(bar_code_full + 8 * stage, (used / L::AHEAD) & 1) && mma_wait(bar_kv_empty + 8 * st, ((ring / L::STAGES) & 1) ^ 1);
-        ++used;
-        ++ring;
-        if (!__all_sync(0xffffffffu, there)) { failed = true; break; }
+        if (!__all_sync(0xffffffffu, mma_wait(bar_code_full + 8 * stage, (used / L::AHEAD) & 1))) { failed = true; break; }
         const int left = s.len - (s.j0 + (i >> 1)) * 128;        // rows of the sequence from this block on
         const uint32_t slot = (block + (i >> 1)) % CK_FLAGS;
+        uint4 code[CH];
+        uint32_t par[CH];
         bool any = false, close = false;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-          const uint32_t pp = lds32(par0 + stage * L::STAGED + ((row_of(k) - row0) * NG + chunk_of(k) * 32 / G) * 4);
-          // lo below 2^15 and scale below 2^11 in size: all values fit; else a closer look
-          close |= row_of(k) < left && ((pp << 17) >= 0x47000000u << 1 || (pp & 0x7fff0000u) >= 0x45000000u);
+          code[k] = lds128(code0 + stage * L::STAGED + (row_of(k) - row0) * L::PITCH + (chunk_of(k) - chunk0) * 16);
+          par[k] = lds32(par0 + stage * L::STAGED + ((row_of(k) - row0) * NG + chunk_of(k) * 32 / G) * 4);
         }
-        close = __any_sync(0xffffffffu, close);
-        uint4 code = lds128(code0 + stage * L::STAGED);
-        uint32_t par = lds32(par0 + stage * L::STAGED + chunk0 * 32 / G * 4);
-#pragma unroll 1
-        for (int k = 0; k < CH; ++k) {
-          const bool own = row_of(k) < left;                    // behind the sequence: zeros, whatever lies there
-          uint32_t word[4] = {own ? code.x : 0u, own ? code.y : 0u, own ? code.z : 0u, own ? code.w : 0u}, pp = own ? par : 0u;
-          if (k + 1 < CH) {
-            code = lds128(code0 + stage * L::STAGED + (row_of(k + 1) - row0) * L::PITCH + (chunk_of(k + 1) - chunk0) * 16);
-            par = lds32(par0 + stage * L::STAGED + ((row_of(k + 1) - row0) * NG + chunk_of(k + 1) * 32 / G) * 4);
-          }
-          if (close) {
-            const bool bad = !fits_half(pp, p.status);
-            if (__any_sync(0xffffffffu, bad)) {
-              uint32_t* notes = s_notes + slot * 16 + (warp & 3);
-              if ((i & 1) && !any) {
-                if (lane < 4) notes[lane * 4] = 0;
-                __syncwarp();
-              }
-              any = true;
-              if (bad && (i & 1)) atomicOr(notes + chunk_of(k) * 32 / G * 4, 1u << (row_of(k) & 31));
-              // a key becomes NaN, and so do the scores of who sees it; a value zero
-              if (bad) pp = i & 1 ? 0u : 0x7fc07fc0u;
-              __syncwarp();
+        if (left < 128) {                                        // behind the sequence: zeros, whatever lies there
+#pragma unroll
+          for (int k = 0; k < CH; ++k) {
+            if (row_of(k) >= left) {
+              code[k] = make_uint4(0, 0, 0, 0);
+              par[k] = 0;
             }
           }
-          const Params16 x = params16(pp);
+        }
+        // lo below 2^15 and scale below 2^11 in size: all values fit; else a closer look
+#pragma unroll
+        for (int k = 0; k < CH; ++k) close |= (par[k] << 17) >= 0x47000000u << 1 || (par[k] & 0x7fff0000u) >= 0x45000000u;
+        if (__any_sync(0xffffffffu, close)) {
+          uint32_t* notes = s_notes + slot * 16 + (warp & 3);
+          if ((i & 1) && lane < 4) notes[lane * 4] = 0;
+          __syncwarp();
+#pragma unroll 1
+          for (int k = 0; k < CH; ++k) {
+            uint32_t pp = par[0];
+#pragma unroll
+            for (int x = 1; x < CH; ++x) pp = k == x ? par[x] : pp;
+            const bool bad = !fits_half(pp, p.status);
+            any |= bad;
+            if (bad && (i & 1)) atomicOr(notes + chunk_of(k) * 32 / G * 4, 1u << (row_of(k) & 31));
+            // a key becomes NaN, and so do the scores of who sees it; a value zero
+#pragma unroll
+            for (int x = 0; x < CH; ++x)
+              if (k == x && bad) par[x] = i & 1 ? 0u : 0x7fc07fc0u;
+          }
+          any = __any_sync(0xffffffffu, any);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_code_empty + 8 * stage);
+        if (!__all_sync(0xffffffffu, mma_wait(bar_kv_empty + 8 * st, ((ring / L::STAGES) & 1) ^ 1))) { failed = true; break; }
+        ++used;
+        ++ring;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+          const uint32_t word[4] = {code[k].x, code[k].y, code[k].z, code[k].w};
+          const Params16 x = params16(par[k]);
           // a nibble in the low bits of a number from 1024 on, or four bits up in one from 64 on: that plus the code; then the code
           // times scale plus lo in one rounding
           const __half2 m1024 = half2_of(0xe400e400u), m64 = half2_of(0xd400d400u), lo2 = half2_of(x.lo2), sc2 = half2_of(x.scale2);
@@ -718,10 +732,7 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
         if ((i & 1) && lane == 0) reinterpret_cast<uint8_t*>(s_any + slot)[warp & 3] = any;
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(bar_code_empty + 8 * stage);
-          mbar_arrive(bar_kv_full + 8 * st);
-        }
+        if (lane == 0) mbar_arrive(bar_kv_full + 8 * st);
       }
       block += s.j1 - s.j0;
     }
@@ -818,11 +829,25 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
           const int t = j * 128 + lane * piece;
           return lane < pieces && j < s.j1 && t < s.len ? table[t >> p.page_shift] : 0;
         };
-        int next = page_of(s.j0);
+        // Staging holds a block and a half, not enough to cover the memory's latency: what follows is called into the L2 before.
+        auto fetch = [&](int j, int page) {
+          const int t = j * 128 + lane * piece;
+          if (lane >= pieces || j >= s.j1 || t >= s.len || page < 0 || page >= p.num_pages) return;
+          const int64_t at = ((static_cast<int64_t>(page) * p.Hk + s.h) << p.page_shift) + (t & ((1 << p.page_shift) - 1));
+          bulk_prefetch(p.k_codes + at * L::PITCH, piece * L::PITCH);
+          bulk_prefetch(p.v_codes + at * L::PITCH, piece * L::PITCH);
+          bulk_prefetch(p.k_params + at * NG, piece * (NG * 4));
+          bulk_prefetch(p.v_params + at * NG, piece * (NG * 4));
+        };
+#pragma unroll 1
+        for (int j = s.j0 + 1; j < min(s.j0 + CK_FETCH, s.j1); ++j) fetch(j, page_of(j));
+        int next = page_of(s.j0), far = page_of(s.j0 + CK_FETCH);
 #pragma unroll 1
         for (int j = s.j0; j < s.j1 && !failed; ++j) {
           int page = next;
+          fetch(j + CK_FETCH, far);
           next = page_of(j + 1);
+          far = page_of(j + 1 + CK_FETCH);
           if (page < 0 || page >= p.num_pages) {
             report(p.status, DEV_BAD_PAGE);
             page = 0;
