@@ -263,8 +263,8 @@ int page_shift_of(const gc_kv4_cache_t& c) {
   return s;
 }
 
-// A CTA of the chunk kernel takes at least two blocks of keys: below that its beginning and the joining cost more than they spare.
-constexpr int CHUNK_LEAST_LOG = 1;
+// A CTA of the chunk kernel takes at least four units of work, a block and a half of keys.
+constexpr int CHUNK_LEAST_LOG = 2;
 
 gc_status_t check_chunk(const char* who, const gc_kv4_cache_t* c, const gc_attention_kv4_chunk_t* d) {
   gc_status_t st = check_cache(who, c);
@@ -278,7 +278,7 @@ gc_status_t check_chunk(const char* who, const gc_kv4_cache_t* c, const gc_atten
   if (d->max_length > 0x7FFFFFFF - 65536) REFUSE(GC_ERR_UNSUPPORTED, "%s: max_length too large", who);
   const int64_t g = d->q_heads / c->kv_heads;
   if (d->q_tokens * g > (1LL << 30) || d->q_tokens > (1LL << 30) || d->batch > (1 << 20)) REFUSE(GC_ERR_UNSUPPORTED, "%s: too many tokens or sequences", who);
-  if (attn_chunk_items(d->q_tokens, d->batch, static_cast<int>(g)) * (d->max_length / 128 + 4LL) > 0x7FFFFFFF)
+  if (attn_chunk_items(d->q_tokens, d->batch, static_cast<int>(g)) * (d->max_length / 128 + 4LL) > 0x7FFFFFFF / 3)
     REFUSE(GC_ERR_UNSUPPORTED, "%s: too many tokens for sequences of up to %d", who, d->max_length);
   return GC_OK;
 }

@@ -19,8 +19,8 @@
 //   warp 15          bulk copies of codes and parameters, as they lie in the pages, a block and a half ahead
 // Where an item has at most 128 rows the two tiles are the same rows: they take the even and the odd blocks of keys, and
 // are joined at the end, the one reading the other's O from tensor memory.
-// The work is a row of units (one block of keys of one item, and two for its beginning; an item is 256 rows of a sequence, times
-// heads), of which every CTA takes an equal stretch; the pieces of an item that stretches cut are joined in their order by a second kernel.
+// The work is a row of units (three for a block of keys of an item, two where its tiles are twins, and six for its beginning; an item is
+// 256 rows of a sequence, times heads), of which every CTA takes an equal stretch; the pieces of an item that stretches cut are joined in their order by a second kernel.
 //   * A value that is not finite must not reach rows that do not see it (0 times NaN): such groups are widened as zeros and
 //     noted in a bit mask per block; a row that does see one gets NaN in that group's columns.
 #include <cuda_fp16.h>
@@ -36,7 +36,7 @@ namespace gc {
 namespace {
 constexpr int CK_THREADS = 512, CK_ROWS = 256;
 constexpr int CK_MAX_LIST = 160;             // items per head that are listed in shared memory
-constexpr int CK_START = 2;                  // what beginning an item costs, in blocks of keys
+constexpr int CK_START = 6, CK_BLOCK = 3, CK_TWIN_BLOCK = 2;      // what beginning an item and a block of its keys cost, in units of about 1700 clocks
 constexpr int CK_FETCH = 6;                  // blocks of keys that are called into the L2 ahead of their copies
 constexpr int CK_FLAGS = 8;                  // blocks whose notes of values that are not finite are kept
 constexpr float CK_RAISE = 4.0f;             // binades a score may exceed the reference by
@@ -82,6 +82,15 @@ __device__ __forceinline__ Params16 params16(uint32_t par) {
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred P;\n\tmbarrier.test_wait.parity.shared::cta.b64 P, [%1], %2;\n\tselp.b32 %0, 1, 0, P;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ void bulk_prefetch(const void* src, uint32_t bytes) {
   asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
 }
@@ -117,6 +126,8 @@ __device__ __forceinline__ int blocks_of(const ChunkParams& p, const ChunkSeq& s
   const int last = (min((i + 1) * CK_ROWS, s.nq * p.g) - 1) / p.g;       // token of the last row
   return (max(min(s.len - s.nq + last + 1, s.len), 1) + 127) >> 7;
 }
+
+__device__ __forceinline__ int block_cost(int rows) { return rows <= 128 ? CK_TWIN_BLOCK : CK_BLOCK; }
 
 // An item of the list: the units before it, its sequence and its number there.
 struct Entry {
@@ -193,7 +204,7 @@ __device__ int2 make_list(const ChunkParams& p, const List& list, int most, int*
     for (int w = warp; w < here; w += CK_THREADS / 32) {
       const int4 x = s_seq[w];
 #pragma unroll 1
-      for (int i = lane; i < x.w && x.x + i < most; i += 32) list.put(x.x + i, blocks_of(p, ChunkSeq{0, x.y, x.z}, i) + CK_START, s0 + w, i);
+      for (int i = lane; i < x.w && x.x + i < most; i += 32) list.put(x.x + i, blocks_of(p, ChunkSeq{0, x.y, x.z}, i) * block_cost(min(x.y * p.g - i * CK_ROWS, CK_ROWS)) + CK_START, s0 + w, i);
     }
     items = min(items + all, most);
     __syncthreads();
@@ -267,9 +278,10 @@ struct Walk {
       s.ahead = q.len - q.nq;
       s.b = x.b;
       s.n = blocks_of(p, q, x.i);
-      const int take = static_cast<int>(min(static_cast<int64_t>(s.n + CK_START - j), left));
-      s.j0 = max(j - CK_START, 0);
-      s.j1 = j + take - CK_START;
+      const int cost = block_cost(s.rows), take = static_cast<int>(min(static_cast<int64_t>(s.n * cost + CK_START - j), left));
+      // (a block belongs to the stretch that has its first unit)
+      s.j0 = (max(j - CK_START, 0) + cost - 1) / cost;
+      s.j1 = (max(j + take - CK_START, 0) + cost - 1) / cost;
       left -= take;
       j = 0;
       if (++e == items) {
@@ -761,6 +773,8 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
             if (twin) mbar_arrive(bar);
             umma_commit(bar);
           };
+          auto kv_there = [&](uint32_t pos) { return mbar_test(bar_kv_full + 8 * (pos % L::STAGES), (pos / L::STAGES) & 1); };
+          bool late = false;                                     // the first half's next scores are still to be issued
           // S of keys 64 h .. 64 h + 63 of the block at ring position `pos`
           auto scores = [&](uint32_t pos, int h) {
             const uint32_t kb = k_lo + (pos % L::STAGES) * (L::TILE >> 4) + h * (64 * 128 >> 4);
@@ -791,8 +805,15 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
               pn += h;
             }
             if (x + 2 < 2 * n) {
-              if (h == 0 && !kv_ready(kpos)) { failed = true; break; }
+              // Keys that are not there yet must not hold up the product with the second half's probabilities, which gives back the place
+              // of the values that are to be widened before those keys.
+              if (h == 0) {
+                late = x >= 0 && !kv_there(kpos);
+                if (late) continue;
+              }
+              if ((h == 0 || late) && !kv_ready(kpos)) { failed = true; break; }
               tc_fence_after();
+              if (late) scores(kpos, 0);
               scores(kpos, h);
               if (h) kv_done(kpos);
               if (x + 3 == 2 * n) umma_commit(bar_q_empty);
@@ -990,7 +1011,7 @@ size_t space_bytes(int ctas, int64_t most_items) {
 // 2^least_log blocks of keys where that is fewer.
 int64_t attn_chunk_items(int64_t q_tokens, int B, int g) { return q_tokens * g / CK_ROWS + B; }
 int attn_chunk_ctas(int64_t items, int Hk, int max_len, int least_log, int num_sms) {
-  const int64_t units = items * Hk * ((max_len + 127) / 128 + CK_START + 1), want = (units >> least_log) + 1;
+  const int64_t units = items * Hk * (((max_len + 127) / 128 + 1) * CK_BLOCK + CK_START), want = (units >> least_log) + 1;
   return static_cast<int>(want < num_sms ? want : num_sms);
 }
 size_t attn_chunk_bytes(int D, int ctas, int64_t most_items) {
