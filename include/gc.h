@@ -432,7 +432,7 @@ typedef struct {
 gc_status_t gc_kv4_weigh(void* cuda_stream, const gc_kv4_cache_t* cache, const gc_kv4_weigh_t* d);
 
 /* Eviction: of every sequence with n = lengths[b] > keep tokens, each key/value head keeps its own `keep`: the newest `recent` ones, and of
- * the others the keep - recent with the largest scores (equal ones: the older; NaN counts as largest).  scores: fp32, paged like the
+ * the others the keep - recent with the largest scores (equal ones: the older; NaN counts as largest).  scores: fp32, 16-byte aligned, paged like the
  * cache.  The kept tokens take positions 0 .. keep - 1: those from there stay where they are, and the holes
  * between them are filled, in order, with the kept ones from behind, in order.  (Attention does not mind the order of the tokens a query sees.)
  * Shorter sequences keep all.  With m = min(n, keep):

@@ -435,8 +435,9 @@ extern "C" gc_status_t gc_kv4_evict(void* cuda_stream, const gc_kv4_cache_t* cac
   if (st != GC_OK) return st;
   if (d->batch == 0) return GC_OK;
   if (!d->scores || !d->lengths || !d->out_lengths || (d->keep && !d->kept)) REFUSE(GC_ERR_INVALID_ARG, "%s: null argument", who);
-  if (misaligned(d->scores, 4) || misaligned(d->lengths, 4) || misaligned(d->out_lengths, 4) || misaligned(d->kept, 4))
+  if (misaligned(d->lengths, 4) || misaligned(d->out_lengths, 4) || misaligned(d->kept, 4))
     REFUSE(GC_ERR_ALIGNMENT, "%s: an array is not aligned to its element size", who);
+  if (misaligned(d->scores, 16)) REFUSE(GC_ERR_ALIGNMENT, "%s: scores must be 16-byte aligned", who);
   if ((st = check_table(who, "block_table", *cache, d->block_table, d->table_width, d->table_stride, d->max_length)) != GC_OK) return st;
   if (d->out_table && (st = check_table(who, "out_table", *cache, d->out_table, d->out_table_width, d->out_table_stride,
                                         d->keep < d->max_length ? d->keep : d->max_length)) != GC_OK)

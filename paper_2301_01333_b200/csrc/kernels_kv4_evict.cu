@@ -18,7 +18,7 @@
 namespace gc {
 
 namespace {
-constexpr int EV_THREADS = 512, EV_WARPS = EV_THREADS / 32;
+constexpr int EV_THREADS = 1024, EV_WARPS = EV_THREADS / 32;
 constexpr int EV_KEYS = 40960;               // keys of a CTA that are kept in shared memory (160 KB)
 constexpr int EV_MOVE_THREADS = 256;
 
@@ -54,7 +54,8 @@ __device__ __forceinline__ int length_of(const EvictParams& p, int b) {
 }  // namespace
 
 __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __grid_constant__ EvictParams p) {
-  extern __shared__ uint32_t s_keys[];                           // [min(positions of this CTA, EV_KEYS)]
+  extern __shared__ uint4 s_keys4[];                             // [min(positions of this CTA, EV_KEYS)]
+  uint32_t* s_keys = reinterpret_cast<uint32_t*>(s_keys4);
   __shared__ uint32_t s_hist[4][256];                            // one a pass: a pass ends with one cluster barrier
   __shared__ uint32_t s_warp[8];
   __shared__ int s_found[2];                                     // digit, elements still wanted below it
@@ -71,6 +72,7 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __gr
     if (p.lengths[b] != n) report(p.status, DEV_BAD_LENGTH);
     p.out_lengths[b] = m;
   }
+#pragma unroll 1
   for (int i = m + rank * EV_THREADS + tid; i < p.keep; i += ranks * EV_THREADS) kept[i] = -1;
   if (n <= p.keep) {                                             // (the same for the whole cluster)
     for (int i = rank * EV_THREADS + tid; i < n; i += ranks * EV_THREADS) kept[i] = i;
@@ -89,8 +91,13 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __gr
   };
   auto key_at = [&](int i) { return held ? s_keys[i] : load_key(base + i); };
   if (held) {
+    // four neighbouring positions at a time, which lie in one page
 #pragma unroll 4
-    for (int i = tid; i < mine; i += EV_THREADS) s_keys[i] = load_key(base + i);
+    for (int i = tid * 4; i < mine; i += EV_THREADS * 4) {
+      const int64_t at = place(p, row, h, base + i);
+      const float4 f = at < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(p.scores + at);
+      *reinterpret_cast<uint4*>(s_keys + i) = at < 0 ? make_uint4(0, 0, 0, 0) : make_uint4(key_of(f.x), key_of(f.y), key_of(f.z), key_of(f.w));
+    }
   }
   __syncthreads();
   // ---- the key of the last token that stays, eight bits at a time
@@ -101,6 +108,7 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __gr
     const int shift = 24 - 8 * pass;
     const uint32_t known = pass ? 0xffffffffu << (shift + 8) : 0u;
     uint32_t* hist = s_hist[pass];
+#pragma unroll 1
     for (int i0 = warp * 32; i0 < mine; i0 += EV_THREADS) {
       const int i = i0 + lane;
       const uint32_t key = i < mine ? key_at(i) : 0u;
@@ -155,6 +163,7 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __gr
   int equal_before = 0;
   if (!none) {
     int c = 0;
+#pragma unroll 1
     for (int i0 = w0; i0 < w1; i0 += 32) c += __popc(__ballot_sync(0xffffffffu, i0 + lane < w1 && key_at(i0 + lane) == prefix));
     if (lane == 0) s_equal[warp] = c;
     const uint32_t at = smem_u32(&s_hist[3][prefix & 255u]);     // the last pass counted just the equal ones
@@ -167,6 +176,7 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __gr
   // f(position, whether it stays, whether it is this warp's), in order
   auto walk = [&](auto f) {
     int eq = equal_before;
+#pragma unroll 1
     for (int i0 = w0; i0 < w1; i0 += 32) {
       const int i = i0 + lane;
       const uint32_t key = i < w1 ? key_at(i) : 0u;
@@ -193,6 +203,7 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __gr
   }
   cluster_sync_all();
   int hole = 0, mover = 0, all_movers = 0;                       // ahead of this warp; movers among the candidates
+#pragma unroll 1
   for (int r = 0; r < ranks; ++r) {
     const int x = static_cast<int>(ld_remote(mapa_shared(smem_u32(&s_counts[0]), r))), y = static_cast<int>(ld_remote(mapa_shared(smem_u32(&s_counts[1]), r)));
     if (r < rank) {
@@ -222,12 +233,14 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __gr
     hole += __popc(hm);
     mover += __popc(mm);
   });
+#pragma unroll 1
   for (int t = cand + rank * EV_THREADS + tid; t < n; t += ranks * EV_THREADS) {
     if (t < p.keep) kept[t] = t;
     else mover_list[all_movers + t - max(cand, p.keep)] = t;
   }
   cluster_sync_all();                                            // also: no CTA leaves before the others have read its counts
   const int count = all_movers + n - max(cand, p.keep);
+#pragma unroll 1
   for (int i = rank * EV_THREADS + tid; i < count; i += ranks * EV_THREADS) kept[__ldcg(hole_list + i)] = __ldcg(mover_list + i);
 }
 

@@ -80,6 +80,7 @@ __global__ void __launch_bounds__(WG_THREADS, wg_blocks(NT)) kv4_weigh_kernel(co
 
   // ---- my stretch of the row of tiles, and the sequence it begins in
   int64_t total = 0;
+#pragma unroll 1
   for (int s = lane; s < p.B; s += 32) {
     total += tiles_of(p, s);
     if (blockIdx.x == 0 && warp == 0 && p.lengths[s] != length_of(p, s)) report(p.status, DEV_BAD_LENGTH);
@@ -88,10 +89,12 @@ __global__ void __launch_bounds__(WG_THREADS, wg_blocks(NT)) kv4_weigh_kernel(co
   for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
   total *= p.Hk;
   const int64_t warps = static_cast<int64_t>(gridDim.x) * WG_WARPS, me = static_cast<int64_t>(blockIdx.x) * WG_WARPS + warp;
-  int64_t cur = total / warps * me + min(me, total % warps);
-  int64_t left = total / warps + (me < total % warps);
+  const int64_t each = (total >> 32) == 0 ? static_cast<int64_t>(static_cast<uint32_t>(total) / static_cast<uint32_t>(warps)) : total / warps, rest = total - each * warps;
+  int64_t cur = each * me + min(me, rest);
+  int64_t left = each + (me < rest);
   if (left == 0) return;
   int b = 0;
+#pragma unroll 1
   for (int s0 = 0; s0 < p.B; s0 += 32) {
     const int s = s0 + lane;
     const int64_t own = s < p.B ? static_cast<int64_t>(tiles_of(p, s)) * p.Hk : 0;
@@ -110,7 +113,7 @@ __global__ void __launch_bounds__(WG_THREADS, wg_blocks(NT)) kv4_weigh_kernel(co
     }
     cur -= __shfl_sync(0xffffffffu, incl, 31);
   }
-  int len = length_of(p, b), nb = tiles_of(p, b), h = static_cast<int>(cur / nb), k0 = static_cast<int>(cur - static_cast<int64_t>(h) * nb);
+  int len = length_of(p, b), nb = tiles_of(p, b), h = static_cast<int>(static_cast<uint32_t>(cur) / static_cast<uint32_t>(nb)), k0 = static_cast<int>(cur - static_cast<int64_t>(h) * nb);
 
   const int page_mask = (1 << p.page_shift) - 1;
   for (;;) {
@@ -122,6 +125,7 @@ __global__ void __launch_bounds__(WG_THREADS, wg_blocks(NT)) kv4_weigh_kernel(co
       const int padded = (chunks + NT - 1) / NT * NT;
       // ---- the queries of this pass as operands: lane (gr, tg) has column gr of a chunk
       __syncwarp();
+#pragma unroll 1
       for (int ch = 0; ch < padded; ++ch) {
         uint8_t* place = smem + ch * L::CHUNK;
         const int col = col_begin + ch * 8 + gr;
@@ -184,18 +188,20 @@ __global__ void __launch_bounds__(WG_THREADS, wg_blocks(NT)) kv4_weigh_kernel(co
       __syncwarp();
 
       // ---- the tiles
-      int pages = 0;                                             // page numbers of 16 tiles, two per tile, one per lane
+      // page numbers of 16 tiles, two per tile, one per lane; the next 16 tiles' on their way
+      auto fetch = [&](int i) {
+        const int t = (i + (lane >> 1)) * WG_TILE + (lane & 1) * 16;
+        return i + (lane >> 1) < i_end && t < len ? row[t >> p.page_shift] : 0;
+      };
+      int pages = 0, pages_next = fetch(i_begin);
       auto load = [&](int i, Tile<D, G>& x) {
         if ((i - i_begin) % 16 == 0) {
-          const int t = (i + (lane >> 1)) * WG_TILE + (lane & 1) * 16;
-          pages = 0;
-          if (i + (lane >> 1) < i_end && t < len) {
-            pages = row[t >> p.page_shift];
-            if (pages < 0 || pages >= p.num_pages) {
-              report(p.status, DEV_BAD_PAGE);
-              pages = -1;
-            }
+          pages = pages_next;
+          if (pages < 0 || pages >= p.num_pages) {
+            report(p.status, DEV_BAD_PAGE);
+            pages = -1;
           }
+          pages_next = fetch(i + 16);
         }
         const int w = (i - i_begin) % 16, t0 = i * WG_TILE;
         int64_t at[2];
@@ -246,6 +252,7 @@ __global__ void __launch_bounds__(WG_THREADS, wg_blocks(NT)) kv4_weigh_kernel(co
         const int t0 = i * WG_TILE;
         const bool edge = t0 + WG_TILE > len - (p.n - 1);        // some column may not see all of it
         float sum[4] = {0.f, 0.f, 0.f, 0.f};                     // tokens gr, gr + 8, gr + 16, gr + 24
+#pragma unroll 1
         for (int ch = 0; ch < padded; ch += NT) {
           const uint8_t* place = smem + ch * L::CHUNK;
           float s[NT][2][4];
@@ -312,14 +319,14 @@ __global__ void __launch_bounds__(WG_THREADS, wg_blocks(NT)) kv4_weigh_kernel(co
         const float got = tg & 2 ? (tg & 1 ? sum[3] : sum[2]) : (tg & 1 ? sum[1] : sum[0]);
         if (x.at >= 0) p.out[x.at] = x.weight + got;
       };
-      Tile<D, G> x, y;
+      Tile<D, G> x;
       load(i_begin, x);
-      for (int i = i_begin; i < i_end; i += 2) {
+#pragma unroll 1
+      for (int i = i_begin; i < i_end; ++i) {
+        Tile<D, G> y;
         if (i + 1 < i_end) load(i + 1, y);
         work(i, x);
-        if (i + 1 >= i_end) break;
-        if (i + 2 < i_end) load(i + 2, x);
-        work(i + 1, y);
+        x = y;
       }
     }
     left -= kn;
