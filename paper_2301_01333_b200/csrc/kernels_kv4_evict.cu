@@ -78,10 +78,10 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __gr
     for (int i = rank * EV_THREADS + tid; i < n; i += ranks * EV_THREADS) kept[i] = i;
     return;
   }
-  // ---- the candidates, and my stretch of them: a warp's part is a multiple of 32
+  // ---- the candidates, and my stretch of them: a warp's part is a multiple of 128
   const int* row = p.table + b * p.table_stride;
   const int cand = n - p.recent;                                 // positions from here on stay
-  const int share = ((cand + ranks * EV_WARPS - 1) / (ranks * EV_WARPS) + 31) & ~31;       // of a warp
+  const int share = ((cand + ranks * EV_WARPS - 1) / (ranks * EV_WARPS) + 127) & ~127;      // of a warp: four positions a lane at a time
   const int base = rank * EV_WARPS * share;                      // first of this CTA's
   const int mine = max(0, min(cand - base, EV_WARPS * share));
   const bool held = EV_WARPS * share <= p.held_keys;
@@ -89,7 +89,18 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __gr
     const int64_t at = place(p, row, h, t);
     return at < 0 ? 0u : key_of(p.scores[at]);
   };
-  auto key_at = [&](int i) { return held ? s_keys[i] : load_key(base + i); };
+  // keys of positions i .. i + 3, zeros behind `end`; and how many of the four there are
+  auto keys_at = [&](int i, int end, uint32_t (&key)[4]) {
+    const int there = min(max(end - i, 0), 4);
+    if (held) {
+      const uint4 x = there ? s_keys4[i >> 2] : make_uint4(0, 0, 0, 0);
+      key[0] = x.x; key[1] = x.y; key[2] = x.z; key[3] = x.w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) key[e] = e < there ? load_key(base + i + e) : 0u;
+    }
+    return there;
+  };
   if (held) {
     // four neighbouring positions at a time, which lie in one page
 #pragma unroll 4
@@ -109,25 +120,38 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __gr
     const uint32_t known = pass ? 0xffffffffu << (shift + 8) : 0u;
     uint32_t* hist = s_hist[pass];
 #pragma unroll 1
-    for (int i0 = warp * 32; i0 < mine; i0 += EV_THREADS) {
-      const int i = i0 + lane;
-      const uint32_t key = i < mine ? key_at(i) : 0u;
-      const bool in = i < mine && ((key ^ prefix) & known) == 0;
-      const uint32_t digit = key >> shift & 255u;
-      // Scores are much alike in their leading bits: the digit of the first lane is counted once for the warp, twice over.
-      uint32_t rest = __ballot_sync(0xffffffffu, in);
-      bool todo = in;
+    for (int i0 = warp * 128; i0 < mine; i0 += EV_THREADS * 4) {
+      uint32_t key[4], digit[4];
+      const int there = keys_at(i0 + lane * 4, mine, key);
+      bool todo[4], some = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        todo[e] = e < there && ((key[e] ^ prefix) & known) == 0;
+        digit[e] = key[e] >> shift & 255u;
+        some |= todo[e];
+      }
+      // Scores are much alike in their leading bits: the digit of the first lane that has one is counted once for the warp, twice over.
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
+        const uint32_t rest = __ballot_sync(0xffffffffu, some);
         if (rest == 0) break;
         const int first = __ffs(rest) - 1;
-        const uint32_t d = __shfl_sync(0xffffffffu, digit, first);
-        const uint32_t same = __ballot_sync(0xffffffffu, todo && digit == d);
-        if (lane == first) atomicAdd(&hist[d], __popc(same));
-        if (digit == d) todo = false;
-        rest &= ~same;
+        const uint32_t d = __shfl_sync(0xffffffffu, todo[0] ? digit[0] : todo[1] ? digit[1] : todo[2] ? digit[2] : digit[3], first);
+        int same = 0;
+        some = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool is = todo[e] && digit[e] == d;
+          same += is;
+          if (is) todo[e] = false;
+          some |= todo[e];
+        }
+        same = __reduce_add_sync(0xffffffffu, same);
+        if (lane == first) atomicAdd(&hist[d], static_cast<uint32_t>(same));
       }
-      if (todo) atomicAdd(&hist[digit], 1u);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (todo[e]) atomicAdd(&hist[digit[e]], 1u);
     }
     cluster_sync_all();
     // all CTAs' counts, and the digit at which the counts from the top reach what is wanted
@@ -164,7 +188,13 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __gr
   if (!none) {
     int c = 0;
 #pragma unroll 1
-    for (int i0 = w0; i0 < w1; i0 += 32) c += __popc(__ballot_sync(0xffffffffu, i0 + lane < w1 && key_at(i0 + lane) == prefix));
+    for (int i0 = w0; i0 < w1; i0 += 128) {
+      uint32_t key[4];
+      const int there = keys_at(i0 + lane * 4, w1, key);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c += e < there && key[e] == prefix;
+    }
+    c = __reduce_add_sync(0xffffffffu, c);
     if (lane == 0) s_equal[warp] = c;
     const uint32_t at = smem_u32(&s_hist[3][prefix & 255u]);     // the last pass counted just the equal ones
     for (int r = lane; r < rank; r += 32) equal_before += static_cast<int>(ld_remote(mapa_shared(at, r)));
@@ -173,24 +203,50 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __gr
     __syncthreads();
     for (int w = 0; w < warp; ++w) equal_before += s_equal[w];
   }
-  // f(position, whether it stays, whether it is this warp's), in order
+  // Sum of v over the lanes before this one; *all: over the warp.
+  auto scan = [&](int v, int* all) {
+    int incl = v;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += o;
+    }
+    *all = __shfl_sync(0xffffffffu, incl, 31);
+    return incl - v;
+  };
+  // f(first of four positions, which of them there are, which of these stay), in order
   auto walk = [&](auto f) {
     int eq = equal_before;
 #pragma unroll 1
-    for (int i0 = w0; i0 < w1; i0 += 32) {
-      const int i = i0 + lane;
-      const uint32_t key = i < w1 ? key_at(i) : 0u;
-      const uint32_t same = __ballot_sync(0xffffffffu, !none && i < w1 && key == prefix);
-      const bool stays = !none && i < w1 && (key > prefix || (key == prefix && eq + __popc(same & ((1u << lane) - 1u)) < want));
-      eq += __popc(same);
-      f(base + i, stays, i < w1);
+    for (int i0 = w0; i0 < w1; i0 += 128) {
+      uint32_t key[4];
+      const int i = i0 + lane * 4, there = keys_at(i, w1, key);
+      int same = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) same += !none && e < there && key[e] == prefix;
+      int rank = 0, all = 0;
+      if (__any_sync(0xffffffffu, same)) rank = scan(same, &all);
+      rank += eq;
+      uint32_t stays = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (none || e >= there) continue;
+        if (key[e] > prefix || (key[e] == prefix && rank < want)) stays |= 1u << e;
+        rank += key[e] == prefix;
+      }
+      eq += all;
+      f(base + i, (1u << there) - 1u, stays);
     }
   };
+  // of four positions from t on, those below the new length
+  auto below = [&](int t) { return t + 4 <= p.keep ? 15u : t >= p.keep ? 0u : (1u << (p.keep - t)) - 1u; };
   int holes = 0, movers = 0;
-  walk([&](int t, bool stays, bool in) {
-    holes += __popc(__ballot_sync(0xffffffffu, in && !stays && t < p.keep));
-    movers += __popc(__ballot_sync(0xffffffffu, in && stays && t >= p.keep));
+  walk([&](int t, uint32_t there, uint32_t stays) {
+    holes += __popc(there & ~stays & below(t));
+    movers += __popc(stays & ~below(t));
   });
+  holes = __reduce_add_sync(0xffffffffu, holes);
+  movers = __reduce_add_sync(0xffffffffu, movers);
   if (lane == 0) {
     s_holes[warp] = holes;
     s_movers[warp] = movers;
@@ -220,18 +276,23 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __gr
   const int lists = p.list_len;                                  // no more holes than that: kept positions, and evicted tokens
   int* hole_list = p.ws + static_cast<int64_t>(unit) * 2 * lists;
   int* mover_list = hole_list + lists;
-  walk([&](int t, bool stays, bool in) {
-    const bool is_hole = in && !stays && t < p.keep, is_mover = in && stays && t >= p.keep;
-    const uint32_t hm = __ballot_sync(0xffffffffu, is_hole), mm = __ballot_sync(0xffffffffu, is_mover), below = (1u << lane) - 1u;
-    if (in && stays && t < p.keep) kept[t] = t;
-    if (is_hole) hole_list[hole + __popc(hm & below)] = t;
-    if (is_mover) mover_list[mover + __popc(mm & below)] = t;
-    if (p.in_place && in && !stays && t >= p.keep) {             // a position that is given up: its score is zero from now on
-      const int64_t at = place(p, row, h, t);
-      if (at >= 0) p.scores[at] = 0.f;
+  walk([&](int t, uint32_t there, uint32_t stays) {
+    const uint32_t in = below(t), is_hole = there & ~stays & in, is_mover = stays & ~in;
+    int all = 0, at = 0;                                         // holes in the lower half of a word, movers in the upper
+    if (__any_sync(0xffffffffu, is_hole | is_mover)) at = scan(__popc(is_hole) | __popc(is_mover) << 16, &all);
+    int hole_at = hole + (at & 0xffff), mover_at = mover + (at >> 16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (stays & in & 1u << e) kept[t + e] = t + e;
+      if (is_hole & 1u << e) hole_list[hole_at++] = t + e;
+      if (is_mover & 1u << e) mover_list[mover_at++] = t + e;
+      if (p.in_place && (there & ~stays & ~in & 1u << e)) {      // a position that is given up: its score is zero from now on
+        const int64_t to = place(p, row, h, t + e);
+        if (to >= 0) p.scores[to] = 0.f;
+      }
     }
-    hole += __popc(hm);
-    mover += __popc(mm);
+    hole += all & 0xffff;
+    mover += all >> 16;
   });
 #pragma unroll 1
   for (int t = cand + rank * EV_THREADS + tid; t < n; t += ranks * EV_THREADS) {
@@ -324,7 +385,7 @@ int evict_ranks(int64_t units, int max_len, int num_sms) {
 cudaError_t launch_kv4_evict(EvictParams p, int D, int G, int num_sms, cudaStream_t s) {
   const int64_t units = static_cast<int64_t>(p.B) * p.Hk;
   const int ranks = evict_ranks(units, p.max_len, num_sms);
-  const int64_t need = static_cast<int64_t>((p.max_len + ranks * EV_WARPS - 1) / (ranks * EV_WARPS) + 31) / 32 * 32 * EV_WARPS;
+  const int64_t need = static_cast<int64_t>((p.max_len + ranks * EV_WARPS - 1) / (ranks * EV_WARPS) + 127) / 128 * 128 * EV_WARPS;
   p.held_keys = static_cast<int>(need < EV_KEYS ? need : EV_KEYS);
   cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kv4_evict_select_kernel), EV_KEYS * 4);
   if (e != cudaSuccess) return e;

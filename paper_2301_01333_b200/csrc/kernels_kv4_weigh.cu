@@ -24,9 +24,10 @@ namespace {
 constexpr int WG_WARPS = 4, WG_THREADS = WG_WARPS * 32;
 constexpr int WG_TILE = 32;
 constexpr int WG_START = 3;                  // what beginning a (sequence, head) costs, in tiles
+constexpr int WG_FETCH = 4;                  // tiles ahead that are called into the L2
 constexpr int WG_CHUNKS = 8;                 // groups of eight columns in one pass
 
-constexpr int wg_blocks(int nt) { return nt == 1 ? 4 : 3; }      // CTAs an SM the registers are cut for
+constexpr int WG_BLOCKS = 3;                 // CTAs an SM the registers are cut for (four of them: 101 us for the batch below, against 90)
 
 template <int D, int G>
 struct WeighLayout {
@@ -69,7 +70,7 @@ struct Tile {
 }  // namespace
 
 template <int D, int G, int NT>
-__global__ void __launch_bounds__(WG_THREADS, wg_blocks(NT)) kv4_weigh_kernel(const __grid_constant__ WeighParams p) {
+__global__ void __launch_bounds__(WG_THREADS, WG_BLOCKS) kv4_weigh_kernel(const __grid_constant__ WeighParams p) {
   using L = WeighLayout<D, G>;
   constexpr int NG = L::NG, KW = L::KW, KP = G >= 64 ? 2 : 1;
   extern __shared__ uint4 smem_u4[];
@@ -204,39 +205,50 @@ __global__ void __launch_bounds__(WG_THREADS, wg_blocks(NT)) kv4_weigh_kernel(co
           pages_next = fetch(i + 16);
         }
         const int w = (i - i_begin) % 16, t0 = i * WG_TILE;
-        int64_t at[2];
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const int page = __shfl_sync(0xffffffffu, pages, 2 * w + y);
-          at[y] = ((static_cast<int64_t>(max(page, 0)) * p.Hk + h) << p.page_shift) + ((t0 + 16 * y) & page_mask);
-          if (y == (tg >> 1)) x.at = page < 0 ? -1 : at[y];
-        }
-        // rows behind the sequence, whose page may be none, are not read
-        const int64_t safe = at[0];
+        // Where the halves' rows begin.  (Rows behind the sequence lie in its last page; a half behind it may have no page: the first one's
+        // rows stand in.)
+        auto begin_of = [&](int page, int t) { return ((static_cast<int64_t>(page) * p.Hk + h) << p.page_shift) + (t & page_mask); };
+        const int page0 = __shfl_sync(0xffffffffu, pages, 2 * w), page1 = __shfl_sync(0xffffffffu, pages, 2 * w + 1);
+        const int64_t at0 = begin_of(max(page0, 0), t0), at1 = t0 + 16 < len ? begin_of(max(page1, 0), t0 + 16) : at0;
+        const uint8_t* src[2] = {p.k_codes + at0 * (D / 2) + gr * (D / 2) + tg * (4 * KP), p.k_codes + at1 * (D / 2) + gr * (D / 2) + tg * (4 * KP)};
+        const uint32_t* ps[2] = {p.k_params + (at0 + gr) * NG, p.k_params + (at1 + gr) * NG};
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int64_t line = t0 + 8 * r + gr < len ? at[r >> 1] + (r & 1) * 8 + gr : safe;
-          const uint8_t* src = p.k_codes + line * (D / 2);
 #pragma unroll
           for (int v = 0; v < KW; v += KP) {
+            const uint8_t* a = src[r >> 1] + (r & 1) * 8 * (D / 2) + v * 16;
             if constexpr (KP == 2) {
-              const uint2 y = *reinterpret_cast<const uint2*>(src + v * 16 + tg * 8);
+              const uint2 y = *reinterpret_cast<const uint2*>(a);
               x.k[r][v] = y.x;
               x.k[r][v + 1] = y.y;
             } else {
-              x.k[r][v] = *reinterpret_cast<const uint32_t*>(src + v * 16 + tg * 4);
+              x.k[r][v] = *reinterpret_cast<const uint32_t*>(a);
             }
           }
-          const uint32_t* ps = p.k_params + line * NG;
+          const uint32_t* a = ps[r >> 1] + (r & 1) * 8 * NG;
           if constexpr (NG == 4) {
-            const uint4 y = *reinterpret_cast<const uint4*>(ps);
+            const uint4 y = *reinterpret_cast<const uint4*>(a);
             x.par[r][0] = y.x; x.par[r][1] = y.y; x.par[r][2] = y.z; x.par[r][3] = y.w;
           } else if constexpr (NG == 2) {
-            const uint2 y = *reinterpret_cast<const uint2*>(ps);
+            const uint2 y = *reinterpret_cast<const uint2*>(a);
             x.par[r][0] = y.x; x.par[r][1] = y.y;
           } else {
 #pragma unroll
-            for (int j = 0; j < NG; ++j) x.par[r][j] = ps[j];
+            for (int j = 0; j < NG; ++j) x.par[r][j] = a[j];
+          }
+        }
+        x.at = tg >> 1 ? (page1 < 0 ? -1 : at1) : (page0 < 0 ? -1 : at0);
+        // The registers hold the next tile, whose loads should find it in the L2: the tile four on is called there.  (16 rows of codes are
+        // D / 16 lines, and their parameters lie in one or two.)
+        {
+          const int z = (i - i_begin) + WG_FETCH, t = t0 + WG_FETCH * WG_TILE + (lane & 16), which = 2 * (z % 16) + (lane >> 4);
+          const int page = __shfl_sync(0xffffffffu, z / 16 == (i - i_begin) / 16 ? pages : pages_next, which);
+          if (t < len && i + WG_FETCH < i_end && page >= 0 && page < p.num_pages) {
+            const int64_t at = begin_of(page, t);
+            const int l = lane & 15;
+            if (l < D / 16) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.k_codes + at * (D / 2) + l * 128));
+            else if (l == D / 16) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.k_params + at * NG));
+            else if (l == D / 16 + 1) asm volatile("prefetch.global.L2 [%0];" ::"l"(pass ? p.out + at : p.weights + at));
           }
         }
         // token (tg / 2) 16 + (tg % 2) 8 + gr of the tile is this lane's
@@ -351,7 +363,7 @@ cudaError_t run(const WeighParams& p, int num_sms, cudaStream_t s) {
   cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), static_cast<size_t>(WG_WARPS) * WG_CHUNKS * WeighLayout<D, G>::CHUNK);
   if (e != cudaSuccess) return e;
   // one wave of CTAs, as many as shared memory and registers let an SM have; fewer where a warp would have less than two tiles
-  int resident = wg_blocks(NT);
+  int resident = WG_BLOCKS;
   const int fit = static_cast<int>(227 * 1024 / (smem + 1024));
   if (fit < resident) resident = fit;
   const int64_t most = static_cast<int64_t>(p.B) * p.Hk * ((p.max_len + WG_TILE - 1) / WG_TILE + WG_START);
