@@ -68,7 +68,7 @@ struct Params16 {
 };
 __device__ __forceinline__ bool fits_half(uint32_t par, uint32_t* status) {
   const float lo = __uint_as_float(par << 16), scale = __uint_as_float(par & 0xffff0000u);
-  if (fmaxf(fabsf(lo), fabsf(fmaf(15.f, scale, lo))) <= CK_LARGEST && fabsf(scale) <= CK_LARGEST) return true;      // (the first holds for a NaN too)
+  if (fabsf(lo) <= CK_LARGEST && fabsf(fmaf(15.f, scale, lo)) <= CK_LARGEST && fabsf(scale) <= CK_LARGEST) return true;
   if (fabsf(lo) < INFINITY && fabsf(scale) < INFINITY) report(status, DEV_LARGE_HALF);
   return false;
 }
@@ -473,16 +473,14 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
       // on, when all rows have handed over probabilities made after this look.
       auto look = [&](int j) {
         const uint32_t slot = (block + j - s.j0) % CK_FLAGS;
-        if (s_any[slot]) {
-#pragma unroll
-          for (int g = 0; g < NG; ++g) {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              const int k = lim - j * 128 - 32 * w;
-              const uint32_t sees = k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u;
-              if (s_notes[slot * 16 + g * 4 + w] & sees) poison |= 1u << g;
-            }
-          }
+        const uint32_t any = s_any[slot];
+        if (any == 0) return;
+#pragma unroll 1
+        for (int x = 0; x < 4 * NG; ++x) {
+          const int g = x >> 2, w = x & 3, k = lim - j * 128 - 32 * w;
+          const uint32_t sees = k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u;
+          // (only the warps that found something have written their words)
+          if ((any >> (8 * w) & 0xffu) && (s_notes[slot * 16 + g * 4 + w] & sees)) poison |= 1u << g;
         }
       };
 #pragma unroll 1
