@@ -711,6 +711,9 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
           }
           any = __any_sync(0xffffffffu, any);
         }
+        // (A bulk copy may overwrite what was read only behind a fence between the two kinds of access: without it, calls in close succession
+        // found codes of a later block in a tile's second half.)
+        fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_code_empty + 8 * stage);
         if (!__all_sync(0xffffffffu, mma_wait(bar_kv_empty + 8 * st, ((ring / L::STAGES) & 1) ^ 1))) { failed = true; break; }
@@ -810,6 +813,9 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
                 if (late) continue;
               }
               if ((h == 0 || late) && !kv_ready(kpos)) { failed = true; break; }
+              // These scores overwrite the probabilities that the product just issued reads, and products of unlike shapes into unlike
+              // accumulators keep no order among themselves: it has to be complete.  (The softmax works on the other half meanwhile.)
+              if (x >= 0 && !((h == 0 || late ? mma_wait(o_full, (pn - h) & 1) : true) && (h == 1 ? mma_wait(o_full + 8, (pn - 1) & 1) : true))) { failed = true; break; }
               tc_fence_after();
               if (late) scores(kpos, 0);
               scores(kpos, h);

@@ -652,6 +652,25 @@ def test_calls_on_a_stream_of_their_own_and_closely_one_after_another(S):
     assert all(torch.equal(x, y) for g in got for x, y in zip(g, want))
 
 
+@pytest.mark.parametrize("new,lens,hq,hk,d,group,page", [([48], [60000], 8, 1, 128, 64, 64), ([1] * 12 + [150, 96], [500 * i for i in range(1, 13)] + [3000, 2000], 16, 4, 128, 64, 64),
+                                                         ([300, 40], [9000, 9000], 4, 2, 64, 32, 16), ([64], [20000], 8, 1, 96, 32, 256)])
+def test_chunk_calls_in_close_succession(S, new, lens, hq, hk, d, group, page):
+    # many blocks of keys to a CTA, and nothing between the calls: every one gives what the first gave
+    cache, q, cu, table, out = chunk_case(S, new, lens, hq, hk, d, group, page, seed=7, tail=0)
+    outs = [torch.zeros_like(out) for _ in range(60)]
+    for o in outs:
+        cache.attend_chunk(q, cu, table, i32(lens), out=o)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, out) for o in outs)
+    ln = i32(lens)
+    for _ in range(5):                                           # without even the lengths' copy in between
+        for o in outs:
+            cache.attend_chunk(q, cu, table, ln, out=o)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, out) for o in outs)
+    cache.query_status()
+
+
 def test_cache_of_more_than_two_to_the_32_bytes(S):
     # 40000 pages of 256 tokens and 8 heads of 128: 5.2 GB of codes, 10.2 million tokens; the sequence lies in the last pages
     pages, page, hk, d = 40000, 256, 8, 128
