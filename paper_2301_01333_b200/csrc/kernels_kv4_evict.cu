@@ -18,7 +18,6 @@
 namespace gc {
 
 namespace {
-constexpr int EV_THREADS = 1024, EV_WARPS = EV_THREADS / 32;
 constexpr int EV_KEYS = 40960;               // keys of a CTA that are kept in shared memory (160 KB)
 constexpr int EV_MOVE_THREADS = 256;
 
@@ -47,15 +46,23 @@ __device__ __forceinline__ int64_t place(const EvictParams& p, const int* row, i
   }
   return ((static_cast<int64_t>(page) * p.Hk + h) << p.page_shift) + (t & ((1 << p.page_shift) - 1));
 }
+// Keys of positions t .. t + 3, t a multiple of four.
+__device__ __noinline__ uint4 keys_of(const EvictParams& p, const int* row, int h, int t) {
+  const int64_t at = place(p, row, h, t);
+  if (at < 0) return make_uint4(0, 0, 0, 0);
+  const float4 f = *reinterpret_cast<const float4*>(p.scores + at);
+  return make_uint4(key_of(f.x), key_of(f.y), key_of(f.z), key_of(f.w));
+}
 __device__ __forceinline__ int length_of(const EvictParams& p, int b) {
   const int len = p.lengths[b];
   return len < 0 ? 0 : min(len, p.max_len);
 }
 }  // namespace
 
+template <int EV_THREADS>
 __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __grid_constant__ EvictParams p) {
+  constexpr int EV_WARPS = EV_THREADS / 32;
   extern __shared__ uint4 s_keys4[];                             // [min(positions of this CTA, EV_KEYS)]
-  uint32_t* s_keys = reinterpret_cast<uint32_t*>(s_keys4);
   __shared__ uint32_t s_hist[4][256];                            // one a pass: a pass ends with one cluster barrier
   __shared__ uint32_t s_warp[8];
   __shared__ int s_found[2];                                     // digit, elements still wanted below it
@@ -85,10 +92,6 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __gr
   const int base = rank * EV_WARPS * share;                      // first of this CTA's
   const int mine = max(0, min(cand - base, EV_WARPS * share));
   const bool held = EV_WARPS * share <= p.held_keys;
-  auto load_key = [&](int t) {
-    const int64_t at = place(p, row, h, t);
-    return at < 0 ? 0u : key_of(p.scores[at]);
-  };
   // keys of positions i .. i + 3, zeros behind `end`; and how many of the four there are
   auto keys_at = [&](int i, int end, uint32_t (&key)[4]) {
     const int there = min(max(end - i, 0), 4);
@@ -96,18 +99,32 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __gr
       const uint4 x = there ? s_keys4[i >> 2] : make_uint4(0, 0, 0, 0);
       key[0] = x.x; key[1] = x.y; key[2] = x.z; key[3] = x.w;
     } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) key[e] = e < there ? load_key(base + i + e) : 0u;
+      const uint4 x = there ? keys_of(p, row, h, base + i) : make_uint4(0, 0, 0, 0);
+      key[0] = x.x; key[1] = x.y; key[2] = x.z; key[3] = x.w;
     }
     return there;
   };
   if (held) {
-    // four neighbouring positions at a time, which lie in one page
-#pragma unroll 4
-    for (int i = tid * 4; i < mine; i += EV_THREADS * 4) {
-      const int64_t at = place(p, row, h, base + i);
-      const float4 f = at < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(p.scores + at);
-      *reinterpret_cast<uint4*>(s_keys + i) = at < 0 ? make_uint4(0, 0, 0, 0) : make_uint4(key_of(f.x), key_of(f.y), key_of(f.z), key_of(f.w));
+    // the pages of several fours first, then their scores: two latencies, whatever the length
+    constexpr int FLY = 4;
+#pragma unroll 1
+    for (int i0 = tid * 4; i0 < mine; i0 += EV_THREADS * 4 * FLY) {
+      int64_t at[FLY];
+      float4 f[FLY];
+#pragma unroll
+      for (int k = 0; k < FLY; ++k) {
+        const int i = i0 + k * EV_THREADS * 4;
+        const int page = i < mine ? row[(base + i) >> p.page_shift] : -1;
+        at[k] = page < 0 || page >= p.num_pages ? -1 : ((static_cast<int64_t>(page) * p.Hk + h) << p.page_shift) + ((base + i) & ((1 << p.page_shift) - 1));
+        if (at[k] < 0 && i < mine) report(p.status, DEV_BAD_PAGE);
+      }
+#pragma unroll
+      for (int k = 0; k < FLY; ++k) f[k] = at[k] < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(p.scores + at[k]);
+#pragma unroll
+      for (int k = 0; k < FLY; ++k) {
+        const int i = i0 + k * EV_THREADS * 4;
+        if (i < mine) s_keys4[i >> 2] = at[k] < 0 ? make_uint4(0, 0, 0, 0) : make_uint4(key_of(f[k].x), key_of(f[k].y), key_of(f[k].z), key_of(f[k].w));
+      }
     }
   }
   __syncthreads();
@@ -286,10 +303,12 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_evict_select_kernel(const __gr
       if (stays & in & 1u << e) kept[t + e] = t + e;
       if (is_hole & 1u << e) hole_list[hole_at++] = t + e;
       if (is_mover & 1u << e) mover_list[mover_at++] = t + e;
-      if (p.in_place && (there & ~stays & ~in & 1u << e)) {      // a position that is given up: its score is zero from now on
-        const int64_t to = place(p, row, h, t + e);
-        if (to >= 0) p.scores[to] = 0.f;
-      }
+    }
+    if (p.in_place && (there & ~stays & ~in)) {                  // positions that are given up: their scores are zero from now on
+      const int64_t to = place(p, row, h, t);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (to >= 0 && (there & ~stays & ~in & 1u << e)) p.scores[to + e] = 0.f;
     }
     hole += all & 0xffff;
     mover += all >> 16;
@@ -385,13 +404,17 @@ int evict_ranks(int64_t units, int max_len, int num_sms) {
 cudaError_t launch_kv4_evict(EvictParams p, int D, int G, int num_sms, cudaStream_t s) {
   const int64_t units = static_cast<int64_t>(p.B) * p.Hk;
   const int ranks = evict_ranks(units, p.max_len, num_sms);
-  const int64_t need = static_cast<int64_t>((p.max_len + ranks * EV_WARPS - 1) / (ranks * EV_WARPS) + 127) / 128 * 128 * EV_WARPS;
+  // 256 threads where a CTA has up to 4096 positions (four at a time and thread), else 1024
+  const bool few = p.max_len <= 4096 * ranks;
+  const int threads = few ? 256 : 1024, warps = threads / 32;
+  const int64_t need = static_cast<int64_t>((p.max_len + ranks * warps - 1) / (ranks * warps) + 127) / 128 * 128 * warps;
   p.held_keys = static_cast<int>(need < EV_KEYS ? need : EV_KEYS);
-  cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kv4_evict_select_kernel), EV_KEYS * 4);
+  auto kern = few ? kv4_evict_select_kernel<256> : kv4_evict_select_kernel<1024>;
+  cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), EV_KEYS * 4);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(units * ranks));
-  cfg.blockDim = dim3(EV_THREADS);
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
   cfg.dynamicSmemBytes = static_cast<size_t>(p.held_keys) * 4;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
@@ -402,7 +425,7 @@ cudaError_t launch_kv4_evict(EvictParams p, int D, int G, int num_sms, cudaStrea
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  e = cudaLaunchKernelEx(&cfg, kv4_evict_select_kernel, p);
+  e = cudaLaunchKernelEx(&cfg, kern, p);
   if (e != cudaSuccess || p.keep == 0) return e;
   if (D == 64) return G == 32 ? move<64, 32>(p, s) : move<64, 64>(p, s);
   if (D == 96) return move<96, 32>(p, s);
