@@ -4,25 +4,36 @@
 //
 // The products are tcgen05's with fp32 accumulators and fp16 operands: K, V and the probabilities are rounded once, to eleven bits.  (In bf16 the
 // rounding of K alone puts the output off by 3-5e-3 of its norm, which is mostly cancellation, where the output's own rounding is 1.7e-3.)  Q, bf16,
-// becomes fp16 exactly after its row is scaled by a power of two; probabilities, at most 2^4 relative to the reference, are lifted by 2^11.
+// becomes fp16 after a warp's 32 rows are scaled by one power of two: exactly down to 2^-31 of their largest element, with an error of
+// 2^-39 of it below; probabilities, at most 2^4 relative to the reference, are lifted by 2^11.
 //
 // A row is a (token, query head) of those that share a key/value head, token by token, so that a block of keys, once widened, serves
 // all of them.  A CTA holds 256 rows in two tiles of 128, and per block of 128 keys at width 128 there are
 // two products of 512 clocks for each tile (2048 in all), as many clocks of exponentials (16 a clock), and 32768 elements to be
 // widened: 3.4 instructions for two of them, 440 of the 2048 issue slots of a scheduler.
-//   warps 0-3, 4-7   softmax of tile 0 / 1, one row per thread (as in the prompt attention)
+//   warps 0-3, 4-7   softmax of tile 0 / 1, one row per thread, 64 keys at a time: each half of a block's scores has its own place in
+//                    tensor memory, barriers and products, its probabilities lie over it
 //   warps 8-11       widen: codes and parameters out of staging, as fp16 into 128-byte-swizzled tiles of a ring.  The eight elements of a word
 //                    come apart as (0,4), (1,5), (2,6), (3,7) and stay in that order: Q's elements are put in the same one, and
 //                    the columns of O are put back in registers at the end.
-//   warps 12, 13     MMA issuers of tile 0 / 1, taking turns
+//   warps 12, 13     MMA issuers of tile 0 / 1.  Products of unlike shapes keep no order among themselves: scores are
+//                    multiplied only once the product that reads the probabilities they overwrite is complete.
 //   warp 14          notes down which pieces of split items this CTA leaves
-//   warp 15          bulk copies of codes and parameters, as they lie in the pages, a block and a half ahead
+//   warp 15          bulk copies of codes and parameters, as they lie in the pages, a block and a half ahead (at width 64 four blocks); six
+//                    blocks ahead they are called into the L2
 // Where an item has at most 128 rows the two tiles are the same rows: they take the even and the odd blocks of keys, and
 // are joined at the end, the one reading the other's O from tensor memory.
 // The work is a row of units (three for a block of keys of an item, two where its tiles are twins, and six for its beginning; an item is
 // 256 rows of a sequence, times heads), of which every CTA takes an equal stretch; the pieces of an item that stretches cut are joined in their order by a second kernel.
 //   * A value that is not finite must not reach rows that do not see it (0 times NaN): such groups are widened as zeros and
 //     noted in a bit mask per block; a row that does see one gets NaN in that group's columns.
+//
+// Measured, calls in a row: the last 1024 tokens of a sequence of 33001, 16 / 4 heads of 128 (0.27 TFLOP): 318 us, 860 TFLOP/s; 32 sequences of
+// up to 4096, chunks of up to 192 tokens, three in four of one, 32 / 8 heads of 128: 176 us.  Tensor pipe 40 %, XU 40 %, ALU 41 %, half an instruction a clock
+// and scheduler of one: what bounds it is the way round of a half block, products, exponentials, probabilities, products, with two halves
+// of two tiles under way (without any arithmetic the handshakes alone take 127 of the 318).  Tried for the first of these calls: 128 scores
+// in registers, unrolled, with registers moved between warps 368 (its code no longer fits the instruction cache); two groups of
+// softmax warps for each tile 359; eight widening warps 347; tiles taking turns 370; staging by loads through the cores 342.
 #include <cuda_fp16.h>
 
 #include <type_traits>

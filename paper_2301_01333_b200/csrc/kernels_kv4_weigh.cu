@@ -8,11 +8,15 @@
 // fp16 after scaling by a power of two, scales and offsets are applied to the sums (kernels_attn_kv4.cu has the details).
 //
 //   * The 32-token tiles of all (sequence, head) stand in one row, of which every warp takes an equal stretch.
-//   * A lane loads its words of a tile straight into registers, a tile ahead: with 64 elements to a group eight bytes of eight
+//   * A lane loads its words of a tile straight into registers, a tile ahead, and calls them into the L2 four tiles ahead: with 64 elements to a group eight bytes of eight
 //     rows, whole sectors.  No shared memory for keys, no barriers.
 //   * The queries of up to 64 columns, as operands, stand in the warp's own shared memory; more columns than that
 //     take further passes over the stretch, which add to the first one's weights.
 //   * After the columns are summed, lane (gr, tg) has the sum of one token: weights are read and written 32 to a request.
+//
+// Measured, calls in a row: 64 sequences of up to 8192 tokens, 32 / 8 heads of 128, one query each: 90 us, 1.9 TB/s, bound by instructions
+// (about 570 a tile, 0.41 a clock and scheduler); 16 queries of one of 65000, 16 / 4 heads: 35 us; 5 sequences of up to 300:
+// 7.2 us, a launch and a chain of latencies.  Keys through a ring of asynchronous copies in shared memory: 88 us for the first, but 8.8 for the last.
 #include <cuda_fp16.h>
 
 #include "ptx.cuh"
@@ -27,7 +31,7 @@ constexpr int WG_START = 3;                  // what beginning a (sequence, head
 constexpr int WG_FETCH = 4;                  // tiles ahead that are called into the L2
 constexpr int WG_CHUNKS = 8;                 // groups of eight columns in one pass
 
-constexpr int WG_BLOCKS = 3;                 // CTAs an SM the registers are cut for (four of them: 101 us for the batch below, against 90)
+constexpr int WG_BLOCKS = 3;                 // CTAs an SM the registers are cut for (four of them: 101 us for the batch of 64, against 90)
 
 template <int D, int G>
 struct WeighLayout {
