@@ -183,6 +183,21 @@ def test_chunk_sizes_of_queries_and_keys(S, power_q, power_k):
     within(out, ref, tol + (2 * torch.expm1(torch.as_tensor(lost, device=DEV)) * 6 if power_k < -10 else 0))
 
 
+@pytest.mark.parametrize("power", [40, 0, -60])
+def test_chunk_infinite_queries_leave_their_neighbours_scale(S, power):
+    # rows are scaled by a power of two, exactly: without the infinity the other rows are the same to the last bit
+    g = gen(6)
+    cache = filled_cache(S, 30, 16, 2, 64, 64, g)
+    table = table_of([400], 16, 30, g)
+    q = (randn(37, 4, 64, g=g) * 2.0 ** power).to(BF)
+    x = q.clone()
+    x[4, 1, 3], x[4, 2, 63], x[36, 0, 0] = math.inf, -math.inf, math.inf
+    want, got = (cache.attend_chunk(y, i32([0, 37]), table, i32([400]), scale=0.125 * 2.0 ** -power) for y in (q, x))
+    same = torch.ones(37, 4, dtype=torch.bool, device=DEV)
+    same[4, 1] = same[4, 2] = same[36, 0] = False
+    assert torch.equal(got[same], want[same]) and torch.isnan(got[~same]).all()
+
+
 def test_chunk_scores_that_rise_and_fall(S):
     for seed, qscale in ((1, 8.0), (2, 0.01), (3, 30.0)):
         chunk_case(S, [90, 300], [1500, 640], 4, 2, 128, 64, 32, seed=seed, qscale=qscale)
