@@ -346,6 +346,9 @@ gc_status_t gc_kv4_append(void* cuda_stream, const gc_kv4_cache_t* cache, int32_
 /* Read the values held at slots[t] into k / v rows; rows of negative slots are left as they were. */
 gc_status_t gc_kv4_read(void* cuda_stream, const gc_kv4_cache_t* cache, int32_t dtype, int64_t tokens,
                         const gc_heads_t* k, const gc_heads_t* v, const int64_t* slots);
+/* The same, but rows of negative slots (and of those beyond the cache, which are recorded) are zero: for outputs not written before. */
+gc_status_t gc_kv4_read_or_zero(void* cuda_stream, const gc_kv4_cache_t* cache, int32_t dtype, int64_t tokens,
+                                const gc_heads_t* k, const gc_heads_t* v, const int64_t* slots);
 
 /* out[b, j, h] = softmax_t(scale * q[b, j, h] . K[t]) V over the cached tokens t < lengths[b] - (queries - 1) + j of
  * sequence b (the new tokens' rows have been appended; length counts them); zero where there is none.  K / V are the

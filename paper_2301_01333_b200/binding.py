@@ -38,6 +38,7 @@ EXPORTS = [
     "gc_qk_norm_rope", "gc_kv4_append", "gc_kv4_read", "gc_attention_kv4_workspace_bytes", "gc_attention_kv4",
     "gc_attention_prompt", "gc_serving_status", "gc_attention_kv4_lse", "gc_attention_kv4_chunk_workspace_bytes",
     "gc_attention_kv4_chunk", "gc_kv4_weigh", "gc_kv4_evict_workspace_bytes", "gc_kv4_evict",
+    "gc_kv4_read_or_zero",
 ]
 
 
@@ -161,7 +162,7 @@ def load_library() -> C.CDLL:
     heads = C.POINTER(gc_heads_t)
     lib.gc_qk_norm_rope.argtypes = [vp, C.POINTER(gc_qk_norm_rope_t)]
     lib.gc_kv4_append.argtypes = [vp, C.POINTER(gc_kv4_cache_t), i32, C.c_int64, heads, heads, vp]
-    lib.gc_kv4_read.argtypes = [vp, C.POINTER(gc_kv4_cache_t), i32, C.c_int64, heads, heads, vp]
+    lib.gc_kv4_read.argtypes = lib.gc_kv4_read_or_zero.argtypes = [vp, C.POINTER(gc_kv4_cache_t), i32, C.c_int64, heads, heads, vp]
     lib.gc_attention_kv4_workspace_bytes.argtypes = [C.POINTER(gc_kv4_cache_t), C.POINTER(gc_attention_kv4_t), C.POINTER(sz)]
     lib.gc_attention_kv4.argtypes = [vp, C.POINTER(gc_kv4_cache_t), C.POINTER(gc_attention_kv4_t), vp, sz]
     lib.gc_attention_prompt.argtypes = [vp, C.POINTER(gc_attention_prompt_t)]
@@ -175,7 +176,8 @@ def load_library() -> C.CDLL:
     lib.gc_kv4_evict.argtypes = [vp, cache, C.POINTER(gc_kv4_evict_t), vp, sz]
     for name in ("gc_qk_norm_rope", "gc_kv4_append", "gc_kv4_read", "gc_attention_kv4_workspace_bytes", "gc_attention_kv4",
                  "gc_attention_prompt", "gc_serving_status", "gc_attention_kv4_lse", "gc_attention_kv4_chunk_workspace_bytes",
-                 "gc_attention_kv4_chunk", "gc_kv4_weigh", "gc_kv4_evict_workspace_bytes", "gc_kv4_evict"):
+                 "gc_attention_kv4_chunk", "gc_kv4_weigh", "gc_kv4_evict_workspace_bytes", "gc_kv4_evict",
+                 "gc_kv4_read_or_zero"):
         getattr(lib, name).restype = i32
     for name in ("gc_partition_create", "gc_compile", "gc_workspace_bytes", "gc_set_workspace", "gc_execute",
                  "gc_host_staging_bytes", "gc_set_host_staging", "gc_execute_host", "gc_execute_host_async",
@@ -356,6 +358,12 @@ def gc_kv4_append(stream: int, cache: gc_kv4_cache_t, dtype: int, tokens: int, k
 
 def gc_kv4_read(stream: int, cache: gc_kv4_cache_t, dtype: int, tokens: int, k: gc_heads_t, v: gc_heads_t, slots: int) -> None:
     st = load_library().gc_kv4_read(stream, cache, dtype, tokens, k, v, slots)
+    if st:
+        raise GcError(st, gc_last_error())
+
+
+def gc_kv4_read_or_zero(stream: int, cache: gc_kv4_cache_t, dtype: int, tokens: int, k: gc_heads_t, v: gc_heads_t, slots: int) -> None:
+    st = load_library().gc_kv4_read_or_zero(stream, cache, dtype, tokens, k, v, slots)
     if st:
         raise GcError(st, gc_last_error())
 

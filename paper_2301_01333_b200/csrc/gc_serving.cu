@@ -183,14 +183,26 @@ extern "C" gc_status_t gc_kv4_append(void* cuda_stream, const gc_kv4_cache_t* ca
   return GC_OK;
 }
 
-extern "C" gc_status_t gc_kv4_read(void* cuda_stream, const gc_kv4_cache_t* cache, int32_t dtype, int64_t tokens, const gc_heads_t* k,
-                                   const gc_heads_t* v, const int64_t* slots) {
-  gc_status_t st = check_rows("gc_kv4_read", cache, dtype, tokens, k, v, slots);
+namespace {
+gc_status_t read(const char* who, void* cuda_stream, const gc_kv4_cache_t* cache, int32_t dtype, int64_t tokens, const gc_heads_t* k,
+                 const gc_heads_t* v, const int64_t* slots, bool zeros) {
+  gc_status_t st = check_rows(who, cache, dtype, tokens, k, v, slots);
   if (st != GC_OK || tokens == 0) return st;
   OnDevice on(cache->cuda_device);
   RUN(on.err());
-  RUN(launch_kv4_read(*cache, dtype, tokens, *k, *v, slots, static_cast<cudaStream_t>(cuda_stream)));
+  RUN(launch_kv4_read(*cache, dtype, tokens, *k, *v, slots, zeros, static_cast<cudaStream_t>(cuda_stream)));
   return GC_OK;
+}
+}  // namespace
+
+extern "C" gc_status_t gc_kv4_read(void* cuda_stream, const gc_kv4_cache_t* cache, int32_t dtype, int64_t tokens, const gc_heads_t* k,
+                                   const gc_heads_t* v, const int64_t* slots) {
+  return read("gc_kv4_read", cuda_stream, cache, dtype, tokens, k, v, slots, false);
+}
+
+extern "C" gc_status_t gc_kv4_read_or_zero(void* cuda_stream, const gc_kv4_cache_t* cache, int32_t dtype, int64_t tokens, const gc_heads_t* k,
+                                           const gc_heads_t* v, const int64_t* slots) {
+  return read("gc_kv4_read_or_zero", cuda_stream, cache, dtype, tokens, k, v, slots, true);
 }
 
 extern "C" gc_status_t gc_attention_kv4_workspace_bytes(const gc_kv4_cache_t* cache, const gc_attention_kv4_t* d, size_t* bytes) {

@@ -28,6 +28,7 @@ struct Kv4Params {
   uint32_t rows, heads;        // rows: tokens * heads
   uint32_t heads_mul, heads_shift;   // row / heads = (row * heads_mul) >> (32 + heads_shift)
   int page_shift;
+  bool zeros;                  // reading: rows of no slot are zero (else left as they were)
   uint32_t* status;
 };
 
@@ -299,7 +300,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_read_kernel(const __grid_const
   }
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
-    if (slot[i] < 0) continue;
+    if (slot[i] < 0 && !(p.zeros && row0 + i * ROWS < p.rows)) continue;       // (code and parameters of no slot are zeros)
     T* dst = static_cast<T*>(x.data) + t[i] * x.token_stride + h[i] * x.head_stride + j * 8;
     if constexpr (sizeof(T) == 2) {
       // pairs (0,4), (1,5), (2,6), (3,7): 128 + code, minus 128, times scale plus lo in one rounding
@@ -360,7 +361,7 @@ cudaError_t dispatch(const Kv4Params& p, int D, int G, bool vec, cudaStream_t s)
 
 template <bool READ>
 cudaError_t launch(const gc_kv4_cache_t& c, int dtype, int64_t tokens, const gc_heads_t& k, const gc_heads_t& v, const int64_t* slots,
-                   cudaStream_t s) {
+                   bool zeros, cudaStream_t s) {
   Kv4Params p = {};
   p.x[0] = k; p.x[1] = v;
   p.codes[0] = static_cast<uint8_t*>(c.k_codes); p.codes[1] = static_cast<uint8_t*>(c.v_codes);
@@ -373,6 +374,7 @@ cudaError_t launch(const gc_kv4_cache_t& c, int dtype, int64_t tokens, const gc_
   while ((2u << p.heads_shift) < p.heads) ++p.heads_shift;
   p.heads_mul = static_cast<uint32_t>(((1ull << (32 + p.heads_shift)) + p.heads - 1) / p.heads);
   while ((1 << p.page_shift) < c.page_size) ++p.page_shift;
+  p.zeros = zeros;
   p.status = c.status;
   const int esz = dtype == GC_F32 ? 4 : 2;
   const bool vec = vec_heads(k, esz) && vec_heads(v, esz);
@@ -383,11 +385,11 @@ cudaError_t launch(const gc_kv4_cache_t& c, int dtype, int64_t tokens, const gc_
 
 cudaError_t launch_kv4_append(const gc_kv4_cache_t& c, int dtype, int64_t tokens, const gc_heads_t& k, const gc_heads_t& v,
                               const int64_t* slots, cudaStream_t s) {
-  return launch<false>(c, dtype, tokens, k, v, slots, s);
+  return launch<false>(c, dtype, tokens, k, v, slots, false, s);
 }
 cudaError_t launch_kv4_read(const gc_kv4_cache_t& c, int dtype, int64_t tokens, const gc_heads_t& k, const gc_heads_t& v,
-                            const int64_t* slots, cudaStream_t s) {
-  return launch<true>(c, dtype, tokens, k, v, slots, s);
+                            const int64_t* slots, bool zeros, cudaStream_t s) {
+  return launch<true>(c, dtype, tokens, k, v, slots, zeros, s);
 }
 
 }  // namespace gc

@@ -158,6 +158,6 @@ cudaError_t launch_qk_norm_rope(const gc_qk_norm_rope_t& d, int num_sms, cudaStr
 cudaError_t launch_kv4_append(const gc_kv4_cache_t& c, int dtype, int64_t tokens, const gc_heads_t& k, const gc_heads_t& v,
                               const int64_t* slots, cudaStream_t s);
 cudaError_t launch_kv4_read(const gc_kv4_cache_t& c, int dtype, int64_t tokens, const gc_heads_t& k, const gc_heads_t& v,
-                            const int64_t* slots, cudaStream_t s);
+                            const int64_t* slots, bool zeros, cudaStream_t s);
 
 }  // namespace gc

@@ -209,10 +209,10 @@ PyObject* kv4_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (cache, slots, k_out, v_out, the cache's four tensors)
+// (cache, slots, k_out, v_out, whether rows of no slot are zero, the cache's four tensors)
 PyObject* kv4_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 5, [&]() -> PyObject* {
-    const gc_kv4_cache_t* c = cache_at(a[0], a[4]);
+  return guarded(n, 6, [&]() -> PyObject* {
+    const gc_kv4_cache_t* c = cache_at(a[0], a[5]);
     const at::Tensor &slots = tensor(a[1], "slots"), &k = tensor(a[2], "k_out"), &v = tensor(a[3], "v_out");
     const at::Device device = device_of(c);
     const int32_t type = row_type(k, "k_out");
@@ -220,7 +220,7 @@ PyObject* kv4_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t* s = static_cast<const int64_t*>(vec(slots, "slots", tokens, at::kLong, device));
     const gc_heads_t kh = heads(k, "k_out", tokens, c->kv_heads, c->head_dim, k.scalar_type(), device, true);
     const gc_heads_t vh = heads(v, "v_out", tokens, c->kv_heads, c->head_dim, k.scalar_type(), device, true);
-    check(gc_kv4_read(stream_of(c->cuda_device), c, type, tokens, &kh, &vh, s));
+    check((a[4] == Py_True ? gc_kv4_read_or_zero : gc_kv4_read)(stream_of(c->cuda_device), c, type, tokens, &kh, &vh, s));
     written(k);
     written(v);
     Py_RETURN_NONE;

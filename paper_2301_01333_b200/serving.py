@@ -167,12 +167,15 @@ class KV4Cache:
             raise TypeError("slots must be a torch.Tensor")
         if slots.dim() != 1:
             raise ValueError(f"slots must be a vector, not {tuple(slots.shape)}")
-        if k_out is None or v_out is None:
-            like = k_out if k_out is not None else v_out
+        fresh = k_out is None and v_out is None
+        if fresh:
+            k_out, v_out = (torch.empty((slots.shape[0], self.kv_heads, self.head_dim), dtype=dtype, device=self.device) for _ in range(2))
+        elif k_out is None or v_out is None:
+            like = v_out if k_out is None else k_out
             shape = (slots.shape[0], self.kv_heads, self.head_dim)
-            made = torch.zeros(shape, dtype=dtype if like is None else like.dtype, device=self.device)
-            k_out, v_out = (made, torch.zeros_like(made)) if like is None else (made if k_out is None else k_out, made if v_out is None else v_out)
-        _serving.kv4_read(self._at, slots, k_out, v_out, self._tensors)
+            made = torch.zeros(shape, dtype=like.dtype, device=self.device)
+            k_out, v_out = made if k_out is None else k_out, made if v_out is None else v_out
+        _serving.kv4_read(self._at, slots, k_out, v_out, fresh, self._tensors)
         return k_out, v_out
 
     def attend(self, q: torch.Tensor, block_table: torch.Tensor, lengths: torch.Tensor, *, scale: Optional[float] = None,

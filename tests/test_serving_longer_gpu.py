@@ -26,6 +26,33 @@ def held(cache, table, i, m):
             for c, p in ((cache.k_codes, cache.k_params), (cache.v_codes, cache.v_params))]
 
 
+# ------------------------------------------------------------------------------------------------ reading into outputs made there
+@pytest.mark.parametrize("dtype", [BF, torch.float32])
+@pytest.mark.parametrize("d,group", SHAPES)
+@pytest.mark.parametrize("tokens", [1, 7, 701])
+def test_read_makes_outputs_of_zeros_where_there_is_no_slot(S, dtype, d, group, tokens):
+    g = gen(tokens)
+    cache = filled_cache(S, 6, 16, 3, d, group, g)
+    slots = torch.randint(-40, 96, (tokens,), generator=g, device=g.device).to(DEV)
+    for beyond in (False, True):
+        if beyond:
+            slots[tokens // 2] = 96
+        spoiled = [torch.full((tokens, 3, d), math.nan, dtype=dtype, device=DEV) for _ in range(2)]       # what the allocator hands out next
+        del spoiled
+        k, v = cache.read(slots, dtype)
+        ko, vo = (torch.zeros(tokens, 3, d, dtype=dtype, device=DEV) for _ in range(2))
+        cache.read(slots, k_out=ko, v_out=vo)
+        assert torch.equal(k, ko) and torch.equal(v, vo) and (k[(slots < 0) | (slots >= 96)] == 0).all()
+        if beyond:
+            with pytest.raises(S.GcError, match="slot"):
+                cache.query_status()
+        else:
+            cache.query_status()
+        ko.fill_(3.0)
+        cache.read(slots.clamp(max=95), k_out=ko)                # rows of a given output stay as they were
+        assert (ko[slots < 0] == 3).all()
+
+
 # ------------------------------------------------------------------------------------------------ chunks
 def chunk_reference(cache, q, new, table, lens, scale):
     """q [tokens, heads, D] -> (o, tolerance) for the rows that sequences own."""
