@@ -407,8 +407,10 @@ int evict_ranks(int64_t units, int max_len, int num_sms) {
 cudaError_t launch_kv4_evict(EvictParams p, int D, int G, int num_sms, cudaStream_t s) {
   const int64_t units = static_cast<int64_t>(p.B) * p.Hk;
   const int ranks = evict_ranks(units, p.max_len, num_sms);
-  // 256 threads where a CTA has up to 4096 positions (four at a time and thread), else 1024
-  const bool few = p.max_len <= 4096 * ranks;
+  // 256 threads where a CTA has up to 4096 positions (four at a time and thread), and up to 16384 where more CTAs than the GPU holds
+  // of the larger ones share it (40 sequences of 5000 x 8 heads: 49 us instead of 69 with the move; of 16384: 184, 187; of 40000, whose
+  // keys fill an SM: 574, 335); else 1024.
+  const bool few = p.max_len <= 4096 * static_cast<int64_t>(ranks) || (p.max_len <= 16384 * static_cast<int64_t>(ranks) && units * ranks > 2 * num_sms);
   const int threads = few ? 256 : 1024, warps = threads / 32;
   const int64_t need = static_cast<int64_t>((p.max_len + ranks * warps - 1) / (ranks * warps) + 127) / 128 * 128 * warps;
   p.held_keys = static_cast<int>(need < EV_KEYS ? need : EV_KEYS);

@@ -501,6 +501,11 @@ def test_evict_on_one_and_on_several_ctas(S, lens, keep, recent, hk, scores_of):
     evict_case(S, lens, keep, recent, hk, 64, 64, 64, scores_of, seed=keep)
 
 
+def test_evict_of_more_sequences_than_ctas_fit(S):
+    # more (sequence, head) pairs than two an SM, each longer than a small CTA's usual share; and some of them short
+    evict_case(S, [4300 if i % 3 else i for i in range(80)], 700, 33, 4, 64, 64, 32, few_values)
+
+
 def test_evict_scores_that_are_all_alike(S):
     evict_case(S, [3000, 100], 700, 20, 2, 64, 64, 32, lambda shape, g: torch.ones(shape, device=DEV), seed=1)     # the oldest stay
 
