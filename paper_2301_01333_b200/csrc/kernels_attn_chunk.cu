@@ -945,33 +945,60 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
   }
 }
 
-// Joins the pieces of the item that begins in CTA blockIdx.x without ending there with the following CTAs' first pieces.  A block
-// has 32 rows and 32 columns: two warps of 16 columns, for each of them four that take every fourth piece and are then joined
+// Joins the pieces of an item that begins in one CTA without ending there: that CTA's second piece, and the following ones' first.  A block
+// has 32 rows and 32 columns: two warps of 16 columns, for each of them WAYS that take every WAYS-th piece and are then joined
 // in shared memory, all in a fixed order.  (With one thread for all pieces of a row, an item in 74 pieces took 115 us.)
-constexpr int CJ_WAYS = 4;
-template <int D>
-__global__ void __launch_bounds__(2 * CJ_WAYS * 32) attn_chunk_join_kernel(const __grid_constant__ ChunkParams p, const int ctas) {
-  __shared__ float4 s_o[CJ_WAYS][2][4][32];
-  __shared__ float2 s_ml[CJ_WAYS][2][32];
+//   FEW    eight warps a column and a block for each item there can be, which looks it up in all notes: where items have eight
+//          pieces and more (48 tokens at the end of 60000: 42 us for the call instead of 46)
+//   else   four, and a block for every CTA, which looks at the item that begins there (many items: 176 us for the batch of 32 sequences,
+//          182 with eight warps; 188 looking items up)
+template <int D, bool FEW>
+__global__ void __launch_bounds__(FEW ? 512 : 256) attn_chunk_join_kernel(const __grid_constant__ ChunkParams p, const int ctas) {
+  constexpr int WAYS = FEW ? 8 : 4;
+  __shared__ float4 s_o[WAYS][2][4][32];
+  __shared__ float2 s_ml[WAYS][2][32];
   wait_for_predecessor();
   const ChunkSpace<D> space(p.ws, ctas);
   const int lane = threadIdx.x & 31, way = threadIdx.x >> 6, half = threadIdx.x >> 5 & 1;
-  const int c0 = blockIdx.x, row = blockIdx.y * 32 + lane, col = blockIdx.z * 32 + half * 16;
+  const int row = blockIdx.y * 32 + lane, col = blockIdx.z * 32 + half * 16;
+  int c0 = blockIdx.x, n = 1;                                    // pieces: up to the first that reaches the item's end
+  if constexpr (FEW) {
+    int skip = blockIdx.x, end = ctas;
+    c0 = -1;
+#pragma unroll 5
+    for (int c = 0; c < ctas; c += 32) {
+      const bool in = c + lane < ctas;
+      const int rows = in ? space.note[c + lane].rows : 0, ends = in ? space.note[c + lane].ends : 0;
+      const uint32_t begin = __ballot_sync(0xffffffffu, rows > 0);
+      uint32_t ending = __ballot_sync(0xffffffffu, ends);
+      if (c0 < 0) {
+        const uint32_t here = __ballot_sync(0xffffffffu, rows > 0 && __popc(begin & ((1u << lane) - 1)) == skip);
+        skip -= __popc(begin);
+        if (!here) continue;
+        c0 = c + __ffs(here) - 1;
+        ending &= ~(here | (here - 1));
+      }
+      if (ending && end == ctas) end = c + __ffs(ending);
+    }
+    if (c0 < 0) return;
+    n = end - c0;
+  }
   const Note note = space.note[c0];
   if (static_cast<int>(blockIdx.y) * 32 >= note.rows) return;
-  int n = 1;                                                     // pieces: up to the first that reaches the item's end
-  for (int c = c0 + 1;; c += 32) {
-    const uint32_t end = __ballot_sync(0xffffffffu, c + lane >= ctas || space.note[c + lane].ends);
-    n += end ? __ffs(end) : 32;
-    if (end) break;
+  if constexpr (!FEW) {
+    for (int c = c0 + 1;; c += 32) {
+      const uint32_t end = __ballot_sync(0xffffffffu, c + lane >= ctas || space.note[c + lane].ends);
+      n += end ? __ffs(end) : 32;
+      if (end) break;
+    }
+    n = min(n, ctas - c0);
   }
-  n = min(n, ctas - c0);
   float m = -INFINITY, l = 0.f;
   float4 a[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) a[k] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 2
-  for (int i = way; i < n; i += CJ_WAYS) {
+  for (int i = way; i < n; i += WAYS) {
     const int64_t piece = 2 * static_cast<int64_t>(c0 + i) + (i == 0);
     const float2 x = space.ml[piece * CK_ROWS + row];
     float4 v[4];
@@ -995,7 +1022,7 @@ __global__ void __launch_bounds__(2 * CJ_WAYS * 32) attn_chunk_join_kernel(const
   __syncthreads();
   if (way != 0 || row >= note.rows) return;
 #pragma unroll
-  for (int w = 1; w < CJ_WAYS; ++w) {
+  for (int w = 1; w < WAYS; ++w) {
     const float2 x = s_ml[w][half][lane];
     const float mn = fmaxf(m, x.x), ref = mn == -INFINITY ? 0.f : mn;
     const float f = ap_ex2(m - ref), g = ap_ex2(x.x - ref);
@@ -1031,7 +1058,10 @@ cudaError_t run(const ChunkParams& p, int ctas, cudaStream_t s) {
   }
   e = launch_following(kern, dim3(static_cast<unsigned>(ctas)), CK_THREADS, (ChunkLayout<D, G>::SMEM), s, p);
   if (e != cudaSuccess || ctas == 1) return e;
-  return launch_following(attn_chunk_join_kernel<D>, dim3(static_cast<unsigned>(ctas), CK_ROWS / 32, D / 32), 2 * CJ_WAYS * 32, 0, s, p, ctas);
+  const int64_t items = static_cast<int64_t>(p.most_items) * p.Hk;
+  const unsigned rows = static_cast<unsigned>((p.q_tokens * p.g < CK_ROWS ? p.q_tokens * p.g + 31 : CK_ROWS) / 32);
+  if (items * 8 <= ctas) return launch_following(attn_chunk_join_kernel<D, true>, dim3(static_cast<unsigned>(items), rows, D / 32), 512, 0, s, p, ctas);
+  return launch_following(attn_chunk_join_kernel<D, false>, dim3(static_cast<unsigned>(ctas), rows, D / 32), 256, 0, s, p, ctas);
 }
 template <int D, int G>
 cudaError_t by_list(const ChunkParams& p, int ctas, cudaStream_t s) {

@@ -13,7 +13,7 @@
 // Bound: the scores read once and the kept rows read and written once; what it takes is a chain of latencies (seven cluster
 // barriers of about a microsecond) and a launch.  Scores are read once, and their keys kept in shared memory while they fit.
 // Measured: from 131071 tokens x 8 heads of 128 to 8192: select 37 us, move 10 (a cold cache); 48 sequences of up to 4099 x 8 heads of 64
-// to 2048: 31 and 23; 5 sequences of up to 300 x 8 heads of 128 to 256: 12 and 6.  Reading the counts of all CTAs at once, and other
+// to 2048: about 28 and 23; 5 sequences of up to 300 x 8 heads of 128 to 256: 12 and 6.  Reading the counts of all CTAs at once, and other
 // unrollings of the passes, changed nothing.
 #include "ptx.cuh"
 #include "serving.cuh"
