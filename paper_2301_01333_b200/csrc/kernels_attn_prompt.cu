@@ -14,10 +14,12 @@
 //                    the product with the first runs while the second is made; at the end of a tile they scale and store its O
 //   warp 8           TMA producer: Q tiles, and K and V blocks through one ring
 //   warps 9, 10      MMA issuers of tile 0 / 1: S = Q K^T (both operands in shared memory), O += P V (P in tensor memory, V as
-//                    stored, keys along the rows).  The tensor core works off one thread's products in order, which is what lets
-//                    S of the next block overwrite P of this one, and makes "S complete" imply "O complete".  Their batches
-//                    take turns.
-// Tensor memory: two score tiles of 128 columns and two outputs of D <= 128: all 512 columns.
+//                    stored, keys along the rows).  A commit covers all that its thread has issued, so that "S complete" implies "O
+//                    complete"; but only products into the same accumulator, of the same shape, are promised to run in their order.
+//                    Where P lies over the scores (widths 96 and 128), S of the next block is issued once the product that
+//                    reads P is complete.  The tiles' batches take turns.
+// Tensor memory: two score tiles of 128 columns and two outputs of D <= 128: all 512 columns at width 128.  At 64 the 64 columns beside
+// each output are free, and P has them for its own.
 // How it got there, for one prompt of 16384 tokens, 16 heads of 128 (1.1 TFLOP): one issuing thread for both tiles 1148 us, with
 // two threads per row 1064 (its instructions were the bottleneck: products alone took 940); an issuing thread per tile with lean
 // descriptors, taking turns (both tiles' products at once complete both scores together, and the tensor core idles while
@@ -64,7 +66,8 @@ struct PromptLayout {
   static constexpr int SUB = 128 * 128;
   static constexpr int TILE = NSUB * SUB;        // 128 rows of Q, K or V
   static constexpr int STAGES = D == 64 ? 8 : 4;
-  static constexpr int BARS = 2 * STAGES + 14;
+  static constexpr int BARS = 2 * STAGES + 16;
+  static constexpr bool OVER = D > 64;           // P lies over the scores it came from (else beside O)
   static constexpr int LIST = AP_MAX_LIST * 8;
   static constexpr size_t SMEM = 1024 + static_cast<size_t>(2 + STAGES) * TILE + LIST + BARS * 8 + 64;
 };
@@ -115,7 +118,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   // [2] each: per tile; part h of the probabilities of tile t at 8 (2 t + h)
   const uint32_t bar_q_full = b0, bar_q_empty = b0 + 16, bar_s_full = b0 + 32, bar_p_full = b0 + 48, bar_o_full = b0 + 80;
   const uint32_t bar_turn = b0 + 96;                            // [2]: the tile may issue its next batch of products
-  const uint32_t bar_kv_full = b0 + 112, bar_kv_empty = bar_kv_full + 8 * L::STAGES;
+  const uint32_t bar_p_read = b0 + 112;                         // [2]: the products that read the tile's probabilities are complete
+  const uint32_t bar_kv_full = b0 + 128, bar_kv_empty = bar_kv_full + 8 * L::STAGES;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + L::BARS);
   int* s_total = reinterpret_cast<int*>(tmem_slot + 1);
 
@@ -127,6 +131,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       mbar_init(bar_s_full + 8 * i, 1);
       mbar_init(bar_o_full + 8 * i, 1);
       mbar_init(bar_turn + 8 * i, 1);
+      mbar_init(bar_p_read + 8 * i, 1);
     }
     for (int i = 0; i < 4; ++i) mbar_init(bar_p_full + 8 * i, 4);
     for (int i = 0; i < L::STAGES; ++i) {
@@ -264,7 +269,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     // ------------------------------------------------------------------ softmax and output
     const int t = warp >> 2, row = tid & 127;
     const uint32_t t_lane = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-    const uint32_t s_addr = t_lane + t * 128, o_addr = t_lane + 256 + t * 128;
+    const uint32_t s_addr = t_lane + t * 128, o_addr = t_lane + 256 + t * 128, p_addr = L::OVER ? s_addr : o_addr + 64;
     uint32_t ring = 0, sn = 0, on = 0;
     const float c = p.c;
     for (int r = 0; !failed; ++r) {
@@ -343,7 +348,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             ls[i & 1] = add2(ls[i & 1], pair2(e0, e1));
             w[i] = ap_pack(e0, e1);
           }
-          tmem_st32(s_addr + h * 32, w);
+          tmem_st32(p_addr + h * 32, w);
           tmem_wait_st();
           tc_fence_before();
           __syncwarp();
@@ -431,17 +436,19 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       const int t = warp - 9;
       const uint32_t idesc_s = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, 128, 128);
       const uint32_t idesc_o = make_idesc(ACC_F32, FMT_BF16, FMT_BF16, 128, D, 0, 1);
-      const uint32_t d_s = tmem_base + t * 128, d_o = tmem_base + 256 + t * 128;
+      const uint32_t d_s = tmem_base + t * 128, d_o = tmem_base + 256 + t * 128, d_p = L::OVER ? d_s : d_o + 64;
       const uint32_t q_lo = desc_lo(smem_u32(sQ) + t * L::TILE, 16), k_lo = desc_lo(smem_u32(sKV), 16), v_lo = desc_lo(smem_u32(sKV), L::SUB);
       const uint32_t q_full = bar_q_full + 8 * t, q_empty = bar_q_empty + 8 * t, s_full = bar_s_full + 8 * t, p_full = bar_p_full + 16 * t,
-                     o_full = bar_o_full + 8 * t;
-      uint32_t ring = 0, qn = 0, pn = 0;
+                     o_full = bar_o_full + 8 * t, p_read = bar_p_read + 8 * t;
+      uint32_t ring = 0, qn = 0, pn = 0, rn = 0;
       auto kv_ready = [&](uint32_t pos) { return mma_wait(bar_kv_full + 8 * (pos % L::STAGES), (pos / L::STAGES) & 1); };
       auto kv_done = [&](uint32_t pos) { umma_commit(bar_kv_empty + 8 * (pos % L::STAGES)); };
       // The tiles take turns, one batch of products (O += P V, next S) each.
       uint32_t turn = 0;
       auto my_turn = [&]() { return mma_wait(bar_turn + 8 * t, (turn++ & 1) ^ (t == 0)); };
       auto your_turn = [&]() { mbar_arrive(bar_turn + 8 * (t ^ 1)); };
+      // Scores that will overwrite probabilities wait for the products that read them, the last ones this thread has committed to p_read.
+      auto p_is_read = [&]() { return !L::OVER || rn == 0 || mma_wait(p_read, (rn - 1) & 1); };
       // S = Q K^T with the K block of ring position `pos`
       auto scores = [&](uint32_t pos) {
         const uint32_t kb = k_lo + (pos % L::STAGES) * (L::TILE >> 4);
@@ -458,7 +465,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         const int n = t ? it.n[1] : it.n[0];
         if (n && !mma_wait(q_full, qn++ & 1)) return false;
         if (max(it.n[0], it.n[1])) {
-          if (!kv_ready(ring) || !my_turn()) return false;
+          if (!kv_ready(ring) || (n && !p_is_read()) || !my_turn()) return false;
           tc_fence_after();
           if (n) scores(ring);
           your_turn();
@@ -487,13 +494,21 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
               const uint32_t vb = v_lo + (vpos % L::STAGES) * (L::TILE >> 4);
               // 16 keys per product, half of them with each part of P
 #pragma unroll
-              for (int k = 0; k < 4; ++k) mma_ts(d_o, d_s + k * 8, vb + k * 128, idesc_o, k || j);
+              for (int k = 0; k < 4; ++k) mma_ts(d_o, d_p + k * 8, vb + k * 128, idesc_o, k || j);
               if (!mma_wait(p_full + 8, pn++ & 1)) { failed = true; break; }
               tc_fence_after();
 #pragma unroll
-              for (int k = 4; k < 8; ++k) mma_ts(d_o, d_s + k * 8, vb + k * 128, idesc_o, 1);
-              if (j + 1 < n) scores(vpos + 1);
-              else umma_commit(o_full);
+              for (int k = 4; k < 8; ++k) mma_ts(d_o, d_p + k * 8, vb + k * 128, idesc_o, 1);
+              if constexpr (L::OVER) {
+                umma_commit(p_read);
+                ++rn;
+              }
+              if (j + 1 == n) umma_commit(o_full);
+              else {
+                if (!p_is_read()) { failed = true; break; }
+                tc_fence_after();
+                scores(vpos + 1);
+              }
             }
             your_turn();
             kv_done(vpos);

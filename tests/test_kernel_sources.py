@@ -53,3 +53,17 @@ def test_registers_are_only_taken_where_the_launch_has_them(name):
     decision: the host has to ask before it launches, and the shares have to add up."""
     code = code_of(name)
     assert re.search(r"numRegs", code) and re.search(r"static_assert\([^;]*REGS", code), f"{name} trusts the compiler's register count"
+
+
+@pytest.mark.parametrize("name", [n for n in SOURCES if re.search(r"\bmma_ts\(", code_of(n))])
+def test_scores_wait_for_the_product_that_reads_what_they_overwrite(name):
+    """Only products into one accumulator, of one shape, are promised to run in the order they were issued in.  Scores that are written over
+    probabilities therefore wait until the product that reads these is complete: a wait lies between the last such product and the
+    next scores, and one ahead of the first scores of an item where the item before may still be read."""
+    code = code_of(name)
+    last = [m.start() for m in re.finditer(r"\bmma_ts\(", code)][-1]
+    nxt = re.search(r"(?<!auto )\bscores\(", code[last:])
+    assert nxt, "scores are issued behind the products with probabilities"
+    assert re.search(r"p_is_read\(\)|mma_wait\(o_full", code[last:last + nxt.start()]), f"{name}: nothing keeps the next scores behind the product that reads"
+    begin = re.search(r"auto begin = .*?scores\(", code, re.S)
+    assert not begin or "p_is_read()" in begin.group(0), f"{name}: the first scores of an item"
