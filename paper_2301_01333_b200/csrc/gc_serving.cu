@@ -313,7 +313,8 @@ gc_status_t check_evict(const char* who, const gc_kv4_cache_t* c, const gc_kv4_e
   if (!d) REFUSE(GC_ERR_INVALID_ARG, "%s: null argument", who);
   if (d->batch < 0 || d->max_length < 0) REFUSE(GC_ERR_SHAPE, "%s: negative size", who);
   if (d->keep < 0 || d->recent < 0 || d->recent > d->keep) REFUSE(GC_ERR_INVALID_ARG, "%s: keep %d, of them recent %d", who, d->keep, d->recent);
-  if (d->max_length > 0x7FFFFFFF - 65536) REFUSE(GC_ERR_UNSUPPORTED, "%s: max_length too large", who);
+  // (positions, old and new, are counted up by all threads of a cluster at a time: room for a step of them)
+  if (d->max_length > 0x7FFFFFFF - 65536 || d->keep > 0x7FFFFFFF - 65536) REFUSE(GC_ERR_UNSUPPORTED, "%s: max_length or keep too large", who);
   const int64_t units = static_cast<int64_t>(d->batch) * c->kv_heads;
   if (units > (1 << 24) || units * d->keep > 0x7FFFFFFF || (units << 8) > 0x7FFFFFFF)
     REFUSE(GC_ERR_UNSUPPORTED, "%s: batch times heads times tokens to keep too large", who);

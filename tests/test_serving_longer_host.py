@@ -72,6 +72,16 @@ def test_evict_refusals(S):
     B.gc_kv4_evict(0, cache(), evict(batch=0), None, 0)
 
 
+def test_evict_refuses_budgets_that_leave_no_room_to_count(S):
+    # new positions are counted in 32 bits, a cluster's threads (8 x 1024) at a time: the last step may not pass 2^31
+    top = (1 << 31) - 1
+    for keep in (top - 65535, top - 8191, top):
+        refused(UNSUPPORTED, lambda: B.gc_kv4_evict_workspace_bytes(cache(kv_heads=1), evict(keep=keep)))
+        refused(UNSUPPORTED, lambda: B.gc_kv4_evict(0, cache(kv_heads=1), evict(keep=keep), P, 1 << 40))
+        refused(UNSUPPORTED, lambda: B.gc_kv4_evict_workspace_bytes(cache(kv_heads=1), evict(keep=0, recent=0, max_length=keep, table_width=1 << 30)))
+    assert B.gc_kv4_evict_workspace_bytes(cache(kv_heads=1), evict(keep=top - 65536)) == 0
+
+
 def test_lse_refusals(S):
     refused(ARG, lambda: B.gc_attention_kv4_lse(0, cache(), attend(), 0, None, 0))
     refused(ALIGN, lambda: B.gc_attention_kv4_lse(0, cache(), attend(), P + 2, None, 0))
