@@ -388,12 +388,13 @@ gc_status_t gc_attention_kv4_lse(void* cuda_stream, const gc_kv4_cache_t* cache,
  * any number; its new tokens' keys and values have been appended and lengths[b] counts them:
  *   out[i, h] = softmax_t(scale * q[i, h] . K[t]) V over the cached tokens t < lengths[b] - nq + 1 + (i - cu_q[b])
  * A row that sees nothing (more new tokens than length) is zero; rows no sequence owns are left as they were.  q, out bf16, rows 16-byte
- * aligned.  Products of fp16 operands summed in fp32: K and V are the values held rounded to fp16, which may not exceed 65504 in size (that is
- * recorded in the status word; below 2^-14 they lose relative accuracy), elements of q keep an absolute 2^-39 of the largest among 32 neighbouring rows, and
+ * aligned.  Products of fp16 operands summed in fp32.  K and V may not exceed 65504 in size (that is recorded in the status word); they are rounded
+ * to fp16, lo and scale of a group first: the values held but for 2^-11 of each and 2^-20 besides, or, where the largest of a sequence and head lies
+ * below 2^-8 (by |lo| + 16 |scale|), 2^-33 of that and 2^-120.  Elements of q keep an absolute 2^-39 of the largest among 32 neighbouring rows, and
  * probabilities are rounded to fp16.  block_table, max_length: as for gc_attention_kv4, and so is what else the status
  * word reports (scores above 2^26 in size, pages and lengths out of bounds), offsets that
- * decrease or leave the packed tokens besides.  What a row does not see has no influence on it, whatever is held there; a
- * group that is not finite counts as NaN.  Sequences may share pages. */
+ * decrease or leave the packed tokens besides.  What a row does not see has no influence on it but for the accuracies above, whatever is
+ * held there; a group that is not finite counts as NaN.  Sequences may share pages. */
 typedef struct {
   int32_t batch, q_heads;
   int64_t q_tokens;              /* rows of q / out in all */

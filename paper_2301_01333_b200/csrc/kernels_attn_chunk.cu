@@ -6,6 +6,11 @@
 // rounding of K alone puts the output off by 3-5e-3 of its norm, which is mostly cancellation, where the output's own rounding is 1.7e-3.)  Q, bf16,
 // becomes fp16 after a warp's 32 rows are scaled by one power of two: exactly down to 2^-31 of their largest element, with an error of
 // 2^-39 of it below; probabilities, at most 2^4 relative to the reference, are lifted by 2^11.
+// K and V so small that fp16 has few bits left for them are widened in units of a power of two, one for each of the two and a CTA's part of an
+// item, which the factor of the scores, and that of O at the end, make up for.  Where a part's first block is of ordinary size the unit is 1
+// and nobody looks any further (22.7 -> 23.0 us for the step below, 176 -> 179 and 317 -> 320 for the other two); else the widening
+// warps look through the parameters of all of its blocks first.  (With units that change along a part, as larger values come: 415 us for the
+// last, for what the softmax has to look at in every block.)
 //
 // A row is a (token, query head) of those that share a key/value head, token by token, so that a block of keys, once widened, serves
 // all of them.  A CTA holds 256 rows in two tiles of 128, and per block of 128 keys at width 128 there are
@@ -53,6 +58,10 @@ constexpr int CK_FLAGS = 8;                  // blocks whose notes of values tha
 constexpr float CK_RAISE = 4.0f;             // binades a score may exceed the reference by
 constexpr float CK_LIFT = 11.0f;             // binades the probabilities are lifted by: at most 2^15, and whole down to 2^-25 of the reference
 constexpr float CK_LARGEST = 65504.0f;       // the largest fp16
+// Keys and values whose largest lies below 2^CK_SMALL are widened in units of 2^-CK_MOST_UNIT at least, in which it lies from 2^CK_TOP to twice
+// that.  (A value is off by half a step, or by 2^-25 where that is more, and as much for lo and 15 times as much for its scale, which
+// are rounded first: by 17 2^-25 in all, or 17 2^-38 of the largest.)
+constexpr int CK_SMALL = -8, CK_TOP = 13, CK_MOST_UNIT = 100;
 template <int D, int G>
 struct ChunkLayout {
   static constexpr int NSUB = (D + 63) / 64;     // 64-element sub-tiles of 128-byte rows
@@ -62,9 +71,10 @@ struct ChunkLayout {
   // codes and parameters of 128 key rows, K's or V's, as they lie in memory, and how many of these there are
   static constexpr int NG = D / G, PITCH = D / 2, CODES = 128 * PITCH, STAGED = CODES + 128 * NG * 4, AHEAD = D == 64 ? 8 : 3;
   static constexpr int BARS = 2 * STAGES + 2 * AHEAD + 16;
-  // Q, ring, staged codes, list, notes [CK_FLAGS][4 groups][4 words], one word a block that sums them up, sums of the second tile [3][128]
-  static constexpr int LIST = CK_MAX_LIST * 8, NOTES = CK_FLAGS * 16 * 4, ANY = CK_FLAGS * 4, SUMS = 3 * 128 * 4;
-  static constexpr size_t SMEM = 1024 + static_cast<size_t>(2 + STAGES) * TILE + AHEAD * STAGED + LIST + NOTES + ANY + SUMS + BARS * 8 + 64 * 4;
+  // Q, ring, staged codes, list, notes [CK_FLAGS][4 groups][4 words], one word a block that sums them up, one a part with its units, sums of
+  // the second tile [3][128]
+  static constexpr int LIST = CK_MAX_LIST * 8, NOTES = CK_FLAGS * 16 * 4, ANY = CK_FLAGS * 4, UNITS = CK_FLAGS * 4, SUMS = 3 * 128 * 4;
+  static constexpr size_t SMEM = 1024 + static_cast<size_t>(2 + STAGES) * TILE + AHEAD * STAGED + LIST + NOTES + ANY + UNITS + SUMS + BARS * 8 + 64 * 4;
 };
 
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
@@ -83,9 +93,10 @@ __device__ __forceinline__ bool fits_half(uint32_t par, uint32_t* status) {
   if (fabsf(lo) < INFINITY && fabsf(scale) < INFINITY) report(status, DEV_LARGE_HALF);
   return false;
 }
-__device__ __forceinline__ Params16 params16(uint32_t par) {
-  const uint32_t lo = pack_half(__uint_as_float(par << 16), __uint_as_float(par << 16));
-  const uint32_t scale = pack_half(__uint_as_float(par & 0xffff0000u), __uint_as_float(par & 0xffff0000u));
+// (by: what they are multiplied by, a power of two)
+__device__ __forceinline__ Params16 params16(uint32_t par, float by) {
+  const float l = __uint_as_float(par << 16) * by, c = __uint_as_float(par & 0xffff0000u) * by;
+  const uint32_t lo = pack_half(l, l), scale = pack_half(c, c);
   return Params16{lo, scale};
 }
 
@@ -329,6 +340,41 @@ struct Note {
   int rows, q0, row0, h;
   int ends, pad[3];
 };
+
+// 2^n for n from -126 to 127.
+__device__ __forceinline__ float exp2_of(int n) { return __uint_as_float(static_cast<uint32_t>(127 + n) << 23); }
+// What the values of a group do not exceed in size, as bits; zero where they are not finite.
+__device__ __forceinline__ uint32_t size_of(uint32_t par) {
+  const float u = fmaf(16.f, fabsf(__uint_as_float(par & 0xffff0000u)), fabsf(__uint_as_float(par << 16)));
+  return u < INFINITY ? __float_as_uint(u) : 0u;
+}
+// u for units of 2^-u.
+__device__ __forceinline__ bool is_small(uint32_t size) { return size < static_cast<uint32_t>(127 + CK_SMALL) << 23; }
+__device__ __forceinline__ uint32_t unit_of(uint32_t size) {
+  return size == 0 || !is_small(size) ? 0u : static_cast<uint32_t>(min(CK_TOP + 127 - static_cast<int>(size >> 23), CK_MOST_UNIT));
+}
+// The unit of the keys, or values, of a part of an item, whose first block's parameters are staged at `staged`: each widening warp finds it for
+// itself, and only calls this (out of line: their loop is at its best when it is short) where all that it has of that block is small.
+template <int D, int G>
+__device__ __noinline__ uint32_t unit_of_part(const ChunkParams& p, const uint32_t* params, uint32_t staged, int b, int h, int j0, int j1, int len, int lane) {
+  constexpr int NG = D / G;
+  uint32_t size = 0;
+  for (int i = lane; i < 128 * NG; i += 32)
+    if (i / NG < len - j0 * 128) size = max(size, size_of(lds32(staged + i * 4)));
+  size = __reduce_max_sync(0xffffffffu, size);
+  if (!is_small(size)) return 0;
+  const int* table = p.table + b * p.table_stride;
+  const int end = min(j1 * 128, len);
+#pragma unroll 4
+  for (int t = (j0 + 1) * 128 + lane; t < end; t += 32) {
+    const int page = table[t >> p.page_shift];
+    if (page < 0 || page >= p.num_pages) continue;               // (reported where it is copied)
+    const int64_t at = (((static_cast<int64_t>(page) * p.Hk + h) << p.page_shift) + (t & ((1 << p.page_shift) - 1))) * NG;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) size = max(size, size_of(params[at + g]));
+  }
+  return unit_of(__reduce_max_sync(0xffffffffu, size));
+}
 }  // namespace
 
 // Workspace: pieces [ctas][2][D / 4][256] of four columns, their (reference, sum) [ctas][2][256], notes [ctas], and the list
@@ -370,7 +416,8 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
   uint2* s_list = reinterpret_cast<uint2*>(s_staging + L::AHEAD * L::STAGED);
   uint32_t* s_notes = reinterpret_cast<uint32_t*>(s_list + CK_MAX_LIST);        // [CK_FLAGS][4][4]
   uint32_t* s_any = s_notes + CK_FLAGS * 16;                    // [CK_FLAGS], a byte per widening warp
-  float* s_second = reinterpret_cast<float*>(s_any + CK_FLAGS); // reference, sum and groups that are not finite of tile 1
+  uint32_t* s_units = s_any + CK_FLAGS;                         // [CK_FLAGS] parts of items: bytes of K and V
+  float* s_second = reinterpret_cast<float*>(s_units + CK_FLAGS);       // reference, sum and groups that are not finite of tile 1
   uint64_t* bars = reinterpret_cast<uint64_t*>(s_second + 3 * 128);
   const uint32_t b0 = smem_u32(bars);
   const uint32_t bar_q_full = b0, bar_q_empty = b0 + 8, bar_s_full = b0 + 16, bar_p_full = b0 + 48, bar_o_full = b0 + 80;
@@ -500,7 +547,10 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_q_full);
       }
-      const float c = factor;                                   // c times the power of two the scores are short of
+      // The unit of this part's keys is known once they have been widened, as the first scores show (tile 1 may have none).
+      if (j_first < s.j1 && !__all_sync(0xffffffffu, mma_wait(bar_s_full + 16 * t, sn & 1))) { failed = true; break; }
+      // c times the power of two the scores are short of
+      const float c = factor * exp2_of(-static_cast<int>(reinterpret_cast<const volatile uint8_t*>(s_units + (qn - 1) % CK_FLAGS)[0]));
       // What was noted of block j's values, once a product that waited for them is known to be issued; they are overwritten eight blocks
       // on, when all rows have handed over probabilities made after this look.
       auto look = [&](int j) {
@@ -620,9 +670,10 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
         l = second ? fmaf(f0, l, f1 * l1) : f0 * l;
         m = mm;
       }
+      const float fall = exp2_of(-static_cast<int>(reinterpret_cast<const volatile uint8_t*>(s_units + (qn - 1) % CK_FLAGS)[1]));
       const bool whole = s.whole();
       const float rl = l == 0.f ? 0.f : whole ? 1.0f / l : 1.f;
-      const float a0 = f0 * rl, a1 = f1 * rl;
+      const float a0 = f0 * rl * fall, a1 = f1 * rl * fall;
       const int64_t piece = 2 * static_cast<int64_t>(me) + (s.j0 == 0);
       const int my_slot = my_row - s.row0;
       float4* po = space.o + piece * (D / 4) * CK_ROWS + my_slot;
@@ -694,10 +745,11 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
     uint32_t to[4];                                             // of the four stores of a chunk, in the first tile
 #pragma unroll
     for (int y = 0; y < 4; ++y) to[y] = smem_u32(sKV) + row0 * 128 + (((chunk0 * 4 + y) ^ (row0 & 7)) << 4);
-    uint32_t ring = 0, used = 0, block = 0;
+    uint32_t ring = 0, used = 0, block = 0, part = 0;            // part: number of the segment
     Seg s;
     while (!failed && walk.next(s)) {
       const int halves = 2 * (s.j1 - s.j0);
+      float k_by = 1.f, v_by = 1.f;
 #pragma unroll 1
       for (int i = 0; i < halves; ++i) {                        // K and V in turn
         const uint32_t stage = used % L::AHEAD, st = ring % L::STAGES;
@@ -743,6 +795,17 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
           }
           any = __any_sync(0xffffffffu, any);
         }
+        if (i < 2) {                                             // the part's first keys and values: their unit
+          bool ordinary = false;
+#pragma unroll
+          for (int k = 0; k < CH; ++k) ordinary |= !is_small(size_of(par[k]));
+          uint32_t u = 0;
+          if (left > (warp & 3) * 32 && !__any_sync(0xffffffffu, ordinary))
+            u = unit_of_part<D, G>(p, i ? p.v_params : p.k_params, smem_u32(s_staging) + stage * L::STAGED + L::CODES, s.b, s.h, s.j0, s.j1, s.len, lane);
+          if (warp == 8 && lane == 0) reinterpret_cast<uint8_t*>(s_units + part % CK_FLAGS)[i] = static_cast<uint8_t>(u);
+          if (i) v_by = exp2_of(static_cast<int>(u));
+          else k_by = exp2_of(static_cast<int>(u));
+        }
         // (A bulk copy may overwrite what was read only behind a fence between the two kinds of access: without it, calls in close succession
         // found codes of a later block in a tile's second half.)
         fence_proxy_async_smem();
@@ -754,7 +817,7 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
           const uint32_t word[4] = {code[k].x, code[k].y, code[k].z, code[k].w};
-          const Params16 x = params16(par[k]);
+          const Params16 x = params16(par[k], i & 1 ? v_by : k_by);
           // a nibble in the low bits of a number from 1024 on, or four bits up in one from 64 on: that plus the code; then the code
           // times scale plus lo in one rounding
           const __half2 m1024 = half2_of(0xe400e400u), m64 = half2_of(0xd400d400u), lo2 = half2_of(x.lo2), sc2 = half2_of(x.scale2);
@@ -780,6 +843,7 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
         if (lane == 0) mbar_arrive(bar_kv_full + 8 * st);
       }
       block += s.j1 - s.j0;
+      ++part;
     }
     if (failed && lane == 0) report(p.status, DEV_TIMEOUT_PRODUCER);
   } else {

@@ -194,7 +194,8 @@ class KV4Cache:
         """Attention of any number of new tokens per sequence, packed: q bf16 [q_tokens, q_heads, head_dim], of which sequence b owns rows
         cu_q[b] .. cu_q[b + 1] (int32 [batch + 1]; none, one or thousands).  Their keys and values have been appended, and
         lengths[b] counts them: row i of nq sees the first lengths[b] - nq + 1 + i tokens.  block_table, lengths, scale and max_length as
-        for ``attend``.  Keys and values enter rounded to fp16; one above 65504 in size is reported by ``query_status()``.  A row that sees nothing is zero; rows no sequence owns
+        for ``attend``.  Keys and values enter rounded to fp16; one above 65504 in size is reported by ``query_status()``, and beside larger ones
+        of its sequence and head they are off by up to 2^-20 (where none reaches 2^-8: by 2^-33 of the largest).  A row that sees nothing is zero; rows no sequence owns
         are left as they were in a given `out`, and are zero in one made here."""
         if not isinstance(q, torch.Tensor):
             raise TypeError("q must be a torch.Tensor")

@@ -210,6 +210,118 @@ def test_chunk_sizes_of_queries_and_keys(S, power_q, power_k):
     within(out, ref, tol + (2 * torch.expm1(torch.as_tensor(lost, device=DEV)) * 6 if power_k < -10 else 0))
 
 
+def lost(cache, params, table, i, m):
+    """What a key or value of sequence i may be off by besides half a step, [heads]: 17 2^-25, or, where a head's largest parameters (the size of
+    lo and of 16 scale together) are below 2^-8 and so in other units, 17 2^-38 of them, but 17 2^-125 at least."""
+    p = params[table[i, :-(-m // cache.page_size)].long()].transpose(1, 2).flatten(0, 1)[:m].double().abs()
+    u = (p[..., 0] + 16 * p[..., 1]).amax((0, 2))
+    return 17 * torch.where(u < 2.0 ** -8, 2.0 ** -38 * u + 2.0 ** -125, torch.full_like(u, 2.0 ** -25))
+
+
+def lifted_reference(cache, q, new, table, lens, scale):
+    """chunk_reference for keys and values of any size."""
+    g = q.shape[1] // cache.kv_heads
+    o = torch.zeros(q.shape, dtype=torch.float64, device=DEV)
+    tol = torch.zeros_like(o)
+    a = 0
+    for i, (n, m) in enumerate(zip(new, lens)):
+        if n and m:
+            k, v = held(cache, table, i, m)
+            k_off, v_off = lost(cache, cache.k_params, table, i, m), lost(cache, cache.v_params, table, i, m)
+            lim = (torch.arange(n, device=DEV) + m - n + 1).clamp(min=0)
+            last = (lim - 1).clamp(min=0)
+            for h in range(q.shape[1]):
+                qq, kk, vv = q[a:a + n, h].double(), k[:, h // g], v[:, h // g]
+                ref, size = R.head_all(qq, kk, vv, lim, scale)
+                top = scale * (qq.abs() @ kk.abs().T)
+                top = torch.cummax(top, -1).values.gather(1, last[:, None])          # of what the row sees
+                vmax = vv.abs().max()
+                expo = (U16 + (kk.shape[1] + 8) * U32) * top + scale * k_off[h // g] * qq.abs().sum(-1, keepdim=True) + 4 * U32
+                # (Means of the same values differ by twice the largest at most, whatever their weights: where scores are so large that their
+                # errors decide, the first term would be infinite.)
+                moved = torch.minimum(2 * expo.clamp(max=30).expm1() * size, 2 * vmax)
+                tol[a:a + n, h] = moved + (2 * U16 + (m + 16) * U32) * size + v_off[h // g] + m * 2.0 ** -36 * vmax + U[BF] * ref.abs()
+                o[a:a + n, h] = ref
+        a += n
+    return o, tol
+
+
+@pytest.mark.parametrize("d,group", SHAPES)
+@pytest.mark.parametrize("power_q,power_k,power_v", [(0, 0, -8), (40, -30, 0), (100, -90, -90), (0, -16, -16), (0, -20, -24), (12, -13, -13), (0, 0, -60), (-60, 10, -30)])
+def test_chunk_keys_and_values_of_any_size(S, d, group, power_q, power_k, power_v):
+    g = gen(5 + d)
+    new, lens, page = [37, 300, 1], [400, 1300, 5000], 16
+    count = sum(-(-m // page) for m in lens)
+    cache = filled_cache(S, count, page, 2, d, group, g)
+    cache.k_params.mul_(2.0 ** power_k)
+    cache.v_params.mul_(2.0 ** power_v)
+    table = table_of(lens, page, count, g)
+    q = (randn(sum(new), 4, d, g=g) * 2.0 ** power_q).to(BF)
+    scale = d ** -0.5 * 2.0 ** (-power_q - power_k)
+    out = cache.attend_chunk(q, i32([0] + new).cumsum(0).to(torch.int32), table, i32(lens), scale=scale)
+    cache.query_status()
+    ref, tol = lifted_reference(cache, q, new, table, lens, scale)
+    within(out, ref, tol)
+    assert (ref.abs().amax() > 16 * tol.amax()).all()            # an output of zeros, or of equal weights, would not pass
+    one = cache.attend(q[-1:, None].contiguous(), table[2:], i32(lens[2:]), scale=scale)[:, 0]
+    if power_v >= -30:                                           # (attend loses smaller values)
+        assert ((out[-1:].double() - one.double()).abs() <= 3 * tol[-1:] + 2 * U[BF] * 2.0 ** power_v).all()
+
+
+@pytest.mark.parametrize("d,group", [(64, 64), (96, 32), (128, 32), (128, 128)])
+@pytest.mark.parametrize("new,lens", [([9, 40], [1500, 700]), ([300], [2100]), ([5], [40000])])
+@pytest.mark.parametrize("ramp", ["up", "down", "steps", "zeros first"])
+def test_chunk_sizes_that_change_along_a_sequence(S, d, group, new, lens, ramp):
+    # keys and values that grow and shrink by dozens of binades, by token
+    g = gen(7)
+    page, hk = 32, 2
+    count = sum(-(-m // page) for m in lens)
+    cache = filled_cache(S, count, page, hk, d, group, g)
+    table = table_of(lens, page, count, g)
+    for i, m in enumerate(lens):
+        t = torch.arange(m, device=DEV)
+        x = t / m
+        by = {"up": -60 * (1 - x), "down": -60 * x, "steps": -20.0 * ((t // 300) % 3), "zeros first": torch.where(t < min(300, m // 2), -math.inf, -30.0)}[ramp].floor()
+        by = torch.exp2(by.clamp(max=0))[:, None, None, None]
+        at = table[i, t // page].long()
+        for p in (cache.k_params, cache.v_params):
+            p[at, :, t % page] = (p[at, :, t % page].float() * by).to(BF)
+    q = randn(sum(new), 4, d, g=g, dtype=BF)
+    for scale in (d ** -0.5, d ** -0.5 * 2.0 ** 20):             # scores that count, or only the small keys' (the large ones' decide their rows)
+        out = cache.attend_chunk(q, i32([0] + new).cumsum(0).to(torch.int32), table, i32(lens), scale=scale)
+        cache.query_status()
+        ref, tol = lifted_reference(cache, q, new, table, lens, scale)
+        within(out, ref, tol)
+
+
+def test_chunk_sizes_do_not_go_by_what_is_not_finite_or_behind_the_sequence(S):
+    # small keys and values next to groups of NaN and infinity, and to anything in the rest of the last page
+    g = gen(8)
+    d, m, n = 128, 333, 40
+    cache = filled_cache(S, 30, 16, 2, d, 32, g)
+    for x in (cache.k_params, cache.v_params):
+        x.mul_(2.0 ** -40)
+    table = table_of([m], 16, 30, g)
+    q = (randn(n, 4, d, g=g) * 2.0 ** 20).to(BF)
+    scale = d ** -0.5 * 2.0 ** 20
+    cu, ln = i32([0, n]), i32([m])
+    want = cache.attend_chunk(q, cu, table, ln, scale=scale)
+    ref, tol = lifted_reference(cache, q, [n], table, [m], scale)
+    within(want, ref, tol)
+    for x in (cache.k_params, cache.v_params):
+        x[table[0, m // 16], :, m % 16:] = 3.0
+    assert torch.equal(cache.attend_chunk(q, cu, table, ln, scale=scale), want)
+    cache.v_params[table[0, 3], 1, 5, 2] = math.nan              # head 1, elements 64 .. 95
+    cache.v_params[table[0, 9], 1, 6, 2, 1] = math.inf
+    cache.k_params[table[0, (m - 1) // 16], 0, (m - 1) % 16, 0, 0] = -math.inf       # the newest token's key of head 0: the last row
+    got = cache.attend_chunk(q, cu, table, ln, scale=scale)
+    seen = torch.zeros_like(got, dtype=torch.bool)
+    seen[:, 2:, 64:96] = True
+    seen[-1, :2] = True
+    assert torch.isnan(got[seen]).all() and torch.equal(got[~seen], want[~seen])
+    cache.query_status()
+
+
 @pytest.mark.parametrize("power", [40, 0, -60])
 def test_chunk_infinite_queries_leave_their_neighbours_scale(S, power):
     # rows are scaled by a power of two, exactly: without the infinity the other rows are the same to the last bit
