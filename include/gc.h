@@ -380,7 +380,8 @@ gc_status_t gc_attention_kv4_workspace_bytes(const gc_kv4_cache_t* cache, const 
 gc_status_t gc_attention_kv4(void* cuda_stream, const gc_kv4_cache_t* cache, const gc_attention_kv4_t* d,
                              void* workspace_dev, size_t workspace_bytes);
 /* The same, and lse[b, j, h] (fp32, dense [batch, queries, q_heads]) = log sum_t exp(scale * q[b, j, h] . K[t]) over the tokens the
- * query sees: what gc_kv4_weigh needs; minus infinity where it sees none. */
+ * query sees: what gc_kv4_weigh needs; minus infinity where it sees none.  Off by up to 2^-18 (exponents are rounded at a size of 64 binades)
+ * besides the roundings of numbers of its own size. */
 gc_status_t gc_attention_kv4_lse(void* cuda_stream, const gc_kv4_cache_t* cache, const gc_attention_kv4_t* d, float* lse_dev,
                                  void* workspace_dev, size_t workspace_bytes);
 

@@ -200,8 +200,8 @@ __device__ __forceinline__ int sequence_at(const Kv4AttnParams& p, int64_t at, i
 }
 
 // The logarithm of the sum of a column's exponentials, from its reference (in binades) and the sum relative to it, which carries
-// a factor of 2^64; minus infinity where the column saw nothing.
-__device__ __forceinline__ float log_of_sum(float m, float l) { return l == 0.f ? -INFINITY : (m + (log2f(l) - 64.f)) * 0.693147180559945309f; }
+// a factor of 2^64 (taken out before the logarithm, which has a step of 2^-17 beyond 64); minus infinity where the column saw nothing.
+__device__ __forceinline__ float log_of_sum(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l * 0x1p-64f)) * 0.693147180559945309f; }
 __device__ __forceinline__ float* lse_of(const Kv4AttnParams& p, int b, int query, int head) {
   return p.lse + (static_cast<int64_t>(b) * p.n + query) * p.Hq + head;
 }

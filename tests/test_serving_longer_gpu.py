@@ -479,6 +479,52 @@ def test_weigh_many_columns(S, n, hq, hk):
     weigh_case(S, [500, 16, 129], n, hq, hk, 64, 32, 16, seed=n + hq, decay=0.5)      # up to 640 of them: several passes
 
 
+@pytest.mark.parametrize("lens", [[1, 2, 3, 5, 7, 11, 31], [100, 333, 511], [1000, 1023], [4099], [12345, 3]])
+@pytest.mark.parametrize("n,hq,hk", [(1, 4, 4), (3, 16, 2)])
+def test_logarithms_and_weights_of_equal_scores(S, lens, n, hq, hk):
+    # Queries of zero: t tokens seen weigh 1 / t each, and the sum of their exponentials is t exactly.  Its logarithm is off by a step or so of the
+    # function and half a step of the constant and of the product, 6 U32 of itself; a weight by that, its exponent's product and the exponential.
+    g = gen(sum(lens))
+    page = 16
+    count = sum(-(-m // page) for m in lens)
+    cache = filled_cache(S, count, page, hk, 64, 32, g)
+    table, ln = table_of(lens, page, count, g), i32(lens)
+    q = torch.zeros(len(lens), n, hq, 64, dtype=BF, device=DEV)
+    lse = torch.empty(len(lens), n, hq, device=DEV)
+    cache.attend(q, table, ln, lse=lse)
+    seen = torch.tensor(lens, device=DEV)[:, None] - (n - 1) + torch.arange(n, device=DEV)
+    ref = torch.where(seen > 0, seen.clamp(min=1).double().log(), -math.inf)[..., None].expand(-1, -1, hq)
+    some = ref > -math.inf
+    assert torch.equal(lse == -math.inf, ~some)
+    assert ((lse.double() - ref)[some].abs() <= 6 * U32 * ref[some]).all()
+    w = cache.weigh(cache.new_weights(), q, lse, table, ln)
+    cache.query_status()
+    for i, m in enumerate(lens):
+        t = torch.arange(m, device=DEV)
+        got = w[table[i, t // page].long(), :, t % page].double()
+        want = sum((t < s).double() / max(int(s), 1) * (hq // hk) for s in seen[i])[:, None]
+        assert ((got - want).abs() <= (10 * math.log(m + 1) + 4 + n * hq) * U32 * want).all()
+
+
+@pytest.mark.parametrize("d,group", SHAPES)
+def test_weight_of_a_single_token_is_one(S, d, group):
+    # What attend and weigh make of a score is the same number.  The exponent of its weight in attend stands near 64, half a step there is 2^-18
+    # binades; the logarithm, the score and their difference are off by half steps of numbers up to their size (the score's power of two, 1.45 times it).
+    g = gen(d)
+    cache = filled_cache(S, 9, 16, 2, d, group, g)
+    table, ln = torch.arange(9, device=DEV, dtype=torch.int32)[:, None], torch.ones(9, dtype=torch.int32, device=DEV)
+    q = randn(9, 1, 8, d, g=g, dtype=BF)
+    lse = torch.empty(9, 1, 8, device=DEV)
+    cache.attend(q, table, ln, lse=lse)
+    for h in range(4):                                           # one query head of a key/value head at a time
+        alone = torch.full_like(lse, -math.inf)
+        alone[..., [h, h + 4]] = lse[..., [h, h + 4]]
+        w = cache.weigh(cache.new_weights(), q, alone, table, ln)
+        off = (w[:, :, 0].double() - 1).abs()
+        assert (off <= math.log(2) * 2.0 ** -18 + 8 * U32 * (1 + 1.45 * alone[:, 0, [h, h + 4]].double().abs())).all()
+        assert (w[:, :, 1:] == 0).all()
+
+
 @pytest.mark.parametrize("decay,out", [(1.0, True), (0.5, False), (0.0, True), (0.0, False)])
 def test_weigh_decay_and_output(S, decay, out):
     weigh_case(S, [100, 64, 65], 2, 8, 2, 128, 64, 32, seed=3, decay=decay, out=out)
