@@ -418,7 +418,8 @@ gc_status_t gc_attention_kv4_chunk(void* cuda_stream, const gc_kv4_cache_t* cach
  *   out[t, hk] = decay * weights[t, hk] + sum over queries j that see t and query heads h that share hk of exp(scale * q[b, j, h] . K[t] - lse[b, j, h])
  * with q, lengths, block_table, max_length and scale as in the attention call, and the lse it gave.  A query whose lse is minus infinity
  * adds nothing; with a decay of 0 what `weights` holds is not looked at.  out may be weights; other places of it are left as they
- * were.  All in fp32 from the exact values held.  A page may be named by one sequence of a call only. */
+ * were.  Sums in fp32 from the exact keys held; elements of a query keep an absolute 2^-36 of its largest.  A page may be named by one sequence of
+ * a call only. */
 typedef struct {
   int32_t batch, queries, q_heads, table_width;
   int64_t table_stride;
