@@ -275,9 +275,6 @@ int page_shift_of(const gc_kv4_cache_t& c) {
   return s;
 }
 
-// A CTA of the chunk kernel takes at least four units of work, a block and a half of keys.
-constexpr int CHUNK_LEAST_LOG = 2;
-
 gc_status_t check_chunk(const char* who, const gc_kv4_cache_t* c, const gc_attention_kv4_chunk_t* d) {
   gc_status_t st = check_cache(who, c);
   if (st != GC_OK) return st;
@@ -302,7 +299,7 @@ struct ChunkLaunch {
 ChunkLaunch lay_out_chunk(const gc_kv4_cache_t& c, const gc_attention_kv4_chunk_t& d, int sms) {
   ChunkLaunch s;
   s.items = attn_chunk_items(d.q_tokens, d.batch, d.q_heads / c.kv_heads);
-  s.ctas = attn_chunk_ctas(s.items, c.kv_heads, d.max_length, CHUNK_LEAST_LOG, sms);
+  s.ctas = attn_chunk_ctas(s.items, c.kv_heads, d.max_length, sms);
   s.bytes = attn_chunk_bytes(c.head_dim, s.ctas, s.items);
   return s;
 }
@@ -373,7 +370,7 @@ extern "C" gc_status_t gc_attention_kv4_chunk(void* cuda_stream, const gc_kv4_ca
   ChunkParams p = {};
   p.B = d->batch; p.Hq = d->q_heads; p.Hk = cache->kv_heads; p.g = d->q_heads / cache->kv_heads;
   p.page_shift = page_shift_of(*cache); p.max_len = d->max_length;
-  p.least_log = CHUNK_LEAST_LOG; p.most_items = static_cast<int>(l.items);
+  p.most_items = static_cast<int>(l.items);
   p.q_tokens = d->q_tokens; p.num_pages = cache->num_pages; p.table_stride = d->table_stride;
   p.c = d->scale * 1.4426950408889634f;
   p.q = static_cast<const __nv_bfloat16*>(d->q.data);

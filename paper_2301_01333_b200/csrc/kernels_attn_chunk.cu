@@ -53,6 +53,10 @@ namespace {
 constexpr int CK_THREADS = 512, CK_ROWS = 256;
 constexpr int CK_MAX_LIST = 160;             // items per head that are listed in shared memory
 constexpr int CK_START = 6, CK_BLOCK = 3, CK_TWIN_BLOCK = 2;      // what beginning an item and a block of its keys cost, in units of about 1700 clocks
+// A CTA takes at least this many units.  The joining kernel reads a piece of every CTA between an item's first and last, so that a
+// stretch has to have some block's first unit in it, wherever it begins inside an item.
+constexpr int CK_LEAST = 4;
+static_assert(CK_LEAST >= CK_BLOCK && CK_LEAST >= CK_TWIN_BLOCK, "a stretch could lie inside one block, and its piece would not be written");
 constexpr int CK_FETCH = 6;                  // blocks of keys that are called into the L2 ahead of their copies
 constexpr int CK_FLAGS = 8;                  // blocks whose notes of values that are not finite are kept
 constexpr float CK_RAISE = 4.0f;             // binades a score may exceed the reference by
@@ -470,9 +474,9 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
   // kernel's end, and this one for the columns.
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t tmem_base = *tmem_slot;
-  // Stretches of at least 2^least_log units: fewer CTAs work where there is little to do.
+  // Stretches of at least CK_LEAST units: fewer CTAs work where there is little to do.
   const int64_t total = static_cast<int64_t>(size.y) * p.Hk;
-  const int64_t fill = (total + (1 << p.least_log) - 1) >> p.least_log;
+  const int64_t fill = quotient(total, CK_LEAST);
   const int working = fill < ctas ? max(static_cast<int>(fill), 1) : ctas, me = static_cast<int>(blockIdx.x);
   const Cuts cuts(total, working);
   Walk<List> walk(p, list, size.x, size.y, me < working ? cuts.at(me) : 0, me < working ? cuts.at(me + 1) : 0);
@@ -1138,10 +1142,10 @@ size_t space_bytes(int ctas, int64_t most_items) {
 }  // namespace
 
 // Items per head there can be at most (a sequence's last one may be short), and CTAs for them: one an SM, or one for every
-// 2^least_log blocks of keys where that is fewer.
+// CK_LEAST units there can be where that is fewer.
 int64_t attn_chunk_items(int64_t q_tokens, int B, int g) { return q_tokens * g / CK_ROWS + B; }
-int attn_chunk_ctas(int64_t items, int Hk, int max_len, int least_log, int num_sms) {
-  const int64_t units = items * Hk * (((max_len + 127) / 128 + 1) * CK_BLOCK + CK_START), want = (units >> least_log) + 1;
+int attn_chunk_ctas(int64_t items, int Hk, int max_len, int num_sms) {
+  const int64_t units = items * Hk * (((max_len + 127) / 128 + 1) * CK_BLOCK + CK_START), want = units / CK_LEAST + 1;
   return static_cast<int>(want < num_sms ? want : num_sms);
 }
 size_t attn_chunk_bytes(int D, int ctas, int64_t most_items) {

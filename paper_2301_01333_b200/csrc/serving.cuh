@@ -79,7 +79,7 @@ cudaError_t launch_attn_kv4(const Kv4AttnParams& p, int head_dim, int group, cud
 struct ChunkParams {
   int B, Hq, Hk, g;
   int page_shift, max_len;
-  int least_log, most_items;        // a CTA takes at least 2^least_log units; items per head there can be
+  int most_items;                   // items per head there can be
   int64_t q_tokens, num_pages, table_stride;
   float c;                          // scale * log2(e)
   const __nv_bfloat16* q;
@@ -97,7 +97,7 @@ struct ChunkParams {
   uint32_t* status;
 };
 int64_t attn_chunk_items(int64_t q_tokens, int B, int g);
-int attn_chunk_ctas(int64_t items, int Hk, int max_len, int least_log, int num_sms);
+int attn_chunk_ctas(int64_t items, int Hk, int max_len, int num_sms);
 size_t attn_chunk_bytes(int D, int ctas, int64_t most_items);
 cudaError_t launch_attn_chunk(const ChunkParams& p, int head_dim, int group, int ctas, cudaStream_t s);
 

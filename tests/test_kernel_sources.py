@@ -67,3 +67,15 @@ def test_scores_wait_for_the_product_that_reads_what_they_overwrite(name):
     assert re.search(r"p_is_read\(\)|mma_wait\(o_full", code[last:last + nxt.start()]), f"{name}: nothing keeps the next scores behind the product that reads"
     begin = re.search(r"auto begin = .*?scores\(", code, re.S)
     assert not begin or "p_is_read()" in begin.group(0), f"{name}: the first scores of an item"
+
+
+def test_every_stretch_of_the_chunk_attention_has_a_block_to_write():
+    """The joining kernel reads a piece of every CTA between an item's first and last: a stretch that lay inside one block of keys would leave its
+    piece unwritten.  The CTAs at work are as many as get CK_LEAST units each, whatever the total comes to."""
+    code = code_of("kernels_attn_chunk.cu")
+    value = {k: int(v) for k, v in re.findall(r"\b(CK_LEAST|CK_START|CK_BLOCK|CK_TWIN_BLOCK) = (\d+)", code)}
+    assert re.search(r"fill = quotient\(total, CK_LEAST\);", code) and re.search(r"static_assert\(CK_LEAST >= CK_BLOCK", code)
+    for total in range(value["CK_START"] + min(value["CK_BLOCK"], value["CK_TWIN_BLOCK"]), 5000):
+        for ctas in (1, 2, 7, 148):
+            working = min(max(total // value["CK_LEAST"], 1), ctas)
+            assert total // working >= value["CK_LEAST"] >= max(value["CK_BLOCK"], value["CK_TWIN_BLOCK"])
