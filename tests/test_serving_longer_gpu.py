@@ -130,6 +130,24 @@ def test_chunk_more_sequences_than_the_list_in_shared_memory(S, d, group):
     chunk_case(S, [3] * 161, [40] * 161, 4, 2, d, group, 16, seed=3)
 
 
+@pytest.mark.parametrize("count", [156, 157, 158])
+def test_chunk_lists_of_either_kind_about_full(S, count):
+    # (3 count + 3) rows of two heads: at most 159, 160 and 161 items a head, of which 160 fit the list in shared memory
+    chunk_case(S, [3] * count, [40 + i % 5 for i in range(count)], 4, 2, 64, 64, 16, seed=count)
+
+
+def test_chunk_list_in_shared_memory_full_of_items(S):
+    chunk_case(S, [1] * 160, [1 + 3 * i for i in range(160)], 1, 1, 64, 64, 16, seed=4, tail=0)      # 160 rows: 160 items
+    chunk_case(S, [256] * 80, [300] * 80, 1, 1, 64, 64, 16, seed=5, tail=0)                          # 80 items, room for 160
+
+
+@pytest.mark.parametrize("hq,hk", [(17, 1), (100, 1), (256, 1), (512, 2)])
+def test_chunk_of_many_heads_that_share(S, hq, hk):
+    # up to an item for every token
+    chunk_case(S, [1, 3, 0, 9], [200, 3, 5, 140], hq, hk, 64, 32, 16, seed=hq)
+    chunk_case(S, [2], [3000], hq, hk, 128, 64, 64, seed=hq + 1)
+
+
 def test_chunk_rows_that_see_nothing(S):
     # more new tokens than the sequence has: the first rows see none; no token at all: all of them
     _, q, _, _, out = chunk_case(S, [10, 6, 300], [4, 0, 130], 4, 2, 64, 32, 16, seed=4)
@@ -525,6 +543,26 @@ def test_weight_of_a_single_token_is_one(S, d, group):
         assert (w[:, :, 1:] == 0).all()
 
 
+@pytest.mark.parametrize("n,hq,hk", [(1, 41, 1), (1, 256, 1), (3, 200, 1), (16, 512, 2)])
+def test_weigh_of_many_heads_that_share(S, n, hq, hk):
+    weigh_case(S, [90, 1, 300], n, hq, hk, 128, 64, 16, seed=n + hq)      # up to 4096 columns
+
+
+def test_tables_without_pages(S):
+    # every sequence is empty, and the tables have no width
+    cache = filled_cache(S, 4, 16, 2, 64, 32, gen(2))
+    table, ln = torch.zeros(3, 0, dtype=torch.int32, device=DEV), i32([0, 0, 0])
+    q = randn(5, 4, 64, g=gen(3), dtype=BF)
+    assert (cache.attend_chunk(q, i32([0, 2, 2, 5]), table, ln) == 0).all()
+    lse, w = torch.zeros(3, 1, 4, device=DEV), torch.rand(4, 2, 16, device=DEV)
+    keep = w.clone()
+    assert (cache.attend(q[:3, None].contiguous(), table, ln, lse=lse) == 0).all() and (lse == -math.inf).all()
+    assert torch.equal(cache.weigh(w, q[:3, None].contiguous(), lse, table, ln), keep)
+    lengths, kept = cache.evict(w, table, ln, 8, 2)
+    assert (lengths == 0).all() and (kept == -1).all() and torch.equal(w, keep)
+    cache.query_status()
+
+
 @pytest.mark.parametrize("decay,out", [(1.0, True), (0.5, False), (0.0, True), (0.0, False)])
 def test_weigh_decay_and_output(S, decay, out):
     weigh_case(S, [100, 64, 65], 2, 8, 2, 128, 64, 32, seed=3, decay=decay, out=out)
@@ -657,6 +695,32 @@ def test_evict_budgets(S, keep, recent, copies):
 @pytest.mark.parametrize("scores_of", [rand, few_values])
 def test_evict_on_one_and_on_several_ctas(S, lens, keep, recent, hk, scores_of):
     evict_case(S, lens, keep, recent, hk, 64, 64, 64, scores_of, seed=keep)
+
+
+def test_evict_copies_of_sequences_that_share_pages(S):
+    # a common beginning, kept by each sequence by its own budget; the sources stay as they are
+    g = gen(9)
+    page, hk, keep, recent = 16, 2, 50, 6
+    cache = filled_cache(S, 40, page, hk, 64, 32, g)
+    order = torch.randperm(40, generator=g, device=DEV).to(torch.int32)
+    table = torch.stack([order[:8], torch.cat([order[:5], order[8:11]]), torch.cat([order[:5], order[11:14]])])
+    lens, to = [128, 100, 40], order[16:28].view(3, 4)
+    scores = rand((40, hk, page), g)
+    before = [x.clone() for x in (cache.k_codes, cache.v_params, scores)]
+    lengths, kept = cache.evict(scores, table, i32(lens), keep, recent, out_table=to)
+    cache.query_status()
+    assert lengths.tolist() == [50, 50, 40]
+    for i, n in enumerate(lens):
+        t = torch.arange(n, device=DEV)
+        mine = before[2][table[i, t // page].long(), :, t % page].tolist()
+        for h in range(hk):
+            ref = kept_reference([x[h] for x in mine], n, keep, recent)
+            assert kept[i, h, :len(ref)].tolist() == ref
+            src, dst = torch.tensor(ref, device=DEV), torch.arange(len(ref), device=DEV)
+            for x, y in zip((cache.k_codes, cache.v_params, scores), before):
+                assert torch.equal(x[to[i, dst // page].long(), h, dst % page], y[table[i, src // page].long(), h, src % page])
+    for x, y in zip((cache.k_codes, cache.v_params, scores), before):
+        assert torch.equal(x[order[:16].long()], y[order[:16].long()])
 
 
 def test_evict_of_more_sequences_than_ctas_fit(S):
