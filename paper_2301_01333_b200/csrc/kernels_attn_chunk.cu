@@ -9,8 +9,8 @@
 // K and V so small that fp16 has few bits left for them are widened in units of a power of two, one for each of the two and a CTA's part of an
 // item, which the factor of the scores, and that of O at the end, make up for.  Where a part's first block is of ordinary size the unit is 1
 // and nobody looks any further (22.7 -> 23.0 us for the step below, 176 -> 179 and 317 -> 320 for the other two); else the widening
-// warps look through the parameters of all of its blocks first.  (With units that change along a part, as larger values come: 415 us for the
-// last, for what the softmax has to look at in every block.)
+// warps look through the parameters of all of its blocks first (values of 2^-20 throughout: 28, 206 and 363 us).  Units that change along a part,
+// as larger values come, cost the ordinary case more than that: 415 us for the last, for what the softmax has to look at in every block.
 //
 // A row is a (token, query head) of those that share a key/value head, token by token, so that a block of keys, once widened, serves
 // all of them.  A CTA holds 256 rows in two tiles of 128, and per block of 128 keys at width 128 there are
@@ -74,10 +74,10 @@ struct ChunkLayout {
   static constexpr int STAGES = D == 64 ? 8 : 4;
   // codes and parameters of 128 key rows, K's or V's, as they lie in memory, and how many of these there are
   static constexpr int NG = D / G, PITCH = D / 2, CODES = 128 * PITCH, STAGED = CODES + 128 * NG * 4, AHEAD = D == 64 ? 8 : 3;
-  static constexpr int BARS = 2 * STAGES + 2 * AHEAD + 16;
-  // Q, ring, staged codes, list, notes [CK_FLAGS][4 groups][4 words], one word a block that sums them up, one a part with its units, sums of
-  // the second tile [3][128]
-  static constexpr int LIST = CK_MAX_LIST * 8, NOTES = CK_FLAGS * 16 * 4, ANY = CK_FLAGS * 4, UNITS = CK_FLAGS * 4, SUMS = 3 * 128 * 4;
+  static constexpr int BARS = 2 * STAGES + 2 * AHEAD + 17;
+  // Q, ring, staged codes, list, notes [CK_FLAGS][4 groups][4 words], one word a block that sums them up, one a part with its units, the widening
+  // warps' sizes [2][4], sums of the second tile [3][128]
+  static constexpr int LIST = CK_MAX_LIST * 8, NOTES = CK_FLAGS * 16 * 4, ANY = CK_FLAGS * 4, UNITS = CK_FLAGS * 4 + 2 * 4 * 4, SUMS = 3 * 128 * 4;
   static constexpr size_t SMEM = 1024 + static_cast<size_t>(2 + STAGES) * TILE + AHEAD * STAGED + LIST + NOTES + ANY + UNITS + SUMS + BARS * 8 + 64 * 4;
 };
 
@@ -357,27 +357,53 @@ __device__ __forceinline__ bool is_small(uint32_t size) { return size < static_c
 __device__ __forceinline__ uint32_t unit_of(uint32_t size) {
   return size == 0 || !is_small(size) ? 0u : static_cast<uint32_t>(min(CK_TOP + 127 - static_cast<int>(size >> 23), CK_MOST_UNIT));
 }
-// The unit of the keys, or values, of a part of an item, whose first block's parameters are staged at `staged`: each widening warp finds it for
-// itself, and only calls this (out of line: their loop is at its best when it is short) where all that it has of that block is small.
+// The unit of the keys, or values, of a part of an item, whose first block's parameters are staged at `staged`.  A widening warp that finds all that it
+// has of that block small calls this (out of line: their loop is at its best when it is short).  Where the whole block is, and others follow, all
+// four do, and each looks through a quarter of the rows; *looks: how often they have.  `sizes` [2][4], and a barrier of four arrivals.
+constexpr uint32_t NO_UNIT = 0xffffffffu;    // a wait ran out
 template <int D, int G>
-__device__ __noinline__ uint32_t unit_of_part(const ChunkParams& p, const uint32_t* params, uint32_t staged, int b, int h, int j0, int j1, int len, int lane) {
-  constexpr int NG = D / G;
+__device__ __noinline__ uint32_t unit_of_part(const ChunkParams& p, const uint32_t* params, uint32_t staged, uint32_t* sizes, uint32_t bar, uint32_t* looks, int b, int h,
+                                              int j0, int j1, int len, int warp, int lane) {
+  constexpr int NG = D / G, FLY = 8;
   uint32_t size = 0;
   for (int i = lane; i < 128 * NG; i += 32)
     if (i / NG < len - j0 * 128) size = max(size, size_of(lds32(staged + i * 4)));
   size = __reduce_max_sync(0xffffffffu, size);
   if (!is_small(size)) return 0;
+  if (j1 - j0 == 1) return unit_of(size);
   const int* table = p.table + b * p.table_stride;
   const int end = min(j1 * 128, len);
-#pragma unroll 4
-  for (int t = (j0 + 1) * 128 + lane; t < end; t += 32) {
-    const int page = table[t >> p.page_shift];
-    if (page < 0 || page >= p.num_pages) continue;               // (reported where it is copied)
-    const int64_t at = (((static_cast<int64_t>(page) * p.Hk + h) << p.page_shift) + (t & ((1 << p.page_shift) - 1))) * NG;
+#pragma unroll 1
+  for (int t0 = (j0 + 1) * 128 + warp * 32 + lane; t0 < end; t0 += 128 * FLY) {
+    int64_t at[FLY];
 #pragma unroll
-    for (int g = 0; g < NG; ++g) size = max(size, size_of(params[at + g]));
+    for (int k = 0; k < FLY; ++k) {
+      const int t = t0 + k * 128, page = t < end ? table[t >> p.page_shift] : -1;
+      // (a page that is none is reported where it is copied)
+      at[k] = page < 0 || page >= p.num_pages ? -1 : ((static_cast<int64_t>(page) * p.Hk + h) << p.page_shift) + (t & ((1 << p.page_shift) - 1));
+    }
+    uint32_t x[FLY][NG];
+#pragma unroll
+    for (int k = 0; k < FLY; ++k) {
+#pragma unroll
+      for (int g = 0; g < NG; ++g) x[k][g] = at[k] < 0 ? 0 : params[at[k] * NG + g];
+    }
+#pragma unroll
+    for (int k = 0; k < FLY; ++k) {
+#pragma unroll
+      for (int g = 0; g < NG; ++g) size = max(size, size_of(x[k][g]));
+    }
   }
-  return unit_of(__reduce_max_sync(0xffffffffu, size));
+  size = __reduce_max_sync(0xffffffffu, size);
+  // (The next look's go into the other four places; those of the one after only come once all have arrived for that.)
+  const uint32_t look = (*looks)++;
+  uint32_t* mine = sizes + (look & 1) * 4;
+  if (lane == 0) {
+    mine[warp] = size;
+    mbar_arrive(bar);
+  }
+  if (!__all_sync(0xffffffffu, mma_wait(bar, look & 1))) return NO_UNIT;
+  return unit_of(max(max(mine[0], mine[1]), max(mine[2], mine[3])));
 }
 }  // namespace
 
@@ -421,12 +447,14 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
   uint32_t* s_notes = reinterpret_cast<uint32_t*>(s_list + CK_MAX_LIST);        // [CK_FLAGS][4][4]
   uint32_t* s_any = s_notes + CK_FLAGS * 16;                    // [CK_FLAGS], a byte per widening warp
   uint32_t* s_units = s_any + CK_FLAGS;                         // [CK_FLAGS] parts of items: bytes of K and V
-  float* s_second = reinterpret_cast<float*>(s_units + CK_FLAGS);       // reference, sum and groups that are not finite of tile 1
+  uint32_t* s_sizes = s_units + CK_FLAGS;                       // [2][4]
+  float* s_second = reinterpret_cast<float*>(s_sizes + 8);      // reference, sum and groups that are not finite of tile 1
   uint64_t* bars = reinterpret_cast<uint64_t*>(s_second + 3 * 128);
   const uint32_t b0 = smem_u32(bars);
   const uint32_t bar_q_full = b0, bar_q_empty = b0 + 8, bar_s_full = b0 + 16, bar_p_full = b0 + 48, bar_o_full = b0 + 80;
   const uint32_t bar_second = b0 + 112, bar_joined = b0 + 120, bar_kv_full = b0 + 128, bar_kv_empty = bar_kv_full + 8 * L::STAGES;
   const uint32_t bar_code_full = bar_kv_empty + 8 * L::STAGES, bar_code_empty = bar_code_full + 8 * L::AHEAD;
+  const uint32_t bar_sizes = bar_code_empty + 8 * L::AHEAD;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + L::BARS);
   int* s_sums = reinterpret_cast<int*>(tmem_slot + 4);
 
@@ -436,6 +464,7 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
     mbar_init(bar_q_empty, 2);                                  // both tiles' issuers
     mbar_init(bar_second, 4);
     mbar_init(bar_joined, 4);
+    mbar_init(bar_sizes, 4);                                    // the widening warps
     for (int i = 0; i < 4; ++i) {
       mbar_init(bar_s_full + 8 * i, 1);
       mbar_init(bar_o_full + 8 * i, 1);
@@ -749,7 +778,7 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
     uint32_t to[4];                                             // of the four stores of a chunk, in the first tile
 #pragma unroll
     for (int y = 0; y < 4; ++y) to[y] = smem_u32(sKV) + row0 * 128 + (((chunk0 * 4 + y) ^ (row0 & 7)) << 4);
-    uint32_t ring = 0, used = 0, block = 0, part = 0;            // part: number of the segment
+    uint32_t ring = 0, used = 0, block = 0, part = 0, looks = 0; // part: number of the segment
     Seg s;
     while (!failed && walk.next(s)) {
       const int halves = 2 * (s.j1 - s.j0);
@@ -805,7 +834,9 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
           for (int k = 0; k < CH; ++k) ordinary |= !is_small(size_of(par[k]));
           uint32_t u = 0;
           if (left > (warp & 3) * 32 && !__any_sync(0xffffffffu, ordinary))
-            u = unit_of_part<D, G>(p, i ? p.v_params : p.k_params, smem_u32(s_staging) + stage * L::STAGED + L::CODES, s.b, s.h, s.j0, s.j1, s.len, lane);
+            u = unit_of_part<D, G>(p, i ? p.v_params : p.k_params, smem_u32(s_staging) + stage * L::STAGED + L::CODES, s_sizes, bar_sizes, &looks, s.b, s.h, s.j0, s.j1, s.len,
+                                   warp & 3, lane);
+          if (u == NO_UNIT) { failed = true; break; }
           if (warp == 8 && lane == 0) reinterpret_cast<uint8_t*>(s_units + part % CK_FLAGS)[i] = static_cast<uint8_t>(u);
           if (i) v_by = exp2_of(static_cast<int>(u));
           else k_by = exp2_of(static_cast<int>(u));
