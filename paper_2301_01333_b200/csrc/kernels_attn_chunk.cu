@@ -8,7 +8,8 @@
 // 2^-39 of it below; probabilities, at most 2^4 relative to the reference, are lifted by 2^11.
 // K and V so small that fp16 has few bits left for them are widened in units of a power of two, one for each of the two and a CTA's part of an
 // item, which the factor of the scores, and that of O at the end, make up for.  Where a part's first block is of ordinary size the unit is 1
-// and nobody looks any further (22.7 -> 23.0 us for the step below, 176 -> 179 and 317 -> 320 for the other two); else the widening
+// and nobody looks any further (22.7 -> 23.0 us for four short sequences, 176 -> 179 and 317 -> 320 for the two calls
+// below); else the widening
 // warps look through the parameters of all of its blocks first (values of 2^-20 throughout: 28, 206 and 363 us).  Units that change along a part,
 // as larger values come, cost the ordinary case more than that: 415 us for the last, for what the softmax has to look at in every block.
 //
@@ -33,10 +34,11 @@
 //   * A value that is not finite must not reach rows that do not see it (0 times NaN): such groups are widened as zeros and
 //     noted in a bit mask per block; a row that does see one gets NaN in that group's columns.
 //
-// Measured, calls in a row: the last 1024 tokens of a sequence of 33001, 16 / 4 heads of 128 (0.27 TFLOP): 318 us, 860 TFLOP/s; 32 sequences of
-// up to 4096, chunks of up to 192 tokens, three in four of one, 32 / 8 heads of 128: 176 us.  Tensor pipe 40 %, XU 40 %, ALU 41 %, half an instruction a clock
-// and scheduler of one: what bounds it is the way round of a half block, products, exponentials, probabilities, products, with two halves
-// of two tiles under way (without any arithmetic the handshakes alone take 127 of the 318).  Tried for the first of these calls: 128 scores
+// Measured, calls in a row: the last 1024 tokens of a sequence of 33001, 16 / 4 heads of 128 (0.27 TFLOP): 317 to 334 us from one GPU to another,
+// 860 to 815 TFLOP/s; 32 sequences of up to 4096, chunks of up to 192 tokens, three in four of one, 32 / 8 heads of 128: 179 us.  Tensor pipe 41 %, XU 41 %, ALU
+// 42 %, half an instruction a clock and scheduler of one: no unit is at its limit; the time goes into the way round of a half block, products,
+// exponentials, probabilities, products, with two halves of two tiles under way (without any arithmetic the handshakes alone took 127 of
+// 318).  At widths 96 and 128 reading and scaling Q spills 360 to 420 bytes a thread, at an item's beginning.  Tried for the first of these calls, then 318: 128 scores
 // in registers, unrolled, with registers moved between warps 368 (its code no longer fits the instruction cache); two groups of
 // softmax warps for each tile 359; eight widening warps 347; tiles taking turns 370; staging by loads through the cores 342.
 #include <cuda_fp16.h>

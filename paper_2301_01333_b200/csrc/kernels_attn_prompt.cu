@@ -24,8 +24,9 @@
 // two threads per row 1064 (its instructions were the bottleneck: products alone took 940); an issuing thread per tile with lean
 // descriptors, taking turns (both tiles' products at once complete both scores together, and the tensor core idles while
 // both softmaxes run: 1242) 957; probabilities in two parts 917; one thread per row, without the votes and sums two threads
-// share, 865 = 1270 TFLOP/s, the tensor pipe busy 71 % of the time (products alone: 714).  All these are replays with pauses in between;
-// back to back, under the power cap, it is 1000 us = 1100 TFLOP/s.  What is left is the way round: scores
+// share, 865 = 1270 TFLOP/s, the tensor pipe busy 71 % of the time (products alone: 714).  All these are replays with pauses in between, and
+// without the wait between a product that reads probabilities and the scores over them.  With it 920 to 965 us called in a row = 1190 to 1140 TFLOP/s, as
+// the power cap has it, and 990 replayed on its own (tensor memory has no columns for P beside the scores at this width; at 64, where it has, 750).  What is left is the way round: scores
 // complete, softmax, probabilities handed over, with only two tiles to alternate between.  No gain: CTA pairs (M = 256, half
 // of K and V in each CTA); part of the exponentials on the FMA pipe (865 without any exponentials as well); probabilities in four
 // parts (945); two score buffers of 64 keys per tile, which takes the hand-over out of the way but makes S slower (N = 64: 1001).

@@ -10,10 +10,11 @@
 //            lowest positions stay, by an ordered count.  Writes, for every new position, the position its token has now.
 //   move     rows of codes, parameters and scores, 16 bytes a thread, on the whole GPU.
 //
-// Bound: the scores read once and the kept rows read and written once; what it takes is a chain of latencies (seven cluster
-// barriers of about a microsecond) and a launch.  Scores are read once, and their keys kept in shared memory while they fit.
-// Measured: from 131071 tokens x 8 heads of 128 to 8192: select 37 us, move 10 (a cold cache); 48 sequences of up to 4099 x 8 heads of 64
-// to 2048: about 28 and 23; 5 sequences of up to 300 x 8 heads of 128 to 256: 12 and 6.  Reading the counts of all CTAs at once, and other
+// Bound: the scores read once and the kept rows read and written once; what it takes is a chain of latencies (six
+// barriers, of the cluster where there is one, and seven passes over the keys) and a launch.  Scores are read once, and their keys kept in shared memory while they fit.
+// Measured, select and move as single launches with a cold cache: from 131071 tokens x 8 heads of 128 to 8192: 38 us and 12; 48 sequences of up to 4099 x 8 heads
+// of 64 to 2048: 30 and 25; 5 sequences of up to 300 x 8 heads of 128 to 256: 14 and 8.  Called in a row 40, 47 and 14 for both together,
+// and in place, scores of given-up positions zeroed and few rows moved, 45, 47 and 16 one call at a time.  Reading the counts of all CTAs at once, and other
 // unrollings of the passes, changed nothing.
 #include "ptx.cuh"
 #include "serving.cuh"

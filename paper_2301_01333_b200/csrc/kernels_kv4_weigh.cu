@@ -14,9 +14,10 @@
 //     take further passes over the stretch, which add to the first one's weights.
 //   * After the columns are summed, lane (gr, tg) has the sum of one token: weights are read and written 32 to a request.
 //
-// Measured, calls in a row: 64 sequences of up to 8192 tokens, 32 / 8 heads of 128, one query each: 90 us, 1.9 TB/s, bound by instructions
-// (about 570 a tile, 0.41 a clock and scheduler); 16 queries of one of 65000, 16 / 4 heads: 35 us; 5 sequences of up to 300:
-// 7.2 us, a launch and a chain of latencies.  Keys through a ring of asynchronous copies in shared memory: 88 us for the first, but 8.8 for the last.
+// Measured, calls in a row: 64 sequences of up to 8192 tokens, 32 / 8 heads of 128, one query each: 90 us, 1.9 TB/s.  Neither the memory nor the
+// issue of instructions (about 570 a tile, 0.38 a clock and scheduler) is at its limit: with 12 warps an SM, 18 % of what it holds, loads
+// and results are waited for.  16 queries of one of 65000, 16 / 4 heads: 35 us, four or five tiles a warp behind 64 columns that every
+// warp prepares for itself; 5 sequences of up to 300: 7.2 us, a launch and a chain of latencies.  Keys through a ring of asynchronous copies in shared memory: 88 us for the first, but 8.8 for the last.
 #include <cuda_fp16.h>
 
 #include "ptx.cuh"
