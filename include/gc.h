@@ -441,6 +441,8 @@ gc_status_t gc_kv4_weigh(void* cuda_stream, const gc_kv4_cache_t* cache, const g
  * the others the keep - recent with the largest scores (equal ones: the older; NaN counts as largest).  scores: fp32, 16-byte aligned, paged like the
  * cache.  The kept tokens take positions 0 .. keep - 1: those from there stay where they are, and the holes
  * between them are filled, in order, with the kept ones from behind, in order.  (Attention does not mind the order of the tokens a query sees.)
+ * Age goes by position: newer ones stand behind.  After an eviction that holds for the tokens appended since, so that `recent` should not exceed
+ * their number when a sequence is cut again; among those kept before, what lies last need not be what came last.
  * Shorter sequences keep all.  With m = min(n, keep):
  *   out_lengths[b] = m;   kept[b, hk, i] = the position, before, of the token at i, or -1 for i >= m   (int32 [batch, kv_heads, keep])
  * out_table null: in place; pages behind m are free then, and the scores of positions m .. n - 1 zero.  Else the kept tokens

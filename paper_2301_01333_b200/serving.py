@@ -225,7 +225,8 @@ class KV4Cache:
         lengths are free then), or, with out_table (int32 [batch, width], pages not in block_table), as copies in other pages, with block_table's
         left as they were.  Scores move along; those of positions given up in place, and of the rest of a copy's last page, are zero.  Returns the
         new lengths (int32 [batch]) and kept, int32 [batch, kv_heads, keep]: where the token at each position was before, -1 behind a
-        sequence.  A page may be named by one sequence of a call only, except that block_table's may be shared where out_table is given."""
+        sequence.  Age goes by position, which after an eviction holds for the tokens appended since: let a sequence grow by at least `recent` before
+        it is cut again.  A page may be named by one sequence of a call only, except that block_table's may be shared where out_table is given."""
         return _serving.kv4_evict(self._at, scores, block_table, lengths, keep, recent, max_length, out_table, self._tensors)
 
     def query_status(self) -> None:

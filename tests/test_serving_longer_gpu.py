@@ -1005,3 +1005,28 @@ def test_outputs_that_were_given_count_as_written(S):
     version(lambda: cache.attend(q1, table, ln, lse=lse), lse)
     version(lambda: cache.weigh(w, q1, lse, table, ln), w)
     version(lambda: cache.evict(w, table, ln, 8, 2), w, cache.k_codes, cache.v_params)
+
+
+def test_evicting_again_after_growing_by_the_recent_ones_keeps_the_newest(S):
+    # the documented use: a sequence is cut once it has grown by `recent`, again and again; ages by a list that follows `kept`
+    g = gen(81)
+    page, hk, keep, recent = 16, 2, 48, 16
+    cache = filled_cache(S, 4, page, hk, 64, 32, g)
+    table = torch.randperm(4, generator=g, device=DEV).to(torch.int32)[None]
+    scores = torch.zeros(4, hk, page, device=DEV)
+    ages, born = [list(range(48)) for _ in range(hk)], 48
+    for _ in range(6):
+        t = torch.arange(48, 64, device=DEV)
+        for h in range(hk):
+            ages[h] += list(range(born, born + recent))
+        born += recent
+        at = table[0, t // page].long()
+        scores[at, :, t % page] = 0
+        t = torch.arange(64, device=DEV)
+        scores[table[0, t // page].long(), :, t % page] += torch.rand(64, hk, generator=g, device=DEV)
+        lengths, kept = cache.evict(scores, table, i32([64]), keep, recent)
+        assert lengths.item() == keep
+        for h in range(hk):
+            ages[h] = [ages[h][x] for x in kept[0, h].tolist()]
+            assert set(range(born - recent, born)) <= set(ages[h])
+    cache.query_status()
