@@ -22,7 +22,7 @@
 //   warps 8-11       widen: codes and parameters out of staging, as fp16 into 128-byte-swizzled tiles of a ring.  The eight elements of a word
 //                    come apart as (0,4), (1,5), (2,6), (3,7) and stay in that order: Q's elements are put in the same one, and
 //                    the columns of O are put back in registers at the end.
-//   warps 12, 13     MMA issuers of tile 0 / 1.  Products of unlike shapes keep no order among themselves: scores are
+//   warps 12, 13     MMA issuers of tile 0 / 1.  Only products into one accumulator, of one shape, are promised to keep their order: scores are
 //                    multiplied only once the product that reads the probabilities they overwrite is complete.
 //   warp 14          notes down which pieces of split items this CTA leaves
 //   warp 15          bulk copies of codes and parameters, as they lie in the pages, a block and a half ahead (at width 64 four blocks); six
@@ -946,8 +946,8 @@ __global__ void __launch_bounds__(CK_THREADS, 1) attn_chunk_kernel(const __grid_
                 if (late) continue;
               }
               if ((h == 0 || late) && !kv_ready(kpos)) { failed = true; break; }
-              // These scores overwrite the probabilities that the product just issued reads, and products of unlike shapes into unlike
-              // accumulators keep no order among themselves: it has to be complete.  (The softmax works on the other half meanwhile.)
+              // These scores overwrite the probabilities that the product just issued reads, and products into unlike accumulators are
+              // promised no order: it has to be complete.  (The softmax works on the other half meanwhile.)
               if (x >= 0 && !((h == 0 || late ? mma_wait(o_full, (pn - h) & 1) : true) && (h == 1 ? mma_wait(o_full + 8, (pn - 1) & 1) : true))) { failed = true; break; }
               tc_fence_after();
               if (late) scores(kpos, 0);

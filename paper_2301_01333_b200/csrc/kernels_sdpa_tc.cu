@@ -298,7 +298,7 @@ sdpa_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
           tc_fence_after();
           // Same buffer: the next unit's scores block by block as the columns free up - and BEFORE this unit's
           // P.V for the block: the softmax warps will wait for those scores, nobody waits for this O yet, and
-          // the tensor pipe runs the MMAs in issue order.
+          // what is issued first mostly runs first (a matter of time only: no product overwrites what one before it reads).
           if (has_next && !next_issued && slots == 2) {
             if (!next_ready) {
               if (!wait_inputs(n + 1)) { failed = true; break; }

@@ -309,7 +309,7 @@ sdpa_wide_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         for (int b = 0; b < NB; ++b) {
           if (!mbar_wait(bar_p_full + 8 * b, upar)) { failed = true; break; }
           // the next unit's scores for this block first: the softmax warps will wait for them, nobody waits for
-          // this O yet, and the tensor pipe runs the MMAs in issue order
+          // this O yet, and what is issued first mostly runs first (a matter of time only: P is in shared memory, behind barriers)
           if (ahead && b >= b_first && !mma1(n + 1, b)) { failed = true; break; }
           const uint32_t st = ring_st, use = ring_use;
           ring_next();
