@@ -1030,3 +1030,27 @@ def test_evicting_again_after_growing_by_the_recent_ones_keeps_the_newest(S):
             ages[h] = [ages[h][x] for x in kept[0, h].tolist()]
             assert set(range(born - recent, born)) <= set(ages[h])
     cache.query_status()
+
+
+@pytest.mark.parametrize("new,lens,hq,hk,d,group,page", [([48], [60000], 8, 1, 128, 64, 64), ([1] * 12 + [150, 96], [500 * i for i in range(1, 13)] + [3000, 2000], 16, 4, 128, 32, 64),
+                                                         ([300, 40], [9000, 9000], 4, 2, 64, 32, 16), ([64], [20000], 8, 1, 96, 32, 256)])
+def test_chunk_calls_over_small_values_in_close_succession(S, new, lens, hq, hk, d, group, page):
+    # parts whose units have to be looked for, among parts of ordinary size: every call gives what the first gave
+    cache, q, cu, table, _ = chunk_case(S, new, lens, hq, hk, d, group, page, seed=7, tail=0)
+    for i, m in enumerate(lens):
+        t = torch.arange(m, device=DEV)
+        at, small = table[i, t // page].long(), (t // 700 % 3 != i % 3)[:, None, None, None]
+        for p, power in ((cache.k_params, -15), (cache.v_params, -22)):
+            p[at, :, t % page] = torch.where(small, p[at, :, t % page] * 2.0 ** power, p[at, :, t % page])
+    ln = i32(lens)
+    want = cache.attend_chunk(q, cu, table, ln)
+    ref, tol = lifted_reference(cache, q, new, table, lens, d ** -0.5)
+    within(want, ref, tol)
+    outs = [torch.zeros_like(want) for _ in range(60)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for o in outs:
+            cache.attend_chunk(q, cu, table, ln, out=o)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+    cache.query_status()
